@@ -101,6 +101,7 @@ typedef enum { DAMP_IN_BF16 = 0, DAMP_IN_FP32 = 1 } damp_in_dtype;
 #define DAMP_DEV_WAIT_TIMEOUT 1u
 #define DAMP_DEV_BAD_SLOT 2u
 #define DAMP_DEV_BAD_HEAD 4u
+#define DAMP_DEV_BAD_TOKEN 8u
 
 /*
  * Shape of one linear-attention layer's state (Sec. 3.1; Sec. 5.1 "Key-channel budget").
@@ -312,6 +313,100 @@ DAMP_API damp_status damp_kda_prefill_chunk(const damp_layout *layout, void *sta
                                             const int32_t *lengths, const uint8_t *perm, const void *q,
                                             const void *k, const void *v, const float *g, const float *beta,
                                             float *o, int32_t in_dtype, void *stream);
+
+/*
+ * Linear attention with a decay per head and no delta rule, on an FP32 state pool: the
+ * third kind of linear-attention layer beside GDN and KDA,
+ *     S_t = e^{g_t} S_{t-1} + k_t v_t^T,   o_t = S_t^T q_t        (FP32)
+ *
+ * damp_lin_decode_step: one token per batch row.
+ *   layout     num_heads, num_qk_heads, d_k, d_v as in damp_gdn_decode_step; k_hi and
+ *              lo_format are ignored; no head map (DAMP_ERR_SHAPE)
+ *   state      float [num_slots][H][d_k][d_v], 16-B aligned, updated in place
+ *   q, k       [B][H_qk][d_k] of in_dtype, 16-B aligned
+ *   v          [B][H][d_v] of in_dtype, 16-B aligned
+ *   g          float [B][H] log-decays, or [H] if g_per_head is not 0; 4-B aligned.
+ *              e^g is 0 for g < -200 (-inf resets the state).
+ *   o          float [B][H][d_v], 4-B aligned; must not overlap the pool or an input
+ * damp_lin_prefill_chunk: a chunk of chunk_len = T tokens per row.
+ *   q, k, v    [B][T][...]; g float [B][T][H], or [H] if g_per_head is not 0
+ *   lengths    int32 [batch] or NULL: row b runs its first min(max(lengths[b], 0), T)
+ *              tokens; a row of length 0 keeps its state.  What q, k, v and g hold past a
+ *              row's length is not used.
+ *   o          float [B][T][H][d_v]; zero past a row's length
+ * slot_idx, num_slots, batch, in_dtype and the status bits as in damp_gdn_decode_step
+ * (the outputs of a row with a bad slot are left as they are).
+ */
+DAMP_API damp_status damp_lin_decode_step(const damp_layout *layout, float *state, int64_t num_slots,
+                                          const int32_t *slot_idx, int32_t batch, const void *q, const void *k,
+                                          const void *v, const float *g, int32_t g_per_head, float *o,
+                                          int32_t in_dtype, void *stream);
+DAMP_API damp_status damp_lin_prefill_chunk(const damp_layout *layout, float *state, int64_t num_slots,
+                                            const int32_t *slot_idx, int32_t batch, int32_t chunk_len,
+                                            const int32_t *lengths, const void *q, const void *k, const void *v,
+                                            const float *g, int32_t g_per_head, float *o, int32_t in_dtype,
+                                            void *stream);
+
+/*
+ * Whole slots of the pools of a model's layers, packed or FP32, in one call.
+ *   pools       host array of n_pools (0 .. 1024) device pointers, each 16-B aligned and
+ *               num_slots slots of slot_bytes[i] bytes (a multiple of 16, 16 at least);
+ *               pools must not overlap each other or the slot lists (DAMP_ERR_ALIAS)
+ *   num_slots   slots of every pool (up to 2^31 - 1; 2^18 for damp_compact_slots)
+ *   n           entries of the slot lists (device int32, 4-B aligned), 0 .. 12288 (copy and
+ *               compact); a negative entry is skipped, one >= num_slots too, and sets
+ *               DAMP_DEV_BAD_SLOT
+ * damp_copy_slots: slot dst[i] receives what slot src[i] held before the call.  The lists
+ *   may overlap (a reorder) and a source may be named any number of times (a fork); the
+ *   destinations must be distinct.  An entry is skipped if either slot is.
+ * damp_zero_slots: slots idx[i] become all zero, the zero state of the packed and the FP32
+ *   pools (the start of a sequence).
+ * damp_compact_slots: moves the live slots slot_idx[0 .. n-1] (negative: no request) into
+ *   the lowest slot numbers.  With m distinct live slots, those below m stay; the others
+ *   move, in ascending order, into the free slots below m in ascending order.
+ *   slot_idx_out  int32 [n]: the new slot of each entry, -1 for skipped ones; must not
+ *                 overlap slot_idx.  Slots left behind keep their bytes.  n_pools may be 0
+ *                 (only the new numbers).
+ */
+DAMP_API damp_status damp_copy_slots(void *const *pools, const int64_t *slot_bytes, int32_t n_pools, int64_t num_slots,
+                                     const int32_t *src, const int32_t *dst, int32_t n, void *stream);
+DAMP_API damp_status damp_zero_slots(void *const *pools, const int64_t *slot_bytes, int32_t n_pools, int64_t num_slots,
+                                     const int32_t *idx, int32_t n, void *stream);
+DAMP_API damp_status damp_compact_slots(void *const *pools, const int64_t *slot_bytes, int32_t n_pools,
+                                        int64_t num_slots, const int32_t *slot_idx, int32_t n, int32_t *slot_idx_out,
+                                        void *stream);
+
+/*
+ * Verification of drafted tokens against the target's probabilities, from given random
+ * numbers (speculative sampling), for `batch` requests with up to n_draft = D drafts each.
+ * With p_i = softmax(target_i / T) and q_i = softmax(draft_i / T), draft x_i is accepted iff
+ * u_i q_i(x_i) < p_i(x_i), up to the first rejection at a; then one token is drawn from
+ * r = max(p_a - q_a, 0) (p_a if r is zero everywhere), or from r = p_L if all L drafts are
+ * accepted, as the t with the largest r_t / noise_t (ties: the lowest).  With uniform u and
+ * exponential noise, the tokens are distributed as samples of the target.  T = 0 is greedy:
+ * x_i is accepted iff it is the lowest index of the target's maximum, which is also the
+ * token drawn.
+ *   target_logits  [B][D + 1] rows of row_stride elements, of which the first vocab are
+ *                  tokens; damp_in_dtype logits_dtype; 16-B aligned
+ *   draft_logits   [B][D] rows likewise, or NULL: q_i is 1 at x_i
+ *                  (NaN and -inf exclude a token, +inf is the largest finite value; a row
+ *                  that excludes every token accepts nothing and draws nothing)
+ *   draft_tokens   int32 [B][D]; one outside 0 .. vocab-1 is rejected and sets
+ *                  DAMP_DEV_BAD_TOKEN
+ *   draft_len      int32 [B] or NULL: drafts of each request, clamped to 0 .. D (NULL: D)
+ *   u              float [B][D] in [0, 1);  noise  float [B][vocab], positive, 16-B aligned
+ *   temperature    float [B] or NULL (1); a value that is not positive means 0
+ *   tokens_out     int32 [B][D + 1]: the accepted drafts, the token drawn, then -1
+ *   count_out      int32 [B]: tokens of the row (accepted + 1, or accepted if none was drawn)
+ * n_draft may be 0 (one token is drawn from p_0; draft_tokens and u may be NULL).
+ * count_out serves as the `lengths` of a chunk that replays the drafts from a saved state.
+ * Pointers are 4-B aligned where not said otherwise; outputs must not overlap an input.
+ */
+DAMP_API damp_status damp_verify_drafts(const void *target_logits, const void *draft_logits, int32_t logits_dtype,
+                                        int64_t row_stride, int32_t vocab, const int32_t *draft_tokens,
+                                        const int32_t *draft_len, int32_t n_draft, const float *u, const float *noise,
+                                        const float *temperature, int32_t batch, int32_t *tokens_out,
+                                        int32_t *count_out, void *stream);
 
 /*
  * Write FP32 states into the packed cache: the hand-off from an FP32 prefix

@@ -11,6 +11,11 @@ DampLibraryError.
     quantize_state(layout, S_fp32, perm, state)            # prefill hand-off
     o = kda_decode_step(layout, state, perm, q, k, v, g, beta)
 
+Linear attention with a decay per head and no delta rule runs on an FP32 pool
+(new_fp32_state) with lin_prefill_chunk and lin_decode_step.  copy_slots, zero_slots and
+compact_slots move whole slots of all layers' pools, packed or FP32; verify_drafts accepts
+drafted tokens, and its counts are the lengths with which a chunk replays them.
+
 A layer whose heads keep different numbers of FP16 key channels (the decay-tiered
 allocation of App. E) is a list of head groups (`head_groups`), one uniform layout,
 pool and permutation table per K_hi, each with a head map into the layer's heads.
@@ -30,7 +35,8 @@ __all__ = [
     "fp32_gdn_decode_step", "fp32_kda_decode_step", "quantize_state", "dequantize_state",
     "pack_tiers", "unpack_tiers", "device_status", "version", "DEV_WAIT_TIMEOUT", "DEV_BAD_SLOT", "DEV_BAD_HEAD",
     "head_groups", "test_kda_wait_timeout", "gdn_decode_step_groups", "kda_decode_step_groups",
-    "calib_accumulate",
+    "calib_accumulate", "lin_decode_step", "lin_prefill_chunk", "copy_slots", "zero_slots", "compact_slots",
+    "verify_drafts", "DEV_BAD_TOKEN",
 ]
 
 LO_U8_AFFINE_G32_H32 = 0
@@ -44,6 +50,7 @@ IN_FP32 = 1
 DEV_WAIT_TIMEOUT = 1
 DEV_BAD_SLOT = 2
 DEV_BAD_HEAD = 4
+DEV_BAD_TOKEN = 8
 
 
 class DampError(RuntimeError):
@@ -539,6 +546,178 @@ def unpack_tiers(layout, state, batch=None, slot_idx=None, num_slots=None, strea
                                    _ptr(codes if codes.numel() else None), _ptr(meta if meta.numel() else None),
                                    _stream(stream)), "damp_unpack_tiers")
     return hi, codes, meta
+
+
+def _new(shape, dtype, like, stream):
+    """An uninitialized output, allocated for the stream that the call runs on."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=like.device)
+
+
+def _given(name, t, shape, dtype):
+    """Raise ValueError unless t is a contiguous CUDA tensor of the shape and type."""
+    if t is None:
+        raise ValueError(f"{name} is required")
+    if t.shape != shape or t.dtype != dtype:
+        _want(name, t, shape, dtype=dtype)
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous CUDA tensor")
+    return t.data_ptr()
+
+
+def _lin(layout, state, q, k, v, g, o, lengths, slot_idx, num_slots, stream, lead_dims):
+    import torch
+    if v is None or v.dim() != lead_dims + 2:
+        raise ValueError(f"v must have {lead_dims + 2} dimensions")
+    if layout.head_map is not None:
+        raise ValueError("the FP32 state holds every head: use a layout without a head map")
+    lead = tuple(v.shape[:lead_dims])
+    B, H = lead[0], layout.num_heads
+    num_slots = _want_pool(layout, state, num_slots, fp32=True)
+    dtype = v.dtype
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError("q, k, v must all be bfloat16 or all float32")
+    if q is not None and k is not None and (q.dtype != dtype or k.dtype != dtype):
+        raise TypeError("q, k, v must all be bfloat16 or all float32")
+    if slot_idx is None and B > num_slots:
+        raise ValueError(f"batch {B} exceeds num_slots {num_slots} without slot_idx")
+    qk_shape = lead + (layout.num_qk_heads, layout.d_k)
+    per_head = g is not None and g.dim() == 1
+    o_shape = lead + (H, layout.d_v)
+    pool = _given("state", state, state.shape, torch.float32)
+    args = [_given("q", q, qk_shape, dtype), _given("k", k, qk_shape, dtype), _given("v", v, o_shape, dtype),
+            _given("g", g, (H,) if per_head else lead + (H,), torch.float32), 1 if per_head else 0]
+    if o is None:
+        o = _new(o_shape, torch.float32, v, stream)
+    args += [_given("o", o, o_shape, torch.float32), IN_BF16 if dtype == torch.bfloat16 else IN_FP32, _stream(stream)]
+    idx = None if slot_idx is None else _given("slot_idx", slot_idx, (B,), torch.int32)
+    c = layout.c()
+    head = [ctypes.byref(c), pool, num_slots, idx, B]
+    if lead_dims == 1:
+        _check(lib().damp_lin_decode_step(*head, *args), "damp_lin_decode_step")
+    else:
+        n = None if lengths is None else _given("lengths", lengths, (B,), torch.int32)
+        _check(lib().damp_lin_prefill_chunk(*head, lead[1], n, *args), "damp_lin_prefill_chunk")
+    return o
+
+
+def lin_decode_step(layout, state, q, k, v, g, o=None, slot_idx=None, num_slots=None, stream=None):
+    """One token of linear attention with a decay per head on an FP32 state [slots, H, d_k, d_v]
+    (in place): S = e^g S + k v^T, o = S^T q.  q, k [B, H_qk, d_k], v [B, H, d_v], g [B, H] or
+    [H]; returns o [B, H, d_v] float32."""
+    return _lin(layout, state, q, k, v, g, o, None, slot_idx, num_slots, stream, 1)
+
+
+def lin_prefill_chunk(layout, state, q, k, v, g, o=None, lengths=None, slot_idx=None, num_slots=None, stream=None):
+    """A chunk of T tokens of linear attention with a decay per head on an FP32 state (in place):
+    q, k [B, T, H_qk, d_k], v [B, T, H, d_v], g [B, T, H] or [H]; row b runs its first lengths[b]
+    tokens.  Returns o [B, T, H, d_v] float32, zero past a row's length."""
+    return _lin(layout, state, q, k, v, g, o, lengths, slot_idx, num_slots, stream, 2)
+
+
+def _pools(pools):
+    """(pointers, bytes per slot, number of pools, slots) of one pool or a list of pools: CUDA
+    tensors [slots, ...], contiguous, of any type, all with the same number of slots."""
+    import torch
+    if isinstance(pools, torch.Tensor):
+        pools = (pools,)
+    n = len(pools)
+    if n == 0:
+        raise ValueError("at least one pool is required")
+    slots = pools[0].shape[0] if pools[0].dim() else 0
+    ptrs, sizes = (ctypes.c_void_p * n)(), (ctypes.c_int64 * n)()
+    for i, t in enumerate(pools):
+        if t.dim() < 2 or not t.is_cuda or not t.is_contiguous():
+            raise ValueError(f"pool {i} must be a contiguous CUDA tensor [slots, ...]")
+        if t.shape[0] != slots or slots == 0:
+            raise ValueError(f"pool {i} has {t.shape[0]} slots, expected {slots} (one at least)")
+        ptrs[i] = t.data_ptr()
+        sizes[i] = t.nbytes // slots
+    return ptrs, sizes, n, slots
+
+
+def _slot_list(name, t):
+    import torch
+    if t is None or t.dim() != 1:
+        raise ValueError(f"{name} must be a one-dimensional int32 CUDA tensor")
+    return _given(name, t, t.shape, torch.int32)
+
+
+def copy_slots(pools, src, dst, stream=None):
+    """Slot dst[i] of every pool receives what slot src[i] held before the call (int32 [n], dst
+    distinct; the lists may overlap).  A source named n times is forked n ways.  An entry with a
+    negative slot is skipped.  pools: one pool or the list of a model's layers, packed or FP32."""
+    if src is not None and dst is not None and src.shape != dst.shape:
+        raise ValueError(f"src has shape {tuple(src.shape)}, dst {tuple(dst.shape)}")
+    ptrs, sizes, n, slots = _pools(pools)
+    _check(lib().damp_copy_slots(ptrs, sizes, n, slots, _slot_list("src", src), _slot_list("dst", dst), src.shape[0],
+                                 _stream(stream)), "damp_copy_slots")
+
+
+def zero_slots(pools, idx, stream=None):
+    """Free slots idx (int32 [n]) of every pool: an all-zero slot is the zero state, the start of
+    a sequence.  Negative entries are skipped."""
+    ptrs, sizes, n, slots = _pools(pools)
+    _check(lib().damp_zero_slots(ptrs, sizes, n, slots, _slot_list("idx", idx), idx.shape[0], _stream(stream)),
+           "damp_zero_slots")
+
+
+def compact_slots(pools, slot_idx, out=None, stream=None):
+    """Move the live slots slot_idx (int32 [B], negative for a finished request) of every pool
+    into the lowest slot numbers; returns the new slot_idx.  With n distinct live slots, those
+    below n stay, the others move in ascending order into the free slots below n in ascending
+    order.  The slots left behind keep their bytes (zero_slots frees them)."""
+    import torch
+    idx = _slot_list("slot_idx", slot_idx)
+    ptrs, sizes, n, slots = _pools(pools)
+    if out is None:
+        out = _new(slot_idx.shape, torch.int32, slot_idx, stream)
+    _check(lib().damp_compact_slots(ptrs, sizes, n, slots, idx, slot_idx.shape[0],
+                                    _given("out", out, slot_idx.shape, torch.int32), _stream(stream)),
+           "damp_compact_slots")
+    return out
+
+
+def verify_drafts(target_logits, draft_tokens, u, noise, draft_logits=None, temperature=None, draft_len=None,
+                  vocab=None, tokens=None, count=None, stream=None):
+    """Speculative sampling: accept a prefix of the drafted tokens and draw the next one.
+
+    target_logits [B, D + 1, ld], draft_logits [B, D, ld] (None: each draft is certain) bfloat16 or
+    float32, of which the first vocab (default ld) entries of a row are tokens; draft_tokens int32
+    [B, D], row b of which the first draft_len[b] (default D) count; u float32 [B, D] uniform in
+    [0, 1); noise float32 [B, vocab] exponential; temperature float32 [B] (default 1, 0: greedy).
+    Returns tokens int32 [B, D + 1] (the accepted drafts, the drawn token, then -1) and count int32
+    [B], the number of tokens of each row: the lengths to replay a chunk with."""
+    import torch
+    if target_logits is None or target_logits.dim() != 3 or target_logits.shape[1] < 1:
+        raise ValueError("target_logits must be a [B, D + 1, vocab] tensor")
+    B, D1, ld = target_logits.shape
+    D = D1 - 1
+    dtype = target_logits.dtype
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError("logits must be bfloat16 or float32")
+    V = ld if vocab is None else int(vocab)
+    if not 1 <= V <= ld:
+        raise ValueError(f"vocab {V} is outside 1 .. {ld}")
+    i32, f32 = torch.int32, torch.float32
+    opt = lambda name, t, shape, dt: None if t is None else _given(name, t, shape, dt)
+    target = _given("target_logits", target_logits, target_logits.shape, dtype)
+    draft = opt("draft_logits", draft_logits, (B, D, ld), dtype)
+    drafted = _given("draft_tokens", draft_tokens, (B, D), i32) if D else None
+    uniform = _given("u", u, (B, D), f32) if D else None
+    args = [target, draft if D else None, IN_BF16 if dtype == torch.bfloat16 else IN_FP32, ld, V, drafted,
+            opt("draft_len", draft_len, (B,), i32), D, uniform, _given("noise", noise, (B, V), f32),
+            opt("temperature", temperature, (B,), f32), B]
+    if tokens is None:
+        tokens = _new((B, D1), i32, target_logits, stream)
+    if count is None:
+        count = _new((B,), i32, target_logits, stream)
+    _check(lib().damp_verify_drafts(*args, _given("tokens", tokens, (B, D1), i32), _given("count", count, (B,), i32),
+                                    _stream(stream)), "damp_verify_drafts")
+    return tokens, count
 
 
 def device_status() -> int:

@@ -51,6 +51,12 @@ SIGNATURES = {
     "damp_calib_log_decay": (_status, [_L, _P, _i32, _i32, _P, _P]),
     "damp_calib_select": (_status, [_L, _P, _i64, _P, _i64, ctypes.c_float, _P, _P, _P]),
     "damp_calib_accumulate": (_status, [_L, _P, _i32, _i32, _P, _P, _P, _P, _P, _i32, _i32, _i32, _P, _P, _P]),
+    "damp_lin_decode_step": (_status, [_L, _P, _i64, _P, _i32, _P, _P, _P, _P, _i32, _P, _i32, _P]),
+    "damp_lin_prefill_chunk": (_status, [_L, _P, _i64, _P, _i32, _i32, _P, _P, _P, _P, _P, _i32, _P, _i32, _P]),
+    "damp_copy_slots": (_status, [_P, _P, _i32, _i64, _P, _P, _i32, _P]),
+    "damp_zero_slots": (_status, [_P, _P, _i32, _i64, _P, _i32, _P]),
+    "damp_compact_slots": (_status, [_P, _P, _i32, _i64, _P, _i32, _P, _P]),
+    "damp_verify_drafts": (_status, [_P, _P, _i32, _i64, _i32, _P, _P, _i32, _P, _P, _P, _i32, _P, _P, _P]),
     "damp_quantize_state": (_status, [_L, _P, _P, _P, _i64, _P, _i32, _P]),
     "damp_dequantize_state": (_status, [_L, _P, _i64, _P, _i32, _P, _P, _P]),
     "damp_pack_tiers": (_status, [_L, _P, _P, _P, _P, _i64, _P, _i32, _P]),

@@ -262,6 +262,101 @@ damp_status prefill(const damp_layout *L, void *state, int64_t num_slots, const 
     return (kda ? launch_prefill_kda(a, s) : launch_prefill_gdn(a, s)) == cudaSuccess ? DAMP_OK : DAMP_ERR_CUDA;
 }
 
+// Linear attention with a decay per head on an FP32 pool: T tokens per row (the step: 1).
+damp_status lin(const damp_layout *L, float *state, int64_t num_slots, const int32_t *slot_idx, int32_t batch, int32_t T,
+                const int32_t *lengths, const void *q, const void *k, const void *v, const float *g, int32_t g_per_head,
+                float *o, int32_t in_dtype, void *stream, bool step) {
+    if (!L) return DAMP_ERR_NULL;
+    damp_layout l2 = *L;  // the FP32 state ignores k_hi and lo_format and holds every model head
+    l2.k_hi = 0;
+    l2.lo_format = 0;
+    damp_status st = check_layout(&l2);
+    if (st != DAMP_OK) return st;
+    if (L->head_map) return DAMP_ERR_SHAPE;
+    if (in_dtype != DAMP_IN_BF16 && in_dtype != DAMP_IN_FP32) return DAMP_ERR_FORMAT;
+    if (batch < 0 || T < 0) return DAMP_ERR_SHAPE;
+    if (batch == 0 || T == 0) return DAMP_OK;
+    const int64_t B = batch, N = B * T, H = L->num_heads, Hq = L->num_qk_heads, dk = L->d_k, dv = L->d_v;
+    if (B * H * (dv / 32) > INT32_MAX) return DAMP_ERR_SHAPE;  // CTAs of one launch
+    Range pool;
+    if ((st = check_pool(state, num_slots, slot_idx, batch, H * dk * dv * 4, &pool)) != DAMP_OK) return st;
+    if (!q || !k || !v || !g || !o) return DAMP_ERR_NULL;
+    if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(g, 4) || !aligned(o, 4) ||
+        (lengths && !aligned(lengths, 4)))
+        return DAMP_ERR_ALIGN;
+    const int64_t esz = in_dtype == DAMP_IN_BF16 ? 2 : 4;
+    const Range ro = range_of(o, N * H * dv * 4);
+    const Range inputs[] = {range_of(q, N * Hq * dk * esz), range_of(k, N * Hq * dk * esz),
+                            range_of(v, N * H * dv * esz), range_of(g, (g_per_head ? H : N * H) * 4),
+                            range_of(slot_idx, slot_idx ? B * 4 : 0), range_of(lengths, lengths ? B * 4 : 0)};
+    if (overlap(ro, pool)) return DAMP_ERR_ALIAS;
+    for (const Range &r : inputs)
+        if (overlap(ro, r) || overlap(pool, r)) return DAMP_ERR_ALIAS;
+    LinArgs a{};
+    a.H = L->num_heads;
+    a.Hqk = L->num_qk_heads;
+    a.dk = L->d_k;
+    a.dv = L->d_v;
+    a.state = state;
+    a.num_slots = num_slots;
+    a.slot_idx = slot_idx;
+    a.batch = batch;
+    a.T = T;
+    a.lengths = lengths;
+    a.q = q;
+    a.k = k;
+    a.v = v;
+    a.g = g;
+    a.g_per_head = g_per_head != 0;
+    a.o = o;
+    a.in_bf16 = in_dtype == DAMP_IN_BF16;
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    return (step ? launch_lin_step(a, s) : launch_lin_chunk(a, s)) == cudaSuccess ? DAMP_OK : DAMP_ERR_CUDA;
+}
+
+// Whole slots of several pools.  Entries src (live slots of a compaction) and dst; launches
+// take kSlotPools pools each.
+enum SlotOp { kCopySlots, kZeroSlots, kCompactSlots };
+
+damp_status slots(void *const *pools, const int64_t *slot_bytes, int32_t n_pools, int64_t num_slots, const int32_t *src,
+                  int32_t *dst, int32_t n, void *stream, SlotOp op) {
+    constexpr int kMaxPools = 1024;
+    if (n_pools < 0 || n_pools > kMaxPools || num_slots < 0 || n < 0) return DAMP_ERR_SHAPE;
+    if (n == 0 || (n_pools == 0 && op != kCompactSlots)) return DAMP_OK;
+    if (num_slots < 1 || num_slots > INT32_MAX) return DAMP_ERR_SHAPE;
+    if (op != kZeroSlots && n > kMaxSlotEntries) return DAMP_ERR_SHAPE;
+    if (op == kCompactSlots && num_slots > kMaxPlanSlots) return DAMP_ERR_SHAPE;
+    if ((n_pools && (!pools || !slot_bytes)) || !dst || (op != kZeroSlots && !src)) return DAMP_ERR_NULL;
+    if (!aligned(dst, 4) || (src && !aligned(src, 4))) return DAMP_ERR_ALIGN;
+    const Range rd = range_of(dst, (int64_t)n * 4), rs = range_of(src, src ? (int64_t)n * 4 : 0);
+    if (op == kCompactSlots && overlap(rd, rs)) return DAMP_ERR_ALIAS;
+    for (int i = 0; i < n_pools; ++i) {
+        if (!pools[i]) return DAMP_ERR_NULL;
+        if (!aligned(pools[i], 16)) return DAMP_ERR_ALIGN;
+        if (slot_bytes[i] < 16 || slot_bytes[i] % 16 || slot_bytes[i] / 16 > INT32_MAX ||
+            slot_bytes[i] > INT64_MAX / num_slots)
+            return DAMP_ERR_SHAPE;
+        const Range r = range_of(pools[i], num_slots * slot_bytes[i]);
+        if (overlap(r, rd) || overlap(r, rs)) return DAMP_ERR_ALIAS;
+        for (int j = 0; j < i; ++j)
+            if (overlap(r, range_of(pools[j], num_slots * slot_bytes[j]))) return DAMP_ERR_ALIAS;
+    }
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    SlotArgs a{};
+    a.n = n;
+    a.num_slots = num_slots;
+    a.src = src;
+    a.dst = dst;
+    if (op == kCompactSlots && launch_compact_plan(a, dst, s) != cudaSuccess) return DAMP_ERR_CUDA;
+    for (int i0 = 0; i0 < n_pools; i0 += kSlotPools) {
+        a.n_pools = n_pools - i0 < kSlotPools ? n_pools - i0 : kSlotPools;
+        for (int i = 0; i < a.n_pools; ++i)
+            a.pools[i] = SlotPool{static_cast<uint8_t *>(pools[i0 + i]), slot_bytes[i0 + i]};
+        if ((op == kZeroSlots ? launch_zero_slots(a, s) : launch_copy_slots(a, s)) != cudaSuccess) return DAMP_ERR_CUDA;
+    }
+    return DAMP_OK;
+}
+
 enum ConvKind { kQ, kDQ, kPack, kUnpack };
 
 damp_status convert(const damp_layout *L, void *state, int64_t num_slots, const int32_t *slot_idx, int32_t batch,
@@ -500,6 +595,76 @@ damp_status damp_kda_prefill_chunk(const damp_layout *layout, void *state, int64
                    stream, true);
 }
 
+damp_status damp_lin_decode_step(const damp_layout *layout, float *state, int64_t num_slots, const int32_t *slot_idx,
+                                 int32_t batch, const void *q, const void *k, const void *v, const float *g,
+                                 int32_t g_per_head, float *o, int32_t in_dtype, void *stream) {
+    return lin(layout, state, num_slots, slot_idx, batch, 1, nullptr, q, k, v, g, g_per_head, o, in_dtype, stream, true);
+}
+
+damp_status damp_lin_prefill_chunk(const damp_layout *layout, float *state, int64_t num_slots, const int32_t *slot_idx,
+                                   int32_t batch, int32_t chunk_len, const int32_t *lengths, const void *q,
+                                   const void *k, const void *v, const float *g, int32_t g_per_head, float *o,
+                                   int32_t in_dtype, void *stream) {
+    return lin(layout, state, num_slots, slot_idx, batch, chunk_len, lengths, q, k, v, g, g_per_head, o, in_dtype, stream,
+               false);
+}
+
+damp_status damp_copy_slots(void *const *pools, const int64_t *slot_bytes, int32_t n_pools, int64_t num_slots,
+                            const int32_t *src, const int32_t *dst, int32_t n, void *stream) {
+    return slots(pools, slot_bytes, n_pools, num_slots, src, const_cast<int32_t *>(dst), n, stream, kCopySlots);
+}
+
+damp_status damp_zero_slots(void *const *pools, const int64_t *slot_bytes, int32_t n_pools, int64_t num_slots,
+                            const int32_t *idx, int32_t n, void *stream) {
+    return slots(pools, slot_bytes, n_pools, num_slots, nullptr, const_cast<int32_t *>(idx), n, stream, kZeroSlots);
+}
+
+damp_status damp_compact_slots(void *const *pools, const int64_t *slot_bytes, int32_t n_pools, int64_t num_slots,
+                               const int32_t *slot_idx, int32_t n, int32_t *slot_idx_out, void *stream) {
+    return slots(pools, slot_bytes, n_pools, num_slots, slot_idx, slot_idx_out, n, stream, kCompactSlots);
+}
+
+damp_status damp_verify_drafts(const void *target_logits, const void *draft_logits, int32_t logits_dtype,
+                               int64_t row_stride, int32_t vocab, const int32_t *draft_tokens, const int32_t *draft_len,
+                               int32_t n_draft, const float *u, const float *noise, const float *temperature,
+                               int32_t batch, int32_t *tokens_out, int32_t *count_out, void *stream) {
+    if (logits_dtype != DAMP_IN_BF16 && logits_dtype != DAMP_IN_FP32) return DAMP_ERR_FORMAT;
+    if (batch < 0 || n_draft < 0 || vocab < 1 || row_stride < vocab) return DAMP_ERR_SHAPE;
+    if (batch == 0) return DAMP_OK;
+    const int64_t B = batch, D = n_draft, esz = logits_dtype == DAMP_IN_BF16 ? 2 : 4;
+    if (row_stride > INT64_MAX / 8 / (B * (D + 1))) return DAMP_ERR_SHAPE;
+    if (!target_logits || !noise || !tokens_out || !count_out || (D && (!draft_tokens || !u))) return DAMP_ERR_NULL;
+    if (!aligned(target_logits, 16) || (draft_logits && !aligned(draft_logits, 16)) || !aligned(noise, 16) ||
+        !aligned(draft_tokens, 4) || !aligned(draft_len, 4) || !aligned(u, 4) || !aligned(temperature, 4) ||
+        !aligned(tokens_out, 4) || !aligned(count_out, 4))
+        return DAMP_ERR_ALIGN;
+    const Range rt = range_of(tokens_out, B * (D + 1) * 4), rc = range_of(count_out, B * 4);
+    const Range inputs[] = {range_of(target_logits, ((B * (D + 1) - 1) * row_stride + vocab) * esz),
+                            range_of(draft_logits, draft_logits && D ? ((B * D - 1) * row_stride + vocab) * esz : 0),
+                            range_of(draft_tokens, draft_tokens ? B * D * 4 : 0),
+                            range_of(draft_len, draft_len ? B * 4 : 0), range_of(u, u ? B * D * 4 : 0),
+                            range_of(noise, B * vocab * 4), range_of(temperature, temperature ? B * 4 : 0)};
+    if (overlap(rt, rc)) return DAMP_ERR_ALIAS;
+    for (const Range &r : inputs)
+        if (overlap(rt, r) || overlap(rc, r)) return DAMP_ERR_ALIAS;
+    VerifyArgs a{};
+    a.target = target_logits;
+    a.draft = draft_logits;
+    a.tokens = draft_tokens;
+    a.draft_len = draft_len;
+    a.u = u;
+    a.noise = noise;
+    a.temperature = temperature;
+    a.batch = batch;
+    a.n_draft = n_draft;
+    a.vocab = vocab;
+    a.bf16 = logits_dtype == DAMP_IN_BF16;
+    a.row_stride = row_stride;
+    a.tokens_out = tokens_out;
+    a.count_out = count_out;
+    return launch_verify(a, static_cast<cudaStream_t>(stream)) == cudaSuccess ? DAMP_OK : DAMP_ERR_CUDA;
+}
+
 damp_status damp_quantize_state(const damp_layout *layout, const float *S, const uint8_t *perm, void *state,
                                 int64_t num_slots, const int32_t *slot_idx, int32_t batch, void *stream) {
     return convert(layout, state, num_slots, slot_idx, batch, perm, const_cast<float *>(S), nullptr, nullptr,
@@ -666,6 +831,12 @@ damp_status damp_device_status(uint32_t *status) {
     if (take_status_quad_kda(&bits) != cudaSuccess) return DAMP_ERR_CUDA;
     all |= bits;
     if (take_status_fp32(&bits) != cudaSuccess) return DAMP_ERR_CUDA;
+    all |= bits;
+    if (take_status_lin(&bits) != cudaSuccess) return DAMP_ERR_CUDA;
+    all |= bits;
+    if (take_status_slots(&bits) != cudaSuccess) return DAMP_ERR_CUDA;
+    all |= bits;
+    if (take_status_verify(&bits) != cudaSuccess) return DAMP_ERR_CUDA;
     all |= bits;
     if (take_status_convert(&bits) != cudaSuccess) return DAMP_ERR_CUDA;
     all |= bits;

@@ -47,6 +47,50 @@ struct ConvArgs {
     uint16_t *meta;
 };
 
+// linear attention with a decay per head on an FP32 state pool
+struct LinArgs {
+    int32_t H, Hqk, dk, dv;
+    float *state;
+    int64_t num_slots;
+    const int32_t *slot_idx;
+    int32_t batch, T;  // tokens per row (1 for the step)
+    const int32_t *lengths;
+    const void *q, *k, *v;
+    const float *g;
+    int32_t g_per_head;  // g [H] instead of one per token and head
+    float *o;
+    int32_t in_bf16;
+    uint32_t *status;  // set by the launchers
+};
+
+// whole slots of the pools of a model's layers
+constexpr int kSlotPools = 64;           // pools per launch
+constexpr int kSlotThreads = 256;
+constexpr int kPlanThreads = 1024;
+constexpr int kMaxSlotEntries = 12288;   // 16-byte slices of all entries fit in 192 KB of shared memory
+constexpr int64_t kMaxPlanSlots = 1 << 18;  // a bit and 1/32 word of counts per slot: 64 KB
+struct SlotPool {
+    uint8_t *base;
+    int64_t slot_bytes;
+};
+struct SlotArgs {
+    SlotPool pools[kSlotPools];
+    int32_t n_pools, n, slice;
+    int64_t num_slots;
+    const int32_t *src, *dst;
+    uint32_t *status;  // set by the launchers
+};
+
+struct VerifyArgs {
+    const void *target, *draft;  // logits [B][D + 1] and [B][D] rows of row_stride elements
+    const int32_t *tokens, *draft_len;
+    const float *u, *noise, *temperature;
+    int32_t batch, n_draft, vocab, bf16;
+    int64_t row_stride;
+    int32_t *tokens_out, *count_out;
+    uint32_t *status;  // set by the launcher
+};
+
 // Launchers (return the CUDA error of the launch; they perform no host-side argument checks).
 cudaError_t launch_packed_gdn(const StepArgs &a, cudaStream_t s);
 cudaError_t launch_packed_kda(const StepArgs &a, cudaStream_t s);
@@ -66,6 +110,12 @@ cudaError_t launch_packed_kda_f8(const StepArgs &a, cudaStream_t s);
 cudaError_t launch_quad_rowabs_gdn(const StepArgs &a, cudaStream_t s);
 cudaError_t launch_quad_rowabs_kda(const StepArgs &a, cudaStream_t s);
 cudaError_t launch_fp32_step(const StepArgs &a, cudaStream_t s);
+cudaError_t launch_lin_step(LinArgs a, cudaStream_t s);
+cudaError_t launch_lin_chunk(LinArgs a, cudaStream_t s);
+cudaError_t launch_copy_slots(SlotArgs a, cudaStream_t s);  // dst[i] <- src[i]
+cudaError_t launch_zero_slots(SlotArgs a, cudaStream_t s);  // dst[i]
+cudaError_t launch_compact_plan(SlotArgs a, int32_t *out, cudaStream_t s);  // live slots src -> new numbers
+cudaError_t launch_verify(VerifyArgs a, cudaStream_t s);
 cudaError_t launch_quantize(const ConvArgs &a, cudaStream_t s);
 cudaError_t launch_dequantize(const ConvArgs &a, cudaStream_t s);
 cudaError_t launch_pack_tiers(const ConvArgs &a, cudaStream_t s);
@@ -100,6 +150,9 @@ cudaError_t take_status_groups_kda(uint32_t *bits);
 cudaError_t take_status_quad_gdn(uint32_t *bits);
 cudaError_t take_status_quad_kda(uint32_t *bits);
 cudaError_t take_status_fp32(uint32_t *bits);
+cudaError_t take_status_lin(uint32_t *bits);
+cudaError_t take_status_slots(uint32_t *bits);
+cudaError_t take_status_verify(uint32_t *bits);
 cudaError_t take_status_convert(uint32_t *bits);
 cudaError_t take_status_rowabs(uint32_t *bits);
 cudaError_t take_status_prefill_gdn(uint32_t *bits);

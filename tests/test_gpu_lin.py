@@ -1,0 +1,213 @@
+"""Linear attention with a decay per head on the GPU against the recurrence in float64:
+the single-token step and chunks of every length class, head layouts, types, gates
+(none, resets, fast), ragged lengths with garbage past them, slots and streams."""
+import math
+
+import pytest
+import torch
+
+import paper_2608_27513_gb300 as damp
+from tests import serving_ref as R
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    from paper_2608_27513_gb300 import build
+    build.build()
+    torch.cuda.init()
+    assert damp.device_status() == 0
+    yield
+    assert damp.device_status() == 0
+
+
+def _inputs(B, T, H, Hqk, dk, dv, dtype, gate, seed=0, slots=None):
+    gen = torch.Generator(device=DEV).manual_seed(seed + 1000 * T + dk)
+    n = lambda *s: torch.randn(*s, generator=gen, device=DEV)
+    slots = B + 2 if slots is None else slots
+    g = {"token": lambda: -torch.nn.functional.softplus(n(B, T, H) + torch.linspace(-6, 2, H, device=DEV)),
+         "head": lambda: -torch.linspace(0.001, 0.8, H, device=DEV),
+         "zero": lambda: torch.zeros(B, T, H, device=DEV),
+         "fast": lambda: -40.0 * torch.rand(B, T, H, generator=gen, device=DEV),
+         "grow": lambda: 0.02 * n(B, T, H),
+         "reset": lambda: torch.where(torch.rand(B, T, H, generator=gen, device=DEV) < 0.1, -math.inf,
+                                      -0.05 * torch.rand(B, T, H, generator=gen, device=DEV)),
+         "lowest": lambda: torch.where(torch.rand(B, T, H, generator=gen, device=DEV) < 0.1,
+                                       torch.finfo(torch.float32).min, -0.3)}[gate]()
+    q, k = n(B, T, Hqk, dk), n(B, T, Hqk, dk)
+    pool = n(slots, H, dk, dv)
+    idx = torch.randperm(slots, generator=gen, device=DEV)[:B].to(torch.int32)
+    return dict(q=(q / dk ** 0.5).to(dtype), k=(k / dk ** 0.5).to(dtype), v=n(B, T, H, dv).to(dtype), g=g), pool, idx
+
+
+def _check_chunk(B, T, H, Hqk, dk, dv, dtype, gate, lengths=None, seed=0):
+    ops, pool, idx = _inputs(B, T, H, Hqk, dk, dv, dtype, gate, seed)
+    L = damp.Layout(H, Hqk, dk, dv, 0)
+    n = None if lengths is None else torch.tensor(lengths, dtype=torch.int32, device=DEV)
+    o_ref, S_ref, oa, Sa = R.lin(pool[idx.long()], **ops, lengths=n)
+    if n is not None:  # what stands past a row's length must not matter
+        past = torch.arange(T, device=DEV)[None] >= n.clamp(0, T)[:, None]
+        for name in ("q", "k", "v"):
+            ops[name][past] = math.nan
+        if ops["g"].dim() == 3:
+            ops["g"][past] = math.nan
+    before = pool.clone()
+    o = damp.lin_prefill_chunk(L, pool, **ops, lengths=n, slot_idx=idx)
+    R.check_lin(o, o_ref, oa, T, dk, "o")
+    R.check_lin(pool[idx.long()], S_ref, Sa, T, dk, "S")
+    others = torch.ones(pool.shape[0], dtype=torch.bool, device=DEV)
+    others[idx.long()] = False
+    assert torch.equal(pool[others], before[others])
+    if n is not None:
+        assert not o[past].any()
+        still = idx[n <= 0].long()
+        assert torch.equal(pool[still], before[still])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T", [1, 2, 5, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 200, 321])
+def test_chunk_lengths(T, dtype):
+    _check_chunk(2, T, 4, 2, 128, 128, dtype, "token")
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("H,Hqk,dk,dv", [(4, 4, 64, 64), (3, 1, 32, 96), (2, 2, 128, 1024), (6, 2, 64, 32), (2, 1, 128, 160),
+                                         (1, 1, 32, 32), (8, 8, 128, 64), (2, 1, 64, 128), (2, 2, 128, 256)])
+def test_chunk_layouts(H, Hqk, dk, dv, dtype):
+    _check_chunk(2, 70, H, Hqk, dk, dv, dtype, "token", seed=1)
+
+
+@pytest.mark.parametrize("gate", ["head", "zero", "fast", "grow", "reset", "lowest"])
+@pytest.mark.parametrize("T", [7, 150])
+@pytest.mark.parametrize("d", [64, 128])
+def test_chunk_gates(gate, T, d):
+    _check_chunk(2, T, 4, 4, d, d, torch.bfloat16, gate, seed=2)
+    _check_chunk(2, T, 4, 4, d, d, torch.float32, gate, seed=3)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T", [5, 64, 130])
+def test_ragged_rows_ignore_what_stands_past_them(T, dtype):
+    _check_chunk(7, T, 2, 1, 128, 128, dtype, "token", lengths=[T, 0, 1, T // 2, T + 9, -3, T - 1], seed=4)
+    _check_chunk(7, T, 2, 1, 64, 64, dtype, "head", lengths=[T, 0, 1, T // 2, T + 9, -3, T - 1], seed=5)
+
+
+@pytest.mark.parametrize("B,H,T", [(1, 2, 3000), (3, 5, 1111), (1, 32, 2049)])
+def test_long_prompts_of_few_rows(B, H, T):
+    _check_chunk(B, T, H, H, 128, 128, torch.bfloat16, "token", seed=6)
+    _check_chunk(B, T, H, H, 128, 128, torch.bfloat16, "head", lengths=[T - 700] + [T] * (B - 1), seed=7)
+
+
+def test_many_rows_fill_the_gpu():
+    _check_chunk(40, 130, 8, 4, 128, 128, torch.bfloat16, "token", lengths=[(37 * i) % 131 for i in range(40)], seed=8)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("H,Hqk,dk,dv", [(4, 4, 64, 64), (3, 1, 32, 96), (2, 2, 128, 1024), (6, 2, 64, 32), (32, 16, 128, 128),
+                                         (1, 1, 32, 32), (5, 5, 128, 160)])
+@pytest.mark.parametrize("gate", ["token", "head", "reset"])
+def test_decode_step(H, Hqk, dk, dv, dtype, gate):
+    B = 5
+    ops, pool, idx = _inputs(B, 1, H, Hqk, dk, dv, dtype, gate, seed=9)
+    o_ref, S_ref, oa, Sa = R.lin(pool[idx.long()], **ops)
+    one = {n: (t if t.dim() == 1 else t[:, 0].contiguous()) for n, t in ops.items()}
+    before = pool.clone()
+    o = damp.lin_decode_step(damp.Layout(H, Hqk, dk, dv, 0), pool, **one, slot_idx=idx)
+    R.check_lin(o, o_ref[:, 0], oa[:, 0], 1, dk, "o")
+    R.check_lin(pool[idx.long()], S_ref, Sa, 1, dk, "S")
+    others = torch.ones(pool.shape[0], dtype=torch.bool, device=DEV)
+    others[idx.long()] = False
+    assert torch.equal(pool[others], before[others])
+
+
+def test_steps_after_a_chunk_continue_it():
+    B, T, H, d = 3, 90, 4, 128
+    ops, pool, idx = _inputs(B, T, H, H, d, d, torch.bfloat16, "token", seed=10)
+    L = damp.Layout(H, H, d, d, 0)
+    o_ref, S_ref, oa, Sa = R.lin(pool[idx.long()], **ops)
+    cut = lambda a, b: {n: t[:, a:b].contiguous() for n, t in ops.items()}
+    o = [damp.lin_prefill_chunk(L, pool, **cut(0, 70), slot_idx=idx),
+         damp.lin_prefill_chunk(L, pool, **cut(70, 87), slot_idx=idx)]
+    o += [damp.lin_decode_step(L, pool, **{n: t[:, 0].contiguous() for n, t in cut(t, t + 1).items()}, slot_idx=idx)[:, None]
+          for t in range(87, 90)]
+    R.check_lin(torch.cat(o, 1), o_ref, oa, T, d, "o")
+    R.check_lin(pool[idx.long()], S_ref, Sa, T, d, "S")
+
+
+@pytest.mark.parametrize("T", [1, 40])
+def test_bad_slots_are_skipped_and_reported(T):
+    H, d = 2, 128
+    ops, pool, _ = _inputs(4, T, H, H, d, d, torch.bfloat16, "token", seed=11, slots=4)
+    idx = torch.tensor([2, -1, 4, 0], dtype=torch.int32, device=DEV)
+    before = pool.clone()
+    o_ref, S_ref, oa, Sa = R.lin(pool[[2, 0]], **{n: t[[0, 3]] for n, t in ops.items()})
+    o = torch.full((4, T, H, d), 7.0, device=DEV)
+    damp.lin_prefill_chunk(damp.Layout(H, H, d, d, 0), pool, **ops, o=o, slot_idx=idx)
+    assert damp.device_status() == damp.DEV_BAD_SLOT
+    R.check_lin(o[[0, 3]], o_ref, oa, T, d, "o")
+    R.check_lin(pool[[2, 0]], S_ref, Sa, T, d, "S")
+    assert torch.equal(pool[[1, 3]], before[[1, 3]]) and bool((o[1:3] == 7.0).all())
+
+
+def test_offsets_past_32_bits():
+    H, d = 32, 128
+    slots = 4200  # 2.2e9 state values
+    pool = torch.zeros(slots, H, d, d, device=DEV)
+    L = damp.Layout(H, H, d, d, 0)
+    for T in (1, 40):
+        ops, small, _ = _inputs(2, T, H, H, d, d, torch.bfloat16, "token", seed=12, slots=2)
+        idx = torch.tensor([slots - 1, 3], dtype=torch.int32, device=DEV)
+        pool[idx.long()] = small
+        o_ref, S_ref, oa, Sa = R.lin(small, **ops)
+        o = damp.lin_prefill_chunk(L, pool, **ops, slot_idx=idx)
+        R.check_lin(o, o_ref, oa, T, d, "o")
+        R.check_lin(pool[idx.long()], S_ref, Sa, T, d, "S")
+    one = {n: t[:, 0].contiguous() for n, t in ops.items()}
+    pool[idx.long()] = small
+    o_ref, S_ref, oa, Sa = R.lin(small, **{n: t[:, :1] for n, t in ops.items()})
+    o = damp.lin_decode_step(L, pool, **one, slot_idx=idx)
+    R.check_lin(o, o_ref[:, 0], oa[:, 0], 1, d, "o")
+    R.check_lin(pool[idx.long()], S_ref, Sa, 1, d, "S")
+
+
+def test_results_repeat_bit_for_bit_and_on_another_stream():
+    B, T, H, d = 3, 600, 4, 128
+    ops, pool, idx = _inputs(B, T, H, H, d, d, torch.bfloat16, "token", seed=13)
+    L = damp.Layout(H, H, d, d, 0)
+    a, b = pool.clone(), pool.clone()
+    o1 = damp.lin_prefill_chunk(L, a, **ops, slot_idx=idx)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    o2 = damp.lin_prefill_chunk(L, b, **ops, slot_idx=idx, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(o1, o2) and torch.equal(a, b)
+
+
+def test_a_graph_replays_the_step_and_the_chunk():
+    B, H, d = 4, 4, 128
+    L = damp.Layout(H, H, d, d, 0)
+    for T in (1, 200):
+        ops, pool, idx = _inputs(B, T, H, H, d, d, torch.bfloat16, "token", seed=14)
+        start = pool.clone()
+        run = lambda: damp.lin_prefill_chunk(L, pool, **ops, slot_idx=idx)
+        o1 = run().clone()
+        end = pool.clone()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            o2 = run()
+        pool.copy_(start)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(o1, o2) and torch.equal(pool, end)
+
+
+def test_empty_calls():
+    L = damp.Layout(2, 2, 64, 64, 0)
+    pool = damp.new_fp32_state(L, 3)
+    z = lambda *s: torch.zeros(*s, device=DEV)
+    o = damp.lin_prefill_chunk(L, pool, z(2, 0, 2, 64), z(2, 0, 2, 64), z(2, 0, 2, 64), z(2, 0, 2))
+    assert o.shape == (2, 0, 2, 64)
+    o = damp.lin_decode_step(L, pool, z(0, 2, 64), z(0, 2, 64), z(0, 2, 64), z(0, 2))
+    assert o.shape == (0, 2, 64) and not pool.any()
