@@ -334,6 +334,13 @@ DAMP_API damp_status damp_kda_prefill_chunk(const damp_layout *layout, void *sta
  *              tokens; a row of length 0 keeps its state.  What q, k, v and g hold past a
  *              row's length is not used.
  *   o          float [B][T][H][d_v]; zero past a row's length
+ *   workspace  damp_lin_prefill_workspace() bytes of scratch, 16-B aligned, of no use to
+ *              any other call while this one runs (0 bytes for most shapes: NULL is then
+ *              allowed); too few are DAMP_ERR_SHAPE
+ *   Chunks of T >= 32 tokens with BF16 inputs, d_k 64 or 128 and d_v a multiple of 128 run
+ *   on the tensor cores; with few rows and heads their tokens are split into segments,
+ *   which is what the workspace is for.  The results differ only in FP32 rounding (the FP32
+ *   operands of the products keep 16 bits).
  * slot_idx, num_slots, batch, in_dtype and the status bits as in damp_gdn_decode_step
  * (the outputs of a row with a bad slot are left as they are).
  */
@@ -345,7 +352,9 @@ DAMP_API damp_status damp_lin_prefill_chunk(const damp_layout *layout, float *st
                                             const int32_t *slot_idx, int32_t batch, int32_t chunk_len,
                                             const int32_t *lengths, const void *q, const void *k, const void *v,
                                             const float *g, int32_t g_per_head, float *o, int32_t in_dtype,
-                                            void *stream);
+                                            void *workspace, int64_t workspace_bytes, void *stream);
+DAMP_API int64_t damp_lin_prefill_workspace(const damp_layout *layout, int32_t batch, int32_t chunk_len,
+                                            int32_t in_dtype);
 
 /*
  * Whole slots of the pools of a model's layers, packed or FP32, in one call.

@@ -592,15 +592,19 @@ def _lin(layout, state, q, k, v, g, o, lengths, slot_idx, num_slots, stream, lea
             _given("g", g, (H,) if per_head else lead + (H,), torch.float32), 1 if per_head else 0]
     if o is None:
         o = _new(o_shape, torch.float32, v, stream)
-    args += [_given("o", o, o_shape, torch.float32), IN_BF16 if dtype == torch.bfloat16 else IN_FP32, _stream(stream)]
+    in_dtype = IN_BF16 if dtype == torch.bfloat16 else IN_FP32
+    args += [_given("o", o, o_shape, torch.float32), in_dtype]
     idx = None if slot_idx is None else _given("slot_idx", slot_idx, (B,), torch.int32)
     c = layout.c()
     head = [ctypes.byref(c), pool, num_slots, idx, B]
     if lead_dims == 1:
-        _check(lib().damp_lin_decode_step(*head, *args), "damp_lin_decode_step")
+        _check(lib().damp_lin_decode_step(*head, *args, _stream(stream)), "damp_lin_decode_step")
     else:
         n = None if lengths is None else _given("lengths", lengths, (B,), torch.int32)
-        _check(lib().damp_lin_prefill_chunk(*head, lead[1], n, *args), "damp_lin_prefill_chunk")
+        need = lib().damp_lin_prefill_workspace(head[0], B, lead[1], in_dtype)
+        ws = _new((need,), torch.uint8, v, stream) if need else None
+        _check(lib().damp_lin_prefill_chunk(*head, lead[1], n, *args, ws.data_ptr() if need else None, need,
+                                            _stream(stream)), "damp_lin_prefill_chunk")
     return o
 
 

@@ -52,7 +52,8 @@ SIGNATURES = {
     "damp_calib_select": (_status, [_L, _P, _i64, _P, _i64, ctypes.c_float, _P, _P, _P]),
     "damp_calib_accumulate": (_status, [_L, _P, _i32, _i32, _P, _P, _P, _P, _P, _i32, _i32, _i32, _P, _P, _P]),
     "damp_lin_decode_step": (_status, [_L, _P, _i64, _P, _i32, _P, _P, _P, _P, _i32, _P, _i32, _P]),
-    "damp_lin_prefill_chunk": (_status, [_L, _P, _i64, _P, _i32, _i32, _P, _P, _P, _P, _P, _i32, _P, _i32, _P]),
+    "damp_lin_prefill_chunk": (_status, [_L, _P, _i64, _P, _i32, _i32, _P, _P, _P, _P, _P, _i32, _P, _i32, _P, _i64, _P]),
+    "damp_lin_prefill_workspace": (_i64, [_L, _i32, _i32, _i32]),
     "damp_copy_slots": (_status, [_P, _P, _i32, _i64, _P, _P, _i32, _P]),
     "damp_zero_slots": (_status, [_P, _P, _i32, _i64, _P, _i32, _P]),
     "damp_compact_slots": (_status, [_P, _P, _i32, _i64, _P, _i32, _P, _P]),

@@ -265,7 +265,7 @@ damp_status prefill(const damp_layout *L, void *state, int64_t num_slots, const 
 // Linear attention with a decay per head on an FP32 pool: T tokens per row (the step: 1).
 damp_status lin(const damp_layout *L, float *state, int64_t num_slots, const int32_t *slot_idx, int32_t batch, int32_t T,
                 const int32_t *lengths, const void *q, const void *k, const void *v, const float *g, int32_t g_per_head,
-                float *o, int32_t in_dtype, void *stream, bool step) {
+                float *o, int32_t in_dtype, void *workspace, int64_t workspace_bytes, void *stream, bool step) {
     if (!L) return DAMP_ERR_NULL;
     damp_layout l2 = *L;  // the FP32 state ignores k_hi and lo_format and holds every model head
     l2.k_hi = 0;
@@ -311,7 +311,19 @@ damp_status lin(const damp_layout *L, float *state, int64_t num_slots, const int
     a.o = o;
     a.in_bf16 = in_dtype == DAMP_IN_BF16;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    return (step ? launch_lin_step(a, s) : launch_lin_chunk(a, s)) == cudaSuccess ? DAMP_OK : DAMP_ERR_CUDA;
+    if (step) return launch_lin_step(a, s) == cudaSuccess ? DAMP_OK : DAMP_ERR_CUDA;
+    if (!lin_tc_takes(a)) return launch_lin_chunk(a, s) == cudaSuccess ? DAMP_OK : DAMP_ERR_CUDA;
+    const int64_t need = (int64_t)lin_tc_workspace(a);
+    if (need) {
+        if (!workspace) return DAMP_ERR_NULL;
+        if (workspace_bytes < need) return DAMP_ERR_SHAPE;
+        if (!aligned(workspace, 16)) return DAMP_ERR_ALIGN;
+        const Range rw = range_of(workspace, need);
+        if (overlap(rw, ro) || overlap(rw, pool)) return DAMP_ERR_ALIAS;
+        for (const Range &r : inputs)
+            if (overlap(rw, r)) return DAMP_ERR_ALIAS;
+    }
+    return launch_lin_tc(a, workspace, s) == cudaSuccess ? DAMP_OK : DAMP_ERR_CUDA;
 }
 
 // Whole slots of several pools.  Entries src (live slots of a compaction) and dst; launches
@@ -598,15 +610,32 @@ damp_status damp_kda_prefill_chunk(const damp_layout *layout, void *state, int64
 damp_status damp_lin_decode_step(const damp_layout *layout, float *state, int64_t num_slots, const int32_t *slot_idx,
                                  int32_t batch, const void *q, const void *k, const void *v, const float *g,
                                  int32_t g_per_head, float *o, int32_t in_dtype, void *stream) {
-    return lin(layout, state, num_slots, slot_idx, batch, 1, nullptr, q, k, v, g, g_per_head, o, in_dtype, stream, true);
+    return lin(layout, state, num_slots, slot_idx, batch, 1, nullptr, q, k, v, g, g_per_head, o, in_dtype, nullptr, 0,
+               stream, true);
 }
 
 damp_status damp_lin_prefill_chunk(const damp_layout *layout, float *state, int64_t num_slots, const int32_t *slot_idx,
                                    int32_t batch, int32_t chunk_len, const int32_t *lengths, const void *q,
                                    const void *k, const void *v, const float *g, int32_t g_per_head, float *o,
-                                   int32_t in_dtype, void *stream) {
-    return lin(layout, state, num_slots, slot_idx, batch, chunk_len, lengths, q, k, v, g, g_per_head, o, in_dtype, stream,
-               false);
+                                   int32_t in_dtype, void *workspace, int64_t workspace_bytes, void *stream) {
+    return lin(layout, state, num_slots, slot_idx, batch, chunk_len, lengths, q, k, v, g, g_per_head, o, in_dtype,
+               workspace, workspace_bytes, stream, false);
+}
+
+int64_t damp_lin_prefill_workspace(const damp_layout *layout, int32_t batch, int32_t chunk_len, int32_t in_dtype) {
+    if (!layout || batch <= 0 || chunk_len <= 0) return 0;
+    damp_layout l2 = *layout;
+    l2.k_hi = 0;
+    l2.lo_format = 0;
+    if (check_layout(&l2) != DAMP_OK) return 0;
+    LinArgs a{};
+    a.H = layout->num_heads;
+    a.dk = layout->d_k;
+    a.dv = layout->d_v;
+    a.batch = batch;
+    a.T = chunk_len;
+    a.in_bf16 = in_dtype == DAMP_IN_BF16;
+    return (int64_t)lin_tc_workspace(a);
 }
 
 damp_status damp_copy_slots(void *const *pools, const int64_t *slot_bytes, int32_t n_pools, int64_t num_slots,
@@ -833,6 +862,8 @@ damp_status damp_device_status(uint32_t *status) {
     if (take_status_fp32(&bits) != cudaSuccess) return DAMP_ERR_CUDA;
     all |= bits;
     if (take_status_lin(&bits) != cudaSuccess) return DAMP_ERR_CUDA;
+    all |= bits;
+    if (take_status_lin_tc(&bits) != cudaSuccess) return DAMP_ERR_CUDA;
     all |= bits;
     if (take_status_slots(&bits) != cudaSuccess) return DAMP_ERR_CUDA;
     all |= bits;

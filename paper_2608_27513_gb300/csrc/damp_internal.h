@@ -112,6 +112,10 @@ cudaError_t launch_quad_rowabs_kda(const StepArgs &a, cudaStream_t s);
 cudaError_t launch_fp32_step(const StepArgs &a, cudaStream_t s);
 cudaError_t launch_lin_step(LinArgs a, cudaStream_t s);
 cudaError_t launch_lin_chunk(LinArgs a, cudaStream_t s);
+bool lin_tc_takes(const LinArgs &a);        // the chunk runs on the tensor cores
+size_t lin_tc_workspace(const LinArgs &a);  // bytes
+cudaError_t launch_lin_tc(LinArgs a, void *workspace, cudaStream_t s);
+cudaError_t take_status_lin_tc(uint32_t *bits);
 cudaError_t launch_copy_slots(SlotArgs a, cudaStream_t s);  // dst[i] <- src[i]
 cudaError_t launch_zero_slots(SlotArgs a, cudaStream_t s);  // dst[i]
 cudaError_t launch_compact_plan(SlotArgs a, int32_t *out, cudaStream_t s);  // live slots src -> new numbers

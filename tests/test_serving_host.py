@@ -34,11 +34,11 @@ def test_lin_rejects_bad_arguments(L, fb):
         lay.update(over.pop("lay", {}))
         c = _lib.DampLayout(*lay.values())
         a = dict(layout=ctypes.byref(c), state=_p(fb, 0), num_slots=4, slot_idx=None, batch=2, T=3, lengths=None, q=_p(fb, 1),
-                 k=_p(fb, 2), v=_p(fb, 3), g=_p(fb, 4), per_head=0, o=_p(fb, 5), dtype=0, stream=None)
+                 k=_p(fb, 2), v=_p(fb, 3), g=_p(fb, 4), per_head=0, o=_p(fb, 5), dtype=0, ws=None, ws_bytes=0, stream=None)
         a.update(over)
         if chunk:
             return L.damp_lin_prefill_chunk(*a.values())
-        return L.damp_lin_decode_step(*(x for n, x in a.items() if n not in ("T", "lengths")))
+        return L.damp_lin_decode_step(*(x for n, x in a.items() if n not in ("T", "lengths", "ws", "ws_bytes")))
 
     for chunk in (False, True):
         assert call(chunk, batch=0) == OK          # nothing enqueued; k_hi and lo_format are ignored
@@ -64,6 +64,18 @@ def test_lin_rejects_bad_arguments(L, fb):
     assert call(True, T=-1) == SHAPE
     assert call(True, lengths=_p(fb, 7, 1)) == ALIGN
     assert call(True, lengths=_p(fb, 5)) == ALIAS
+    # one long row of few heads is split: its scratch
+    lay, T = dict(d_k=64, d_v=128), 640
+    c = _lib.DampLayout(2, 2, 64, 128, 0, 0, 0, None)
+    need = L.damp_lin_prefill_workspace(ctypes.byref(c), 1, T, 0)
+    if need:  # (the split goes by the number of SMs, which is not known without a GPU)
+        assert call(True, lay=lay, T=T, batch=1) == NULL
+        assert call(True, lay=lay, T=T, batch=1, ws=_p(fb, 6), ws_bytes=need - 1) == SHAPE
+        assert call(True, lay=lay, T=T, batch=1, ws=_p(fb, 6, 4), ws_bytes=need) == ALIGN
+        assert call(True, lay=lay, T=T, batch=1, ws=_p(fb, 5, 64), ws_bytes=need) == ALIAS
+    assert L.damp_lin_prefill_workspace(ctypes.byref(c), 0, T, 0) == 0
+    assert L.damp_lin_prefill_workspace(ctypes.byref(c), 1, T, 1) == 0
+    assert L.damp_lin_prefill_workspace(None, 1, T, 0) == 0
 
 
 def test_slots_reject_bad_arguments(L, fb):
