@@ -362,7 +362,7 @@ DAMP_API int64_t damp_lin_prefill_workspace(const damp_layout *layout, int32_t b
  *               num_slots slots of slot_bytes[i] bytes (a multiple of 16, 16 at least);
  *               pools must not overlap each other or the slot lists (DAMP_ERR_ALIAS)
  *   num_slots   slots of every pool (up to 2^31 - 1; 2^18 for damp_compact_slots)
- *   n           entries of the slot lists (device int32, 4-B aligned), 0 .. 12288 (copy and
+ *   n           entries of the slot lists (device int32, 4-B aligned), 0 .. 4096 (copy and
  *               compact); a negative entry is skipped, one >= num_slots too, and sets
  *               DAMP_DEV_BAD_SLOT
  * damp_copy_slots: slot dst[i] receives what slot src[i] held before the call.  The lists

@@ -67,7 +67,7 @@ struct LinArgs {
 constexpr int kSlotPools = 64;           // pools per launch
 constexpr int kSlotThreads = 256;
 constexpr int kPlanThreads = 1024;
-constexpr int kMaxSlotEntries = 12288;   // 16-byte slices of all entries fit in 192 KB of shared memory
+constexpr int kMaxSlotEntries = 4096;    // two 16-byte slices and 16 bytes of lists of each fit in shared memory
 constexpr int64_t kMaxPlanSlots = 1 << 18;  // a bit and 1/32 word of counts per slot: 64 KB
 struct SlotPool {
     uint8_t *base;
