@@ -18,14 +18,17 @@
 // again and 48 KB.  Accumulation and the state are FP32.  G is summed in FP64 and kept as
 // two floats, so that G_i - G_j keeps its digits where both are large (fast decays).
 //
-// Two CTAs per SM (112 KB of shared memory, 256 of the 512 tensor-memory columns each)
-// overlap one's products with the other's conversions; the next piece's q, k and v are
-// fetched while the current one is finished.  Bound by the bytes of q, k, v and o, with
-// the conversions next.
+// q, k and v come by tensor copies (TMA, 128-byte swizzle), issued as soon as the products that
+// read the tile before are done.  Warp 4, which has no part in P and K~, issues copies and
+// products and sums the next piece's gates meanwhile.  Two CTAs per SM (110 KB of shared memory,
+// 256 of the 512 tensor-memory columns each) overlap one's products with the other's
+// conversions.  Bound by the conversions, with the bytes of q, k, v and o next.
 //
 // Few (slot, head) pairs and many tokens: the tokens are split into segments.  A first
 // launch computes what each segment adds to the state (k and v only), a second one starts
 // every segment from the joined state before it.
+#include <cuda.h>
+
 #include "damp_internal.h"
 #include "prefill_tc.cuh"
 
@@ -39,6 +42,7 @@ namespace {
 
 constexpr int kLtC = 64;
 constexpr int kLtThreads = 256;
+constexpr int kLtBox = 64 * 128;  // bytes of a copied box: 64 tokens x 64 bf16
 constexpr uint32_t kLtCols = 256;
 // tensor-memory columns: Q K^T, then O2 | O1 | S_0 as bf16 parts, then what the piece adds
 constexpr uint32_t kLtG = 0, kLtO1 = 64, kLtS = 128;
@@ -47,22 +51,22 @@ template <int DK>
 struct LtSmem {  // bytes from the base of the dynamic shared memory
     static constexpr int tile = kLtC * DK * 2;
     static constexpr int vtile = kLtC * 128 * 2;
-    static constexpr int q = 0;              // rows 0-63 of [Q; K]
-    static constexpr int k = tile;           // rows 64-127
-    static constexpr int v = 2 * tile;       // two buffers
-    static constexpr int kd = v + 2 * vtile; // K~ hi, lo
-    static constexpr int p = kd + 2 * tile;  // P hi, lo
-    static constexpr int g = p + 2 * kLtC * kLtC * 2;  // (hi, lo) of G in base 2, 64 pairs
-    static constexpr int eg = g + 512;       // e^{G_i}
-    static constexpr int bar = eg + 256;     // two mbarriers, the tensor-memory address
-    static constexpr int bytes = bar + 32;
+    // 64-column boxes: [q box 0][k box 0][q box 1][k box 1], so that [Q; K] is one operand of 128 rows
+    static constexpr int q = 0, k = kLtBox;
+    static constexpr int v = 2 * tile;        // two buffers of two boxes
+    static constexpr int kd = v + 2 * vtile;  // K~ hi, lo
+    static constexpr int p = kd + 2 * tile;   // P hi, lo: columns 0-31 of 64 rows, columns 32-63 of rows 32-63
+    static constexpr int ppart = 64 * 64 + 32 * 64;
+    static constexpr int g = p + 2 * ppart;   // two buffers: (hi, lo) of G in base 2, 64 pairs, and e^{G_i}
+    static constexpr int gbuf = 512 + 256;
+    static constexpr int bar = g + 2 * gbuf;  // seven mbarriers, the tensor-memory address
+    static constexpr int bytes = bar + 64;
 };
 
 struct LinTcParams {
     float *state;
     int64_t num_slots;
     const int32_t *slot_idx, *lengths;
-    const uint8_t *q, *k, *v;
     const float *g;
     float *o;
     float *part;      // [batch * H * nc][nseg][DK][128]: states and additions of the segments
@@ -77,9 +81,18 @@ __device__ __forceinline__ float lt_ex2(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// 16 bytes, or zeros where the row is past the tokens
-__device__ __forceinline__ void cp_async16_or_zero(uint32_t dst, const void *src, bool live) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16u : 0u) : "memory");
+// one box of a [batch][token][head][channel] tensor at (channel, head, token, row) into shared memory
+__device__ __forceinline__ void lt_copy_box(uint32_t dst, const CUtensorMap *map, int ch, int head, int t, int b, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(
+                     dst),
+                 "l"(map), "r"(ch), "r"(head), "r"(t), "r"(b), "r"(bar)
+                 : "memory");
+}
+// descriptor of an operand in 128-byte swizzled boxes.  K-major: rows of 128 bytes, 8 rows `sbo`
+// apart, a K step of 16 is 32 bytes.  MN-major: 64 columns per box, boxes `lbo` apart, 8 rows of K
+// `sbo` apart.
+__device__ __forceinline__ uint64_t lt_desc_sw(uint32_t addr, uint32_t lbo, uint32_t sbo) {
+    return tc_desc(addr, lbo, sbo) | (2ull << 61);
 }
 __device__ __forceinline__ void lt_ld16(uint32_t taddr, float (&v)[16]) {
     uint32_t r[16];
@@ -91,6 +104,22 @@ __device__ __forceinline__ void lt_ld16(uint32_t taddr, float (&v)[16]) {
                  : "memory");
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+}
+// eight columns at two addresses
+__device__ __forceinline__ void lt_ld8x2(uint32_t ta, uint32_t tb, float (&a)[8], float (&b)[8]) {
+    uint32_t r[8], s[8];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%16];\n"
+                 "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%8,%9,%10,%11,%12,%13,%14,%15}, [%17];\n"
+                 "tcgen05.wait::ld.sync.aligned;"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+                   "=r"(s[0]), "=r"(s[1]), "=r"(s[2]), "=r"(s[3]), "=r"(s[4]), "=r"(s[5]), "=r"(s[6]), "=r"(s[7])
+                 : "r"(ta), "r"(tb)
+                 : "memory");
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        a[i] = __uint_as_float(r[i]);
+        b[i] = __uint_as_float(s[i]);
+    }
 }
 __device__ __forceinline__ void lt_st8(uint32_t taddr, const uint32_t (&r)[8]) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr), "r"(r[0]),
@@ -114,34 +143,39 @@ __device__ __forceinline__ void split2_pair(float2 x, uint32_t &h, uint32_t &l) 
     memcpy(&l, &l2, 4);
 }
 
-// 64 rows of CELLS 16-byte cells (row stride `ld` bytes in global memory) into the layout of
-// the operands: cell c of row t at (t >> 3) CELLS 128 + c 128 + (t & 7) 16.  Eight lanes
-// write 128 contiguous bytes and four take 64 contiguous bytes of a row.
-template <int CELLS>
-__device__ __forceinline__ void lt_load(uint32_t dst, const uint8_t *src, int64_t ld, int n, int warp, int lane) {
-    const int t0 = lane & 7, c0 = lane >> 3;
-#pragma unroll
-    for (int r = 0; r < CELLS / 4; ++r) {
-        const int u = r * 8 + warp;
-        const int t = (u / (CELLS / 4)) * 8 + t0, c = (u % (CELLS / 4)) * 4 + c0;
-        const bool live = t < n;
-        cp_async16_or_zero(dst + (uint32_t)((t >> 3) * CELLS * 128 + c * 128 + (t & 7) * 16),
-                           src + (int64_t)(live ? t : 0) * ld + 16 * c, live);
-    }
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
+// a sum of two floats, hi + lo
+struct Pair {
+    float hi, lo;
+};
+__device__ __forceinline__ Pair add_pair(Pair a, Pair b) {
+    const float s = a.hi + b.hi, t = s - a.hi;
+    const float e = ((a.hi - (s - t)) + (b.hi - t)) + (a.lo + b.lo);  // the rounding of s, and the low parts
+    const float h = s + e;
+    return Pair{h, e - (h - s)};
 }
 
 // STATE: only what the segment adds to the state and its decay
 template <int DK, bool STATE>
-__global__ void __launch_bounds__(kLtThreads, 2) lin_tc_kernel(const LinTcParams p) {
-    extern __shared__ __align__(128) uint8_t smem[];
+__global__ void __launch_bounds__(kLtThreads, 2)
+    lin_tc_kernel(const LinTcParams p, const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
+                  const __grid_constant__ CUtensorMap vmap) {
+    extern __shared__ __align__(1024) uint8_t smem[];
     using M = LtSmem<DK>;
     constexpr int CELLS = DK / 8;
     constexpr int NR = DK / 2;  // state rows of a thread
-    constexpr uint32_t kIdG = tc_idesc(64, false, false), kIdO2 = tc_idesc(64, true, false), kIdS = tc_idesc(DK, true, true);
+    constexpr uint32_t kIdG = tc_idesc(64, false, false), kIdO2 = tc_idesc(64, true, false), kIdO2b = tc_idesc(32, true, false),
+                       kIdS = tc_idesc(DK, true, true);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const bool issuer = warp == 4;
     const int row = 32 * (warp & 3) + lane, half = warp >> 2;
     const uint32_t sb = smem_u32(smem);
-    const uint32_t bar1 = sb + M::bar, bar2 = bar1 + 8, s_taddr = bar1 + 16;
+    // copies landed; products done: Q K^T, O1, the addition to S, O2; operands written: K~, P
+    const uint32_t bar_full = sb + M::bar, bar_qk = bar_full + 8, bar_o1 = bar_full + 16, bar_ds = bar_full + 24,
+                   bar_o2 = bar_full + 32, bar_kd = bar_full + 40, bar_p = bar_full + 48, s_taddr = bar_full + 56;
 
     const int seg = (int)(blockIdx.x % (STATE ? p.nseg - 1 : p.nseg));
     const int item = (int)(blockIdx.x / (STATE ? p.nseg - 1 : p.nseg));
@@ -167,25 +201,64 @@ __global__ void __launch_bounds__(kLtThreads, 2) lin_tc_kernel(const LinTcParams
                      : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
+    constexpr int kKdWarps = STATE ? 8 : 4, kPWarps = 3;
     if (tid == 0) {
-        mbar_init(bar1, 1);
-        mbar_init(bar2, 1);
+        mbar_init(bar_full, 1);
+        mbar_init(bar_qk, 1);
+        mbar_init(bar_o1, 1);
+        mbar_init(bar_ds, 1);
+        mbar_init(bar_o2, 1);
+        mbar_init(bar_kd, 32 * kKdWarps);
+        mbar_init(bar_p, 32 * kPWarps);
         fence_mbar_init();
     }
-    const int64_t qk_ld = (int64_t)p.Hqk * DK * 2, v_ld = (int64_t)p.H * p.dv * 2;
-    const int64_t qk_off = ((int64_t)b * T * p.Hqk + (int64_t)h * p.Hqk / p.H) * DK * 2;
-    const uint8_t *const q0 = p.q + qk_off, *const k0 = p.k + qk_off;
-    const uint8_t *const v0 = p.v + (((int64_t)b * T * p.H + h) * p.dv + c * 128) * 2;
-    auto load_qk = [&](int t) {
-        if (!STATE) lt_load<CELLS>(sb + M::q, q0 + t * qk_ld, qk_ld, t_end - t, warp, lane);
-        lt_load<CELLS>(sb + M::k, k0 + t * qk_ld, qk_ld, t_end - t, warp, lane);
+    const int hq = (int)((int64_t)h * p.Hqk / p.H);
+    constexpr int QKBOX = DK / 64;  // boxes of q or k
+    auto copy_qk = [&](int t) {  // one thread
+#pragma unroll
+        for (int j = 0; j < QKBOX; ++j) {
+            if (!STATE) lt_copy_box(sb + M::q + 2 * kLtBox * j, &qmap, 64 * j, hq, t, b, bar_full);
+            lt_copy_box(sb + M::k + 2 * kLtBox * j, &kmap, 64 * j, hq, t, b, bar_full);
+        }
     };
-    auto load_v = [&](int t, int buf) {
-        lt_load<16>(sb + M::v + buf * M::vtile, v0 + t * v_ld, v_ld, t_end - t, warp, lane);
+    auto copy_v = [&](int t, uint32_t buf) {  // one thread; the bytes of the piece's q and k too
+        mbar_arrive_expect_tx(bar_full, ((STATE ? 1 : 2) * QKBOX + 2) * kLtBox);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) lt_copy_box(sb + M::v + buf * M::vtile + kLtBox * j, &vmap, c * 128 + 64 * j, h, t, b, bar_full);
     };
-    load_qk(t_begin);
-    load_v(t_begin, 0);
-    cp_async_commit();
+    // Gates of a piece (the issuing warp; lane l holds tokens 2l and 2l + 1): inclusive sums in base 2
+    // as pairs of floats, so that G_i - G_j keeps its digits where both are large.
+    const float *const g0 = p.g_per_head ? p.g + h : p.g + (int64_t)b * T * p.H + h;
+    const int64_t gstep = p.g_per_head ? 0 : p.H;
+    float ga = 0.f, gb = 0.f;
+    Pair dec_total{0.f, 0.f};  // base-2 log of the segment's decay
+    auto gate = [&](int t) -> float {
+        if (t >= t_end) return 0.f;
+        const float x = g0[(int64_t)t * gstep];
+        return x < -200.f ? -200.f : x;  // e^-200 is 0 in FP32 (-inf: a reset)
+    };
+    auto fetch_gates = [&](int t) {
+        ga = gate(t + 2 * lane);
+        gb = gate(t + 2 * lane + 1);
+    };
+    auto sum_gates = [&](int buf) {
+        constexpr float kLog2eF = 1.4426950408889634f;
+        const Pair x0{ga * kLog2eF, 0.f}, x1{gb * kLog2eF, 0.f}, own = add_pair(x0, x1);
+        Pair x = own;
+#pragma unroll
+        for (int m = 1; m < 32; m <<= 1) {
+            const Pair y{__shfl_up_sync(kFull, x.hi, m), __shfl_up_sync(kFull, x.lo, m)};
+            if (lane >= m) x = add_pair(x, y);
+        }
+        Pair before{__shfl_up_sync(kFull, x.hi, 1), __shfl_up_sync(kFull, x.lo, 1)};
+        if (lane == 0) before = Pair{0.f, 0.f};
+        const Pair first = add_pair(before, x0);
+        const uint32_t at = sb + M::g + (uint32_t)(buf * M::gbuf);
+        sts128(at + 16 * lane, make_uint4(__float_as_uint(first.hi), __float_as_uint(first.lo), __float_as_uint(x.hi), __float_as_uint(x.lo)));
+        sts32(at + 512 + 8 * lane, __float_as_uint(lt_ex2(first.hi)));
+        sts32(at + 512 + 8 * lane + 4, __float_as_uint(lt_ex2(x.hi)));
+        if (STATE) dec_total = add_pair(dec_total, Pair{__shfl_sync(kFull, x.hi, 31), __shfl_sync(kFull, x.lo, 31)});
+    };
 
     // the state before the segment, transposed: value column `row`, key channels NR half ..
     float2 S[NR / 2];
@@ -203,131 +276,146 @@ __global__ void __launch_bounds__(kLtThreads, 2) lin_tc_kernel(const LinTcParams
             dst[(2 * r + 1) * ld] = S[r].y;
         }
     };
-    // Parts of a split row: 0 the state before it (the last segment overwrites the pool's while
-    // others may still start), 1 the state after segment 0, s what segment s - 1 adds.
-    const bool whole = seg == 0 && t_end == len;  // the row is one segment
-    if (STATE && seg > 0) {
-#pragma unroll
-        for (int r = 0; r < NR / 2; ++r) S[r] = make_float2(0.f, 0.f);
-    } else if (STATE || whole) {
-        load_state(st, p.dv);
-        if (STATE) store_state(part0, 128);
-    } else {
-        load_state(part0 + (seg > 0 ? DK * 128 : 0), 128);
-        for (int s = 2; s <= seg; ++s) {
-            const float2 d2 = splat2(dec0[s]);
-            const float *const ps = part0 + (int64_t)s * DK * 128;
-#pragma unroll
-            for (int r = 0; r < NR / 2; ++r) S[r] = fma2(S[r], d2, make_float2(ps[(2 * r) * 128], ps[(2 * r + 1) * 128]));
-        }
+    if (issuer) {
+        fetch_gates(t_begin);
+        sum_gates(0);
+        fetch_gates(t_begin + kLtC);
     }
-    if (!STATE) {
-        // columns 32-63 of rows 0-31 of P are above the diagonal: zero for every piece
-        const int part = tid >> 7, r = (tid >> 2) & 31, cell = 4 + (tid & 3);
-        sts128(sb + M::p + (uint32_t)(part * 8192 + (r >> 3) * 1024 + cell * 128 + (r & 7) * 16), make_uint4(0u, 0u, 0u, 0u));
+    {
+        // Parts of a split row: 0 the state before it (the last segment overwrites the pool's while
+        // others may still start), 1 the state after segment 0, s what segment s - 1 adds.
+        const bool whole = seg == 0 && t_end == len;  // the row is one segment
+        if (STATE && seg > 0) {
+#pragma unroll
+            for (int r = 0; r < NR / 2; ++r) S[r] = make_float2(0.f, 0.f);
+        } else if (STATE || whole) {
+            load_state(st, p.dv);
+            if (STATE) store_state(part0, 128);
+        } else {
+            load_state(part0 + (seg > 0 ? DK * 128 : 0), 128);
+            for (int s = 2; s <= seg; ++s) {
+                const float2 d2 = splat2(dec0[s]);
+                const float *const ps = part0 + (int64_t)s * DK * 128;
+#pragma unroll
+                for (int r = 0; r < NR / 2; ++r) S[r] = fma2(S[r], d2, make_float2(ps[(2 * r) * 128], ps[(2 * r + 1) * 128]));
+            }
+        }
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    if (tid == 128) {
+        copy_v(t_begin, 0);
+        copy_qk(t_begin);
+    }
     const uint32_t tmem = lds32(s_taddr);
     const uint32_t tl = tmem + ((uint32_t)(32 * (warp & 3)) << 16);
     const uint32_t tS = tl + kLtS + (uint32_t)(NR * half);  // this thread's columns of both uses
 
     // S as two bf16 parts: the half's hi words, then its lo words
-    auto store_parts = [&](int r8, const float2 *x) {  // 16 rows from 16 r8
-        uint32_t hw[8], lw[8];
+    auto store_parts = [&]() {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) split2_pair(x[i], hw[i], lw[i]);
-        lt_st8(tS + 8 * r8, hw);
-        lt_st8(tS + NR / 2 + 8 * r8, lw);
-    };
-    if (!STATE) {
+        for (int r8 = 0; r8 < NR / 16; ++r8) {  // 16 rows
+            uint32_t hw[8], lw[8];
 #pragma unroll
-        for (int r8 = 0; r8 < NR / 16; ++r8) store_parts(r8, S + 8 * r8);
+            for (int i = 0; i < 8; ++i) split2_pair(S[8 * r8 + i], hw[i], lw[i]);
+            lt_st8(tS + 8 * r8, hw);
+            lt_st8(tS + NR / 2 + 8 * r8, lw);
+        }
         lt_wait_st();
-    }
-
-    // gates of a piece: lane l holds tokens 2l and 2l + 1
-    const float *const g0 = p.g_per_head ? p.g + h : p.g + (int64_t)b * T * p.H + h;
-    const int64_t gstep = p.g_per_head ? 0 : p.H;
-    auto gate = [&](int t) -> float {
-        if (t >= t_end) return 0.f;
-        const float x = g0[(int64_t)t * gstep];
-        return x < -200.f ? -200.f : x;  // e^-200 is 0 in FP32 (-inf: a reset)
     };
-    float ga = 0.f, gb = 0.f;
-    if (warp == 0) {
-        ga = gate(t_begin + 2 * lane);
-        gb = gate(t_begin + 2 * lane + 1);
-    }
-    double dec_total = 0.0;  // warp 0: base-2 log of the segment's decay
+    if (!STATE) store_parts();
+
     bool ok = true;
-    uint32_t last1 = 0, last2 = 0;  // phases of the last products issued
-    int buf = 0;
+    uint32_t buf = 0;  // buffers and the phase of every barrier
 #pragma unroll 1
     for (int t0 = t_begin; t0 < t_end; t0 += kLtC, buf ^= 1) {
-        const int n = min(kLtC, t_end - t0);
         const bool more = t0 + kLtC < t_end;
-        const uint32_t vt = sb + M::v + (uint32_t)(buf * M::vtile);
-        cp_async_wait_all();
-        fence_proxy_async_smem();
+        const uint32_t vt = sb + M::v + buf * M::vtile, sg = sb + M::g + buf * M::gbuf;
+        ok &= mbar_wait_bounded(bar_full, buf);
+        const int n = t_end - t0;  // tokens of the piece (64 or more: all)
+        if (n < kLtC) {  // v past the row's length may hold anything: zero, as 0 times it has to be
+            for (int i = tid; i < (kLtC - n) * 16; i += kLtThreads)
+                sts128(vt + (uint32_t)((i & 1) * kLtBox + (n + (i >> 4)) * 128 + ((i >> 1) & 7) * 16), make_uint4(0u, 0u, 0u, 0u));
+            fence_proxy_async_smem();
+        }
         tc_fence_before();
-        __syncthreads();
+        ok = __syncthreads_and(ok);
         tc_fence_after();
-        if (!STATE && tid == 128) {
+        if (!ok) break;
+        auto issue_add = [&]() {  // what the piece adds to S
+            if (!STATE) ok &= mbar_wait_bounded(bar_o1, buf);  // it goes over O1's operand
+            ok &= mbar_wait_bounded(bar_kd, buf);
+            tc_fence_after();
+            if (lane == 0) {
 #pragma unroll
-            for (int ks = 0; ks < DK / 16; ++ks) {
-                const uint64_t d = tc_desc(sb + M::q + 256 * ks, 128, 16 * DK);
-                tc_mma(tmem + kLtG, d, tc_desc(sb + M::k + 256 * ks, 128, 16 * DK), kIdG, ks != 0);
+                for (int part = 0; part < 2; ++part)
+#pragma unroll
+                    for (int ks = 0; ks < kLtC / 16; ++ks)
+                        tc_mma(tmem + kLtS, lt_desc_sw(vt + 2048 * ks, kLtBox, 1024),
+                               tc_desc(sb + M::kd + M::tile * part + 32 * DK * ks, 16 * DK, 128), kIdS, (part | ks) != 0);
+                tc_commit(bar_ds);
+                if (more) copy_qk(t0 + kLtC);  // q and k are read
             }
-            tc_commit(bar1);
+            __syncwarp();
+        };
+        if (issuer) {
+            if (lane == 0) {
+                if (!STATE) {
 #pragma unroll
-            for (int part = 0; part < 2; ++part)
+                    for (int ks = 0; ks < DK / 16; ++ks) {
+                        const uint32_t off = (uint32_t)(2 * kLtBox * (ks / 4) + 32 * (ks % 4));
+                        tc_mma(tmem + kLtG, lt_desc_sw(sb + M::q + off, 16, 1024), lt_desc_sw(sb + M::k + off, 16, 1024), kIdG, ks != 0);
+                    }
+                    tc_commit(bar_qk);
 #pragma unroll
-                for (int ks = 0; ks < DK / 16; ++ks) {
-                    constexpr int HS = DK / 32;  // K steps per half
-                    const uint32_t a = tmem + kLtS + (uint32_t)(NR * (ks / HS) + NR / 2 * part + 8 * (ks % HS));
-                    lt_mma_ta(tmem + kLtO1, a, tc_desc(sb + M::q + 256 * ks, 128, 16 * DK), kIdG, (part | ks) != 0);
+                    for (int part = 0; part < 2; ++part)
+#pragma unroll
+                        for (int ks = 0; ks < DK / 16; ++ks) {
+                            constexpr int HS = DK / 32;  // K steps per half
+                            const uint32_t a = tmem + kLtS + (uint32_t)(NR * (ks / HS) + NR / 2 * part + 8 * (ks % HS));
+                            const uint32_t off = (uint32_t)(2 * kLtBox * (ks / 4) + 32 * (ks % 4));
+                            lt_mma_ta(tmem + kLtO1, a, lt_desc_sw(sb + M::q + off, 16, 1024), kIdG, (part | ks) != 0);
+                        }
+                    tc_commit(bar_o1);
                 }
-            tc_commit(bar2);
-        }
-        last1 = last2 = 0;
-        if (more) load_v(t0 + kLtC, buf ^ 1);
-        if (warp == 0) {  // inclusive sums of the gates, base 2
-            constexpr double kLog2eD = 1.4426950408889634074;
-            const double a0 = (double)ga * kLog2eD, a1 = a0 + (double)gb * kLog2eD;
-            double x = a1;
-#pragma unroll
-            for (int m = 1; m < 32; m <<= 1) {
-                const double y = __shfl_up_sync(kFull, x, m);
-                if (lane >= m) x += y;
+                if (more) copy_v(t0 + kLtC, buf ^ 1);
             }
-            dec_total += __shfl_sync(kFull, x, 31);
-            const double x0 = x - a1 + a0;
-            const float h0 = (float)x0, h1 = (float)x;
-            sts128(sb + M::g + 16 * lane, make_uint4(__float_as_uint(h0), __float_as_uint((float)(x0 - (double)h0)),
-                                                     __float_as_uint(h1), __float_as_uint((float)(x - (double)h1))));
-            sts32(sb + M::eg + 8 * lane, __float_as_uint(lt_ex2(h0)));
-            sts32(sb + M::eg + 8 * lane + 4, __float_as_uint(lt_ex2(h1)));
+            __syncwarp();
             if (more) {
-                ga = gate(t0 + kLtC + 2 * lane);
-                gb = gate(t0 + kLtC + 2 * lane + 1);
+                sum_gates(buf ^ 1);
+                fetch_gates(t0 + 2 * kLtC);
+            }
+            if (!STATE) {
+                issue_add();
+                ok &= mbar_wait_bounded(bar_p, buf);
+                tc_fence_after();
+                if (lane == 0) {
+#pragma unroll
+                    for (int part = 0; part < 2; ++part)
+#pragma unroll
+                        for (int ks = 0; ks < kLtC / 16; ++ks) {
+                            const uint64_t a = lt_desc_sw(vt + 2048 * ks, kLtBox, 1024);
+                            const uint32_t pp = sb + M::p + M::ppart * part;
+                            if (ks < 2) tc_mma(tmem + kLtG, a, tc_desc(pp + 256 * ks, 128, 512), kIdO2, (part | ks) != 0);
+                            else tc_mma(tmem + kLtG + 32, a, tc_desc(pp + 4096 + 256 * (ks - 2), 128, 512), kIdO2b, 1);
+                        }
+                    tc_commit(bar_o2);
+                }
+                __syncwarp();
             }
         }
-        if (!STATE) ok &= mbar_wait_bounded(bar1, 0);
-        if (!__syncthreads_and(ok)) break;
-        tc_fence_after();
-        // warps 0, 1, 5: P (rows 0-31; rows 32-63, columns 0-31 and 32-63);
-        // warps 2, 3, 6, 7: K~ (warps 4 and, with the state alone, 0, 1, 5 have none)
-        if ((warp & 3) >= 2) {
-            const int kt = (warp & 1) * 32 + lane;  // token
-            const uint32_t gj = sb + M::g + 8 * kt, gC = sb + M::g + 8 * 63;
+        if (STATE || (warp & 3) >= 2) {  // K~
+            constexpr int NC = STATE ? CELLS / 4 : CELLS / 2;  // cells of a thread
+            const int kt = STATE ? tid & 63 : (warp & 1) * 32 + lane, c0 = NC * (STATE ? tid >> 6 : half);
+            const uint32_t gj = sg + 8 * kt, gC = sg + 8 * 63;
             const float2 f = splat2(lt_ex2((ldsf(gC) - ldsf(gj)) + (ldsf(gC + 4) - ldsf(gj + 4))));
-            const uint32_t cell = (uint32_t)((kt >> 3) * CELLS * 128 + (kt & 7) * 16);
-#pragma unroll 4
-            for (int i = 0; i < CELLS / 2; ++i) {
-                const uint32_t off = cell + (uint32_t)((CELLS / 2 * half + i) * 128);
-                const uint4 w4 = lds128(sb + M::k + off);
+            const uint32_t cell = (uint32_t)((kt >> 3) * CELLS * 128 + (kt & 7) * 16 + c0 * 128);
+#pragma unroll 2
+            for (int i = 0; i < NC; ++i) {
+                const uint32_t off = cell + (uint32_t)(i * 128);
+                uint4 w4 = lds128(sb + M::k + (uint32_t)(2 * kLtBox * ((c0 + i) >> 3) + kt * 128 + (((c0 + i) ^ kt) & 7) * 16));
+                if (kt >= n) w4 = make_uint4(0u, 0u, 0u, 0u);  // past the row's length
                 const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
                 uint32_t hw[4], lw[4];
 #pragma unroll
@@ -336,63 +424,44 @@ __global__ void __launch_bounds__(kLtThreads, 2) lin_tc_kernel(const LinTcParams
                 sts128(sb + M::kd + off, make_uint4(hw[0], hw[1], hw[2], hw[3]));
                 sts128(sb + M::kd + M::tile + off, make_uint4(lw[0], lw[1], lw[2], lw[3]));
             }
-        } else if (!STATE && warp != 4) {
-            const float gih = ldsf(sb + M::g + 8 * row), gil = ldsf(sb + M::g + 8 * row + 4);
+            fence_proxy_async_smem();
+            mbar_arrive(bar_kd);
+        } else if (!issuer) {  // P: rows 0-31; rows 32-63, columns 0-31 and 32-63
+            ok &= mbar_wait_bounded(bar_qk, buf);
+            tc_fence_after();
+            const float gih = ldsf(sg + 8 * row), gil = ldsf(sg + 8 * row + 4);
+            const uint32_t prow = sb + M::p + (half ? 4096u + (uint32_t)(((row - 32) >> 3) * 512) : (uint32_t)((row >> 3) * 512)) +
+                                  (uint32_t)((row & 7) * 16);
 #pragma unroll
             for (int j0 = 0; j0 < 32; j0 += 16) {
                 float x[16];
                 lt_ld16(tl + kLtG + 32 * half + j0, x);
                 const int jb = 32 * half + j0;
 #pragma unroll
-                for (int e = 0; e < 16; e += 2) {
-                    const uint4 gg = lds128(sb + M::g + 8 * (jb + e));
-                    const float d0 = (gih - __uint_as_float(gg.x)) + (gil - __uint_as_float(gg.y));
-                    const float d1 = (gih - __uint_as_float(gg.z)) + (gil - __uint_as_float(gg.w));
-                    x[e] = jb + e <= row ? x[e] * lt_ex2(d0) : 0.f;
-                    x[e + 1] = jb + e + 1 <= row ? x[e + 1] * lt_ex2(d1) : 0.f;
-                }
-#pragma unroll
                 for (int g8 = 0; g8 < 2; ++g8) {
                     uint32_t hw[4], lw[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) split2_pair(make_float2(x[8 * g8 + 2 * e], x[8 * g8 + 2 * e + 1]), hw[e], lw[e]);
-                    const uint32_t off = (uint32_t)((row >> 3) * 1024 + (jb / 8 + g8) * 128 + (row & 7) * 16);
-                    sts128(sb + M::p + off, make_uint4(hw[0], hw[1], hw[2], hw[3]));
-                    sts128(sb + M::p + 8192 + off, make_uint4(lw[0], lw[1], lw[2], lw[3]));
+                    for (int e = 0; e < 4; ++e) {
+                        const int j = jb + 8 * g8 + 2 * e;
+                        const uint4 gg = lds128(sg + 8 * j);
+                        const float d0 = (gih - __uint_as_float(gg.x)) + (gil - __uint_as_float(gg.y));
+                        const float d1 = (gih - __uint_as_float(gg.z)) + (gil - __uint_as_float(gg.w));
+                        split2_pair(make_float2(j <= row ? x[8 * g8 + 2 * e] * lt_ex2(d0) : 0.f,
+                                                j + 1 <= row ? x[8 * g8 + 2 * e + 1] * lt_ex2(d1) : 0.f),
+                                    hw[e], lw[e]);
+                    }
+                    const uint32_t at = prow + (uint32_t)((j0 / 8 + g8) * 128);
+                    sts128(at, make_uint4(hw[0], hw[1], hw[2], hw[3]));
+                    sts128(at + M::ppart, make_uint4(lw[0], lw[1], lw[2], lw[3]));
                 }
             }
+            tc_fence_before();  // Q K^T is read: O2 goes over it
+            fence_proxy_async_smem();
+            mbar_arrive(bar_p);
         }
-        fence_proxy_async_smem();
-        if (!STATE) ok &= mbar_wait_bounded(bar2, 0);
-        tc_fence_before();
-        if (!__syncthreads_and(ok)) break;
-        tc_fence_after();
-        if (tid == 128) {
-#pragma unroll
-            for (int part = 0; part < 2; ++part)
-#pragma unroll
-                for (int ks = 0; ks < kLtC / 16; ++ks)
-                    tc_mma(tmem + kLtS, tc_desc(vt + 4096 * ks, 2048, 128),
-                           tc_desc(sb + M::kd + M::tile * part + 32 * DK * ks, 16 * DK, 128), kIdS, (part | ks) != 0);
-            tc_commit(bar1);
-            if (!STATE) {
-#pragma unroll
-                for (int part = 0; part < 2; ++part)
-#pragma unroll
-                    for (int ks = 0; ks < kLtC / 16; ++ks)
-                        tc_mma(tmem + kLtG, tc_desc(vt + 4096 * ks, 2048, 128),
-                               tc_desc(sb + M::p + 8192 * part + 256 * ks, 128, 1024), kIdO2, (part | ks) != 0);
-                tc_commit(bar2);
-            }
-        }
-        if (more) {
-            load_qk(t0 + kLtC);
-            cp_async_commit();
-        }
-        last1 = STATE ? (uint32_t)buf : 1u;
-        last2 = 1;
-        const float2 eC = splat2(ldsf(sb + M::eg + 4 * 63));
-        ok &= mbar_wait_bounded(bar1, last1);
+        if (STATE && issuer) issue_add();
+        const float2 eC = splat2(ldsf(sg + 512 + 4 * 63));
+        ok &= mbar_wait_bounded(bar_ds, buf);
         tc_fence_after();
 #pragma unroll
         for (int r8 = 0; r8 < NR / 16; ++r8) {
@@ -401,49 +470,41 @@ __global__ void __launch_bounds__(kLtThreads, 2) lin_tc_kernel(const LinTcParams
 #pragma unroll
             for (int i = 0; i < 8; ++i) S[8 * r8 + i] = fma2(S[8 * r8 + i], eC, make_float2(d[2 * i], d[2 * i + 1]));
         }
-        if (!STATE && more) {
-#pragma unroll
-            for (int r8 = 0; r8 < NR / 16; ++r8) store_parts(r8, S + 8 * r8);
-        }
         if (!STATE) {
-            ok &= mbar_wait_bounded(bar2, 1);
+            if (more) store_parts();
+            ok &= mbar_wait_bounded(bar_o2, buf);
             tc_fence_after();
-            float *const oc = o + (int64_t)(t0 + 32 * half) * ostep;
+            float *oc = o + (int64_t)(t0 + 32 * half) * ostep;
             const int nh = n - 32 * half;
+#pragma unroll 1
+            for (int j0 = 0; j0 < 32 && j0 < nh; j0 += 8) {
+                float o1[8], o2[8];
+                lt_ld8x2(tl + kLtO1 + 32 * half + j0, tl + kLtG + 32 * half + j0, o1, o2);
 #pragma unroll
-            for (int j0 = 0; j0 < 32; j0 += 16) {
-                if (j0 < nh) {
-                    float o1[16], o2[16];
-                    lt_ld16(tl + kLtO1 + 32 * half + j0, o1);
-                    lt_ld16(tl + kLtG + 32 * half + j0, o2);
+                for (int e = 0; e < 8; e += 4) {
+                    const uint4 eg = lds128(sg + 512 + 4 * (32 * half + j0 + e));
+                    const float ev[4] = {__uint_as_float(eg.x), __uint_as_float(eg.y), __uint_as_float(eg.z), __uint_as_float(eg.w)};
 #pragma unroll
-                    for (int e = 0; e < 16; e += 4) {
-                        const uint4 eg = lds128(sb + M::eg + 4 * (32 * half + j0 + e));
-                        const float ev[4] = {__uint_as_float(eg.x), __uint_as_float(eg.y), __uint_as_float(eg.z), __uint_as_float(eg.w)};
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            if (j0 + e + i < nh) oc[(j0 + e + i) * ostep] = fmaf(ev[i], o1[e + i], o2[e + i]);
-                    }
+                    for (int i = 0; i < 4; ++i, oc += ostep)
+                        if (j0 + e + i < nh) *oc = fmaf(ev[i], o1[e + i], o2[e + i]);
                 }
             }
         }
-        lt_wait_st();
     }
-    ok = __syncthreads_and(ok);
+    if (ok) ok = __syncthreads_and(ok);
     if (ok) {
         if (STATE) {
+            if (tid == 128) p.part_dec[(int64_t)item * p.nseg + seg + 1] = lt_ex2(dec_total.hi);
             store_state(part0 + (int64_t)(seg + 1) * DK * 128, 128);
-            if (tid == 0) p.part_dec[(int64_t)item * p.nseg + seg + 1] = lt_ex2((float)dec_total);
         } else if (t_end == len) {
             store_state(st, p.dv);
         }
-    } else {  // products that did not complete in time get one more bounded wait
+    } else {  // copies and products that did not complete in time get one more bounded wait
         if (tid == 0) atomicOr(p.status, (uint32_t)kDevWaitTimeout);
-        mbar_wait_bounded(bar1, last1);
-        mbar_wait_bounded(bar2, last2);
+        mbar_wait_bounded(bar_full, buf);
+        mbar_wait_bounded(bar_ds, buf ^ 1);
+        if (!STATE) mbar_wait_bounded(bar_o2, buf ^ 1);
     }
-    cp_async_commit();
-    cp_async_wait_all();
     tc_fence_before();
     __syncthreads();
     if (warp == 0) {
@@ -464,12 +525,50 @@ int lin_tc_segments(const LinArgs &a, int *seg_len) {
     return (pieces + per - 1) / per;
 }
 
+// cuTensorMapEncodeTiled through the runtime (libdamp does not link the driver library)
+using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                 const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+cudaError_t encode_tiled(EncodeTiled *out) {
+    static std::atomic<EncodeTiled> cached{nullptr};
+    EncodeTiled f = cached.load(std::memory_order_acquire);
+    if (!f) {
+        void *ptr = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &ptr, 12000, cudaEnableDefault, &found);
+        if (e != cudaSuccess) return e;
+        if (found != cudaDriverEntryPointSuccess || !ptr) return cudaErrorNotSupported;
+        f = reinterpret_cast<EncodeTiled>(ptr);
+        cached.store(f, std::memory_order_release);
+    }
+    *out = f;
+    return cudaSuccess;
+}
+// boxes of 64 channels x 64 tokens of one head and batch row; tokens past T read as zeros
+cudaError_t lin_tc_map(CUtensorMap *map, const void *base, int channels, int heads, int T, int batch) {
+    EncodeTiled encode;
+    const cudaError_t e = encode_tiled(&encode);
+    if (e != cudaSuccess) return e;
+    const cuuint64_t dims[4] = {(cuuint64_t)channels, (cuuint64_t)heads, (cuuint64_t)T, (cuuint64_t)batch};
+    const cuuint64_t row = (cuuint64_t)channels * 2;
+    const cuuint64_t strides[3] = {row, row * (cuuint64_t)heads, row * (cuuint64_t)heads * (cuuint64_t)T};
+    const cuuint32_t box[4] = {64, 1, kLtC, 1}, steps[4] = {1, 1, 1, 1};
+    const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(base), dims, strides, box, steps,
+                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+struct LinTcMaps {
+    CUtensorMap q, k, v;
+};
+
 template <int DK, bool STATE>
-cudaError_t lin_tc_launch(const LinTcParams &p, int64_t ctas, cudaStream_t s) {
+cudaError_t lin_tc_launch(const LinTcParams &p, const LinTcMaps &m, int64_t ctas, cudaStream_t s) {
     const void *const kern = reinterpret_cast<const void *>(lin_tc_kernel<DK, STATE>);
     const cudaError_t e = ensure_smem_limit(kern, LtSmem<DK>::bytes);
     if (e != cudaSuccess) return e;
-    lin_tc_kernel<DK, STATE><<<(unsigned)ctas, kLtThreads, LtSmem<DK>::bytes, s>>>(p);
+    lin_tc_kernel<DK, STATE><<<(unsigned)ctas, kLtThreads, LtSmem<DK>::bytes, s>>>(p, m.q, m.k, m.v);
     return cudaGetLastError();
 }
 
@@ -496,9 +595,10 @@ cudaError_t launch_lin_tc(LinArgs a, void *workspace, cudaStream_t s) {
     p.num_slots = a.num_slots;
     p.slot_idx = a.slot_idx;
     p.lengths = a.lengths;
-    p.q = static_cast<const uint8_t *>(a.q);
-    p.k = static_cast<const uint8_t *>(a.k);
-    p.v = static_cast<const uint8_t *>(a.v);
+    LinTcMaps m;
+    if ((e = lin_tc_map(&m.q, a.q, a.dk, a.Hqk, a.T, a.batch)) != cudaSuccess) return e;
+    if ((e = lin_tc_map(&m.k, a.k, a.dk, a.Hqk, a.T, a.batch)) != cudaSuccess) return e;
+    if ((e = lin_tc_map(&m.v, a.v, a.dv, a.H, a.T, a.batch)) != cudaSuccess) return e;
     p.g = a.g;
     p.o = a.o;
     p.H = a.H;
@@ -512,10 +612,10 @@ cudaError_t launch_lin_tc(LinArgs a, void *workspace, cudaStream_t s) {
     if (p.nseg > 1) {
         p.part = static_cast<float *>(workspace);
         p.part_dec = p.part + items * p.nseg * a.dk * 128;
-        e = a.dk == 64 ? lin_tc_launch<64, true>(p, items * (p.nseg - 1), s) : lin_tc_launch<128, true>(p, items * (p.nseg - 1), s);
+        e = a.dk == 64 ? lin_tc_launch<64, true>(p, m, items * (p.nseg - 1), s) : lin_tc_launch<128, true>(p, m, items * (p.nseg - 1), s);
         if (e != cudaSuccess) return e;
     }
-    return a.dk == 64 ? lin_tc_launch<64, false>(p, items * p.nseg, s) : lin_tc_launch<128, false>(p, items * p.nseg, s);
+    return a.dk == 64 ? lin_tc_launch<64, false>(p, m, items * p.nseg, s) : lin_tc_launch<128, false>(p, m, items * p.nseg, s);
 }
 
 cudaError_t take_status_lin_tc(uint32_t *bits) {
