@@ -232,18 +232,16 @@ __global__ void __launch_bounds__(kLtThreads, 2)
     const int64_t gstep = p.g_per_head ? 0 : p.H;
     float ga = 0.f, gb = 0.f;
     Pair dec_total{0.f, 0.f};  // base-2 log of the segment's decay
-    auto gate = [&](int t) -> float {
-        if (t >= t_end) return 0.f;
-        const float x = g0[(int64_t)t * gstep];
-        return x < -200.f ? -200.f : x;  // e^-200 is 0 in FP32 (-inf: a reset)
-    };
-    auto fetch_gates = [&](int t) {
-        ga = gate(t + 2 * lane);
-        gb = gate(t + 2 * lane + 1);
+    auto fetch_gates = [&](int t) {  // used a piece later
+        t += 2 * lane;
+        ga = t < t_end ? g0[(int64_t)t * gstep] : 0.f;
+        gb = t + 1 < t_end ? g0[(int64_t)(t + 1) * gstep] : 0.f;
     };
     auto sum_gates = [&](int buf) {
         constexpr float kLog2eF = 1.4426950408889634f;
-        const Pair x0{ga * kLog2eF, 0.f}, x1{gb * kLog2eF, 0.f}, own = add_pair(x0, x1);
+        // below -200, e^g is 0 in FP32 (-inf: a reset)
+        const Pair x0{(ga < -200.f ? -200.f : ga) * kLog2eF, 0.f}, x1{(gb < -200.f ? -200.f : gb) * kLog2eF, 0.f},
+            own = add_pair(x0, x1);
         Pair x = own;
 #pragma unroll
         for (int m = 1; m < 32; m <<= 1) {
@@ -382,11 +380,11 @@ __global__ void __launch_bounds__(kLtThreads, 2)
                 if (more) copy_v(t0 + kLtC, buf ^ 1);
             }
             __syncwarp();
-            if (more) {
-                sum_gates(buf ^ 1);
-                fetch_gates(t0 + 2 * kLtC);
-            }
             if (!STATE) {
+                if (more) {
+                    sum_gates(buf ^ 1);
+                    fetch_gates(t0 + 2 * kLtC);
+                }
                 issue_add();
                 ok &= mbar_wait_bounded(bar_p, buf);
                 tc_fence_after();
@@ -411,7 +409,7 @@ __global__ void __launch_bounds__(kLtThreads, 2)
             const uint32_t gj = sg + 8 * kt, gC = sg + 8 * 63;
             const float2 f = splat2(lt_ex2((ldsf(gC) - ldsf(gj)) + (ldsf(gC + 4) - ldsf(gj + 4))));
             const uint32_t cell = (uint32_t)((kt >> 3) * CELLS * 128 + (kt & 7) * 16 + c0 * 128);
-#pragma unroll 2
+#pragma unroll 4
             for (int i = 0; i < NC; ++i) {
                 const uint32_t off = cell + (uint32_t)(i * 128);
                 uint4 w4 = lds128(sb + M::k + (uint32_t)(2 * kLtBox * ((c0 + i) >> 3) + kt * 128 + (((c0 + i) ^ kt) & 7) * 16));
@@ -459,7 +457,13 @@ __global__ void __launch_bounds__(kLtThreads, 2)
             fence_proxy_async_smem();
             mbar_arrive(bar_p);
         }
-        if (STATE && issuer) issue_add();
+        if (STATE && issuer) {
+            issue_add();
+            if (more) {
+                sum_gates(buf ^ 1);
+                fetch_gates(t0 + 2 * kLtC);
+            }
+        }
         const float2 eC = splat2(ldsf(sg + 512 + 4 * 63));
         ok &= mbar_wait_bounded(bar_ds, buf);
         tc_fence_after();
@@ -474,19 +478,21 @@ __global__ void __launch_bounds__(kLtThreads, 2)
             if (more) store_parts();
             ok &= mbar_wait_bounded(bar_o2, buf);
             tc_fence_after();
-            float *oc = o + (int64_t)(t0 + 32 * half) * ostep;
+            float *const oc = o + (int64_t)(t0 + 32 * half) * ostep;
             const int nh = n - 32 * half;
-#pragma unroll 1
-            for (int j0 = 0; j0 < 32 && j0 < nh; j0 += 8) {
+#pragma unroll
+            for (int j0 = 0; j0 < 32; j0 += 8) {
+                if (j0 >= nh) break;
                 float o1[8], o2[8];
                 lt_ld8x2(tl + kLtO1 + 32 * half + j0, tl + kLtG + 32 * half + j0, o1, o2);
+                float *oj = oc + j0 * ostep;
 #pragma unroll
                 for (int e = 0; e < 8; e += 4) {
                     const uint4 eg = lds128(sg + 512 + 4 * (32 * half + j0 + e));
                     const float ev[4] = {__uint_as_float(eg.x), __uint_as_float(eg.y), __uint_as_float(eg.z), __uint_as_float(eg.w)};
 #pragma unroll
-                    for (int i = 0; i < 4; ++i, oc += ostep)
-                        if (j0 + e + i < nh) *oc = fmaf(ev[i], o1[e + i], o2[e + i]);
+                    for (int i = 0; i < 4; ++i, oj += ostep)
+                        if (j0 + e + i < nh) *oj = fmaf(ev[i], o1[e + i], o2[e + i]);
                 }
             }
         }
