@@ -312,8 +312,8 @@ damp_status lin(const damp_layout *L, float *state, int64_t num_slots, const int
     a.in_bf16 = in_dtype == DAMP_IN_BF16;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (step) return launch_lin_step(a, s) == cudaSuccess ? DAMP_OK : DAMP_ERR_CUDA;
-    if (!lin_tc_takes(a)) return launch_lin_chunk(a, s) == cudaSuccess ? DAMP_OK : DAMP_ERR_CUDA;
-    const int64_t need = (int64_t)lin_tc_workspace(a);
+    const bool tc = lin_tc_takes(a);
+    const int64_t need = (int64_t)(tc ? lin_tc_workspace(a) : lin_chunk_workspace(a));
     if (need) {
         if (!workspace) return DAMP_ERR_NULL;
         if (workspace_bytes < need) return DAMP_ERR_SHAPE;
@@ -323,7 +323,7 @@ damp_status lin(const damp_layout *L, float *state, int64_t num_slots, const int
         for (const Range &r : inputs)
             if (overlap(rw, r)) return DAMP_ERR_ALIAS;
     }
-    return launch_lin_tc(a, workspace, s) == cudaSuccess ? DAMP_OK : DAMP_ERR_CUDA;
+    return (tc ? launch_lin_tc(a, workspace, s) : launch_lin_chunk(a, workspace, s)) == cudaSuccess ? DAMP_OK : DAMP_ERR_CUDA;
 }
 
 // Whole slots of several pools.  Entries src (live slots of a compaction) and dst; launches
@@ -635,7 +635,7 @@ int64_t damp_lin_prefill_workspace(const damp_layout *layout, int32_t batch, int
     a.batch = batch;
     a.T = chunk_len;
     a.in_bf16 = in_dtype == DAMP_IN_BF16;
-    return (int64_t)lin_tc_workspace(a);
+    return (int64_t)(lin_tc_takes(a) ? lin_tc_workspace(a) : lin_chunk_workspace(a));
 }
 
 damp_status damp_copy_slots(void *const *pools, const int64_t *slot_bytes, int32_t n_pools, int64_t num_slots,

@@ -111,7 +111,8 @@ cudaError_t launch_quad_rowabs_gdn(const StepArgs &a, cudaStream_t s);
 cudaError_t launch_quad_rowabs_kda(const StepArgs &a, cudaStream_t s);
 cudaError_t launch_fp32_step(const StepArgs &a, cudaStream_t s);
 cudaError_t launch_lin_step(LinArgs a, cudaStream_t s);
-cudaError_t launch_lin_chunk(LinArgs a, cudaStream_t s);
+cudaError_t launch_lin_chunk(LinArgs a, void *workspace, cudaStream_t s);
+size_t lin_chunk_workspace(const LinArgs &a);  // bytes
 bool lin_tc_takes(const LinArgs &a);        // the chunk runs on the tensor cores
 size_t lin_tc_workspace(const LinArgs &a);  // bytes
 cudaError_t launch_lin_tc(LinArgs a, void *workspace, cudaStream_t s);

@@ -8,12 +8,18 @@
 // thread in flight at once; the column sums of o go over the rows of the CTA through
 // shared memory.  Bound by the state's bytes (read + write).
 //
-// Chunk (any type, any supported size).  A lane owns one value column for all d_k rows
-// in registers, so both the update and o_t = S_t^T q_t are thread-local; k and q of
-// kRecTok tokens at a time are staged in shared memory and read as broadcasts.  Bound by
-// the FP32 pipe: 3 d_k operations per token and column.
+// Chunk (any type, any supported size).  The same tile per CTA, held in registers over the
+// tokens; k, q and v of kGroup tokens are staged in shared memory one group ahead, a thread
+// sums its rows' share of the kGroup outputs, and the shares are joined over the rows once
+// per group.  Up to about 16 tokens the state's bytes bound it, beyond that the FP32 pipe
+// (three operations per state value and token).  Few (slot, head) pairs and many tokens: the
+// tokens are split into segments; a first launch computes what each segment adds to the
+// state, a second one starts every segment from the joined state before it (twice the work,
+// so from three segments on).
 #include "damp_common.cuh"
 #include "damp_internal.h"
+
+#include <algorithm>
 
 namespace damp {
 
@@ -96,83 +102,214 @@ __global__ void __launch_bounds__(256) lin_step_kernel(const LinArgs p) {
     }
 }
 
-constexpr int kRecTok = 16;   // tokens staged at a time
-constexpr int kRecWarps = 4;  // value blocks of 32 columns per CTA
+constexpr int kGroup = 8;  // tokens staged at a time
 
-template <int DK, bool BF16>
-__global__ void __launch_bounds__(32 * kRecWarps) lin_chunk_kernel(const LinArgs p) {
-    __shared__ __align__(16) float sk[kRecTok][DK], sq[kRecTok][DK];
-    __shared__ float sa[kRecTok];
-    const int V = p.dv / 32;
-    const int nc = (V + kRecWarps - 1) / kRecWarps;
-    const int c = blockIdx.x % nc;
-    const int h = (blockIdx.x / nc) % p.H;
-    const int b = blockIdx.x / nc / p.H;
+// STATE: only what the segment adds to the state and its decay.  Parts of a split row: 0 the state
+// before it (the last segment overwrites the pool's while others may still start), 1 the state after
+// segment 0, s what segment s - 1 adds.
+template <int DK, int CW, bool BF16, bool STATE>
+__global__ void __launch_bounds__(256, 2) lin_chunk_kernel(const LinArgs p, int nseg, int seg_len, float *part, float *part_dec) {
+    constexpr int TPR = CW / 4;     // threads per state row
+    constexpr int RPI = 256 / TPR;  // row groups of the CTA
+    constexpr int R = DK / RPI;     // consecutive rows of a thread (RPI is at most 32)
+    // one buffer of operands: the barrier before the shares are joined also ends their use (the state
+    // alone joins nothing and has two)
+    constexpr int NB = STATE ? 2 : 1;
+    __shared__ __align__(16) float sk[NB][kGroup][DK], sq[STATE ? 1 : NB][kGroup][DK], sv[NB][kGroup][CW];
+    __shared__ float sa[NB][kGroup];
+    __shared__ __align__(16) float share[STATE ? 1 : 8][kGroup][CW];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int segs = STATE ? nseg - 1 : nseg;
+    const int seg = (int)(blockIdx.x % segs), nc = p.dv / CW;
+    const int64_t item = blockIdx.x / segs;
+    const int c = (int)(item % nc), h = (int)(item / nc % p.H), b = (int)(item / nc / p.H);
     const int64_t slot = p.slot_idx ? (int64_t)p.slot_idx[b] : (int64_t)b;
     if (slot < 0 || slot >= p.num_slots) {
-        if (threadIdx.x == 0) atomicOr(p.status, (uint32_t)kDevBadSlot);
+        if (tid == 0) atomicOr(p.status, (uint32_t)kDevBadSlot);
         return;
     }
-    const int T = p.T;
-    const int len = p.lengths ? min(max(p.lengths[b], 0), T) : T;
-    const int lane = threadIdx.x & 31, vb = c * kRecWarps + (threadIdx.x >> 5);
-    const bool on = vb < V;
-    const int hq = (h * p.Hqk) / p.H;
-    const int col = vb * 32 + lane;
-    float *const S = p.state + (slot * p.H + h) * DK * (int64_t)p.dv + col;
-    float *const o = p.o + ((int64_t)b * T * p.H + h) * p.dv + col;
+    const int T = p.T, len = p.lengths ? min(max(p.lengths[b], 0), T) : T;
+    const int t_begin = seg * seg_len, t_stop = min(t_begin + seg_len, T), t_end = min(t_stop, len);
     const int64_t ostep = (int64_t)p.H * p.dv;
-    float2 x[DK / 2];
-    if (on && len > 0) {
-#pragma unroll
-        for (int u = 0; u < DK / 2; ++u) x[u] = make_float2(S[(2 * u) * (int64_t)p.dv], S[(2 * u + 1) * (int64_t)p.dv]);
+    float *const o = p.o + ((int64_t)b * T * p.H + h) * p.dv + c * CW;
+    if (!STATE) {  // rows past the length
+        for (int i = tid; i < (t_stop - max(len, t_begin)) * CW; i += 256)
+            o[(int64_t)(max(len, t_begin) + i / CW) * ostep + i % CW] = 0.f;
     }
-    for (int t0 = 0; t0 < len; t0 += kRecTok) {
-        const int n = min(kRecTok, len - t0);
-        __syncthreads();
-        for (int i = threadIdx.x; i < n * DK / 4; i += 32 * kRecWarps) {
-            const int t = i / (DK / 4), u = 4 * (i % (DK / 4));
-            const int64_t off = (((int64_t)b * T + t0 + t) * p.Hqk + hq) * DK + u;
-            *reinterpret_cast<float4 *>(&sk[t][u]) = load_in4<BF16>(p.k, off);
-            *reinterpret_cast<float4 *>(&sq[t][u]) = load_in4<BF16>(p.q, off);
+    if (t_begin >= len) return;
+    if (STATE && t_end == len) return;  // no live segment follows
+    const bool vec_o = (reinterpret_cast<uintptr_t>(p.o) & 15) == 0;
+
+    const int col = 4 * (tid % TPR), row0 = R * (tid / TPR);
+    float4 *const S = reinterpret_cast<float4 *>(p.state + ((slot * p.H + h) * DK + row0) * p.dv + c * CW + col);
+    float *const parts = part + item * nseg * DK * CW + row0 * CW + col;
+    float2 x[R][2];
+    auto load_state = [&](const float4 *src, int64_t ld) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const float4 y = src[r * ld];
+            x[r][0] = make_float2(y.x, y.y);
+            x[r][1] = make_float2(y.z, y.w);
         }
-        if ((int)threadIdx.x < n)
-            sa[threadIdx.x] = expf(lin_gate(p.g[p.g_per_head ? h : ((int64_t)b * T + t0 + threadIdx.x) * p.H + h]));
-        __syncthreads();
-        if (!on) continue;
-        float vn[kRecTok];
+    };
+    auto store_state = [&](float4 *dst, int64_t ld) {
 #pragma unroll
-        for (int t = 0; t < kRecTok; ++t)
-            vn[t] = t < n ? load_in(p.v, (((int64_t)b * T + t0 + t) * p.H + h) * p.dv + col, BF16) : 0.f;
-#pragma unroll 1
-        for (int t = 0; t < n; ++t) {
-            float vt = 0.f;
+        for (int r = 0; r < R; ++r) dst[r * ld] = make_float4(x[r][0].x, x[r][0].y, x[r][1].x, x[r][1].y);
+    };
+    auto part_of = [&](int s) { return reinterpret_cast<float4 *>(parts + (int64_t)s * DK * CW); };
+
+    // the next group's operands, in registers: a float4 of q, of k and of v per thread
+    const int hq = (int)((int64_t)h * p.Hqk / p.H);
+    const int qt = tid / (DK / 4), qu = 4 * (tid % (DK / 4)), vt = tid / TPR;
+    const int64_t qoff = (((int64_t)b * T + qt) * p.Hqk + hq) * DK + qu;
+    const int64_t voff = (((int64_t)b * T + vt) * p.H + h) * p.dv + c * CW + col;
+    float4 nk, nq, nv;
+    float na = 1.f;
+    auto fetch = [&](int t0) {
+        nk = nq = nv = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (qt < kGroup && t0 + qt < t_end) {
+            nk = load_in4<BF16>(p.k, qoff + (int64_t)t0 * p.Hqk * DK);
+            if (!STATE) nq = load_in4<BF16>(p.q, qoff + (int64_t)t0 * p.Hqk * DK);
+        }
+        if (vt < kGroup && t0 + vt < t_end) nv = load_in4<BF16>(p.v, voff + (int64_t)t0 * ostep);
+        if (tid < kGroup)
+            na = t0 + tid < t_end ? p.g[p.g_per_head ? h : ((int64_t)b * T + t0 + tid) * p.H + h] : 0.f;
+    };
+    fetch(t_begin);
+    if (STATE && seg > 0) {
 #pragma unroll
-            for (int i = 0; i < kRecTok; ++i) vt = i == t ? vn[i] : vt;
-            const float2 v2 = splat2(vt), a2 = splat2(sa[t]);
-            float2 s0 = splat2(0.f), s1 = s0;
+        for (int r = 0; r < R; ++r) x[r][0] = x[r][1] = make_float2(0.f, 0.f);
+    } else if (STATE || (seg == 0 && t_end == len)) {
+        load_state(S, p.dv / 4);
+        if (STATE) store_state(part_of(0), CW / 4);
+    } else {
+        load_state(part_of(seg > 0), CW / 4);
+        for (int s = 2; s <= seg; ++s) {
+            const float2 d = splat2(part_dec[item * nseg + s]);
+            const float4 *const src = part_of(s);
 #pragma unroll
-            for (int u = 0; u < DK / 2; u += 2) {
-                const float4 k4 = *reinterpret_cast<const float4 *>(&sk[t][2 * u]);
-                const float4 q4 = *reinterpret_cast<const float4 *>(&sq[t][2 * u]);
-                x[u] = fma2(x[u], a2, mul2(make_float2(k4.x, k4.y), v2));
-                x[u + 1] = fma2(x[u + 1], a2, mul2(make_float2(k4.z, k4.w), v2));
-                s0 = fma2(x[u], make_float2(q4.x, q4.y), s0);
-                s1 = fma2(x[u + 1], make_float2(q4.z, q4.w), s1);
+            for (int r = 0; r < R; ++r) {
+                const float4 y = src[r * (CW / 4)];
+                x[r][0] = fma2(x[r][0], d, make_float2(y.x, y.y));
+                x[r][1] = fma2(x[r][1], d, make_float2(y.z, y.w));
             }
-            const float2 s = add2(s0, s1);
-            o[(int64_t)(t0 + t) * ostep] = s.x + s.y;
         }
     }
-    if (!on) return;
-    if (len > 0) {
+    float decay = 1.f;
+    int buf = 0;
+#pragma unroll 1
+    for (int t0 = t_begin; t0 < t_end; t0 += kGroup, buf ^= NB - 1) {
+        if (qt < kGroup) {
+            *reinterpret_cast<float4 *>(&sk[buf][qt][qu]) = nk;
+            if (!STATE) *reinterpret_cast<float4 *>(&sq[buf][qt][qu]) = nq;
+        }
+        if (vt < kGroup) *reinterpret_cast<float4 *>(&sv[buf][vt][col]) = nv;
+        if (tid < kGroup) sa[buf][tid] = expf(lin_gate(na));
+        __syncthreads();
+        if (t0 + kGroup < t_end) fetch(t0 + kGroup);
+        const int n = min(kGroup, t_end - t0);
+        float2 acc[STATE ? 1 : kGroup][2];
 #pragma unroll
-        for (int u = 0; u < DK / 2; ++u) {
-            S[(2 * u) * (int64_t)p.dv] = x[u].x;
-            S[(2 * u + 1) * (int64_t)p.dv] = x[u].y;
+        for (int t = 0; t < kGroup; ++t) {
+            if (t < n) {
+                const float a1 = sa[buf][t];
+                const float2 a = splat2(a1);
+                if (STATE) decay *= a1;
+                const float4 v4 = *reinterpret_cast<const float4 *>(&sv[buf][t][col]);
+                const float2 v0 = make_float2(v4.x, v4.y), v1 = make_float2(v4.z, v4.w);
+                float2 o0 = make_float2(0.f, 0.f), o1 = o0;
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const float2 k = splat2(sk[buf][t][row0 + r]);
+                    x[r][0] = fma2(x[r][0], a, mul2(k, v0));
+                    x[r][1] = fma2(x[r][1], a, mul2(k, v1));
+                    if (!STATE) {
+                        const float2 q = splat2(sq[buf][t][row0 + r]);
+                        o0 = fma2(x[r][0], q, o0);
+                        o1 = fma2(x[r][1], q, o1);
+                    }
+                }
+                if (!STATE) {
+                    acc[t][0] = o0;
+                    acc[t][1] = o1;
+                }
+            }
+        }
+        if (!STATE) {
+#pragma unroll
+            for (int t = 0; t < kGroup; ++t) {
+                if (t < n) {
+                    float4 y = make_float4(acc[t][0].x, acc[t][0].y, acc[t][1].x, acc[t][1].y);
+#pragma unroll
+                    for (int m = 16; m >= TPR; m >>= 1) {  // rows of the same warp
+                        y.x += __shfl_xor_sync(kFull, y.x, m);
+                        y.y += __shfl_xor_sync(kFull, y.y, m);
+                        y.z += __shfl_xor_sync(kFull, y.z, m);
+                        y.w += __shfl_xor_sync(kFull, y.w, m);
+                    }
+                    if (lane < TPR) *reinterpret_cast<float4 *>(&share[warp][t][col]) = y;
+                }
+            }
+            __syncthreads();
+            if (vt < n) {  // token vt, columns col .. col + 3
+                float4 y = *reinterpret_cast<const float4 *>(&share[0][vt][col]);
+#pragma unroll
+                for (int w = 1; w < 8; ++w) {
+                    const float4 z = *reinterpret_cast<const float4 *>(&share[w][vt][col]);
+                    y = make_float4(y.x + z.x, y.y + z.y, y.z + z.z, y.w + z.w);
+                }
+                float *const dst = o + (int64_t)(t0 + vt) * ostep + col;
+                if (vec_o) {
+                    *reinterpret_cast<float4 *>(dst) = y;
+                } else {
+                    dst[0] = y.x;
+                    dst[1] = y.y;
+                    dst[2] = y.z;
+                    dst[3] = y.w;
+                }
+            }
         }
     }
-    for (int t = len; t < T; ++t) o[(int64_t)t * ostep] = 0.f;
+    if (STATE) {
+        store_state(part_of(seg + 1), CW / 4);
+        if (tid == 0) part_dec[item * nseg + seg + 1] = decay;
+    } else if (t_end == len) {
+        store_state(S, p.dv / 4);
+    }
+}
+
+static int lin_chunk_columns(const LinArgs &p) { return p.dv % 128 == 0 ? 128 : p.dv % 64 == 0 ? 64 : 32; }
+
+// segments (1: no split) and the tokens of each
+static int lin_chunk_segments(const LinArgs &p, int *seg_len) {
+    const int64_t items = (int64_t)p.batch * p.H * (p.dv / lin_chunk_columns(p));
+    int64_t nseg = std::min<int64_t>(2 * (int64_t)sm_count() / std::max<int64_t>(items, 1), p.T / 64);
+    if (nseg < 3) nseg = 1;
+    *seg_len = (int)((p.T + nseg * kGroup - 1) / (nseg * kGroup)) * kGroup;
+    return (p.T + *seg_len - 1) / *seg_len;
+}
+
+size_t lin_chunk_workspace(const LinArgs &p) {
+    int seg_len;
+    const int cw = lin_chunk_columns(p), nseg = lin_chunk_segments(p, &seg_len);
+    return nseg > 1 ? (size_t)p.batch * p.H * (p.dv / cw) * nseg * (p.dk * cw + 1) * 4 : 0;
+}
+
+template <int DK, int CW, bool BF16>
+static void lin_chunk_run(const LinArgs &p, void *workspace, cudaStream_t s) {
+    int seg_len;
+    const int nseg = lin_chunk_segments(p, &seg_len);
+    const int64_t items = (int64_t)p.batch * p.H * (p.dv / CW);
+    float *const part = static_cast<float *>(workspace), *const dec = part + (nseg > 1 ? items * nseg * DK * CW : 0);
+    if (nseg > 1) lin_chunk_kernel<DK, CW, BF16, true><<<(unsigned)(items * (nseg - 1)), 256, 0, s>>>(p, nseg, seg_len, part, dec);
+    lin_chunk_kernel<DK, CW, BF16, false><<<(unsigned)(items * nseg), 256, 0, s>>>(p, nseg, seg_len, part, dec);
+}
+template <int DK, bool BF16>
+static void lin_chunk_pick(const LinArgs &p, void *workspace, cudaStream_t s) {
+    const int cw = lin_chunk_columns(p);
+    if (cw == 128) lin_chunk_run<DK, 128, BF16>(p, workspace, s);
+    else if (cw == 64) lin_chunk_run<DK, 64, BF16>(p, workspace, s);
+    else lin_chunk_run<DK, 32, BF16>(p, workspace, s);
 }
 
 template <int DK, bool BF16>
@@ -197,15 +334,12 @@ cudaError_t launch_lin_step(LinArgs p, cudaStream_t s) {
     return cudaGetLastError();
 }
 
-cudaError_t launch_lin_chunk(LinArgs p, cudaStream_t s) {
+cudaError_t launch_lin_chunk(LinArgs p, void *workspace, cudaStream_t s) {
     const cudaError_t e = lin_status_word(p);
     if (e != cudaSuccess) return e;
-    const int V = p.dv / 32;
-    const unsigned grid = (unsigned)((int64_t)p.batch * p.H * ((V + kRecWarps - 1) / kRecWarps));
-    const unsigned block = 32 * kRecWarps;
-    if (p.dk == 32) p.in_bf16 ? lin_chunk_kernel<32, true><<<grid, block, 0, s>>>(p) : lin_chunk_kernel<32, false><<<grid, block, 0, s>>>(p);
-    else if (p.dk == 64) p.in_bf16 ? lin_chunk_kernel<64, true><<<grid, block, 0, s>>>(p) : lin_chunk_kernel<64, false><<<grid, block, 0, s>>>(p);
-    else p.in_bf16 ? lin_chunk_kernel<128, true><<<grid, block, 0, s>>>(p) : lin_chunk_kernel<128, false><<<grid, block, 0, s>>>(p);
+    if (p.dk == 32) p.in_bf16 ? lin_chunk_pick<32, true>(p, workspace, s) : lin_chunk_pick<32, false>(p, workspace, s);
+    else if (p.dk == 64) p.in_bf16 ? lin_chunk_pick<64, true>(p, workspace, s) : lin_chunk_pick<64, false>(p, workspace, s);
+    else p.in_bf16 ? lin_chunk_pick<128, true>(p, workspace, s) : lin_chunk_pick<128, false>(p, workspace, s);
     return cudaGetLastError();
 }
 

@@ -581,11 +581,10 @@ cudaError_t lin_tc_launch(const LinTcParams &p, const LinTcMaps &m, int64_t ctas
 }  // namespace
 
 bool lin_tc_takes(const LinArgs &a) {
-    return a.in_bf16 && (a.dk == 64 || a.dk == 128) && a.dv % 128 == 0 && a.T >= 32;
+    return a.in_bf16 && (a.dk == 64 || a.dk == 128) && a.dv % 128 == 0 && a.T > 16;
 }
 
 size_t lin_tc_workspace(const LinArgs &a) {
-    if (!lin_tc_takes(a)) return 0;
     int seg_len;
     const int64_t nseg = lin_tc_segments(a, &seg_len);
     const int64_t parts = nseg > 1 ? (int64_t)a.batch * a.H * (a.dv / 128) * nseg : 0;

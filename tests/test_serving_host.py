@@ -74,7 +74,7 @@ def test_lin_rejects_bad_arguments(L, fb):
         assert call(True, lay=lay, T=T, batch=1, ws=_p(fb, 6, 4), ws_bytes=need) == ALIGN
         assert call(True, lay=lay, T=T, batch=1, ws=_p(fb, 5, 64), ws_bytes=need) == ALIAS
     assert L.damp_lin_prefill_workspace(ctypes.byref(c), 0, T, 0) == 0
-    assert L.damp_lin_prefill_workspace(ctypes.byref(c), 1, T, 1) == 0
+    assert L.damp_lin_prefill_workspace(ctypes.byref(c), 1, 5, 0) == 0
     assert L.damp_lin_prefill_workspace(None, 1, T, 0) == 0
 
 
