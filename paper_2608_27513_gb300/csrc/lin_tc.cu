@@ -9,20 +9,22 @@
 //     S_0^T Q^T           -> O1 (A from tensor memory)
 //     V^T (K~ = e^{G_C - G_j} k_j)    -> what the piece adds to S^T
 //     V^T P^T, P = (e^{G_i - G_j} q_i.k_j)_{j<=i}  -> O2;  o_i = O2_i + e^{G_i} O1_i
-// One CTA owns 128 value columns of a (slot, head).  The state stays in registers in FP32
-// (thread = value column and half the key channels); only its operand copy is rounded.
+// One CTA per SM walks over items of 128 value columns of a (slot, head); an item's state
+// stays in registers in FP32 (thread = value column and half the key channels) and only its
+// operand copy is rounded.
 //
 // Rounding.  q, k and v are bf16 inputs and enter exactly.  The FP32 operands (S_0, K~, P)
-// enter as two bf16 parts hi + lo, which leaves at most 2^-16 of a value (2.4e-6 in the
-// mean): one part alone would leave 2^-8, a third part costs half as much tensor time
-// again and 48 KB.  Accumulation and the state are FP32.  G is summed in FP64 and kept as
-// two floats, so that G_i - G_j keeps its digits where both are large (fast decays).
+// enter as three bf16 parts hi + mid + lo, 24 bits as FP32 has (two parts leave 2.9e-6 of the
+// result instead of 3e-7).  Accumulation and the
+// state are FP32.  G is summed as pairs of floats, so that G_i - G_j keeps its digits where
+// both are large (fast decays).
 //
-// q, k and v come by tensor copies (TMA, 128-byte swizzle), issued as soon as the products that
-// read the tile before are done.  Warp 4, which has no part in P and K~, issues copies and
-// products and sums the next piece's gates meanwhile.  Two CTAs per SM (110 KB of shared memory,
-// 256 of the 512 tensor-memory columns each) overlap one's products with the other's
-// conversions.  Bound by the conversions, with the bytes of q, k, v and o next.
+// Sixteen warps in two groups that meet only at mbarriers.  Warps 0-7 hold the state: they
+// add what a piece adds and write the next operand parts to tensor memory.  Warps 8-15 turn
+// Q K^T into P and k into K~, one piece ahead of the outputs that they combine and store;
+// warp 12, which has no part in P and K~, issues the products, warp 13 the copies (TMA, 128-byte
+// swizzle, three stages) with the sums of the gates.  Bound by the conversions of warps 8-15, with
+// the bytes of q, k, v and o and the tensor time next.
 //
 // Few (slot, head) pairs and many tokens: the tokens are split into segments.  A first
 // launch computes what each segment adds to the state (k and v only), a second one starts
@@ -41,26 +43,29 @@ static __device__ uint32_t g_status_lin_tc;
 namespace {
 
 constexpr int kLtC = 64;
-constexpr int kLtThreads = 256;
+constexpr int kLtThreads = 512;
 constexpr int kLtBox = 64 * 128;  // bytes of a copied box: 64 tokens x 64 bf16
-constexpr uint32_t kLtCols = 256;
-// tensor-memory columns: Q K^T, then O2 | O1 | S_0 as bf16 parts, then what the piece adds
-constexpr uint32_t kLtG = 0, kLtO1 = 64, kLtS = 128;
+constexpr uint32_t kLtCols = 512;
+// tensor-memory columns: Q K^T | O1 | O2 | what the piece adds to S | S_0 as three bf16 parts
+constexpr uint32_t kLtG = 0, kLtO1 = 64, kLtO2 = 128, kLtD = 192, kLtS = 320;
+constexpr int kLtStages = 3;
+constexpr int kLtGates = 4;  // a piece's sums may be read while the copies of the third piece after it start
 
-template <int DK>
+template <int DK, bool STATE>
 struct LtSmem {  // bytes from the base of the dynamic shared memory
     static constexpr int tile = kLtC * DK * 2;
-    static constexpr int vtile = kLtC * 128 * 2;
-    // 64-column boxes: [q box 0][k box 0][q box 1][k box 1], so that [Q; K] is one operand of 128 rows
-    static constexpr int q = 0, k = kLtBox;
-    static constexpr int v = 2 * tile;        // two buffers of two boxes
-    static constexpr int kd = v + 2 * vtile;  // K~ hi, lo
-    static constexpr int p = kd + 2 * tile;   // P hi, lo: columns 0-31 of 64 rows, columns 32-63 of rows 32-63
+    // a stage: 64-column boxes [q box 0][k box 0][q box 1][k box 1], so that [Q; K] is one operand of
+    // 128 rows (the state alone: k boxes only), and two boxes of v
+    static constexpr int q = 0, k = STATE ? 0 : kLtBox, step = STATE ? kLtBox : 2 * kLtBox, v = STATE ? tile : 2 * tile;
+    static constexpr int stage = v + 2 * kLtBox;
+    static constexpr int kdn = STATE ? 2 : 1;     // buffers of K~
+    static constexpr int kd = kLtStages * stage;  // K~, three parts
+    static constexpr int p = kd + kdn * 3 * tile; // P, three parts: columns 0-31 of 64 rows, columns 32-63 of rows 32-63
     static constexpr int ppart = 64 * 64 + 32 * 64;
-    static constexpr int g = p + 2 * ppart;   // two buffers: (hi, lo) of G in base 2, 64 pairs, and e^{G_i}
+    static constexpr int g = p + (STATE ? 0 : 3 * ppart);  // per piece: (hi, lo) of G in base 2, 64 pairs, and e^{G_i}
     static constexpr int gbuf = 512 + 256;
-    static constexpr int bar = g + 2 * gbuf;  // seven mbarriers, the tensor-memory address
-    static constexpr int bytes = bar + 64;
+    static constexpr int bar = g + kLtGates * gbuf;  // mbarriers, the tensor-memory address
+    static constexpr int bytes = bar + 160;
 };
 
 struct LinTcParams {
@@ -72,7 +77,7 @@ struct LinTcParams {
     float *part;      // [batch * H * nc][nseg][DK][128]: states and additions of the segments
     float *part_dec;  // [batch * H * nc][nseg]: the decay of segment s - 1
     int32_t H, Hqk, dv, nc, T, g_per_head;
-    int32_t nseg, seg_len;
+    int32_t nseg, seg_len, items;  // items: with their segments
     uint32_t *status;
 };
 
@@ -105,21 +110,14 @@ __device__ __forceinline__ void lt_ld16(uint32_t taddr, float (&v)[16]) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
 }
-// eight columns at two addresses
-__device__ __forceinline__ void lt_ld8x2(uint32_t ta, uint32_t tb, float (&a)[8], float (&b)[8]) {
-    uint32_t r[8], s[8];
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%16];\n"
-                 "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%8,%9,%10,%11,%12,%13,%14,%15}, [%17];\n"
-                 "tcgen05.wait::ld.sync.aligned;"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-                   "=r"(s[0]), "=r"(s[1]), "=r"(s[2]), "=r"(s[3]), "=r"(s[4]), "=r"(s[5]), "=r"(s[6]), "=r"(s[7])
-                 : "r"(ta), "r"(tb)
+__device__ __forceinline__ void lt_ld8(uint32_t taddr, float (&v)[8]) {
+    uint32_t r[8];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\ntcgen05.wait::ld.sync.aligned;"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(taddr)
                  : "memory");
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        a[i] = __uint_as_float(r[i]);
-        b[i] = __uint_as_float(s[i]);
-    }
+    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]);
 }
 __device__ __forceinline__ void lt_st8(uint32_t taddr, const uint32_t (&r)[8]) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr), "r"(r[0]),
@@ -127,20 +125,49 @@ __device__ __forceinline__ void lt_st8(uint32_t taddr, const uint32_t (&r)[8]) {
                  : "memory");
 }
 __device__ __forceinline__ void lt_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-// A from tensor memory (K-major: two bf16 per column)
-__device__ __forceinline__ void lt_mma_ta(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
-    asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\n"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d),
-                 "r"(a), "l"(b), "r"(idesc), "r"(acc)
+// Products are issued by whole warps in step, one elected lane each: the descriptors then stay in
+// uniform registers (a branch to one lane moves every operand of every product there one by one,
+// 85 clocks per product).
+struct LtDesc {  // a shared-memory descriptor whose low word is the same in all lanes
+    uint32_t lo, hi;
+};
+__device__ __forceinline__ LtDesc lt_uniform(uint64_t d) {
+    return LtDesc{__reduce_max_sync(kFull, (uint32_t)d), __reduce_max_sync(kFull, (uint32_t)(d >> 32))};
+}
+__device__ __forceinline__ LtDesc lt_at(LtDesc d, uint32_t off) { return LtDesc{d.lo + (off >> 4), d.hi}; }  // `off` bytes further
+__device__ __forceinline__ void lt_mma(uint32_t d, LtDesc a, LtDesc b, uint32_t idesc, uint32_t acc) {
+    asm volatile("{\n.reg .pred p, e;\n.reg .b64 da, db;\nelect.sync _|e, 0xffffffff;\nsetp.ne.u32 p, %6, 0;\n"
+                 "mov.b64 da, {%1, %2};\nmov.b64 db, {%3, %4};\n"
+                 "@e tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %5, p;\n}" ::"r"(d),
+                 "r"(a.lo), "r"(a.hi), "r"(b.lo), "r"(b.hi), "r"(idesc), "r"(acc)
                  : "memory");
 }
-// x = hi + lo as bf16 parts, two values per word
-__device__ __forceinline__ void split2_pair(float2 x, uint32_t &h, uint32_t &l) {
-    const __nv_bfloat162 h2 = __floats2bfloat162_rn(x.x, x.y);
-    memcpy(&h, &h2, 4);
-    const float2 r = add2(x, make_float2(-__uint_as_float(h << 16), -__uint_as_float(h & 0xffff0000u)));  // exact
-    const __nv_bfloat162 l2 = __floats2bfloat162_rn(r.x, r.y);
-    memcpy(&l, &l2, 4);
+// A from tensor memory (K-major: two bf16 per column)
+__device__ __forceinline__ void lt_mma_ta(uint32_t d, uint32_t a, LtDesc b, uint32_t idesc, uint32_t acc) {
+    asm volatile("{\n.reg .pred p, e;\n.reg .b64 db;\nelect.sync _|e, 0xffffffff;\nsetp.ne.u32 p, %5, 0;\n"
+                 "mov.b64 db, {%2, %3};\n"
+                 "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %4, p;\n}" ::"r"(d),
+                 "r"(a), "r"(b.lo), "r"(b.hi), "r"(idesc), "r"(acc)
+                 : "memory");
+}
+__device__ __forceinline__ void lt_commit(uint32_t bar) {
+    asm volatile("{\n.reg .pred e;\nelect.sync _|e, 0xffffffff;\n"
+                 "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}" ::"r"(bar)
+                 : "memory");
+}
+
+// x = hi + mid + lo as bf16 parts, two values per word: each part cuts off eight significant bits of
+// what is left, so that the three hold x exactly
+__device__ __forceinline__ void lt_split(float2 x, uint32_t &h, uint32_t &m, uint32_t &l) {
+    auto minus_upper = [](float2 y) {
+        return make_float2(-__uint_as_float(__float_as_uint(y.x) & 0xffff0000u), -__uint_as_float(__float_as_uint(y.y) & 0xffff0000u));
+    };
+    auto uppers = [](float2 y) { return prmt(__float_as_uint(y.x), __float_as_uint(y.y), 0x7632u); };
+    h = uppers(x);
+    x = add2(x, minus_upper(x));
+    m = uppers(x);
+    x = add2(x, minus_upper(x));
+    l = uppers(x);
 }
 
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
@@ -158,359 +185,490 @@ __device__ __forceinline__ Pair add_pair(Pair a, Pair b) {
     return Pair{h, e - (h - s)};
 }
 
+// A piece of work: one segment of one row, head and 128 value columns
+struct LtItem {
+    int b, h, c, seg, len, t_begin, t_end;
+    int64_t slot, index;  // index: of the row, head and columns
+    bool live;            // has tokens (and, for the state alone, a live segment after it)
+};
+
 // STATE: only what the segment adds to the state and its decay
 template <int DK, bool STATE>
-__global__ void __launch_bounds__(kLtThreads, 2)
+__global__ void __launch_bounds__(kLtThreads, 1)
     lin_tc_kernel(const LinTcParams p, const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
                   const __grid_constant__ CUtensorMap vmap) {
     extern __shared__ __align__(1024) uint8_t smem[];
-    using M = LtSmem<DK>;
+    using M = LtSmem<DK, STATE>;
     constexpr int CELLS = DK / 8;
     constexpr int NR = DK / 2;  // state rows of a thread
     constexpr uint32_t kIdG = tc_idesc(64, false, false), kIdO2 = tc_idesc(64, true, false), kIdO2b = tc_idesc(32, true, false),
                        kIdS = tc_idesc(DK, true, true);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const bool issuer = warp == 4;
-    const int row = 32 * (warp & 3) + lane, half = warp >> 2;
+    const int row = 32 * (warp & 3) + lane, half = (warp >> 2) & 1;
     const uint32_t sb = smem_u32(smem);
-    // copies landed; products done: Q K^T, O1, the addition to S, O2; operands written: K~, P
-    const uint32_t bar_full = sb + M::bar, bar_qk = bar_full + 8, bar_o1 = bar_full + 16, bar_ds = bar_full + 24,
-                   bar_o2 = bar_full + 32, bar_kd = bar_full + 40, bar_p = bar_full + 48, s_taddr = bar_full + 56;
-
-    const int seg = (int)(blockIdx.x % (STATE ? p.nseg - 1 : p.nseg));
-    const int item = (int)(blockIdx.x / (STATE ? p.nseg - 1 : p.nseg));
-    const int c = item % p.nc, h = (item / p.nc) % p.H, b = item / p.nc / p.H;
-    const int64_t slot = p.slot_idx ? (int64_t)p.slot_idx[b] : (int64_t)b;
-    if (slot < 0 || slot >= p.num_slots) {
-        if (tid == 0) atomicOr(p.status, (uint32_t)kDevBadSlot);
-        return;
+    // Barriers, one phase per piece (`full` and `free`: per piece of a stage; `ds` and `kd`: two each, of even and odd
+    // pieces, as a phase can be told from the next one only).  Copies landed, and all products of the stage done; products done: Q K^T, O1, the addition to
+    // S, O2; written: K~, P, the parts of S; read: the addition, the outputs.
+    const uint32_t bar_full = sb + M::bar, bar_free = bar_full + 24, bar_qk = bar_full + 48, bar_o1 = bar_qk + 8, bar_ds = bar_qk + 16, bar_o2 = bar_qk + 32,
+                   bar_kd = bar_qk + 40, bar_p = bar_qk + 56, bar_sp = bar_qk + 64, bar_dsr = bar_qk + 72, bar_or = bar_qk + 80,
+                   s_taddr = bar_qk + 88;
+    constexpr int kKdWarps = STATE ? 6 : 4;  // warps 10, 11, 14, 15 (the state alone: all of 8-15 but 12 and 13)
+    if (tid == 0) {
+        for (int i = 0; i < kLtStages; ++i) {
+            mbar_init(bar_full + 8 * i, 1);
+            mbar_init(bar_free + 8 * i, 1);
+        }
+        mbar_init(bar_qk, 1);
+        mbar_init(bar_o1, 1);
+        mbar_init(bar_ds, 1);
+        mbar_init(bar_ds + 8, 1);
+        mbar_init(bar_o2, 1);
+        mbar_init(bar_kd, 32 * kKdWarps);
+        mbar_init(bar_kd + 8, 32 * kKdWarps);
+        mbar_init(bar_p, 96);
+        mbar_init(bar_sp, 256);
+        mbar_init(bar_dsr, 256);
+        mbar_init(bar_or, 32 * 7);  // warps 8-15 but 12
+        fence_mbar_init();
     }
-    const int T = p.T;
-    const int len = p.lengths ? min(max(p.lengths[b], 0), T) : T;
-    const int t_begin = seg * p.seg_len, t_stop = min(t_begin + p.seg_len, T), t_end = min(t_stop, len);
-    const int64_t ostep = (int64_t)p.H * p.dv;
-    float *const o = p.o + ((int64_t)b * T * p.H + h) * p.dv + c * 128 + row;
-    if (!STATE) {  // rows past the length
-        for (int t = max(len, t_begin) + half; t < t_stop; t += 2) o[(int64_t)t * ostep] = 0.f;
-    }
-    if (t_begin >= len) return;
-    if (STATE && t_end == len) return;  // no live segment follows
-
     if (warp == 0) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(s_taddr), "r"(kLtCols)
                      : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
-    constexpr int kKdWarps = STATE ? 8 : 4, kPWarps = 3;
-    if (tid == 0) {
-        mbar_init(bar_full, 1);
-        mbar_init(bar_qk, 1);
-        mbar_init(bar_o1, 1);
-        mbar_init(bar_ds, 1);
-        mbar_init(bar_o2, 1);
-        mbar_init(bar_kd, 32 * kKdWarps);
-        mbar_init(bar_p, 32 * kPWarps);
-        fence_mbar_init();
-    }
-    const int hq = (int)((int64_t)h * p.Hqk / p.H);
-    constexpr int QKBOX = DK / 64;  // boxes of q or k
-    auto copy_qk = [&](int t) {  // one thread
-#pragma unroll
-        for (int j = 0; j < QKBOX; ++j) {
-            if (!STATE) lt_copy_box(sb + M::q + 2 * kLtBox * j, &qmap, 64 * j, hq, t, b, bar_full);
-            lt_copy_box(sb + M::k + 2 * kLtBox * j, &kmap, 64 * j, hq, t, b, bar_full);
-        }
-    };
-    auto copy_v = [&](int t, uint32_t buf) {  // one thread; the bytes of the piece's q and k too
-        mbar_arrive_expect_tx(bar_full, ((STATE ? 1 : 2) * QKBOX + 2) * kLtBox);
-#pragma unroll
-        for (int j = 0; j < 2; ++j) lt_copy_box(sb + M::v + buf * M::vtile + kLtBox * j, &vmap, c * 128 + 64 * j, h, t, b, bar_full);
-    };
-    // Gates of a piece (the issuing warp; lane l holds tokens 2l and 2l + 1): inclusive sums in base 2
-    // as pairs of floats, so that G_i - G_j keeps its digits where both are large.
-    const float *const g0 = p.g_per_head ? p.g + h : p.g + (int64_t)b * T * p.H + h;
-    const int64_t gstep = p.g_per_head ? 0 : p.H;
-    float ga = 0.f, gb = 0.f;
-    Pair dec_total{0.f, 0.f};  // base-2 log of the segment's decay
-    auto fetch_gates = [&](int t) {  // used a piece later
-        t += 2 * lane;
-        ga = t < t_end ? g0[(int64_t)t * gstep] : 0.f;
-        gb = t + 1 < t_end ? g0[(int64_t)(t + 1) * gstep] : 0.f;
-    };
-    auto sum_gates = [&](int buf) {
-        constexpr float kLog2eF = 1.4426950408889634f;
-        // below -200, e^g is 0 in FP32 (-inf: a reset)
-        const Pair x0{(ga < -200.f ? -200.f : ga) * kLog2eF, 0.f}, x1{(gb < -200.f ? -200.f : gb) * kLog2eF, 0.f},
-            own = add_pair(x0, x1);
-        Pair x = own;
-#pragma unroll
-        for (int m = 1; m < 32; m <<= 1) {
-            const Pair y{__shfl_up_sync(kFull, x.hi, m), __shfl_up_sync(kFull, x.lo, m)};
-            if (lane >= m) x = add_pair(x, y);
-        }
-        Pair before{__shfl_up_sync(kFull, x.hi, 1), __shfl_up_sync(kFull, x.lo, 1)};
-        if (lane == 0) before = Pair{0.f, 0.f};
-        const Pair first = add_pair(before, x0);
-        const uint32_t at = sb + M::g + (uint32_t)(buf * M::gbuf);
-        sts128(at + 16 * lane, make_uint4(__float_as_uint(first.hi), __float_as_uint(first.lo), __float_as_uint(x.hi), __float_as_uint(x.lo)));
-        sts32(at + 512 + 8 * lane, __float_as_uint(lt_ex2(first.hi)));
-        sts32(at + 512 + 8 * lane + 4, __float_as_uint(lt_ex2(x.hi)));
-        if (STATE) dec_total = add_pair(dec_total, Pair{__shfl_sync(kFull, x.hi, 31), __shfl_sync(kFull, x.lo, 31)});
-    };
-
-    // the state before the segment, transposed: value column `row`, key channels NR half ..
-    float2 S[NR / 2];
-    float *const st = p.state + ((slot * p.H + h) * DK + NR * half) * (int64_t)p.dv + c * 128 + row;
-    float *const part0 = p.part + ((int64_t)item * p.nseg * DK + NR * half) * 128 + row;
-    const float *const dec0 = p.part_dec + (int64_t)item * p.nseg;
-    auto load_state = [&](const float *src, int64_t ld) {
-#pragma unroll
-        for (int r = 0; r < NR / 2; ++r) S[r] = make_float2(src[(2 * r) * ld], src[(2 * r + 1) * ld]);
-    };
-    auto store_state = [&](float *dst, int64_t ld) {
-#pragma unroll
-        for (int r = 0; r < NR / 2; ++r) {
-            dst[(2 * r) * ld] = S[r].x;
-            dst[(2 * r + 1) * ld] = S[r].y;
-        }
-    };
-    if (issuer) {
-        fetch_gates(t_begin);
-        sum_gates(0);
-        fetch_gates(t_begin + kLtC);
-    }
-    {
-        // Parts of a split row: 0 the state before it (the last segment overwrites the pool's while
-        // others may still start), 1 the state after segment 0, s what segment s - 1 adds.
-        const bool whole = seg == 0 && t_end == len;  // the row is one segment
-        if (STATE && seg > 0) {
-#pragma unroll
-            for (int r = 0; r < NR / 2; ++r) S[r] = make_float2(0.f, 0.f);
-        } else if (STATE || whole) {
-            load_state(st, p.dv);
-            if (STATE) store_state(part0, 128);
-        } else {
-            load_state(part0 + (seg > 0 ? DK * 128 : 0), 128);
-            for (int s = 2; s <= seg; ++s) {
-                const float2 d2 = splat2(dec0[s]);
-                const float *const ps = part0 + (int64_t)s * DK * 128;
-#pragma unroll
-                for (int r = 0; r < NR / 2; ++r) S[r] = fma2(S[r], d2, make_float2(ps[(2 * r) * 128], ps[(2 * r + 1) * 128]));
-            }
-        }
-    }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (tid == 128) {
-        copy_v(t_begin, 0);
-        copy_qk(t_begin);
-    }
     const uint32_t tmem = lds32(s_taddr);
-    const uint32_t tl = tmem + ((uint32_t)(32 * (warp & 3)) << 16);
-    const uint32_t tS = tl + kLtS + (uint32_t)(NR * half);  // this thread's columns of both uses
+    const uint32_t tl = tmem + ((uint32_t)(32 * (warp & 3)) << 16);  // this warp's lanes
 
-    // S as two bf16 parts: the half's hi words, then its lo words
-    auto store_parts = [&]() {
-#pragma unroll
-        for (int r8 = 0; r8 < NR / 16; ++r8) {  // 16 rows
-            uint32_t hw[8], lw[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) split2_pair(S[8 * r8 + i], hw[i], lw[i]);
-            lt_st8(tS + 8 * r8, hw);
-            lt_st8(tS + NR / 2 + 8 * r8, lw);
-        }
-        lt_wait_st();
+    const int T = p.T, segs = STATE ? p.nseg - 1 : p.nseg;
+    auto item_at = [&](int i) {
+        LtItem x;
+        x.seg = i % segs;
+        x.index = i / segs;
+        x.c = (int)(x.index % p.nc);
+        x.h = (int)(x.index / p.nc % p.H);
+        x.b = (int)(x.index / p.nc / p.H);
+        x.slot = p.slot_idx ? (int64_t)p.slot_idx[x.b] : (int64_t)x.b;
+        x.len = p.lengths ? min(max(p.lengths[x.b], 0), T) : T;
+        x.t_begin = x.seg * p.seg_len;
+        x.t_end = min(min(x.t_begin + p.seg_len, T), x.len);
+        x.live = x.slot >= 0 && x.slot < p.num_slots && x.t_begin < x.len && !(STATE && x.t_end == x.len);
+        return x;
     };
-    if (!STATE) store_parts();
-
     bool ok = true;
-    uint32_t buf = 0;  // buffers and the phase of every barrier
-#pragma unroll 1
-    for (int t0 = t_begin; t0 < t_end; t0 += kLtC, buf ^= 1) {
-        const bool more = t0 + kLtC < t_end;
-        const uint32_t vt = sb + M::v + buf * M::vtile, sg = sb + M::g + buf * M::gbuf;
-        ok &= mbar_wait_bounded(bar_full, buf);
-        const int n = t_end - t0;  // tokens of the piece (64 or more: all)
-        if (n < kLtC) {  // v past the row's length may hold anything: zero, as 0 times it has to be
-            for (int i = tid; i < (kLtC - n) * 16; i += kLtThreads)
-                sts128(vt + (uint32_t)((i & 1) * kLtBox + (n + (i >> 4)) * 128 + ((i >> 1) & 7) * 16), make_uint4(0u, 0u, 0u, 0u));
-            fence_proxy_async_smem();
-        }
-        tc_fence_before();
-        ok = __syncthreads_and(ok);
-        tc_fence_after();
-        if (!ok) break;
-        auto issue_add = [&]() {  // what the piece adds to S
-            if (!STATE) ok &= mbar_wait_bounded(bar_o1, buf);  // it goes over O1's operand
-            ok &= mbar_wait_bounded(bar_kd, buf);
-            tc_fence_after();
-            if (lane == 0) {
-#pragma unroll
-                for (int part = 0; part < 2; ++part)
-#pragma unroll
-                    for (int ks = 0; ks < kLtC / 16; ++ks)
-                        tc_mma(tmem + kLtS, lt_desc_sw(vt + 2048 * ks, kLtBox, 1024),
-                               tc_desc(sb + M::kd + M::tile * part + 32 * DK * ks, 16 * DK, 128), kIdS, (part | ks) != 0);
-                tc_commit(bar_ds);
-                if (more) copy_qk(t0 + kLtC);  // q and k are read
+    auto wait = [&](uint32_t bar, uint32_t phase) {  // the warp's lanes agree
+        if (ok) ok = __all_sync(kFull, mbar_wait_bounded(bar, phase & 1u));
+        return ok;
+    };
+    auto wait_ds = [&](uint32_t w) { return wait(bar_ds + 8 * (w & 1u), w >> 1); };
+    auto stage_of = [&](uint32_t u) { return sb + (u % kLtStages) * M::stage; };
+    auto gates_of = [&](uint32_t u) { return sb + M::g + (u % kLtGates) * M::gbuf; };
+    uint32_t u = 0;  // pieces so far: the stage and the phases of a piece
+
+    if (warp < 8) {
+        // ---- the state: value column `row`, key channels NR half .. ----
+        const uint32_t tD = tl + kLtD + (uint32_t)(NR * half), tS = tl + kLtS + (uint32_t)(3 * NR / 2 * half);
+        for (int i = blockIdx.x; i < p.items && ok; i += gridDim.x) {
+            const LtItem x = item_at(i);
+            if (x.slot < 0 || x.slot >= p.num_slots) {
+                if (tid == 0) atomicOr(p.status, (uint32_t)kDevBadSlot);
+                continue;
             }
-            __syncwarp();
+            if (!STATE) {  // rows past the length
+                const int64_t ostep = (int64_t)p.H * p.dv;
+                float *const o = p.o + ((int64_t)x.b * T * p.H + x.h) * p.dv + x.c * 128 + row;
+                for (int t = max(x.len, x.t_begin) + half; t < min(x.t_begin + p.seg_len, T); t += 2) o[t * ostep] = 0.f;
+            }
+            if (!x.live) continue;
+            float2 S[NR / 2];
+            float *const st = p.state + ((x.slot * p.H + x.h) * DK + NR * half) * (int64_t)p.dv + x.c * 128 + row;
+            float *const part0 = p.part + (x.index * p.nseg * DK + NR * half) * 128 + row;
+            auto load_state = [&](const float *src, int64_t ld) {
+#pragma unroll
+                for (int r = 0; r < NR / 2; ++r) S[r] = make_float2(src[(2 * r) * ld], src[(2 * r + 1) * ld]);
+            };
+            auto store_state = [&](float *dst, int64_t ld) {
+#pragma unroll
+                for (int r = 0; r < NR / 2; ++r) {
+                    dst[(2 * r) * ld] = S[r].x;
+                    dst[(2 * r + 1) * ld] = S[r].y;
+                }
+            };
+            // Parts of a split row: 0 the state before it (the last segment overwrites the pool's while
+            // others may still start), 1 the state after segment 0, s what segment s - 1 adds; joined
+            // between the launches to the state before segment s.
+            if (STATE && x.seg > 0) {
+#pragma unroll
+                for (int r = 0; r < NR / 2; ++r) S[r] = make_float2(0.f, 0.f);
+            } else if (STATE || (x.seg == 0 && x.t_end == x.len)) {
+                load_state(st, p.dv);
+                if (STATE) store_state(part0, 128);
+            } else {
+                load_state(part0 + (int64_t)x.seg * DK * 128, 128);
+            }
+            // S as three bf16 parts: the half's hi words, mid words, lo words
+            auto write_parts = [&]() {
+#pragma unroll
+                for (int r8 = 0; r8 < NR / 16; ++r8) {  // 16 rows
+                    uint32_t hw[8], mw[8], lw[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) lt_split(S[8 * r8 + e], hw[e], mw[e], lw[e]);
+                    lt_st8(tS + 8 * r8, hw);
+                    lt_st8(tS + NR / 2 + 8 * r8, mw);
+                    lt_st8(tS + NR + 8 * r8, lw);
+                }
+                lt_wait_st();
+                tc_fence_before();
+                mbar_arrive(bar_sp);
+            };
+            if (!STATE) {
+                if (u > 0 && !wait(bar_o1, u - 1)) break;
+                write_parts();
+            }
+#pragma unroll 1
+            for (int t0 = x.t_begin; t0 < x.t_end; t0 += kLtC, ++u) {
+                if (!wait_ds(u)) break;
+                tc_fence_after();
+                const float2 eC = splat2(ldsf(gates_of(u) + 512 + 4 * 63));
+#pragma unroll
+                for (int r8 = 0; r8 < NR / 16; ++r8) {
+                    float d[16];
+                    lt_ld16(tD + 16 * r8, d);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) S[8 * r8 + e] = fma2(S[8 * r8 + e], eC, make_float2(d[2 * e], d[2 * e + 1]));
+                }
+                tc_fence_before();
+                mbar_arrive(bar_dsr);
+                if (!STATE && t0 + kLtC < x.t_end) {
+                    if (!wait(bar_o1, u)) break;
+                    write_parts();
+                }
+            }
+            if (!ok) break;
+            if (STATE) store_state(part0 + (int64_t)(x.seg + 1) * DK * 128, 128);
+            else if (x.t_end == x.len) store_state(st, p.dv);
+        }
+    } else if (warp == 12) {
+        // ---- products ----
+        const LtDesc dp = lt_uniform(tc_desc(sb + M::p, 128, 512));
+        const uint32_t tm = __reduce_max_sync(kFull, tmem);
+        auto more_items = [&](int i) {  // a live item after item i
+            for (i += gridDim.x; i < p.items; i += gridDim.x)
+                if (item_at(i).live) return true;
+            return false;
         };
-        if (issuer) {
-            if (lane == 0) {
+        auto landed = [&](uint32_t w) { return wait(bar_full + 8 * (w % kLtStages), w / kLtStages); };
+        for (int i = blockIdx.x; i < p.items && ok; i += gridDim.x) {
+            const LtItem x = item_at(i);
+            if (!x.live) continue;
+#pragma unroll 1
+            for (int t0 = x.t_begin; t0 < x.t_end; t0 += kLtC, ++u) {
+                const uint32_t at = stage_of(u), vt = at + M::v;
+                const LtDesc dv = lt_uniform(lt_desc_sw(vt, kLtBox, 1024));
+                if (!landed(u)) break;
+                const int n = x.t_end - t0;
+                if (n < kLtC) {  // v past the row's length may hold anything: zero, as 0 times it has to be
+                    for (int e = lane; e < (kLtC - n) * 16; e += 32)
+                        sts128(vt + (uint32_t)((e & 1) * kLtBox + (n + (e >> 4)) * 128 + ((e >> 1) & 7) * 16), make_uint4(0u, 0u, 0u, 0u));
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                }
+                // K step ks of the products Q K^T
+                auto mma_qk = [&](LtDesc q, LtDesc k, int ks) {
+                    const uint32_t off = (uint32_t)(M::step * (ks / 4) + 32 * (ks % 4));
+                    lt_mma(tm + kLtG, lt_at(q, off), lt_at(k, off), kIdG, ks != 0);
+                };
+                if (!STATE && u == 0) {
+                    const LtDesc q = lt_uniform(lt_desc_sw(at + M::q, 16, 1024)), k = lt_uniform(lt_desc_sw(at + M::k, 16, 1024));
+#pragma unroll
+                    for (int ks = 0; ks < DK / 16; ++ks) mma_qk(q, k, ks);
+                    lt_commit(bar_qk);
+                }
+                // what the piece adds to S
+                if (!wait(bar_kd + 8 * (u & 1u), u >> 1) || (u > 0 && !wait(bar_dsr, u - 1))) break;
+                tc_fence_after();
+                {
+                    const LtDesc kd = lt_uniform(tc_desc(sb + M::kd + (STATE ? (u & 1u) * 3 * M::tile : 0u), 16 * DK, 128));
+#pragma unroll
+                    for (int part = 0; part < 3; ++part)
+#pragma unroll
+                        for (int ks = 0; ks < kLtC / 16; ++ks)
+                            lt_mma(tm + kLtD, lt_at(dv, 2048 * ks), lt_at(kd, M::tile * part + 32 * DK * ks), kIdS, (part | ks) != 0);
+                    lt_commit(bar_ds + 8 * (u & 1u));
+                }
                 if (!STATE) {
+                    // the next piece's Q K^T first: its conversion is next
+                    if (!wait(bar_p, u)) break;
+                    const LtDesc q = lt_uniform(lt_desc_sw(at + M::q, 16, 1024));
+                    if (t0 + kLtC < x.t_end || more_items(i)) {
+                        if (!landed(u + 1)) break;
+                        tc_fence_after();
+                        const uint32_t to = stage_of(u + 1);
+                        const LtDesc q1 = lt_uniform(lt_desc_sw(to + M::q, 16, 1024)), k1 = lt_uniform(lt_desc_sw(to + M::k, 16, 1024));
 #pragma unroll
-                    for (int ks = 0; ks < DK / 16; ++ks) {
-                        const uint32_t off = (uint32_t)(2 * kLtBox * (ks / 4) + 32 * (ks % 4));
-                        tc_mma(tmem + kLtG, lt_desc_sw(sb + M::q + off, 16, 1024), lt_desc_sw(sb + M::k + off, 16, 1024), kIdG, ks != 0);
+                        for (int ks = 0; ks < DK / 16; ++ks) mma_qk(q1, k1, ks);
+                        lt_commit(bar_qk);
                     }
-                    tc_commit(bar_qk);
+                    if (!wait(bar_sp, u) || (u > 0 && !wait(bar_or, u - 1))) break;
+                    tc_fence_after();
 #pragma unroll
-                    for (int part = 0; part < 2; ++part)
+                    for (int part = 0; part < 3; ++part)
 #pragma unroll
                         for (int ks = 0; ks < DK / 16; ++ks) {
                             constexpr int HS = DK / 32;  // K steps per half
-                            const uint32_t a = tmem + kLtS + (uint32_t)(NR * (ks / HS) + NR / 2 * part + 8 * (ks % HS));
-                            const uint32_t off = (uint32_t)(2 * kLtBox * (ks / 4) + 32 * (ks % 4));
-                            lt_mma_ta(tmem + kLtO1, a, lt_desc_sw(sb + M::q + off, 16, 1024), kIdG, (part | ks) != 0);
+                            lt_mma_ta(tm + kLtO1, tm + kLtS + (uint32_t)(3 * NR / 2 * (ks / HS) + NR / 2 * part + 8 * (ks % HS)),
+                                      lt_at(q, M::step * (ks / 4) + 32 * (ks % 4)), kIdG, (part | ks) != 0);
                         }
-                    tc_commit(bar_o1);
-                }
-                if (more) copy_v(t0 + kLtC, buf ^ 1);
-            }
-            __syncwarp();
-            if (!STATE) {
-                if (more) {
-                    sum_gates(buf ^ 1);
-                    fetch_gates(t0 + 2 * kLtC);
-                }
-                issue_add();
-                ok &= mbar_wait_bounded(bar_p, buf);
-                tc_fence_after();
-                if (lane == 0) {
+                    lt_commit(bar_o1);
 #pragma unroll
-                    for (int part = 0; part < 2; ++part)
+                    for (int part = 0; part < 3; ++part)
 #pragma unroll
                         for (int ks = 0; ks < kLtC / 16; ++ks) {
-                            const uint64_t a = lt_desc_sw(vt + 2048 * ks, kLtBox, 1024);
-                            const uint32_t pp = sb + M::p + M::ppart * part;
-                            if (ks < 2) tc_mma(tmem + kLtG, a, tc_desc(pp + 256 * ks, 128, 512), kIdO2, (part | ks) != 0);
-                            else tc_mma(tmem + kLtG + 32, a, tc_desc(pp + 4096 + 256 * (ks - 2), 128, 512), kIdO2b, 1);
+                            if (ks < 2) lt_mma(tm + kLtO2, lt_at(dv, 2048 * ks), lt_at(dp, M::ppart * part + 256 * ks), kIdO2, (part | ks) != 0);
+                            else lt_mma(tm + kLtO2 + 32, lt_at(dv, 2048 * ks), lt_at(dp, M::ppart * part + 4096 + 256 * (ks - 2)), kIdO2b, 1);
                         }
-                    tc_commit(bar_o2);
+                    lt_commit(bar_o2);
                 }
-                __syncwarp();
+                lt_commit(bar_free + 8 * (u % kLtStages));
             }
         }
-        if (STATE || (warp & 3) >= 2) {  // K~
-            constexpr int NC = STATE ? CELLS / 4 : CELLS / 2;  // cells of a thread
-            const int kt = STATE ? tid & 63 : (warp & 1) * 32 + lane, c0 = NC * (STATE ? tid >> 6 : half);
-            const uint32_t gj = sg + 8 * kt, gC = sg + 8 * 63;
-            const float2 f = splat2(lt_ex2((ldsf(gC) - ldsf(gj)) + (ldsf(gC + 4) - ldsf(gj + 4))));
-            const uint32_t cell = (uint32_t)((kt >> 3) * CELLS * 128 + (kt & 7) * 16 + c0 * 128);
-#pragma unroll 4
-            for (int i = 0; i < NC; ++i) {
-                const uint32_t off = cell + (uint32_t)(i * 128);
-                uint4 w4 = lds128(sb + M::k + (uint32_t)(2 * kLtBox * ((c0 + i) >> 3) + kt * 128 + (((c0 + i) ^ kt) & 7) * 16));
-                if (kt >= n) w4 = make_uint4(0u, 0u, 0u, 0u);  // past the row's length
-                const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
-                uint32_t hw[4], lw[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    split2_pair(mul2(make_float2(__uint_as_float(w[e] << 16), __uint_as_float(w[e] & 0xffff0000u)), f), hw[e], lw[e]);
-                sts128(sb + M::kd + off, make_uint4(hw[0], hw[1], hw[2], hw[3]));
-                sts128(sb + M::kd + M::tile + off, make_uint4(lw[0], lw[1], lw[2], lw[3]));
+        if (!ok) {  // products that did not complete in time get one more bounded wait
+            mbar_wait_bounded(bar_ds + 8 * (u & 1u), (u >> 1) & 1u);
+            if (!STATE) mbar_wait_bounded(bar_o2, u & 1u);
+        }
+        __syncwarp();
+    } else {
+        // ---- K~ and P of a piece, then the outputs of the piece before; warp 13 copies ----
+        struct Next {  // the next piece to copy; its gates are in gate_a, gate_b (tokens 2 lane, 2 lane + 1)
+            int i, t;
+            LtItem x;
+            uint32_t u;
+        } nx;
+        float gate_a = 0.f, gate_b = 0.f;
+        nx.i = (int)blockIdx.x;
+        nx.u = 0;
+        Pair dec_total{0.f, 0.f};  // base-2 log of the segment's decay (the state alone)
+        auto find_live = [&]() {
+            for (; nx.i < p.items; nx.i += gridDim.x) {
+                nx.x = item_at(nx.i);
+                if (nx.x.live) break;
             }
-            fence_proxy_async_smem();
-            mbar_arrive(bar_kd);
-        } else if (!issuer) {  // P: rows 0-31; rows 32-63, columns 0-31 and 32-63
-            ok &= mbar_wait_bounded(bar_qk, buf);
-            tc_fence_after();
-            const float gih = ldsf(sg + 8 * row), gil = ldsf(sg + 8 * row + 4);
-            const uint32_t prow = sb + M::p + (half ? 4096u + (uint32_t)(((row - 32) >> 3) * 512) : (uint32_t)((row >> 3) * 512)) +
-                                  (uint32_t)((row & 7) * 16);
+            nx.t = nx.x.t_begin;
+        };
+        auto fetch_gates = [&]() {  // a piece ahead of their use
+            if (nx.i >= p.items) return;
+            const LtItem &x = nx.x;
+            const float *const g0 = p.g_per_head ? p.g + x.h : p.g + (int64_t)x.b * T * p.H + x.h;
+            const int64_t gstep = p.g_per_head ? 0 : p.H;
+            const int t = nx.t + 2 * lane;
+            gate_a = gate_b = 0.f;
+            if (t < x.t_end) gate_a = __ldg(g0 + (int64_t)t * gstep);
+            if (t + 1 < x.t_end) gate_b = __ldg(g0 + (int64_t)(t + 1) * gstep);
+        };
+        // Gates of a piece: inclusive sums in base 2 as pairs of floats (lane l: tokens 2l and 2l + 1),
+        // then the copies, whose barrier also says that the sums are there.
+        auto copy_next = [&]() {
+            if (nx.i >= p.items) return;
+            if (nx.u >= kLtStages && !wait(bar_free + 8 * (nx.u % kLtStages), nx.u / kLtStages - 1)) return;
+            const LtItem &x = nx.x;
+            const uint32_t full = bar_full + 8 * (nx.u % kLtStages), at = stage_of(nx.u), sg = gates_of(nx.u);
+            if (lane == 0) {
+                constexpr int QKBOX = DK / 64;  // boxes of q or k
+                const int hq = (int)((int64_t)x.h * p.Hqk / p.H);
+                // the bytes now, the barrier's arrival after the sums
+                asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(full),
+                             "r"(((STATE ? 1 : 2) * QKBOX + 2) * kLtBox)
+                             : "memory");
 #pragma unroll
-            for (int j0 = 0; j0 < 32; j0 += 16) {
-                float x[16];
-                lt_ld16(tl + kLtG + 32 * half + j0, x);
-                const int jb = 32 * half + j0;
+                for (int j = 0; j < QKBOX; ++j) {
+                    if (!STATE) lt_copy_box(at + M::q + M::step * j, &qmap, 64 * j, hq, nx.t, x.b, full);
+                    lt_copy_box(at + M::k + M::step * j, &kmap, 64 * j, hq, nx.t, x.b, full);
+                }
 #pragma unroll
-                for (int g8 = 0; g8 < 2; ++g8) {
-                    uint32_t hw[4], lw[4];
+                for (int j = 0; j < 2; ++j) lt_copy_box(at + M::v + kLtBox * j, &vmap, x.c * 128 + 64 * j, x.h, nx.t, x.b, full);
+            }
+            __syncwarp();
+            constexpr float kLog2eF = 1.4426950408889634f;
+            const float ga = gate_a < -200.f ? -200.f : gate_a;  // e^-200 is 0 in FP32 (-inf: a reset)
+            const float gb = gate_b < -200.f ? -200.f : gate_b;
+            const Pair x0{ga * kLog2eF, 0.f};
+            Pair s = add_pair(x0, Pair{gb * kLog2eF, 0.f});
+#pragma unroll
+            for (int m = 1; m < 32; m <<= 1) {
+                const Pair y{__shfl_up_sync(kFull, s.hi, m), __shfl_up_sync(kFull, s.lo, m)};
+                if (lane >= m) s = add_pair(s, y);
+            }
+            Pair before{__shfl_up_sync(kFull, s.hi, 1), __shfl_up_sync(kFull, s.lo, 1)};
+            if (lane == 0) before = Pair{0.f, 0.f};
+            const Pair first = add_pair(before, x0);
+            sts128(sg + 16 * lane, make_uint4(__float_as_uint(first.hi), __float_as_uint(first.lo), __float_as_uint(s.hi), __float_as_uint(s.lo)));
+            sts32(sg + 512 + 8 * lane, __float_as_uint(lt_ex2(first.hi)));
+            sts32(sg + 512 + 8 * lane + 4, __float_as_uint(lt_ex2(s.hi)));
+            __syncwarp();
+            if (lane == 0) mbar_arrive(full);
+            if (STATE) {
+                dec_total = add_pair(dec_total, Pair{__shfl_sync(kFull, s.hi, 31), __shfl_sync(kFull, s.lo, 31)});
+                if (nx.t + kLtC >= x.t_end) {
+                    if (lane == 0) p.part_dec[x.index * p.nseg + x.seg + 1] = lt_ex2(dec_total.hi);
+                    dec_total = Pair{0.f, 0.f};
+                }
+            }
+            ++nx.u;
+            nx.t += kLtC;
+            if (nx.t >= x.t_end) {
+                nx.i += gridDim.x;
+                find_live();
+            }
+            fetch_gates();
+        };
+        auto convert = [&](int n) {
+            const uint32_t sg = gates_of(u), ks = stage_of(u) + M::k;
+            if (!wait(bar_full + 8 * (u % kLtStages), u / kLtStages)) return;
+            if (STATE || (warp & 3) >= 2) {  // K~ = e^{G_C - G_j} k_j
+                if (u >= M::kdn && !wait_ds(u - M::kdn)) return;
+                const uint32_t kd = sb + M::kd + (STATE ? (u & 1u) * 3 * M::tile : 0u);
+                const float Ch = ldsf(sg + 8 * 63), Cl = ldsf(sg + 8 * 63 + 4);
+                // Small loop bodies here and below: the roles run different code at the same time, and what is
+                // unrolled whole misses the instruction caches.
+                auto fetch = [&](int t, int c) { return lds128(ks + (uint32_t)(M::step * (c >> 3) + t * 128 + ((c ^ t) & 7) * 16)); };
+                auto cell = [&](uint4 w4, int t, int c, float2 f) {
+                    if (t >= n) w4 = make_uint4(0u, 0u, 0u, 0u);  // past the row's length
+                    const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
+                    uint32_t hw[4], mw[4], lw[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        lt_split(mul2(make_float2(__uint_as_float(w[e] << 16), __uint_as_float(w[e] & 0xffff0000u)), f), hw[e], mw[e], lw[e]);
+                    const uint32_t dst = kd + (uint32_t)((t >> 3) * CELLS * 128 + c * 128 + (t & 7) * 16);
+                    sts128(dst, make_uint4(hw[0], hw[1], hw[2], hw[3]));
+                    sts128(dst + M::tile, make_uint4(mw[0], mw[1], mw[2], mw[3]));
+                    sts128(dst + 2 * M::tile, make_uint4(lw[0], lw[1], lw[2], lw[3]));
+                };
+                auto factor = [&](int t) { return splat2(lt_ex2((Ch - ldsf(sg + 8 * t)) + (Cl - ldsf(sg + 8 * t + 4)))); };
+                if (STATE) {
+                    constexpr int E = (kLtC * CELLS + 32 * kKdWarps - 1) / (32 * kKdWarps);
+                    const int first = 32 * (warp < 12 ? warp - 8 : warp - 10) + lane;
+                    uint4 w = fetch(first % kLtC, first / kLtC);
+                    float2 f = factor(first % kLtC);
+#pragma unroll 1
+                    for (int i = 0; i < E; ++i) {
+                        const int e = first + 32 * kKdWarps * i, e1 = min(e + 32 * kKdWarps, kLtC * CELLS - 1);
+                        const uint4 w1 = fetch(e1 % kLtC, e1 / kLtC);
+                        const float2 f1 = factor(e1 % kLtC);
+                        if (e < kLtC * CELLS) cell(w, e % kLtC, e / kLtC, f);
+                        w = w1;
+                        f = f1;
+                    }
+                } else {
+                    const int t = (warp & 1) * 32 + lane, c0 = CELLS / 2 * half;
+                    const float2 f = factor(t);
+                    uint4 w = fetch(t, c0);
+#pragma unroll 1
+                    for (int i = 0; i < CELLS / 2; ++i) {
+                        const uint4 w1 = fetch(t, c0 + min(i + 1, CELLS / 2 - 1));
+                        cell(w, t, c0 + i, f);
+                        w = w1;
+                    }
+                }
+                fence_proxy_async_smem();
+                mbar_arrive(bar_kd + 8 * (u & 1u));
+            } else {  // P: rows 0-31; rows 32-63, columns 0-31 and 32-63
+                if (!wait(bar_qk, u) || (u > 0 && !wait(bar_o2, u - 1))) return;
+                tc_fence_after();
+                const float gih = ldsf(sg + 8 * row), gil = ldsf(sg + 8 * row + 4);
+                const uint32_t prow = sb + M::p + (half ? 4096u + (uint32_t)(((row - 32) >> 3) * 512) : (uint32_t)((row >> 3) * 512)) +
+                                      (uint32_t)((row & 7) * 16);
+#pragma unroll 1
+                for (int g8 = 0; g8 < 4; ++g8) {
+                    const int j8 = 32 * half + 8 * g8;
+                    float x[8];
+                    lt_ld8(tl + kLtG + j8, x);
+                    uint4 gates[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) gates[e] = lds128(sg + 8 * (j8 + 2 * e));
+                    uint32_t hw[4], mw[4], lw[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const int j = jb + 8 * g8 + 2 * e;
-                        const uint4 gg = lds128(sg + 8 * j);
-                        const float d0 = (gih - __uint_as_float(gg.x)) + (gil - __uint_as_float(gg.y));
-                        const float d1 = (gih - __uint_as_float(gg.z)) + (gil - __uint_as_float(gg.w));
-                        split2_pair(make_float2(j <= row ? x[8 * g8 + 2 * e] * lt_ex2(d0) : 0.f,
-                                                j + 1 <= row ? x[8 * g8 + 2 * e + 1] * lt_ex2(d1) : 0.f),
-                                    hw[e], lw[e]);
+                        const int j = j8 + 2 * e;
+                        const float d0 = (gih - __uint_as_float(gates[e].x)) + (gil - __uint_as_float(gates[e].y));
+                        const float d1 = (gih - __uint_as_float(gates[e].z)) + (gil - __uint_as_float(gates[e].w));
+                        lt_split(make_float2(j <= row ? x[2 * e] * lt_ex2(d0) : 0.f, j + 1 <= row ? x[2 * e + 1] * lt_ex2(d1) : 0.f),
+                                 hw[e], mw[e], lw[e]);
                     }
-                    const uint32_t at = prow + (uint32_t)((j0 / 8 + g8) * 128);
+                    const uint32_t at = prow + (uint32_t)(g8 * 128);
                     sts128(at, make_uint4(hw[0], hw[1], hw[2], hw[3]));
-                    sts128(at + M::ppart, make_uint4(lw[0], lw[1], lw[2], lw[3]));
+                    sts128(at + M::ppart, make_uint4(mw[0], mw[1], mw[2], mw[3]));
+                    sts128(at + 2 * M::ppart, make_uint4(lw[0], lw[1], lw[2], lw[3]));
                 }
+                tc_fence_before();  // Q K^T is read
+                fence_proxy_async_smem();
+                mbar_arrive(bar_p);
             }
-            tc_fence_before();  // Q K^T is read: O2 goes over it
-            fence_proxy_async_smem();
-            mbar_arrive(bar_p);
-        }
-        if (STATE && issuer) {
-            issue_add();
-            if (more) {
-                sum_gates(buf ^ 1);
-                fetch_gates(t0 + 2 * kLtC);
-            }
-        }
-        const float2 eC = splat2(ldsf(sg + 512 + 4 * 63));
-        ok &= mbar_wait_bounded(bar_ds, buf);
-        tc_fence_after();
-#pragma unroll
-        for (int r8 = 0; r8 < NR / 16; ++r8) {
-            float d[16];
-            lt_ld16(tS + 16 * r8, d);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) S[8 * r8 + i] = fma2(S[8 * r8 + i], eC, make_float2(d[2 * i], d[2 * i + 1]));
-        }
-        if (!STATE) {
-            if (more) store_parts();
-            ok &= mbar_wait_bounded(bar_o2, buf);
+        };
+        // o_i = O2_i + e^{G_i} O1_i of piece w: this warp's value columns and 32 tokens (warp 8: all 64,
+        // those of warp 12 too)
+        const int64_t ostep = (int64_t)p.H * p.dv;
+        auto output = [&](uint32_t w, float *dst, int n) {
+            if (!wait(bar_o2, w)) return;
             tc_fence_after();
-            float *const oc = o + (int64_t)(t0 + 32 * half) * ostep;
-            const int nh = n - 32 * half;
+            const int j_end = warp == 8 ? 64 : 32 * half + 32;
+            const uint32_t eg = gates_of(w) + 512;
+            float *oj = dst + (int64_t)(32 * half) * ostep;
+#pragma unroll 1
+            for (int j = 32 * half; j < j_end; j += 16) {  // 16 tokens
+                float o1[16], o2[16];
+                lt_ld16(tl + kLtO1 + j, o1);
+                lt_ld16(tl + kLtO2 + j, o2);
+                if (j + 16 == j_end) tc_fence_before();
 #pragma unroll
-            for (int j0 = 0; j0 < 32; j0 += 8) {
-                if (j0 >= nh) break;
-                float o1[8], o2[8];
-                lt_ld8x2(tl + kLtO1 + 32 * half + j0, tl + kLtG + 32 * half + j0, o1, o2);
-                float *oj = oc + j0 * ostep;
+                for (int e = 0; e < 16; e += 4) {
+                    const uint4 g4 = lds128(eg + 4 * (j + e));
+                    o1[e] = fmaf(__uint_as_float(g4.x), o1[e], o2[e]);
+                    o1[e + 1] = fmaf(__uint_as_float(g4.y), o1[e + 1], o2[e + 1]);
+                    o1[e + 2] = fmaf(__uint_as_float(g4.z), o1[e + 2], o2[e + 2]);
+                    o1[e + 3] = fmaf(__uint_as_float(g4.w), o1[e + 3], o2[e + 3]);
+                }
+                if (j + 16 == j_end) mbar_arrive(bar_or);
+                const int nh = n - j;
 #pragma unroll
-                for (int e = 0; e < 8; e += 4) {
-                    const uint4 eg = lds128(sg + 512 + 4 * (32 * half + j0 + e));
-                    const float ev[4] = {__uint_as_float(eg.x), __uint_as_float(eg.y), __uint_as_float(eg.z), __uint_as_float(eg.w)};
-#pragma unroll
-                    for (int i = 0; i < 4; ++i, oj += ostep)
-                        if (j0 + e + i < nh) *oj = fmaf(ev[i], o1[e + i], o2[e + i]);
+                for (int e = 0; e < 16; ++e, oj += ostep)
+                    if (e < nh) *oj = o1[e];
+            }
+        };
+        if (warp == 13) {
+            find_live();
+            fetch_gates();
+            for (int i = 0; i < kLtStages; ++i) copy_next();
+            while (STATE && nx.i < p.items && ok) copy_next();
+        }
+        float *before = nullptr;  // the piece whose outputs are due
+        int before_n = 0;
+        for (int i = blockIdx.x; i < p.items && ok && !(STATE && warp == 13); i += gridDim.x) {
+            const LtItem x = item_at(i);
+            if (!x.live) continue;
+            float *const o = p.o + ((int64_t)x.b * T * p.H + x.h) * p.dv + x.c * 128 + row;
+#pragma unroll 1
+            for (int t0 = x.t_begin; t0 < x.t_end && ok; t0 += kLtC, ++u) {
+                convert(x.t_end - t0);
+                if (!STATE) {
+                    if (before) {
+                        output(u - 1, before, before_n);
+                        if (warp == 13) copy_next();
+                    }
+                    before = o + (int64_t)t0 * ostep;
+                    before_n = x.t_end - t0;
                 }
             }
         }
-    }
-    if (ok) ok = __syncthreads_and(ok);
-    if (ok) {
-        if (STATE) {
-            if (tid == 128) p.part_dec[(int64_t)item * p.nseg + seg + 1] = lt_ex2(dec_total.hi);
-            store_state(part0 + (int64_t)(seg + 1) * DK * 128, 128);
-        } else if (t_end == len) {
-            store_state(st, p.dv);
+        if (!STATE && before && ok) output(u - 1, before, before_n);
+        if (!ok && warp == 13) {  // copies that did not land in time get one more bounded wait
+            for (uint32_t w = nx.u > kLtStages ? nx.u - kLtStages : 0; w < nx.u; ++w)
+                mbar_wait_bounded(bar_full + 8 * (w % kLtStages), (w / kLtStages) & 1u);
         }
-    } else {  // copies and products that did not complete in time get one more bounded wait
-        if (tid == 0) atomicOr(p.status, (uint32_t)kDevWaitTimeout);
-        mbar_wait_bounded(bar_full, buf);
-        mbar_wait_bounded(bar_ds, buf ^ 1);
-        if (!STATE) mbar_wait_bounded(bar_o2, buf ^ 1);
     }
+    if (!ok && lane == 0) atomicOr(p.status, (uint32_t)kDevWaitTimeout);
+    __syncwarp();
     tc_fence_before();
     __syncthreads();
     if (warp == 0) {
@@ -519,14 +677,40 @@ __global__ void __launch_bounds__(kLtThreads, 2)
     }
 }
 
-// segments of a launch (1: no split) and the tokens of each
+// part s of every split row, head and columns, from what segment s - 1 adds to the state before segment s
+__global__ void __launch_bounds__(256) lin_tc_join_kernel(const LinTcParams p, int dk) {
+    const int64_t n = (int64_t)dk * 32, e = (int64_t)blockIdx.x * 256 + threadIdx.x, index = e / n;  // 16 bytes each
+    const int b = (int)(index / p.nc / p.H);
+    const int len = p.lengths ? min(max(p.lengths[b], 0), p.T) : p.T;
+    float4 *const at = reinterpret_cast<float4 *>(p.part) + index * p.nseg * n + e % n;
+    if (2 * (int64_t)p.seg_len >= len) return;  // two segments at most
+    const int64_t slot = p.slot_idx ? (int64_t)p.slot_idx[b] : (int64_t)b;
+    if (slot < 0 || slot >= p.num_slots) return;  // a skipped row has no parts
+    float4 S = at[n];
+    for (int s = 2; s < p.nseg && s * (int64_t)p.seg_len < len; ++s) {
+        const float d = p.part_dec[index * p.nseg + s];
+        const float4 x = at[s * n];
+        S = make_float4(fmaf(S.x, d, x.x), fmaf(S.y, d, x.y), fmaf(S.z, d, x.z), fmaf(S.w, d, x.w));
+        at[s * n] = S;
+    }
+}
+
+// Segments of a launch (1: no split) and the tokens of each.  The CTAs (one per SM) take the items
+// in rounds; the cost of a choice is its rounds times the pieces of an item and about three more
+// for its start and end, and half as much again for the launch that computes the states.
 int lin_tc_segments(const LinArgs &a, int *seg_len) {
-    const int64_t items = (int64_t)a.batch * a.H * (a.dv / 128);
+    const int64_t items = (int64_t)a.batch * a.H * (a.dv / 128), sms = sm_count();
     const int pieces = (a.T + kLtC - 1) / kLtC;
-    const int64_t room = 2 * (int64_t)sm_count();
-    int nseg = (int)std::min<int64_t>(room / std::max<int64_t>(items, 1), pieces / 4);
-    if (nseg < 2) nseg = 1;
-    const int per = (pieces + nseg - 1) / nseg;  // pieces of a segment
+    auto cost = [&](int nseg) {
+        const int64_t per = (pieces + nseg - 1) / nseg + 3;
+        const int64_t main = (items * nseg + sms - 1) / sms * per, states = nseg > 1 ? (items * (nseg - 1) + sms - 1) / sms * per : 0;
+        return 2 * main + states;
+    };
+    int best = 1;
+    if (items < 2 * sms)
+        for (int nseg = 2; nseg <= std::min(pieces / 4, 64); ++nseg)
+            if (cost(nseg) < cost(best)) best = nseg;
+    const int per = (pieces + best - 1) / best;  // pieces of a segment
     *seg_len = per * kLtC;
     return (pieces + per - 1) / per;
 }
@@ -570,11 +754,13 @@ struct LinTcMaps {
 };
 
 template <int DK, bool STATE>
-cudaError_t lin_tc_launch(const LinTcParams &p, const LinTcMaps &m, int64_t ctas, cudaStream_t s) {
+cudaError_t lin_tc_launch(const LinTcParams &p, const LinTcMaps &m, int64_t items, cudaStream_t s) {
     const void *const kern = reinterpret_cast<const void *>(lin_tc_kernel<DK, STATE>);
-    const cudaError_t e = ensure_smem_limit(kern, LtSmem<DK>::bytes);
+    const cudaError_t e = ensure_smem_limit(kern, LtSmem<DK, STATE>::bytes);
     if (e != cudaSuccess) return e;
-    lin_tc_kernel<DK, STATE><<<(unsigned)ctas, kLtThreads, LtSmem<DK>::bytes, s>>>(p, m.q, m.k, m.v);
+    LinTcParams q = p;
+    q.items = (int32_t)items;
+    lin_tc_kernel<DK, STATE><<<(unsigned)std::min<int64_t>(items, sm_count()), kLtThreads, LtSmem<DK, STATE>::bytes, s>>>(q, m.q, m.k, m.v);
     return cudaGetLastError();
 }
 
@@ -619,6 +805,8 @@ cudaError_t launch_lin_tc(LinArgs a, void *workspace, cudaStream_t s) {
         p.part_dec = p.part + items * p.nseg * a.dk * 128;
         e = a.dk == 64 ? lin_tc_launch<64, true>(p, m, items * (p.nseg - 1), s) : lin_tc_launch<128, true>(p, m, items * (p.nseg - 1), s);
         if (e != cudaSuccess) return e;
+        if (p.nseg > 2) lin_tc_join_kernel<<<(unsigned)(items * a.dk / 8), 256, 0, s>>>(p, a.dk);
+        if ((e = cudaGetLastError()) != cudaSuccess) return e;
     }
     return a.dk == 64 ? lin_tc_launch<64, false>(p, m, items * p.nseg, s) : lin_tc_launch<128, false>(p, m, items * p.nseg, s);
 }
