@@ -391,7 +391,7 @@ __global__ void __launch_bounds__(kLtThreads, 1)
                 tc_fence_after();
                 {
                     const LtDesc kd = lt_uniform(tc_desc(sb + M::kd + (STATE ? (u & 1u) * 3 * M::tile : 0u), 16 * DK, 128));
-#pragma unroll
+#pragma unroll 1
                     for (int part = 0; part < 3; ++part)
 #pragma unroll
                         for (int ks = 0; ks < kLtC / 16; ++ks)
@@ -413,7 +413,7 @@ __global__ void __launch_bounds__(kLtThreads, 1)
                     }
                     if (!wait(bar_sp, u) || (u > 0 && !wait(bar_or, u - 1))) break;
                     tc_fence_after();
-#pragma unroll
+#pragma unroll 1
                     for (int part = 0; part < 3; ++part)
 #pragma unroll
                         for (int ks = 0; ks < DK / 16; ++ks) {
@@ -422,7 +422,7 @@ __global__ void __launch_bounds__(kLtThreads, 1)
                                       lt_at(q, M::step * (ks / 4) + 32 * (ks % 4)), kIdG, (part | ks) != 0);
                         }
                     lt_commit(bar_o1);
-#pragma unroll
+#pragma unroll 1
                     for (int part = 0; part < 3; ++part)
 #pragma unroll
                         for (int ks = 0; ks < kLtC / 16; ++ks) {
