@@ -23,7 +23,7 @@
 // add what a piece adds and write the next operand parts to tensor memory.  Warps 8-15 turn
 // Q K^T into P and k into K~, one piece ahead of the outputs that they combine and store;
 // warp 12, which has no part in P and K~, issues the products, warp 13 the copies (TMA, 128-byte
-// swizzle, three stages) with the sums of the gates.  Bound by the conversions of warps 8-15, with
+// swizzle, three stages) and warp 9 sums the gates.  Bound by the conversions of warps 8-15, with
 // the bytes of q, k, v and o and the tensor time next.
 //
 // Few (slot, head) pairs and many tokens: the tokens are split into segments.  A first
@@ -54,9 +54,9 @@ constexpr int kLtGates = 4;  // a piece's sums may be read while the copies of t
 template <int DK, bool STATE>
 struct LtSmem {  // bytes from the base of the dynamic shared memory
     static constexpr int tile = kLtC * DK * 2;
-    // a stage: 64-column boxes [q box 0][k box 0][q box 1][k box 1], so that [Q; K] is one operand of
-    // 128 rows (the state alone: k boxes only), and two boxes of v
-    static constexpr int q = 0, k = STATE ? 0 : kLtBox, step = STATE ? kLtBox : 2 * kLtBox, v = STATE ? tile : 2 * tile;
+    // a stage: the 64-column boxes of q (not for the state alone), k and v.  Q K^T takes 128 rows from q
+    // on: the upper 64 are other boxes of the stage, and their products are not used.
+    static constexpr int q = 0, k = STATE ? 0 : tile, v = STATE ? tile : 2 * tile;
     static constexpr int stage = v + 2 * kLtBox;
     static constexpr int kdn = STATE ? 2 : 1;     // buffers of K~
     static constexpr int kd = kLtStages * stage;  // K~, three parts
@@ -86,12 +86,13 @@ __device__ __forceinline__ float lt_ex2(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// one box of a [batch][token][head][channel] tensor at (channel, head, token, row) into shared memory
-__device__ __forceinline__ void lt_copy_box(uint32_t dst, const CUtensorMap *map, int ch, int head, int t, int b, uint32_t bar) {
-    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(
-                     dst),
-                 "l"(map), "r"(ch), "r"(head), "r"(t), "r"(b), "r"(bar)
-                 : "memory");
+// the boxes of 64 tokens of a head of a [batch][token][head][channel] tensor, from 64-channel group
+// `group` on, into shared memory
+__device__ __forceinline__ void lt_copy_boxes(uint32_t dst, const CUtensorMap *map, int group, int head, int t, int b, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(dst),
+        "l"(map), "r"(0), "r"(head), "r"(t), "r"(group), "r"(b), "r"(bar)
+        : "memory");
 }
 // descriptor of an operand in 128-byte swizzled boxes.  K-major: rows of 128 bytes, 8 rows `sbo`
 // apart, a K step of 16 is 32 bytes.  MN-major: 64 columns per box, boxes `lbo` apart, 8 rows of K
@@ -215,7 +216,7 @@ __global__ void __launch_bounds__(kLtThreads, 1)
     constexpr int kKdWarps = STATE ? 6 : 4;  // warps 10, 11, 14, 15 (the state alone: all of 8-15 but 12 and 13)
     if (tid == 0) {
         for (int i = 0; i < kLtStages; ++i) {
-            mbar_init(bar_full + 8 * i, 1);
+            mbar_init(bar_full + 8 * i, 2);
             mbar_init(bar_free + 8 * i, 1);
         }
         mbar_init(bar_qk, 1);
@@ -296,6 +297,17 @@ __global__ void __launch_bounds__(kLtThreads, 1)
                     dst[(2 * r + 1) * ld] = S[r].y;
                 }
             };
+            // the next item's state into L2 while this one is worked on
+            if (!STATE && i + (int)gridDim.x < p.items) {
+                const LtItem y = item_at(i + gridDim.x);
+                if (y.live) {
+                    const bool part = !(y.seg == 0 && y.t_end == y.len);
+                    const float *const from = part ? p.part + (y.index * p.nseg + y.seg) * DK * 128
+                                                   : p.state + ((y.slot * p.H + y.h) * DK) * (int64_t)p.dv + y.c * 128;
+                    for (int l = tid; l < DK * 4; l += 256)  // lines of 128 bytes
+                        asm volatile("prefetch.global.L2 [%0];" ::"l"(from + (int64_t)(l >> 2) * (part ? 128 : p.dv) + 32 * (l & 3)));
+                }
+            }
             // Parts of a split row: 0 the state before it (the last segment overwrites the pool's while
             // others may still start), 1 the state after segment 0, s what segment s - 1 adds; joined
             // between the launches to the state before segment s.
@@ -377,7 +389,7 @@ __global__ void __launch_bounds__(kLtThreads, 1)
                 }
                 // K step ks of the products Q K^T
                 auto mma_qk = [&](LtDesc q, LtDesc k, int ks) {
-                    const uint32_t off = (uint32_t)(M::step * (ks / 4) + 32 * (ks % 4));
+                    const uint32_t off = (uint32_t)(kLtBox * (ks / 4) + 32 * (ks % 4));
                     lt_mma(tm + kLtG, lt_at(q, off), lt_at(k, off), kIdG, ks != 0);
                 };
                 if (!STATE && u == 0) {
@@ -419,7 +431,7 @@ __global__ void __launch_bounds__(kLtThreads, 1)
                         for (int ks = 0; ks < DK / 16; ++ks) {
                             constexpr int HS = DK / 32;  // K steps per half
                             lt_mma_ta(tm + kLtO1, tm + kLtS + (uint32_t)(3 * NR / 2 * (ks / HS) + NR / 2 * part + 8 * (ks % HS)),
-                                      lt_at(q, M::step * (ks / 4) + 32 * (ks % 4)), kIdG, (part | ks) != 0);
+                                      lt_at(q, kLtBox * (ks / 4) + 32 * (ks % 4)), kIdG, (part | ks) != 0);
                         }
                     lt_commit(bar_o1);
 #pragma unroll 1
@@ -440,16 +452,15 @@ __global__ void __launch_bounds__(kLtThreads, 1)
         }
         __syncwarp();
     } else {
-        // ---- K~ and P of a piece, then the outputs of the piece before; warp 13 copies ----
-        struct Next {  // the next piece to copy; its gates are in gate_a, gate_b (tokens 2 lane, 2 lane + 1)
+        // ---- K~ and P of a piece, then the outputs of the piece before; warp 13 copies, warp 9 sums ----
+        // The next piece to copy (warp 13) or to sum the gates of (warp 9; the state alone: warp 13 too)
+        struct Next {
             int i, t;
             LtItem x;
             uint32_t u;
         } nx;
-        float gate_a = 0.f, gate_b = 0.f;
         nx.i = (int)blockIdx.x;
         nx.u = 0;
-        Pair dec_total{0.f, 0.f};  // base-2 log of the segment's decay (the state alone)
         auto find_live = [&]() {
             for (; nx.i < p.items; nx.i += gridDim.x) {
                 nx.x = item_at(nx.i);
@@ -457,7 +468,29 @@ __global__ void __launch_bounds__(kLtThreads, 1)
             }
             nx.t = nx.x.t_begin;
         };
-        auto fetch_gates = [&]() {  // a piece ahead of their use
+        auto advance = [&]() {
+            ++nx.u;
+            nx.t += kLtC;
+            if (nx.t >= nx.x.t_end) {
+                nx.i += gridDim.x;
+                find_live();
+            }
+        };
+        auto copy_piece = [&]() {
+            const LtItem &x = nx.x;
+            const uint32_t full = bar_full + 8 * (nx.u % kLtStages), at = stage_of(nx.u);
+            if (lane == 0) {
+                const int hq = (int)((int64_t)x.h * p.Hqk / p.H);
+                mbar_arrive_expect_tx(full, ((STATE ? 1 : 2) * (DK / 64) + 2) * kLtBox);
+                if (!STATE) lt_copy_boxes(at + M::q, &qmap, 0, hq, nx.t, x.b, full);
+                lt_copy_boxes(at + M::k, &kmap, 0, hq, nx.t, x.b, full);
+                lt_copy_boxes(at + M::v, &vmap, 2 * x.c, x.h, nx.t, x.b, full);
+            }
+            __syncwarp();
+        };
+        float gate_a = 0.f, gate_b = 0.f;   // tokens 2 lane and 2 lane + 1 of the next piece
+        Pair dec_total{0.f, 0.f};           // base-2 log of the segment's decay (the state alone)
+        auto fetch_gates = [&]() {          // a piece ahead of their use
             if (nx.i >= p.items) return;
             const LtItem &x = nx.x;
             const float *const g0 = p.g_per_head ? p.g + x.h : p.g + (int64_t)x.b * T * p.H + x.h;
@@ -467,29 +500,10 @@ __global__ void __launch_bounds__(kLtThreads, 1)
             if (t < x.t_end) gate_a = __ldg(g0 + (int64_t)t * gstep);
             if (t + 1 < x.t_end) gate_b = __ldg(g0 + (int64_t)(t + 1) * gstep);
         };
-        // Gates of a piece: inclusive sums in base 2 as pairs of floats (lane l: tokens 2l and 2l + 1),
-        // then the copies, whose barrier also says that the sums are there.
-        auto copy_next = [&]() {
-            if (nx.i >= p.items) return;
-            if (nx.u >= kLtStages && !wait(bar_free + 8 * (nx.u % kLtStages), nx.u / kLtStages - 1)) return;
+        // inclusive sums of a piece's gates in base 2 as pairs of floats; `full` waits for them too
+        auto sum_gates = [&]() {
             const LtItem &x = nx.x;
-            const uint32_t full = bar_full + 8 * (nx.u % kLtStages), at = stage_of(nx.u), sg = gates_of(nx.u);
-            if (lane == 0) {
-                constexpr int QKBOX = DK / 64;  // boxes of q or k
-                const int hq = (int)((int64_t)x.h * p.Hqk / p.H);
-                // the bytes now, the barrier's arrival after the sums
-                asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(full),
-                             "r"(((STATE ? 1 : 2) * QKBOX + 2) * kLtBox)
-                             : "memory");
-#pragma unroll
-                for (int j = 0; j < QKBOX; ++j) {
-                    if (!STATE) lt_copy_box(at + M::q + M::step * j, &qmap, 64 * j, hq, nx.t, x.b, full);
-                    lt_copy_box(at + M::k + M::step * j, &kmap, 64 * j, hq, nx.t, x.b, full);
-                }
-#pragma unroll
-                for (int j = 0; j < 2; ++j) lt_copy_box(at + M::v + kLtBox * j, &vmap, x.c * 128 + 64 * j, x.h, nx.t, x.b, full);
-            }
-            __syncwarp();
+            const uint32_t sg = gates_of(nx.u);
             constexpr float kLog2eF = 1.4426950408889634f;
             const float ga = gate_a < -200.f ? -200.f : gate_a;  // e^-200 is 0 in FP32 (-inf: a reset)
             const float gb = gate_b < -200.f ? -200.f : gate_b;
@@ -507,7 +521,7 @@ __global__ void __launch_bounds__(kLtThreads, 1)
             sts32(sg + 512 + 8 * lane, __float_as_uint(lt_ex2(first.hi)));
             sts32(sg + 512 + 8 * lane + 4, __float_as_uint(lt_ex2(s.hi)));
             __syncwarp();
-            if (lane == 0) mbar_arrive(full);
+            if (lane == 0) mbar_arrive(bar_full + 8 * (nx.u % kLtStages));
             if (STATE) {
                 dec_total = add_pair(dec_total, Pair{__shfl_sync(kFull, s.hi, 31), __shfl_sync(kFull, s.lo, 31)});
                 if (nx.t + kLtC >= x.t_end) {
@@ -515,13 +529,18 @@ __global__ void __launch_bounds__(kLtThreads, 1)
                     dec_total = Pair{0.f, 0.f};
                 }
             }
-            ++nx.u;
-            nx.t += kLtC;
-            if (nx.t >= x.t_end) {
-                nx.i += gridDim.x;
-                find_live();
+        };
+        // the piece after the last of warp 13 or 9, once its stage is free (warp 9: its buffer of sums is,
+        // with the outputs of three pieces before)
+        auto next_piece = [&]() {
+            if (nx.i >= p.items) return;
+            if (warp == 13) {
+                if (nx.u >= kLtStages && !wait(bar_free + 8 * (nx.u % kLtStages), nx.u / kLtStages - 1)) return;
+                copy_piece();
             }
-            fetch_gates();
+            if (STATE || warp == 9) sum_gates();
+            advance();
+            if (STATE || warp == 9) fetch_gates();
         };
         auto convert = [&](int n) {
             const uint32_t sg = gates_of(u), ks = stage_of(u) + M::k;
@@ -532,7 +551,7 @@ __global__ void __launch_bounds__(kLtThreads, 1)
                 const float Ch = ldsf(sg + 8 * 63), Cl = ldsf(sg + 8 * 63 + 4);
                 // Small loop bodies here and below: the roles run different code at the same time, and what is
                 // unrolled whole misses the instruction caches.
-                auto fetch = [&](int t, int c) { return lds128(ks + (uint32_t)(M::step * (c >> 3) + t * 128 + ((c ^ t) & 7) * 16)); };
+                auto fetch = [&](int t, int c) { return lds128(ks + (uint32_t)(kLtBox * (c >> 3) + t * 128 + ((c ^ t) & 7) * 16)); };
                 auto cell = [&](uint4 w4, int t, int c, float2 f) {
                     if (t >= n) w4 = make_uint4(0u, 0u, 0u, 0u);  // past the row's length
                     const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
@@ -636,11 +655,11 @@ __global__ void __launch_bounds__(kLtThreads, 1)
                     if (e < nh) *oj = o1[e];
             }
         };
-        if (warp == 13) {
+        if (warp == 13 || (!STATE && warp == 9)) {
             find_live();
-            fetch_gates();
-            for (int i = 0; i < kLtStages; ++i) copy_next();
-            while (STATE && nx.i < p.items && ok) copy_next();
+            if (STATE || warp == 9) fetch_gates();
+            for (int i = 0; i < kLtStages; ++i) next_piece();
+            while (STATE && nx.i < p.items && ok) next_piece();
         }
         float *before = nullptr;  // the piece whose outputs are due
         int before_n = 0;
@@ -654,7 +673,7 @@ __global__ void __launch_bounds__(kLtThreads, 1)
                 if (!STATE) {
                     if (before) {
                         output(u - 1, before, before_n);
-                        if (warp == 13) copy_next();
+                        if (warp == 13 || warp == 9) next_piece();
                     }
                     before = o + (int64_t)t0 * ostep;
                     before_n = x.t_end - t0;
@@ -734,16 +753,17 @@ cudaError_t encode_tiled(EncodeTiled *out) {
     *out = f;
     return cudaSuccess;
 }
-// boxes of 64 channels x 64 tokens of one head and batch row; tokens past T read as zeros
-cudaError_t lin_tc_map(CUtensorMap *map, const void *base, int channels, int heads, int T, int batch) {
+// boxes of 64 channels x 64 tokens of one head and batch row, `groups` of 64 channels at once (64-channel
+// groups are the fourth dimension: a box of one follows the other); tokens past T read as zeros
+cudaError_t lin_tc_map(CUtensorMap *map, const void *base, int channels, int heads, int T, int batch, int groups) {
     EncodeTiled encode;
     const cudaError_t e = encode_tiled(&encode);
     if (e != cudaSuccess) return e;
-    const cuuint64_t dims[4] = {(cuuint64_t)channels, (cuuint64_t)heads, (cuuint64_t)T, (cuuint64_t)batch};
+    const cuuint64_t dims[5] = {64, (cuuint64_t)heads, (cuuint64_t)T, (cuuint64_t)channels / 64, (cuuint64_t)batch};
     const cuuint64_t row = (cuuint64_t)channels * 2;
-    const cuuint64_t strides[3] = {row, row * (cuuint64_t)heads, row * (cuuint64_t)heads * (cuuint64_t)T};
-    const cuuint32_t box[4] = {64, 1, kLtC, 1}, steps[4] = {1, 1, 1, 1};
-    const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(base), dims, strides, box, steps,
+    const cuuint64_t strides[4] = {row, row * (cuuint64_t)heads, 128, row * (cuuint64_t)heads * (cuuint64_t)T};
+    const cuuint32_t box[5] = {64, 1, kLtC, (cuuint32_t)groups, 1}, steps[5] = {1, 1, 1, 1, 1};
+    const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void *>(base), dims, strides, box, steps,
                               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
@@ -787,9 +807,9 @@ cudaError_t launch_lin_tc(LinArgs a, void *workspace, cudaStream_t s) {
     p.slot_idx = a.slot_idx;
     p.lengths = a.lengths;
     LinTcMaps m;
-    if ((e = lin_tc_map(&m.q, a.q, a.dk, a.Hqk, a.T, a.batch)) != cudaSuccess) return e;
-    if ((e = lin_tc_map(&m.k, a.k, a.dk, a.Hqk, a.T, a.batch)) != cudaSuccess) return e;
-    if ((e = lin_tc_map(&m.v, a.v, a.dv, a.H, a.T, a.batch)) != cudaSuccess) return e;
+    if ((e = lin_tc_map(&m.q, a.q, a.dk, a.Hqk, a.T, a.batch, a.dk / 64)) != cudaSuccess) return e;
+    if ((e = lin_tc_map(&m.k, a.k, a.dk, a.Hqk, a.T, a.batch, a.dk / 64)) != cudaSuccess) return e;
+    if ((e = lin_tc_map(&m.v, a.v, a.dv, a.H, a.T, a.batch, 2)) != cudaSuccess) return e;
     p.g = a.g;
     p.o = a.o;
     p.H = a.H;
