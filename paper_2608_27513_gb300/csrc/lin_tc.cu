@@ -244,19 +244,45 @@ __global__ void __launch_bounds__(kLtThreads, 1)
     const uint32_t tl = tmem + ((uint32_t)(32 * (warp & 3)) << 16);  // this warp's lanes
 
     const int T = p.T, segs = STATE ? p.nseg - 1 : p.nseg;
-    auto item_at = [&](int i) {
+    // The items of this CTA in order.  A cursor holds the next one's row values, fetched an item ahead.
+    struct Cursor {
+        int i, slot, len;
+    };
+    auto fetch_row = [&](Cursor &c) {
+        if (c.i >= p.items) return;
+        const int b = (int)(c.i / segs / p.nc / p.H);
+        c.slot = b;
+        c.len = T;
+        if (p.slot_idx) asm volatile("ld.global.nc.b32 %0, [%1];" : "=r"(c.slot) : "l"(p.slot_idx + b));
+        if (p.lengths) asm volatile("ld.global.nc.b32 %0, [%1];" : "=r"(c.len) : "l"(p.lengths + b));
+    };
+    auto first_item = [&]() {
+        Cursor c{(int)blockIdx.x, 0, 0};
+        fetch_row(c);
+        return c;
+    };
+    auto item_at = [&](const Cursor &c) {
         LtItem x;
-        x.seg = i % segs;
-        x.index = i / segs;
+        x.seg = c.i % segs;
+        x.index = c.i / segs;
         x.c = (int)(x.index % p.nc);
         x.h = (int)(x.index / p.nc % p.H);
         x.b = (int)(x.index / p.nc / p.H);
-        x.slot = p.slot_idx ? (int64_t)p.slot_idx[x.b] : (int64_t)x.b;
-        x.len = p.lengths ? min(max(p.lengths[x.b], 0), T) : T;
+        x.slot = c.slot;
+        x.len = min(max(c.len, 0), T);
         x.t_begin = x.seg * p.seg_len;
         x.t_end = min(min(x.t_begin + p.seg_len, T), x.len);
         x.live = x.slot >= 0 && x.slot < p.num_slots && x.t_begin < x.len && !(STATE && x.t_end == x.len);
         return x;
+    };
+    auto step_item = [&](Cursor &c) {
+        c.i += gridDim.x;
+        fetch_row(c);
+    };
+    auto to_live = [&](Cursor &c) {  // to the next item with work; false: there is none
+        for (; c.i < p.items; step_item(c))
+            if (item_at(c).live) return true;
+        return false;
     };
     bool ok = true;
     auto wait = [&](uint32_t bar, uint32_t phase) {  // the warp's lanes agree
@@ -271,18 +297,23 @@ __global__ void __launch_bounds__(kLtThreads, 1)
     if (warp < 8) {
         // ---- the state: value column `row`, key channels NR half .. ----
         const uint32_t tD = tl + kLtD + (uint32_t)(NR * half), tS = tl + kLtS + (uint32_t)(3 * NR / 2 * half);
-        for (int i = blockIdx.x; i < p.items && ok; i += gridDim.x) {
-            const LtItem x = item_at(i);
-            if (x.slot < 0 || x.slot >= p.num_slots) {
-                if (tid == 0) atomicOr(p.status, (uint32_t)kDevBadSlot);
+        auto clear_rows = [&](const LtItem &x) {  // past the length
+            if (STATE) return;
+            const int64_t ostep = (int64_t)p.H * p.dv;
+            float *const o = p.o + ((int64_t)x.b * T * p.H + x.h) * p.dv + x.c * 128 + row;
+            for (int t = max(x.len, x.t_begin) + half; t < min(x.t_begin + p.seg_len, T); t += 2) o[t * ostep] = 0.f;
+        };
+        for (Cursor cur = first_item(); cur.i < p.items && ok;) {
+            const LtItem x = item_at(cur);
+            step_item(cur);
+            if (!x.live) {
+                if (x.slot < 0 || x.slot >= p.num_slots) {
+                    if (tid == 0) atomicOr(p.status, (uint32_t)kDevBadSlot);
+                } else {
+                    clear_rows(x);
+                }
                 continue;
             }
-            if (!STATE) {  // rows past the length
-                const int64_t ostep = (int64_t)p.H * p.dv;
-                float *const o = p.o + ((int64_t)x.b * T * p.H + x.h) * p.dv + x.c * 128 + row;
-                for (int t = max(x.len, x.t_begin) + half; t < min(x.t_begin + p.seg_len, T); t += 2) o[t * ostep] = 0.f;
-            }
-            if (!x.live) continue;
             float2 S[NR / 2];
             float *const st = p.state + ((x.slot * p.H + x.h) * DK + NR * half) * (int64_t)p.dv + x.c * 128 + row;
             float *const part0 = p.part + (x.index * p.nseg * DK + NR * half) * 128 + row;
@@ -297,17 +328,6 @@ __global__ void __launch_bounds__(kLtThreads, 1)
                     dst[(2 * r + 1) * ld] = S[r].y;
                 }
             };
-            // the next item's state into L2 while this one is worked on
-            if (!STATE && i + (int)gridDim.x < p.items) {
-                const LtItem y = item_at(i + gridDim.x);
-                if (y.live) {
-                    const bool part = !(y.seg == 0 && y.t_end == y.len);
-                    const float *const from = part ? p.part + (y.index * p.nseg + y.seg) * DK * 128
-                                                   : p.state + ((y.slot * p.H + y.h) * DK) * (int64_t)p.dv + y.c * 128;
-                    for (int l = tid; l < DK * 4; l += 256)  // lines of 128 bytes
-                        asm volatile("prefetch.global.L2 [%0];" ::"l"(from + (int64_t)(l >> 2) * (part ? 128 : p.dv) + 32 * (l & 3)));
-                }
-            }
             // Parts of a split row: 0 the state before it (the last segment overwrites the pool's while
             // others may still start), 1 the state after segment 0, s what segment s - 1 adds; joined
             // between the launches to the state before segment s.
@@ -338,6 +358,15 @@ __global__ void __launch_bounds__(kLtThreads, 1)
             if (!STATE) {
                 if (u > 0 && !wait(bar_o1, u - 1)) break;
                 write_parts();
+                clear_rows(x);
+                if (cur.i < p.items) {  // the next item's state into L2 while this one is worked on
+                    const LtItem y = item_at(cur);
+                    const bool whole = y.seg == 0 && y.t_end == y.len;
+                    const float *const from = whole ? p.state + ((y.slot * p.H + y.h) * DK) * (int64_t)p.dv + y.c * 128
+                                                    : p.part + (y.index * p.nseg + y.seg) * DK * 128;
+                    for (int l = tid; l < DK * 4 && y.live; l += 256)  // lines of 128 bytes
+                        asm volatile("prefetch.global.L2 [%0];" ::"l"(from + (int64_t)(l >> 2) * (whole ? p.dv : 128) + 32 * (l & 3)));
+                }
             }
 #pragma unroll 1
             for (int t0 = x.t_begin; t0 < x.t_end; t0 += kLtC, ++u) {
@@ -366,15 +395,10 @@ __global__ void __launch_bounds__(kLtThreads, 1)
         // ---- products ----
         const LtDesc dp = lt_uniform(tc_desc(sb + M::p, 128, 512));
         const uint32_t tm = __reduce_max_sync(kFull, tmem);
-        auto more_items = [&](int i) {  // a live item after item i
-            for (i += gridDim.x; i < p.items; i += gridDim.x)
-                if (item_at(i).live) return true;
-            return false;
-        };
         auto landed = [&](uint32_t w) { return wait(bar_full + 8 * (w % kLtStages), w / kLtStages); };
-        for (int i = blockIdx.x; i < p.items && ok; i += gridDim.x) {
-            const LtItem x = item_at(i);
-            if (!x.live) continue;
+        for (Cursor cur = first_item(); ok && to_live(cur);) {
+            const LtItem x = item_at(cur);
+            step_item(cur);
 #pragma unroll 1
             for (int t0 = x.t_begin; t0 < x.t_end; t0 += kLtC, ++u) {
                 const uint32_t at = stage_of(u), vt = at + M::v;
@@ -414,7 +438,7 @@ __global__ void __launch_bounds__(kLtThreads, 1)
                     // the next piece's Q K^T first: its conversion is next
                     if (!wait(bar_p, u)) break;
                     const LtDesc q = lt_uniform(lt_desc_sw(at + M::q, 16, 1024));
-                    if (t0 + kLtC < x.t_end || more_items(i)) {
+                    if (t0 + kLtC < x.t_end || to_live(cur)) {
                         if (!landed(u + 1)) break;
                         tc_fence_after();
                         const uint32_t to = stage_of(u + 1);
@@ -455,26 +479,25 @@ __global__ void __launch_bounds__(kLtThreads, 1)
         // ---- K~ and P of a piece, then the outputs of the piece before; warp 13 copies, warp 9 sums ----
         // The next piece to copy (warp 13) or to sum the gates of (warp 9; the state alone: warp 13 too)
         struct Next {
-            int i, t;
+            Cursor cur;
+            bool live;
+            int t;
             LtItem x;
             uint32_t u;
         } nx;
-        nx.i = (int)blockIdx.x;
+        nx.cur = first_item();
         nx.u = 0;
         auto find_live = [&]() {
-            for (; nx.i < p.items; nx.i += gridDim.x) {
-                nx.x = item_at(nx.i);
-                if (nx.x.live) break;
-            }
+            nx.live = to_live(nx.cur);
+            if (!nx.live) return;
+            nx.x = item_at(nx.cur);
             nx.t = nx.x.t_begin;
+            step_item(nx.cur);
         };
         auto advance = [&]() {
             ++nx.u;
             nx.t += kLtC;
-            if (nx.t >= nx.x.t_end) {
-                nx.i += gridDim.x;
-                find_live();
-            }
+            if (nx.t >= nx.x.t_end) find_live();
         };
         auto copy_piece = [&]() {
             const LtItem &x = nx.x;
@@ -491,7 +514,7 @@ __global__ void __launch_bounds__(kLtThreads, 1)
         float gate_a = 0.f, gate_b = 0.f;   // tokens 2 lane and 2 lane + 1 of the next piece
         Pair dec_total{0.f, 0.f};           // base-2 log of the segment's decay (the state alone)
         auto fetch_gates = [&]() {          // a piece ahead of their use
-            if (nx.i >= p.items) return;
+            if (!nx.live) return;
             const LtItem &x = nx.x;
             const float *const g0 = p.g_per_head ? p.g + x.h : p.g + (int64_t)x.b * T * p.H + x.h;
             const int64_t gstep = p.g_per_head ? 0 : p.H;
@@ -533,7 +556,7 @@ __global__ void __launch_bounds__(kLtThreads, 1)
         // the piece after the last of warp 13 or 9, once its stage is free (warp 9: its buffer of sums is,
         // with the outputs of three pieces before)
         auto next_piece = [&]() {
-            if (nx.i >= p.items) return;
+            if (!nx.live) return;
             if (warp == 13) {
                 if (nx.u >= kLtStages && !wait(bar_free + 8 * (nx.u % kLtStages), nx.u / kLtStages - 1)) return;
                 copy_piece();
@@ -659,13 +682,13 @@ __global__ void __launch_bounds__(kLtThreads, 1)
             find_live();
             if (STATE || warp == 9) fetch_gates();
             for (int i = 0; i < kLtStages; ++i) next_piece();
-            while (STATE && nx.i < p.items && ok) next_piece();
+            while (STATE && nx.live && ok) next_piece();
         }
         float *before = nullptr;  // the piece whose outputs are due
         int before_n = 0;
-        for (int i = blockIdx.x; i < p.items && ok && !(STATE && warp == 13); i += gridDim.x) {
-            const LtItem x = item_at(i);
-            if (!x.live) continue;
+        for (Cursor cur = first_item(); ok && !(STATE && warp == 13) && to_live(cur);) {
+            const LtItem x = item_at(cur);
+            step_item(cur);
             float *const o = p.o + ((int64_t)x.b * T * p.H + x.h) * p.dv + x.c * 128 + row;
 #pragma unroll 1
             for (int t0 = x.t_begin; t0 < x.t_end && ok; t0 += kLtC, ++u) {
