@@ -65,7 +65,8 @@ struct LtSmem {  // bytes from the base of the dynamic shared memory
     static constexpr int g = p + (STATE ? 0 : 3 * ppart);  // per piece: (hi, lo) of G in base 2, 64 pairs, and e^{G_i}
     static constexpr int gbuf = 512 + 256;
     static constexpr int bar = g + kLtGates * gbuf;  // mbarriers, the tensor-memory address
-    static constexpr int bytes = bar + 160;
+    static constexpr int zero = bar + 160;  // 512 bytes: an output row past a row's length
+    static constexpr int bytes = zero + 512;
 };
 
 struct LinTcParams {
@@ -232,6 +233,10 @@ __global__ void __launch_bounds__(kLtThreads, 1)
         mbar_init(bar_or, 32 * 7);  // warps 8-15 but 12
         fence_mbar_init();
     }
+    if (tid >= 480) {
+        sts128(sb + M::zero + 16 * (tid - 480), make_uint4(0u, 0u, 0u, 0u));
+        fence_proxy_async_smem();
+    }
     if (warp == 0) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(s_taddr), "r"(kLtCols)
                      : "memory");
@@ -243,6 +248,7 @@ __global__ void __launch_bounds__(kLtThreads, 1)
     const uint32_t tmem = lds32(s_taddr);
     const uint32_t tl = tmem + ((uint32_t)(32 * (warp & 3)) << 16);  // this warp's lanes
 
+    const bool bulk_clear = (reinterpret_cast<uintptr_t>(p.o) & 15) == 0;  // warp 13 clears the rows of live items
     const int T = p.T, segs = STATE ? p.nseg - 1 : p.nseg;
     // The items of this CTA in order.  A cursor holds the next one's row values, fetched an item ahead.
     struct Cursor {
@@ -298,7 +304,7 @@ __global__ void __launch_bounds__(kLtThreads, 1)
         // ---- the state: value column `row`, key channels NR half .. ----
         const uint32_t tD = tl + kLtD + (uint32_t)(NR * half), tS = tl + kLtS + (uint32_t)(3 * NR / 2 * half);
         auto clear_rows = [&](const LtItem &x) {  // past the length
-            if (STATE) return;
+            if (STATE || (x.live && bulk_clear)) return;
             const int64_t ostep = (int64_t)p.H * p.dv;
             float *const o = p.o + ((int64_t)x.b * T * p.H + x.h) * p.dv + x.c * 128 + row;
             for (int t = max(x.len, x.t_begin) + half; t < min(x.t_begin + p.seg_len, T); t += 2) o[t * ostep] = 0.f;
@@ -559,6 +565,17 @@ __global__ void __launch_bounds__(kLtThreads, 1)
             if (!nx.live) return;
             if (warp == 13) {
                 if (nx.u >= kLtStages && !wait(bar_free + 8 * (nx.u % kLtStages), nx.u / kLtStages - 1)) return;
+                if (!STATE && bulk_clear && nx.t == nx.x.t_begin) {  // output rows past the row's length
+                    const LtItem &x = nx.x;
+                    const int t1 = min(x.t_begin + p.seg_len, T);
+                    float *const o = p.o + ((int64_t)x.b * T * p.H + x.h) * p.dv + x.c * 128;
+                    for (int t = x.len + lane; t < t1; t += 32)
+                        asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], 512;" ::"l"(o + (int64_t)t * p.H * p.dv),
+                                     "r"(sb + M::zero)
+                                     : "memory");
+                    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                    __syncwarp();
+                }
                 copy_piece();
             }
             if (STATE || warp == 9) sum_gates();
@@ -704,6 +721,7 @@ __global__ void __launch_bounds__(kLtThreads, 1)
             }
         }
         if (!STATE && before && ok) output(u - 1, before, before_n);
+        asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
         if (!ok && warp == 13) {  // copies that did not land in time get one more bounded wait
             for (uint32_t w = nx.u > kLtStages ? nx.u - kLtStages : 0; w < nx.u; ++w)
                 mbar_wait_bounded(bar_full + 8 * (w % kLtStages), (w / kLtStages) & 1u);
