@@ -337,7 +337,7 @@ DAMP_API damp_status damp_kda_prefill_chunk(const damp_layout *layout, void *sta
  *   workspace  damp_lin_prefill_workspace() bytes of scratch, 16-B aligned, of no use to
  *              any other call while this one runs (0 bytes for most shapes: NULL is then
  *              allowed); too few are DAMP_ERR_SHAPE
- *   Chunks of T > 16 tokens with BF16 inputs, d_k 64 or 128 and d_v a multiple of 128 run
+ *   Chunks of T > 16 tokens with BF16 inputs, d_k 64 or 128 and d_v a multiple of 64 run
  *   on the tensor cores; with few rows and heads the tokens are split into segments,
  *   which is what the workspace is for.  The results differ only in FP32 rounding (the FP32
  *   operands of the products keep 16 bits).

@@ -9,7 +9,8 @@
 //     S_0^T Q^T           -> O1 (A from tensor memory)
 //     V^T (K~ = e^{G_C - G_j} k_j)    -> what the piece adds to S^T
 //     V^T P^T, P = (e^{G_i - G_j} q_i.k_j)_{j<=i}  -> O2;  o_i = O2_i + e^{G_i} O1_i
-// One CTA per SM walks over items of 128 value columns of a (slot, head); an item's state
+// One CTA per SM walks over items of 128 value columns of a (slot, head) (64 of a last block: the
+// upper lanes then hold zeros); an item's state
 // stays in registers in FP32 (thread = value column and half the key channels) and only its
 // operand copy is rounded.
 //
@@ -195,7 +196,8 @@ struct LtItem {
 };
 
 // STATE: only what the segment adds to the state and its decay
-template <int DK, bool STATE>
+// FULL: d_v is a multiple of 128 (no block of 64 columns)
+template <int DK, bool STATE, bool FULL>
 __global__ void __launch_bounds__(kLtThreads, 1)
     lin_tc_kernel(const LinTcParams p, const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
                   const __grid_constant__ CUtensorMap vmap) {
@@ -304,7 +306,7 @@ __global__ void __launch_bounds__(kLtThreads, 1)
         // ---- the state: value column `row`, key channels NR half .. ----
         const uint32_t tD = tl + kLtD + (uint32_t)(NR * half), tS = tl + kLtS + (uint32_t)(3 * NR / 2 * half);
         auto clear_rows = [&](const LtItem &x) {  // past the length
-            if (STATE || (x.live && bulk_clear)) return;
+            if (STATE || (x.live && bulk_clear) || !(FULL || x.c * 128 + row < p.dv)) return;
             const int64_t ostep = (int64_t)p.H * p.dv;
             float *const o = p.o + ((int64_t)x.b * T * p.H + x.h) * p.dv + x.c * 128 + row;
             for (int t = max(x.len, x.t_begin) + half; t < min(x.t_begin + p.seg_len, T); t += 2) o[t * ostep] = 0.f;
@@ -321,7 +323,8 @@ __global__ void __launch_bounds__(kLtThreads, 1)
                 continue;
             }
             float2 S[NR / 2];
-            float *const st = p.state + ((x.slot * p.H + x.h) * DK + NR * half) * (int64_t)p.dv + x.c * 128 + row;
+            const bool on = FULL || x.c * 128 + row < p.dv;
+            float *const st = p.state + ((x.slot * p.H + x.h) * DK + NR * half) * (int64_t)p.dv + x.c * 128 + (on ? row : 0);
             float *const part0 = p.part + (x.index * p.nseg * DK + NR * half) * 128 + row;
             auto load_state = [&](const float *src, int64_t ld) {
 #pragma unroll
@@ -342,6 +345,10 @@ __global__ void __launch_bounds__(kLtThreads, 1)
                 for (int r = 0; r < NR / 2; ++r) S[r] = make_float2(0.f, 0.f);
             } else if (STATE || (x.seg == 0 && x.t_end == x.len)) {
                 load_state(st, p.dv);
+                if (!on) {
+#pragma unroll
+                    for (int r = 0; r < NR / 2; ++r) S[r] = make_float2(0.f, 0.f);
+                }
                 if (STATE) store_state(part0, 128);
             } else {
                 load_state(part0 + (int64_t)x.seg * DK * 128, 128);
@@ -370,8 +377,10 @@ __global__ void __launch_bounds__(kLtThreads, 1)
                     const bool whole = y.seg == 0 && y.t_end == y.len;
                     const float *const from = whole ? p.state + ((y.slot * p.H + y.h) * DK) * (int64_t)p.dv + y.c * 128
                                                     : p.part + (y.index * p.nseg + y.seg) * DK * 128;
-                    for (int l = tid; l < DK * 4 && y.live; l += 256)  // lines of 128 bytes
-                        asm volatile("prefetch.global.L2 [%0];" ::"l"(from + (int64_t)(l >> 2) * (whole ? p.dv : 128) + 32 * (l & 3)));
+                    const int lines = whole ? min(4, (p.dv - y.c * 128) / 32) : 4;  // of 128 bytes in a row
+                    for (int l = tid; l < DK * 4 && y.live; l += 256)
+                        if ((l & 3) < lines)
+                            asm volatile("prefetch.global.L2 [%0];" ::"l"(from + (int64_t)(l >> 2) * (whole ? p.dv : 128) + 32 * (l & 3)));
                 }
             }
 #pragma unroll 1
@@ -395,7 +404,7 @@ __global__ void __launch_bounds__(kLtThreads, 1)
             }
             if (!ok) break;
             if (STATE) store_state(part0 + (int64_t)(x.seg + 1) * DK * 128, 128);
-            else if (x.t_end == x.len) store_state(st, p.dv);
+            else if (x.t_end == x.len && on) store_state(st, p.dv);
         }
     } else if (warp == 12) {
         // ---- products ----
@@ -570,8 +579,8 @@ __global__ void __launch_bounds__(kLtThreads, 1)
                     const int t1 = min(x.t_begin + p.seg_len, T);
                     float *const o = p.o + ((int64_t)x.b * T * p.H + x.h) * p.dv + x.c * 128;
                     for (int t = x.len + lane; t < t1; t += 32)
-                        asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], 512;" ::"l"(o + (int64_t)t * p.H * p.dv),
-                                     "r"(sb + M::zero)
+                        asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(o + (int64_t)t * p.H * p.dv),
+                                     "r"(sb + M::zero), "r"(4 * min(128, p.dv - x.c * 128))
                                      : "memory");
                     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                     __syncwarp();
@@ -668,7 +677,7 @@ __global__ void __launch_bounds__(kLtThreads, 1)
         // o_i = O2_i + e^{G_i} O1_i of piece w: this warp's value columns and 32 tokens (warp 8: all 64,
         // those of warp 12 too)
         const int64_t ostep = (int64_t)p.H * p.dv;
-        auto output = [&](uint32_t w, float *dst, int n) {
+        auto output = [&](uint32_t w, float *dst, int n, bool on) {
             if (!wait(bar_o2, w)) return;
             tc_fence_after();
             const int j_end = warp == 8 ? 64 : 32 * half + 32;
@@ -689,7 +698,7 @@ __global__ void __launch_bounds__(kLtThreads, 1)
                     o1[e + 3] = fmaf(__uint_as_float(g4.w), o1[e + 3], o2[e + 3]);
                 }
                 if (j + 16 == j_end) mbar_arrive(bar_or);
-                const int nh = n - j;
+                const int nh = FULL || on ? n - j : 0;
 #pragma unroll
                 for (int e = 0; e < 16; ++e, oj += ostep)
                     if (e < nh) *oj = o1[e];
@@ -703,6 +712,7 @@ __global__ void __launch_bounds__(kLtThreads, 1)
         }
         float *before = nullptr;  // the piece whose outputs are due
         int before_n = 0;
+        bool before_on = false;
         for (Cursor cur = first_item(); ok && !(STATE && warp == 13) && to_live(cur);) {
             const LtItem x = item_at(cur);
             step_item(cur);
@@ -712,15 +722,16 @@ __global__ void __launch_bounds__(kLtThreads, 1)
                 convert(x.t_end - t0);
                 if (!STATE) {
                     if (before) {
-                        output(u - 1, before, before_n);
+                        output(u - 1, before, before_n, before_on);
                         if (warp == 13 || warp == 9) next_piece();
                     }
                     before = o + (int64_t)t0 * ostep;
                     before_n = x.t_end - t0;
+                    before_on = FULL || x.c * 128 + row < p.dv;
                 }
             }
         }
-        if (!STATE && before && ok) output(u - 1, before, before_n);
+        if (!STATE && before && ok) output(u - 1, before, before_n, before_on);
         asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
         if (!ok && warp == 13) {  // copies that did not land in time get one more bounded wait
             for (uint32_t w = nx.u > kLtStages ? nx.u - kLtStages : 0; w < nx.u; ++w)
@@ -759,7 +770,7 @@ __global__ void __launch_bounds__(256) lin_tc_join_kernel(const LinTcParams p, i
 // in rounds; the cost of a choice is its rounds times the pieces of an item and about three more
 // for its start and end, and half as much again for the launch that computes the states.
 int lin_tc_segments(const LinArgs &a, int *seg_len) {
-    const int64_t items = (int64_t)a.batch * a.H * (a.dv / 128), sms = sm_count();
+    const int64_t items = (int64_t)a.batch * a.H * ((a.dv + 127) / 128), sms = sm_count();
     const int pieces = (a.T + kLtC - 1) / kLtC;
     auto cost = [&](int nseg) {
         const int64_t per = (pieces + nseg - 1) / nseg + 3;
@@ -814,27 +825,33 @@ struct LinTcMaps {
     CUtensorMap q, k, v;
 };
 
-template <int DK, bool STATE>
-cudaError_t lin_tc_launch(const LinTcParams &p, const LinTcMaps &m, int64_t items, cudaStream_t s) {
-    const void *const kern = reinterpret_cast<const void *>(lin_tc_kernel<DK, STATE>);
+template <int DK, bool STATE, bool FULL>
+cudaError_t lin_tc_launch_one(const LinTcParams &p, const LinTcMaps &m, int64_t items, cudaStream_t s) {
+    const void *const kern = reinterpret_cast<const void *>(lin_tc_kernel<DK, STATE, FULL>);
     const cudaError_t e = ensure_smem_limit(kern, LtSmem<DK, STATE>::bytes);
     if (e != cudaSuccess) return e;
     LinTcParams q = p;
     q.items = (int32_t)items;
-    lin_tc_kernel<DK, STATE><<<(unsigned)std::min<int64_t>(items, sm_count()), kLtThreads, LtSmem<DK, STATE>::bytes, s>>>(q, m.q, m.k, m.v);
+    lin_tc_kernel<DK, STATE, FULL><<<(unsigned)std::min<int64_t>(items, sm_count()), kLtThreads, LtSmem<DK, STATE>::bytes, s>>>(q, m.q, m.k, m.v);
     return cudaGetLastError();
+}
+
+template <bool STATE>
+cudaError_t lin_tc_launch(const LinTcParams &p, const LinTcMaps &m, int dk, int64_t items, cudaStream_t s) {
+    if (p.dv % 128 == 0) return dk == 64 ? lin_tc_launch_one<64, STATE, true>(p, m, items, s) : lin_tc_launch_one<128, STATE, true>(p, m, items, s);
+    return dk == 64 ? lin_tc_launch_one<64, STATE, false>(p, m, items, s) : lin_tc_launch_one<128, STATE, false>(p, m, items, s);
 }
 
 }  // namespace
 
 bool lin_tc_takes(const LinArgs &a) {
-    return a.in_bf16 && (a.dk == 64 || a.dk == 128) && a.dv % 128 == 0 && a.T > 16;
+    return a.in_bf16 && (a.dk == 64 || a.dk == 128) && a.dv % 64 == 0 && a.T > 16;
 }
 
 size_t lin_tc_workspace(const LinArgs &a) {
     int seg_len;
     const int64_t nseg = lin_tc_segments(a, &seg_len);
-    const int64_t parts = nseg > 1 ? (int64_t)a.batch * a.H * (a.dv / 128) * nseg : 0;
+    const int64_t parts = nseg > 1 ? (int64_t)a.batch * a.H * ((a.dv + 127) / 128) * nseg : 0;
     return (size_t)(parts * (a.dk * 128 + 1) * 4);
 }
 
@@ -856,7 +873,7 @@ cudaError_t launch_lin_tc(LinArgs a, void *workspace, cudaStream_t s) {
     p.H = a.H;
     p.Hqk = a.Hqk;
     p.dv = a.dv;
-    p.nc = a.dv / 128;
+    p.nc = (a.dv + 127) / 128;
     p.T = a.T;
     p.g_per_head = a.g_per_head;
     p.nseg = lin_tc_segments(a, &p.seg_len);
@@ -864,12 +881,12 @@ cudaError_t launch_lin_tc(LinArgs a, void *workspace, cudaStream_t s) {
     if (p.nseg > 1) {
         p.part = static_cast<float *>(workspace);
         p.part_dec = p.part + items * p.nseg * a.dk * 128;
-        e = a.dk == 64 ? lin_tc_launch<64, true>(p, m, items * (p.nseg - 1), s) : lin_tc_launch<128, true>(p, m, items * (p.nseg - 1), s);
+        e = lin_tc_launch<true>(p, m, a.dk, items * (p.nseg - 1), s);
         if (e != cudaSuccess) return e;
         if (p.nseg > 2) lin_tc_join_kernel<<<(unsigned)(items * a.dk / 8), 256, 0, s>>>(p, a.dk);
         if ((e = cudaGetLastError()) != cudaSuccess) return e;
     }
-    return a.dk == 64 ? lin_tc_launch<64, false>(p, m, items * p.nseg, s) : lin_tc_launch<128, false>(p, m, items * p.nseg, s);
+    return lin_tc_launch<false>(p, m, a.dk, items * p.nseg, s);
 }
 
 cudaError_t take_status_lin_tc(uint32_t *bits) {
