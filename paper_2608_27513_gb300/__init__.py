@@ -116,8 +116,12 @@ def _ptr(t):
 
 def _stream(stream):
     import torch
-    s = torch.cuda.current_stream() if stream is None else stream
-    return ctypes.c_void_p(s.cuda_stream)
+    if stream is not None:
+        return ctypes.c_void_p(stream.cuda_stream)
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # a Stream object costs microseconds
+    if raw is None:
+        return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    return ctypes.c_void_p(raw(torch.cuda.current_device()))
 
 
 def _check(status: int, what: str):
@@ -558,7 +562,7 @@ def _new(shape, dtype, like, stream):
 
 
 def _given(name, t, shape, dtype):
-    """Raise ValueError unless t is a contiguous CUDA tensor of the shape and type."""
+    """The address of t; ValueError unless it is a contiguous CUDA tensor of the shape and type."""
     if t is None:
         raise ValueError(f"{name} is required")
     if t.shape != shape or t.dtype != dtype:
@@ -570,41 +574,50 @@ def _given(name, t, shape, dtype):
 
 def _lin(layout, state, q, k, v, g, o, lengths, slot_idx, num_slots, stream, lead_dims):
     import torch
+    f32, i32 = torch.float32, torch.int32
     if v is None or v.dim() != lead_dims + 2:
         raise ValueError(f"v must have {lead_dims + 2} dimensions")
     if layout.head_map is not None:
         raise ValueError("the FP32 state holds every head: use a layout without a head map")
-    lead = tuple(v.shape[:lead_dims])
-    B, H = lead[0], layout.num_heads
-    num_slots = _want_pool(layout, state, num_slots, fp32=True)
     dtype = v.dtype
-    if dtype not in (torch.bfloat16, torch.float32):
+    bf16 = dtype == torch.bfloat16
+    if not bf16 and dtype != f32 or q is not None and q.dtype != dtype or k is not None and k.dtype != dtype:
         raise TypeError("q, k, v must all be bfloat16 or all float32")
-    if q is not None and k is not None and (q.dtype != dtype or k.dtype != dtype):
-        raise TypeError("q, k, v must all be bfloat16 or all float32")
-    if slot_idx is None and B > num_slots:
-        raise ValueError(f"batch {B} exceeds num_slots {num_slots} without slot_idx")
-    qk_shape = lead + (layout.num_qk_heads, layout.d_k)
+    if state is None or state.dim() != 4:
+        raise ValueError("state must be a [slots, H, d_k, d_v] tensor")
+    lead = v.shape[:lead_dims]
+    B, H, dk, dv = lead[0], layout.num_heads, layout.d_k, layout.d_v
+    slots = state.shape[0]
+    pool = _given("state", state, (slots, H, dk, dv), f32)
+    if num_slots is not None:
+        if not 0 <= num_slots <= slots:
+            raise ValueError(f"num_slots {num_slots} exceeds the {slots} slots of state")
+        slots = int(num_slots)
+    idx = None
+    if slot_idx is not None:
+        idx = _given("slot_idx", slot_idx, (B,), i32)
+    elif B > slots:
+        raise ValueError(f"batch {B} exceeds num_slots {slots} without slot_idx")
+    qk_shape, o_shape = lead + (layout.num_qk_heads, dk), lead + (H, dv)
     per_head = g is not None and g.dim() == 1
-    o_shape = lead + (H, layout.d_v)
-    pool = _given("state", state, state.shape, torch.float32)
-    args = [_given("q", q, qk_shape, dtype), _given("k", k, qk_shape, dtype), _given("v", v, o_shape, dtype),
-            _given("g", g, (H,) if per_head else lead + (H,), torch.float32), 1 if per_head else 0]
+    qp, kp, vp = _given("q", q, qk_shape, dtype), _given("k", k, qk_shape, dtype), _given("v", v, o_shape, dtype)
+    gp = _given("g", g, (H,) if per_head else lead + (H,), f32)
+    n = None if lengths is None else _given("lengths", lengths, (B,), i32)
     if o is None:
-        o = _new(o_shape, torch.float32, v, stream)
-    in_dtype = IN_BF16 if dtype == torch.bfloat16 else IN_FP32
-    args += [_given("o", o, o_shape, torch.float32), in_dtype]
-    idx = None if slot_idx is None else _given("slot_idx", slot_idx, (B,), torch.int32)
-    c = layout.c()
-    head = [ctypes.byref(c), pool, num_slots, idx, B]
+        o = _new(o_shape, f32, v, stream)
+    op = _given("o", o, o_shape, f32)
+    c = ctypes.byref(layout.c())
+    in_dtype = IN_BF16 if bf16 else IN_FP32
+    L = lib()
     if lead_dims == 1:
-        _check(lib().damp_lin_decode_step(*head, *args, _stream(stream)), "damp_lin_decode_step")
+        _check(L.damp_lin_decode_step(c, pool, slots, idx, B, qp, kp, vp, gp, per_head, op, in_dtype, _stream(stream)),
+               "damp_lin_decode_step")
     else:
-        n = None if lengths is None else _given("lengths", lengths, (B,), torch.int32)
-        need = lib().damp_lin_prefill_workspace(head[0], B, lead[1], in_dtype)
+        T = lead[1]
+        need = L.damp_lin_prefill_workspace(c, B, T, in_dtype)
         ws = _new((need,), torch.uint8, v, stream) if need else None
-        _check(lib().damp_lin_prefill_chunk(*head, lead[1], n, *args, ws.data_ptr() if need else None, need,
-                                            _stream(stream)), "damp_lin_prefill_chunk")
+        _check(L.damp_lin_prefill_chunk(c, pool, slots, idx, B, T, n, qp, kp, vp, gp, per_head, op, in_dtype,
+                                        ws.data_ptr() if need else None, need, _stream(stream)), "damp_lin_prefill_chunk")
     return o
 
 
