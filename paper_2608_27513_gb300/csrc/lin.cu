@@ -29,6 +29,17 @@ static __device__ uint32_t g_status_lin;
 // a reset), and a NaN stays one
 __device__ __forceinline__ float lin_gate(float g) { return g < -200.f ? -200.f : g; }
 
+// e^g = a (1 + lo): a rounded, and what the rounding lost.  A gate that is the same for every token
+// would lose it every time in the same direction (400 tokens: 1e-5).
+struct Decay {
+    float a, lo;
+};
+__device__ __forceinline__ Decay lin_decay(float g) {
+    g = lin_gate(g);
+    const float a = expf(g);
+    return Decay{a, a >= 0.5f && a <= 2.f ? g - log1pf(a - 1.f) : 0.f};  // a - 1 is exact
+}
+
 template <bool BF16>
 __device__ __forceinline__ float4 load_in4(const void *p, int64_t i) {
     if (BF16) {
@@ -68,16 +79,17 @@ __global__ void __launch_bounds__(256) lin_step_kernel(const LinArgs p) {
     }
     const int64_t voff = ((int64_t)b * p.H + h) * p.dv + c * CW + col;
     const float4 v = load_in4<BF16>(p.v, voff);
-    const float a = expf(lin_gate(p.g[p.g_per_head ? h : (int64_t)b * p.H + h]));
+    const Decay d = lin_decay(p.g[p.g_per_head ? h : (int64_t)b * p.H + h]);
+    const float a = d.a, lo = a * d.lo;
     __syncthreads();
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const float kr = sk[row0 + r * RPI], qr = sq[row0 + r * RPI];
-        x[r].x = fmaf(x[r].x, a, kr * v.x);
-        x[r].y = fmaf(x[r].y, a, kr * v.y);
-        x[r].z = fmaf(x[r].z, a, kr * v.z);
-        x[r].w = fmaf(x[r].w, a, kr * v.w);
+        x[r].x = fmaf(x[r].x, a, fmaf(x[r].x, lo, kr * v.x));
+        x[r].y = fmaf(x[r].y, a, fmaf(x[r].y, lo, kr * v.y));
+        x[r].z = fmaf(x[r].z, a, fmaf(x[r].z, lo, kr * v.z));
+        x[r].w = fmaf(x[r].w, a, fmaf(x[r].w, lo, kr * v.w));
         S[r * ld] = x[r];
         o.x = fmaf(x[r].x, qr, o.x);
         o.y = fmaf(x[r].y, qr, o.y);
@@ -116,7 +128,7 @@ __global__ void __launch_bounds__(256, 2) lin_chunk_kernel(const LinArgs p, int 
     // alone joins nothing and has two)
     constexpr int NB = STATE ? 2 : 1;
     __shared__ __align__(16) float sk[NB][kGroup][DK], sq[STATE ? 1 : NB][kGroup][DK], sv[NB][kGroup][CW];
-    __shared__ float sa[NB][kGroup];
+    __shared__ Decay sa[NB][kGroup];
     __shared__ __align__(16) float share[STATE ? 1 : 8][kGroup][CW];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int segs = STATE ? nseg - 1 : nseg;
@@ -204,16 +216,18 @@ __global__ void __launch_bounds__(256, 2) lin_chunk_kernel(const LinArgs p, int 
             if (!STATE) *reinterpret_cast<float4 *>(&sq[buf][qt][qu]) = nq;
         }
         if (vt < kGroup) *reinterpret_cast<float4 *>(&sv[buf][vt][col]) = nv;
-        if (tid < kGroup) sa[buf][tid] = expf(lin_gate(na));
+        if (tid < kGroup) sa[buf][tid] = lin_decay(na);
         __syncthreads();
         if (t0 + kGroup < t_end) fetch(t0 + kGroup);
         const int n = min(kGroup, t_end - t0);
+        float lost = 0.f;
         float2 acc[STATE ? 1 : kGroup][2];
 #pragma unroll
         for (int t = 0; t < kGroup; ++t) {
             if (t < n) {
-                const float a1 = sa[buf][t];
+                const float a1 = sa[buf][t].a;
                 const float2 a = splat2(a1);
+                lost += sa[buf][t].lo;
                 if (STATE) decay *= a1;
                 const float4 v4 = *reinterpret_cast<const float4 *>(&sv[buf][t][col]);
                 const float2 v0 = make_float2(v4.x, v4.y), v1 = make_float2(v4.z, v4.w);
@@ -234,6 +248,12 @@ __global__ void __launch_bounds__(256, 2) lin_chunk_kernel(const LinArgs p, int 
                     acc[t][1] = o1;
                 }
             }
+        }
+        if (STATE) decay = fmaf(decay, lost, decay);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {  // what the group's decays lost to rounding
+            x[r][0] = fma2(x[r][0], splat2(lost), x[r][0]);
+            x[r][1] = fma2(x[r][1], splat2(lost), x[r][1]);
         }
         if (!STATE) {
 #pragma unroll

@@ -181,6 +181,23 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
 struct Pair {
     float hi, lo;
 };
+// 2^x within an ulp (ex2.approx is within three): 2^round(x) times the Taylor series of 2^f, |f| <= 1/2,
+// whose ninth term is below 6e-9.  For the factors that a state meets again and again; P takes lt_ex2.
+__device__ __forceinline__ float lt_exp2(Pair x) {
+    const float n = rintf(fminf(fmaxf(x.hi, -160.f), 160.f));
+    const float f = (x.hi - n) + x.lo;
+    float y = 1.525273381e-5f;  // ln2^7 / 7!
+    y = fmaf(y, f, 1.540353039e-4f);
+    y = fmaf(y, f, 1.333355815e-3f);
+    y = fmaf(y, f, 9.618129108e-3f);
+    y = fmaf(y, f, 5.550410866e-2f);
+    y = fmaf(y, f, 2.402265070e-1f);
+    y = fmaf(y, f, 6.931471806e-1f);
+    y = fmaf(y, f, 1.f);
+    const float n1 = rintf(0.5f * n);  // 2^n in two factors: n may be below -126
+    const float r = y * __uint_as_float((uint32_t)((int)n1 + 127) << 23) * __uint_as_float((uint32_t)((int)(n - n1) + 127) << 23);
+    return x.hi < -160.f ? 0.f : x.hi != x.hi ? x.hi : r;
+}
 __device__ __forceinline__ Pair add_pair(Pair a, Pair b) {
     const float s = a.hi + b.hi, t = s - a.hi;
     const float e = ((a.hi - (s - t)) + (b.hi - t)) + (a.lo + b.lo);  // the rounding of s, and the low parts
@@ -407,7 +424,7 @@ __global__ void __launch_bounds__(kLtThreads, 1)
             else if (x.t_end == x.len && on) store_state(st, p.dv);
         }
     } else if (warp == 12) {
-        // ---- products ----
+        // ---- products (the small parts first: a sum is cut off at its own size after every step) ----
         const LtDesc dp = lt_uniform(tc_desc(sb + M::p, 128, 512));
         const uint32_t tm = __reduce_max_sync(kFull, tmem);
         auto landed = [&](uint32_t w) { return wait(bar_full + 8 * (w % kLtStages), w / kLtStages); };
@@ -443,10 +460,10 @@ __global__ void __launch_bounds__(kLtThreads, 1)
                 {
                     const LtDesc kd = lt_uniform(tc_desc(sb + M::kd + (STATE ? (u & 1u) * 3 * M::tile : 0u), 16 * DK, 128));
 #pragma unroll 1
-                    for (int part = 0; part < 3; ++part)
+                    for (int part = 2; part >= 0; --part)
 #pragma unroll
                         for (int ks = 0; ks < kLtC / 16; ++ks)
-                            lt_mma(tm + kLtD, lt_at(dv, 2048 * ks), lt_at(kd, M::tile * part + 32 * DK * ks), kIdS, (part | ks) != 0);
+                            lt_mma(tm + kLtD, lt_at(dv, 2048 * ks), lt_at(kd, M::tile * part + 32 * DK * ks), kIdS, part != 2 || ks != 0);
                     lt_commit(bar_ds + 8 * (u & 1u));
                 }
                 if (!STATE) {
@@ -465,19 +482,19 @@ __global__ void __launch_bounds__(kLtThreads, 1)
                     if (!wait(bar_sp, u) || (u > 0 && !wait(bar_or, u - 1))) break;
                     tc_fence_after();
 #pragma unroll 1
-                    for (int part = 0; part < 3; ++part)
+                    for (int part = 2; part >= 0; --part)
 #pragma unroll
                         for (int ks = 0; ks < DK / 16; ++ks) {
                             constexpr int HS = DK / 32;  // K steps per half
                             lt_mma_ta(tm + kLtO1, tm + kLtS + (uint32_t)(3 * NR / 2 * (ks / HS) + NR / 2 * part + 8 * (ks % HS)),
-                                      lt_at(q, kLtBox * (ks / 4) + 32 * (ks % 4)), kIdG, (part | ks) != 0);
+                                      lt_at(q, kLtBox * (ks / 4) + 32 * (ks % 4)), kIdG, part != 2 || ks != 0);
                         }
                     lt_commit(bar_o1);
 #pragma unroll 1
-                    for (int part = 0; part < 3; ++part)
+                    for (int part = 2; part >= 0; --part)
 #pragma unroll
                         for (int ks = 0; ks < kLtC / 16; ++ks) {
-                            if (ks < 2) lt_mma(tm + kLtO2, lt_at(dv, 2048 * ks), lt_at(dp, M::ppart * part + 256 * ks), kIdO2, (part | ks) != 0);
+                            if (ks < 2) lt_mma(tm + kLtO2, lt_at(dv, 2048 * ks), lt_at(dp, M::ppart * part + 256 * ks), kIdO2, part != 2 || ks != 0);
                             else lt_mma(tm + kLtO2 + 32, lt_at(dv, 2048 * ks), lt_at(dp, M::ppart * part + 4096 + 256 * (ks - 2)), kIdO2b, 1);
                         }
                     lt_commit(bar_o2);
@@ -556,14 +573,14 @@ __global__ void __launch_bounds__(kLtThreads, 1)
             if (lane == 0) before = Pair{0.f, 0.f};
             const Pair first = add_pair(before, x0);
             sts128(sg + 16 * lane, make_uint4(__float_as_uint(first.hi), __float_as_uint(first.lo), __float_as_uint(s.hi), __float_as_uint(s.lo)));
-            sts32(sg + 512 + 8 * lane, __float_as_uint(lt_ex2(first.hi)));
-            sts32(sg + 512 + 8 * lane + 4, __float_as_uint(lt_ex2(s.hi)));
+            sts32(sg + 512 + 8 * lane, __float_as_uint(lt_exp2(first)));
+            sts32(sg + 512 + 8 * lane + 4, __float_as_uint(lt_exp2(s)));
             __syncwarp();
             if (lane == 0) mbar_arrive(bar_full + 8 * (nx.u % kLtStages));
             if (STATE) {
                 dec_total = add_pair(dec_total, Pair{__shfl_sync(kFull, s.hi, 31), __shfl_sync(kFull, s.lo, 31)});
                 if (nx.t + kLtC >= x.t_end) {
-                    if (lane == 0) p.part_dec[x.index * p.nseg + x.seg + 1] = lt_ex2(dec_total.hi);
+                    if (lane == 0) p.part_dec[x.index * p.nseg + x.seg + 1] = lt_exp2(dec_total);
                     dec_total = Pair{0.f, 0.f};
                 }
             }
@@ -613,20 +630,18 @@ __global__ void __launch_bounds__(kLtThreads, 1)
                     sts128(dst + M::tile, make_uint4(mw[0], mw[1], mw[2], mw[3]));
                     sts128(dst + 2 * M::tile, make_uint4(lw[0], lw[1], lw[2], lw[3]));
                 };
-                auto factor = [&](int t) { return splat2(lt_ex2((Ch - ldsf(sg + 8 * t)) + (Cl - ldsf(sg + 8 * t + 4)))); };
+                auto factor = [&](int t) { return splat2(lt_exp2(Pair{Ch - ldsf(sg + 8 * t), Cl - ldsf(sg + 8 * t + 4)})); };
                 if (STATE) {
-                    constexpr int E = (kLtC * CELLS + 32 * kKdWarps - 1) / (32 * kKdWarps);
                     const int first = 32 * (warp < 12 ? warp - 8 : warp - 10) + lane;
-                    uint4 w = fetch(first % kLtC, first / kLtC);
-                    float2 f = factor(first % kLtC);
+                    static_assert(32 * kKdWarps % kLtC == 0 || !STATE, "a thread's cells are of one token");
+                    const int t = first % kLtC;
+                    const float2 f = factor(t);
+                    uint4 w = fetch(t, first / kLtC);
 #pragma unroll 1
-                    for (int i = 0; i < E; ++i) {
-                        const int e = first + 32 * kKdWarps * i, e1 = min(e + 32 * kKdWarps, kLtC * CELLS - 1);
-                        const uint4 w1 = fetch(e1 % kLtC, e1 / kLtC);
-                        const float2 f1 = factor(e1 % kLtC);
-                        if (e < kLtC * CELLS) cell(w, e % kLtC, e / kLtC, f);
+                    for (int e = first; e < kLtC * CELLS; e += 32 * kKdWarps) {
+                        const uint4 w1 = fetch(t, min(e + 32 * kKdWarps, kLtC * CELLS - 1) / kLtC);
+                        cell(w, t, e / kLtC, f);
                         w = w1;
-                        f = f1;
                     }
                 } else {
                     const int t = (warp & 1) * 32 + lane, c0 = CELLS / 2 * half;
