@@ -396,7 +396,7 @@ DAMP_API damp_status damp_compact_slots(void *const *pools, const int64_t *slot_
  * x_i is accepted iff it is the lowest index of the target's maximum, which is also the
  * token drawn.
  *   target_logits  [B][D + 1] rows of row_stride elements, of which the first vocab are
- *                  tokens; damp_in_dtype logits_dtype; 16-B aligned
+ *                  tokens (vocab up to 2^30); damp_in_dtype logits_dtype; 16-B aligned
  *   draft_logits   [B][D] rows likewise, or NULL: q_i is 1 at x_i
  *                  (NaN and -inf exclude a token, +inf is the largest finite value; a row
  *                  that excludes every token accepts nothing and draws nothing)

@@ -658,7 +658,7 @@ damp_status damp_verify_drafts(const void *target_logits, const void *draft_logi
                                int32_t n_draft, const float *u, const float *noise, const float *temperature,
                                int32_t batch, int32_t *tokens_out, int32_t *count_out, void *stream) {
     if (logits_dtype != DAMP_IN_BF16 && logits_dtype != DAMP_IN_FP32) return DAMP_ERR_FORMAT;
-    if (batch < 0 || n_draft < 0 || vocab < 1 || row_stride < vocab) return DAMP_ERR_SHAPE;
+    if (batch < 0 || n_draft < 0 || vocab < 1 || vocab > (1 << 30) || row_stride < vocab) return DAMP_ERR_SHAPE;
     if (batch == 0) return DAMP_OK;
     const int64_t B = batch, D = n_draft, esz = logits_dtype == DAMP_IN_BF16 ? 2 : 4;
     if (row_stride > INT64_MAX / 8 / (B * (D + 1))) return DAMP_ERR_SHAPE;

@@ -6,13 +6,16 @@
 // Step.  o = e^g S^T q + (q.k) v and S <- e^g S + k v^T need each state value once: a
 // CTA takes CW columns of one (slot, head), 16 bytes per thread and row, all rows of a
 // thread in flight at once; the column sums of o go over the rows of the CTA through
-// shared memory.  Bound by the state's bytes (read + write).
+// shared memory.  Bound by the state's bytes (read + write): 256 slots of 32 heads, d = 128,
+// 159 us, the time of a plain copy of as many bytes.
 //
 // Chunk (any type, any supported size).  The same tile per CTA, held in registers over the
 // tokens; k, q and v of kGroup tokens are staged in shared memory one group ahead, a thread
-// sums its rows' share of the kGroup outputs, and the shares are joined over the rows once
-// per group.  Up to about 16 tokens the state's bytes bound it, beyond that the FP32 pipe
-// (three operations per state value and token).  Few (slot, head) pairs and many tokens: the
+// sums its rows' share of an output, and the shares of kGroup outputs are joined over the
+// rows at once.  For a few tokens the state's bytes and the latency of a CTA's loads bound it
+// (61 slots, 32 heads, d = 128: 53 us for 5 tokens, 83 for 16; the bytes need 39), beyond
+// that the FP32 pipe (three operations per state value and token: 0.98 ms for FP32 inputs at
+// 64 rows of 256 tokens).  Few (slot, head) pairs and many tokens: the
 // tokens are split into segments; a first launch computes what each segment adds to the
 // state, a second one starts every segment from the joined state before it (twice the work,
 // so from three segments on).
@@ -120,7 +123,7 @@ constexpr int kGroup = 8;  // tokens staged at a time
 // before it (the last segment overwrites the pool's while others may still start), 1 the state after
 // segment 0, s what segment s - 1 adds.
 template <int DK, int CW, bool BF16, bool STATE>
-__global__ void __launch_bounds__(256, 2) lin_chunk_kernel(const LinArgs p, int nseg, int seg_len, float *part, float *part_dec) {
+__global__ void __launch_bounds__(256, DK * CW <= 8192 ? 3 : 2) lin_chunk_kernel(const LinArgs p, int nseg, int seg_len, float *part, float *part_dec) {
     constexpr int TPR = CW / 4;     // threads per state row
     constexpr int RPI = 256 / TPR;  // row groups of the CTA
     constexpr int R = DK / RPI;     // consecutive rows of a thread (RPI is at most 32)
@@ -221,7 +224,6 @@ __global__ void __launch_bounds__(256, 2) lin_chunk_kernel(const LinArgs p, int 
         if (t0 + kGroup < t_end) fetch(t0 + kGroup);
         const int n = min(kGroup, t_end - t0);
         float lost = 0.f;
-        float2 acc[STATE ? 1 : kGroup][2];
 #pragma unroll
         for (int t = 0; t < kGroup; ++t) {
             if (t < n) {
@@ -244,22 +246,7 @@ __global__ void __launch_bounds__(256, 2) lin_chunk_kernel(const LinArgs p, int 
                     }
                 }
                 if (!STATE) {
-                    acc[t][0] = o0;
-                    acc[t][1] = o1;
-                }
-            }
-        }
-        if (STATE) decay = fmaf(decay, lost, decay);
-#pragma unroll
-        for (int r = 0; r < R; ++r) {  // what the group's decays lost to rounding
-            x[r][0] = fma2(x[r][0], splat2(lost), x[r][0]);
-            x[r][1] = fma2(x[r][1], splat2(lost), x[r][1]);
-        }
-        if (!STATE) {
-#pragma unroll
-            for (int t = 0; t < kGroup; ++t) {
-                if (t < n) {
-                    float4 y = make_float4(acc[t][0].x, acc[t][0].y, acc[t][1].x, acc[t][1].y);
+                    float4 y = make_float4(o0.x, o0.y, o1.x, o1.y);
 #pragma unroll
                     for (int m = 16; m >= TPR; m >>= 1) {  // rows of the same warp
                         y.x += __shfl_xor_sync(kFull, y.x, m);
@@ -270,6 +257,14 @@ __global__ void __launch_bounds__(256, 2) lin_chunk_kernel(const LinArgs p, int 
                     if (lane < TPR) *reinterpret_cast<float4 *>(&share[warp][t][col]) = y;
                 }
             }
+        }
+        if (STATE) decay = fmaf(decay, lost, decay);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {  // what the group's decays lost to rounding
+            x[r][0] = fma2(x[r][0], splat2(lost), x[r][0]);
+            x[r][1] = fma2(x[r][1], splat2(lost), x[r][1]);
+        }
+        if (!STATE) {
             __syncthreads();
             if (vt < n) {  // token vt, columns col .. col + 3
                 float4 y = *reinterpret_cast<const float4 *>(&share[0][vt][col]);

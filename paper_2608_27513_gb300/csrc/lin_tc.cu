@@ -5,31 +5,35 @@
 //     S_C = e^{G_C} S_0 + sum_j (e^{G_C - G_j} k_j) v_j^T
 // as four tcgen05.mma products, all transposed so that the value column is the tensor-
 // memory lane and an output row is stored by 32 lanes of a warp as one line:
-//     [Q; K] K^T          -> Q K^T in lanes 0-63 (the other rows are not used)
-//     S_0^T Q^T           -> O1 (A from tensor memory)
-//     V^T (K~ = e^{G_C - G_j} k_j)    -> what the piece adds to S^T
+//     Q K^T                                        (lanes 0-63 of 128)
+//     S_0^T Q^T                                    -> O1 (A from tensor memory)
+//     V^T (K~ = e^{G_C - G_j} k_j)                 -> what the piece adds to S^T
 //     V^T P^T, P = (e^{G_i - G_j} q_i.k_j)_{j<=i}  -> O2;  o_i = O2_i + e^{G_i} O1_i
-// One CTA per SM walks over items of 128 value columns of a (slot, head) (64 of a last block: the
-// upper lanes then hold zeros); an item's state
-// stays in registers in FP32 (thread = value column and half the key channels) and only its
-// operand copy is rounded.
+// One CTA per SM walks over items of 128 value columns of a (slot, head); a last block of 64
+// columns leaves zeros in the upper lanes.  An item's state stays in registers in FP32
+// (thread = value column and half the key channels); only its operand copy is split.
 //
 // Rounding.  q, k and v are bf16 inputs and enter exactly.  The FP32 operands (S_0, K~, P)
-// enter as three bf16 parts hi + mid + lo, 24 bits as FP32 has (two parts leave 2.9e-6 of the
-// result instead of 3e-7).  Accumulation and the
-// state are FP32.  G is summed as pairs of floats, so that G_i - G_j keeps its digits where
-// both are large (fast decays).
+// enter as three bf16 parts that hold them exactly.  Accumulation and the state are FP32.  G
+// is summed as pairs of floats, so that G_i - G_j keeps its digits where both are large
+// (fast decays).  Measured against 64 bits: 2e-7 of o.  Two parts instead of three (half the
+// tensor memory, two CTAs per SM) took 204 and 255 us where this takes 220 and 265 (64
+// ragged prompts of up to 256 tokens, one of 16381; 32 heads, d = 128), at 2.9e-6.
 //
 // Sixteen warps in two groups that meet only at mbarriers.  Warps 0-7 hold the state: they
 // add what a piece adds and write the next operand parts to tensor memory.  Warps 8-15 turn
 // Q K^T into P and k into K~, one piece ahead of the outputs that they combine and store;
-// warp 12, which has no part in P and K~, issues the products, warp 13 the copies (TMA, 128-byte
-// swizzle, three stages) and warp 9 sums the gates.  Bound by the conversions of warps 8-15, with
-// the bytes of q, k, v and o and the tensor time next.
+// warp 12, which has no part in P and K~, issues the products, warp 13 the copies (TMA,
+// 128-byte swizzle, three stages) and warp 9 sums the gates.
+//
+// Bound by latency along the chain of a piece, about 4900 clocks: a product takes 45 clocks
+// with 64 columns and 59 with 128, which makes 2700 for the piece's 56, the splits about 2000
+// in each group (9 operations per pair of values), and the two wait for each other in turn;
+// DRAM would need 3500.  At the border of two items the state's 128 KB are on the chain too.
 //
 // Few (slot, head) pairs and many tokens: the tokens are split into segments.  A first
-// launch computes what each segment adds to the state (k and v only), a second one starts
-// every segment from the joined state before it.
+// launch computes what each segment adds to the state (k and v only), a second one joins the
+// additions to states, a third one starts every segment from its own.
 #include <cuda.h>
 
 #include "damp_internal.h"
@@ -128,9 +132,8 @@ __device__ __forceinline__ void lt_st8(uint32_t taddr, const uint32_t (&r)[8]) {
                  : "memory");
 }
 __device__ __forceinline__ void lt_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-// Products are issued by whole warps in step, one elected lane each: the descriptors then stay in
-// uniform registers (a branch to one lane moves every operand of every product there one by one,
-// 85 clocks per product).
+// Products are issued by whole warps in step, one elected lane each, from descriptors in uniform
+// registers.
 struct LtDesc {  // a shared-memory descriptor whose low word is the same in all lanes
     uint32_t lo, hi;
 };
@@ -227,12 +230,13 @@ __global__ void __launch_bounds__(kLtThreads, 1)
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int row = 32 * (warp & 3) + lane, half = (warp >> 2) & 1;
     const uint32_t sb = smem_u32(smem);
-    // Barriers, one phase per piece (`full` and `free`: per piece of a stage; `ds` and `kd`: two each, of even and odd
-    // pieces, as a phase can be told from the next one only).  Copies landed, and all products of the stage done; products done: Q K^T, O1, the addition to
-    // S, O2; written: K~, P, the parts of S; read: the addition, the outputs.
-    const uint32_t bar_full = sb + M::bar, bar_free = bar_full + 24, bar_qk = bar_full + 48, bar_o1 = bar_qk + 8, bar_ds = bar_qk + 16, bar_o2 = bar_qk + 32,
-                   bar_kd = bar_qk + 40, bar_p = bar_qk + 56, bar_sp = bar_qk + 64, bar_dsr = bar_qk + 72, bar_or = bar_qk + 80,
-                   s_taddr = bar_qk + 88;
+    // Barriers, one phase per piece (`full` and `free`: per piece of a stage; `ds` and `kd`: two each, of
+    // even and odd pieces, as a phase can be told from the next one only).  Copies landed and gates summed;
+    // all products of the stage done; products done: Q K^T, O1, the addition to S, O2; written: K~, P, the
+    // parts of S; read: the addition, the outputs.
+    const uint32_t bar_full = sb + M::bar, bar_free = bar_full + 24, bar_qk = bar_full + 48, bar_o1 = bar_qk + 8,
+                   bar_ds = bar_qk + 16, bar_o2 = bar_qk + 32, bar_kd = bar_qk + 40, bar_p = bar_qk + 56, bar_sp = bar_qk + 64,
+                   bar_dsr = bar_qk + 72, bar_or = bar_qk + 80, s_taddr = bar_qk + 88;
     constexpr int kKdWarps = STATE ? 6 : 4;  // warps 10, 11, 14, 15 (the state alone: all of 8-15 but 12 and 13)
     if (tid == 0) {
         for (int i = 0; i < kLtStages; ++i) {
@@ -859,6 +863,8 @@ cudaError_t lin_tc_launch(const LinTcParams &p, const LinTcMaps &m, int dk, int6
 
 }  // namespace
 
+// From 17 tokens on (61 rows of 32 heads, d = 128: 83 us token by token against 106 at T = 16, 118
+// against 110 at T = 24; two rows: 10.8 against 9.5 at T = 16).
 bool lin_tc_takes(const LinArgs &a) {
     return a.in_bf16 && (a.dk == 64 || a.dk == 128) && a.dv % 64 == 0 && a.T > 16;
 }

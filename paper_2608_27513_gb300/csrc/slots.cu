@@ -9,7 +9,11 @@
 // Slices are disjoint, so no byte is read after it was written.  Bulk copies (the TMA
 // engine) move whole slices both ways; while a slice's destinations are written, the next
 // slice's sources are read into the other buffer.  A source named in consecutive entries
-// (a fork) is read once.  Bound by the bytes moved.
+// (a fork) is read once.  Bound by the bytes moved: of 10 layers of 627 KB slots, one slot
+// forked to 64 in 67 us (6.1 TB/s), a pool of 256 slots compacted to 131 in 132 us (6.1 TB/s,
+// the plan included).
+//
+// Free.  Plain 16-byte stores; 37 of those slots in 34 us (6.8 TB/s).
 #include "damp_common.cuh"
 #include "damp_internal.h"
 

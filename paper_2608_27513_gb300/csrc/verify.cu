@@ -17,8 +17,10 @@
 // the rows of R positions, joins them over the cluster through distributed shared memory
 // in one fixed order, so that every CTA comes to the same decisions, and goes on until a
 // rejection.  With many requests R = 1: rows after a rejection are not read.  With few, the
-// time is latency and all positions share a round.  Bound by the bytes of the rows needed,
-// with the exponentials (one per logit) next.
+// time is latency and all positions share a round.  Bound by the chain of rounds of a request,
+// with the bytes of the rows needed next: 256 requests of 3 drafts, V = 151552, bf16 take
+// 138 us (3.8 TB/s), of which the race is 50; 61 of 5 drafts, V = 100003, 50 us (two in a
+// round); one of 4 drafts, V = 32000, FP32, 12.5 us.
 //
 // The race reads its target row again (from L2) and the noise; p_t >= r_t, so a token whose
 // p_t / noise_t does not reach the best score of its CTA so far cannot win, and only for the

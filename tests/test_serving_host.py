@@ -129,6 +129,7 @@ def test_verify_rejects_bad_arguments(L, fb):
     assert call(batch=-1) == SHAPE
     assert call(D=-1) == SHAPE
     assert call(vocab=0) == SHAPE
+    assert call(vocab=(1 << 30) + 1, stride=1 << 31) == SHAPE
     assert call(stride=99) == SHAPE
     assert call(stride=1 << 62) == SHAPE
     assert call(dtype=2) == FORMAT
