@@ -35,12 +35,12 @@ __device__ __forceinline__ float lin_gate(float g) { return g < -200.f ? -200.f 
 // e^g = a (1 + lo): a rounded, and what the rounding lost.  A gate that is the same for every token
 // would lose it every time in the same direction (400 tokens: 1e-5).
 struct Decay {
-    float a, lo;
+    float a, lo, g;
 };
 __device__ __forceinline__ Decay lin_decay(float g) {
     g = lin_gate(g);
     const float a = expf(g);
-    return Decay{a, a >= 0.5f && a <= 2.f ? g - log1pf(a - 1.f) : 0.f};  // a - 1 is exact
+    return Decay{a, a >= 0.5f && a <= 2.f ? g - log1pf(a - 1.f) : 0.f, g};  // a - 1 is exact
 }
 
 template <bool BF16>
@@ -210,7 +210,7 @@ __global__ void __launch_bounds__(256, DK * CW <= 8192 ? 3 : 2) lin_chunk_kernel
             }
         }
     }
-    float decay = 1.f;
+    float gates = 0.f;  // of the segment so far
     int buf = 0;
 #pragma unroll 1
     for (int t0 = t_begin; t0 < t_end; t0 += kGroup, buf ^= NB - 1) {
@@ -230,7 +230,7 @@ __global__ void __launch_bounds__(256, DK * CW <= 8192 ? 3 : 2) lin_chunk_kernel
                 const float a1 = sa[buf][t].a;
                 const float2 a = splat2(a1);
                 lost += sa[buf][t].lo;
-                if (STATE) decay *= a1;
+                if (STATE) gates += sa[buf][t].g;
                 const float4 v4 = *reinterpret_cast<const float4 *>(&sv[buf][t][col]);
                 const float2 v0 = make_float2(v4.x, v4.y), v1 = make_float2(v4.z, v4.w);
                 float2 o0 = make_float2(0.f, 0.f), o1 = o0;
@@ -258,7 +258,6 @@ __global__ void __launch_bounds__(256, DK * CW <= 8192 ? 3 : 2) lin_chunk_kernel
                 }
             }
         }
-        if (STATE) decay = fmaf(decay, lost, decay);
 #pragma unroll
         for (int r = 0; r < R; ++r) {  // what the group's decays lost to rounding
             x[r][0] = fma2(x[r][0], splat2(lost), x[r][0]);
@@ -287,7 +286,10 @@ __global__ void __launch_bounds__(256, DK * CW <= 8192 ? 3 : 2) lin_chunk_kernel
     }
     if (STATE) {
         store_state(part_of(seg + 1), CW / 4);
-        if (tid == 0) part_dec[item * nseg + seg + 1] = decay;
+        if (tid == 0) {  // from the sum: a product would round the same way in every segment
+            const Decay d = lin_decay(gates);
+            part_dec[item * nseg + seg + 1] = fmaf(d.a, d.lo, d.a);
+        }
     } else if (t_end == len) {
         store_state(S, p.dv / 4);
     }

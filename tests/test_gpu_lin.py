@@ -203,6 +203,41 @@ def test_a_graph_replays_the_step_and_the_chunk():
         assert torch.equal(o1, o2) and torch.equal(pool, end)
 
 
+@pytest.mark.parametrize("T,d", [(9, 128), (70, 128), (70, 64), (9, 32)])
+@pytest.mark.parametrize("offset", [0, 1, 3])
+def test_outputs_of_any_alignment_and_nothing_beside_them(T, d, offset):
+    """o needs 4-byte alignment only, and no call writes before or after o or the slots."""
+    B, H, poison = 5, 2, 12345.0
+    ops, pool, _ = _inputs(B, T, H, H, d, d, torch.bfloat16, "token", seed=15, slots=B)
+    n = torch.tensor([T, 0, 3, T - 1, T // 2], dtype=torch.int32, device=DEV)
+    o_ref, S_ref, oa, Sa = R.lin(pool, **ops, lengths=n)
+    raw = torch.full((64 + offset + B * T * H * d + 64,), poison, device=DEV)
+    o = raw[64 + offset:64 + offset + B * T * H * d].view(B, T, H, d)
+    held = torch.full((B + 2, H, d, d), poison, device=DEV)
+    held[1:-1] = pool
+    damp.lin_prefill_chunk(damp.Layout(H, H, d, d, 0), held[1:-1], **ops, o=o, lengths=n)
+    R.check_lin(o, o_ref, oa, T, d, "o")
+    R.check_lin(held[1:-1], S_ref, Sa, T, d, "S")
+    assert not o[torch.arange(T, device=DEV)[None] >= n[:, None]].any()
+    assert bool((raw[:64 + offset] == poison).all() and (raw[-64:] == poison).all())
+    assert bool((held[[0, -1]] == poison).all())
+
+
+@pytest.mark.parametrize("dtype,T", [(torch.bfloat16, 3000), (torch.float32, 1500)])
+def test_constant_slow_gates_keep_their_digits(dtype, T):
+    """One gate for all tokens loses the same rounding every time: the error of a head that
+    remembers up to 3000 tokens stays that of as many random roundings, sqrt(3000 / 3) = 32 units
+    of 2^-24."""
+    H, d = 2, 64
+    ops, pool, idx = _inputs(1, T, H, H, d, d, dtype, "token", seed=16)
+    ops["g"] = torch.tensor([-3e-4, -2.7e-3], device=DEV)
+    o_ref, S_ref, _, _ = R.lin(pool[idx.long()], **ops)
+    o = damp.lin_prefill_chunk(damp.Layout(H, H, d, d, 0), pool, **ops, slot_idx=idx)
+    limit = 32 * R.EPS
+    assert (o.double() - o_ref).norm() <= limit * o_ref.norm()
+    assert (pool[idx.long()].double() - S_ref).norm() <= limit * S_ref.norm()
+
+
 def test_empty_calls():
     L = damp.Layout(2, 2, 64, 64, 0)
     pool = damp.new_fp32_state(L, 3)
