@@ -13,7 +13,7 @@
 // tokens; k, q and v of kGroup tokens are staged in shared memory one group ahead, a thread
 // sums its rows' share of an output, and the shares of kGroup outputs are joined over the
 // rows at once.  For a few tokens the state's bytes and the latency of a CTA's loads bound it
-// (61 slots, 32 heads, d = 128: 53 us for 5 tokens, 83 for 16; the bytes need 39), beyond
+// (61 slots, 32 heads, d = 128: 49 us for 5 tokens, 83 for 16; the bytes need 39), beyond
 // that the FP32 pipe (three operations per state value and token: 0.98 ms for FP32 inputs at
 // 64 rows of 256 tokens).  Few (slot, head) pairs and many tokens: the
 // tokens are split into segments; a first launch computes what each segment adds to the
@@ -117,13 +117,15 @@ __global__ void __launch_bounds__(256) lin_step_kernel(const LinArgs p) {
     }
 }
 
+__device__ __forceinline__ void prefetch_l2(const void *p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
+
 constexpr int kGroup = 8;  // tokens staged at a time
 
 // STATE: only what the segment adds to the state and its decay.  Parts of a split row: 0 the state
 // before it (the last segment overwrites the pool's while others may still start), 1 the state after
 // segment 0, s what segment s - 1 adds.
 template <int DK, int CW, bool BF16, bool STATE>
-__global__ void __launch_bounds__(256, DK * CW <= 8192 ? 3 : 2) lin_chunk_kernel(const LinArgs p, int nseg, int seg_len, float *part, float *part_dec) {
+__global__ void __launch_bounds__(256, DK * CW <= 8192 ? 3 : 2) lin_chunk_kernel(const LinArgs p, int nseg, int seg_len, int ahead, float *part, float *part_dec) {
     constexpr int TPR = CW / 4;     // threads per state row
     constexpr int RPI = 256 / TPR;  // row groups of the CTA
     constexpr int R = DK / RPI;     // consecutive rows of a thread (RPI is at most 32)
@@ -208,6 +210,27 @@ __global__ void __launch_bounds__(256, DK * CW <= 8192 ? 3 : 2) lin_chunk_kernel
                 x[r][0] = fma2(x[r][0], d, make_float2(y.x, y.y));
                 x[r][1] = fma2(x[r][1], d, make_float2(y.z, y.w));
             }
+        }
+    }
+    if (!STATE && ahead > 0 && blockIdx.x + (unsigned)ahead < gridDim.x) {
+        // what the CTA that takes this one's place reads first, into L2 (one segment: a CTA is an item)
+        const int64_t item2 = (int64_t)blockIdx.x + ahead;
+        const int c2 = (int)(item2 % nc), h2 = (int)(item2 / nc % p.H), b2 = (int)(item2 / nc / p.H);
+        const int64_t slot2 = p.slot_idx ? (int64_t)p.slot_idx[b2] : (int64_t)b2;
+        const int len2 = p.lengths ? min(p.lengths[b2], T) : T;
+        if (slot2 >= 0 && slot2 < p.num_slots && len2 > 0) {
+            constexpr int L = CW / 32;  // lines of 128 bytes in a row of the tile
+            const float *const s2 = p.state + (slot2 * p.H + h2) * DK * (int64_t)p.dv + c2 * CW;
+            for (int l = tid; l < DK * L; l += 256) prefetch_l2(s2 + (int64_t)(l / L) * p.dv + 32 * (l % L));
+            constexpr int E = BF16 ? 2 : 4;
+            const int hq2 = (int)((int64_t)h2 * p.Hqk / p.H);
+            if (qt < min(kGroup, len2) && qu * E % 128 == 0) {
+                const int64_t at = ((((int64_t)b2 * T + qt) * p.Hqk + hq2) * DK + qu) * E;
+                prefetch_l2(static_cast<const char *>(p.k) + at);
+                prefetch_l2(static_cast<const char *>(p.q) + at);
+            }
+            if (vt < min(kGroup, len2) && col * E % 128 == 0)
+                prefetch_l2(static_cast<const char *>(p.v) + ((((int64_t)b2 * T + vt) * p.H + h2) * p.dv + c2 * CW + col) * E);
         }
     }
     float gates = 0.f;  // of the segment so far
@@ -318,8 +341,13 @@ static void lin_chunk_run(const LinArgs &p, void *workspace, cudaStream_t s) {
     const int nseg = lin_chunk_segments(p, &seg_len);
     const int64_t items = (int64_t)p.batch * p.H * (p.dv / CW);
     float *const part = static_cast<float *>(workspace), *const dec = part + (nseg > 1 ? items * nseg * DK * CW : 0);
-    if (nseg > 1) lin_chunk_kernel<DK, CW, BF16, true><<<(unsigned)(items * (nseg - 1)), 256, 0, s>>>(p, nseg, seg_len, part, dec);
-    lin_chunk_kernel<DK, CW, BF16, false><<<(unsigned)(items * nseg), 256, 0, s>>>(p, nseg, seg_len, part, dec);
+    // A CTA of at most one group is mostly waiting for its tile, which the CTA a wave before it brings
+    // into L2 (61 slots, 32 heads, d = 128, with and without: 2 tokens 44 and 53 us, 5 50 and 55, 8 59
+    // and 61; 304 CTAs ahead instead of 152 take 1 us more).  More tokens (16: 88 and 86) and small
+    // tiles (d = 64: 19.4 and 18.3) do without.
+    const int ahead = nseg == 1 && p.T <= kGroup && DK * CW >= 8192 ? sm_count() : 0;
+    if (nseg > 1) lin_chunk_kernel<DK, CW, BF16, true><<<(unsigned)(items * (nseg - 1)), 256, 0, s>>>(p, nseg, seg_len, ahead, part, dec);
+    lin_chunk_kernel<DK, CW, BF16, false><<<(unsigned)(items * nseg), 256, 0, s>>>(p, nseg, seg_len, ahead, part, dec);
 }
 template <int DK, bool BF16>
 static void lin_chunk_pick(const LinArgs &p, void *workspace, cudaStream_t s) {
