@@ -13,7 +13,7 @@
 // tokens; k, q and v of kGroup tokens are staged in shared memory one group ahead, a thread
 // sums its rows' share of an output, and the shares of kGroup outputs are joined over the
 // rows at once.  For a few tokens the state's bytes and the latency of a CTA's loads bound it
-// (61 slots, 32 heads, d = 128: 49 us for 5 tokens, 83 for 16; the bytes need 39), beyond
+// (61 slots, 32 heads, d = 128: 46 us for 5 tokens, 83 for 16; the bytes need 39), beyond
 // that the FP32 pipe (three operations per state value and token: 0.98 ms for FP32 inputs at
 // 64 rows of 256 tokens).  Few (slot, head) pairs and many tokens: the
 // tokens are split into segments; a first launch computes what each segment adds to the

@@ -17,7 +17,7 @@
 // enter as three bf16 parts that hold them exactly.  Accumulation and the state are FP32.  G
 // is summed as pairs of floats, so that G_i - G_j keeps its digits where both are large
 // (fast decays).  Measured against 64 bits: 2e-7 of o.  Two parts instead of three (half the
-// tensor memory, two CTAs per SM) took 204 and 255 us where this takes 220 and 265 (64
+// tensor memory, two CTAs per SM) took 204 and 255 us where this takes 209 and 270 (64
 // ragged prompts of up to 256 tokens, one of 16381; 32 heads, d = 128), at 2.9e-6.
 //
 // Sixteen warps in two groups that meet only at mbarriers.  Warps 0-7 hold the state: they
@@ -29,7 +29,8 @@
 // Bound by latency along the chain of a piece, about 4900 clocks: a product takes 45 clocks
 // with 64 columns and 59 with 128, which makes 2700 for the piece's 56, the splits about 2000
 // in each group (9 operations per pair of values), and the two wait for each other in turn;
-// DRAM would need 3500.  At the border of two items the state's 128 KB are on the chain too.
+// DRAM would need 3500.  At the border of two items the state's 128 KB are on the chain too;
+// they are brought into L2 ahead by warp 13 (61 slots of 128 tokens: 165 us without, 135 with).
 //
 // Few (slot, head) pairs and many tokens: the tokens are split into segments.  A first
 // launch computes what each segment adds to the state (k and v only), a second one joins the
@@ -279,7 +280,7 @@ __global__ void __launch_bounds__(kLtThreads, 1)
     };
     auto fetch_row = [&](Cursor &c) {
         if (c.i >= p.items) return;
-        const int b = (int)(c.i / segs / p.nc / p.H);
+        const int b = c.i / segs / p.nc / p.H;
         c.slot = b;
         c.len = T;
         if (p.slot_idx) asm volatile("ld.global.nc.b32 %0, [%1];" : "=r"(c.slot) : "l"(p.slot_idx + b));
@@ -292,11 +293,12 @@ __global__ void __launch_bounds__(kLtThreads, 1)
     };
     auto item_at = [&](const Cursor &c) {
         LtItem x;
-        x.seg = c.i % segs;
-        x.index = c.i / segs;
-        x.c = (int)(x.index % p.nc);
-        x.h = (int)(x.index / p.nc % p.H);
-        x.b = (int)(x.index / p.nc / p.H);
+        const int index = c.i / segs, row = index / p.nc;
+        x.seg = c.i - index * segs;
+        x.index = index;
+        x.c = index - row * p.nc;
+        x.b = row / p.H;
+        x.h = row - x.b * p.H;
         x.slot = c.slot;
         x.len = min(max(c.len, 0), T);
         x.t_begin = x.seg * p.seg_len;
@@ -393,16 +395,6 @@ __global__ void __launch_bounds__(kLtThreads, 1)
                 if (u > 0 && !wait(bar_o1, u - 1)) break;
                 write_parts();
                 clear_rows(x);
-                if (cur.i < p.items) {  // the next item's state into L2 while this one is worked on
-                    const LtItem y = item_at(cur);
-                    const bool whole = y.seg == 0 && y.t_end == y.len;
-                    const float *const from = whole ? p.state + ((y.slot * p.H + y.h) * DK) * (int64_t)p.dv + y.c * 128
-                                                    : p.part + (y.index * p.nseg + y.seg) * DK * 128;
-                    const int lines = whole ? min(4, (p.dv - y.c * 128) / 32) : 4;  // of 128 bytes in a row
-                    for (int l = tid; l < DK * 4 && y.live; l += 256)
-                        if ((l & 3) < lines)
-                            asm volatile("prefetch.global.L2 [%0];" ::"l"(from + (int64_t)(l >> 2) * (whole ? p.dv : 128) + 32 * (l & 3)));
-                }
             }
 #pragma unroll 1
             for (int t0 = x.t_begin; t0 < x.t_end; t0 += kLtC, ++u) {
@@ -607,6 +599,15 @@ __global__ void __launch_bounds__(kLtThreads, 1)
                     __syncwarp();
                 }
                 copy_piece();
+                // its state into L2, up to three items ahead of its use (a segment's is there from the join)
+                if (!STATE && nx.t == nx.x.t_begin && p.nseg == 1) {
+                    const LtItem &x = nx.x;
+                    const float *const from = p.state + ((x.slot * p.H + x.h) * DK + (lane >> 2)) * (int64_t)p.dv + x.c * 128 + 32 * (lane & 3);
+                    if (FULL || x.c * 128 + 32 * (lane & 3) < p.dv) {
+#pragma unroll 4
+                        for (int r = 0; r < DK; r += 8) asm volatile("prefetch.global.L2 [%0];" ::"l"(from + (int64_t)r * p.dv));
+                    }
+                }
             }
             if (STATE || warp == 9) sum_gates();
             advance();
