@@ -17,7 +17,7 @@
 // enter as three bf16 parts that hold them exactly.  Accumulation and the state are FP32.  G
 // is summed as pairs of floats, so that G_i - G_j keeps its digits where both are large
 // (fast decays).  Measured against 64 bits: 2e-7 of o.  Two parts instead of three (half the
-// tensor memory, two CTAs per SM) took 204 and 255 us where this takes 209 and 270 (64
+// tensor memory, two CTAs per SM) took 204 and 255 us where this takes 209 and 263 (64
 // ragged prompts of up to 256 tokens, one of 16381; 32 heads, d = 128), at 2.9e-6.
 //
 // Sixteen warps in two groups that meet only at mbarriers.  Warps 0-7 hold the state: they
@@ -57,6 +57,8 @@ constexpr uint32_t kLtG = 0, kLtO1 = 64, kLtO2 = 128, kLtD = 192, kLtS = 320;
 constexpr int kLtStages = 3;
 constexpr int kLtGates = 4;  // a piece's sums may be read while the copies of the third piece after it start
 
+constexpr int kLtSorted = 256;  // rows at most that are taken by length
+
 template <int DK, bool STATE>
 struct LtSmem {  // bytes from the base of the dynamic shared memory
     static constexpr int tile = kLtC * DK * 2;
@@ -72,7 +74,9 @@ struct LtSmem {  // bytes from the base of the dynamic shared memory
     static constexpr int gbuf = 512 + 256;
     static constexpr int bar = g + kLtGates * gbuf;  // mbarriers, the tensor-memory address
     static constexpr int zero = bar + 160;  // 512 bytes: an output row past a row's length
-    static constexpr int bytes = zero + 512;
+    static constexpr int order = zero + 512;  // rows by falling length: 16 bits each
+    static constexpr int bytes = order + (STATE ? 0 : 2 * kLtSorted);
+    static_assert(STATE || 4 * kLtSorted <= 3 * ppart, "pieces of the rows");
 };
 
 struct LinTcParams {
@@ -85,6 +89,7 @@ struct LinTcParams {
     float *part_dec;  // [batch * H * nc][nseg]: the decay of segment s - 1
     int32_t H, Hqk, dv, nc, T, g_per_head;
     int32_t nseg, seg_len, items;  // items: with their segments
+    int32_t sorted;                // rows to take by length (0: in their order)
     uint32_t *status;
 };
 
@@ -257,6 +262,20 @@ __global__ void __launch_bounds__(kLtThreads, 1)
         mbar_init(bar_or, 32 * 7);  // warps 8-15 but 12
         fence_mbar_init();
     }
+    // Rows of different lengths: the long ones first, and every other round of items backwards, so that
+    // the CTAs end together.
+    if (!STATE && p.sorted) {
+        uint32_t *const pieces = reinterpret_cast<uint32_t *>(smem + M::p);  // of the rows, where P will be
+        if (tid < p.sorted) pieces[tid] = (uint32_t)(min(max(p.lengths[tid], 0), p.T) + kLtC - 1) / kLtC;
+        __syncthreads();
+        if (tid < p.sorted) {
+            const uint32_t own = pieces[tid];
+            int before = 0;
+#pragma unroll 4
+            for (int r = 0; r < p.sorted; ++r) before += pieces[r] > own || (pieces[r] == own && r < tid);
+            reinterpret_cast<uint16_t *>(smem + M::order)[before] = (uint16_t)tid;
+        }
+    }
     if (tid >= 480) {
         sts128(sb + M::zero + 16 * (tid - 480), make_uint4(0u, 0u, 0u, 0u));
         fence_proxy_async_smem();
@@ -276,18 +295,19 @@ __global__ void __launch_bounds__(kLtThreads, 1)
     const int T = p.T, segs = STATE ? p.nseg - 1 : p.nseg;
     // The items of this CTA in order.  A cursor holds the next one's row values, fetched an item ahead.
     struct Cursor {
-        int i, slot, len;
+        int i, step, slot, len;
     };
+    auto row_of = [&](int b) { return !STATE && p.sorted ? (int)reinterpret_cast<const uint16_t *>(smem + M::order)[b] : b; };
     auto fetch_row = [&](Cursor &c) {
         if (c.i >= p.items) return;
-        const int b = c.i / segs / p.nc / p.H;
+        const int b = row_of(c.i / segs / p.nc / p.H);
         c.slot = b;
         c.len = T;
         if (p.slot_idx) asm volatile("ld.global.nc.b32 %0, [%1];" : "=r"(c.slot) : "l"(p.slot_idx + b));
         if (p.lengths) asm volatile("ld.global.nc.b32 %0, [%1];" : "=r"(c.len) : "l"(p.lengths + b));
     };
     auto first_item = [&]() {
-        Cursor c{(int)blockIdx.x, 0, 0};
+        Cursor c{(int)blockIdx.x, 2 * (int)(gridDim.x - blockIdx.x) - 1, 0, 0};
         fetch_row(c);
         return c;
     };
@@ -297,8 +317,9 @@ __global__ void __launch_bounds__(kLtThreads, 1)
         x.seg = c.i - index * segs;
         x.index = index;
         x.c = index - row * p.nc;
-        x.b = row / p.H;
-        x.h = row - x.b * p.H;
+        const int b = row / p.H;
+        x.b = row_of(b);
+        x.h = row - b * p.H;
         x.slot = c.slot;
         x.len = min(max(c.len, 0), T);
         x.t_begin = x.seg * p.seg_len;
@@ -307,7 +328,8 @@ __global__ void __launch_bounds__(kLtThreads, 1)
         return x;
     };
     auto step_item = [&](Cursor &c) {
-        c.i += gridDim.x;
+        c.i += c.step;
+        c.step = 2 * (int)gridDim.x - c.step;
         fetch_row(c);
     };
     auto to_live = [&](Cursor &c) {  // to the next item with work; false: there is none
@@ -900,6 +922,11 @@ cudaError_t launch_lin_tc(LinArgs a, void *workspace, cudaStream_t s) {
     p.g_per_head = a.g_per_head;
     p.nseg = lin_tc_segments(a, &p.seg_len);
     const int64_t items = (int64_t)a.batch * a.H * p.nc;
+    // Rows by length where a CTA has a few items (16 rows of 250 to 1000 tokens, 32 heads: 201 us in
+    // their order, 189 by length; 4 rows, 48 heads: 103 and 89).  With many items the lengths even out
+    // by themselves (200 rows of 75 to 300 tokens, 16 heads: 350 in their order, 357 by length).
+    const int64_t sms = sm_count();
+    p.sorted = a.lengths && p.nseg == 1 && a.batch <= kLtSorted && items > sms && items <= 8 * sms ? (int32_t)a.batch : 0;
     if (p.nseg > 1) {
         p.part = static_cast<float *>(workspace);
         p.part_dec = p.part + items * p.nseg * a.dk * 128;

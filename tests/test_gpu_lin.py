@@ -94,6 +94,17 @@ def test_ragged_rows_ignore_what_stands_past_them(T, dtype):
     _check_chunk(7, T, 2, 1, 64, 64, dtype, "head", lengths=[T, 0, 1, T // 2, T + 9, -3, T - 1], seed=5)
 
 
+@pytest.mark.parametrize("H, dk, dv", [(40, 128, 128), (24, 128, 192), (33, 64, 128)])
+def test_rows_of_many_lengths_in_any_order(H, dk, dv):
+    """More blocks than SMs: rows of equal lengths, empty ones, longer ones than the chunk."""
+    _check_chunk(9, 150, H, H, dk, dv, torch.bfloat16, "token", lengths=[1, 150, 0, 64, 65, 150, -3, 129, 200])
+
+
+@pytest.mark.parametrize("B", [255, 256, 257])
+def test_many_rows_of_many_lengths(B):
+    _check_chunk(B, 70, 3, 3, 64, 64, torch.bfloat16, "token", lengths=[(37 * b) % 73 - 1 for b in range(B)])
+
+
 @pytest.mark.parametrize("B,H,T", [(1, 2, 3000), (3, 5, 1111), (1, 32, 2049)])
 def test_long_prompts_of_few_rows(B, H, T):
     _check_chunk(B, T, H, H, 128, 128, torch.bfloat16, "token", seed=6)
