@@ -75,7 +75,7 @@ __global__ void __launch_bounds__(256) lin_step_kernel(const LinArgs p) {
     float4 x[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) x[r] = S[r * ld];
-    const int64_t qoff = ((int64_t)b * p.Hqk + (h * p.Hqk) / p.H) * DK;
+    const int64_t qoff = ((int64_t)b * p.Hqk + h / (p.H / p.Hqk)) * DK;  // (h H_qk may pass 32 bits)
     if (threadIdx.x < DK) {
         sk[threadIdx.x] = load_in(p.k, qoff + threadIdx.x, BF16);
         sq[threadIdx.x] = load_in(p.q, qoff + threadIdx.x, BF16);

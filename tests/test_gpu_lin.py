@@ -133,6 +133,20 @@ def test_decode_step(H, Hqk, dk, dv, dtype, gate):
     assert torch.equal(pool[others], before[others])
 
 
+@pytest.mark.parametrize("H,Hqk", [(46400, 46400), (66000, 33000)])
+@pytest.mark.parametrize("T", [1, 3])
+def test_head_counts_whose_product_passes_32_bits(H, Hqk, T):
+    ops, pool, idx = _inputs(1, T, H, Hqk, 32, 32, torch.float32, "token", seed=17, slots=1)
+    o_ref, S_ref, oa, Sa = R.lin(pool, **ops)
+    L = damp.Layout(H, Hqk, 32, 32, 0)
+    if T == 1:
+        o = damp.lin_decode_step(L, pool, **{n: t[:, 0].contiguous() for n, t in ops.items()})[:, None]
+    else:
+        o = damp.lin_prefill_chunk(L, pool, **ops)
+    R.check_lin(o, o_ref, oa, T, 32, "o")
+    R.check_lin(pool, S_ref, Sa, T, 32, "S")
+
+
 def test_steps_after_a_chunk_continue_it():
     B, T, H, d = 3, 90, 4, 128
     ops, pool, idx = _inputs(B, T, H, H, d, d, torch.bfloat16, "token", seed=10)
