@@ -116,7 +116,9 @@ typedef enum { DAMP_IN_BF16 = 0, DAMP_IN_FP32 = 1 } damp_in_dtype;
  *   head_map             device int32 [H]: the model head (0 .. H_m-1) of each held head,
  *                        or NULL for the identity (then H_m must equal H)
  * Held head h is model head m = head_map[h] (or h); it reads q/k head floor(m*H_qk/H_m)
- * (GQA; H_m must be a multiple of H_qk), and its per-head operands and outputs are row m
+ * (GQA; H_m must be a multiple of H_qk; the FP32 and packed single-token steps, but not the
+ * row-absmax one, and damp_calib_accumulate want (H_m - 1) H_qk below 2^31: DAMP_ERR_SHAPE),
+ * and its per-head operands and outputs are row m
  * of [*][H_m][...] tensors, while its permutation and packed records are row h of the pool.
  *
  * Head groups.  A layer whose heads protect different numbers of key channels (the

@@ -73,6 +73,9 @@ damp_status check_pool(const void *state, int64_t num_slots, const int32_t *slot
     return DAMP_OK;
 }
 
+// The single-token kernels take the query head of head m as (m H_qk) / H_m in 32 bits.
+bool heads_fit_step(const damp_layout *L) { return (model_heads_of(L) - 1) * L->num_qk_heads <= INT32_MAX; }
+
 cudaError_t launch_step(const StepArgs &a, bool packed, cudaStream_t s, bool waittest = false) {
     if (waittest) return launch_packed_kda_waittest(a, s);
     if (!packed) return launch_fp32_step(a, s);
@@ -107,6 +110,8 @@ damp_status step(const damp_layout *L, void *state, int64_t num_slots, const int
         if (L->head_map) return DAMP_ERR_SHAPE;
     }
     if (uniform && L->k_hi != 0) return DAMP_ERR_SHAPE;
+    // (the row-absmax step goes to a kernel with 64-bit products)
+    if (!heads_fit_step(L) && !(packed && L->lo_format == DAMP_LO_S8_ABSMAX_ROW)) return DAMP_ERR_SHAPE;
     if (in_dtype != DAMP_IN_BF16 && in_dtype != DAMP_IN_FP32) return DAMP_ERR_FORMAT;
     if (waittest && (L->d_k != 128 || L->d_v != 128 || L->k_hi != 10 || L->lo_format != DAMP_LO_U8_AFFINE_G32_H32 ||
                      in_dtype != DAMP_IN_BF16 || L->head_map))
@@ -762,6 +767,7 @@ damp_status damp_calib_accumulate(const damp_layout *layout, float *S, int32_t n
     damp_status st = check_layout(layout);
     if (st != DAMP_OK) return st;
     if (layout->head_map) return DAMP_ERR_SHAPE;  // the trajectories hold every head of the layer
+    if (!heads_fit_step(layout)) return DAMP_ERR_SHAPE;
     if (in_dtype != DAMP_IN_BF16 && in_dtype != DAMP_IN_FP32) return DAMP_ERR_FORMAT;
     if (n_docs < 0 || n_tokens < 0 || every < 1) return DAMP_ERR_SHAPE;
     if (!E_acc || !G_acc) return DAMP_ERR_NULL;

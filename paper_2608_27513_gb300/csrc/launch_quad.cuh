@@ -17,6 +17,7 @@ static cudaError_t launch_quad_rowabs_impl(const StepArgs &a, cudaStream_t strea
     if (a.dk != 128 || a.dv != 128 || !a.in_bf16 || a.fmt != 2) return cudaErrorNotSupported;
     const int64_t units = (int64_t)a.batch * a.H;
     if (units >= (int64_t(1) << 29)) return cudaErrorNotSupported;  // 32-bit unit and tile indices
+    if (((int64_t)a.Hm - 1) * a.Hqk > INT32_MAX) return cudaErrorNotSupported;  // and query heads
     void (*kern)(QuadParams) = nullptr;
     int smem = 0, rec = 0;
 #define DAMP_QFR(KC_)                                                        \

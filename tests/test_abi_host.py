@@ -312,3 +312,24 @@ def test_calib_accumulate_rejects_bad_arguments_before_launch(L):
     c.head_map = fb.ptrs[8]
     assert L.damp_calib_accumulate(ctypes.byref(c), fb[0], 4, 8, fb[1], fb[2], fb[3], fb[4], fb[5], 0, 1, 8, fb[6],
                                    fb[7], None) == 2                   # a head group: not a whole layer
+
+
+def test_steps_refuse_head_counts_whose_product_passes_32_bits(L):
+    """The single-token kernels compute (head x query heads) in 32 bits: 46341^2 is the first
+    square that does not fit."""
+    p = [ctypes.c_void_p((i + 1) << 40) for i in range(8)]  # addresses far apart, never dereferenced
+    SHAPE, n = 2, 46400
+
+    def layout(**kw):
+        return ctypes.byref(_layout(**{**dict(num_heads=n, num_qk_heads=n, d_k=32, d_v=32, k_hi=0), **kw}).c())
+
+    for name in ("damp_gdn_decode_step", "damp_kda_decode_step", "damp_u8_gdn_decode_step", "damp_u8_kda_decode_step"):
+        args = (p[0], 1, None, 1, p[1], p[2], p[3], p[4], p[5], p[6], p[7], 0, None)
+        for fmt in (0, 1, 3, 4, 5):
+            assert getattr(L, name)(layout(lo_format=fmt), *args) == SHAPE
+    for name in ("damp_fp32_gdn_decode_step", "damp_fp32_kda_decode_step"):
+        assert getattr(L, name)(layout(), p[0], 1, None, 1, p[1], p[2], p[3], p[4], p[5], p[6], 0, None) == SHAPE
+    assert L.damp_calib_accumulate(layout(), p[0], 1, 1, p[1], p[2], p[3], p[4], p[5], 0, 0, 1, p[6], p[7], None) == SHAPE
+    # the largest product that fits is not refused for its shape: (H - 1) H_qk = 46340 * 46341 < 2^31
+    args = (p[0], 1, None, 1, p[1], p[2], p[3], p[4], p[5], p[6], None, 0, None)
+    assert L.damp_gdn_decode_step(layout(num_heads=46341, num_qk_heads=46341), *args) == 1  # o is NULL
