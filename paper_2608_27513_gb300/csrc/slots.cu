@@ -251,11 +251,11 @@ cudaError_t launch_zero_slots(SlotArgs p, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     p.slice = 65536;
     const int64_t slices = (largest_slot(p) + p.slice - 1) / p.slice;
-    for (int z0 = 0; z0 < p.n; z0 += 65535) {
+    for (int64_t z0 = 0; z0 < p.n; z0 += 65535) {  // (the last step may pass 2^31)
         SlotArgs q = p;
         q.dst = p.dst + z0;
-        zero_slots_kernel<<<dim3((unsigned)slices, (unsigned)p.n_pools, (unsigned)std::min(65535, p.n - z0)), kSlotThreads, 0,
-                            s>>>(q);
+        zero_slots_kernel<<<dim3((unsigned)slices, (unsigned)p.n_pools, (unsigned)std::min<int64_t>(65535, p.n - z0)),
+                            kSlotThreads, 0, s>>>(q);
     }
     return cudaGetLastError();
 }

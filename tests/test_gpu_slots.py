@@ -175,6 +175,16 @@ def test_offsets_past_32_bits():
     assert not pool[5].any() and not pool[0].any() and torch.equal(pool[4], last)
 
 
+def test_free_lists_up_to_the_last_32_bit_length():
+    pool = _pool(4, 16)
+    want = pool.clone()
+    want[[1, 2]] = 0
+    idx = torch.full(((1 << 31) - 1,), -1, dtype=torch.int32, device=DEV)
+    idx[65535 * 32768 - 1], idx[-1] = 1, 2  # the last entry of a full launch, and the last of all
+    damp.zero_slots(pool, idx)
+    assert torch.equal(pool, want)
+
+
 def test_another_stream_and_a_graph():
     pools = [_pool(20, 20224, 1), _pool(20, 4096, 2)]
     src, dst, live = _i32([3, 4, 5]), _i32([4, 5, 3]), _i32([19, 3, 18, 0])
