@@ -85,8 +85,9 @@ class Server:
         return torch.nn.functional.rms_norm(x, x.shape[-1:]) @ self.head
 
     def prompt(self, tokens, lengths):
-        """Admits requests: prompts [B, T], row b of lengths[b] tokens; all but the last token run."""
+        """Admits requests: prompts [B, T], row b of lengths[b] (1 .. T) tokens; all but the last token run."""
         B = tokens.shape[0]
+        lengths = lengths.clamp(1, tokens.shape[1])
         self.slot_idx = torch.arange(B, dtype=torch.int32, device=self.device)
         damp.zero_slots(self.pools, self.slot_idx)
         self.logits(tokens, lengths=lengths - 1)
@@ -118,7 +119,9 @@ class Server:
                                            temperature=temperature)
         damp.copy_slots(self.pools, saved, self.slot_idx)
         self.logits(chunk, lengths=count)
-        self.last = tokens.gather(1, count.long()[:, None] - 1)
+        # logits that exclude every token give none (count 0): the request stays where it was
+        last = tokens.gather(1, (count.long()[:, None] - 1).clamp(min=0))
+        self.last = torch.where(count[:, None] > 0, last, self.last)
         return tokens, count
 
     def step(self, temperature):

@@ -64,3 +64,24 @@ def test_mixed_layers_finish_and_compact(kinds):
         assert torch.equal(p[s.slot_idx.long()], k)
     tokens, count = s.round(4, temperature[~done].contiguous())
     assert tokens.shape == (5, 5) and bool((count >= 1).all())
+
+
+def test_requests_without_a_token_stay_where_they_were():
+    """Logits that are no numbers exclude every token: nothing is accepted or drawn, and the next
+    round goes on from the same token and state.  Prompt lengths are held to 1 .. T."""
+    from speculative_serving import Server
+    B = 4
+    temperature = torch.full((B,), 0.8, device="cuda")
+    s = Server(("lin", "lin"), slots=B, seed=3)
+    prompts = torch.randint(0, s.vocab, (B, 20), generator=s.gen, device="cuda")
+    s.prompt(prompts, torch.tensor([0, 1, 20, 33], dtype=torch.int32, device="cuda"))
+    assert s.last[:, 0].tolist() == prompts[range(B), [0, 0, 19, 19]].tolist()
+    s.round(3, temperature)
+    head, last, states = s.head, s.last.clone(), [p[s.slot_idx.long()].clone() for p in s.pools]
+    s.head = torch.full_like(head, float("nan"))
+    tokens, count = s.round(3, temperature)
+    assert not count.any() and bool((tokens == -1).all()) and torch.equal(s.last, last)
+    assert all(torch.equal(p[s.slot_idx.long()], t) for p, t in zip(s.pools, states))
+    s.head = head
+    tokens, count = s.round(3, temperature)
+    assert bool((count >= 1).all()) and bool((tokens[:, 0] >= 0).all())
