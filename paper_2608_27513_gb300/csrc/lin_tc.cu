@@ -41,6 +41,7 @@
 #include "prefill_tc.cuh"
 
 #include <algorithm>
+#include <cfloat>
 
 namespace damp {
 
@@ -92,6 +93,10 @@ struct LinTcParams {
     int32_t sorted;                // rows to take by length (0: in their order)
     uint32_t *status;
 };
+// the inputs of the tensor maps, for the outputs of pieces with a value of v that is not finite
+struct LinTcInputs {
+    const __nv_bfloat16 *q, *k, *v;
+};
 
 __device__ __forceinline__ float lt_ex2(float x) {
     float y;
@@ -131,6 +136,11 @@ __device__ __forceinline__ void lt_ld8(uint32_t taddr, float (&v)[8]) {
                  : "memory");
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ float lt_ld1(uint32_t taddr) {
+    uint32_t r;
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\ntcgen05.wait::ld.sync.aligned;" : "=r"(r) : "r"(taddr) : "memory");
+    return __uint_as_float(r);
 }
 __device__ __forceinline__ void lt_st8(uint32_t taddr, const uint32_t (&r)[8]) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr), "r"(r[0]),
@@ -214,6 +224,47 @@ __device__ __forceinline__ Pair add_pair(Pair a, Pair b) {
     return Pair{h, e - (h - s)};
 }
 
+// o_i = e^{G_i} O1_i + sum_{j<=i} e^{G_i - G_j} (q_i.k_j) v_j of tokens i = i0 .. i1-1 of a piece, a
+// sum per lane's value column and no term after i: for pieces with a v_j that is not finite, which the
+// product V^T P^T takes times zero into the outputs before it.  A lane takes the dot products of keys
+// `lane` and 32 + lane.  o: the piece's token 0 in the lane's column `row` of outputs o0.
+template <int DK>
+__device__ __noinline__ void lt_outputs(const LinTcInputs in, int H, int Hqk, int dv, const float *o0, float *o, int row, uint32_t sg,
+                                        uint32_t o1, int i0, int i1, bool on) {
+    const int64_t v_step = (int64_t)H * dv, at = o - o0 - row, t0 = at / v_step;  // token 0 of the piece
+    const int64_t qk_step = (int64_t)Hqk * DK, qk = t0 * qk_step + (at - t0 * v_step) / dv * Hqk / H * DK;
+    const __nv_bfloat16 *const q = in.q + qk, *const k = in.k + qk, *const v = in.v + (o - o0);
+    const int lane = threadIdx.x & 31;
+#pragma unroll 1
+    for (int i = i0; i < i1; ++i) {
+        const float gih = ldsf(sg + 8 * i), gil = ldsf(sg + 8 * i + 4);
+        float sum = ldsf(sg + 512 + 4 * i) * lt_ld1(o1 + i);
+#pragma unroll 1
+        for (int j0 = 0; j0 <= i; j0 += 32) {
+            const int j = min(j0 + lane, i);
+            const uint4 *const qi = reinterpret_cast<const uint4 *>(q + i * qk_step), *const kj = reinterpret_cast<const uint4 *>(k + j * qk_step);
+            float2 dot = make_float2(0.f, 0.f);
+#pragma unroll 4
+            for (int c = 0; c < DK / 8; ++c) {
+                const uint4 a = qi[c], b = kj[c];
+                const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, bw[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    dot = fma2(make_float2(__uint_as_float(aw[e] << 16), __uint_as_float(aw[e] & 0xffff0000u)),
+                               make_float2(__uint_as_float(bw[e] << 16), __uint_as_float(bw[e] & 0xffff0000u)), dot);
+            }
+            const float p = (dot.x + dot.y) * lt_ex2((gih - ldsf(sg + 8 * j)) + (gil - ldsf(sg + 8 * j + 4)));
+            const int n = min(32, i + 1 - j0);
+#pragma unroll 4
+            for (int e = 0; e < n; ++e) {
+                const float pe = __shfl_sync(kFull, p, e);
+                if (on) sum = fmaf(pe, __bfloat162float(v[(j0 + e) * v_step]), sum);
+            }
+        }
+        if (on) o[i * v_step] = sum;
+    }
+}
+
 // A piece of work: one segment of one row, head and 128 value columns
 struct LtItem {
     int b, h, c, seg, len, t_begin, t_end;
@@ -226,7 +277,7 @@ struct LtItem {
 template <int DK, bool STATE, bool FULL>
 __global__ void __launch_bounds__(kLtThreads, 1)
     lin_tc_kernel(const LinTcParams p, const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
-                  const __grid_constant__ CUtensorMap vmap) {
+                  const __grid_constant__ CUtensorMap vmap, const LinTcInputs in) {
     extern __shared__ __align__(1024) uint8_t smem[];
     using M = LtSmem<DK, STATE>;
     constexpr int CELLS = DK / 8;
@@ -730,7 +781,10 @@ __global__ void __launch_bounds__(kLtThreads, 1)
                 float o1[16], o2[16];
                 lt_ld16(tl + kLtO1 + j, o1);
                 lt_ld16(tl + kLtO2 + j, o2);
-                if (j + 16 == j_end) tc_fence_before();
+                // a v_j that is not finite is in every output of the product, in the first one too (looked
+                // for after the combination, with a jump past the rest, which costs the long prompt 262 -> 270 us;
+                // elsewhere in the loop, with d = 64, up to 12 %)
+                const bool bad = (FULL || on) && !(fabsf(o2[0]) <= FLT_MAX);
 #pragma unroll
                 for (int e = 0; e < 16; e += 4) {
                     const uint4 g4 = lds128(eg + 4 * (j + e));
@@ -739,7 +793,19 @@ __global__ void __launch_bounds__(kLtThreads, 1)
                     o1[e + 2] = fmaf(__uint_as_float(g4.z), o1[e + 2], o2[e + 2]);
                     o1[e + 3] = fmaf(__uint_as_float(g4.w), o1[e + 3], o2[e + 3]);
                 }
-                if (j + 16 == j_end) mbar_arrive(bar_or);
+                if (!STATE && __any_sync(kFull, bad)) {
+                    lt_outputs<DK>(in, p.H, p.Hqk, p.dv, p.o, dst, row, gates_of(w), tl + kLtO1, j, min(j + 16, n), FULL || on);
+                    if (j + 16 == j_end) {
+                        tc_fence_before();
+                        mbar_arrive(bar_or);
+                    }
+                    oj += 16 * ostep;
+                    continue;
+                }
+                if (j + 16 == j_end) {
+                    tc_fence_before();
+                    mbar_arrive(bar_or);
+                }
                 const int nh = FULL || on ? n - j : 0;
 #pragma unroll
                 for (int e = 0; e < 16; ++e, oj += ostep)
@@ -865,6 +931,7 @@ cudaError_t lin_tc_map(CUtensorMap *map, const void *base, int channels, int hea
 
 struct LinTcMaps {
     CUtensorMap q, k, v;
+    LinTcInputs in;
 };
 
 template <int DK, bool STATE, bool FULL>
@@ -874,7 +941,7 @@ cudaError_t lin_tc_launch_one(const LinTcParams &p, const LinTcMaps &m, int64_t 
     if (e != cudaSuccess) return e;
     LinTcParams q = p;
     q.items = (int32_t)items;
-    lin_tc_kernel<DK, STATE, FULL><<<(unsigned)std::min<int64_t>(items, sm_count()), kLtThreads, LtSmem<DK, STATE>::bytes, s>>>(q, m.q, m.k, m.v);
+    lin_tc_kernel<DK, STATE, FULL><<<(unsigned)std::min<int64_t>(items, sm_count()), kLtThreads, LtSmem<DK, STATE>::bytes, s>>>(q, m.q, m.k, m.v, m.in);
     return cudaGetLastError();
 }
 
@@ -909,6 +976,7 @@ cudaError_t launch_lin_tc(LinArgs a, void *workspace, cudaStream_t s) {
     p.slot_idx = a.slot_idx;
     p.lengths = a.lengths;
     LinTcMaps m;
+    m.in = LinTcInputs{static_cast<const __nv_bfloat16 *>(a.q), static_cast<const __nv_bfloat16 *>(a.k), static_cast<const __nv_bfloat16 *>(a.v)};
     if ((e = lin_tc_map(&m.q, a.q, a.dk, a.Hqk, a.T, a.batch, a.dk / 64)) != cudaSuccess) return e;
     if ((e = lin_tc_map(&m.k, a.k, a.dk, a.Hqk, a.T, a.batch, a.dk / 64)) != cudaSuccess) return e;
     if ((e = lin_tc_map(&m.v, a.v, a.dv, a.H, a.T, a.batch, 2)) != cudaSuccess) return e;

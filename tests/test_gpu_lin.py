@@ -147,6 +147,36 @@ def test_head_counts_whose_product_passes_32_bits(H, Hqk, T):
     R.check_lin(pool, S_ref, Sa, T, 32, "S")
 
 
+def _check_not_finite(got, want, absolute, T, dk, what):
+    """Values that are not finite stand where the recurrence has them and nowhere else (an
+    infinity may have become a NaN); the others are held to their bounds."""
+    finite = want.isfinite()
+    assert torch.equal(got.isfinite(), finite), what
+    R.check_lin(got[finite], want[finite], absolute[finite], T, dk, what)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T", [1, 9, 17, 64, 150, 700])
+@pytest.mark.parametrize("H,dk,dv", [(2, 128, 128), (3, 64, 64), (2, 128, 192), (2, 64, 128)])
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+def test_values_that_are_not_finite_reach_no_earlier_output(H, dk, dv, T, dtype, bad):
+    """A row with values of v that are not finite in the first, the last and some other tokens, one
+    with a key, one with a query, one with a state that is not, and one without any."""
+    ops, pool, idx = _inputs(6, T, H, H, dk, dv, dtype, "token", seed=18)
+    n = torch.tensor([T, T, T, max(1, T // 2), T, T], dtype=torch.int32, device=DEV)
+    ops["v"][0, T - 1, 0, 3] = ops["v"][0, T // 2, 1, dv - 1] = ops["v"][0, T // 3, 0, 40] = bad
+    ops["v"][0, 0, 1, 33] = bad
+    ops["k"][1, T // 2, 0, 5] = bad
+    ops["q"][2, T // 2, 1, 6] = bad
+    ops["v"][3, int(n[3]):] = bad  # past the row's length
+    pool[idx[4].long(), 0, 7, 8] = bad
+    o_ref, S_ref, oa, Sa = R.lin(pool[idx.long()], **ops, lengths=n)
+    o = damp.lin_prefill_chunk(damp.Layout(H, H, dk, dv, 0), pool, **ops, lengths=n, slot_idx=idx)
+    _check_not_finite(o, o_ref, oa, T, dk, "o")
+    _check_not_finite(pool[idx.long()], S_ref, Sa, T, dk, "S")
+    assert bool(o[5].isfinite().all()) and bool(pool[idx[5].long()].isfinite().all())
+
+
 def test_steps_after_a_chunk_continue_it():
     B, T, H, d = 3, 90, 4, 128
     ops, pool, idx = _inputs(B, T, H, H, d, d, torch.bfloat16, "token", seed=10)
