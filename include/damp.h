@@ -344,7 +344,7 @@ DAMP_API damp_status damp_kda_prefill_chunk(const damp_layout *layout, void *sta
  *   which is what the workspace is for.  The results differ only in FP32 rounding (the FP32
  *   operands of the products keep 16 bits).
  *   A value that is not finite reaches the outputs and state values that depend on it in the
- *   recurrence, and no others; in a chunk an infinity may become a NaN on its way.
+ *   recurrence, and no others; beyond 16 tokens an infinity may become a NaN on its way.
  * slot_idx, num_slots, batch, in_dtype and the status bits as in damp_gdn_decode_step
  * (the outputs of a row with a bad slot are left as they are).
  */

@@ -23,6 +23,7 @@
 #include "damp_internal.h"
 
 #include <algorithm>
+#include <cfloat>
 
 namespace damp {
 
@@ -41,6 +42,15 @@ __device__ __forceinline__ Decay lin_decay(float g) {
     g = lin_gate(g);
     const float a = expf(g);
     return Decay{a, a >= 0.5f && a <= 2.f ? g - log1pf(a - 1.f) : 0.f, g};  // a - 1 is exact
+}
+
+// x with its infinities as the largest finite value, for the remainder: infinity times a remainder of
+// 0 or of the other sign would make a NaN where the recurrence has an infinity (a NaN needs no care, it
+// stays one in the product with a)
+__device__ __forceinline__ float finite(float x) {
+    float y;
+    asm("min.xorsign.abs.f32 %0, %1, %2;" : "=f"(y) : "f"(x), "f"(FLT_MAX));
+    return y;
 }
 
 template <bool BF16>
@@ -89,10 +99,10 @@ __global__ void __launch_bounds__(256) lin_step_kernel(const LinArgs p) {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const float kr = sk[row0 + r * RPI], qr = sq[row0 + r * RPI];
-        x[r].x = fmaf(x[r].x, a, fmaf(x[r].x, lo, kr * v.x));
-        x[r].y = fmaf(x[r].y, a, fmaf(x[r].y, lo, kr * v.y));
-        x[r].z = fmaf(x[r].z, a, fmaf(x[r].z, lo, kr * v.z));
-        x[r].w = fmaf(x[r].w, a, fmaf(x[r].w, lo, kr * v.w));
+        x[r].x = fmaf(x[r].x, a, fmaf(finite(x[r].x), lo, kr * v.x));
+        x[r].y = fmaf(x[r].y, a, fmaf(finite(x[r].y), lo, kr * v.y));
+        x[r].z = fmaf(x[r].z, a, fmaf(finite(x[r].z), lo, kr * v.z));
+        x[r].w = fmaf(x[r].w, a, fmaf(finite(x[r].w), lo, kr * v.w));
         S[r * ld] = x[r];
         o.x = fmaf(x[r].x, qr, o.x);
         o.y = fmaf(x[r].y, qr, o.y);
@@ -233,7 +243,7 @@ __global__ void __launch_bounds__(256, DK * CW <= 8192 ? 3 : 2) lin_chunk_kernel
                 prefetch_l2(static_cast<const char *>(p.v) + ((((int64_t)b2 * T + vt) * p.H + h2) * p.dv + c2 * CW + col) * E);
         }
     }
-    float gates = 0.f;  // of the segment so far
+    float gates = 0.f, lost = 0.f;  // of the segment so far
     int buf = 0;
 #pragma unroll 1
     for (int t0 = t_begin; t0 < t_end; t0 += kGroup, buf ^= NB - 1) {
@@ -246,7 +256,6 @@ __global__ void __launch_bounds__(256, DK * CW <= 8192 ? 3 : 2) lin_chunk_kernel
         __syncthreads();
         if (t0 + kGroup < t_end) fetch(t0 + kGroup);
         const int n = min(kGroup, t_end - t0);
-        float lost = 0.f;
 #pragma unroll
         for (int t = 0; t < kGroup; ++t) {
             if (t < n) {
@@ -281,10 +290,16 @@ __global__ void __launch_bounds__(256, DK * CW <= 8192 ? 3 : 2) lin_chunk_kernel
                 }
             }
         }
+        // What the decays lost to rounding, once it makes a unit of 1: as a factor, which leaves an
+        // infinity what it is
+        const float regain = 1.f + lost;
+        lost -= regain - 1.f;
+        if (regain != 1.f) {
 #pragma unroll
-        for (int r = 0; r < R; ++r) {  // what the group's decays lost to rounding
-            x[r][0] = fma2(x[r][0], splat2(lost), x[r][0]);
-            x[r][1] = fma2(x[r][1], splat2(lost), x[r][1]);
+            for (int r = 0; r < R; ++r) {
+                x[r][0] = mul2(x[r][0], splat2(regain));
+                x[r][1] = mul2(x[r][1], splat2(regain));
+            }
         }
         if (!STATE) {
             __syncthreads();

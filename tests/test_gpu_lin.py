@@ -177,6 +177,41 @@ def test_values_that_are_not_finite_reach_no_earlier_output(H, dk, dv, T, dtype,
     assert bool(o[5].isfinite().all()) and bool(pool[idx[5].long()].isfinite().all())
 
 
+@pytest.mark.parametrize("dtype,T", [(torch.bfloat16, 0), (torch.float32, 0), (torch.bfloat16, 16), (torch.float32, 16),
+                                     (torch.float32, 130)])
+@pytest.mark.parametrize("d", [32, 64, 128])
+@pytest.mark.parametrize("where", ["S", "v", "k", "overflow"])
+def test_infinities_stay_infinities_token_by_token(where, d, dtype, T):
+    """T = 0: the single-token step.  Gates whose decays are rounded up and down."""
+    H, n = 2, max(T, 1)
+    ops, pool, idx = _inputs(2, n, H, H, d, d, dtype, "token", seed=19)
+    ops["g"] = -0.02 * torch.rand(2, n, H, device=DEV, generator=torch.Generator(device=DEV).manual_seed(19))
+    ops["k"], ops["q"] = ops["k"].abs(), ops["q"].abs() + 1e-3  # no difference of two infinities
+    if where == "S":
+        pool[idx[0].long(), :, 3, 5], pool[idx[0].long(), 1, 7, 6] = math.inf, -math.inf
+    elif where == "overflow":  # beyond the largest finite value after the first token
+        pool[idx[0].long(), :, 3, 5] = 3.4e38
+        ops["k"][0, 0, :, 3], ops["v"][0, 0, :, 5] = 1.0, 2e38
+    else:
+        ops[where][0, n // 2, :, 5] = math.inf
+        if where == "k":
+            ops["v"] = ops["v"].abs()
+    o_ref, S_ref, _, _ = R.lin(pool[idx.long()], **ops)
+    if where == "overflow":  # float64 does not overflow
+        S_ref[0, :, 3, 5] = math.inf
+    L = damp.Layout(H, H, d, d, 0)
+    if T:
+        o = damp.lin_prefill_chunk(L, pool, **ops, slot_idx=idx)
+    else:
+        o = damp.lin_decode_step(L, pool, **{name: t[:, 0].contiguous() for name, t in ops.items()}, slot_idx=idx)[:, None]
+    for got, want in ((pool[idx.long()], S_ref), (o, o_ref)):
+        if where == "overflow" and got is o:
+            continue  # q.S may overflow in one order of its terms and not in another
+        for test in (torch.isposinf, torch.isneginf, torch.isnan):
+            assert torch.equal(test(got), test(want)), test
+        assert got.isinf().any()
+
+
 def test_steps_after_a_chunk_continue_it():
     B, T, H, d = 3, 90, 4, 128
     ops, pool, idx = _inputs(B, T, H, H, d, d, torch.bfloat16, "token", seed=10)
