@@ -328,7 +328,7 @@ DAMP_API damp_status damp_kda_prefill_chunk(const damp_layout *layout, void *sta
  *   q, k       [B][H_qk][d_k] of in_dtype, 16-B aligned
  *   v          [B][H][d_v] of in_dtype, 16-B aligned
  *   g          float [B][H] log-decays, or [H] if g_per_head is not 0; 4-B aligned.
- *              e^g is 0 for g < -200 (-inf resets the state).
+ *              e^g is 0 for g < -200 (-inf resets a finite state; damp_zero_slots any).
  *   o          float [B][H][d_v], 4-B aligned; must not overlap the pool or an input
  * damp_lin_prefill_chunk: a chunk of chunk_len = T tokens per row.
  *   q, k, v    [B][T][...]; g float [B][T][H], or [H] if g_per_head is not 0
@@ -342,7 +342,7 @@ DAMP_API damp_status damp_kda_prefill_chunk(const damp_layout *layout, void *sta
  *   Chunks of T > 16 tokens with BF16 inputs, d_k 64 or 128 and d_v a multiple of 64 run
  *   on the tensor cores; with few rows and heads the tokens are split into segments,
  *   which is what the workspace is for.  The results differ only in FP32 rounding (the FP32
- *   operands of the products keep 16 bits).
+ *   operands of the products enter as three BF16 parts that hold them exactly).
  *   A value that is not finite reaches the outputs and state values that depend on it in the
  *   recurrence, and no others; beyond 16 tokens an infinity may become a NaN on its way.
  * slot_idx, num_slots, batch, in_dtype and the status bits as in damp_gdn_decode_step
