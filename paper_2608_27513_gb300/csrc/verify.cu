@@ -174,17 +174,20 @@ __device__ __forceinline__ void clear(Best &a) { a = Best{-INFINITY, -1}; }
 
 // What a thread collects over its vectors of a row, as they are.  Sums are of 2^{x scale - c} with
 // an integer c (the running maximum's exponent, rounded up): x scale - c is one fused operation
-// with one rounding, and c changes by exact factors.
+// with one rounding, and c changes by exact factors.  c is kSoftLow at least (the initial one stands for
+// an empty sum), which leaves tokens masked with a large negative number out of the sum; a row whose
+// maximum is lower than that is summed element by element.
+constexpr float kSoftLow = -0x1p20f;
 struct SoftRun {
     float m, c, s;
-    __device__ __forceinline__ SoftRun() : m(-INFINITY), c(0.f), s(0.f) {}
+    __device__ __forceinline__ SoftRun() : m(-INFINITY), c(-FLT_MAX), s(0.f) {}
     template <bool BF16, int N>
     __device__ __forceinline__ void add(const uint4 (&x)[N], float scale, int, int) {
         constexpr int VE = BF16 ? 8 : 4;
         const float top = largest<BF16>(x);
         if (top > m) {
             m = top;
-            const float c1 = ceilf(top * scale);
+            const float c1 = ceilf(fmaxf(top * scale, kSoftLow));
             s *= ex2(c - c1);
             c = c1;
         }
@@ -202,10 +205,11 @@ struct SoftRun {
         }
         s += (t[0].x + t[0].y) + (t[1].x + t[1].y);
     }
-    // false: an infinity or a NaN, or a maximum too large for whole exponents to be exact
+    // false: an infinity or a NaN beside other elements, or a maximum too large for whole exponents to be
+    // exact
     __device__ __forceinline__ bool result(Soft &a, float scale) const {
-        a = Soft{m, m == -INFINITY ? s : s * ex2(fmaf(-m, scale, c))};
-        return s <= FLT_MAX && (m == -INFINITY || fabsf(m * scale) < 0x1p20f);
+        a = Soft{m, s == 0.f ? 0.f : s * ex2(fmaf(-m, scale, c))};
+        return s <= FLT_MAX && m * scale < 0x1p20f;
     }
 };
 struct BestRun {
@@ -232,6 +236,12 @@ struct BestRun {
         return true;
     }
 };
+// a joined row, with a sum of -1 if its maximum is where the sums are not exact
+__device__ __forceinline__ Soft marked(Soft a, float scale, bool single) {
+    if (!single && a.m > -INFINITY && a.m * scale < kSoftLow) a.s = -1.f;
+    return a;
+}
+__device__ __forceinline__ Best marked(Best a, float, bool) { return a; }
 __device__ __forceinline__ SoftRun run_of(Soft) { return SoftRun(); }
 __device__ __forceinline__ BestRun run_of(Best) { return BestRun(); }
 
@@ -246,9 +256,10 @@ __device__ __forceinline__ int warps_per_row(int rows) {
 // order, into its own slots of the ring (asynchronous 16-byte copies, a group per batch, also
 // empty ones) and reads only those: the copies run on across the ends of rows and no barrier is
 // needed.
+// `single`: element by element in any case.
 template <bool BF16, class P, class Row>
 __device__ __forceinline__ void scan_rows(const Row &row, int rows, int e0, int e1, float scale, P (*red)[kVerWarps],
-                                          uint32_t ring) {
+                                          uint32_t ring, bool single = false) {
     constexpr int VE = BF16 ? 8 : 4, AHEAD = kVerDepth / kVerBatch, SLOT = kVerThreads * 16;
     constexpr uint32_t none = BF16 ? 0xff80ff80u : 0xff800000u;  // -inf
     const int lane = threadIdx.x & 31, per = warps_per_row(rows), groups = kVerWarps / per;
@@ -298,7 +309,7 @@ __device__ __forceinline__ void scan_rows(const Row &row, int rows, int e0, int 
             run.template add<BF16>(x, scale, now.first + v * VE, step * VE);
             copy_next();
         }
-        if (!run.result(a, scale)) {  // again, element by element
+        if (!run.result(a, scale) || single) {  // again, element by element
             clear(a);
             for (int v = tid; v < now.nv; v += step)
                 for (int e = 0; e < VE; ++e) add_one(a, clean(load_in(now.vec + v, e, BF16)), scale, now.first + v * VE + e);
@@ -312,10 +323,10 @@ __device__ __forceinline__ void scan_rows(const Row &row, int rows, int e0, int 
 
 // red[r][0 .. warps-1] of every CTA joined, and over the cluster, into total[r], for `rows` rows;
 // `part` is exchanged (alternate buffers in consecutive calls: a CTA that has passed
-// the next call's barrier has read this call's).
+// the next call's barrier has read this call's).  `single`: of rows scanned so.
 template <class P>
 __device__ __forceinline__ void join_cluster(P (*red)[kVerWarps], P *part, P *total, int rows, int warps, float scale,
-                                             int CL) {
+                                             int CL, bool single = false) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     __syncthreads();
     if (warp < rows) {
@@ -331,7 +342,7 @@ __device__ __forceinline__ void join_cluster(P (*red)[kVerWarps], P *part, P *to
         clear(a);
         if (lane < CL) a = peer(part + warp, (uint32_t)lane);
         a = join_warp<kVerCluster / 2>(a, scale);
-        if (lane == 0) total[warp] = a;
+        if (lane == 0) total[warp] = marked(a, scale, single);
     }
     __syncthreads();
 }
@@ -394,22 +405,27 @@ __global__ void __launch_bounds__(kVerThreads, 4) verify_kernel(const VerifyArgs
         }
     } else {
         const int per = point_mass ? 1 : 2;  // rows of a position
+        bool single = false;                 // this and the later rows are summed element by element
         for (bool done = false; !done; flip ^= 1) {
             const int n = min(round, L + 1 - a), a0 = a;
             const int rows = per * n - (per == 2 && a0 + n > L ? 1 : 0);  // position L has no draft
             fetch_drafts(a0, n);
             scan_rows<BF16>([&](int r) { return per == 1 ? trow(a0 + r) : r & 1 ? drow(a0 + (r >> 1)) : trow(a0 + (r >> 1)); },
-                            rows, e0, e1, scale, red_s, ring);
-            join_cluster(red_s, part_s[flip], total_s, rows, warps_per_row(rows), scale, CL);
+                            rows, e0, e1, scale, red_s, ring, single);
+            join_cluster(red_s, part_s[flip], total_s, rows, warps_per_row(rows), scale, CL, single);
             for (int r = 0; r < n && !done; ++r) {
                 P = total_s[per * r];
+                if (per == 2 && a < L) Q = total_s[2 * r + 1];
+                if (fminf(P.s, Q.s) < 0.f) {  // marked: this position again
+                    single = true;
+                    break;
+                }
                 if (a == L) {
                     done = true;
                     break;
                 }
                 const int x = drafted[flip][r];
                 report(x);
-                if (!point_mass) Q = total_s[2 * r + 1];
                 bool ok = false;
                 if (x >= 0 && P.s > 0.f) {
                     const float px = ex2((logit_t[flip][r] - P.m) * scale) / P.s;

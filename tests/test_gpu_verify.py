@@ -131,6 +131,68 @@ def test_excluded_tokens():
         _check(target, tokens, u, noise, draft)
 
 
+LOW = -(2.0 ** 20) / math.log2(math.e)  # where a row's exponents leave the fast sums
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("kind", ["-1e4", "-1e9", "lowest", "few -1e9", "shift -200", "log-probabilities", "shift -1e9", "border"])
+@pytest.mark.parametrize("T", [1.0, 0.1, 3.0])
+@pytest.mark.parametrize("B,V", [(6, 20011), (40, 999)])
+def test_low_logits(B, V, T, kind, dtype):
+    """Tokens masked with large negative numbers, logits far below 0, whole rows of masked tokens."""
+    target, draft, tokens, u, noise = _inputs(B, 3, V, dtype, seed=13, spread=0.3, scale=2.0 * T)
+    gen = torch.Generator(device=DEV).manual_seed(V)
+    value = {"-1e4": -1e4, "-1e9": -1e9, "few -1e9": -1e9, "lowest": torch.finfo(dtype).min}.get(kind)
+    if value is not None:
+        off = torch.rand(B, 1, V, generator=gen, device=DEV) < (0.01 if kind.startswith("few") else 0.99)
+        off[1] = True  # every token masked: all are equally likely
+        off[2, :, :V // 2] = True
+        target.masked_fill_(off, value), draft.masked_fill_(off, value)
+    elif kind == "log-probabilities":
+        target, draft = (z.float().log_softmax(-1).to(dtype) for z in (target, draft))
+    else:
+        down = {"shift -200": -200.0, "shift -1e9": -1e9, "border": LOW * T}[kind]
+        target, draft = (target.float() + down).to(dtype), (draft.float() + down).to(dtype)
+        if kind == "border":  # rows above, across and below
+            target[0], draft[0] = target[0] + 300, draft[0] + 300
+            target[1], draft[1] = target[1] - 300, draft[1] - 300
+    race = torch.empty(B, 3, V, device=DEV).exponential_(generator=gen)
+    tokens = ((draft.float() - draft.float().amax(-1, keepdim=True)) / T - race.log()).argmax(-1).to(torch.int32)
+    _check(target, tokens, u, noise, draft, temperature=torch.full((B,), T, device=DEV))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_low_logits_take_no_longer(dtype):
+    """Masked tokens, shifted logits and log-probabilities at a low temperature are as many bytes and
+    operations as other logits; a quarter more time is left for the clock and the memory."""
+    B, D, V = 32, 3, 65536
+    target, draft, tokens, u, noise = _inputs(B, D, V, dtype, seed=14)
+    off = torch.rand(B, 1, V, device=DEV) < 0.999
+    low = {"as they are": (target, draft, 1.0), "shift -200": (target - 200, draft - 200, 1.0),
+           "log-probabilities": (target.float().log_softmax(-1).to(dtype), draft.float().log_softmax(-1).to(dtype), 0.1)}
+    for value in (-1e4, -1e9, torch.finfo(dtype).min):
+        low[value] = (target.masked_fill(off, value), draft.masked_fill(off, value), 1.0)
+    u = torch.zeros_like(u)  # every draft with a probability is accepted: all rows are read
+    time = {}
+    for name, (t, d, temp) in low.items():
+        x = d.argmax(-1).to(torch.int32)
+        args = dict(draft_logits=d, temperature=torch.full((B,), temp, device=DEV))
+        graph = torch.cuda.CUDAGraph()
+        assert bool((damp.verify_drafts(t, x, u, noise, **args)[1] == D + 1).all())
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph):
+            for _ in range(20):
+                damp.verify_drafts(t, x, u, noise, **args)
+        best = math.inf
+        for _ in range(7):
+            start, end = torch.cuda.Event(True), torch.cuda.Event(True)
+            start.record(), graph.replay(), end.record()
+            torch.cuda.synchronize()
+            best = min(best, start.elapsed_time(end))
+        time[name] = best
+    assert all(t <= 1.25 * time["as they are"] for t in time.values()), time
+
+
 def test_rows_that_exclude_every_token():
     target, draft, tokens, u, noise = _inputs(6, 2, 700, torch.bfloat16, seed=8, spread=0.0)
     target[0] = -math.inf
