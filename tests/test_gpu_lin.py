@@ -111,6 +111,35 @@ def test_long_prompts_of_few_rows(B, H, T):
     _check_chunk(B, T, H, H, 128, 128, torch.bfloat16, "head", lengths=[T - 700] + [T] * (B - 1), seed=7)
 
 
+@pytest.mark.parametrize("dtype,H,Hqk,dk,dv", [(torch.float32, 2, 1, 128, 128), (torch.float32, 2, 2, 64, 64), (torch.bfloat16, 3, 3, 32, 64),
+                                               (torch.bfloat16, 2, 2, 128, 96), (torch.bfloat16, 2, 1, 128, 128),
+                                               (torch.bfloat16, 2, 2, 64, 192)])
+@pytest.mark.parametrize("T", [700, 1111])
+def test_long_rows_end_in_every_segment(T, dtype, H, Hqk, dk, dv):
+    """Few rows and many tokens are split into segments: rows that end in the first one, at the borders
+    of segments (multiples of 8 or 64 tokens), in their middle, and nowhere."""
+    for lengths in ([T, 0, 1, T // 2, T - 1], [T // 2, 64, 65, T // 3, T], [8 * (T // 16), 8 * (T // 24) + 1, 320, 384, 8 * (T // 8)]):
+        _check_chunk(5, T, H, Hqk, dk, dv, dtype, "token", lengths=lengths, seed=20)
+    _check_chunk(3, T, H, Hqk, dk, dv, dtype, "head", lengths=[T - 200, T + 5, -1], seed=21)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("lengths", [None, [900, 500, 900, 31]])
+def test_bad_slots_of_long_rows_are_skipped_and_reported(lengths, dtype):
+    H, d, T = 2, 128, 900
+    ops, pool, _ = _inputs(4, T, H, H, d, d, dtype, "token", seed=22, slots=4)
+    idx = torch.tensor([2, -1, 4, 0], dtype=torch.int32, device=DEV)
+    n = None if lengths is None else torch.tensor(lengths, dtype=torch.int32, device=DEV)
+    before = pool.clone()
+    o_ref, S_ref, oa, Sa = R.lin(pool[[2, 0]], **{name: t[[0, 3]] for name, t in ops.items()}, lengths=None if n is None else n[[0, 3]])
+    o = torch.full((4, T, H, d), 7.0, device=DEV)
+    damp.lin_prefill_chunk(damp.Layout(H, H, d, d, 0), pool, **ops, o=o, lengths=n, slot_idx=idx)
+    assert damp.device_status() == damp.DEV_BAD_SLOT
+    R.check_lin(o[[0, 3]], o_ref, oa, T, d, "o")
+    R.check_lin(pool[[2, 0]], S_ref, Sa, T, d, "S")
+    assert torch.equal(pool[[1, 3]], before[[1, 3]]) and bool((o[1:3] == 7.0).all())
+
+
 def test_many_rows_fill_the_gpu():
     _check_chunk(40, 130, 8, 4, 128, 128, torch.bfloat16, "token", lengths=[(37 * i) % 131 for i in range(40)], seed=8)
 

@@ -240,6 +240,28 @@ def test_emitted_tokens_follow_the_target(with_draft):
     assert bool(((second - p[1]).abs() <= 5 * (p[1] * (1 - p[1]) / m).sqrt()).all())
 
 
+def test_pairs_of_emitted_tokens_follow_the_target():
+    """Of requests whose first draft was accepted, the first token and the second are independent (the
+    second row does not depend on the first token here) and the second follows the target's p_1: every
+    cell of their table is within five standard deviations, and the first token's frequencies among
+    all requests times its acceptance, min(p_0, q_0), too."""
+    n, V, D = 400000, 6, 2
+    gen = torch.Generator(device=DEV).manual_seed(15)
+    row = torch.randn(1, D + 1, V, generator=gen, device=DEV)
+    near = row[:, :D] + torch.randn(1, D, V, generator=gen, device=DEV)
+    target, draft = row.expand(n, D + 1, V).contiguous(), near.expand(n, D, V).contiguous()
+    race = torch.empty(n, D, V, device=DEV).exponential_(generator=gen)
+    tokens = (draft - race.log()).argmax(-1).to(torch.int32)
+    u = torch.rand(n, D, generator=gen, device=DEV)
+    noise = torch.empty(n, V, device=DEV).exponential_(generator=gen)
+    out, count = damp.verify_drafts(target, tokens, u, noise, draft_logits=draft)
+    p, q = row[0].double().softmax(-1).cpu(), near[0].double().softmax(-1).cpu()
+    two = out[count >= 2].cpu().long()
+    table = (V * two[:, 0] + two[:, 1]).bincount(minlength=V * V).double().view(V, V) / n
+    want = torch.minimum(p[0], q[0])[:, None] * p[1][None, :]
+    assert bool(((table - want).abs() <= 5 * (want * (1 - want) / n).sqrt()).all())
+
+
 def test_repeatable_on_another_stream_and_in_a_graph():
     target, draft, tokens, u, noise = _inputs(9, 3, 20001, torch.bfloat16, seed=11)
     run = lambda **kw: damp.verify_drafts(target, tokens, u, noise, draft_logits=draft, **kw)
