@@ -10,15 +10,21 @@
 //     V^T (K~ = e^{G_C - G_j} k_j)                 -> what the piece adds to S^T
 //     V^T P^T, P = (e^{G_i - G_j} q_i.k_j)_{j<=i}  -> O2;  o_i = O2_i + e^{G_i} O1_i
 // One CTA per SM walks over items of 128 value columns of a (slot, head); a last block of 64
-// columns leaves zeros in the upper lanes.  An item's state stays in registers in FP32
+// columns leaves zeros in the upper lanes.  An item's state stays with its threads in FP32
 // (thread = value column and half the key channels); only its operand copy is split.
 //
 // Rounding.  q, k and v are bf16 inputs and enter exactly.  The FP32 operands (S_0, K~, P)
 // enter as three bf16 parts that hold them exactly.  Accumulation and the state are FP32.  G
 // is summed as pairs of floats, so that G_i - G_j keeps its digits where both are large
 // (fast decays).  Measured against 64 bits: 2e-7 of o.  Two parts instead of three (half the
-// tensor memory, two CTAs per SM) took 204 and 255 us where this takes 209 and 263 (64
+// tensor memory, two CTAs per SM) took 204 and 255 us where three took 209 and 263 (64
 // ragged prompts of up to 256 tokens, one of 16381; 32 heads, d = 128), at 2.9e-6.
+//
+// Values that are not finite.  The products are masked by zeros in P, and 0 times a v_j that is
+// not finite is a NaN in the outputs before token j: blocks of outputs with such a value are
+// summed plainly (lt_outputs; 350 us a piece: 64 prompts of 256 tokens take 19 ms if every
+// piece has one).  Everything else is causal as it stands.  A part split off an infinity is a
+// NaN, so an infinite state gives NaN outputs; in the registers it stays infinite.
 //
 // Sixteen warps in two groups that meet only at mbarriers.  Warps 0-7 hold the state: they
 // add what a piece adds and write the next operand parts to tensor memory.  Warps 8-15 turn
@@ -26,11 +32,17 @@
 // warp 12, which has no part in P and K~, issues the products, warp 13 the copies (TMA,
 // 128-byte swizzle, three stages) and warp 9 sums the gates.
 //
-// Bound by latency along the chain of a piece, about 4900 clocks: a product takes 45 clocks
-// with 64 columns and 59 with 128, which makes 2700 for the piece's 56, the splits about 2000
-// in each group (9 operations per pair of values), and the two wait for each other in turn;
-// DRAM would need 3500.  At the border of two items the state's 128 KB are on the chain too;
-// they are brought into L2 ahead by warp 13 (61 slots of 128 tokens: 165 us without, 135 with).
+// Bound by latency along two chains (d = 128, 32 heads, 250 rows: 53 items per SM; 1.94 GHz).
+// A further piece of an item takes 3.2 us, 6200 clocks (rows of 256 and 512 tokens: 880 and
+// 1559 us): a product takes 45 clocks with 64 columns and 59 with 128, which makes 2700 for the
+// piece's 56, the splits about 2000 in each group (9 operations per pair of values), and the two
+// wait for each other in turn; DRAM would need 1.8 us.  The border of two items takes another 3
+// to 5 us (rows of 64 tokens, one piece: 437 us, 8.2 us an item; of 128: 506, 9.5), more than
+// half of the time of short rows: warps 0-7 store 64 values per thread, load 64 and split them
+// while the products wait; DRAM would need 2.9 us for the 128 KB.  The next states are brought
+// into L2 ahead by warp 13 (61 slots of 128 tokens: 139 us without, 131 with; of 17: 105 and 88).
+// At d = 128 the 128 registers of a thread do not hold a role's values all the time: 372 bytes
+// of spill stores and 372 of loads (`-Xptxas -v`; d = 64: 12 and 4).
 //
 // Few (slot, head) pairs and many tokens: the tokens are split into segments.  A first
 // launch computes what each segment adds to the state (k and v only), a second one joins the
@@ -953,8 +965,8 @@ cudaError_t lin_tc_launch(const LinTcParams &p, const LinTcMaps &m, int dk, int6
 
 }  // namespace
 
-// From 17 tokens on (61 rows of 32 heads, d = 128: 83 us token by token against 106 at T = 16, 118
-// against 110 at T = 24; two rows: 10.8 against 9.5 at T = 16).
+// From 17 tokens on (61 rows of 32 heads, d = 128: 84 us token by token against 87 at T = 16, 118
+// against 89 at T = 24; two rows: 9.3 against 9.5 at T = 16).
 bool lin_tc_takes(const LinArgs &a) {
     return a.in_bf16 && (a.dk == 64 || a.dk == 128) && a.dv % 64 == 0 && a.T > 16;
 }
@@ -990,9 +1002,9 @@ cudaError_t launch_lin_tc(LinArgs a, void *workspace, cudaStream_t s) {
     p.g_per_head = a.g_per_head;
     p.nseg = lin_tc_segments(a, &p.seg_len);
     const int64_t items = (int64_t)a.batch * a.H * p.nc;
-    // Rows by length where a CTA has a few items (16 rows of 250 to 1000 tokens, 32 heads: 201 us in
-    // their order, 189 by length; 4 rows, 48 heads: 103 and 89).  With many items the lengths even out
-    // by themselves (200 rows of 75 to 300 tokens, 16 heads: 350 in their order, 357 by length).
+    // Rows by length where a CTA has a few items (16 rows of 250 to 1000 tokens, 32 heads: 189 us in
+    // their order, 183 by length; 4 rows, 48 heads: 95 and 89; but 24 rows of 128 to 512 tokens, 32 heads:
+    // 144 and 151).  With many items the lengths even out by themselves (200 rows of 75 to 300 tokens, 16 heads: 350 in their order, 357 by length).
     const int64_t sms = sm_count();
     p.sorted = a.lengths && p.nseg == 1 && a.batch <= kLtSorted && items > sms && items <= 8 * sms ? (int32_t)a.batch : 0;
     if (p.nseg > 1) {

@@ -19,8 +19,11 @@
 // rejection.  With many requests R = 1: rows after a rejection are not read.  With few, the
 // time is latency and all positions share a round.  Bound by the chain of rounds of a request,
 // with the bytes of the rows needed next: 256 requests of 3 drafts, V = 151552, bf16 take
-// 138 us (3.8 TB/s), of which the race is 50; 61 of 5 drafts, V = 100003, 50 us (two in a
-// round); one of 4 drafts, V = 32000, FP32, 12.5 us.
+// 135 us (3.8 TB/s), of which the race is 50; 61 of 5 drafts, V = 100003, 50 us (two in a
+// round); one of 4 drafts, V = 32000, FP32, 12.7 us.  Tokens masked with a large negative number,
+// shifted logits and log-probabilities take as long (64 of 3 drafts, V = 100000: 41 us each).
+// Rows whose largest logit is infinite or more than 727000 temperatures (2^20 in base 2) from 0 are
+// summed element by element after the fast pass, at about twice the time, as are parts with NaN.
 //
 // The race reads its target row again (from L2) and the noise; p_t >= r_t, so a token whose
 // p_t / noise_t does not reach the best score of its CTA so far cannot win, and only for the
@@ -606,10 +609,10 @@ cudaError_t launch_verify(VerifyArgs p, cudaStream_t s) {
     const cudaError_t e = symbol_address_cached(&g_status_verify, cache, &p.status);
     if (e != cudaSuccess) return e;
     // CTAs per request: 8 while there are at most 8 CTAs per SM, parts of 2048 tokens at least (256
-    // requests of 3 drafts, V = 151552: 4 CTAs 133 us, 2 CTAs 141, 8 CTAs 151).  Positions of a round:
-    // one where the CTAs fill the GPU (the same: 133 us, two 138, four 148), up to four where the time
-    // is latency (one request of 4 drafts, V = 32000: four 12.7 us, one 16.7; 61 requests of 5 drafts,
-    // V = 100003: two 49.6 us, one 56.2).
+    // requests of 3 drafts, V = 151552: 4 CTAs 135 us, 2 CTAs 148, 8 CTAs 151).  Positions of a round:
+    // one where the CTAs fill the GPU (the same: 135 us, two 139, four 151), up to four where the time
+    // is latency (one request of 4 drafts, V = 32000: four 12.7 us, one 16.5; 61 requests of 5 drafts,
+    // V = 100003: two 50.5 us, one 56.8).
     const int64_t sms = sm_count();
     int CL = kVerCluster;
     while (CL > 1 && (p.batch * (int64_t)CL > 8 * sms || p.vocab / CL < 2048)) CL /= 2;
