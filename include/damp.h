@@ -345,6 +345,7 @@ DAMP_API damp_status damp_kda_prefill_chunk(const damp_layout *layout, void *sta
  *   operands of the products enter as three BF16 parts that hold them exactly).
  *   A value that is not finite reaches the outputs and state values that depend on it in the
  *   recurrence, and no others; beyond 16 tokens an infinity may become a NaN on its way.
+ *   (A decay e^g is infinite from g = 89 on; beyond 16 tokens gates are summed first.)
  * slot_idx, num_slots, batch, in_dtype and the status bits as in damp_gdn_decode_step
  * (the outputs of a row with a bad slot are left as they are).
  */

@@ -93,7 +93,7 @@ __global__ void __launch_bounds__(256) lin_step_kernel(const LinArgs p) {
     const int64_t voff = ((int64_t)b * p.H + h) * p.dv + c * CW + col;
     const float4 v = load_in4<BF16>(p.v, voff);
     const Decay d = lin_decay(p.g[p.g_per_head ? h : (int64_t)b * p.H + h]);
-    const float a = d.a, lo = a * d.lo;
+    const float a = d.a, lo = fminf(a, 2.f) * d.lo;  // (there is a remainder up to 2, and a may be infinite)
     __syncthreads();
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll

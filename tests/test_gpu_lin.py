@@ -241,6 +241,32 @@ def test_infinities_stay_infinities_token_by_token(where, d, dtype, T):
         assert got.isinf().any()
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T", [0, 1, 5, 16, 40, 150])
+@pytest.mark.parametrize("gate", [100.0, math.inf, math.nan])
+def test_gates_beyond_the_largest_number(gate, T, dtype):
+    """e^g is infinite in FP32 from g = 89 on: the state of that head becomes infinite with its
+    signs (T = 0: the single-token step), or a NaN for a gate that is one; the other head is untouched.
+    On the tensor cores the gates are summed first, and with the later decays e^100 is in range again."""
+    H, d, n = 2, 64, max(T, 1)
+    if gate == 100.0 and T > 16 and dtype == torch.bfloat16:
+        pytest.skip("the sum of the gates is in range")
+    ops, pool, idx = _inputs(2, n, H, H, d, d, dtype, "token", seed=23)
+    ops["g"][0, n // 2, 1] = gate
+    o_ref, S_ref, oa, Sa = R.lin(pool[idx.long()], **{**ops, "g": torch.where(ops["g"] > 89, math.inf, ops["g"])})
+    L = damp.Layout(H, H, d, d, 0)
+    if T:
+        o = damp.lin_prefill_chunk(L, pool, **ops, slot_idx=idx)
+    else:
+        o = damp.lin_decode_step(L, pool, **{name: t[:, 0].contiguous() for name, t in ops.items()}, slot_idx=idx)[:, None]
+    S = pool[idx.long()]
+    for test in (torch.isposinf, torch.isneginf, torch.isnan) if T <= 16 else ():
+        assert torch.equal(test(S), test(S_ref))
+    _check_not_finite(o, o_ref, oa, n, d, "o")
+    _check_not_finite(S, S_ref, Sa, n, d, "S")
+    assert not S[0, 1].isfinite().any() and bool(S[0, 0].isfinite().all())
+
+
 def test_steps_after_a_chunk_continue_it():
     B, T, H, d = 3, 90, 4, 128
     ops, pool, idx = _inputs(B, T, H, H, d, d, torch.bfloat16, "token", seed=10)
