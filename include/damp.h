@@ -102,6 +102,7 @@ typedef enum { DAMP_IN_BF16 = 0, DAMP_IN_FP32 = 1 } damp_in_dtype;
 #define DAMP_DEV_BAD_SLOT 2u
 #define DAMP_DEV_BAD_HEAD 4u
 #define DAMP_DEV_BAD_TOKEN 8u
+#define DAMP_DEV_NOT_FINITE 16u
 
 /*
  * Shape of one linear-attention layer's state (Sec. 3.1; Sec. 5.1 "Key-channel budget").
@@ -421,6 +422,102 @@ DAMP_API damp_status damp_verify_drafts(const void *target_logits, const void *d
                                         const int32_t *draft_len, int32_t n_draft, const float *u, const float *noise,
                                         const float *temperature, int32_t batch, int32_t *tokens_out,
                                         int32_t *count_out, void *stream);
+
+/*
+ * Softmax-attention layers between the recurrent ones (hybrid models): rotary positions, an
+ * 8-bit cache of keys and values, attention over it.
+ *
+ * damp_rotary: turns the first rotary_dim values of every head by the token's position.  Pair
+ *   i, (x_i, x_{i + rotary_dim/2}) or with `interleaved` (x_2i, x_{2i+1}), becomes
+ *   scale (a cos t - b sin t, b cos t + a sin t), t = position * freq[i]; the other values of
+ *   a head are copied.  The angle is exact modulo a turn for any position.
+ *   q, k        [tokens][heads or kv_heads][d] of dtype, q_stride / k_stride elements from token
+ *               to token (heads d at least); k may be NULL with kv_heads 0
+ *   positions   int32 [batch][T] (tokens = batch T), or [batch] if positions_per_row is not 0:
+ *               token t of row b is then at positions[b] + t
+ *   freq        double [rotary_dim / 2], radians per position, 8-B aligned
+ *   q_out, k_out  [tokens][heads][d], contiguous; the input itself where that is contiguous too,
+ *               otherwise without overlap with any input
+ *   d 1 .. 1024, rotary_dim even, 2 .. d; up to 1024 heads each; pointers aligned to their
+ *   element (16-B aligned ones with strides of whole 16 bytes run on vectors); up to 2^31 - 1
+ *   tokens.
+ */
+DAMP_API damp_status damp_rotary(const void *q, int64_t q_stride, int32_t heads, const void *k, int64_t k_stride,
+                                 int32_t kv_heads, int32_t d, int32_t dtype, const int32_t *positions,
+                                 int32_t positions_per_row, int32_t batch, int32_t T, const double *freq,
+                                 int32_t rotary_dim, int32_t interleaved, float scale, void *q_out, void *k_out,
+                                 void *stream);
+
+/* Shape of a softmax-attention layer: num_heads query heads (a multiple of num_kv_heads; head h
+ * reads KV head h / (num_heads / num_kv_heads)), up to 65536; d 64, 128 or 256 for keys and values. */
+typedef struct {
+    int32_t num_heads;
+    int32_t num_kv_heads;
+    int32_t d;
+} damp_cache_layout;
+
+/*
+ * The cache: a pool of num_pages pages of 32 tokens.  Page p, KV head h is a record of
+ * 64 d + 16 bytes at (p num_kv_heads + h) (64 d + 16): 32 key rows of d codes, 32 value rows,
+ * the FP32 scales of the keys and of the values, 8 unused bytes.  Code c (uint8) stands for
+ * (c - 128) s.  Chunk m of 16 codes of the row of token t lies at chunk m ^ (h(t) mod d/16),
+ * h(t) = (t & 7) ^ ((t & 1) << 2).  Pages are slots of damp_copy_slots (a shared page is copied
+ * before it is written) and damp_zero_slots.
+ *   cache       the pool, 16-B aligned
+ *   pages       int32 [batch][table]: token j of row b lies in page pages[b][j / 32]; entries of
+ *               pages that hold no token are not read.  A bad one sets DAMP_DEV_BAD_SLOT: its
+ *               tokens are not written, read as zeros, and no query sees them.
+ *   batch       up to 4096; table up to 2^25; num_pages up to 2^31 - 1
+ *
+ * damp_cache_append: writes new tokens at start[b] .. of row b.
+ *   k, v        [batch][T][num_kv_heads][d] of dtype, k_stride / v_stride elements from token to
+ *               token; 16-B aligned, strides multiples of 16 bytes
+ *   start       int32 [batch]: tokens that row b holds (a negative one skips the row and sets
+ *               DAMP_DEV_BAD_SLOT, as do tokens beyond the table)
+ *   lengths     int32 [batch] or NULL: the first min(max(lengths[b], 0), T) of T tokens are new
+ *   For a (page, head), keys or values, with the largest magnitude a of the values written and
+ *   the page's earlier scale s0 (0 if the page has no earlier token):  s = max(a / 127, s0)
+ *   (0 below 2^-126), r = 1 / s, code = 128 + rne(x r); where s > s0 the earlier codes become
+ *   128 + rne((c - 128) (s0 r)).  Each operation is rounded to FP32 (codes depend on how the
+ *   tokens of a page were split into calls, by half a step for each growth).  NaN is stored as
+ *   0, an infinity as the block's largest magnitude; both set DAMP_DEV_NOT_FINITE.
+ *   The pages that a call writes must be distinct.
+ * damp_cache_read: k, v [batch][T][num_kv_heads][d] of dtype (contiguous, 16-B aligned) become
+ *   the values of tokens start[b] + t (start NULL: t), zeros from lengths[b] on (the tokens
+ *   held) and before 0.
+ * damp_cache_attend: o = softmax over the row's tokens of (scale q.k) v.
+ *   q           [batch][T][num_heads][d] of dtype, q_stride elements from token to token; 16-B
+ *               aligned, the stride a multiple of 16 bytes
+ *   lengths     int32 [batch]: tokens held, those of the queries among them (their keys and values
+ *               are appended before); clamped to 0 .. 32 table
+ *   q_lengths   int32 [batch] or NULL (T): queries of each row, clamped to 0 .. T
+ *   scale       positive;  window  0, or the number of tokens that a query sees, its own the last
+ *   o           [batch][T][num_heads][d] of dtype, 16-B aligned: query t of row b is token
+ *               j = lengths[b] - q_lengths[b] + t and sees tokens max(0, j - window + 1) .. j.
+ *               A query that sees none gives zeros, and so do those past q_lengths[b].
+ *   workspace   damp_cache_attend_workspace() bytes, 16-B aligned, of no use to any other call
+ *               while this one runs
+ *   Maxima, sums and outputs are FP32; weights enter the product with the values in FP16 (FP32
+ *   inputs: as two FP16 parts each).  A NaN or infinity in a query reaches its own head's output
+ *   alone.  How rows are split over the GPU depends on the lengths of the batch, and with it the
+ *   last bits.  ceil(T num_heads / num_kv_heads / 16) batch num_kv_heads table must be below 2^31.
+ * Outputs must not overlap the cache or an input.  Integers are 4-B aligned.
+ */
+DAMP_API int64_t damp_cache_page_bytes(const damp_cache_layout *layout); /* all heads; 0 if the layout is invalid */
+DAMP_API damp_status damp_cache_append(const damp_cache_layout *layout, void *cache, int64_t num_pages,
+                                       const int32_t *pages, int32_t table, int32_t batch, int32_t T,
+                                       const int32_t *start, const int32_t *lengths, const void *k, int64_t k_stride,
+                                       const void *v, int64_t v_stride, int32_t dtype, void *stream);
+DAMP_API damp_status damp_cache_read(const damp_cache_layout *layout, const void *cache, int64_t num_pages,
+                                     const int32_t *pages, int32_t table, int32_t batch, int32_t T,
+                                     const int32_t *start, const int32_t *lengths, void *k, void *v, int32_t dtype,
+                                     void *stream);
+DAMP_API damp_status damp_cache_attend(const damp_cache_layout *layout, const void *cache, int64_t num_pages,
+                                       const int32_t *pages, int32_t table, int32_t batch, int32_t T,
+                                       const int32_t *lengths, const int32_t *q_lengths, const void *q,
+                                       int64_t q_stride, float scale, int32_t window, void *o, int32_t dtype,
+                                       void *workspace, int64_t workspace_bytes, void *stream);
+DAMP_API int64_t damp_cache_attend_workspace(const damp_cache_layout *layout, int32_t batch, int32_t T, int32_t dtype);
 
 /*
  * Write FP32 states into the packed cache: the hand-off from an FP32 prefix

@@ -16,6 +16,11 @@ Linear attention with a decay per head and no delta rule runs on an FP32 pool
 compact_slots move whole slots of all layers' pools, packed or FP32; verify_drafts accepts
 drafted tokens, and its counts are the lengths with which a chunk replays them.
 
+The softmax-attention layers of hybrid models keep their keys and values in 8 bits, in pages of
+32 tokens (CacheLayout, new_cache): rotary turns q and k, cache_append writes new tokens,
+cache_attend attends over the cache (one token a row, drafted tokens, prompts), cache_read
+reads values back.  Pages are slots of copy_slots and zero_slots.
+
 A layer whose heads keep different numbers of FP16 key channels (the decay-tiered
 allocation of App. E) is a list of head groups (`head_groups`), one uniform layout,
 pool and permutation table per K_hi, each with a head map into the layer's heads.
@@ -25,7 +30,7 @@ from __future__ import annotations
 import ctypes
 from dataclasses import dataclass, field
 
-from ._lib import DampLayout, DampLibraryError, lib
+from ._lib import DampCacheLayout, DampLayout, DampLibraryError, lib
 
 __all__ = [
     "Layout", "DampError", "DampLibraryError", "LO_U8_AFFINE_G32_H32", "LO_U8_AFFINE_G32", "LO_S8_ABSMAX_ROW", "LO_U4_AFFINE_G32_H32",
@@ -36,7 +41,8 @@ __all__ = [
     "pack_tiers", "unpack_tiers", "device_status", "version", "DEV_WAIT_TIMEOUT", "DEV_BAD_SLOT", "DEV_BAD_HEAD",
     "head_groups", "test_kda_wait_timeout", "gdn_decode_step_groups", "kda_decode_step_groups",
     "calib_accumulate", "lin_decode_step", "lin_prefill_chunk", "copy_slots", "zero_slots", "compact_slots",
-    "verify_drafts", "DEV_BAD_TOKEN",
+    "verify_drafts", "DEV_BAD_TOKEN", "CacheLayout", "CACHE_PAGE", "new_cache", "cache_page_bytes", "cache_append",
+    "cache_read", "cache_attend", "rotary", "rotary_frequencies", "DEV_NOT_FINITE",
 ]
 
 LO_U8_AFFINE_G32_H32 = 0
@@ -51,6 +57,8 @@ DEV_WAIT_TIMEOUT = 1
 DEV_BAD_SLOT = 2
 DEV_BAD_HEAD = 4
 DEV_BAD_TOKEN = 8
+DEV_NOT_FINITE = 16
+CACHE_PAGE = 32  # tokens of a page of the 8-bit cache
 
 
 class DampError(RuntimeError):
@@ -735,6 +743,233 @@ def verify_drafts(target_logits, draft_tokens, u, noise, draft_logits=None, temp
     _check(lib().damp_verify_drafts(*args, _given("tokens", tokens, (B, D1), i32), _given("count", count, (B,), i32),
                                     _stream(stream)), "damp_verify_drafts")
     return tokens, count
+
+
+@dataclass(frozen=True)
+class CacheLayout:
+    """damp_cache_layout: query heads, KV heads (a divisor of them) and the head dimension (64, 128 or
+    256) of a softmax-attention layer."""
+    num_heads: int
+    num_kv_heads: int
+    d: int
+
+    def c(self) -> DampCacheLayout:
+        return DampCacheLayout(self.num_heads, self.num_kv_heads, self.d)
+
+    @property
+    def record_bytes(self) -> int:
+        """Bytes of a page of one KV head."""
+        return 2 * CACHE_PAGE * self.d + 16
+
+
+def cache_page_bytes(layout: CacheLayout) -> int:
+    """Bytes of a page, all KV heads; 0 if the layout is invalid."""
+    return int(lib().damp_cache_page_bytes(ctypes.byref(layout.c())))
+
+
+def new_cache(layout: CacheLayout, num_pages: int, device="cuda"):
+    """A zeroed pool uint8 [num_pages, num_kv_heads, record_bytes] of pages of CACHE_PAGE tokens."""
+    import torch
+    return torch.zeros((num_pages, layout.num_kv_heads, layout.record_bytes), dtype=torch.uint8, device=device)
+
+
+def _token_rows(name, t, B, T, H, d, dtype):
+    """(address, elements from token to token) of t [B, T, H, d]: a tensor whose tokens are evenly
+    spaced (contiguous, or a slice of the heads of a larger projection)."""
+    if t is None:
+        raise ValueError(f"{name} is required")
+    if t.shape != (B, T, H, d) or t.dtype != dtype:
+        _want(name, t, (B, T, H, d), dtype=dtype)
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if t.is_contiguous():
+        return t.data_ptr(), H * d
+    sb, st, sh, sd = t.stride()
+    step = st if T > 1 else sb
+    if (sd != 1 and d > 1) or (sh != d and H > 1) or (T > 1 and B > 1 and sb != T * st) or step < H * d:
+        raise ValueError(f"{name} must hold whole contiguous tokens [heads, d] at an even distance")
+    return t.data_ptr(), step
+
+
+def _same_device(first, *others):
+    """ValueError unless all tensors lie on the current device."""
+    import torch
+    at = torch.cuda.current_device()
+    for t in (first, *others):
+        if t is not None and t.get_device() != at:
+            raise ValueError(f"tensors must lie on the current device ({at}), got device {t.get_device()}")
+
+
+def _float_type(name, t):
+    import torch
+    if t is None or not isinstance(t, torch.Tensor):
+        raise ValueError(f"{name} is required")
+    if t.dtype == torch.bfloat16:
+        return IN_BF16
+    if t.dtype == torch.float32:
+        return IN_FP32
+    raise TypeError(f"{name} must be bfloat16 or float32")
+
+
+def rotary_frequencies(dim, base=10000.0, scaling="none", factor=1.0, trained=4096, turns=(32.0, 1.0), device="cuda"):
+    """(freq, scale) for rotary: float64 [dim / 2] radians per position, base^(-2 i / dim), and the factor
+    of the rotated part.  For contexts `factor` times the `trained` length: "linear" divides every
+    frequency by factor; "ntk" raises the base to base factor^(dim / (dim - 2)), which divides the lowest
+    by factor and leaves the highest; "yarn" divides those that make fewer than turns[1] turns within the
+    trained length, keeps those that make more than turns[0], mixes linearly in i between the two, and
+    gives the scale 0.1 ln(factor) + 1."""
+    import math
+
+    import torch
+    if dim < 2 or dim % 2:
+        raise ValueError("dim must be even, 2 at least")
+    if not base > 1 or not factor >= 1:
+        raise ValueError("base must be above 1, factor 1 at least")
+    i = torch.arange(dim // 2, dtype=torch.float64)
+    if scaling == "ntk":
+        if dim == 2:
+            raise ValueError("ntk scaling needs a dim above 2")
+        base = base * factor ** (dim / (dim - 2))
+    freq, scale = base ** (-2.0 * i / dim), 1.0
+    if scaling == "linear":
+        freq = freq / factor
+    elif scaling == "yarn":
+        at = [dim * math.log(trained / (2 * math.pi * n)) / (2 * math.log(base)) for n in turns]
+        low, high = max(math.floor(at[0]), 0), min(math.ceil(at[1]), dim - 1)
+        stretched = ((i - low) / max(high - low, 0.001)).clamp(0, 1)
+        freq = freq * (1 - stretched) + freq / factor * stretched
+        scale = 0.1 * math.log(factor) + 1.0
+    elif scaling not in ("none", "ntk"):
+        raise ValueError("scaling must be none, linear, ntk or yarn")
+    return freq.to(device), scale
+
+
+def rotary(q, k, positions, freq, interleaved=False, scale=1.0, q_out=None, k_out=None, stream=None):
+    """Rotary positions: q [B, T, H, d] and k [B, T, H_kv, d] (or None) bfloat16 or float32, of each head the
+    first 2 len(freq) values turned by position * freq (float64, rotary_frequencies) and multiplied by scale,
+    the others copied.  positions int32 [B, T], or [B]: of the first token of each row.  q and k may be
+    slices of the heads of one projection.  Returns (q, k) rotated, contiguous; q_out and k_out may be
+    q and k themselves where those are contiguous."""
+    import torch
+    dt = _float_type("q", q)
+    if q.dim() != 4 or (k is not None and k.dim() != 4):
+        raise ValueError("q and k must be [B, T, heads, d] tensors")
+    if freq is None or freq.dim() != 1:
+        raise ValueError("freq must be a float64 tensor [rotary_dim / 2]")
+    if positions is None or positions.dim() not in (1, 2):
+        raise ValueError("positions must be an int32 tensor [B, T] or [B]")
+    B, T, H, d = q.shape
+    Hk = 0 if k is None else k.shape[2]
+    qp, qs = _token_rows("q", q, B, T, H, d, q.dtype)
+    kp, ks = (None, 0) if k is None else _token_rows("k", k, B, T, Hk, d, q.dtype)
+    per_row = positions.dim() == 1
+    pos = _given("positions", positions, (B,) if per_row else (B, T), torch.int32)
+    f = _given("freq", freq, freq.shape, torch.float64)
+    if q_out is None:
+        q_out = _new(q.shape, q.dtype, q, stream)
+    if k is not None and k_out is None:
+        k_out = _new(k.shape, k.dtype, k, stream)
+    if k is None and k_out is not None:
+        raise ValueError("k_out without k")
+    _same_device(q, k, positions, freq, q_out, k_out)
+    _check(lib().damp_rotary(qp, qs, H, kp, ks, Hk, d, dt, pos, per_row, B, T, f, 2 * freq.shape[0], bool(interleaved),
+                             float(scale), _given("q_out", q_out, q.shape, q.dtype),
+                             None if k is None else _given("k_out", k_out, k.shape, k.dtype), _stream(stream)), "damp_rotary")
+    return q_out, k_out
+
+
+def _cache(layout, cache, pages, B):
+    """(pool address, pages, table address, entries of a row) of a cache and its page table."""
+    import torch
+    if cache is None or cache.dim() != 3:
+        raise ValueError("cache must be a [num_pages, num_kv_heads, record_bytes] tensor")
+    pool = _given("cache", cache, (cache.shape[0], layout.num_kv_heads, layout.record_bytes), torch.uint8)
+    if pages is None or pages.dim() != 2:
+        raise ValueError("pages must be an int32 tensor [B, pages of a row]")
+    return pool, cache.shape[0], _given("pages", pages, (B, pages.shape[1]), torch.int32), pages.shape[1]
+
+
+def _per_row(name, t, B):
+    import torch
+    return None if t is None else _given(name, t, (B,), torch.int32)
+
+
+def cache_append(layout, cache, k, v, pages, start, lengths=None, stream=None):
+    """Write new tokens into the 8-bit cache (in place): k, v [B, T, H_kv, d] bfloat16 or float32; token t of
+    row b becomes token start[b] + t of the row (start int32 [B]: the tokens it holds), whose page is
+    pages[b, (start[b] + t) // CACHE_PAGE] (int32 [B, W]).  Row b has lengths[b] new tokens (default T).
+    k and v may be slices of the heads of one projection.  The pages written must be distinct."""
+    dt = _float_type("k", k)
+    if k.dim() != 4:
+        raise ValueError("k must be a [B, T, num_kv_heads, d] tensor")
+    B, T = k.shape[:2]
+    pool, n, table, W = _cache(layout, cache, pages, B)
+    kp, ks = _token_rows("k", k, B, T, layout.num_kv_heads, layout.d, k.dtype)
+    vp, vs = _token_rows("v", v, B, T, layout.num_kv_heads, layout.d, k.dtype)
+    if start is None:
+        raise ValueError("start is required")
+    _same_device(cache, k, v, pages, start, lengths)
+    _check(lib().damp_cache_append(ctypes.byref(layout.c()), pool, n, table, W, B, T, _per_row("start", start, B),
+                                   _per_row("lengths", lengths, B), kp, ks, vp, vs, dt, _stream(stream)), "damp_cache_append")
+
+
+def cache_read(layout, cache, pages, lengths, tokens, start=None, dtype=None, k=None, v=None, stream=None):
+    """Read values back: k, v [B, tokens, H_kv, d] of dtype (default bfloat16) hold tokens start[b] ..
+    start[b] + tokens - 1 of each row (start int32 [B], default 0), zeros from lengths[b] on (the tokens
+    that row b holds)."""
+    import torch
+    if pages is None or pages.dim() != 2:
+        raise ValueError("pages must be an int32 tensor [B, pages of a row]")
+    if lengths is None:
+        raise ValueError("lengths is required")
+    B, T = pages.shape[0], int(tokens)
+    if T < 0:
+        raise ValueError("tokens must not be negative")
+    if dtype is None:
+        dtype = torch.bfloat16 if k is None else k.dtype
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError("dtype must be bfloat16 or float32")
+    pool, n, table, W = _cache(layout, cache, pages, B)
+    shape = (B, T, layout.num_kv_heads, layout.d)
+    if k is None:
+        k = _new(shape, dtype, cache, stream)
+    if v is None:
+        v = _new(shape, dtype, cache, stream)
+    _same_device(cache, pages, lengths, start, k, v)
+    _check(lib().damp_cache_read(ctypes.byref(layout.c()), pool, n, table, W, B, T, _per_row("start", start, B),
+                                 _per_row("lengths", lengths, B), _given("k", k, shape, dtype), _given("v", v, shape, dtype),
+                                 IN_BF16 if dtype == torch.bfloat16 else IN_FP32, _stream(stream)), "damp_cache_read")
+    return k, v
+
+
+def cache_attend(layout, cache, q, pages, lengths, q_lengths=None, scale=None, window=None, o=None, stream=None):
+    """Attention over the 8-bit cache: q [B, T, H, d] bfloat16 or float32; row b holds lengths[b] tokens
+    (int32 [B]), the last q_lengths[b] (default T) of which are its queries' own: query t is token
+    j = lengths[b] - q_lengths[b] + t and sees tokens up to j, the last `window` of them if given.
+    scale: of q.k (default d^-1/2).  Returns o [B, T, H, d] of q's type, zeros past q_lengths[b].  T = 1 is a
+    decode step, a few tokens a draft, many a prompt (append their keys and values first)."""
+    import torch
+    dt = _float_type("q", q)
+    if q.dim() != 4:
+        raise ValueError("q must be a [B, T, num_heads, d] tensor")
+    if lengths is None:
+        raise ValueError("lengths is required")
+    if window is not None and window < 1:
+        raise ValueError("window must be 1 at least")
+    B, T, H, d = q.shape[0], q.shape[1], layout.num_heads, layout.d
+    pool, n, table, W = _cache(layout, cache, pages, B)
+    qp, qs = _token_rows("q", q, B, T, H, d, q.dtype)
+    if o is None:
+        o = _new((B, T, H, d), q.dtype, q, stream)
+    _same_device(cache, q, pages, lengths, q_lengths, o)
+    c, L = ctypes.byref(layout.c()), lib()
+    need = L.damp_cache_attend_workspace(c, B, T, dt)
+    ws = _new((need,), torch.uint8, q, stream) if need else None
+    _check(L.damp_cache_attend(c, pool, n, table, W, B, T, _per_row("lengths", lengths, B),
+                               _per_row("q_lengths", q_lengths, B), qp, qs, d ** -0.5 if scale is None else float(scale),
+                               0 if window is None else min(int(window), (1 << 31) - 1), _given("o", o, (B, T, H, d), q.dtype), dt,
+                               None if ws is None else ws.data_ptr(), need, _stream(stream)), "damp_cache_attend")
+    return o
 
 
 def device_status() -> int:

@@ -22,8 +22,13 @@ class DampLayout(ctypes.Structure):
                 ("model_heads", ctypes.c_int32), ("head_map", ctypes.c_void_p)]
 
 
+class DampCacheLayout(ctypes.Structure):
+    _fields_ = [("num_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32), ("d", ctypes.c_int32)]
+
+
 _P = ctypes.c_void_p
 _L = ctypes.POINTER(DampLayout)
+_C = ctypes.POINTER(DampCacheLayout)
 _i32, _i64 = ctypes.c_int32, ctypes.c_int64
 _status = ctypes.c_int
 
@@ -58,6 +63,12 @@ SIGNATURES = {
     "damp_zero_slots": (_status, [_P, _P, _i32, _i64, _P, _i32, _P]),
     "damp_compact_slots": (_status, [_P, _P, _i32, _i64, _P, _i32, _P, _P]),
     "damp_verify_drafts": (_status, [_P, _P, _i32, _i64, _i32, _P, _P, _i32, _P, _P, _P, _i32, _P, _P, _P]),
+    "damp_rotary": (_status, [_P, _i64, _i32, _P, _i64, _i32, _i32, _i32, _P, _i32, _i32, _i32, _P, _i32, _i32, ctypes.c_float, _P, _P, _P]),
+    "damp_cache_page_bytes": (_i64, [_C]),
+    "damp_cache_append": (_status, [_C, _P, _i64, _P, _i32, _i32, _i32, _P, _P, _P, _i64, _P, _i64, _i32, _P]),
+    "damp_cache_read": (_status, [_C, _P, _i64, _P, _i32, _i32, _i32, _P, _P, _P, _P, _i32, _P]),
+    "damp_cache_attend": (_status, [_C, _P, _i64, _P, _i32, _i32, _i32, _P, _P, _P, _i64, ctypes.c_float, _i32, _P, _i32, _P, _i64, _P]),
+    "damp_cache_attend_workspace": (_i64, [_C, _i32, _i32, _i32]),
     "damp_quantize_state": (_status, [_L, _P, _P, _P, _i64, _P, _i32, _P]),
     "damp_dequantize_state": (_status, [_L, _P, _i64, _P, _i32, _P, _P, _P]),
     "damp_pack_tiers": (_status, [_L, _P, _P, _P, _P, _i64, _P, _i32, _P]),

@@ -1,0 +1,767 @@
+// attend.cu -- attention over the 8-bit cache: o_r = sum_j softmax_j(scale q_r.k_j) v_j.
+//
+// The rows of an item are the (query token, query head) pairs that share a (batch row, KV head), 16
+// or 32 of them; its keys are the pages from the first that its first query sees to the last that
+// its last query sees.  All pages of all items form one sequence, which is cut into equal ranges,
+// one per warp: the work is even whatever the lengths are, and the host need not know them.  A warp
+// keeps one item's running maximum m, sum l and output o in registers and passes over each page
+// once.  An item that lies inside a warp's range is written at once; parts of an item are left in
+// the workspace as (o, m, l) and joined by a second, dependent launch.
+//
+// A warp's pages come by one bulk copy each (keys, values, scales) into a ring of its own; no warp
+// waits for another.  Products run on m16n8k16 with FP16 operands and FP32 sums.  Codes minus 128
+// are exact in FP16.  A query row is scaled by a power of two to below 2^15 and rounded to FP16:
+// BF16 values lose nothing above 2^-39 of the row's largest (FP32: two FP16 parts, 22 bits).
+// Weights p s_v / 2^e, where 2^e is the running power of two above the pages' value scales, lie in
+// 0 .. 1 and enter as FP16 times 2^10 (2^-12 relative down to 2^-24 of the largest; an output in
+// BF16 is rounded to 2^-9 anyway), as two parts for FP32.  Sums, maxima and outputs are FP32.
+//
+// The contraction index of Q K^T is permuted so that a lane's operands are 16 consecutive codes,
+// and the columns of P V so that a lane reads 16 consecutive codes of 4 tokens: 16-byte loads
+// without bank conflicts, one byte permute and one subtraction per two codes.
+#include "cache.cuh"
+
+#include <algorithm>
+#include <cfloat>
+#include <climits>
+
+namespace damp {
+
+static __device__ uint32_t g_status_attend;
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kJoinThreads = 256;
+constexpr int kNoRow = INT_MIN / 2;  // below every token, with a window too (2^30 at most)
+
+// the pages of an item in its row's table
+struct AttItem {
+    int first, pages;
+};
+// the rows' tokens: held tokens, queries
+struct AttRow {
+    int len, n;
+};
+__device__ __forceinline__ AttRow att_row(const AttendArgs &p, int b) {
+    AttRow r;
+    r.len = cache_clamp(p.lengths[b], p.table);
+    r.n = p.q_lengths ? max(0, min(p.q_lengths[b], p.T)) : p.T;
+    return r;
+}
+__device__ __forceinline__ AttItem att_item(const AttendArgs &p, AttRow w, int rt, int R, int G) {
+    const int t0 = rt * R / G, t1 = min(w.n - 1, (rt * R + R - 1) / G);
+    const int hi = w.len - w.n + t1;  // the last token that its last query sees
+    if (t0 > t1 || hi < 0) return AttItem{0, 0};
+    const int lo = p.window ? max(0, w.len - w.n + t0 - (p.window - 1)) : 0;
+    return AttItem{lo / kCachePage, hi / kCachePage - lo / kCachePage + 1};
+}
+__device__ __forceinline__ int att_tiles(int n, int R, int G) { return (n * G + R - 1) / R; }
+
+template <int D, int MT, bool F32>
+struct AttCfg {
+    static constexpr int R = 16 * MT;
+    static constexpr int parts = F32 ? 2 : 1;
+    static constexpr int warps = D == 256 ? 4 : 8;
+    static constexpr int threads = warps * 32;
+    static constexpr int rec = cache_record_bytes(D);
+    static constexpr bool q_smem = MT * (D / 2 + parts * D / 4) > 128;  // registers of o and q
+    static constexpr int qbytes = q_smem ? MT * parts * (D / 16) * 512 : 0;
+    static constexpr int stages = std::min(4, (215000 / warps - qbytes) / (rec + 48));
+    static constexpr int ring = stages * rec;
+    static constexpr int warp_bytes = ring + qbytes + stages * 48;  // 32 bytes about the page, the barrier
+    static_assert(stages >= 2, "ring");
+};
+
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// bytes 0 and 2 (or as `sel` says) of w as FP16 codes minus 128: 0x64 above a byte is 1024 + byte
+__device__ __forceinline__ uint32_t half_codes(uint32_t w, uint32_t sel) {
+    const uint32_t h = prmt(w, 0x64646464u, sel);
+    const __half2 y = __hadd2(*reinterpret_cast<const __half2 *>(&h), __half2(__ushort_as_half(0xE480), __ushort_as_half(0xE480)));  // -1152
+    return *reinterpret_cast<const uint32_t *>(&y);
+}
+__device__ __forceinline__ uint32_t half_pair(float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+// a and b as FP16 parts
+__device__ __forceinline__ void split_pair(float a, float b, uint32_t &hi, uint32_t &lo) {
+    const __half2 h = __floats2half2_rn(a, b);
+    const float2 f = __half22float2(h);
+    hi = *reinterpret_cast<const uint32_t *>(&h);
+    lo = half_pair(a - f.x, b - f.y);
+}
+__device__ __forceinline__ uint2 lds64(uint32_t a) {
+    uint2 v;
+    asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
+    return v;
+}
+__device__ __forceinline__ float quad_max(float x) {
+    x = fmaxf(x, __shfl_xor_sync(kFull, x, 1));
+    return fmaxf(x, __shfl_xor_sync(kFull, x, 2));
+}
+__device__ __forceinline__ float quad_sum(float x) {
+    x += __shfl_xor_sync(kFull, x, 1);
+    return x + __shfl_xor_sync(kFull, x, 2);
+}
+// 16 values of a query row
+template <bool BF>
+__device__ __forceinline__ void load16(const void *p, int64_t at, bool live, float (&x)[16]) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = 0.f;
+    if (!live) return;
+    if (BF) {
+        const uint4 *g = reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(p) + at);
+        const uint4 w[2] = {g[0], g[1]};
+        const uint32_t *u = reinterpret_cast<const uint32_t *>(w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            x[2 * i] = __uint_as_float(u[i] << 16);
+            x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+        }
+    } else {
+        const float4 *g = reinterpret_cast<const float4 *>(static_cast<const float *>(p) + at);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float4 w = g[i];
+            x[4 * i] = w.x, x[4 * i + 1] = w.y, x[4 * i + 2] = w.z, x[4 * i + 3] = w.w;
+        }
+    }
+}
+// N (8 or 16) consecutive outputs
+template <bool BF, int N>
+__device__ __forceinline__ void store_out(void *o, int64_t at, const float (&x)[N]) {
+    if (BF) {
+        uint32_t w[N / 2];
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) {
+            const __nv_bfloat162 z = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+            memcpy(&w[i], &z, 4);
+        }
+#pragma unroll
+        for (int i = 0; i < N / 8; ++i)
+            stg128(static_cast<__nv_bfloat16 *>(o) + at + 8 * i, make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]));
+    } else {
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i)
+            *reinterpret_cast<float4 *>(static_cast<float *>(o) + at + 4 * i) = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+    }
+}
+
+// Workspace: the number of pages before each batch row (a KV head's), then the parts: o [warp][2][R][D] and
+// (m, l) [warp][2][R].  A warp leaves part 1 of an item that starts in its range, else part 0.
+struct AttWork {
+    int32_t *before;
+    float *o;
+    float2 *ml;
+};
+__host__ __device__ inline int64_t att_before_bytes(int batch) { return ((int64_t)(batch + 1) * 4 + 15) & ~15ll; }
+__host__ __device__ inline AttWork att_work(uint8_t *w, int batch, int warps, int R, int D) {
+    AttWork a;
+    a.before = reinterpret_cast<int32_t *>(w);
+    a.o = reinterpret_cast<float *>(w + att_before_bytes(batch));
+    a.ml = reinterpret_cast<float2 *>(a.o + (int64_t)warps * 2 * R * D);
+    return a;
+}
+__device__ __forceinline__ int att_per(int total, int warps) { return max(1, (total + warps - 1) / warps); }
+
+// before[b]: the pages of batch rows before b, for one KV head
+__device__ void att_count(const AttendArgs &p, int R, int G, int32_t *before) {
+    const int tiles = att_tiles(p.T, R, G);
+    for (int b = threadIdx.x; b <= p.batch; b += blockDim.x) before[b] = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < p.batch * tiles; i += blockDim.x) {
+        const int b = i / tiles;
+        const int n = att_item(p, att_row(p, b), i - b * tiles, R, G).pages;
+        if (tiles == 1) before[b + 1] = n;
+        else if (n) atomicAdd(before + b + 1, n);
+    }
+    __syncthreads();
+    if (threadIdx.x < 32) {
+        int sum = 0;
+        for (int at = 0; at < p.batch; at += 32) {
+            const int b = at + threadIdx.x;
+            int n = b < p.batch ? before[b + 1] : 0;
+#pragma unroll
+            for (int i = 1; i < 32; i <<= 1) {
+                const int y = __shfl_up_sync(kFull, n, i);
+                if ((int)threadIdx.x >= i) n += y;
+            }
+            if (b < p.batch) before[b + 1] = sum + n;
+            sum += __shfl_sync(kFull, n, 31);
+        }
+    }
+    __syncthreads();
+}
+
+struct AttPage {  // a page of the sequence, 32 bytes
+    int b, rt, h, page;    // page: in the row's table
+    int begin, count;      // of its item, in the sequence
+    int bad, unused;
+};
+
+template <int D, int MT, bool F32>
+__global__ void __launch_bounds__(AttCfg<D, MT, F32>::threads, 1) attend_kernel(const AttendArgs p) {
+    using C = AttCfg<D, MT, F32>;
+    constexpr int R = C::R, kSteps = D / 16, kCols = D / 8;  // K steps of Q K^T, column tiles of P V
+    constexpr bool BF = !F32;
+    extern __shared__ __align__(128) uint8_t sm[];
+    int32_t *const before = reinterpret_cast<int32_t *>(sm + C::warps * C::warp_bytes);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+    const int G = p.H / p.Hk;
+    uint8_t *const mine = sm + warp * C::warp_bytes;
+    uint8_t *const about = mine + C::ring + C::qbytes;  // [stages] AttPage, then the barriers
+    const uint32_t ring = smem_u32(mine), qs = ring + C::ring, bars = smem_u32(about) + C::stages * 32;
+    if (lane == 0) {
+        for (int i = 0; i < C::stages; ++i) mbar_init(bars + 8 * i, 1);
+        fence_mbar_init();
+    }
+    att_count(p, R, G, before);
+    const int warps = gridDim.x * C::warps;
+    const AttWork work = att_work(p.workspace, p.batch, warps, R, D);
+    if (blockIdx.x == 0)
+        for (int b = threadIdx.x; b <= p.batch; b += C::threads) work.before[b] = before[b];
+    const int total = before[p.batch] * p.Hk, per = att_per(total, warps);
+    // warps of one range after the other lie on different SMs
+    const int range = warp * gridDim.x + blockIdx.x;
+    const int end = min(total, (int)min((int64_t)total, ((int64_t)range + 1) * per));
+    const int begin = (int)min((int64_t)end, (int64_t)range * per);
+
+    // ---- the ring: lane l knows page base + l of the sequence ----
+    int base = begin - 32;
+    AttPage my{};
+    int my_tile = 0;  // where the tile of rows of `my` begins in the sequence
+    const uint8_t *my_record = nullptr;
+    bool failed = false;
+    auto fetch = [&](int f, int stage) {  // all lanes
+        if (f - base >= 32) {
+            base = f;
+            const int x = f + lane;
+            if (x < end) {
+                int lo = 0, hi = p.batch;  // before[lo] Hk <= x < before[hi] Hk
+                while (hi - lo > 1) {
+                    const int mid = (lo + hi) >> 1;
+                    if (before[mid] * p.Hk <= x) lo = mid;
+                    else hi = mid;
+                }
+                const AttRow w = att_row(p, lo);
+                int rt = 0, tile = before[lo] * p.Hk;
+                if (my_record && lo == my.b) rt = my.rt, tile = my_tile;  // pages come in order
+                AttItem it = att_item(p, w, rt, R, G);
+                while (x - tile >= it.pages * p.Hk) {
+                    tile += it.pages * p.Hk;
+                    it = att_item(p, w, ++rt, R, G);
+                }
+                my_tile = tile;
+                const int at = x - tile;
+                my.b = lo;
+                my.rt = rt;
+                my.h = at / it.pages;
+                const int i = at - my.h * it.pages;
+                my.page = it.first + i;
+                my.begin = x - i;
+                my.count = it.pages;
+                const int64_t slot = cache_page(p.pages[(int64_t)lo * p.table + my.page], p.num_pages);
+                my.bad = slot < 0;
+                my_record = p.pool + (slot * p.Hk + my.h) * C::rec;
+            }
+        }
+        if (lane == f - base) {
+            AttPage *const to = reinterpret_cast<AttPage *>(about) + stage;
+            *to = my;
+            const uint32_t bar = bars + 8 * stage;
+            fence_proxy_async_smem();
+            if (my.bad) {
+                atomicOr(p.status, kDevBadSlot);
+                mbar_arrive_expect_tx(bar, 0);
+            } else {
+                mbar_arrive_expect_tx(bar, C::rec);
+                bulk_g2s(ring + stage * C::rec, my_record, C::rec, bar);
+            }
+        }
+    };
+    __syncwarp();
+    for (int i = 0; i < C::stages - 1; ++i)
+        if (begin + i < end) fetch(begin + i, i);
+
+    // ---- the item at hand ----
+    int item = -1;  // its first page in the sequence
+    AttPage now{};
+    float o[MT][kCols][4], m[MT][2], l[MT][2], factor[MT][2];
+    int limit[MT][2];  // the last token that a row sees
+    uint32_t q[C::q_smem ? 1 : MT][C::q_smem ? 1 : C::parts][C::q_smem ? 1 : kSteps][4];
+    int ve = 0;  // exponent field of the outputs' unit
+
+    auto finish = [&]() {
+        const bool whole = now.begin >= begin && now.begin + now.count <= end;
+        const int slot = 2 * range + (now.begin >= begin ? 1 : 0);
+        const float unit = __uint_as_float((uint32_t)ve << 23) * (1.f / 1024.f);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+            for (int hh = 0; hh < 2; ++hh) {
+                const int r = mt * 16 + hh * 8 + g;  // in the item
+                const int row = now.rt * R + r, t = row / G;
+                const float sum = quad_sum(l[mt][hh]);
+                const bool live = limit[mt][hh] != kNoRow;
+                const float y = whole ? (sum == 0.f ? 0.f : unit / sum) : unit;
+                const int64_t to = ((int64_t)(now.b * (int64_t)p.T + t) * p.H + now.h * G + (row - t * G)) * D;
+                float *const part = work.o + ((int64_t)slot * R + r) * D;
+                if (live) {
+                    if (!whole && c == 0) work.ml[(int64_t)slot * R + r] = make_float2(m[mt][hh], sum);
+                    constexpr int N = D == 64 ? 8 : 16;
+#pragma unroll
+                    for (int k = 0; k < 2 * kCols / N; ++k) {  // runs of N columns
+                        const int col = (k >> 1) * 128 + 2 * N * c + N * (k & 1);
+                        float x[N];
+#pragma unroll
+                        for (int i = 0; i < N; ++i) x[i] = o[mt][(k >> 1) * 16 + i][2 * hh + (k & 1)] * y;
+                        if (whole)
+                            store_out<BF, N>(p.o, to + col, x);
+                        else
+                            store_out<false, N>(part, col, x);
+                    }
+                }
+            }
+        }
+    };
+    auto start = [&]() {
+        const AttRow w = att_row(p, now.b);
+        __syncwarp();
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            int64_t from[2];
+            bool live[2];
+            float up[2];
+#pragma unroll
+            for (int hh = 0; hh < 2; ++hh) {
+                const int row = now.rt * R + mt * 16 + hh * 8 + g, t = row / G;
+                live[hh] = t < w.n;
+                limit[mt][hh] = live[hh] ? w.len - w.n + t : kNoRow;
+                from[hh] = ((int64_t)now.b * p.T + t) * p.q_stride + (int64_t)(now.h * G + (row - t * G)) * D;
+                float top = 0.f;
+#pragma unroll
+                for (int j = 0; j < D / 64; ++j) {
+                    float x[16];
+                    load16<BF>(p.q, from[hh] + 16 * (c + 4 * j), live[hh], x);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(x[i]));
+                }
+                top = quad_max(top);
+                const int e = min(max((int)(__float_as_uint(top) >> 23), 15), 254);  // up to below 2^15
+                up[hh] = __uint_as_float((uint32_t)(268 - e) << 23);
+                factor[mt][hh] = p.scale * kLog2e / up[hh];
+                m[mt][hh] = -INFINITY;
+                l[mt][hh] = 0.f;
+            }
+#pragma unroll
+            for (int j = 0; j < D / 64; ++j) {
+                float x[2][16];
+#pragma unroll
+                for (int hh = 0; hh < 2; ++hh) {
+                    load16<BF>(p.q, from[hh] + 16 * (c + 4 * j), live[hh], x[hh]);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[hh][i] *= up[hh];
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    uint32_t hi[4], lo[4];
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+#pragma unroll
+                        for (int hh = 0; hh < 2; ++hh) {
+                            if (F32)
+                                split_pair(x[hh][4 * i + 2 * k], x[hh][4 * i + 2 * k + 1], hi[2 * k + hh], lo[2 * k + hh]);
+                            else
+                                hi[2 * k + hh] = half_pair(x[hh][4 * i + 2 * k], x[hh][4 * i + 2 * k + 1]);
+                        }
+                    }
+                    const int step = 4 * j + i;
+                    if constexpr (C::q_smem) {
+                        const uint32_t at = qs + ((mt * C::parts) * kSteps + step) * 512 + lane * 16;
+                        sts128(at, make_uint4(hi[0], hi[1], hi[2], hi[3]));
+                        if (F32) sts128(at + kSteps * 512, make_uint4(lo[0], lo[1], lo[2], lo[3]));
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            q[mt][0][step][k] = hi[k];
+                            if constexpr (F32) q[mt][1][step][k] = lo[k];
+                        }
+                    }
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < kCols; ++i) o[mt][i][0] = o[mt][i][1] = o[mt][i][2] = o[mt][i][3] = 0.f;
+        }
+        ve = 0;
+        __syncwarp();
+    };
+
+    const int kswz = cache_swizzle(g, D), vswz[2] = {cache_swizzle(2 * c, D), cache_swizzle(2 * c + 1, D)};
+    int stage = 0;
+    uint32_t parity = 0;
+    for (int f = begin; f < end && !failed; ++f) {
+        {
+            const int ahead = f + C::stages - 1;
+            __syncwarp();  // the stage that is filled next has been read by all lanes
+            if (ahead < end) fetch(ahead, stage == 0 ? C::stages - 1 : stage - 1);
+        }
+        if (!mbar_wait_bounded(bars + 8 * stage, parity)) failed = true;
+        if (__any_sync(kFull, failed)) {
+            failed = true;
+            for (int x = f + 1; x < min(end, f + C::stages); ++x) {  // the other copies in flight
+                if (++stage == C::stages) stage = 0, parity ^= 1u;
+                mbar_wait_bounded(bars + 8 * stage, parity);
+            }
+            break;
+        }
+        const AttPage *const info = reinterpret_cast<const AttPage *>(about) + stage;
+        if (info->begin != item) {
+            if (item >= 0) finish();
+            now = *info;
+            item = now.begin;
+            start();
+        }
+        const int page = info->page;
+        const uint32_t kb = ring + stage * C::rec, vb = kb + cache_rows_bytes(D);
+        if (!info->bad) {
+            const float ks = __uint_as_float(lds32(vb + cache_rows_bytes(D))), vs = __uint_as_float(lds32(vb + cache_rows_bytes(D) + 4));
+            float s[MT][4][4];
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int nt = 0; nt < 4; ++nt) s[mt][nt][0] = s[mt][nt][1] = s[mt][nt][2] = s[mt][nt][3] = 0.f;
+#pragma unroll
+            for (int j = 0; j < D / 64; ++j) {
+                uint4 kk[4];
+#pragma unroll
+                for (int nt = 0; nt < 4; ++nt) kk[nt] = lds128(kb + (8 * nt + g) * D + 16 * ((c + 4 * j) ^ kswz));
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int step = 4 * j + i;
+                    uint32_t a[MT][C::parts][4];
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                        for (int pt = 0; pt < C::parts; ++pt) {
+                            if constexpr (C::q_smem) {
+                                const uint4 w = lds128(qs + ((mt * C::parts + pt) * kSteps + step) * 512 + lane * 16);
+                                a[mt][pt][0] = w.x, a[mt][pt][1] = w.y, a[mt][pt][2] = w.z, a[mt][pt][3] = w.w;
+                            } else {
+#pragma unroll
+                                for (int k = 0; k < 4; ++k) a[mt][pt][k] = q[mt][pt][step][k];
+                            }
+                        }
+#pragma unroll
+                    for (int nt = 0; nt < 4; ++nt) {
+                        const uint32_t w = i == 0 ? kk[nt].x : i == 1 ? kk[nt].y : i == 2 ? kk[nt].z : kk[nt].w;
+                        const uint32_t b0 = half_codes(w, 0x4140u), b1 = half_codes(w, 0x4342u);
+#pragma unroll
+                        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                            for (int pt = 0; pt < C::parts; ++pt) mma16816(s[mt][nt], a[mt][pt], b0, b1);
+                    }
+                }
+            }
+            // the outputs' unit: a power of two above every value scale so far
+            const int e = min((int)(__float_as_uint(vs) >> 23) + 1, 253);
+            const int ve_new = max(ve, vs > 0.f ? e : 0);
+            const float wscale = vs * __uint_as_float((uint32_t)(254 - max(ve_new, 1)) << 23) * 1024.f;
+            const int shift = 127 + ve - ve_new;
+            const float vcorr = shift > 0 ? __uint_as_float((uint32_t)shift << 23) : 0.f;
+            bool moved = ve_new != ve;
+            ve = ve_new;
+            const int at = page * kCachePage;
+            bool edge = false;
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int hh = 0; hh < 2; ++hh) {
+                    const int k = limit[mt][hh];
+                    edge = edge || (k != kNoRow && (k < at + kCachePage - 1 || (p.window && k - (p.window - 1) > at)));
+                }
+            const bool masked = __any_sync(kFull, edge);
+            uint32_t pa[MT][C::parts][4][2];  // [column tile][row half]
+            float corr[MT][2];
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+                for (int hh = 0; hh < 2; ++hh) {
+                    const float fac = factor[mt][hh] * ks;
+                    float x[8], top = -INFINITY;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[i] = s[mt][i >> 1][2 * hh + (i & 1)] * fac;
+                    if (masked) {
+                        const int k = limit[mt][hh], from = p.window ? k - (p.window - 1) : 0;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const int token = at + 8 * (i >> 1) + 2 * c + (i & 1);
+                            if (token > k || token < from) x[i] = -INFINITY;
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) top = fmaxf(top, x[i]);
+                    const float mn = fmaxf(m[mt][hh], quad_max(top)), mu = mn == -INFINITY ? 0.f : mn;
+                    corr[mt][hh] = ex2(m[mt][hh] - mu);
+                    moved = moved || mn != m[mt][hh];
+                    m[mt][hh] = mn;
+                    float sum = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        x[i] = ex2(x[i] - mu);
+                        sum += x[i];
+                        x[i] *= wscale;
+                    }
+                    l[mt][hh] = fmaf(l[mt][hh], corr[mt][hh], sum);
+#pragma unroll
+                    for (int nt = 0; nt < 4; ++nt) {
+                        if constexpr (F32)
+                            split_pair(x[2 * nt], x[2 * nt + 1], pa[mt][0][nt][hh], pa[mt][1][nt][hh]);
+                        else
+                            pa[mt][0][nt][hh] = half_pair(x[2 * nt], x[2 * nt + 1]);
+                    }
+                }
+            }
+            if (__any_sync(kFull, moved)) {
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                    for (int i = 0; i < kCols; ++i)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) o[mt][i][k] *= corr[mt][k >> 1] * vcorr;
+            }
+#pragma unroll
+            for (int s2 = 0; s2 < 2; ++s2) {
+                uint32_t a[MT][C::parts][4];
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                    for (int pt = 0; pt < C::parts; ++pt)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) a[mt][pt][k] = pa[mt][pt][2 * s2 + (k >> 1)][k & 1];
+#pragma unroll
+                for (int grp = 0; grp < (D + 127) / 128; ++grp) {
+                    constexpr int W = D == 64 ? 2 : 4;  // words of codes per token
+                    uint32_t w[4][W];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const uint32_t row = vb + (16 * s2 + 8 * (k >> 1) + 2 * c + (k & 1)) * D;
+                        if constexpr (D == 64) {
+                            const uint2 y = lds64(row + 16 * ((g >> 1) ^ vswz[k & 1]) + 8 * (g & 1));
+                            w[k][0] = y.x, w[k][1] = y.y;
+                        } else {
+                            const uint4 y = lds128(row + 16 * ((g + 8 * grp) ^ vswz[k & 1]));
+                            w[k][0] = y.x, w[k][1] = y.y, w[k][W - 2] = y.z, w[k][W - 1] = y.w;
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < W; ++i) {
+                        const uint32_t t0 = prmt(w[0][i], w[1][i], 0x5140u), t1 = prmt(w[0][i], w[1][i], 0x7362u);
+                        const uint32_t u0 = prmt(w[2][i], w[3][i], 0x5140u), u1 = prmt(w[2][i], w[3][i], 0x7362u);
+                        const uint32_t b0[4] = {half_codes(t0, 0x4140u), half_codes(t0, 0x4342u), half_codes(t1, 0x4140u), half_codes(t1, 0x4342u)};
+                        const uint32_t b1[4] = {half_codes(u0, 0x4140u), half_codes(u0, 0x4342u), half_codes(u1, 0x4140u), half_codes(u1, 0x4342u)};
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+#pragma unroll
+                            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                                for (int pt = 0; pt < C::parts; ++pt) mma16816(o[mt][grp * 16 + 4 * i + k], a[mt][pt], b0[k], b1[k]);
+                    }
+                }
+            }
+        }
+        if (++stage == C::stages) {
+            stage = 0;
+            parity ^= 1u;
+        }
+    }
+    if (failed) {
+        if (lane == 0) atomicOr(p.status, kDevWaitTimeout);
+    } else if (item >= 0) {
+        finish();
+    }
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
+// Joins the parts of items that several warps worked on; clears the rows that no warp worked on.
+// One CTA per item, `wpr` warps per row.
+template <int D, bool BF>
+__global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(const AttendArgs p, int R, int warps, int wpr) {
+    constexpr int V = D / 32;  // columns of a lane
+    __shared__ float part[kJoinThreads / 32][D + 2];
+    __shared__ int sums[kJoinThreads / 32];
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const AttWork work = att_work(p.workspace, p.batch, warps, R, D);
+    const int G = p.H / p.Hk, tiles = att_tiles(p.T, R, G);
+    const int h = blockIdx.x % p.Hk, bt = blockIdx.x / p.Hk, rt = bt % tiles, b = bt / tiles;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const AttRow w = att_row(p, b);
+    const AttItem it = att_item(p, w, rt, R, G);
+    int ahead = 0;  // pages of the row's earlier items
+    if (tiles > 1) {
+        for (int i = threadIdx.x; i < rt; i += kJoinThreads) ahead += att_item(p, w, i, R, G).pages;
+        ahead = __reduce_add_sync(kFull, ahead);
+        if (lane == 0) sums[warp] = ahead;
+        __syncthreads();
+        ahead = 0;
+        for (int i = 0; i < kJoinThreads / 32; ++i) ahead += sums[i];
+    }
+    const int total = work.before[p.batch] * p.Hk, per = att_per(total, warps);
+    const int begin = (work.before[b] + ahead) * p.Hk + h * it.pages;
+    const int first = begin / per, last = it.pages ? (begin + it.pages - 1) / per : first;
+    const int team = warp / wpr, mate = warp % wpr, teams = kJoinThreads / 32 / wpr;
+    for (int r0 = blockIdx.y * teams; r0 < R; r0 += gridDim.y * teams) {
+        const int r = r0 + team;
+        const int row = rt * R + r, t = row / G;
+        const bool inside = r < R && t < p.T;
+        const bool empty = t >= w.n || it.pages == 0;
+        if (!inside && wpr == 1) continue;
+        const bool joins = inside && !empty && first != last;
+        float o[V], M = -INFINITY, L = 0.f;
+#pragma unroll
+        for (int i = 0; i < V; ++i) o[i] = 0.f;
+        if (joins) {
+            constexpr int U = 8;
+            for (int x0 = first + mate; x0 <= last; x0 += U * wpr) {
+                float2 ml[U];
+                float y[U][V];
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int x = x0 + u * wpr;
+                    ml[u] = make_float2(-INFINITY, 0.f);
+                    if (x <= last) {
+                        const int64_t slot = 2 * (int64_t)x + (begin >= x * (int64_t)per ? 1 : 0);
+                        ml[u] = work.ml[slot * R + r];
+                        const float *from = work.o + (slot * R + r) * D + lane * V;
+#pragma unroll
+                        for (int i = 0; i < V; i += 2) {
+                            const float2 z = *reinterpret_cast<const float2 *>(from + i);
+                            y[u][i] = z.x;
+                            y[u][i + 1] = z.y;
+                        }
+                    }
+                }
+                float Mn = M;
+#pragma unroll
+                for (int u = 0; u < U; ++u) Mn = fmaxf(Mn, ml[u].x);
+                const float mu = Mn == -INFINITY ? 0.f : Mn, old = ex2(M - mu);
+                M = Mn;
+                L *= old;
+#pragma unroll
+                for (int i = 0; i < V; ++i) o[i] *= old;
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    if (x0 + u * wpr <= last) {
+                        const float f = ex2(ml[u].x - mu);
+                        L = fmaf(ml[u].y, f, L);
+#pragma unroll
+                        for (int i = 0; i < V; ++i) o[i] = fmaf(y[u][i], f, o[i]);
+                    }
+                }
+            }
+        }
+        if (wpr > 1) {
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < V; ++i) part[warp][lane * V + i] = o[i];
+            if (lane == 0) part[warp][D] = M, part[warp][D + 1] = L;
+            __syncthreads();
+            if (joins && mate == 0) {
+                float Mn = -INFINITY;
+                for (int x = 0; x < wpr; ++x) Mn = fmaxf(Mn, part[warp + x][D]);
+                const float mu = Mn == -INFINITY ? 0.f : Mn;
+                L = 0.f;
+#pragma unroll
+                for (int i = 0; i < V; ++i) o[i] = 0.f;
+                for (int x = 0; x < wpr; ++x) {
+                    const float f = ex2(part[warp + x][D] - mu);
+                    L = fmaf(part[warp + x][D + 1], f, L);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) o[i] = fmaf(part[warp + x][lane * V + i], f, o[i]);
+                }
+            }
+        }
+        if (inside && mate == 0 && (empty || joins)) {
+            const float y = empty || L == 0.f ? 0.f : 1.f / L;
+            const int64_t to = (((int64_t)b * p.T + t) * p.H + h * G + (row - t * G)) * D + lane * V;
+#pragma unroll
+            for (int i = 0; i < V; i += 2) {
+                const float a = empty ? 0.f : o[i] * y, z = empty ? 0.f : o[i + 1] * y;
+                if (BF)
+                    *reinterpret_cast<__nv_bfloat162 *>(static_cast<__nv_bfloat16 *>(p.o) + to + i) = __floats2bfloat162_rn(a, z);
+                else
+                    *reinterpret_cast<float2 *>(static_cast<float *>(p.o) + to + i) = make_float2(a, z);
+            }
+        }
+    }
+}
+
+// rows of an item: 16, or 32 where a KV head has more and the registers hold them
+int att_tile(const AttendArgs &a) { return a.in_bf16 && a.d <= 128 && (int64_t)a.T * (a.H / a.Hk) > 16 ? 2 : 1; }
+int att_warps(const AttendArgs &a) { return sm_count() * (a.d == 256 ? 4 : 8); }
+
+template <int D, int MT, bool F32>
+cudaError_t launch_as(const AttendArgs &a, cudaStream_t s) {
+    using C = AttCfg<D, MT, F32>;
+    const int smem = C::warps * C::warp_bytes + (a.batch + 1) * 4;
+    cudaError_t e = ensure_smem_limit(reinterpret_cast<const void *>(attend_kernel<D, MT, F32>), smem);
+    if (e != cudaSuccess) return e;
+    const int grid = sm_count();
+    attend_kernel<D, MT, F32><<<grid, C::threads, smem, s>>>(a);
+    e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    const int G = a.H / a.Hk, R = C::R;
+    const int64_t items = (int64_t)a.batch * (((int64_t)a.T * G + R - 1) / R) * a.Hk;
+    const int rows = (int)std::min<int64_t>(R, (int64_t)a.T * G);
+    // a CTA per row, its warps sharing the row's parts, while there are few items; else per item
+    const bool few = items * rows <= 4 * grid;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)items, few ? (unsigned)rows : 1);
+    cfg.blockDim = dim3(kJoinThreads);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, attend_join_kernel<D, !F32>, a, R, grid * C::warps, few ? kJoinThreads / 32 : 1);
+}
+template <int D>
+cudaError_t launch_d(const AttendArgs &a, cudaStream_t s) {
+    if (!a.in_bf16) return launch_as<D, 1, true>(a, s);
+    if constexpr (D <= 128)
+        if (att_tile(a) == 2) return launch_as<D, 2, false>(a, s);
+    return launch_as<D, 1, false>(a, s);
+}
+
+}  // namespace
+
+int64_t attend_workspace(const AttendArgs &a) {
+    const int64_t R = 16 * att_tile(a), W = att_warps(a);
+    return att_before_bytes(a.batch) + W * 2 * R * ((int64_t)a.d * 4 + 8);
+}
+
+cudaError_t launch_attend(AttendArgs a, cudaStream_t s) {
+    static std::atomic<uint32_t *> cache[64];
+    const cudaError_t e = symbol_address_cached(&g_status_attend, cache, &a.status);
+    if (e != cudaSuccess) return e;
+    return a.d == 64 ? launch_d<64>(a, s) : a.d == 128 ? launch_d<128>(a, s) : launch_d<256>(a, s);
+}
+
+cudaError_t take_status_attend(uint32_t *bits) {
+    uint32_t zero = 0;
+    cudaError_t e = cudaMemcpyFromSymbol(bits, g_status_attend, sizeof(uint32_t));
+    if (e != cudaSuccess) return e;
+    return cudaMemcpyToSymbol(g_status_attend, &zero, sizeof(uint32_t));
+}
+
+}  // namespace damp

@@ -1,0 +1,264 @@
+// cache.cu -- writing and reading the 8-bit cache of softmax-attention layers.
+//
+// Append.  With s the scale of a (page, KV head, keys or values), r = 1/s, a value x is stored as
+// code rne(x r) + 128, held to 1 .. 255; s = amax/127 over the values that the call writes into the
+// page, or the scale that the page's earlier tokens have, if that is larger.  Where an open page's
+// scale grows from s to s', its earlier codes become rne(c (s r')): off by another half step of s'.
+// Every operation is one FP32 rounding, so that the codes are defined to the bit.  Scales below
+// 2^-126 are 0 (the block then holds zeros).  A NaN is stored as 0; an infinity takes no part in
+// the maximum and is held to the block's largest value; both set a status bit.
+//
+// An item is one (row, page, head, keys or values): 128 threads, or a warp where a page receives 8
+// tokens at most.  A thread keeps the values of its chunks of 16 in registers between the maximum
+// and the codes, so each value is read once; codes are stored 16 bytes at a time.
+//
+// Read.  A thread turns 16 codes into 16 values.  Both are bound by the bytes.
+#include "cache.cuh"
+
+#include <algorithm>
+#include <cfloat>
+
+namespace damp {
+
+static __device__ uint32_t g_status_cache;
+
+namespace {
+
+constexpr int kAppThreads = 128;
+constexpr int kReadThreads = 256;
+
+// 16 values of a row
+template <bool BF>
+struct Sixteen {
+    uint4 w[BF ? 2 : 4];
+    __device__ __forceinline__ void load(const void *p, int64_t at) {
+        const uint4 *g = reinterpret_cast<const uint4 *>(static_cast<const uint8_t *>(p) + at * (BF ? 2 : 4));
+#pragma unroll
+        for (int i = 0; i < (BF ? 2 : 4); ++i) w[i] = g[i];
+    }
+    __device__ __forceinline__ float2 pair(int i) const {  // values 2 i and 2 i + 1
+        const uint32_t *u = reinterpret_cast<const uint32_t *>(w);
+        if (BF) return make_float2(__uint_as_float(u[i] << 16), __uint_as_float(u[i] & 0xffff0000u));
+        return make_float2(__uint_as_float(u[2 * i]), __uint_as_float(u[2 * i + 1]));
+    }
+};
+
+__device__ __forceinline__ float finite_abs(float x, bool &bad) {
+    const float a = fabsf(x);
+    if (a <= FLT_MAX) return a;
+    bad = true;  // NaN or infinity
+    return 0.f;
+}
+// rne(x) + 128 in the low byte, |x| <= 127
+__device__ __forceinline__ uint32_t code_of(float x) { return __float_as_uint(__fadd_rn(x, 12582912.f + 128.f)); }
+__device__ __forceinline__ uint32_t code4(float a, float b, float c, float d) {
+    return prmt(prmt(code_of(a), code_of(b), 0x0040u), prmt(code_of(c), code_of(d), 0x0040u), 0x5410u);
+}
+__device__ __forceinline__ float scaled(float x, float r) {  // held to the codes' range; NaN: 0
+    const float y = __fmul_rn(x, r);
+    return y == y ? fminf(fmaxf(y, -127.f), 127.f) : 0.f;
+}
+
+// TPI threads per item (32: warps on their own, 128: the CTA)
+template <int D, int TPI, bool BF>
+__global__ void __launch_bounds__(kAppThreads) cache_append_kernel(const CacheArgs p, int touched) {
+    constexpr int kChunks = D / 16;
+    constexpr int kUnits = TPI == 32 ? 8 * kChunks / 32 : kCachePage * kChunks / kAppThreads;  // of a thread
+    static_assert(kUnits >= 1, "units");
+    __shared__ float part[4];
+    const int lane = threadIdx.x & 31;
+    const int tid = TPI == 32 ? lane : threadIdx.x;
+    const int64_t item = TPI == 32 ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5) : (int64_t)blockIdx.x;
+    // keys and values, heads, pages, rows from the fastest
+    const int which = (int)(item & 1);
+    const int64_t ih = item >> 1;
+    const int h = (int)(ih % p.Hk);
+    const int64_t ip = ih / p.Hk;
+    const int b = (int)(ip / touched);
+    if (b >= p.batch) return;  // (a whole warp; with 128 threads an item, never)
+    const int start = p.start[b];
+    const int fresh = p.lengths ? max(0, min(p.lengths[b], p.T)) : p.T;
+    const int first_page = max(start, 0) / kCachePage;
+    const int64_t page = first_page + ip % touched;  // of the row
+    const int64_t lo = max((int64_t)start, page * kCachePage), hi = min((int64_t)start + fresh, (page + 1) * kCachePage);
+    if (start < 0 || lo >= hi) {
+        if (start < 0 && fresh > 0 && tid == 0) atomicOr(p.status, kDevBadSlot);
+        return;
+    }
+    const int64_t slot = page < p.table ? cache_page(p.pages[(int64_t)b * p.table + page], p.num_pages) : -1;
+    if (slot < 0) {
+        if (tid == 0) atomicOr(p.status, kDevBadSlot);
+        return;
+    }
+    uint8_t *const record = p.pool + (slot * p.Hk + h) * cache_record_bytes(D);
+    uint8_t *const rows = record + which * cache_rows_bytes(D);
+    float *const scale_at = reinterpret_cast<float *>(record + 2 * cache_rows_bytes(D)) + which;
+    const int t0 = (int)(lo - page * kCachePage);  // in the page
+    const int n = (int)(hi - lo) * kChunks;
+    const float before = t0 ? *scale_at : 0.f;
+    const void *const x = which ? p.v : p.k;
+    const int64_t stride = which ? p.v_stride : p.k_stride;
+    const int64_t from = ((int64_t)b * p.T + (lo - start)) * stride + (int64_t)h * D;
+
+    Sixteen<BF> val[kUnits];
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+        const int u = tid + i * TPI;
+        if (u < n) val[i].load(x, from + (u / kChunks) * stride + (u % kChunks) * 16);
+    }
+    float top = 0.f;
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+        if (tid + i * TPI < n) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float2 y = val[i].pair(e);
+                top = fmaxf(top, fmaxf(finite_abs(y.x, bad), finite_abs(y.y, bad)));
+            }
+        }
+    }
+    if (bad) atomicOr(p.status, kDevNotFinite);
+    top = __uint_as_float(__reduce_max_sync(kFull, __float_as_uint(top)));  // not negative: ordered as integers
+    if (TPI == 128) {
+        if (lane == 0) part[threadIdx.x >> 5] = top;
+        __syncthreads();
+        top = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
+    }
+    float s = __fdiv_rn(top, 127.f);
+    if (s < FLT_MIN) s = 0.f;
+    s = fmaxf(s, before);  // before is read by all threads above, written below, after the barrier or in step
+    const float r = s > 0.f ? __fdiv_rn(1.f, s) : 0.f;
+    if (TPI == 32) __syncwarp();
+    if (tid == 0 && (s != before || t0 == 0)) *scale_at = s;
+    if (t0 && s != before) {  // the earlier tokens of an open page
+        const float f = __fmul_rn(before, r);
+        for (int u = tid; u < t0 * kChunks; u += TPI) {
+            uint4 *const at = reinterpret_cast<uint4 *>(rows + 16 * u);  // each chunk where it lies
+            uint4 c = *at;
+            uint32_t *const w = reinterpret_cast<uint32_t *>(&c);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float y[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[e] = __fmul_rn((float)((int)((w[i] >> (8 * e)) & 255u) - 128), f);
+                w[i] = code4(y[0], y[1], y[2], y[3]);
+            }
+            *at = c;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+        const int u = tid + i * TPI;
+        if (u < n) {
+            uint32_t w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float2 y = val[i].pair(2 * e), z = val[i].pair(2 * e + 1);
+                w[e] = code4(scaled(y.x, r), scaled(y.y, r), scaled(z.x, r), scaled(z.y, r));
+            }
+            *reinterpret_cast<uint4 *>(rows + cache_chunk(t0 + u / kChunks, u % kChunks, D)) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    }
+}
+
+template <int D, bool BF>
+__global__ void __launch_bounds__(kReadThreads) cache_read_kernel(const CacheArgs p) {
+    constexpr int kChunks = D / 16;
+    const int64_t u = (int64_t)blockIdx.x * kReadThreads + threadIdx.x;
+    const int which = blockIdx.y;
+    const int m = (int)(u % kChunks);
+    const int64_t uh = u / kChunks, ut = uh / p.Hk;
+    const int h = (int)(uh - ut * p.Hk);
+    const int64_t b = ut / p.T;
+    if (b >= p.batch) return;
+    const int64_t token = (p.start ? (int64_t)p.start[b] : 0) + (ut - b * p.T);
+    float x[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = 0.f;
+    if (token >= 0 && token < cache_clamp(p.lengths[b], p.table)) {
+        const int64_t slot = cache_page(p.pages[b * p.table + token / kCachePage], p.num_pages);
+        if (slot < 0) {
+            if (m == 0) atomicOr(p.status, kDevBadSlot);
+        } else {
+            const uint8_t *const record = p.pool + (slot * p.Hk + h) * cache_record_bytes(D);
+            const uint4 c = *reinterpret_cast<const uint4 *>(record + which * cache_rows_bytes(D) + cache_chunk((int)(token % kCachePage), m, D));
+            const float s = reinterpret_cast<const float *>(record + 2 * cache_rows_bytes(D))[which];
+            const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = (u8_biased(w[i / 4], i % 4) - (8388608.f + 128.f)) * s;
+        }
+    }
+    const int64_t to = u * 16;
+    void *const out = which ? p.v : p.k;
+    if (BF) {
+        uint4 w[2];
+        uint32_t *const y = reinterpret_cast<uint32_t *>(w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const __nv_bfloat162 z = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+            memcpy(&y[i], &z, 4);
+        }
+        uint4 *const g = reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(out) + to);
+        g[0] = w[0];
+        g[1] = w[1];
+    } else {
+        float4 *const g = reinterpret_cast<float4 *>(static_cast<float *>(out) + to);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) g[i] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+    }
+}
+
+template <int D, bool BF>
+void append_as(const CacheArgs &a, cudaStream_t s) {
+    const int touched = (a.T + kCachePage - 2) / kCachePage + 1;  // pages that T tokens may lie in
+    const int64_t items = 2 * (int64_t)a.Hk * a.batch * touched;
+    if (a.T <= 8)
+        cache_append_kernel<D, 32, BF><<<(unsigned)((items + 3) / 4), kAppThreads, 0, s>>>(a, touched);
+    else
+        cache_append_kernel<D, 128, BF><<<(unsigned)items, kAppThreads, 0, s>>>(a, touched);
+}
+template <int D, bool BF>
+void read_as(const CacheArgs &a, cudaStream_t s) {
+    const int64_t units = (int64_t)a.batch * a.T * a.Hk * (D / 16);
+    cache_read_kernel<D, BF><<<dim3((unsigned)((units + kReadThreads - 1) / kReadThreads), 2), kReadThreads, 0, s>>>(a);
+}
+#define DAMP_BY_D(f, a, s)                                                                      \
+    do {                                                                                        \
+        if (a.d == 64)                                                                          \
+            a.in_bf16 ? f<64, true>(a, s) : f<64, false>(a, s);                                 \
+        else if (a.d == 128)                                                                    \
+            a.in_bf16 ? f<128, true>(a, s) : f<128, false>(a, s);                               \
+        else                                                                                    \
+            a.in_bf16 ? f<256, true>(a, s) : f<256, false>(a, s);                               \
+    } while (0)
+
+cudaError_t status_word(uint32_t **out) {
+    static std::atomic<uint32_t *> cache[64];
+    return symbol_address_cached(&g_status_cache, cache, out);
+}
+
+}  // namespace
+
+cudaError_t launch_cache_append(CacheArgs a, cudaStream_t s) {
+    const cudaError_t e = status_word(&a.status);
+    if (e != cudaSuccess) return e;
+    DAMP_BY_D(append_as, a, s);
+    return cudaGetLastError();
+}
+
+cudaError_t launch_cache_read(CacheArgs a, cudaStream_t s) {
+    const cudaError_t e = status_word(&a.status);
+    if (e != cudaSuccess) return e;
+    DAMP_BY_D(read_as, a, s);
+    return cudaGetLastError();
+}
+
+cudaError_t take_status_cache(uint32_t *bits) {
+    uint32_t zero = 0;
+    cudaError_t e = cudaMemcpyFromSymbol(bits, g_status_cache, sizeof(uint32_t));
+    if (e != cudaSuccess) return e;
+    return cudaMemcpyToSymbol(g_status_cache, &zero, sizeof(uint32_t));
+}
+
+}  // namespace damp

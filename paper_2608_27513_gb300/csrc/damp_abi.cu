@@ -432,6 +432,37 @@ damp_status convert(const damp_layout *L, void *state, int64_t num_slots, const 
     return e == cudaSuccess ? DAMP_OK : DAMP_ERR_CUDA;
 }
 
+damp_status check_cache(const damp_cache_layout *L) {
+    if (!L) return DAMP_ERR_NULL;
+    if (L->num_kv_heads < 1 || L->num_heads < 1 || L->num_heads > 65536 || L->num_heads % L->num_kv_heads)
+        return DAMP_ERR_SHAPE;
+    return L->d == 64 || L->d == 128 || L->d == 256 ? DAMP_OK : DAMP_ERR_SHAPE;
+}
+
+// what the calls on a cache have in common; es: bytes of an element
+damp_status cache_args(const damp_cache_layout *L, void *cache, int64_t num_pages, const int32_t *pages, int32_t table,
+                       int32_t batch, int32_t T, int32_t dtype, CacheArgs *a, Range *pool, Range *lists, int64_t *es) {
+    const damp_status st = check_cache(L);
+    if (st != DAMP_OK) return st;
+    if (dtype != DAMP_IN_BF16 && dtype != DAMP_IN_FP32) return DAMP_ERR_FORMAT;
+    if (num_pages < 1 || num_pages > INT32_MAX || table < 1 || table > (1 << 25) || batch < 0 || batch > kCacheMaxBatch || T < 0)
+        return DAMP_ERR_SHAPE;
+    a->H = L->num_heads;
+    a->Hk = L->num_kv_heads;
+    a->d = L->d;
+    a->pool = static_cast<uint8_t *>(cache);
+    a->num_pages = num_pages;
+    a->pages = pages;
+    a->table = table;
+    a->batch = batch;
+    a->T = T;
+    a->in_bf16 = dtype == DAMP_IN_BF16;
+    *es = a->in_bf16 ? 2 : 4;
+    *pool = range_of(cache, num_pages * a->Hk * (64 * L->d + 16));
+    *lists = range_of(pages, (int64_t)batch * table * 4);
+    return DAMP_OK;
+}
+
 }  // namespace
 
 int sm_count() { return device_attr(g_sm_count, cudaDevAttrMultiProcessorCount, 1); }
@@ -699,6 +730,178 @@ damp_status damp_verify_drafts(const void *target_logits, const void *draft_logi
     return launch_verify(a, static_cast<cudaStream_t>(stream)) == cudaSuccess ? DAMP_OK : DAMP_ERR_CUDA;
 }
 
+damp_status damp_rotary(const void *q, int64_t q_stride, int32_t heads, const void *k, int64_t k_stride,
+                        int32_t kv_heads, int32_t d, int32_t dtype, const int32_t *positions, int32_t positions_per_row,
+                        int32_t batch, int32_t T, const double *freq, int32_t rotary_dim, int32_t interleaved,
+                        float scale, void *q_out, void *k_out, void *stream) {
+    if (dtype != DAMP_IN_BF16 && dtype != DAMP_IN_FP32) return DAMP_ERR_FORMAT;
+    if (d < 1 || d > 1024 || rotary_dim < 2 || rotary_dim > d || rotary_dim % 2 || heads < 1 || heads > 1024 ||
+        kv_heads < 0 || kv_heads > 1024 || batch < 0 || T < 0)
+        return DAMP_ERR_SHAPE;
+    const int64_t n = (int64_t)batch * T, es = dtype == DAMP_IN_BF16 ? 2 : 4;
+    if (n > INT32_MAX) return DAMP_ERR_SHAPE;
+    if (n == 0) return DAMP_OK;
+    RotaryArgs a{};
+    a.x[0] = q, a.x[1] = k;
+    a.out[0] = q_out, a.out[1] = k_out;
+    a.stride[0] = q_stride, a.stride[1] = k_stride;
+    a.heads[0] = heads, a.heads[1] = kv_heads;
+    Range in[2] = {}, out[2] = {};
+    if (!positions || !freq) return DAMP_ERR_NULL;
+    for (int i = 0; i < 2; ++i) {
+        if (a.heads[i] == 0) continue;
+        const int64_t row = (int64_t)a.heads[i] * d;
+        if (!a.x[i] || !a.out[i]) return DAMP_ERR_NULL;
+        if (a.stride[i] < row || a.stride[i] > INT64_MAX / 16 / n) return DAMP_ERR_SHAPE;
+        if (!aligned(a.x[i], es) || !aligned(a.out[i], es)) return DAMP_ERR_ALIGN;
+        in[i] = range_of(a.x[i], ((n - 1) * a.stride[i] + row) * es);
+        out[i] = range_of(a.out[i], n * row * es);
+    }
+    if (!aligned(positions, 4) || !aligned(freq, 8)) return DAMP_ERR_ALIGN;
+    const Range rp = range_of(positions, (positions_per_row ? (int64_t)batch : n) * 4), rf = range_of(freq, (int64_t)rotary_dim * 4);
+    if (overlap(out[0], out[1])) return DAMP_ERR_ALIAS;
+    for (int i = 0; i < 2; ++i) {
+        if (overlap(out[i], rp) || overlap(out[i], rf) || overlap(out[i], in[1 - i])) return DAMP_ERR_ALIAS;
+        const bool in_place = a.out[i] == a.x[i] && a.stride[i] == (int64_t)a.heads[i] * d;
+        if (!in_place && overlap(out[i], in[i])) return DAMP_ERR_ALIAS;
+    }
+    a.d = d;
+    a.r = rotary_dim;
+    a.positions = positions;
+    a.per_row = positions_per_row != 0;
+    a.T = T;
+    a.tokens = n;
+    a.freq = freq;
+    a.scale = scale;
+    a.interleaved = interleaved != 0;
+    a.in_bf16 = dtype == DAMP_IN_BF16;
+    return launch_rotary(a, static_cast<cudaStream_t>(stream)) == cudaSuccess ? DAMP_OK : DAMP_ERR_CUDA;
+}
+
+int64_t damp_cache_page_bytes(const damp_cache_layout *layout) {
+    return check_cache(layout) == DAMP_OK ? (int64_t)layout->num_kv_heads * (64 * layout->d + 16) : 0;
+}
+
+damp_status damp_cache_append(const damp_cache_layout *layout, void *cache, int64_t num_pages, const int32_t *pages,
+                              int32_t table, int32_t batch, int32_t T, const int32_t *start, const int32_t *lengths,
+                              const void *k, int64_t k_stride, const void *v, int64_t v_stride, int32_t dtype,
+                              void *stream) {
+    CacheArgs a{};
+    Range pool, lists;
+    int64_t es = 0;
+    damp_status st = cache_args(layout, cache, num_pages, pages, table, batch, T, dtype, &a, &pool, &lists, &es);
+    if (st != DAMP_OK) return st;
+    const int64_t n = (int64_t)batch * T, row = (int64_t)a.Hk * a.d;
+    if (k_stride < row || v_stride < row || k_stride * es % 16 || v_stride * es % 16) return DAMP_ERR_SHAPE;
+    if (n == 0) return DAMP_OK;
+    if (k_stride > INT64_MAX / 16 / n || v_stride > INT64_MAX / 16 / n) return DAMP_ERR_SHAPE;
+    if (2 * row / a.d * batch > INT32_MAX / ((T + 30) / 32 + 1)) return DAMP_ERR_SHAPE;  // CTAs
+    if (!cache || !pages || !start || !k || !v) return DAMP_ERR_NULL;
+    if (!aligned(cache, 16) || !aligned(pages, 4) || !aligned(start, 4) || !aligned(lengths, 4) || !aligned(k, 16) ||
+        !aligned(v, 16))
+        return DAMP_ERR_ALIGN;
+    const Range inputs[] = {lists, range_of(start, (int64_t)batch * 4), range_of(lengths, lengths ? (int64_t)batch * 4 : 0),
+                            range_of(k, ((n - 1) * k_stride + row) * es), range_of(v, ((n - 1) * v_stride + row) * es)};
+    for (const Range &r : inputs)
+        if (overlap(pool, r)) return DAMP_ERR_ALIAS;
+    a.start = start;
+    a.lengths = lengths;
+    a.k = const_cast<void *>(k);
+    a.v = const_cast<void *>(v);
+    a.k_stride = k_stride;
+    a.v_stride = v_stride;
+    return launch_cache_append(a, static_cast<cudaStream_t>(stream)) == cudaSuccess ? DAMP_OK : DAMP_ERR_CUDA;
+}
+
+damp_status damp_cache_read(const damp_cache_layout *layout, const void *cache, int64_t num_pages, const int32_t *pages,
+                            int32_t table, int32_t batch, int32_t T, const int32_t *start, const int32_t *lengths,
+                            void *k, void *v, int32_t dtype, void *stream) {
+    CacheArgs a{};
+    Range pool, lists;
+    int64_t es = 0;
+    damp_status st = cache_args(layout, const_cast<void *>(cache), num_pages, pages, table, batch, T, dtype, &a, &pool,
+                                &lists, &es);
+    if (st != DAMP_OK) return st;
+    const int64_t n = (int64_t)batch * T, row = (int64_t)a.Hk * a.d;
+    if (n == 0) return DAMP_OK;
+    if (n > INT64_MAX / 16 / row || n * row / 4096 >= INT32_MAX) return DAMP_ERR_SHAPE;  // CTAs of 4096 values
+    if (!cache || !pages || !lengths || !k || !v) return DAMP_ERR_NULL;
+    if (!aligned(cache, 16) || !aligned(pages, 4) || !aligned(start, 4) || !aligned(lengths, 4) || !aligned(k, 16) ||
+        !aligned(v, 16))
+        return DAMP_ERR_ALIGN;
+    const Range rk = range_of(k, n * row * es), rv = range_of(v, n * row * es);
+    const Range inputs[] = {pool, lists, range_of(start, start ? (int64_t)batch * 4 : 0), range_of(lengths, (int64_t)batch * 4)};
+    if (overlap(rk, rv)) return DAMP_ERR_ALIAS;
+    for (const Range &r : inputs)
+        if (overlap(rk, r) || overlap(rv, r)) return DAMP_ERR_ALIAS;
+    a.start = start;
+    a.lengths = lengths;
+    a.k = k;
+    a.v = v;
+    return launch_cache_read(a, static_cast<cudaStream_t>(stream)) == cudaSuccess ? DAMP_OK : DAMP_ERR_CUDA;
+}
+
+int64_t damp_cache_attend_workspace(const damp_cache_layout *layout, int32_t batch, int32_t T, int32_t dtype) {
+    if (check_cache(layout) != DAMP_OK || batch < 1 || batch > kCacheMaxBatch || T < 1) return 0;
+    AttendArgs a{};
+    a.H = layout->num_heads;
+    a.Hk = layout->num_kv_heads;
+    a.d = layout->d;
+    a.batch = batch;
+    a.T = T;
+    a.in_bf16 = dtype == DAMP_IN_BF16;
+    return attend_workspace(a);
+}
+
+damp_status damp_cache_attend(const damp_cache_layout *layout, const void *cache, int64_t num_pages,
+                              const int32_t *pages, int32_t table, int32_t batch, int32_t T, const int32_t *lengths,
+                              const int32_t *q_lengths, const void *q, int64_t q_stride, float scale, int32_t window,
+                              void *o, int32_t dtype, void *workspace, int64_t workspace_bytes, void *stream) {
+    CacheArgs c{};
+    Range pool, lists;
+    int64_t es = 0;
+    damp_status st = cache_args(layout, const_cast<void *>(cache), num_pages, pages, table, batch, T, dtype, &c, &pool,
+                                &lists, &es);
+    if (st != DAMP_OK) return st;
+    const int64_t n = (int64_t)batch * T, row = (int64_t)c.H * c.d, G = c.H / c.Hk;
+    if (window < 0 || !(scale > 0.f) || !(scale <= 3.4e38f) || q_stride < row || q_stride * es % 16) return DAMP_ERR_SHAPE;
+    if (n == 0) return DAMP_OK;
+    if (q_stride > INT64_MAX / 16 / n || T * G > (1 << 26)) return DAMP_ERR_SHAPE;
+    // pages of all items of 16 rows
+    if (((T * G + 15) / 16) * batch * c.Hk > INT32_MAX / table) return DAMP_ERR_SHAPE;
+    AttendArgs a{};
+    a.H = c.H;
+    a.Hk = c.Hk;
+    a.d = c.d;
+    a.batch = batch;
+    a.T = T;
+    a.in_bf16 = c.in_bf16;
+    if (workspace_bytes < attend_workspace(a)) return DAMP_ERR_SHAPE;
+    if (!cache || !pages || !lengths || !q || !o || !workspace) return DAMP_ERR_NULL;
+    if (!aligned(cache, 16) || !aligned(pages, 4) || !aligned(lengths, 4) || !aligned(q_lengths, 4) || !aligned(q, 16) ||
+        !aligned(o, 16) || !aligned(workspace, 16))
+        return DAMP_ERR_ALIGN;
+    const Range ro = range_of(o, n * row * es), rw = range_of(workspace, workspace_bytes);
+    const Range inputs[] = {pool, lists, range_of(lengths, (int64_t)batch * 4), range_of(q_lengths, q_lengths ? (int64_t)batch * 4 : 0),
+                            range_of(q, ((n - 1) * q_stride + row) * es)};
+    if (overlap(ro, rw)) return DAMP_ERR_ALIAS;
+    for (const Range &r : inputs)
+        if (overlap(ro, r) || overlap(rw, r)) return DAMP_ERR_ALIAS;
+    a.pool = c.pool;
+    a.num_pages = num_pages;
+    a.pages = pages;
+    a.table = table;
+    a.lengths = lengths;
+    a.q_lengths = q_lengths;
+    a.q = q;
+    a.q_stride = q_stride;
+    a.scale = scale;
+    a.window = window >= (1 << 30) ? 0 : window;  // a table holds 2^30 tokens at most
+    a.o = o;
+    a.workspace = static_cast<uint8_t *>(workspace);
+    return launch_attend(a, static_cast<cudaStream_t>(stream)) == cudaSuccess ? DAMP_OK : DAMP_ERR_CUDA;
+}
+
 damp_status damp_quantize_state(const damp_layout *layout, const float *S, const uint8_t *perm, void *state,
                                 int64_t num_slots, const int32_t *slot_idx, int32_t batch, void *stream) {
     return convert(layout, state, num_slots, slot_idx, batch, perm, const_cast<float *>(S), nullptr, nullptr,
@@ -874,6 +1077,10 @@ damp_status damp_device_status(uint32_t *status) {
     if (take_status_slots(&bits) != cudaSuccess) return DAMP_ERR_CUDA;
     all |= bits;
     if (take_status_verify(&bits) != cudaSuccess) return DAMP_ERR_CUDA;
+    all |= bits;
+    if (take_status_cache(&bits) != cudaSuccess) return DAMP_ERR_CUDA;
+    all |= bits;
+    if (take_status_attend(&bits) != cudaSuccess) return DAMP_ERR_CUDA;
     all |= bits;
     if (take_status_convert(&bits) != cudaSuccess) return DAMP_ERR_CUDA;
     all |= bits;

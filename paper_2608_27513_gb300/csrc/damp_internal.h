@@ -91,6 +91,55 @@ struct VerifyArgs {
     uint32_t *status;  // set by the launcher
 };
 
+// rotary positions
+struct RotaryArgs {
+    const void *x[2];      // q, k (or NULL): rows of heads x d values, stride elements from token to token
+    void *out[2];          // contiguous
+    int64_t stride[2];
+    int32_t heads[2];
+    int32_t d, r;          // head dimension, its rotated part
+    const int32_t *positions;
+    int32_t per_row, T;    // positions per row of T tokens, or per token
+    int64_t tokens;
+    const double *freq;    // radians per position, r / 2
+    float scale;
+    int32_t interleaved, in_bf16;
+};
+
+// the 8-bit cache of softmax-attention layers (cache.cuh)
+constexpr int kCachePage = 32;         // tokens of a page
+constexpr int kCacheMaxBatch = 4096;   // rows of a call
+struct CacheArgs {
+    int32_t H, Hk, d;
+    uint8_t *pool;
+    int64_t num_pages;
+    const int32_t *pages;  // [batch][table]
+    int32_t table;
+    int32_t batch, T;
+    const int32_t *start, *lengths;  // append: tokens held, new ones (or NULL: T); read: first token (or NULL: 0), tokens held
+    void *k, *v;
+    int64_t k_stride, v_stride;  // elements from token to token
+    int32_t in_bf16;
+    uint32_t *status;  // set by the launchers
+};
+struct AttendArgs {
+    int32_t H, Hk, d;
+    const uint8_t *pool;
+    int64_t num_pages;
+    const int32_t *pages;
+    int32_t table;
+    int32_t batch, T;
+    const int32_t *lengths, *q_lengths;  // tokens held with the queries' own; queries (or NULL: T)
+    const void *q;
+    int64_t q_stride;
+    float scale;
+    int32_t window;  // 0: none
+    void *o;
+    int32_t in_bf16;
+    uint8_t *workspace;
+    uint32_t *status;  // set by the launchers
+};
+
 // Launchers (return the CUDA error of the launch; they perform no host-side argument checks).
 cudaError_t launch_packed_gdn(const StepArgs &a, cudaStream_t s);
 cudaError_t launch_packed_kda(const StepArgs &a, cudaStream_t s);
@@ -121,6 +170,11 @@ cudaError_t launch_copy_slots(SlotArgs a, cudaStream_t s);  // dst[i] <- src[i]
 cudaError_t launch_zero_slots(SlotArgs a, cudaStream_t s);  // dst[i]
 cudaError_t launch_compact_plan(SlotArgs a, int32_t *out, cudaStream_t s);  // live slots src -> new numbers
 cudaError_t launch_verify(VerifyArgs a, cudaStream_t s);
+cudaError_t launch_rotary(const RotaryArgs &a, cudaStream_t s);
+cudaError_t launch_cache_append(CacheArgs a, cudaStream_t s);
+cudaError_t launch_cache_read(CacheArgs a, cudaStream_t s);
+cudaError_t launch_attend(AttendArgs a, cudaStream_t s);
+int64_t attend_workspace(const AttendArgs &a);  // bytes
 cudaError_t launch_quantize(const ConvArgs &a, cudaStream_t s);
 cudaError_t launch_dequantize(const ConvArgs &a, cudaStream_t s);
 cudaError_t launch_pack_tiers(const ConvArgs &a, cudaStream_t s);
@@ -158,6 +212,8 @@ cudaError_t take_status_fp32(uint32_t *bits);
 cudaError_t take_status_lin(uint32_t *bits);
 cudaError_t take_status_slots(uint32_t *bits);
 cudaError_t take_status_verify(uint32_t *bits);
+cudaError_t take_status_cache(uint32_t *bits);
+cudaError_t take_status_attend(uint32_t *bits);
 cudaError_t take_status_convert(uint32_t *bits);
 cudaError_t take_status_rowabs(uint32_t *bits);
 cudaError_t take_status_prefill_gdn(uint32_t *bits);
