@@ -19,11 +19,9 @@
 // The contraction index of Q K^T is permuted so that a lane's operands are 16 consecutive codes,
 // and the columns of P V so that a lane reads 16 consecutive codes of 4 tokens: 16-byte loads
 // without bank conflicts, one byte permute and one subtraction per two codes.
-#include "cache.cuh"
+#include "attend.cuh"
 
 #include <algorithm>
-#include <cfloat>
-#include <climits>
 
 namespace damp {
 
@@ -31,33 +29,7 @@ static __device__ uint32_t g_status_attend;
 
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kJoinThreads = 256;
-constexpr int kNoRow = INT_MIN / 2;  // below every token, with a window too (2^30 at most)
-
-// the pages of an item in its row's table
-struct AttItem {
-    int first, pages;
-};
-// the rows' tokens: held tokens, queries
-struct AttRow {
-    int len, n;
-};
-__device__ __forceinline__ AttRow att_row(const AttendArgs &p, int b) {
-    AttRow r;
-    r.len = cache_clamp(p.lengths[b], p.table);
-    r.n = p.q_lengths ? max(0, min(p.q_lengths[b], p.T)) : p.T;
-    return r;
-}
-__device__ __forceinline__ AttItem att_item(const AttendArgs &p, AttRow w, int rt, int R, int G) {
-    const int t0 = rt * R / G, t1 = min(w.n - 1, (rt * R + R - 1) / G);
-    const int hi = w.len - w.n + t1;  // the last token that its last query sees
-    if (t0 > t1 || hi < 0) return AttItem{0, 0};
-    const int lo = p.window ? max(0, w.len - w.n + t0 - (p.window - 1)) : 0;
-    return AttItem{lo / kCachePage, hi / kCachePage - lo / kCachePage + 1};
-}
-__device__ __forceinline__ int att_tiles(int n, int R, int G) { return (n * G + R - 1) / R; }
-
 template <int D, int MT, bool F32>
 struct AttCfg {
     static constexpr int R = 16 * MT;
@@ -73,11 +45,6 @@ struct AttCfg {
     static_assert(stages >= 2, "ring");
 };
 
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
 __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
@@ -137,72 +104,6 @@ __device__ __forceinline__ void load16(const void *p, int64_t at, bool live, flo
         }
     }
 }
-// N (8 or 16) consecutive outputs
-template <bool BF, int N>
-__device__ __forceinline__ void store_out(void *o, int64_t at, const float (&x)[N]) {
-    if (BF) {
-        uint32_t w[N / 2];
-#pragma unroll
-        for (int i = 0; i < N / 2; ++i) {
-            const __nv_bfloat162 z = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-            memcpy(&w[i], &z, 4);
-        }
-#pragma unroll
-        for (int i = 0; i < N / 8; ++i)
-            stg128(static_cast<__nv_bfloat16 *>(o) + at + 8 * i, make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]));
-    } else {
-#pragma unroll
-        for (int i = 0; i < N / 4; ++i)
-            *reinterpret_cast<float4 *>(static_cast<float *>(o) + at + 4 * i) = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
-    }
-}
-
-// Workspace: the number of pages before each batch row (a KV head's), then the parts: o [warp][2][R][D] and
-// (m, l) [warp][2][R].  A warp leaves part 1 of an item that starts in its range, else part 0.
-struct AttWork {
-    int32_t *before;
-    float *o;
-    float2 *ml;
-};
-__host__ __device__ inline int64_t att_before_bytes(int batch) { return ((int64_t)(batch + 1) * 4 + 15) & ~15ll; }
-__host__ __device__ inline AttWork att_work(uint8_t *w, int batch, int warps, int R, int D) {
-    AttWork a;
-    a.before = reinterpret_cast<int32_t *>(w);
-    a.o = reinterpret_cast<float *>(w + att_before_bytes(batch));
-    a.ml = reinterpret_cast<float2 *>(a.o + (int64_t)warps * 2 * R * D);
-    return a;
-}
-__device__ __forceinline__ int att_per(int total, int warps) { return max(1, (total + warps - 1) / warps); }
-
-// before[b]: the pages of batch rows before b, for one KV head
-__device__ void att_count(const AttendArgs &p, int R, int G, int32_t *before) {
-    const int tiles = att_tiles(p.T, R, G);
-    for (int b = threadIdx.x; b <= p.batch; b += blockDim.x) before[b] = 0;
-    __syncthreads();
-    for (int i = threadIdx.x; i < p.batch * tiles; i += blockDim.x) {
-        const int b = i / tiles;
-        const int n = att_item(p, att_row(p, b), i - b * tiles, R, G).pages;
-        if (tiles == 1) before[b + 1] = n;
-        else if (n) atomicAdd(before + b + 1, n);
-    }
-    __syncthreads();
-    if (threadIdx.x < 32) {
-        int sum = 0;
-        for (int at = 0; at < p.batch; at += 32) {
-            const int b = at + threadIdx.x;
-            int n = b < p.batch ? before[b + 1] : 0;
-#pragma unroll
-            for (int i = 1; i < 32; i <<= 1) {
-                const int y = __shfl_up_sync(kFull, n, i);
-                if ((int)threadIdx.x >= i) n += y;
-            }
-            if (b < p.batch) before[b + 1] = sum + n;
-            sum += __shfl_sync(kFull, n, 31);
-        }
-    }
-    __syncthreads();
-}
-
 struct AttPage {  // a page of the sequence, 32 bytes
     int b, rt, h, page;    // page: in the row's table
     int begin, count;      // of its item, in the sequence
@@ -225,7 +126,7 @@ __global__ void __launch_bounds__(AttCfg<D, MT, F32>::threads, 1) attend_kernel(
         for (int i = 0; i < C::stages; ++i) mbar_init(bars + 8 * i, 1);
         fence_mbar_init();
     }
-    att_count(p, R, G, before);
+    att_count(p, R, G, 1, before);
     const int warps = gridDim.x * C::warps;
     const AttWork work = att_work(p.workspace, p.batch, warps, R, D);
     if (blockIdx.x == 0)
@@ -592,38 +493,38 @@ __global__ void __launch_bounds__(AttCfg<D, MT, F32>::threads, 1) attend_kernel(
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
-// Joins the parts of items that several warps worked on; clears the rows that no warp worked on.
-// One CTA per item, `wpr` warps per row.
+// Joins the parts of items that several ranges hold; clears the rows of none.  `wpr` warps per row,
+// blockIdx.y: parts of an item's rows.
 template <int D, bool BF>
-__global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(const AttendArgs p, int R, int warps, int wpr) {
+__global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(const AttendArgs p, int R, int ranges, int unit, int wpr) {
     constexpr int V = D / 32;  // columns of a lane
     __shared__ float part[kJoinThreads / 32][D + 2];
     __shared__ int sums[kJoinThreads / 32];
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const AttWork work = att_work(p.workspace, p.batch, warps, R, D);
+    const AttWork work = att_work(p.workspace, p.batch, ranges, R, D);
     const int G = p.H / p.Hk, tiles = att_tiles(p.T, R, G);
     const int h = blockIdx.x % p.Hk, bt = blockIdx.x / p.Hk, rt = bt % tiles, b = bt / tiles;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const AttRow w = att_row(p, b);
-    const AttItem it = att_item(p, w, rt, R, G);
-    int ahead = 0;  // pages of the row's earlier items
+    const int units = att_units(att_item(p, w, rt, R, G).pages, unit);
+    int ahead = 0;  // units of the row's earlier items
     if (tiles > 1) {
-        for (int i = threadIdx.x; i < rt; i += kJoinThreads) ahead += att_item(p, w, i, R, G).pages;
+        for (int i = threadIdx.x; i < rt; i += kJoinThreads) ahead += att_units(att_item(p, w, i, R, G).pages, unit);
         ahead = __reduce_add_sync(kFull, ahead);
         if (lane == 0) sums[warp] = ahead;
         __syncthreads();
         ahead = 0;
         for (int i = 0; i < kJoinThreads / 32; ++i) ahead += sums[i];
     }
-    const int total = work.before[p.batch] * p.Hk, per = att_per(total, warps);
-    const int begin = (work.before[b] + ahead) * p.Hk + h * it.pages;
-    const int first = begin / per, last = it.pages ? (begin + it.pages - 1) / per : first;
+    const int total = work.before[p.batch] * p.Hk, per = att_per(total, ranges);
+    const int begin = (work.before[b] + ahead) * p.Hk + h * units;
+    const int first = begin / per, last = units ? (begin + units - 1) / per : first;
     const int team = warp / wpr, mate = warp % wpr, teams = kJoinThreads / 32 / wpr;
     for (int r0 = blockIdx.y * teams; r0 < R; r0 += gridDim.y * teams) {
         const int r = r0 + team;
         const int row = rt * R + r, t = row / G;
         const bool inside = r < R && t < p.T;
-        const bool empty = t >= w.n || it.pages == 0;
+        const bool empty = t >= w.n || units == 0;
         if (!inside && wpr == 1) continue;
         const bool joins = inside && !empty && first != last;
         float o[V], M = -INFINITY, L = 0.f;
@@ -705,10 +606,25 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(const AttendA
     }
 }
 
-// rows of an item: 16, or 32 where a KV head has more and the registers hold them
-int att_tile(const AttendArgs &a) { return a.in_bf16 && a.d <= 128 && (int64_t)a.T * (a.H / a.Hk) > 16 ? 2 : 1; }
-int att_warps(const AttendArgs &a) { return sm_count() * (a.d == 256 ? 4 : 8); }
-
+template <int D, bool BF>
+cudaError_t launch_join(const AttendArgs &a, int R, int ranges, int unit, cudaStream_t s) {
+    const int G = a.H / a.Hk;
+    const int64_t items = (int64_t)a.batch * (((int64_t)a.T * G + R - 1) / R) * a.Hk;
+    const int rows = (int)std::min<int64_t>(R, (int64_t)a.T * G);
+    // a CTA per row, its warps sharing the row's parts, while there are few items; else a warp per row, 32
+    // rows per CTA at most
+    const bool few = items * rows <= 4 * sm_count();
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)items, few ? (unsigned)rows : (unsigned)((rows + 31) / 32));
+    cfg.blockDim = dim3(kJoinThreads);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, attend_join_kernel<D, BF>, a, R, ranges, unit, few ? kJoinThreads / 32 : 1);
+}
 template <int D, int MT, bool F32>
 cudaError_t launch_as(const AttendArgs &a, cudaStream_t s) {
     using C = AttCfg<D, MT, F32>;
@@ -718,36 +634,23 @@ cudaError_t launch_as(const AttendArgs &a, cudaStream_t s) {
     const int grid = sm_count();
     attend_kernel<D, MT, F32><<<grid, C::threads, smem, s>>>(a);
     e = cudaGetLastError();
-    if (e != cudaSuccess) return e;
-    const int G = a.H / a.Hk, R = C::R;
-    const int64_t items = (int64_t)a.batch * (((int64_t)a.T * G + R - 1) / R) * a.Hk;
-    const int rows = (int)std::min<int64_t>(R, (int64_t)a.T * G);
-    // a CTA per row, its warps sharing the row's parts, while there are few items; else per item
-    const bool few = items * rows <= 4 * grid;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)items, few ? (unsigned)rows : 1);
-    cfg.blockDim = dim3(kJoinThreads);
-    cfg.stream = s;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, attend_join_kernel<D, !F32>, a, R, grid * C::warps, few ? kJoinThreads / 32 : 1);
+    return e != cudaSuccess ? e : launch_join<D, !F32>(a, C::R, grid * C::warps, 1, s);
 }
 template <int D>
 cudaError_t launch_d(const AttendArgs &a, cudaStream_t s) {
-    if (!a.in_bf16) return launch_as<D, 1, true>(a, s);
-    if constexpr (D <= 128)
-        if (att_tile(a) == 2) return launch_as<D, 2, false>(a, s);
-    return launch_as<D, 1, false>(a, s);
+    if (attend_tc_takes(a)) {
+        const cudaError_t e = launch_attend_tc(a, sm_count(), s);
+        return e != cudaSuccess ? e : launch_join<D, true>(a, attend_tc_rows(a), sm_count(), kTcUnit, s);
+    }
+    return a.in_bf16 ? launch_as<D, 1, false>(a, s) : launch_as<D, 1, true>(a, s);
 }
 
 }  // namespace
 
 int64_t attend_workspace(const AttendArgs &a) {
-    const int64_t R = 16 * att_tile(a), W = att_warps(a);
-    return att_before_bytes(a.batch) + W * 2 * R * ((int64_t)a.d * 4 + 8);
+    const bool tc = attend_tc_takes(a);
+    const int64_t R = tc ? attend_tc_rows(a) : 16, ranges = (int64_t)sm_count() * (tc ? 1 : a.d == 256 ? 4 : 8);
+    return att_before_bytes(a.batch) + ranges * 2 * R * ((int64_t)a.d * 4 + 8);
 }
 
 cudaError_t launch_attend(AttendArgs a, cudaStream_t s) {

@@ -1,0 +1,122 @@
+// attend.cuh -- what the kernels of attention over the 8-bit cache share: the items and their pages, the
+// sequence of all items' pages, the workspace of parts.
+//
+// The rows of an item are R (query token, query head) pairs that share a (batch row, KV head); its keys
+// are the pages from the first that its first query sees to the last that its last query sees.
+// The items' pages, `unit` at a time, form one sequence, in the order of batch rows, tiles of R rows and
+// KV heads, which is cut into equal ranges.
+#pragma once
+
+#include "cache.cuh"
+
+#include <cfloat>
+#include <climits>
+
+namespace damp {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kNoRow = INT_MIN / 2;  // below every token, with a window too (2^30 at most)
+
+
+// the pages of an item in its row's table
+struct AttItem {
+    int first, pages;
+};
+// the rows' tokens: held tokens, queries
+struct AttRow {
+    int len, n;
+};
+__device__ __forceinline__ AttRow att_row(const AttendArgs &p, int b) {
+    AttRow r;
+    r.len = cache_clamp(p.lengths[b], p.table);
+    r.n = p.q_lengths ? max(0, min(p.q_lengths[b], p.T)) : p.T;
+    return r;
+}
+__device__ __forceinline__ AttItem att_item(const AttendArgs &p, AttRow w, int rt, int R, int G) {
+    const int t0 = rt * R / G, t1 = min(w.n - 1, (rt * R + R - 1) / G);
+    const int hi = w.len - w.n + t1;  // the last token that its last query sees
+    if (t0 > t1 || hi < 0) return AttItem{0, 0};
+    const int lo = p.window ? max(0, w.len - w.n + t0 - (p.window - 1)) : 0;
+    return AttItem{lo / kCachePage, hi / kCachePage - lo / kCachePage + 1};
+}
+__device__ __forceinline__ int att_tiles(int n, int R, int G) { return (n * G + R - 1) / R; }
+__device__ __forceinline__ int att_units(int pages, int unit) { return (pages + unit - 1) / unit; }
+
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// N (8 or 16) consecutive outputs
+template <bool BF, int N>
+__device__ __forceinline__ void store_out(void *o, int64_t at, const float (&x)[N]) {
+    if (BF) {
+        uint32_t w[N / 2];
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) {
+            const __nv_bfloat162 z = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+            memcpy(&w[i], &z, 4);
+        }
+#pragma unroll
+        for (int i = 0; i < N / 8; ++i)
+            stg128(static_cast<__nv_bfloat16 *>(o) + at + 8 * i, make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]));
+    } else {
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i)
+            *reinterpret_cast<float4 *>(static_cast<float *>(o) + at + 4 * i) = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+    }
+}
+
+// Workspace: the units before each batch row (a KV head's), then the parts: o [range][2][R][D] and
+// (m, l) [range][2][R].  A range leaves part 1 of an item that starts in it, else part 0.
+struct AttWork {
+    int32_t *before;
+    float *o;
+    float2 *ml;
+};
+__host__ __device__ inline int64_t att_before_bytes(int batch) { return ((int64_t)(batch + 1) * 4 + 15) & ~15ll; }
+__host__ __device__ inline AttWork att_work(uint8_t *w, int batch, int ranges, int R, int D) {
+    AttWork a;
+    a.before = reinterpret_cast<int32_t *>(w);
+    a.o = reinterpret_cast<float *>(w + att_before_bytes(batch));
+    a.ml = reinterpret_cast<float2 *>(a.o + (int64_t)ranges * 2 * R * D);
+    return a;
+}
+__device__ __forceinline__ int att_per(int total, int ranges) { return max(1, (total + ranges - 1) / ranges); }
+
+// before[b]: the units of batch rows before b, for one KV head (all threads)
+__device__ inline void att_count(const AttendArgs &p, int R, int G, int unit, int32_t *before) {
+    const int tiles = att_tiles(p.T, R, G);
+    for (int b = threadIdx.x; b <= p.batch; b += blockDim.x) before[b] = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < p.batch * tiles; i += blockDim.x) {
+        const int b = i / tiles;
+        const int n = att_units(att_item(p, att_row(p, b), i - b * tiles, R, G).pages, unit);
+        if (tiles == 1) before[b + 1] = n;
+        else if (n) atomicAdd(before + b + 1, n);
+    }
+    __syncthreads();
+    if (threadIdx.x < 32) {
+        int sum = 0;
+        for (int at = 0; at < p.batch; at += 32) {
+            const int b = at + threadIdx.x;
+            int n = b < p.batch ? before[b + 1] : 0;
+#pragma unroll
+            for (int i = 1; i < 32; i <<= 1) {
+                const int y = __shfl_up_sync(kFull, n, i);
+                if ((int)threadIdx.x >= i) n += y;
+            }
+            if (b < p.batch) before[b + 1] = sum + n;
+            sum += __shfl_sync(kFull, n, 31);
+        }
+    }
+    __syncthreads();
+}
+
+// the products of prompts and drafts on the tensor cores (attend_tc.cu)
+bool attend_tc_takes(const AttendArgs &a);
+int attend_tc_rows(const AttendArgs &a);  // of an item
+cudaError_t launch_attend_tc(AttendArgs a, int grid, cudaStream_t s);
+constexpr int kTcUnit = 4;  // pages of a key tile
+
+}  // namespace damp

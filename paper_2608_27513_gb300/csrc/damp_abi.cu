@@ -1082,6 +1082,8 @@ damp_status damp_device_status(uint32_t *status) {
     all |= bits;
     if (take_status_attend(&bits) != cudaSuccess) return DAMP_ERR_CUDA;
     all |= bits;
+    if (take_status_attend_tc(&bits) != cudaSuccess) return DAMP_ERR_CUDA;
+    all |= bits;
     if (take_status_convert(&bits) != cudaSuccess) return DAMP_ERR_CUDA;
     all |= bits;
     if (take_status_rowabs(&bits) != cudaSuccess) return DAMP_ERR_CUDA;

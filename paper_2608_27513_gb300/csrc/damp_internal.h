@@ -214,6 +214,7 @@ cudaError_t take_status_slots(uint32_t *bits);
 cudaError_t take_status_verify(uint32_t *bits);
 cudaError_t take_status_cache(uint32_t *bits);
 cudaError_t take_status_attend(uint32_t *bits);
+cudaError_t take_status_attend_tc(uint32_t *bits);
 cudaError_t take_status_convert(uint32_t *bits);
 cudaError_t take_status_rowabs(uint32_t *bits);
 cudaError_t take_status_prefill_gdn(uint32_t *bits);
