@@ -640,7 +640,7 @@ template <int D>
 cudaError_t launch_d(const AttendArgs &a, cudaStream_t s) {
     if (attend_tc_takes(a)) {
         const cudaError_t e = launch_attend_tc(a, sm_count(), s);
-        return e != cudaSuccess ? e : launch_join<D, true>(a, attend_tc_rows(a), sm_count(), kTcUnit, s);
+        return e != cudaSuccess ? e : launch_join<D, true>(a, attend_tc_rows(a), sm_count(), attend_tc_unit(a), s);
     }
     return a.in_bf16 ? launch_as<D, 1, false>(a, s) : launch_as<D, 1, true>(a, s);
 }

@@ -117,6 +117,6 @@ __device__ inline void att_count(const AttendArgs &p, int R, int G, int unit, in
 bool attend_tc_takes(const AttendArgs &a);
 int attend_tc_rows(const AttendArgs &a);  // of an item
 cudaError_t launch_attend_tc(AttendArgs a, int grid, cudaStream_t s);
-constexpr int kTcUnit = 4;  // pages of a key tile
+int attend_tc_unit(const AttendArgs &a);  // pages of a key tile
 
 }  // namespace damp

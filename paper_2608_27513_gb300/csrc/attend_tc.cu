@@ -31,50 +31,64 @@ static __device__ uint32_t g_status_attend_tc;
 
 namespace {
 
-constexpr int kAtThreads = 13 * 32;
-constexpr int kAtTile = 128;  // tokens of a key tile
+constexpr int kAtThreads = 16 * 32;  // (warps 14 and 15 only complete a warpgroup)
+constexpr int kAtSoftRegs = 176, kAtTurnRegs = 96, kAtIssueRegs = 64;  // of 128 each at launch
 constexpr uint32_t kAtCols = 512;
 constexpr uint32_t kAtO = 256;  // S blocks at columns 0 and 128, O from here on
 constexpr float kAtLag = 4.f;
-constexpr int kAtNotes = 4;
+constexpr int kAtNotes = 8;
+constexpr int kAtMaxPages = 4;  // of a key tile
 
 struct AtNote {  // of a key tile: what the softmax needs of its pages
-    float factor[kTcUnit];  // key scale
-    float weight[kTcUnit];  // log2 of 2^10 times value scale over 2^e
-    float back[kTcUnit];    // 2^-weight, exactly what the sums divide by
-    int e;                  // exponent field of 2^e
-    int hidden;             // bit i: page i is bad or missing
+    float factor[kAtMaxPages];  // key scale
+    float weight[kAtMaxPages];  // log2 of 2^10 times value scale over 2^e
+    float back[kAtMaxPages];    // 2^-weight, exactly what the sums divide by
+    int e;                      // exponent field of 2^e
+    int hidden;                 // bit i: page i is bad or missing
     int unused[2];
 };
 
 template <int D, int SUB>
 struct AtSmem {
-    static constexpr int tile = kAtTile * D * 2;
+    static constexpr int tokens = D == 256 ? 64 : 128;  // of a key tile
+    static constexpr int pages = tokens / kCachePage;
+    static constexpr int q_tile = 128 * D * 2, tile = tokens * D * 2;
     static constexpr int buffers = D == 256 ? 1 : 2;  // of K and of V
-    static constexpr int q = 0, k = SUB * tile, v = k + buffers * tile;
-    static constexpr int note = v + buffers * tile;
+    static constexpr int codes = tokens * D;          // of K or of V
+    static constexpr int stages = D == 64 ? 4 : D == 256 ? 3 : SUB == 1 ? 2 : 1;  // of codes
+    static constexpr int q = 0, k = SUB * q_tile, v = k + buffers * tile;
+    static constexpr int kc = v + buffers * tile, vc = kc + stages * codes;
+    static constexpr int note = vc + stages * codes;
     static constexpr int bar = note + kAtNotes * (int)sizeof(AtNote);
-    static constexpr int before = bar + 256;
+    static constexpr int bytes = bar + 384;
+    static constexpr int before = k;  // until the roles begin
+    static_assert(SUB * q_tile + 4 * (kCacheMaxBatch + 1) <= kc, "before");
     static constexpr int sm_warps = 4 * SUB, turn_warps = 12 - sm_warps;
 };
 // mbarriers
-enum { kBarQ = 0, kBarKFull = 1, kBarKFree = 3, kBarVFull = 5, kBarVFree = 7, kBarS = 9, kBarP = 11, kBarNote = 13, kBarDone = 17, kBarPV = 18, kBarCount = 19 };
+enum { kBarQ = 0, kBarDone = 2, kBarKFull = 4, kBarKFree = 6, kBarVFull = 8, kBarVFree = 10, kBarS = 12, kBarP = 14, kBarPV = 16, kBarNote = 17,
+       kBarKcFull = kBarNote + kAtNotes, kBarKcFree = kBarKcFull + 4, kBarVcFull = kBarKcFree + 4, kBarVcFree = kBarVcFull + 4, kBarCount = kBarVcFree + 4 };
+static_assert(kBarCount * 8 <= 384, "barriers");
 
 // instruction descriptor: f16 x f16 -> FP32, M = 128, N columns, B MN-major if set
 __host__ __device__ constexpr uint32_t at_idesc(int n, bool b_mn) {
     return (1u << 4) | (b_mn ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
 }
-// Products are issued by a whole warp in step, one elected lane each.
-__device__ __forceinline__ void at_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
-    asm volatile("{\n.reg .pred p, e;\nelect.sync _|e, 0xffffffff;\nsetp.ne.u32 p, %4, 0;\n"
-                 "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
-                 "l"(a), "l"(b), "r"(idesc), "r"(acc)
+// Products are issued by a whole warp in step, one elected lane each, from descriptors whose words are
+// in uniform registers (a reduction's result is).
+__device__ __forceinline__ uint32_t at_uniform(uint32_t x) { return __reduce_max_sync(kFull, x); }
+__device__ __forceinline__ void at_mma(uint32_t d, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t acc) {
+    asm volatile("{\n.reg .pred p, e;\n.reg .b64 da, db;\nelect.sync _|e, 0xffffffff;\nsetp.ne.u32 p, %6, 0;\n"
+                 "mov.b64 da, {%1, %2};\nmov.b64 db, {%3, %4};\n"
+                 "@e tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %5, p;\n}" ::"r"(d),
+                 "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(acc)
                  : "memory");
 }
-__device__ __forceinline__ void at_mma_ta(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
-    asm volatile("{\n.reg .pred p, e;\nelect.sync _|e, 0xffffffff;\nsetp.ne.u32 p, %4, 0;\n"
-                 "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d),
-                 "r"(a), "l"(b), "r"(idesc), "r"(acc)
+__device__ __forceinline__ void at_mma_ta(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t acc) {
+    asm volatile("{\n.reg .pred p, e;\n.reg .b64 db;\nelect.sync _|e, 0xffffffff;\nsetp.ne.u32 p, %5, 0;\n"
+                 "mov.b64 db, {%2, %3};\n"
+                 "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %4, p;\n}" ::"r"(d),
+                 "r"(a), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(acc)
                  : "memory");
 }
 __device__ __forceinline__ void at_commit(uint32_t bar) {
@@ -85,24 +99,17 @@ __device__ __forceinline__ void at_commit(uint32_t bar) {
 __device__ __forceinline__ void at_arrive(uint32_t bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
-// 32 columns of a thread's lane, to be used after at_ld_wait on them
-__device__ __forceinline__ void at_ld32(uint32_t taddr, uint32_t (&r)[32]) {
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-                 "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+// 16 columns of a thread's lane, to be used after at_ld_wait on them
+__device__ __forceinline__ void at_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]),
-                   "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]),
-                   "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]),
-                   "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
                  : "r"(taddr));
 }
-__device__ __forceinline__ void at_ld_wait(uint32_t (&r)[32]) {
+__device__ __forceinline__ void at_ld_wait(uint32_t (&r)[16]) {
     asm volatile("tcgen05.wait::ld.sync.aligned;"
                  : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
-                   "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]),
-                   "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]),
-                   "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]),
-                   "+r"(r[29]), "+r"(r[30]), "+r"(r[31])::"memory");
+                   "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])::"memory");
 }
 __device__ __forceinline__ void at_st16(uint32_t taddr, const uint32_t (&r)[16]) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
@@ -110,17 +117,16 @@ __device__ __forceinline__ void at_st16(uint32_t taddr, const uint32_t (&r)[16])
                  "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
                  : "memory");
 }
-__device__ __forceinline__ void at_st32(uint32_t taddr, const uint32_t (&r)[32]) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-                 "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(taddr),
-                 "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-                 "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
-                 "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
-                 "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
-                 : "memory");
-}
 __device__ __forceinline__ void at_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+template <int N>
+__device__ __forceinline__ void at_more_regs() {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+}
+template <int N>
+__device__ __forceinline__ void at_fewer_regs() {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+}
 __device__ __forceinline__ uint32_t at_half2(float a, float b) {  // a in the low half
     const __half2 h = __floats2half2_rn(a, b);
     return *reinterpret_cast<const uint32_t *>(&h);
@@ -137,14 +143,14 @@ struct AtItem {
     int b, rt, h, first, pages, tiles, begin;
     AttRow row;
 };
-__device__ __forceinline__ void at_set(AtItem &it, const AttendArgs &p, int R, int G) {
+__device__ __forceinline__ void at_set(AtItem &it, const AttendArgs &p, int R, int G, int unit) {
     const AttItem x = att_item(p, it.row, it.rt, R, G);
     it.first = x.first;
     it.pages = x.pages;
-    it.tiles = att_units(x.pages, kTcUnit);
+    it.tiles = att_units(x.pages, unit);
 }
 // the item that unit x < total lies in
-__device__ __forceinline__ AtItem at_seek(const AttendArgs &p, const int32_t *before, int x, int R, int G) {
+__device__ __forceinline__ AtItem at_seek(const AttendArgs &p, const int32_t *before, int x, int R, int G, int unit) {
     AtItem it;
     int lo = 0, hi = p.batch;
     while (hi - lo > 1) {
@@ -159,7 +165,7 @@ __device__ __forceinline__ AtItem at_seek(const AttendArgs &p, const int32_t *be
     const int lane = threadIdx.x & 31;
     for (;; it.rt += 32) {  // 32 tiles of rows at a time
         const int rt = it.rt + lane;
-        int n = rt < att_tiles(it.row.n, R, G) ? att_units(att_item(p, it.row, rt, R, G).pages, kTcUnit) * p.Hk : 0;
+        int n = rt < att_tiles(it.row.n, R, G) ? att_units(att_item(p, it.row, rt, R, G).pages, unit) * p.Hk : 0;
         int sum = n;
 #pragma unroll
         for (int i = 1; i < 32; i <<= 1) {
@@ -176,13 +182,13 @@ __device__ __forceinline__ AtItem at_seek(const AttendArgs &p, const int32_t *be
         at += __shfl_sync(kFull, sum, 31);
         if (it.rt > att_tiles(it.row.n, R, G)) break;  // (not reached: x lies in this row)
     }
-    at_set(it, p, R, G);
+    at_set(it, p, R, G, unit);
     it.h = it.tiles ? (x - at) / it.tiles : 0;
     it.begin = at + it.h * it.tiles;
     return it;
 }
 // the item after `it`, given that there is one
-__device__ __forceinline__ void at_next(AtItem &it, const AttendArgs &p, int R, int G) {
+__device__ __forceinline__ void at_next(AtItem &it, const AttendArgs &p, int R, int G, int unit) {
     it.begin += it.tiles;
     if (++it.h < p.Hk) return;
     it.h = 0;
@@ -192,7 +198,7 @@ __device__ __forceinline__ void at_next(AtItem &it, const AttendArgs &p, int R, 
             if (++it.b >= p.batch) return;
             it.row = att_row(p, it.b);
         }
-        at_set(it, p, R, G);
+        at_set(it, p, R, G, unit);
     } while (it.tiles == 0);
 }
 
@@ -213,18 +219,18 @@ struct AtWait {  // bounded waits, all of which give up once one has
 template <int D, int SUB>
 __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendArgs p) {
     using M = AtSmem<D, SUB>;
-    constexpr int R = 128 * SUB;
+    constexpr int R = 128 * SUB, TN = M::tokens, PG = M::pages;
     extern __shared__ __align__(1024) uint8_t sm[];
     __shared__ uint32_t s_dead, s_tmem;
-    int32_t *const before = reinterpret_cast<int32_t *>(sm + M::before);
     const uint32_t sb = smem_u32(sm);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int G = p.H / p.Hk;
     auto bar = [&](int i) { return sb + M::bar + 8 * i; };
     if (threadIdx.x == 0) {
         s_dead = 0;
-        mbar_init(bar(kBarQ), 128 * SUB);
         for (int i = 0; i < 2; ++i) {
+            mbar_init(bar(kBarQ + i), 128);
+            mbar_init(bar(kBarDone + i), 1);
             mbar_init(bar(kBarKFull + i), M::turn_warps);
             mbar_init(bar(kBarKFree + i), 1);
             mbar_init(bar(kBarVFull + i), M::turn_warps);
@@ -232,9 +238,14 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
             mbar_init(bar(kBarS + i), 1);
             mbar_init(bar(kBarP + i), 128);
         }
-        for (int i = 0; i < kAtNotes; ++i) mbar_init(bar(kBarNote + i), 1);
-        mbar_init(bar(kBarDone), 1);
         mbar_init(bar(kBarPV), 1);
+        for (int i = 0; i < kAtNotes; ++i) mbar_init(bar(kBarNote + i), 1);
+        for (int i = 0; i < M::stages; ++i) {
+            mbar_init(bar(kBarKcFull + i), 1);
+            mbar_init(bar(kBarKcFree + i), M::turn_warps);
+            mbar_init(bar(kBarVcFull + i), 1);
+            mbar_init(bar(kBarVcFree + i), M::turn_warps);
+        }
         fence_mbar_init();
     }
     if (warp == 12) {
@@ -242,7 +253,8 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
         tc_fence_before();
     }
-    att_count(p, R, G, kTcUnit, before);  // (synchronizes)
+    int32_t *const before = reinterpret_cast<int32_t *>(sm + M::before);
+    att_count(p, R, G, PG, before);  // (synchronizes)
     tc_fence_after();
     const uint32_t tmem = s_tmem;
     const AttWork work = att_work(p.workspace, p.batch, gridDim.x, R, D);
@@ -251,61 +263,74 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
     const int total = before[p.batch] * p.Hk, per = att_per(total, gridDim.x);
     const int end = (int)min((int64_t)total, ((int64_t)blockIdx.x + 1) * per);
     const int begin = (int)min((int64_t)end, (int64_t)blockIdx.x * per);
+    AtItem it{};
+    if (begin < end) it = at_seek(p, before, begin, R, G, PG);
+    __syncthreads();  // `before` is given up
     const AtWait wait{&s_dead};
+    auto together = [](bool ok) { return __all_sync(kFull, ok) != 0; };
+    const uint32_t n_tiles = (uint32_t)(end - begin);  // of this range
 
     if (begin < end && warp < M::sm_warps) {
+        at_more_regs<kAtSoftRegs>();
         // ---- softmax: thread = row of a block ----
-        const int x = warp >> 2;                 // block of rows
-        const int row = threadIdx.x & 127;       // in the block: the lane of tensor memory
+        const int x = warp >> 2;            // block of rows
+        const int row = threadIdx.x & 127;  // in the block: the lane of tensor memory
         const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         const uint32_t o_at = lanes + kAtO + x * D;
-        AtItem it = at_seek(p, before, begin, R, G);
-        uint32_t tile = 0;  // of this range
-        uint32_t items = 0;
+        // Rows move between global and shared memory 8 at a time, 4 chunks of 16 bytes each: lane = (row, chunk);
+        // in shared memory a chunk of 8 rows is a core matrix.
+        const uint32_t stage = sb + M::q + x * M::q_tile + (warp & 3) * (64 * D) + (lane & 7) * 16 + (lane >> 3) * 128;
+        const uint32_t stage_row = sb + M::q + x * M::q_tile + (row >> 3) * (16 * D) + (row & 7) * 16;
+        uint32_t tile = 0, items = 0;
         bool ok = true;
         for (int at = begin; at < end && ok; ++items) {
-            if (items) at_next(it, p, R, G);
+            if (items) at_next(it, p, R, G, PG);
             const int last = min(end, it.begin + it.tiles);
             const int r = it.rt * R + x * 128 + row, t = r / G;
             const bool live = t < it.row.n;
             const int limit = live ? it.row.len - it.row.n + t : kNoRow;
             const int from = p.window && live ? limit - (p.window - 1) : 0;
             const int head = it.h * G + (r - t * G);
-            // q, scaled by a power of two to below 2^15
-            float factor;
-            {
-                const uint4 *const q = reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(p.q) +
-                                                                       ((int64_t)it.b * p.T + t) * p.q_stride + (int64_t)head * D);
-                uint32_t top = 0;  // largest magnitude of the bf16 values, both halves
-                constexpr int kC = D / 8;
-                constexpr int kHold = D == 256 ? 1 : kC;  // chunks kept between the passes
-                uint4 hold[kHold];
+            float factor = 0.f;
+            {  // q, scaled by a power of two to below 2^15
+                const int64_t mine = live ? ((int64_t)it.b * p.T + t) * p.q_stride + (int64_t)head * D : -1;
+                constexpr int kC = D / 32;  // chunks of a lane in 8 rows
 #pragma unroll
-                for (int i = 0; i < kC; ++i) {
-                    const uint4 w = live ? q[i] : make_uint4(0, 0, 0, 0);
-                    if (kHold == kC) hold[i < kHold ? i : 0] = w;
-                    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+                for (int g0 = 0; g0 < 4; g0 += 2) {
+                    uint4 w[2][kC];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) top = __vmaxu2(top, u[k] & 0x7fff7fffu);
-                }
-                const uint32_t most = max(top >> 16, top & 0xffffu);
-                const int e = min(max((int)(most >> 7), 15), 254);
-                const float up = __uint_as_float((uint32_t)(268 - e) << 23);
-                factor = p.scale * kLog2e / up;
-                const uint32_t to = sb + M::q + x * M::tile + (row >> 3) * (16 * D) + (row & 7) * 16;
+                    for (int g = 0; g < 2; ++g) {
+                        const int64_t src = __shfl_sync(kFull, mine, 8 * (g0 + g) + (lane & 7));
+                        const uint4 *const q = reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(p.q) + src) + (lane >> 3);
 #pragma unroll
-                for (int i = 0; i < kC; ++i) {
-                    const uint4 w = kHold == kC ? hold[i < kHold ? i : 0] : live ? q[i] : make_uint4(0, 0, 0, 0);
-                    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-                    uint32_t h[4];
+                        for (int i = 0; i < kC; ++i) w[g][i] = src >= 0 ? q[4 * i] : make_uint4(0, 0, 0, 0);
+                    }
 #pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        h[k] = at_half2(__uint_as_float(u[k] << 16) * up, __uint_as_float(u[k] & 0xffff0000u) * up);
-                    sts128(to + i * 128, make_uint4(h[0], h[1], h[2], h[3]));
+                    for (int g = 0; g < 2; ++g) {
+                        uint32_t top = 0;  // largest magnitudes of both halves of the words
+#pragma unroll
+                        for (int i = 0; i < kC; ++i)
+                            top = __vmaxu2(__vmaxu2(__vmaxu2(top, w[g][i].x & 0x7fff7fffu), __vmaxu2(w[g][i].y & 0x7fff7fffu, w[g][i].z & 0x7fff7fffu)),
+                                           w[g][i].w & 0x7fff7fffu);
+                        top = __vmaxu2(top, __shfl_xor_sync(kFull, top, 8));
+                        top = __vmaxu2(top, __shfl_xor_sync(kFull, top, 16));
+                        const int e = min(max((int)(max(top >> 16, top & 0xffffu) >> 7), 15), 254);
+                        const float up = __uint_as_float((uint32_t)(268 - e) << 23);
+                        if ((lane >> 3) == g0 + g) factor = p.scale * kLog2e / up;  // of this thread's own row
+#pragma unroll
+                        for (int i = 0; i < kC; ++i) {
+                            const uint32_t u[4] = {w[g][i].x, w[g][i].y, w[g][i].z, w[g][i].w};
+                            uint32_t h[4];
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)
+                                h[k] = at_half2(__uint_as_float(u[k] << 16) * up, __uint_as_float(u[k] & 0xffff0000u) * up);
+                            sts128(stage + (g0 + g) * (16 * D) + i * 512, make_uint4(h[0], h[1], h[2], h[3]));
+                        }
+                    }
                 }
                 fence_proxy_async_smem();
                 tc_fence_before();
-                at_arrive(bar(kBarQ));
+                at_arrive(bar(kBarQ + x));
             }
             float ref = -INFINITY, sum = 0.f;
             int ve = 0;
@@ -313,46 +338,48 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
             for (; at < last; ++at, ++tile) {
                 const int sbuf = SUB == 2 ? x : tile & 1;
                 const uint32_t s_at = lanes + sbuf * 128;
-                const uint32_t n_bar = bar(kBarNote + tile % kAtNotes);
-                ok = wait(n_bar, (tile / kAtNotes) & 1) && wait(bar(kBarS + sbuf), (SUB == 2 ? tile : tile >> 1) & 1);
-                if (!__all_sync(kFull, ok)) {
-                    ok = false;
-                    break;
-                }
+                ok = together(wait(bar(kBarNote + tile % kAtNotes), (tile / kAtNotes) & 1) &&
+                              wait(bar(kBarS + sbuf), (SUB == 2 ? tile : tile >> 1) & 1));
+                if (!ok) break;
                 tc_fence_after();
                 const AtNote *const note = reinterpret_cast<const AtNote *>(sm + M::note) + tile % kAtNotes;
                 const int i = at - it.begin;
-                const int token = (it.first + i * kTcUnit) * kCachePage;  // of column 0
+                const int token = (it.first + i * PG) * kCachePage;  // of column 0
                 const int hidden = note->hidden, e = note->e;
-                float f[kTcUnit];
+                float f[PG];
 #pragma unroll
-                for (int c = 0; c < kTcUnit; ++c) f[c] = fmaxf(factor * note->factor[c], FLT_MIN);  // not 0: times a hidden -inf
-                const bool masked = __any_sync(kFull, hidden != 0 || (limit != kNoRow && (limit < token + kAtTile - 1 || from > token)));
-                auto hide = [&](uint32_t (&s)[32], int c) {
-                    const int lo = from - (token + 32 * c), hi = limit - (token + 32 * c);
-                    const bool all = (hidden >> c) & 1;
+                for (int c = 0; c < PG; ++c) f[c] = fmaxf(factor * note->factor[c], FLT_MIN);  // not 0: times a hidden -inf
+                const bool masked = __any_sync(kFull, hidden != 0 || (limit != kNoRow && (limit < token + TN - 1 || from > token)));
+                uint32_t s[2 * PG][16];
 #pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        if (j > hi || j < lo || all) s[j] = 0xff800000u;
-                };
-                uint32_t s[2][32];
-                float top = -INFINITY;
-                at_ld32(s_at, s[0]);
+                for (int c = 0; c < 2 * PG; ++c) at_ld16(s_at + 16 * c, s[c]);
 #pragma unroll
-                for (int c = 0; c < kTcUnit; ++c) {
-                    at_ld_wait(s[c & 1]);
-                    if (c + 1 < kTcUnit) at_ld32(s_at + 32 * (c + 1), s[(c + 1) & 1]);
-                    if (masked) hide(s[c & 1], c);
-                    float m[2] = {-INFINITY, -INFINITY};
+                for (int c = 0; c < 2 * PG; ++c) at_ld_wait(s[c]);
+                if (masked) {
+                    const int lo = from - token, hi = limit - token;
 #pragma unroll
-                    for (int j = 0; j < 32; j += 4) {
-                        m[0] = fmax3(m[0], __uint_as_float(s[c & 1][j]), __uint_as_float(s[c & 1][j + 1]));
-                        m[1] = fmax3(m[1], __uint_as_float(s[c & 1][j + 2]), __uint_as_float(s[c & 1][j + 3]));
+                    for (int c = 0; c < 2 * PG; ++c) {
+                        const bool all = (hidden >> (c >> 1)) & 1;
+#pragma unroll
+                        for (int j = 0; j < 16; ++j)
+                            if (16 * c + j > hi || 16 * c + j < lo || all) s[c][j] = 0xff800000u;
                     }
-                    top = fmaxf(top, fmaxf(m[0], m[1]) * f[c]);
                 }
-                at_ld32(s_at, s[0]);
-                const bool moves = top > ref + kAtLag || (ref == -INFINITY && top > ref);
+                float top = -INFINITY;
+#pragma unroll
+                for (int c = 0; c < 2 * PG; c += 2) {
+                    float m[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const uint32_t(&v)[16] = s[c + (k >> 1)];
+                        const int at8 = 8 * (k & 1);
+                        m[k] = fmax3(__uint_as_float(v[at8]), __uint_as_float(v[at8 + 1]), __uint_as_float(v[at8 + 2]));
+                        m[k] = fmax3(m[k], __uint_as_float(v[at8 + 3]), __uint_as_float(v[at8 + 4]));
+                        m[k] = fmax3(m[k], __uint_as_float(v[at8 + 5]), fmaxf(__uint_as_float(v[at8 + 6]), __uint_as_float(v[at8 + 7])));
+                    }
+                    top = fmaxf(top, fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])) * f[c / 2]);
+                }
+                const bool moves = top > ref + kAtLag;
                 const float ref_new = moves ? top : ref;
                 float corr = moves ? ex2(ref - ref_new) : 1.f;
                 sum *= corr;
@@ -363,37 +390,31 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
                 }
                 if (i != first_tile && __any_sync(kFull, moves || e != ve)) {
                     if (SUB == 1) {  // the last product into O may still run
-                        ok = wait(bar(kBarPV), (tile - 1) & 1);
-                        if (!__all_sync(kFull, ok)) {
-                            at_ld_wait(s[0]);
-                            ok = false;
-                            break;
-                        }
+                        ok = together(wait(bar(kBarPV), (tile - 1) & 1));
+                        if (!ok) break;
                         tc_fence_after();
                     }
-                    at_ld_wait(s[0]);
 #pragma unroll 1
-                    for (int c = 0; c < D / 32; ++c) {
-                        at_ld32(o_at + 32 * c, s[1]);
-                        at_ld_wait(s[1]);
+                    for (int c = 0; c < D / 16; ++c) {
+                        uint32_t y[16];
+                        at_ld16(o_at + 16 * c, y);
+                        at_ld_wait(y);
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) s[1][j] = __float_as_uint(__uint_as_float(s[1][j]) * corr);
-                        at_st32(o_at + 32 * c, s[1]);
+                        for (int j = 0; j < 16; ++j) y[j] = __float_as_uint(__uint_as_float(y[j]) * corr);
+                        at_st16(o_at + 16 * c, y);
                     }
                 }
                 ve = e;
                 const float base = ref == -INFINITY ? 0.f : -ref;
 #pragma unroll
-                for (int c = 0; c < kTcUnit; ++c) {
-                    at_ld_wait(s[c & 1]);
-                    if (c + 1 < kTcUnit) at_ld32(s_at + 32 * (c + 1), s[(c + 1) & 1]);
-                    if (masked) hide(s[c & 1], c);
+                for (int c = 0; c < PG; ++c) {
                     const float2 f2 = splat2(f[c]), a2 = splat2(base + note->weight[c]);
                     float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
                     uint32_t w[16];
 #pragma unroll
                     for (int j = 0; j < 16; ++j) {
-                        const float2 y = fma2(make_float2(__uint_as_float(s[c & 1][2 * j]), __uint_as_float(s[c & 1][2 * j + 1])), f2, a2);
+                        const uint32_t(&v)[16] = s[2 * c + (j >> 3)];
+                        const float2 y = fma2(make_float2(__uint_as_float(v[2 * (j & 7)]), __uint_as_float(v[2 * (j & 7) + 1])), f2, a2);
                         const float2 z = make_float2(ex2(y.x), ex2(y.y));
                         part[j & 1] = add2(part[j & 1], z);
                         w[j] = at_half2(z.x, z.y);
@@ -407,223 +428,250 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
                 at_arrive(bar(kBarP + sbuf));
             }
             if (!ok) break;
-            // the item's products are done
-            ok = wait(bar(kBarDone), items & 1);
-            if (!__all_sync(kFull, ok)) {
-                ok = false;
-                break;
-            }
+            ok = together(wait(bar(kBarDone + x), items & 1));  // the item's products into O
+            if (!ok) break;
             tc_fence_after();
             const bool whole = it.begin >= begin && it.begin + it.tiles <= end;
-            const int slot = 2 * blockIdx.x + (it.begin >= begin ? 1 : 0);
             const float unit = __uint_as_float((uint32_t)ve << 23) * (1.f / 1024.f);
-            const float y = whole ? (sum == 0.f ? 0.f : unit / sum) : unit;
-            const int64_t to = (((int64_t)it.b * p.T + t) * p.H + head) * D;
-            float *const part = work.o + ((int64_t)slot * R + x * 128 + row) * D;
-            if (live && !whole) work.ml[(int64_t)slot * R + x * 128 + row] = make_float2(ref, sum);
+            if (whole) {
+                const float y = sum == 0.f ? 0.f : unit / sum;
 #pragma unroll 1
-            for (int c = 0; c < D / 32; ++c) {
-                uint32_t s[32];
-                at_ld32(o_at + 32 * c, s);
-                at_ld_wait(s);
-                if (live) {
+                for (int c = 0; c < D / 32; ++c) {
+                    uint32_t both[2][16];
+                    at_ld16(o_at + 32 * c, both[0]);
+                    at_ld16(o_at + 32 * c + 16, both[1]);
+                    at_ld_wait(both[0]);
+                    at_ld_wait(both[1]);
 #pragma unroll
-                    for (int k = 0; k < 2; ++k) {
+                    for (int k = 0; k < 4; ++k) {
+                        const uint32_t *const s = &both[k >> 1][8 * (k & 1)];
+                        uint32_t h[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const __nv_bfloat162 z = __floats2bfloat162_rn(__uint_as_float(s[2 * j]) * y, __uint_as_float(s[2 * j + 1]) * y);
+                            memcpy(&h[j], &z, 4);
+                        }
+                        sts128(stage_row + (4 * c + k) * 128, make_uint4(h[0], h[1], h[2], h[3]));
+                    }
+                }
+                __syncwarp();
+                const int64_t mine = live ? (((int64_t)it.b * p.T + t) * p.H + head) * D : -1;
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const int64_t dst = __shfl_sync(kFull, mine, 8 * g + (lane & 7));
+                    __nv_bfloat16 *const o = static_cast<__nv_bfloat16 *>(p.o) + dst + 8 * (lane >> 3);
+#pragma unroll
+                    for (int i = 0; i < D / 32; ++i) {
+                        const uint4 w = lds128(stage + g * (16 * D) + i * 512);
+                        if (dst >= 0) stg128(o + 32 * i, w);
+                    }
+                }
+                __syncwarp();
+            } else {
+                const int64_t slot = (int64_t)(2 * blockIdx.x + (it.begin >= begin ? 1 : 0)) * R + x * 128 + row;
+                if (live) work.ml[slot] = make_float2(ref, sum);
+#pragma unroll 1
+                for (int c = 0; c < D / 16; ++c) {
+                    uint32_t s[16];
+                    at_ld16(o_at + 16 * c, s);
+                    at_ld_wait(s);
+                    if (live) {
                         float z[16];
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) z[j] = __uint_as_float(s[16 * k + j]) * y;
-                        if (whole)
-                            store_out<true, 16>(p.o, to + 32 * c + 16 * k, z);
-                        else
-                            store_out<false, 16>(part, 32 * c + 16 * k, z);
+                        for (int j = 0; j < 16; ++j) z[j] = __uint_as_float(s[j]) * unit;
+                        store_out<false, 16>(work.o + slot * D, 16 * c, z);
                     }
                 }
             }
             tc_fence_before();
         }
     } else if (begin < end && warp < 12) {
+        at_fewer_regs<kAtTurnRegs>();
         // ---- codes into operands ----
         constexpr int kQuads = D / 64;                             // 4 chunks of 16 codes
-        constexpr int kUnits = 16 * kQuads / M::turn_warps;        // of 8 tokens x 4 chunks, of a warp
+        constexpr int kUnits = (TN / 8) * kQuads / M::turn_warps;  // of 8 tokens x 4 chunks, of a warp
         const int w = warp - M::sm_warps;
         const int tok = lane & 7, mi = lane >> 3;
-        AtItem it = at_seek(p, before, begin, R, G);
-        int lt = begin;  // the tile that is loaded next
-        int ve = 0;
-        uint4 kreg[kUnits], vreg[kUnits];
-        // lane c < 4: page c of the tile that is loaded next, and of the one at hand
-        int slot = -1, slot_now = -1, h_now = 0, h_next = 0;
-        bool fresh_next = true, fresh_now = true;  // starts an item
-        bool bad_next = false, bad_now = false;
-        auto find = [&]() {  // the pages of tile lt
-            if (lt >= it.begin + it.tiles) {
-                at_next(it, p, R, G);
-                fresh_next = true;
-            }
-            const int i = (lt - it.begin) * kTcUnit + lane;
-            slot = -1;
-            bad_next = false;
-            if (lane < kTcUnit && i < it.pages) {
-                const int32_t e = p.pages[(int64_t)it.b * p.table + it.first + i];
-                slot = (int)cache_page(e, p.num_pages);
-                bad_next = slot < 0;
-            }
-            h_next = it.h;
-        };
-        auto load = [&](uint4 (&r)[kUnits], int which) {
+        auto turn = [&](uint32_t from, uint32_t free, uint32_t to, uint32_t to_free, bool wait_free, uint32_t parity, uint32_t full) {
+            uint4 c[kUnits];
 #pragma unroll
             for (int j = 0; j < kUnits; ++j) {
                 const int u = w + j * M::turn_warps, tg = u / kQuads, mq = u % kQuads;
-                const int s = __shfl_sync(kFull, slot_now, tg >> 2);
-                const int t = (tg & 3) * 8 + tok, m = mq * 4 + mi;
-                r[j] = make_uint4(0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u);  // zeros
-                if (s >= 0)
-                    r[j] = __ldg(reinterpret_cast<const uint4 *>(p.pool + ((int64_t)s * p.Hk + h_now) * cache_record_bytes(D) +
-                                                                which * cache_rows_bytes(D) + cache_chunk(t, m, D)));
+                c[j] = lds128(from + tg * 8 * D + cache_chunk(tok, mq * 4 + mi, D));
             }
-        };
-        auto turn = [&](const uint4 (&r)[kUnits], uint32_t to) {
+            __syncwarp();
+            if (lane == 0) at_arrive(free);
+            if (wait_free && !together(wait(to_free, parity))) return false;
 #pragma unroll
             for (int j = 0; j < kUnits; ++j) {
                 const int u = w + j * M::turn_warps, tg = u / kQuads, mq = u % kQuads;
                 const uint32_t at = to + tg * (16 * D) + (mq * 4 + mi) * 256 + tok * 16;
-                const uint4 c = r[j];
-                sts128(at, make_uint4(at_codes(c.x, 0x4140u), at_codes(c.x, 0x4342u), at_codes(c.y, 0x4140u), at_codes(c.y, 0x4342u)));
-                sts128(at + 128, make_uint4(at_codes(c.z, 0x4140u), at_codes(c.z, 0x4342u), at_codes(c.w, 0x4140u), at_codes(c.w, 0x4342u)));
+                sts128(at, make_uint4(at_codes(c[j].x, 0x4140u), at_codes(c[j].x, 0x4342u), at_codes(c[j].y, 0x4140u), at_codes(c[j].y, 0x4342u)));
+                sts128(at + 128, make_uint4(at_codes(c[j].z, 0x4140u), at_codes(c[j].z, 0x4342u), at_codes(c[j].w, 0x4140u), at_codes(c[j].w, 0x4342u)));
             }
-        };
-        float2 scales = make_float2(0.f, 0.f);
-        auto step = [&]() {  // the tile that was next is at hand
-            slot_now = slot;
-            h_now = h_next;
-            fresh_now = fresh_next;
-            bad_now = bad_next;
-            fresh_next = false;
-            scales = make_float2(0.f, 0.f);
-            if (w == 0 && slot_now >= 0)
-                scales = *reinterpret_cast<const float2 *>(p.pool + ((int64_t)slot_now * p.Hk + h_now) * cache_record_bytes(D) + 2 * cache_rows_bytes(D));
-        };
-        find();
-        step();
-        load(kreg, 0);
-        load(vreg, 1);
-        ++lt;
-        if (lt < end) find();
-        bool ok = true;
-        const int tiles = end - begin;
-        for (int i = 0; i < tiles; ++i) {
-            const int buf = M::buffers == 2 ? i & 1 : 0, use = M::buffers == 2 ? i >> 1 : i;
-            if (use) ok = wait(bar(kBarKFree + buf), (use - 1) & 1);
-            if (!__all_sync(kFull, ok)) break;
-            if (w == 0) {
-                AtNote *const note = reinterpret_cast<AtNote *>(sm + M::note) + i % kAtNotes;
-                if (fresh_now) ve = 0;
-                int e = scales.y > 0.f ? min((int)(__float_as_uint(scales.y) >> 23) + 1, 253) : 0;
-                e = max(e, __shfl_xor_sync(kFull, e, 1));
-                e = max(e, __shfl_xor_sync(kFull, e, 2));
-                ve = max(max(ve, 1), __shfl_sync(kFull, e, 0));
-                const float rel = fmaxf(scales.y * __uint_as_float((uint32_t)(254 - ve) << 23), 9.0949470177292824e-13f);  // 2^-40
-                const unsigned hidden = __ballot_sync(kFull, slot_now < 0) & ((1u << kTcUnit) - 1u);
-                if (lane < kTcUnit) {
-                    // a block of zeros stands for zeros at any scale
-                    const float u = scales.y > 0.f ? rel * 1024.f : 1024.f;
-                    note->factor[lane] = scales.x > 0.f ? scales.x : 1.f;
-                    note->weight[lane] = __log2f(u);
-                    note->back[lane] = 1.f / u;
-                }
-                if (lane == 0) {
-                    note->e = ve;
-                    note->hidden = (int)hidden;
-                }
-                if (bad_now) atomicOr(p.status, kDevBadSlot);
-                __syncwarp();
-                if (lane == 0) at_arrive(bar(kBarNote + i % kAtNotes));
-            }
-            turn(kreg, sb + M::k + buf * M::tile);
             fence_proxy_async_smem();
             __syncwarp();
-            if (lane == 0) at_arrive(bar(kBarKFull + buf));
-            const bool more = i + 1 < tiles;
-            if (more) {
-                step();
-                load(kreg, 0);
-            }
-            if (use) ok = wait(bar(kBarVFree + buf), (use - 1) & 1);
-            if (!__all_sync(kFull, ok)) break;
-            turn(vreg, sb + M::v + buf * M::tile);
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) at_arrive(bar(kBarVFull + buf));
-            if (more) {
-                load(vreg, 1);
-                ++lt;
-                if (lt < end) find();
-            }
+            if (lane == 0) at_arrive(full);
+            return true;
+        };
+        for (uint32_t i = 0; i < n_tiles; ++i) {
+            const uint32_t buf = M::buffers == 2 ? i & 1 : 0, use = M::buffers == 2 ? i >> 1 : i;
+            const uint32_t st = i % M::stages, lap = i / M::stages;
+            if (!together(wait(bar(kBarKcFull + st), lap & 1))) break;
+            if (!turn(sb + M::kc + st * M::codes, bar(kBarKcFree + st), sb + M::k + buf * M::tile, bar(kBarKFree + buf), use != 0, (use - 1) & 1,
+                      bar(kBarKFull + buf)))
+                break;
+            if (!together(wait(bar(kBarVcFull + st), lap & 1))) break;
+            if (!turn(sb + M::vc + st * M::codes, bar(kBarVcFree + st), sb + M::v + buf * M::tile, bar(kBarVFree + buf), use != 0, (use - 1) & 1,
+                      bar(kBarVFull + buf)))
+                break;
         }
-    } else if (begin < end) {
-        // ---- the products ----
-        constexpr uint32_t kIdS = at_idesc(kAtTile, false), kIdO = at_idesc(D, true);
-        AtItem it = at_seek(p, before, begin, R, G);
-        uint32_t tile = 0, items = 0;
+    } else if (begin < end && warp >= 13) {
+        at_fewer_regs<kAtIssueRegs>();
+        if (warp == 13) {
+        // ---- the pages' copies, and what the softmax needs of them: lane = page of a tile ----
+        auto entry = [&](int x) {  // of tile x, which lies in `it`
+            const int i = (x - it.begin) * PG + lane;
+            return lane < PG && i < it.pages ? p.pages[(int64_t)it.b * p.table + it.first + i] : INT_MIN;
+        };
+        int32_t next = entry(begin);
+        int h_next = it.h, ve = 0;
+        bool fresh_next = true;
+        uint32_t i = 0;
         bool ok = true;
-        auto key_buf = [&](uint32_t t) { return M::buffers == 2 ? t & 1u : 0u; };
-        auto key_use = [&](uint32_t t) { return (M::buffers == 2 ? t >> 1 : t) & 1u; };
-        auto scores = [&](uint32_t t, int x) {  // Q_x K_t^T; SUB = 1: into the buffer of the tile
-            const uint32_t d = tmem + 128 * (SUB == 2 ? x : t & 1);
-            const uint64_t a = tc_desc(sb + M::q + x * M::tile, 128, 16 * D), b = tc_desc(sb + M::k + key_buf(t) * M::tile, 128, 16 * D);
-#pragma unroll
-            for (int k = 0; k < D / 16; ++k) at_mma(d, a + 16 * k, b + 16 * k, kIdS, k != 0);
-            at_commit(bar(kBarS + (SUB == 2 ? x : t & 1)));
-        };
-        auto outputs = [&](uint32_t t, int x, bool first) {  // O_x += P V_t
-            const uint32_t a = tmem + 128 * (SUB == 2 ? x : t & 1);
-            const uint64_t b = tc_desc(sb + M::v + key_buf(t) * M::tile, 16 * D, 128);
-#pragma unroll
-            for (int k = 0; k < kAtTile / 16; ++k) at_mma_ta(tmem + kAtO + x * D, a + 8 * k, b + 2 * D * k, kIdO, !(first && k == 0));
-        };
-        for (int at = begin; at < end && ok; ++items) {
-            if (items) at_next(it, p, R, G);
-            const int last = min(end, it.begin + it.tiles), n = last - at;
-            ok = wait(bar(kBarQ), items & 1) && wait(bar(kBarKFull + key_buf(tile)), key_use(tile));
-            if (!__all_sync(kFull, ok)) break;
-            tc_fence_after();
-            for (int x = 0; x < SUB; ++x) scores(tile, x);
-            at_commit(bar(kBarKFree + key_buf(tile)));
-            for (int i = 0; i < n && ok; ++i, ++tile) {
-                const bool more = i + 1 < n;
-                if (SUB == 1 && more) {
-                    ok = wait(bar(kBarKFull + key_buf(tile + 1)), key_use(tile + 1));
-                    if (!__all_sync(kFull, ok)) break;
-                    tc_fence_after();
-                    scores(tile + 1, 0);
-                    at_commit(bar(kBarKFree + key_buf(tile + 1)));
+        for (; i < n_tiles; ++i) {
+            const int32_t e = next;
+            const int h = h_next;
+            if (fresh_next) ve = 1;
+            fresh_next = false;
+            if (i + 1 < n_tiles) {
+                const int x = begin + (int)i + 1;
+                if (x >= it.begin + it.tiles) {
+                    at_next(it, p, R, G, PG);
+                    fresh_next = true;
+                    h_next = it.h;
                 }
-                for (int x = 0; x < SUB && ok; ++x) {
-                    const int s = SUB == 2 ? x : (int)(tile & 1);
-                    ok = wait(bar(kBarP + s), (SUB == 2 ? tile : tile >> 1) & 1) && wait(bar(kBarVFull + key_buf(tile)), key_use(tile));
-                    if (SUB == 2 && more && ok) ok = wait(bar(kBarKFull + key_buf(tile + 1)), key_use(tile + 1));
-                    if (!__all_sync(kFull, ok)) {
-                        ok = false;
-                        break;
-                    }
-                    tc_fence_after();
-                    outputs(tile, x, i == 0);
-                    if (x == SUB - 1) at_commit(bar(kBarVFree + key_buf(tile)));
-                    if (SUB == 1) at_commit(bar(kBarPV));
-                    if (SUB == 2 && more) {
-                        scores(tile + 1, x);
-                        if (x == 1) at_commit(bar(kBarKFree + key_buf(tile + 1)));
-                    }
+                next = entry(x);
+            }
+            const int64_t slot = cache_page(e, p.num_pages);
+            const uint8_t *const record = p.pool + (slot * p.Hk + h) * cache_record_bytes(D);
+            if (slot < 0 && e != INT_MIN && lane < PG) atomicOr(p.status, kDevBadSlot);
+            const bool here = lane < PG && slot >= 0;
+            const unsigned shown = __ballot_sync(kFull, here);
+            float2 scales = make_float2(0.f, 0.f);
+            if (here) scales = *reinterpret_cast<const float2 *>(record + 2 * cache_rows_bytes(D));
+            const uint32_t st = i % M::stages, lap = i / M::stages;
+            const uint32_t bytes = __popc(shown) * cache_rows_bytes(D);
+#pragma unroll
+            for (int which = 0; which < 2; ++which) {
+                const uint32_t full = bar((which ? kBarVcFull : kBarKcFull) + st);
+                if (lap) ok = together(wait(bar((which ? kBarVcFree : kBarKcFree) + st), (lap - 1) & 1));
+                if (!ok) break;
+                if (lane == 0) mbar_arrive_expect_tx(full, bytes);
+                __syncwarp();
+                if (here) {
+                    fence_proxy_async_smem();
+                    bulk_g2s(sb + (which ? M::vc : M::kc) + st * M::codes + lane * cache_rows_bytes(D), record + which * cache_rows_bytes(D),
+                             cache_rows_bytes(D), full);
                 }
             }
             if (!ok) break;
-            at_commit(bar(kBarDone));
-            at = last;
+            AtNote *const note = reinterpret_cast<AtNote *>(sm + M::note) + i % kAtNotes;
+            ve = max(ve, (int)__reduce_max_sync(kFull, scales.y > 0.f ? min((__float_as_uint(scales.y) >> 23) + 1u, 253u) : 0u));
+            if (lane < PG) {
+                // value scales below 2^-40 of the unit count as that; a block of zeros stands for zeros at any scale
+                const float rel = fmaxf(scales.y * __uint_as_float((uint32_t)(254 - ve) << 23), 9.0949470177292824e-13f);
+                const float u = scales.y > 0.f ? rel * 1024.f : 1024.f;
+                note->factor[lane] = scales.x > 0.f ? scales.x : 1.f;
+                note->weight[lane] = __log2f(u);
+                note->back[lane] = 1.f / u;
+            }
+            if (lane == 0) {
+                note->e = ve;
+                note->hidden = (int)(~shown & ((1u << PG) - 1u));
+            }
+            __syncwarp();
+            if (lane == 0) at_arrive(bar(kBarNote + i % kAtNotes));
         }
-        if (!ok) {  // what was issued ends by itself; no other product is issued
-            at_commit(bar(kBarDone));
+        // copies in flight end before the shared memory does (they are waited for by the warps that read them, unless
+        // those gave up)
+        if (!ok || s_dead) {
+            for (uint32_t k = i > (uint32_t)M::stages ? i - M::stages : 0; k < i; ++k) {
+                mbar_wait_bounded(bar(kBarKcFull + k % M::stages), (k / M::stages) & 1);
+                mbar_wait_bounded(bar(kBarVcFull + k % M::stages), (k / M::stages) & 1);
+            }
+        }
+        }
+    } else if (begin < end) {
+        // ---- the products ----
+        at_fewer_regs<kAtIssueRegs>();
+        constexpr uint32_t kIdS = at_idesc(TN, false), kIdO = at_idesc(D, true);
+        auto key_buf = [&](uint32_t t) { return M::buffers == 2 ? t & 1u : 0u; };
+        auto key_use = [&](uint32_t t) { return (M::buffers == 2 ? t >> 1 : t) & 1u; };
+        const uint64_t dq = tc_desc(sb + M::q, 128, 16 * D), dk = tc_desc(sb + M::k, 128, 16 * D), dv = tc_desc(sb + M::v, 16 * D, 128);
+        const uint32_t q_lo = at_uniform((uint32_t)dq), k_lo = at_uniform((uint32_t)dk), v_lo = at_uniform((uint32_t)dv);
+        const uint32_t k_hi = at_uniform((uint32_t)(dk >> 32)), v_hi = at_uniform((uint32_t)(dv >> 32)), tm = at_uniform(tmem);
+        auto scores = [&](uint32_t t, int x) {  // Q_x K_t^T; SUB = 1: into the buffer of the tile
+            const uint32_t s = SUB == 2 ? (uint32_t)x : at_uniform(t & 1);
+            const uint32_t d = tm + 128 * s, a = q_lo + x * (M::q_tile >> 4), b = k_lo + at_uniform(key_buf(t)) * (M::tile >> 4);
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) at_mma(d, a + 16 * k, k_hi, b + 16 * k, k_hi, kIdS, k != 0);
+            at_commit(bar(kBarS + s));
+            if (x == SUB - 1) at_commit(bar(kBarKFree + key_buf(t)));
+        };
+        auto outputs = [&](uint32_t t, int x, bool first) {  // O_x += P V_t
+            const uint32_t s = SUB == 2 ? (uint32_t)x : at_uniform(t & 1);
+            const uint32_t a = tm + 128 * s, d = tm + kAtO + x * D, b = v_lo + at_uniform(key_buf(t)) * (M::tile >> 4);
+            const uint32_t add = at_uniform(first ? 0u : 1u);
+#pragma unroll
+            for (int k = 0; k < TN / 16; ++k) at_mma_ta(d, a + 8 * k, b + 2 * D * k, v_hi, kIdO, k ? 1u : add);
+            if (x == SUB - 1) at_commit(bar(kBarVFree + key_buf(t)));
+            if (SUB == 1) at_commit(bar(kBarPV));
+        };
+        auto keys = [&](uint32_t t) { return wait(bar(kBarKFull + key_buf(t)), key_use(t)); };
+        uint32_t items = 0;
+        bool ok = true, first = true;
+#pragma unroll
+        for (int x = 0; x < SUB; ++x) {
+            ok = ok && together(wait(bar(kBarQ + x), 0) && keys(0));
+            if (!ok) break;
+            tc_fence_after();
+            scores(0, x);
+        }
+        for (uint32_t t = 0; t < n_tiles && ok; ++t) {
+            const bool more = t + 1 < n_tiles;
+            const bool last = begin + (int)t + 1 == min(end, it.begin + it.tiles);  // of the item
+            if (SUB == 1 && !last) {
+                ok = together(keys(t + 1));
+                if (!ok) break;
+                tc_fence_after();
+                scores(t + 1, 0);
+            }
+#pragma unroll
+            for (int x = 0; x < SUB; ++x) {
+                ok = together(wait(bar(kBarP + (SUB == 2 ? x : (int)(t & 1))), (SUB == 2 ? t : t >> 1) & 1) &&
+                              wait(bar(kBarVFull + key_buf(t)), key_use(t)) && (SUB == 1 || last || keys(t + 1)));
+                if (!ok) break;
+                tc_fence_after();
+                outputs(t, x, first);
+                if (last) at_commit(bar(kBarDone + x));
+                if (SUB == 2 && !last) scores(t + 1, x);
+            }
+            first = last;
+            if (last && more && ok) {
+                at_next(it, p, R, G, PG);
+                ++items;
+#pragma unroll
+                for (int x = 0; x < SUB; ++x) {
+                    ok = together(wait(bar(kBarQ + x), items & 1) && keys(t + 1));
+                    if (!ok) break;
+                    tc_fence_after();
+                    scores(t + 1, x);
+                }
+            }
+        }
+        if (!ok)  // what was issued ends by itself; no other product is issued
             for (int i = 0; i < 1000; ++i) __nanosleep(1000);
-        }
     }
     __syncwarp();
     tc_fence_before();
@@ -638,7 +686,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
 template <int D, int SUB>
 cudaError_t launch_tc(const AttendArgs &a, int grid, cudaStream_t s) {
     using M = AtSmem<D, SUB>;
-    const int smem = M::before + (a.batch + 1) * 4;
+    const int smem = M::bytes;
     const cudaError_t e = ensure_smem_limit(reinterpret_cast<const void *>(attend_tc_kernel<D, SUB>), smem);
     if (e != cudaSuccess) return e;
     attend_tc_kernel<D, SUB><<<grid, kAtThreads, smem, s>>>(a);
@@ -648,6 +696,8 @@ cudaError_t launch_tc(const AttendArgs &a, int grid, cudaStream_t s) {
 }  // namespace
 
 bool attend_tc_takes(const AttendArgs &a) { return a.in_bf16 && (int64_t)a.T * (a.H / a.Hk) > 16; }
+
+int attend_tc_unit(const AttendArgs &a) { return a.d == 256 ? 2 : 4; }
 
 int attend_tc_rows(const AttendArgs &a) { return a.d <= 128 && (int64_t)a.T * (a.H / a.Hk) > 128 ? 256 : 128; }
 
