@@ -31,7 +31,7 @@ static __device__ uint32_t g_status_attend_tc;
 
 namespace {
 
-constexpr int kAtThreads = 16 * 32;  // (warps 14 and 15 only complete a warpgroup)
+constexpr int kAtThreads = 16 * 32;  // (warps 13 and 15 only complete a warpgroup)
 constexpr int kAtSoftRegs = 176, kAtTurnRegs = 96, kAtIssueRegs = 64;  // of 128 each at launch
 constexpr uint32_t kAtCols = 512;
 constexpr uint32_t kAtO = 256;  // S blocks at columns 0 and 128, O from here on
@@ -66,7 +66,8 @@ struct AtSmem {
     static constexpr int sm_warps = 4 * SUB, turn_warps = 12 - sm_warps;
 };
 // mbarriers
-enum { kBarQ = 0, kBarDone = 2, kBarKFull = 4, kBarKFree = 6, kBarVFull = 8, kBarVFree = 10, kBarS = 12, kBarP = 14, kBarPV = 16, kBarNote = 17,
+enum { kBarQ = 0, kBarDone = 2, kBarKFull = 4, kBarKFree = 6, kBarVFull = 8, kBarVFree = 10, kBarS = 12, kBarP = 14, kBarPV = 18, kBarNote = 19,  // P: halves of two buffers
+      
        kBarKcFull = kBarNote + kAtNotes, kBarKcFree = kBarKcFull + 4, kBarVcFull = kBarKcFree + 4, kBarVcFree = kBarVcFull + 4, kBarCount = kBarVcFree + 4 };
 static_assert(kBarCount * 8 <= 384, "barriers");
 
@@ -77,18 +78,43 @@ __host__ __device__ constexpr uint32_t at_idesc(int n, bool b_mn) {
 // Products are issued by a whole warp in step, one elected lane each, from descriptors whose words are
 // in uniform registers (a reduction's result is).
 __device__ __forceinline__ uint32_t at_uniform(uint32_t x) { return __reduce_max_sync(kFull, x); }
-__device__ __forceinline__ void at_mma(uint32_t d, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t acc) {
+// four K steps: the descriptors' low words advance by a_step and b_step each
+template <int A, int B>
+__device__ __forceinline__ void at_mma4(uint32_t d, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t acc) {
     asm volatile("{\n.reg .pred p, e;\n.reg .b64 da, db;\nelect.sync _|e, 0xffffffff;\nsetp.ne.u32 p, %6, 0;\n"
                  "mov.b64 da, {%1, %2};\nmov.b64 db, {%3, %4};\n"
+                 "@e tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %5, p;\n"
+                 "add.s64 da, da, %7;\nadd.s64 db, db, %8;\nsetp.ne.u32 p, %5, 0;\n"
+                 "@e tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %5, p;\n"
+                 "add.s64 da, da, %7;\nadd.s64 db, db, %8;\n"
+                 "@e tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %5, p;\n"
+                 "add.s64 da, da, %7;\nadd.s64 db, db, %8;\n"
                  "@e tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %5, p;\n}" ::"r"(d),
-                 "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(acc)
+                 "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(acc), "n"(A), "n"(B)
                  : "memory");
 }
-__device__ __forceinline__ void at_mma_ta(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t acc) {
-    asm volatile("{\n.reg .pred p, e;\n.reg .b64 db;\nelect.sync _|e, 0xffffffff;\nsetp.ne.u32 p, %5, 0;\n"
-                 "mov.b64 db, {%2, %3};\n"
-                 "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %4, p;\n}" ::"r"(d),
-                 "r"(a), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(acc)
+template <int A, int B>
+__device__ __forceinline__ void at_mma4_ta(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t acc) {
+    asm volatile("{\n.reg .pred p, e;\n.reg .b64 db;\n.reg .b32 ta;\nelect.sync _|e, 0xffffffff;\nsetp.ne.u32 p, %5, 0;\n"
+                 "mov.b32 ta, %1;\nmov.b64 db, {%2, %3};\n"
+                 "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [ta], db, %4, p;\n"
+                 "add.s32 ta, ta, %6;\nadd.s64 db, db, %7;\nsetp.ne.u32 p, %4, 0;\n"
+                 "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [ta], db, %4, p;\n"
+                 "add.s32 ta, ta, %6;\nadd.s64 db, db, %7;\n"
+                 "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [ta], db, %4, p;\n"
+                 "add.s32 ta, ta, %6;\nadd.s64 db, db, %7;\n"
+                 "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [ta], db, %4, p;\n}" ::"r"(d),
+                 "r"(a), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(acc), "n"(A), "n"(B)
+                 : "memory");
+}
+template <int A, int B>
+__device__ __forceinline__ void at_mma2_ta(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t acc) {
+    asm volatile("{\n.reg .pred p, e;\n.reg .b64 db;\n.reg .b32 ta;\nelect.sync _|e, 0xffffffff;\nsetp.ne.u32 p, %5, 0;\n"
+                 "mov.b32 ta, %1;\nmov.b64 db, {%2, %3};\n"
+                 "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [ta], db, %4, p;\n"
+                 "add.s32 ta, ta, %6;\nadd.s64 db, db, %7;\nsetp.ne.u32 p, %4, 0;\n"
+                 "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [ta], db, %4, p;\n}" ::"r"(d),
+                 "r"(a), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(acc), "n"(A), "n"(B)
                  : "memory");
 }
 __device__ __forceinline__ void at_commit(uint32_t bar) {
@@ -202,17 +228,27 @@ __device__ __forceinline__ void at_next(AtItem &it, const AttendArgs &p, int R, 
     } while (it.tiles == 0);
 }
 
-struct AtWait {  // bounded waits, all of which give up once one has
+// suspended for up to a millisecond at a time, so that a waiting warp leaves the issue slots to others
+__device__ __forceinline__ bool at_try_wait(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok)
+                 : "r"(bar), "r"(parity), "r"(1000000u)
+                 : "memory");
+    return ok != 0;
+}
+struct AtWait {  // bounded waits (about 2 s), all of which give up once one has
     volatile uint32_t *dead;
     __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity) const {
-        if (mbar_try_wait(bar, parity)) return true;
+        if (at_try_wait(bar, parity)) return true;
         const uint64_t t0 = global_timer_ns();
-        for (uint32_t i = 0; i < (1u << 26); ++i) {
-            if (mbar_try_wait(bar, parity)) return true;
-            if ((i & 255u) == 255u && (*dead || global_timer_ns() - t0 > 2000000000ull)) break;
+        for (uint32_t i = 0; !at_try_wait(bar, parity); ++i) {
+            if (*dead || global_timer_ns() - t0 > 2000000000ull || i >> 27) {
+                *dead = 1;
+                return false;
+            }
         }
-        *dead = 1;
-        return false;
+        return true;
     }
 };
 
@@ -229,14 +265,15 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
     if (threadIdx.x == 0) {
         s_dead = 0;
         for (int i = 0; i < 2; ++i) {
-            mbar_init(bar(kBarQ + i), 128);
+            mbar_init(bar(kBarQ + i), 4);
             mbar_init(bar(kBarDone + i), 1);
             mbar_init(bar(kBarKFull + i), M::turn_warps);
             mbar_init(bar(kBarKFree + i), 1);
             mbar_init(bar(kBarVFull + i), M::turn_warps);
             mbar_init(bar(kBarVFree + i), 1);
             mbar_init(bar(kBarS + i), 1);
-            mbar_init(bar(kBarP + i), 128);
+            mbar_init(bar(kBarP + 2 * i), 4);
+            mbar_init(bar(kBarP + 2 * i + 1), 4);
         }
         mbar_init(bar(kBarPV), 1);
         for (int i = 0; i < kAtNotes; ++i) mbar_init(bar(kBarNote + i), 1);
@@ -330,7 +367,8 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
                 }
                 fence_proxy_async_smem();
                 tc_fence_before();
-                at_arrive(bar(kBarQ + x));
+                __syncwarp();
+                if (lane == 0) at_arrive(bar(kBarQ + x));
             }
             float ref = -INFINITY, sum = 0.f;
             int ve = 0;
@@ -338,18 +376,15 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
             for (; at < last; ++at, ++tile) {
                 const int sbuf = SUB == 2 ? x : tile & 1;
                 const uint32_t s_at = lanes + sbuf * 128;
-                ok = together(wait(bar(kBarNote + tile % kAtNotes), (tile / kAtNotes) & 1) &&
-                              wait(bar(kBarS + sbuf), (SUB == 2 ? tile : tile >> 1) & 1));
-                if (!ok) break;
-                tc_fence_after();
+                ok = wait(bar(kBarNote + tile % kAtNotes), (tile / kAtNotes) & 1);
                 const AtNote *const note = reinterpret_cast<const AtNote *>(sm + M::note) + tile % kAtNotes;
                 const int i = at - it.begin;
                 const int token = (it.first + i * PG) * kCachePage;  // of column 0
                 const int hidden = note->hidden, e = note->e;
-                float f[PG];
-#pragma unroll
-                for (int c = 0; c < PG; ++c) f[c] = fmaxf(factor * note->factor[c], FLT_MIN);  // not 0: times a hidden -inf
                 const bool masked = __any_sync(kFull, hidden != 0 || (limit != kNoRow && (limit < token + TN - 1 || from > token)));
+                ok = together(ok && wait(bar(kBarS + sbuf), (SUB == 2 ? tile : tile >> 1) & 1));
+                if (!ok) break;
+                tc_fence_after();
                 uint32_t s[2 * PG][16];
 #pragma unroll
                 for (int c = 0; c < 2 * PG; ++c) at_ld16(s_at + 16 * c, s[c]);
@@ -367,17 +402,12 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
                 }
                 float top = -INFINITY;
 #pragma unroll
-                for (int c = 0; c < 2 * PG; c += 2) {
-                    float m[4];
+                for (int c = 0; c < PG; ++c) {
+                    float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const uint32_t(&v)[16] = s[c + (k >> 1)];
-                        const int at8 = 8 * (k & 1);
-                        m[k] = fmax3(__uint_as_float(v[at8]), __uint_as_float(v[at8 + 1]), __uint_as_float(v[at8 + 2]));
-                        m[k] = fmax3(m[k], __uint_as_float(v[at8 + 3]), __uint_as_float(v[at8 + 4]));
-                        m[k] = fmax3(m[k], __uint_as_float(v[at8 + 5]), fmaxf(__uint_as_float(v[at8 + 6]), __uint_as_float(v[at8 + 7])));
-                    }
-                    top = fmaxf(top, fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])) * f[c / 2]);
+                    for (int j = 0; j < 32; j += 2)
+                        m[(j >> 1) & 3] = fmax3(m[(j >> 1) & 3], __uint_as_float(s[2 * c + (j >> 4)][j & 15]), __uint_as_float(s[2 * c + (j >> 4)][(j & 15) + 1]));
+                    top = fmaxf(top, fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])) * fmaxf(factor * note->factor[c], FLT_MIN));  // not 0: times a hidden -inf
                 }
                 const bool moves = top > ref + kAtLag;
                 const float ref_new = moves ? top : ref;
@@ -408,24 +438,30 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
                 const float base = ref == -INFINITY ? 0.f : -ref;
 #pragma unroll
                 for (int c = 0; c < PG; ++c) {
-                    const float2 f2 = splat2(f[c]), a2 = splat2(base + note->weight[c]);
+                    const float2 f2 = splat2(fmaxf(factor * note->factor[c], FLT_MIN)), a2 = splat2(base + note->weight[c]);
+                    float2 z[16];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j)
+                        z[j] = fma2(make_float2(__uint_as_float(s[2 * c + (j >> 3)][2 * (j & 7)]), __uint_as_float(s[2 * c + (j >> 3)][2 * (j & 7) + 1])), f2, a2);
                     float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
                     uint32_t w[16];
 #pragma unroll
+                    for (int j = 0; j < 16; ++j) z[j] = make_float2(ex2(z[j].x), ex2(z[j].y));
+#pragma unroll
                     for (int j = 0; j < 16; ++j) {
-                        const uint32_t(&v)[16] = s[2 * c + (j >> 3)];
-                        const float2 y = fma2(make_float2(__uint_as_float(v[2 * (j & 7)]), __uint_as_float(v[2 * (j & 7) + 1])), f2, a2);
-                        const float2 z = make_float2(ex2(y.x), ex2(y.y));
-                        part[j & 1] = add2(part[j & 1], z);
-                        w[j] = at_half2(z.x, z.y);
+                        part[j & 1] = add2(part[j & 1], z[j]);
+                        w[j] = at_half2(z[j].x, z[j].y);
                     }
                     at_st16(s_at + 16 * c, w);
                     const float2 both = add2(part[0], part[1]);
                     sum = fmaf(both.x + both.y, note->back[c], sum);
+                    if (c == PG / 2 - 1 || c == PG - 1) {  // half of the tokens
+                        at_st_wait();
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) at_arrive(bar(kBarP + 2 * sbuf + (c == PG - 1)));
+                    }
                 }
-                at_st_wait();
-                tc_fence_before();
-                at_arrive(bar(kBarP + sbuf));
             }
             if (!ok) break;
             ok = together(wait(bar(kBarDone + x), items & 1));  // the item's products into O
@@ -526,9 +562,9 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
                       bar(kBarVFull + buf)))
                 break;
         }
-    } else if (begin < end && warp >= 13) {
+    } else if (begin < end) {
         at_fewer_regs<kAtIssueRegs>();
-        if (warp == 13) {
+        if (warp == 14) {
         // ---- the pages' copies, and what the softmax needs of them: lane = page of a tile ----
         auto entry = [&](int x) {  // of tile x, which lies in `it`
             const int i = (x - it.begin) * PG + lane;
@@ -601,39 +637,30 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
                 mbar_wait_bounded(bar(kBarVcFull + k % M::stages), (k / M::stages) & 1);
             }
         }
-        }
-    } else if (begin < end) {
+        } else if (warp == 12) {
         // ---- the products ----
-        at_fewer_regs<kAtIssueRegs>();
         constexpr uint32_t kIdS = at_idesc(TN, false), kIdO = at_idesc(D, true);
         auto key_buf = [&](uint32_t t) { return M::buffers == 2 ? t & 1u : 0u; };
         auto key_use = [&](uint32_t t) { return (M::buffers == 2 ? t >> 1 : t) & 1u; };
         const uint64_t dq = tc_desc(sb + M::q, 128, 16 * D), dk = tc_desc(sb + M::k, 128, 16 * D), dv = tc_desc(sb + M::v, 16 * D, 128);
         const uint32_t q_lo = at_uniform((uint32_t)dq), k_lo = at_uniform((uint32_t)dk), v_lo = at_uniform((uint32_t)dv);
         const uint32_t k_hi = at_uniform((uint32_t)(dk >> 32)), v_hi = at_uniform((uint32_t)(dv >> 32)), tm = at_uniform(tmem);
-        auto scores = [&](uint32_t t, int x) {  // Q_x K_t^T; SUB = 1: into the buffer of the tile
-            const uint32_t s = SUB == 2 ? (uint32_t)x : at_uniform(t & 1);
-            const uint32_t d = tm + 128 * s, a = q_lo + x * (M::q_tile >> 4), b = k_lo + at_uniform(key_buf(t)) * (M::tile >> 4);
-#pragma unroll
-            for (int k = 0; k < D / 16; ++k) at_mma(d, a + 16 * k, k_hi, b + 16 * k, k_hi, kIdS, k != 0);
-            at_commit(bar(kBarS + s));
+        auto s_buf = [&](uint32_t t, int x) { return SUB == 2 ? (uint32_t)x : t & 1u; };
+        auto s_use = [&](uint32_t t) { return (SUB == 2 ? t : t >> 1) & 1u; };
+        auto scores = [&](uint32_t t, int x) {  // S = Q_x K_t^T
+            const uint32_t d = tm + 128 * at_uniform(s_buf(t, x)), b = k_lo + at_uniform(key_buf(t)) * (M::tile >> 4);
+            const uint32_t a = q_lo + at_uniform(x) * (M::q_tile >> 4);
+#pragma unroll 1
+            for (int k = 0; k < D / 16; k += 4) at_mma4<16, 16>(d, a + 16 * k, k_hi, b + 16 * k, k_hi, kIdS, k != 0);
+            at_commit(bar(kBarS + s_buf(t, x)));
             if (x == SUB - 1) at_commit(bar(kBarKFree + key_buf(t)));
-        };
-        auto outputs = [&](uint32_t t, int x, bool first) {  // O_x += P V_t
-            const uint32_t s = SUB == 2 ? (uint32_t)x : at_uniform(t & 1);
-            const uint32_t a = tm + 128 * s, d = tm + kAtO + x * D, b = v_lo + at_uniform(key_buf(t)) * (M::tile >> 4);
-            const uint32_t add = at_uniform(first ? 0u : 1u);
-#pragma unroll
-            for (int k = 0; k < TN / 16; ++k) at_mma_ta(d, a + 8 * k, b + 2 * D * k, v_hi, kIdO, k ? 1u : add);
-            if (x == SUB - 1) at_commit(bar(kBarVFree + key_buf(t)));
-            if (SUB == 1) at_commit(bar(kBarPV));
         };
         auto keys = [&](uint32_t t) { return wait(bar(kBarKFull + key_buf(t)), key_use(t)); };
         uint32_t items = 0;
         bool ok = true, first = true;
-#pragma unroll
+#pragma unroll 1
         for (int x = 0; x < SUB; ++x) {
-            ok = ok && together(wait(bar(kBarQ + x), 0) && keys(0));
+            ok = together(ok && wait(bar(kBarQ + x), 0) && keys(0));
             if (!ok) break;
             tc_fence_after();
             scores(0, x);
@@ -641,19 +668,32 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
         for (uint32_t t = 0; t < n_tiles && ok; ++t) {
             const bool more = t + 1 < n_tiles;
             const bool last = begin + (int)t + 1 == min(end, it.begin + it.tiles);  // of the item
+            ok = (last || keys(t + 1)) && wait(bar(kBarVFull + key_buf(t)), key_use(t));
             if (SUB == 1 && !last) {
-                ok = together(keys(t + 1));
-                if (!ok) break;
+                if (!together(ok)) break;
                 tc_fence_after();
                 scores(t + 1, 0);
             }
-#pragma unroll
+#pragma unroll 1
             for (int x = 0; x < SUB; ++x) {
-                ok = together(wait(bar(kBarP + (SUB == 2 ? x : (int)(t & 1))), (SUB == 2 ? t : t >> 1) & 1) &&
-                              wait(bar(kBarVFull + key_buf(t)), key_use(t)) && (SUB == 1 || last || keys(t + 1)));
+#pragma unroll 1
+                for (int half = 0; half < 2; ++half) {  // O_x += P V_t, half of the tokens
+                    ok = together(ok && wait(bar(kBarP + 2 * s_buf(t, x) + half), s_use(t)));
+                    if (!ok) break;
+                    tc_fence_after();
+                    constexpr int kSteps = TN / 32;
+                    const uint32_t h = at_uniform(half);
+                    const uint32_t a = tm + 128 * at_uniform(s_buf(t, x)) + 8 * kSteps * h;
+                    const uint32_t b = v_lo + at_uniform(key_buf(t)) * (M::tile >> 4) + 2 * D * kSteps * h;
+                    const uint32_t add = at_uniform(first && half == 0 ? 0u : 1u), d = tm + kAtO + D * at_uniform(x);
+                    if constexpr (kSteps == 4)
+                        at_mma4_ta<8, 2 * D>(d, a, b, v_hi, kIdO, add);
+                    else
+                        at_mma2_ta<8, 2 * D>(d, a, b, v_hi, kIdO, add);
+                }
                 if (!ok) break;
-                tc_fence_after();
-                outputs(t, x, first);
+                if (x == SUB - 1) at_commit(bar(kBarVFree + key_buf(t)));
+                if (SUB == 1) at_commit(bar(kBarPV));
                 if (last) at_commit(bar(kBarDone + x));
                 if (SUB == 2 && !last) scores(t + 1, x);
             }
@@ -661,9 +701,9 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
             if (last && more && ok) {
                 at_next(it, p, R, G, PG);
                 ++items;
-#pragma unroll
+#pragma unroll 1
                 for (int x = 0; x < SUB; ++x) {
-                    ok = together(wait(bar(kBarQ + x), items & 1) && keys(t + 1));
+                    ok = together(ok && wait(bar(kBarQ + x), items & 1) && keys(t + 1));
                     if (!ok) break;
                     tc_fence_after();
                     scores(t + 1, x);
@@ -672,6 +712,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
         }
         if (!ok)  // what was issued ends by itself; no other product is issued
             for (int i = 0; i < 1000; ++i) __nanosleep(1000);
+        }
     }
     __syncwarp();
     tc_fence_before();
