@@ -31,7 +31,7 @@ static __device__ uint32_t g_status_attend_tc;
 
 namespace {
 
-constexpr int kAtThreads = 16 * 32;  // (warps 13 and 15 only complete a warpgroup)
+constexpr int kAtThreads = 16 * 32;  // (warp 15 only completes a warpgroup)
 constexpr int kAtSoftRegs = 176, kAtTurnRegs = 96, kAtIssueRegs = 64;  // of 128 each at launch
 constexpr uint32_t kAtCols = 512;
 constexpr uint32_t kAtO = 256;  // S blocks at columns 0 and 128, O from here on
@@ -66,7 +66,7 @@ struct AtSmem {
     static constexpr int sm_warps = 4 * SUB, turn_warps = 12 - sm_warps;
 };
 // mbarriers
-enum { kBarQ = 0, kBarDone = 2, kBarKFull = 4, kBarKFree = 6, kBarVFull = 8, kBarVFree = 10, kBarS = 12, kBarP = 14, kBarPV = 18, kBarNote = 19,  // P: halves of two buffers
+enum { kBarQ = 0, kBarDone = 2, kBarKFull = 4, kBarKFree = 6, kBarVFull = 8, kBarVFree = 10, kBarS = 12, kBarP = 14, kBarPV = 18, kBarTurn = 19, kBarNote = 21,  // P: halves of two buffers
       
        kBarKcFull = kBarNote + kAtNotes, kBarKcFree = kBarKcFull + 4, kBarVcFull = kBarKcFree + 4, kBarVcFree = kBarVcFull + 4, kBarCount = kBarVcFree + 4 };
 static_assert(kBarCount * 8 <= 384, "barriers");
@@ -268,9 +268,10 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
             mbar_init(bar(kBarQ + i), 4);
             mbar_init(bar(kBarDone + i), 1);
             mbar_init(bar(kBarKFull + i), M::turn_warps);
-            mbar_init(bar(kBarKFree + i), 1);
+            mbar_init(bar(kBarKFree + i), SUB);
             mbar_init(bar(kBarVFull + i), M::turn_warps);
-            mbar_init(bar(kBarVFree + i), 1);
+            mbar_init(bar(kBarVFree + i), SUB);
+            mbar_init(bar(kBarTurn + i), 1);
             mbar_init(bar(kBarS + i), 1);
             mbar_init(bar(kBarP + 2 * i), 4);
             mbar_init(bar(kBarP + 2 * i + 1), 4);
@@ -637,77 +638,72 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
                 mbar_wait_bounded(bar(kBarVcFull + k % M::stages), (k / M::stages) & 1);
             }
         }
-        } else if (warp == 12) {
-        // ---- the products ----
+        } else if (warp - 12 < SUB) {
+        // ---- the products: a warp per block of rows; with two blocks they take turns, a tile's P V and the next tile's
+        // Q K^T at a time, so that one block's softmax runs under the other's products ----
         constexpr uint32_t kIdS = at_idesc(TN, false), kIdO = at_idesc(D, true);
+        const int x = warp - 12;
         auto key_buf = [&](uint32_t t) { return M::buffers == 2 ? t & 1u : 0u; };
         auto key_use = [&](uint32_t t) { return (M::buffers == 2 ? t >> 1 : t) & 1u; };
-        const uint64_t dq = tc_desc(sb + M::q, 128, 16 * D), dk = tc_desc(sb + M::k, 128, 16 * D), dv = tc_desc(sb + M::v, 16 * D, 128);
+        const uint64_t dq = tc_desc(sb + M::q + x * M::q_tile, 128, 16 * D), dk = tc_desc(sb + M::k, 128, 16 * D), dv = tc_desc(sb + M::v, 16 * D, 128);
         const uint32_t q_lo = at_uniform((uint32_t)dq), k_lo = at_uniform((uint32_t)dk), v_lo = at_uniform((uint32_t)dv);
         const uint32_t k_hi = at_uniform((uint32_t)(dk >> 32)), v_hi = at_uniform((uint32_t)(dv >> 32)), tm = at_uniform(tmem);
-        auto s_buf = [&](uint32_t t, int x) { return SUB == 2 ? (uint32_t)x : t & 1u; };
+        const uint32_t tm_o = at_uniform(tmem + kAtO + x * D);
+        auto s_buf = [&](uint32_t t) { return SUB == 2 ? (uint32_t)x : t & 1u; };
         auto s_use = [&](uint32_t t) { return (SUB == 2 ? t : t >> 1) & 1u; };
-        auto scores = [&](uint32_t t, int x) {  // S = Q_x K_t^T
-            const uint32_t d = tm + 128 * at_uniform(s_buf(t, x)), b = k_lo + at_uniform(key_buf(t)) * (M::tile >> 4);
-            const uint32_t a = q_lo + at_uniform(x) * (M::q_tile >> 4);
+        auto scores = [&](uint32_t t) {  // S = Q_x K_t^T
+            const uint32_t d = tm + 128 * at_uniform(s_buf(t)), b = k_lo + at_uniform(key_buf(t)) * (M::tile >> 4);
 #pragma unroll 1
-            for (int k = 0; k < D / 16; k += 4) at_mma4<16, 16>(d, a + 16 * k, k_hi, b + 16 * k, k_hi, kIdS, k != 0);
-            at_commit(bar(kBarS + s_buf(t, x)));
-            if (x == SUB - 1) at_commit(bar(kBarKFree + key_buf(t)));
+            for (int k = 0; k < D / 16; k += 4) at_mma4<16, 16>(d, q_lo + 16 * k, k_hi, b + 16 * k, k_hi, kIdS, k != 0);
+            at_commit(bar(kBarS + s_buf(t)));
+            at_commit(bar(kBarKFree + key_buf(t)));
         };
         auto keys = [&](uint32_t t) { return wait(bar(kBarKFull + key_buf(t)), key_use(t)); };
         uint32_t items = 0;
-        bool ok = true, first = true;
-#pragma unroll 1
-        for (int x = 0; x < SUB; ++x) {
-            ok = together(ok && wait(bar(kBarQ + x), 0) && keys(0));
-            if (!ok) break;
+        bool ok = together(wait(bar(kBarQ + x), 0) && keys(0)), first = true;
+        if (ok) {
             tc_fence_after();
-            scores(0, x);
+            scores(0);
         }
         for (uint32_t t = 0; t < n_tiles && ok; ++t) {
             const bool more = t + 1 < n_tiles;
             const bool last = begin + (int)t + 1 == min(end, it.begin + it.tiles);  // of the item
             ok = (last || keys(t + 1)) && wait(bar(kBarVFull + key_buf(t)), key_use(t));
+            if (SUB == 2) ok = ok && (x ? wait(bar(kBarTurn), t & 1) : t == 0 || wait(bar(kBarTurn + 1), (t - 1) & 1));
             if (SUB == 1 && !last) {
                 if (!together(ok)) break;
                 tc_fence_after();
-                scores(t + 1, 0);
+                scores(t + 1);
             }
 #pragma unroll 1
-            for (int x = 0; x < SUB; ++x) {
-#pragma unroll 1
-                for (int half = 0; half < 2; ++half) {  // O_x += P V_t, half of the tokens
-                    ok = together(ok && wait(bar(kBarP + 2 * s_buf(t, x) + half), s_use(t)));
-                    if (!ok) break;
-                    tc_fence_after();
-                    constexpr int kSteps = TN / 32;
-                    const uint32_t h = at_uniform(half);
-                    const uint32_t a = tm + 128 * at_uniform(s_buf(t, x)) + 8 * kSteps * h;
-                    const uint32_t b = v_lo + at_uniform(key_buf(t)) * (M::tile >> 4) + 2 * D * kSteps * h;
-                    const uint32_t add = at_uniform(first && half == 0 ? 0u : 1u), d = tm + kAtO + D * at_uniform(x);
-                    if constexpr (kSteps == 4)
-                        at_mma4_ta<8, 2 * D>(d, a, b, v_hi, kIdO, add);
-                    else
-                        at_mma2_ta<8, 2 * D>(d, a, b, v_hi, kIdO, add);
-                }
+            for (int half = 0; half < 2; ++half) {  // O_x += P V_t, half of the tokens
+                ok = together(ok && wait(bar(kBarP + 2 * s_buf(t) + half), s_use(t)));
                 if (!ok) break;
-                if (x == SUB - 1) at_commit(bar(kBarVFree + key_buf(t)));
-                if (SUB == 1) at_commit(bar(kBarPV));
-                if (last) at_commit(bar(kBarDone + x));
-                if (SUB == 2 && !last) scores(t + 1, x);
+                tc_fence_after();
+                constexpr int kSteps = TN / 32;
+                const uint32_t h = at_uniform(half);
+                const uint32_t a = tm + 128 * at_uniform(s_buf(t)) + 8 * kSteps * h;
+                const uint32_t b = v_lo + at_uniform(key_buf(t)) * (M::tile >> 4) + 2 * D * kSteps * h;
+                const uint32_t add = at_uniform(first && half == 0 ? 0u : 1u);
+                if constexpr (kSteps == 4)
+                    at_mma4_ta<8, 2 * D>(tm_o, a, b, v_hi, kIdO, add);
+                else
+                    at_mma2_ta<8, 2 * D>(tm_o, a, b, v_hi, kIdO, add);
             }
+            if (!ok) break;
+            if (SUB == 2 && !last) scores(t + 1);
+            at_commit(bar(kBarVFree + key_buf(t)));
+            if (SUB == 1) at_commit(bar(kBarPV));
+            if (last) at_commit(bar(kBarDone + x));
+            if (SUB == 2 && lane == 0) at_arrive(bar(kBarTurn + x));
             first = last;
-            if (last && more && ok) {
+            if (last && more) {
                 at_next(it, p, R, G, PG);
                 ++items;
-#pragma unroll 1
-                for (int x = 0; x < SUB; ++x) {
-                    ok = together(ok && wait(bar(kBarQ + x), items & 1) && keys(t + 1));
-                    if (!ok) break;
-                    tc_fence_after();
-                    scores(t + 1, x);
-                }
+                ok = together(wait(bar(kBarQ + x), items & 1) && keys(t + 1));
+                if (!ok) break;
+                tc_fence_after();
+                scores(t + 1);
             }
         }
         if (!ok)  // what was issued ends by itself; no other product is issued
