@@ -753,8 +753,15 @@ class CacheLayout:
     num_kv_heads: int
     d: int
 
+    def __post_init__(self):
+        # what every call needs of the layout, made once
+        c = DampCacheLayout(self.num_heads, self.num_kv_heads, self.d)
+        object.__setattr__(self, "_c", c)
+        object.__setattr__(self, "_ref", ctypes.byref(c))
+        object.__setattr__(self, "_workspace", {})
+
     def c(self) -> DampCacheLayout:
-        return DampCacheLayout(self.num_heads, self.num_kv_heads, self.d)
+        return self._c
 
     @property
     def record_bytes(self) -> int:
@@ -764,7 +771,7 @@ class CacheLayout:
 
 def cache_page_bytes(layout: CacheLayout) -> int:
     """Bytes of a page, all KV heads; 0 if the layout is invalid."""
-    return int(lib().damp_cache_page_bytes(ctypes.byref(layout.c())))
+    return int(lib().damp_cache_page_bytes(layout._ref))
 
 
 def new_cache(layout: CacheLayout, num_pages: int, device="cuda"):
@@ -773,15 +780,16 @@ def new_cache(layout: CacheLayout, num_pages: int, device="cuda"):
     return torch.zeros((num_pages, layout.num_kv_heads, layout.record_bytes), dtype=torch.uint8, device=device)
 
 
-def _token_rows(name, t, B, T, H, d, dtype):
-    """(address, elements from token to token) of t [B, T, H, d]: a tensor whose tokens are evenly
+def _token_rows(name, t, shape, dtype, device):
+    """(address, elements from token to token) of t [B, T, H, d] on the device: a tensor whose tokens are evenly
     spaced (contiguous, or a slice of the heads of a larger projection)."""
     if t is None:
         raise ValueError(f"{name} is required")
-    if t.shape != (B, T, H, d) or t.dtype != dtype:
-        _want(name, t, (B, T, H, d), dtype=dtype)
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be a CUDA tensor")
+    if t.shape != shape or t.dtype != dtype:
+        _want(name, t, shape, dtype=dtype)
+    if t.get_device() != device:
+        _wrong_device(name, t, device)
+    B, T, H, d = shape
     if t.is_contiguous():
         return t.data_ptr(), H * d
     sb, st, sh, sd = t.stride()
@@ -791,24 +799,28 @@ def _token_rows(name, t, B, T, H, d, dtype):
     return t.data_ptr(), step
 
 
-def _same_device(first, *others):
-    """ValueError unless all tensors lie on the current device."""
-    import torch
-    at = torch.cuda.current_device()
-    for t in (first, *others):
-        if t is not None and t.get_device() != at:
-            raise ValueError(f"tensors must lie on the current device ({at}), got device {t.get_device()}")
+def _wrong_device(name, t, device):
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    raise ValueError(f"{name} lies on device {t.get_device()}, the current device is {device}")
 
 
-def _float_type(name, t):
-    import torch
-    if t is None or not isinstance(t, torch.Tensor):
+def _here(name, t, shape, dtype, device):
+    """As _given, for a tensor of the current device."""
+    if t is None:
         raise ValueError(f"{name} is required")
-    if t.dtype == torch.bfloat16:
-        return IN_BF16
-    if t.dtype == torch.float32:
-        return IN_FP32
-    raise TypeError(f"{name} must be bfloat16 or float32")
+    if t.shape != shape or t.dtype != dtype:
+        _want(name, t, shape, dtype=dtype)
+    if t.get_device() != device:
+        _wrong_device(name, t, device)
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _call_device(torch, first):
+    """The current device (no call on it where there is none: the first tensor is then refused)."""
+    return torch.cuda.current_device() if first.is_cuda else 0
 
 
 def rotary_frequencies(dim, base=10000.0, scaling="none", factor=1.0, trained=4096, turns=(32.0, 1.0), device="cuda"):
@@ -851,47 +863,48 @@ def rotary(q, k, positions, freq, interleaved=False, scale=1.0, q_out=None, k_ou
     slices of the heads of one projection.  Returns (q, k) rotated, contiguous; q_out and k_out may be
     q and k themselves where those are contiguous."""
     import torch
-    dt = _float_type("q", q)
-    if q.dim() != 4 or (k is not None and k.dim() != 4):
+    if q is None or q.dim() != 4 or (k is not None and k.dim() != 4):
         raise ValueError("q and k must be [B, T, heads, d] tensors")
     if freq is None or freq.dim() != 1:
         raise ValueError("freq must be a float64 tensor [rotary_dim / 2]")
     if positions is None or positions.dim() not in (1, 2):
         raise ValueError("positions must be an int32 tensor [B, T] or [B]")
-    B, T, H, d = q.shape
-    Hk = 0 if k is None else k.shape[2]
-    qp, qs = _token_rows("q", q, B, T, H, d, q.dtype)
-    kp, ks = (None, 0) if k is None else _token_rows("k", k, B, T, Hk, d, q.dtype)
-    per_row = positions.dim() == 1
-    pos = _given("positions", positions, (B,) if per_row else (B, T), torch.int32)
-    f = _given("freq", freq, freq.shape, torch.float64)
-    if q_out is None:
-        q_out = _new(q.shape, q.dtype, q, stream)
-    if k is not None and k_out is None:
-        k_out = _new(k.shape, k.dtype, k, stream)
     if k is None and k_out is not None:
         raise ValueError("k_out without k")
-    _same_device(q, k, positions, freq, q_out, k_out)
-    _check(lib().damp_rotary(qp, qs, H, kp, ks, Hk, d, dt, pos, per_row, B, T, f, 2 * freq.shape[0], bool(interleaved),
-                             float(scale), _given("q_out", q_out, q.shape, q.dtype),
-                             None if k is None else _given("k_out", k_out, k.shape, k.dtype), _stream(stream)), "damp_rotary")
+    dtype, dev = q.dtype, _call_device(torch, q)
+    if dtype != torch.bfloat16 and dtype != torch.float32:
+        raise TypeError("q must be bfloat16 or float32")
+    shape = q.shape
+    B, T, H, d = shape
+    per_row = positions.dim() == 1
+    qp, qs = _token_rows("q", q, shape, dtype, dev)
+    if q_out is None:
+        q_out = _new(shape, dtype, q, stream)
+    kp = ks = ko = None
+    Hk = 0
+    if k is not None:
+        Hk = k.shape[2]
+        k_shape = (B, T, Hk, d)
+        kp, ks = _token_rows("k", k, k_shape, dtype, dev)
+        if k_out is None:
+            k_out = _new(k_shape, dtype, k, stream)
+        ko = _here("k_out", k_out, k_shape, dtype, dev)
+    _check(lib().damp_rotary(qp, qs, H, kp, ks or 0, Hk, d, IN_BF16 if dtype == torch.bfloat16 else IN_FP32,
+                             _here("positions", positions, (B,) if per_row else (B, T), torch.int32, dev), per_row, B, T,
+                             _here("freq", freq, freq.shape, torch.float64, dev), 2 * freq.shape[0], bool(interleaved), scale,
+                             _here("q_out", q_out, shape, dtype, dev), ko, _stream(stream)), "damp_rotary")
     return q_out, k_out
 
 
-def _cache(layout, cache, pages, B):
+def _cache(layout, cache, pages, B, dev, i32, u8):
     """(pool address, pages, table address, entries of a row) of a cache and its page table."""
-    import torch
     if cache is None or cache.dim() != 3:
         raise ValueError("cache must be a [num_pages, num_kv_heads, record_bytes] tensor")
-    pool = _given("cache", cache, (cache.shape[0], layout.num_kv_heads, layout.record_bytes), torch.uint8)
     if pages is None or pages.dim() != 2:
         raise ValueError("pages must be an int32 tensor [B, pages of a row]")
-    return pool, cache.shape[0], _given("pages", pages, (B, pages.shape[1]), torch.int32), pages.shape[1]
-
-
-def _per_row(name, t, B):
-    import torch
-    return None if t is None else _given(name, t, (B,), torch.int32)
+    n, W = cache.shape[0], pages.shape[1]
+    return (_here("cache", cache, (n, layout.num_kv_heads, 2 * CACHE_PAGE * layout.d + 16), u8, dev), n,
+            _here("pages", pages, (B, W), i32, dev), W)
 
 
 def cache_append(layout, cache, k, v, pages, start, lengths=None, stream=None):
@@ -899,18 +912,20 @@ def cache_append(layout, cache, k, v, pages, start, lengths=None, stream=None):
     row b becomes token start[b] + t of the row (start int32 [B]: the tokens it holds), whose page is
     pages[b, (start[b] + t) // CACHE_PAGE] (int32 [B, W]).  Row b has lengths[b] new tokens (default T).
     k and v may be slices of the heads of one projection.  The pages written must be distinct."""
-    dt = _float_type("k", k)
-    if k.dim() != 4:
+    import torch
+    if k is None or k.dim() != 4:
         raise ValueError("k must be a [B, T, num_kv_heads, d] tensor")
-    B, T = k.shape[:2]
-    pool, n, table, W = _cache(layout, cache, pages, B)
-    kp, ks = _token_rows("k", k, B, T, layout.num_kv_heads, layout.d, k.dtype)
-    vp, vs = _token_rows("v", v, B, T, layout.num_kv_heads, layout.d, k.dtype)
-    if start is None:
-        raise ValueError("start is required")
-    _same_device(cache, k, v, pages, start, lengths)
-    _check(lib().damp_cache_append(ctypes.byref(layout.c()), pool, n, table, W, B, T, _per_row("start", start, B),
-                                   _per_row("lengths", lengths, B), kp, ks, vp, vs, dt, _stream(stream)), "damp_cache_append")
+    dtype, dev, i32 = k.dtype, _call_device(torch, k), torch.int32
+    if dtype != torch.bfloat16 and dtype != torch.float32:
+        raise TypeError("k must be bfloat16 or float32")
+    B, T = k.shape[0], k.shape[1]
+    shape = (B, T, layout.num_kv_heads, layout.d)
+    kp, ks = _token_rows("k", k, shape, dtype, dev)
+    vp, vs = _token_rows("v", v, shape, dtype, dev)
+    pool, n, table, W = _cache(layout, cache, pages, B, dev, i32, torch.uint8)
+    _check(lib().damp_cache_append(layout._ref, pool, n, table, W, B, T, _here("start", start, (B,), i32, dev),
+                                   None if lengths is None else _here("lengths", lengths, (B,), i32, dev), kp, ks, vp, vs,
+                                   IN_BF16 if dtype == torch.bfloat16 else IN_FP32, _stream(stream)), "damp_cache_append")
 
 
 def cache_read(layout, cache, pages, lengths, tokens, start=None, dtype=None, k=None, v=None, stream=None):
@@ -918,26 +933,26 @@ def cache_read(layout, cache, pages, lengths, tokens, start=None, dtype=None, k=
     start[b] + tokens - 1 of each row (start int32 [B], default 0), zeros from lengths[b] on (the tokens
     that row b holds)."""
     import torch
+    if cache is None:
+        raise ValueError("cache is required")
     if pages is None or pages.dim() != 2:
         raise ValueError("pages must be an int32 tensor [B, pages of a row]")
-    if lengths is None:
-        raise ValueError("lengths is required")
-    B, T = pages.shape[0], int(tokens)
+    B, T, dev, i32 = pages.shape[0], int(tokens), _call_device(torch, cache), torch.int32
     if T < 0:
         raise ValueError("tokens must not be negative")
     if dtype is None:
         dtype = torch.bfloat16 if k is None else k.dtype
-    if dtype not in (torch.bfloat16, torch.float32):
+    if dtype != torch.bfloat16 and dtype != torch.float32:
         raise TypeError("dtype must be bfloat16 or float32")
-    pool, n, table, W = _cache(layout, cache, pages, B)
+    pool, n, table, W = _cache(layout, cache, pages, B, dev, i32, torch.uint8)
+    held = _here("lengths", lengths, (B,), i32, dev)
     shape = (B, T, layout.num_kv_heads, layout.d)
     if k is None:
         k = _new(shape, dtype, cache, stream)
     if v is None:
         v = _new(shape, dtype, cache, stream)
-    _same_device(cache, pages, lengths, start, k, v)
-    _check(lib().damp_cache_read(ctypes.byref(layout.c()), pool, n, table, W, B, T, _per_row("start", start, B),
-                                 _per_row("lengths", lengths, B), _given("k", k, shape, dtype), _given("v", v, shape, dtype),
+    _check(lib().damp_cache_read(layout._ref, pool, n, table, W, B, T, None if start is None else _here("start", start, (B,), i32, dev),
+                                 held, _here("k", k, shape, dtype, dev), _here("v", v, shape, dtype, dev),
                                  IN_BF16 if dtype == torch.bfloat16 else IN_FP32, _stream(stream)), "damp_cache_read")
     return k, v
 
@@ -949,26 +964,28 @@ def cache_attend(layout, cache, q, pages, lengths, q_lengths=None, scale=None, w
     scale: of q.k (default d^-1/2).  Returns o [B, T, H, d] of q's type, zeros past q_lengths[b].  T = 1 is a
     decode step, a few tokens a draft, many a prompt (append their keys and values first)."""
     import torch
-    dt = _float_type("q", q)
-    if q.dim() != 4:
+    if q is None or q.dim() != 4:
         raise ValueError("q must be a [B, T, num_heads, d] tensor")
-    if lengths is None:
-        raise ValueError("lengths is required")
     if window is not None and window < 1:
         raise ValueError("window must be 1 at least")
-    B, T, H, d = q.shape[0], q.shape[1], layout.num_heads, layout.d
-    pool, n, table, W = _cache(layout, cache, pages, B)
-    qp, qs = _token_rows("q", q, B, T, H, d, q.dtype)
+    dtype, dev, i32 = q.dtype, _call_device(torch, q), torch.int32
+    if dtype != torch.bfloat16 and dtype != torch.float32:
+        raise TypeError("q must be bfloat16 or float32")
+    B, T, d = q.shape[0], q.shape[1], layout.d
+    shape, dt = (B, T, layout.num_heads, d), IN_BF16 if dtype == torch.bfloat16 else IN_FP32
+    qp, qs = _token_rows("q", q, shape, dtype, dev)
+    pool, n, table, W = _cache(layout, cache, pages, B, dev, i32, torch.uint8)
+    held = _here("lengths", lengths, (B,), i32, dev)
     if o is None:
-        o = _new((B, T, H, d), q.dtype, q, stream)
-    _same_device(cache, q, pages, lengths, q_lengths, o)
-    c, L = ctypes.byref(layout.c()), lib()
-    need = L.damp_cache_attend_workspace(c, B, T, dt)
-    ws = _new((need,), torch.uint8, q, stream) if need else None
-    _check(L.damp_cache_attend(c, pool, n, table, W, B, T, _per_row("lengths", lengths, B),
-                               _per_row("q_lengths", q_lengths, B), qp, qs, d ** -0.5 if scale is None else float(scale),
-                               0 if window is None else min(int(window), (1 << 31) - 1), _given("o", o, (B, T, H, d), q.dtype), dt,
-                               None if ws is None else ws.data_ptr(), need, _stream(stream)), "damp_cache_attend")
+        o = _new(shape, dtype, q, stream)
+    c, L = layout._ref, lib()
+    need = layout._workspace.get((dev, B, T, dt))
+    if need is None:
+        need = layout._workspace[dev, B, T, dt] = L.damp_cache_attend_workspace(c, B, T, dt)
+    ws = _new((need,), torch.uint8, q, stream)
+    _check(L.damp_cache_attend(c, pool, n, table, W, B, T, held, None if q_lengths is None else _here("q_lengths", q_lengths, (B,), i32, dev),
+                               qp, qs, d ** -0.5 if scale is None else scale, 0 if window is None else min(window, 0x7fffffff),
+                               _here("o", o, shape, dtype, dev), dt, ws.data_ptr(), need, _stream(stream)), "damp_cache_attend")
     return o
 
 

@@ -128,9 +128,7 @@ __global__ void __launch_bounds__(AttCfg<D, MT, F32>::threads, 1) attend_kernel(
     }
     att_count(p, R, G, 1, before);
     const int warps = gridDim.x * C::warps;
-    const AttWork work = att_work(p.workspace, p.batch, warps, R, D);
-    if (blockIdx.x == 0)
-        for (int b = threadIdx.x; b <= p.batch; b += C::threads) work.before[b] = before[b];
+    const AttWork work = att_work(p.workspace, warps, R);
     const int total = before[p.batch] * p.Hk, per = att_per(total, warps);
     // warps of one range after the other lie on different SMs
     const int range = warp * gridDim.x + blockIdx.x;
@@ -490,59 +488,64 @@ __global__ void __launch_bounds__(AttCfg<D, MT, F32>::threads, 1) attend_kernel(
     } else if (item >= 0) {
         finish();
     }
+    if (lane == 0) {
+        const bool split = !failed && item >= 0 && now.begin >= begin && now.begin + now.count > end;
+        work.split[range] = split ? AttSplit{now.b, now.rt, now.h, (now.begin + now.count - 1) / per} : AttSplit{0, 0, 0, -1};
+    }
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
-// Joins the parts of items that several ranges hold; clears the rows of none.  `wpr` warps per row,
-// blockIdx.y: parts of an item's rows.
+// Joins the parts of items that several ranges hold (blockIdx.x: the range that the item starts in, blockIdx.y:
+// parts of its rows, wpr: warps per row), and clears, in the blocks after those, the outputs of queries that see
+// no token or are none: blocks of `slice` queries of a row.
 template <int D, bool BF>
-__global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(const AttendArgs p, int R, int ranges, int unit, int wpr) {
+__global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(const AttendArgs p, int R, int ranges, int rows, int wpr, int slice) {
     constexpr int V = D / 32;  // columns of a lane
     __shared__ float part[kJoinThreads / 32][D + 2];
-    __shared__ int sums[kJoinThreads / 32];
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    const AttWork work = att_work(p.workspace, p.batch, ranges, R, D);
-    const int G = p.H / p.Hk, tiles = att_tiles(p.T, R, G);
-    const int h = blockIdx.x % p.Hk, bt = blockIdx.x / p.Hk, rt = bt % tiles, b = bt / tiles;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const AttRow w = att_row(p, b);
-    const int units = att_units(att_item(p, w, rt, R, G).pages, unit);
-    int ahead = 0;  // units of the row's earlier items
-    if (tiles > 1) {
-        for (int i = threadIdx.x; i < rt; i += kJoinThreads) ahead += att_units(att_item(p, w, i, R, G).pages, unit);
-        ahead = __reduce_add_sync(kFull, ahead);
-        if (lane == 0) sums[warp] = ahead;
-        __syncthreads();
-        ahead = 0;
-        for (int i = 0; i < kJoinThreads / 32; ++i) ahead += sums[i];
+    const int G = p.H / p.Hk;
+    if ((int)blockIdx.x >= ranges) {
+        if (blockIdx.y) return;
+        const int i = blockIdx.x - ranges, slices = (p.T + slice - 1) / slice, b = i / slices;
+        const AttRow w = att_row(p, b);
+        const int t0 = (i - b * slices) * slice, t1 = min(p.T, t0 + slice);
+        constexpr int kChunk = BF ? 8 : 4;  // values of 16 bytes
+        const int64_t token = (int64_t)p.H * D / kChunk;
+        for (int side = 0; side < 2; ++side) {  // before the first token, after the last query
+            const int lo = side ? max(t0, w.n) : t0, hi = side ? t1 : min(t1, w.n - w.len);
+            uint4 *const o = static_cast<uint4 *>(p.o) + ((int64_t)b * p.T + lo) * token;
+            for (int64_t k = threadIdx.x; k < (hi - lo) * token; k += kJoinThreads) o[k] = make_uint4(0, 0, 0, 0);
+        }
+        return;
     }
-    const int total = work.before[p.batch] * p.Hk, per = att_per(total, ranges);
-    const int begin = (work.before[b] + ahead) * p.Hk + h * units;
-    const int first = begin / per, last = units ? (begin + units - 1) / per : first;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const AttWork work = att_work(p.workspace, ranges, R);
+    const int first = blockIdx.x;
+    const AttSplit it = work.split[first];
+    if (it.last < 0) return;
+    const int n = p.q_lengths ? max(0, min(p.q_lengths[it.b], p.T)) : p.T;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int team = warp / wpr, mate = warp % wpr, teams = kJoinThreads / 32 / wpr;
-    for (int r0 = blockIdx.y * teams; r0 < R; r0 += gridDim.y * teams) {
+    for (int r0 = blockIdx.y * teams; r0 < rows; r0 += gridDim.y * teams) {
         const int r = r0 + team;
-        const int row = rt * R + r, t = row / G;
-        const bool inside = r < R && t < p.T;
-        const bool empty = t >= w.n || units == 0;
-        if (!inside && wpr == 1) continue;
-        const bool joins = inside && !empty && first != last;
+        const int row = it.rt * R + r, t = row / G;
+        const bool live = r < rows && t < n;
+        if (!live && wpr == 1) continue;
         float o[V], M = -INFINITY, L = 0.f;
 #pragma unroll
         for (int i = 0; i < V; ++i) o[i] = 0.f;
-        if (joins) {
-            constexpr int U = 8;
-            for (int x0 = first + mate; x0 <= last; x0 += U * wpr) {
+        if (live) {
+            constexpr int U = D == 256 ? 4 : 8;
+            for (int x0 = first + mate; x0 <= it.last; x0 += U * wpr) {
                 float2 ml[U];
                 float y[U][V];
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     const int x = x0 + u * wpr;
                     ml[u] = make_float2(-INFINITY, 0.f);
-                    if (x <= last) {
-                        const int64_t slot = 2 * (int64_t)x + (begin >= x * (int64_t)per ? 1 : 0);
-                        ml[u] = work.ml[slot * R + r];
-                        const float *from = work.o + (slot * R + r) * D + lane * V;
+                    if (x <= it.last) {
+                        const int64_t slot = (2 * (int64_t)x + (x == first ? 1 : 0)) * R + r;
+                        ml[u] = work.ml[slot];
+                        const float *from = work.o + slot * D + lane * V;
 #pragma unroll
                         for (int i = 0; i < V; i += 2) {
                             const float2 z = *reinterpret_cast<const float2 *>(from + i);
@@ -561,7 +564,7 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(const AttendA
                 for (int i = 0; i < V; ++i) o[i] *= old;
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
-                    if (x0 + u * wpr <= last) {
+                    if (x0 + u * wpr <= it.last) {
                         const float f = ex2(ml[u].x - mu);
                         L = fmaf(ml[u].y, f, L);
 #pragma unroll
@@ -576,7 +579,7 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(const AttendA
             for (int i = 0; i < V; ++i) part[warp][lane * V + i] = o[i];
             if (lane == 0) part[warp][D] = M, part[warp][D + 1] = L;
             __syncthreads();
-            if (joins && mate == 0) {
+            if (live && mate == 0) {
                 float Mn = -INFINITY;
                 for (int x = 0; x < wpr; ++x) Mn = fmaxf(Mn, part[warp + x][D]);
                 const float mu = Mn == -INFINITY ? 0.f : Mn;
@@ -591,31 +594,29 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(const AttendA
                 }
             }
         }
-        if (inside && mate == 0 && (empty || joins)) {
-            const float y = empty || L == 0.f ? 0.f : 1.f / L;
-            const int64_t to = (((int64_t)b * p.T + t) * p.H + h * G + (row - t * G)) * D + lane * V;
+        if (live && mate == 0) {
+            const float y = L == 0.f ? 0.f : 1.f / L;
+            const int64_t to = (((int64_t)it.b * p.T + t) * p.H + it.h * G + (row - t * G)) * D + lane * V;
 #pragma unroll
             for (int i = 0; i < V; i += 2) {
-                const float a = empty ? 0.f : o[i] * y, z = empty ? 0.f : o[i + 1] * y;
                 if (BF)
-                    *reinterpret_cast<__nv_bfloat162 *>(static_cast<__nv_bfloat16 *>(p.o) + to + i) = __floats2bfloat162_rn(a, z);
+                    *reinterpret_cast<__nv_bfloat162 *>(static_cast<__nv_bfloat16 *>(p.o) + to + i) = __floats2bfloat162_rn(o[i] * y, o[i + 1] * y);
                 else
-                    *reinterpret_cast<float2 *>(static_cast<float *>(p.o) + to + i) = make_float2(a, z);
+                    *reinterpret_cast<float2 *>(static_cast<float *>(p.o) + to + i) = make_float2(o[i] * y, o[i + 1] * y);
             }
         }
     }
 }
 
 template <int D, bool BF>
-cudaError_t launch_join(const AttendArgs &a, int R, int ranges, int unit, cudaStream_t s) {
-    const int G = a.H / a.Hk;
-    const int64_t items = (int64_t)a.batch * (((int64_t)a.T * G + R - 1) / R) * a.Hk;
-    const int rows = (int)std::min<int64_t>(R, (int64_t)a.T * G);
-    // a CTA per row, its warps sharing the row's parts, while there are few items; else a warp per row, 32
-    // rows per CTA at most
-    const bool few = items * rows <= 4 * sm_count();
+cudaError_t launch_join(const AttendArgs &a, int R, int ranges, cudaStream_t s) {
+    const int rows = (int)std::min<int64_t>(R, (int64_t)a.T * (a.H / a.Hk));
+    int wpr = kJoinThreads / 32;  // as many warps per row as a CTA has for its rows, one row each at least
+    while (wpr > 1 && wpr * rows > kJoinThreads / 32) wpr /= 2;
+    const int slice = (int)std::max<int64_t>(1, (256 << 10) / ((int64_t)a.H * a.d * (BF ? 2 : 4)));
+    const int64_t clear = (int64_t)a.batch * ((a.T + slice - 1) / slice);
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)items, few ? (unsigned)rows : (unsigned)((rows + 31) / 32));
+    cfg.gridDim = dim3((unsigned)(ranges + clear), (unsigned)((rows + 31) / 32));
     cfg.blockDim = dim3(kJoinThreads);
     cfg.stream = s;
     cudaLaunchAttribute attr[1];
@@ -623,7 +624,7 @@ cudaError_t launch_join(const AttendArgs &a, int R, int ranges, int unit, cudaSt
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, attend_join_kernel<D, BF>, a, R, ranges, unit, few ? kJoinThreads / 32 : 1);
+    return cudaLaunchKernelEx(&cfg, attend_join_kernel<D, BF>, a, R, ranges, rows, wpr, slice);
 }
 template <int D, int MT, bool F32>
 cudaError_t launch_as(const AttendArgs &a, cudaStream_t s) {
@@ -634,13 +635,13 @@ cudaError_t launch_as(const AttendArgs &a, cudaStream_t s) {
     const int grid = sm_count();
     attend_kernel<D, MT, F32><<<grid, C::threads, smem, s>>>(a);
     e = cudaGetLastError();
-    return e != cudaSuccess ? e : launch_join<D, !F32>(a, C::R, grid * C::warps, 1, s);
+    return e != cudaSuccess ? e : launch_join<D, !F32>(a, C::R, grid * C::warps, s);
 }
 template <int D>
 cudaError_t launch_d(const AttendArgs &a, cudaStream_t s) {
     if (attend_tc_takes(a)) {
         const cudaError_t e = launch_attend_tc(a, sm_count(), s);
-        return e != cudaSuccess ? e : launch_join<D, true>(a, attend_tc_rows(a), sm_count(), attend_tc_unit(a), s);
+        return e != cudaSuccess ? e : launch_join<D, true>(a, attend_tc_rows(a), sm_count(), s);
     }
     return a.in_bf16 ? launch_as<D, 1, false>(a, s) : launch_as<D, 1, true>(a, s);
 }
@@ -649,8 +650,7 @@ cudaError_t launch_d(const AttendArgs &a, cudaStream_t s) {
 
 int64_t attend_workspace(const AttendArgs &a) {
     const bool tc = attend_tc_takes(a);
-    const int64_t R = tc ? attend_tc_rows(a) : 16, ranges = (int64_t)sm_count() * (tc ? 1 : a.d == 256 ? 4 : 8);
-    return att_before_bytes(a.batch) + ranges * 2 * R * ((int64_t)a.d * 4 + 8);
+    return att_work_bytes(sm_count() * (tc ? 1 : a.d == 256 ? 4 : 8), tc ? attend_tc_rows(a) : 16, a.d);
 }
 
 cudaError_t launch_attend(AttendArgs a, cudaStream_t s) {

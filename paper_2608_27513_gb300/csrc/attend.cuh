@@ -67,19 +67,25 @@ __device__ __forceinline__ void store_out(void *o, int64_t at, const float (&x)[
     }
 }
 
-// Workspace: the units before each batch row (a KV head's), then the parts: o [range][2][R][D] and
-// (m, l) [range][2][R].  A range leaves part 1 of an item that starts in it, else part 0.
-struct AttWork {
-    int32_t *before;
-    float *o;
-    float2 *ml;
+// Workspace: for each range the item that starts in it and does not end in it, the parts' (m, l) [range][2][R]
+// and o [range][2][R][D].  A range leaves part 1 of an item that starts in it, else part 0.
+struct AttSplit {
+    int b, rt, h;
+    int last;  // the range that it ends in; -1: there is no such item
 };
-__host__ __device__ inline int64_t att_before_bytes(int batch) { return ((int64_t)(batch + 1) * 4 + 15) & ~15ll; }
-__host__ __device__ inline AttWork att_work(uint8_t *w, int batch, int ranges, int R, int D) {
+struct AttWork {
+    AttSplit *split;
+    float2 *ml;
+    float *o;
+};
+__host__ __device__ inline int64_t att_work_bytes(int ranges, int R, int D) {
+    return (int64_t)ranges * (16 + 2 * (int64_t)R * (8 + 4 * D));
+}
+__host__ __device__ inline AttWork att_work(uint8_t *w, int ranges, int R) {
     AttWork a;
-    a.before = reinterpret_cast<int32_t *>(w);
-    a.o = reinterpret_cast<float *>(w + att_before_bytes(batch));
-    a.ml = reinterpret_cast<float2 *>(a.o + (int64_t)ranges * 2 * R * D);
+    a.split = reinterpret_cast<AttSplit *>(w);
+    a.ml = reinterpret_cast<float2 *>(a.split + ranges);
+    a.o = reinterpret_cast<float *>(a.ml + (int64_t)ranges * 2 * R);
     return a;
 }
 __device__ __forceinline__ int att_per(int total, int ranges) { return max(1, (total + ranges - 1) / ranges); }
@@ -117,6 +123,5 @@ __device__ inline void att_count(const AttendArgs &p, int R, int G, int unit, in
 bool attend_tc_takes(const AttendArgs &a);
 int attend_tc_rows(const AttendArgs &a);  // of an item
 cudaError_t launch_attend_tc(AttendArgs a, int grid, cudaStream_t s);
-int attend_tc_unit(const AttendArgs &a);  // pages of a key tile
 
 }  // namespace damp

@@ -295,9 +295,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
     att_count(p, R, G, PG, before);  // (synchronizes)
     tc_fence_after();
     const uint32_t tmem = s_tmem;
-    const AttWork work = att_work(p.workspace, p.batch, gridDim.x, R, D);
-    if (blockIdx.x == 0)
-        for (int b = threadIdx.x; b <= p.batch; b += kAtThreads) work.before[b] = before[b];
+    const AttWork work = att_work(p.workspace, gridDim.x, R);
     const int total = before[p.batch] * p.Hk, per = att_per(total, gridDim.x);
     const int end = (int)min((int64_t)total, ((int64_t)blockIdx.x + 1) * per);
     const int begin = (int)min((int64_t)end, (int64_t)blockIdx.x * per);
@@ -307,6 +305,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
     const AtWait wait{&s_dead};
     auto together = [](bool ok) { return __all_sync(kFull, ok) != 0; };
     const uint32_t n_tiles = (uint32_t)(end - begin);  // of this range
+    AttSplit split{0, 0, 0, -1};  // (thread 0)
 
     if (begin < end && warp < M::sm_warps) {
         at_more_regs<kAtSoftRegs>();
@@ -522,6 +521,10 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
             }
             tc_fence_before();
         }
+        if (threadIdx.x == 0 && ok && it.begin >= begin && it.begin + it.tiles > end) {
+            split.b = it.b, split.rt = it.rt, split.h = it.h;
+            split.last = (it.begin + it.tiles - 1) / per;
+        }
     } else if (begin < end && warp < 12) {
         at_fewer_regs<kAtTurnRegs>();
         // ---- codes into operands ----
@@ -710,6 +713,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
             for (int i = 0; i < 1000; ++i) __nanosleep(1000);
         }
     }
+    if (threadIdx.x == 0) work.split[blockIdx.x] = split;
     __syncwarp();
     tc_fence_before();
     __syncthreads();
@@ -733,8 +737,6 @@ cudaError_t launch_tc(const AttendArgs &a, int grid, cudaStream_t s) {
 }  // namespace
 
 bool attend_tc_takes(const AttendArgs &a) { return a.in_bf16 && (int64_t)a.T * (a.H / a.Hk) > 16; }
-
-int attend_tc_unit(const AttendArgs &a) { return a.d == 256 ? 2 : 4; }
 
 int attend_tc_rows(const AttendArgs &a) { return a.d <= 128 && (int64_t)a.T * (a.H / a.Hk) > 128 ? 256 : 128; }
 

@@ -12,7 +12,7 @@
 // tokens at most.  A thread keeps the values of its chunks of 16 in registers between the maximum
 // and the codes, so each value is read once; codes are stored 16 bytes at a time.
 //
-// Read.  A thread turns 16 codes into 16 values.  Both are bound by the bytes.
+// Read.  A thread turns chunks of 16 codes into values.  Both are bound by the bytes.
 #include "cache.cuh"
 
 #include <algorithm>
@@ -85,6 +85,18 @@ __global__ void __launch_bounds__(kAppThreads) cache_append_kernel(const CacheAr
         if (start < 0 && fresh > 0 && tid == 0) atomicOr(p.status, kDevBadSlot);
         return;
     }
+    const int t0 = (int)(lo - page * kCachePage);  // in the page
+    const int n = (int)(hi - lo) * kChunks;
+    const void *const x = which ? p.v : p.k;
+    const int64_t stride = which ? p.v_stride : p.k_stride;
+    const int64_t from = ((int64_t)b * p.T + (lo - start)) * stride + (int64_t)h * D;
+
+    Sixteen<BF> val[kUnits];  // on their way while the page is looked up
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+        const int u = tid + i * TPI;
+        if (u < n) val[i].load(x, from + (u / kChunks) * stride + (u % kChunks) * 16);
+    }
     const int64_t slot = page < p.table ? cache_page(p.pages[(int64_t)b * p.table + page], p.num_pages) : -1;
     if (slot < 0) {
         if (tid == 0) atomicOr(p.status, kDevBadSlot);
@@ -93,19 +105,7 @@ __global__ void __launch_bounds__(kAppThreads) cache_append_kernel(const CacheAr
     uint8_t *const record = p.pool + (slot * p.Hk + h) * cache_record_bytes(D);
     uint8_t *const rows = record + which * cache_rows_bytes(D);
     float *const scale_at = reinterpret_cast<float *>(record + 2 * cache_rows_bytes(D)) + which;
-    const int t0 = (int)(lo - page * kCachePage);  // in the page
-    const int n = (int)(hi - lo) * kChunks;
     const float before = t0 ? *scale_at : 0.f;
-    const void *const x = which ? p.v : p.k;
-    const int64_t stride = which ? p.v_stride : p.k_stride;
-    const int64_t from = ((int64_t)b * p.T + (lo - start)) * stride + (int64_t)h * D;
-
-    Sixteen<BF> val[kUnits];
-#pragma unroll
-    for (int i = 0; i < kUnits; ++i) {
-        const int u = tid + i * TPI;
-        if (u < n) val[i].load(x, from + (u / kChunks) * stride + (u % kChunks) * 16);
-    }
     float top = 0.f;
     bool bad = false;
 #pragma unroll
@@ -162,50 +162,68 @@ __global__ void __launch_bounds__(kAppThreads) cache_append_kernel(const CacheAr
     }
 }
 
+// A thread reads 16 keys and 16 values of kReadTokens tokens, all on their way at once.
+constexpr int kReadTokens = 2;
 template <int D, bool BF>
 __global__ void __launch_bounds__(kReadThreads) cache_read_kernel(const CacheArgs p) {
     constexpr int kChunks = D / 16;
-    const int64_t u = (int64_t)blockIdx.x * kReadThreads + threadIdx.x;
-    const int which = blockIdx.y;
-    const int m = (int)(u % kChunks);
-    const int64_t uh = u / kChunks, ut = uh / p.Hk;
-    const int h = (int)(uh - ut * p.Hk);
-    const int64_t b = ut / p.T;
-    if (b >= p.batch) return;
-    const int64_t token = (p.start ? (int64_t)p.start[b] : 0) + (ut - b * p.T);
-    float x[16];
+    uint4 code[kReadTokens][2];
+    float2 scale[kReadTokens];
+    int64_t unit[kReadTokens];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = 0.f;
-    if (token >= 0 && token < cache_clamp(p.lengths[b], p.table)) {
-        const int64_t slot = cache_page(p.pages[b * p.table + token / kCachePage], p.num_pages);
-        if (slot < 0) {
-            if (m == 0) atomicOr(p.status, kDevBadSlot);
-        } else {
-            const uint8_t *const record = p.pool + (slot * p.Hk + h) * cache_record_bytes(D);
-            const uint4 c = *reinterpret_cast<const uint4 *>(record + which * cache_rows_bytes(D) + cache_chunk((int)(token % kCachePage), m, D));
-            const float s = reinterpret_cast<const float *>(record + 2 * cache_rows_bytes(D))[which];
-            const uint32_t w[4] = {c.x, c.y, c.z, c.w};
-#pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] = (u8_biased(w[i / 4], i % 4) - (8388608.f + 128.f)) * s;
+    for (int i = 0; i < kReadTokens; ++i) {
+        const int64_t u = ((int64_t)blockIdx.x * kReadTokens + i) * kReadThreads + threadIdx.x;
+        const int m = (int)(u % kChunks);
+        const int64_t uh = u / kChunks, ut = uh / p.Hk;
+        const int h = (int)(uh - ut * p.Hk);
+        const int64_t b = ut / p.T;
+        unit[i] = b < p.batch ? u : -1;
+        scale[i] = make_float2(0.f, 0.f);
+        code[i][0] = code[i][1] = make_uint4(0, 0, 0, 0);
+        if (b < p.batch) {
+            const int64_t token = (p.start ? (int64_t)p.start[b] : 0) + (ut - b * p.T);
+            if (token >= 0 && token < cache_clamp(p.lengths[b], p.table)) {
+                const int64_t slot = cache_page(p.pages[b * p.table + token / kCachePage], p.num_pages);
+                if (slot < 0) {
+                    if (m == 0) atomicOr(p.status, kDevBadSlot);
+                } else {
+                    const uint8_t *const record = p.pool + (slot * p.Hk + h) * cache_record_bytes(D);
+                    const uint8_t *const at = record + cache_chunk((int)(token % kCachePage), m, D);
+                    code[i][0] = __ldg(reinterpret_cast<const uint4 *>(at));
+                    code[i][1] = __ldg(reinterpret_cast<const uint4 *>(at + cache_rows_bytes(D)));
+                    scale[i] = __ldg(reinterpret_cast<const float2 *>(record + 2 * cache_rows_bytes(D)));
+                }
+            }
         }
     }
-    const int64_t to = u * 16;
-    void *const out = which ? p.v : p.k;
-    if (BF) {
-        uint4 w[2];
-        uint32_t *const y = reinterpret_cast<uint32_t *>(w);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const __nv_bfloat162 z = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-            memcpy(&y[i], &z, 4);
+    for (int i = 0; i < kReadTokens; ++i) {
+        if (unit[i] < 0) continue;
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            const uint4 c = code[i][which];
+            const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+            const float s = which ? scale[i].y : scale[i].x;
+            float x[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[e] = s > 0.f ? (u8_biased(w[e / 4], e % 4) - (8388608.f + 128.f)) * s : 0.f;
+            void *const out = which ? p.v : p.k;
+            if (BF) {
+                uint32_t y[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const __nv_bfloat162 z = __floats2bfloat162_rn(x[2 * e], x[2 * e + 1]);
+                    memcpy(&y[e], &z, 4);
+                }
+                uint4 *const g = reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(out) + unit[i] * 16);
+                g[0] = make_uint4(y[0], y[1], y[2], y[3]);
+                g[1] = make_uint4(y[4], y[5], y[6], y[7]);
+            } else {
+                float4 *const g = reinterpret_cast<float4 *>(static_cast<float *>(out) + unit[i] * 16);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) g[e] = make_float4(x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]);
+            }
         }
-        uint4 *const g = reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(out) + to);
-        g[0] = w[0];
-        g[1] = w[1];
-    } else {
-        float4 *const g = reinterpret_cast<float4 *>(static_cast<float *>(out) + to);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) g[i] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
     }
 }
 
@@ -221,7 +239,8 @@ void append_as(const CacheArgs &a, cudaStream_t s) {
 template <int D, bool BF>
 void read_as(const CacheArgs &a, cudaStream_t s) {
     const int64_t units = (int64_t)a.batch * a.T * a.Hk * (D / 16);
-    cache_read_kernel<D, BF><<<dim3((unsigned)((units + kReadThreads - 1) / kReadThreads), 2), kReadThreads, 0, s>>>(a);
+    const int64_t per = kReadTokens * kReadThreads;
+    cache_read_kernel<D, BF><<<(unsigned)((units + per - 1) / per), kReadThreads, 0, s>>>(a);
 }
 #define DAMP_BY_D(f, a, s)                                                                      \
     do {                                                                                        \
