@@ -72,6 +72,8 @@ __device__ __forceinline__ void store_out(void *o, int64_t at, const float (&x)[
 struct AttSplit {
     int b, rt, h;
     int last;  // the range that it ends in; -1: there is no such item
+    int rows;  // of queries
+    int unused[3];
 };
 struct AttWork {
     AttSplit *split;
@@ -79,7 +81,7 @@ struct AttWork {
     float *o;
 };
 __host__ __device__ inline int64_t att_work_bytes(int ranges, int R, int D) {
-    return (int64_t)ranges * (16 + 2 * (int64_t)R * (8 + 4 * D));
+    return (int64_t)ranges * (32 + 2 * (int64_t)R * (8 + 4 * D));
 }
 __host__ __device__ inline AttWork att_work(uint8_t *w, int ranges, int R) {
     AttWork a;

@@ -262,6 +262,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int G = p.H / p.Hk;
     auto bar = [&](int i) { return sb + M::bar + 8 * i; };
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // the join waits for the end of this grid itself
     if (threadIdx.x == 0) {
         s_dead = 0;
         for (int i = 0; i < 2; ++i) {
@@ -305,7 +306,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
     const AtWait wait{&s_dead};
     auto together = [](bool ok) { return __all_sync(kFull, ok) != 0; };
     const uint32_t n_tiles = (uint32_t)(end - begin);  // of this range
-    AttSplit split{0, 0, 0, -1};  // (thread 0)
+    AttSplit split{0, 0, 0, -1, 0, {0, 0, 0}};  // (thread 0)
 
     if (begin < end && warp < M::sm_warps) {
         at_more_regs<kAtSoftRegs>();
@@ -524,6 +525,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
         if (threadIdx.x == 0 && ok && it.begin >= begin && it.begin + it.tiles > end) {
             split.b = it.b, split.rt = it.rt, split.h = it.h;
             split.last = (it.begin + it.tiles - 1) / per;
+            split.rows = min(R, it.row.n * G - it.rt * R);
         }
     } else if (begin < end && warp < 12) {
         at_fewer_regs<kAtTurnRegs>();
@@ -721,7 +723,6 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
     if (threadIdx.x == 0 && s_dead) atomicOr(p.status, kDevWaitTimeout);
     if (warp == 12)
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kAtCols) : "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
 template <int D, int SUB>

@@ -43,11 +43,9 @@ struct Sixteen {
     }
 };
 
-__device__ __forceinline__ float finite_abs(float x, bool &bad) {
+__device__ __forceinline__ float finite_abs(float x) {
     const float a = fabsf(x);
-    if (a <= FLT_MAX) return a;
-    bad = true;  // NaN or infinity
-    return 0.f;
+    return a <= FLT_MAX ? a : 0.f;
 }
 // rne(x) + 128 in the low byte, |x| <= 127
 __device__ __forceinline__ uint32_t code_of(float x) { return __float_as_uint(__fadd_rn(x, 12582912.f + 128.f)); }
@@ -106,19 +104,33 @@ __global__ void __launch_bounds__(kAppThreads) cache_append_kernel(const CacheAr
     uint8_t *const rows = record + which * cache_rows_bytes(D);
     float *const scale_at = reinterpret_cast<float *>(record + 2 * cache_rows_bytes(D)) + which;
     const float before = t0 ? *scale_at : 0.f;
-    float top = 0.f;
-    bool bad = false;
+    // magnitudes as integers, which order them and show what is not finite
+    uint32_t most = 0;
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {
         if (tid + i * TPI < n) {
+            const uint32_t *const w = reinterpret_cast<const uint32_t *>(val[i].w);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float2 y = val[i].pair(e);
-                top = fmaxf(top, fmaxf(finite_abs(y.x, bad), finite_abs(y.y, bad)));
+            for (int e = 0; e < (BF ? 8 : 16); ++e) most = BF ? __vmaxu2(most, w[e] & 0x7fff7fffu) : max(most, w[e] & 0x7fffffffu);
+        }
+    }
+    if (BF) most = max(most & 0xffff0000u, most << 16);
+    float top = __uint_as_float(most);
+    const bool bad = most >= 0x7f800000u;
+    if (bad) {
+        atomicOr(p.status, kDevNotFinite);
+        top = 0.f;
+#pragma unroll
+        for (int i = 0; i < kUnits; ++i) {
+            if (tid + i * TPI < n) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float2 y = val[i].pair(e);
+                    top = fmaxf(top, fmaxf(finite_abs(y.x), finite_abs(y.y)));
+                }
             }
         }
     }
-    if (bad) atomicOr(p.status, kDevNotFinite);
     top = __uint_as_float(__reduce_max_sync(kFull, __float_as_uint(top)));  // not negative: ordered as integers
     if (TPI == 128) {
         if (lane == 0) part[threadIdx.x >> 5] = top;
@@ -155,31 +167,35 @@ __global__ void __launch_bounds__(kAppThreads) cache_append_kernel(const CacheAr
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const float2 y = val[i].pair(2 * e), z = val[i].pair(2 * e + 1);
-                w[e] = code4(scaled(y.x, r), scaled(y.y, r), scaled(z.x, r), scaled(z.y, r));
+                // |x| <= 127 s, s and r rounded once each: x r rounds to 127 at most where all is finite
+                w[e] = bad ? code4(scaled(y.x, r), scaled(y.y, r), scaled(z.x, r), scaled(z.y, r))
+                           : code4(__fmul_rn(y.x, r), __fmul_rn(y.y, r), __fmul_rn(z.x, r), __fmul_rn(z.y, r));
             }
             *reinterpret_cast<uint4 *>(rows + cache_chunk(t0 + u / kChunks, u % kChunks, D)) = make_uint4(w[0], w[1], w[2], w[3]);
         }
     }
 }
 
-// A thread reads 16 keys and 16 values of kReadTokens tokens, all on their way at once.
+// A thread turns N keys and N values, 16 bytes each once they are turned (so that a warp's stores are whole
+// lines), of kReadTokens tokens, all on their way at once.
 constexpr int kReadTokens = 2;
 template <int D, bool BF>
 __global__ void __launch_bounds__(kReadThreads) cache_read_kernel(const CacheArgs p) {
-    constexpr int kChunks = D / 16;
-    uint4 code[kReadTokens][2];
+    constexpr int N = BF ? 8 : 4, kParts = D / N;
+    uint32_t code[kReadTokens][2][N / 4];
     float2 scale[kReadTokens];
     int64_t unit[kReadTokens];
 #pragma unroll
     for (int i = 0; i < kReadTokens; ++i) {
         const int64_t u = ((int64_t)blockIdx.x * kReadTokens + i) * kReadThreads + threadIdx.x;
-        const int m = (int)(u % kChunks);
-        const int64_t uh = u / kChunks, ut = uh / p.Hk;
+        const int m = (int)(u % kParts);
+        const int64_t uh = u / kParts, ut = uh / p.Hk;
         const int h = (int)(uh - ut * p.Hk);
         const int64_t b = ut / p.T;
         unit[i] = b < p.batch ? u : -1;
         scale[i] = make_float2(0.f, 0.f);
-        code[i][0] = code[i][1] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int k = 0; k < N / 4; ++k) code[i][0][k] = code[i][1][k] = 0x80808080u;  // zeros
         if (b < p.batch) {
             const int64_t token = (p.start ? (int64_t)p.start[b] : 0) + (ut - b * p.T);
             if (token >= 0 && token < cache_clamp(p.lengths[b], p.table)) {
@@ -188,9 +204,17 @@ __global__ void __launch_bounds__(kReadThreads) cache_read_kernel(const CacheArg
                     if (m == 0) atomicOr(p.status, kDevBadSlot);
                 } else {
                     const uint8_t *const record = p.pool + (slot * p.Hk + h) * cache_record_bytes(D);
-                    const uint8_t *const at = record + cache_chunk((int)(token % kCachePage), m, D);
-                    code[i][0] = __ldg(reinterpret_cast<const uint4 *>(at));
-                    code[i][1] = __ldg(reinterpret_cast<const uint4 *>(at + cache_rows_bytes(D)));
+                    const uint8_t *const at = record + cache_chunk((int)(token % kCachePage), m * N / 16, D) + m * N % 16;
+#pragma unroll
+                    for (int which = 0; which < 2; ++which) {
+                        const uint8_t *const from = at + which * cache_rows_bytes(D);
+                        if constexpr (N == 8) {
+                            const uint2 w = __ldg(reinterpret_cast<const uint2 *>(from));
+                            code[i][which][0] = w.x, code[i][which][N / 4 - 1] = w.y;
+                        } else {
+                            code[i][which][0] = __ldg(reinterpret_cast<const uint32_t *>(from));
+                        }
+                    }
                     scale[i] = __ldg(reinterpret_cast<const float2 *>(record + 2 * cache_rows_bytes(D)));
                 }
             }
@@ -201,28 +225,21 @@ __global__ void __launch_bounds__(kReadThreads) cache_read_kernel(const CacheArg
         if (unit[i] < 0) continue;
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
-            const uint4 c = code[i][which];
-            const uint32_t w[4] = {c.x, c.y, c.z, c.w};
             const float s = which ? scale[i].y : scale[i].x;
-            float x[16];
+            float x[N];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) x[e] = s > 0.f ? (u8_biased(w[e / 4], e % 4) - (8388608.f + 128.f)) * s : 0.f;
-            void *const out = which ? p.v : p.k;
-            if (BF) {
-                uint32_t y[8];
+            for (int e = 0; e < N; ++e) x[e] = (u8_biased(code[i][which][e / 4], e % 4) - (8388608.f + 128.f)) * s;
+            uint32_t y[4];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const __nv_bfloat162 z = __floats2bfloat162_rn(x[2 * e], x[2 * e + 1]);
+            for (int e = 0; e < 4; ++e) {
+                if (BF) {
+                    const __nv_bfloat162 z = __floats2bfloat162_rn(x[2 * e % N], x[(2 * e + 1) % N]);
                     memcpy(&y[e], &z, 4);
+                } else {
+                    y[e] = __float_as_uint(x[e]);
                 }
-                uint4 *const g = reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(out) + unit[i] * 16);
-                g[0] = make_uint4(y[0], y[1], y[2], y[3]);
-                g[1] = make_uint4(y[4], y[5], y[6], y[7]);
-            } else {
-                float4 *const g = reinterpret_cast<float4 *>(static_cast<float *>(out) + unit[i] * 16);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) g[e] = make_float4(x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]);
             }
+            stg128(static_cast<uint4 *>(which ? p.v : p.k) + unit[i], make_uint4(y[0], y[1], y[2], y[3]));
         }
     }
 }
@@ -238,7 +255,7 @@ void append_as(const CacheArgs &a, cudaStream_t s) {
 }
 template <int D, bool BF>
 void read_as(const CacheArgs &a, cudaStream_t s) {
-    const int64_t units = (int64_t)a.batch * a.T * a.Hk * (D / 16);
+    const int64_t units = (int64_t)a.batch * a.T * a.Hk * (D / (BF ? 8 : 4));
     const int64_t per = kReadTokens * kReadThreads;
     cache_read_kernel<D, BF><<<(unsigned)((units + per - 1) / per), kReadThreads, 0, s>>>(a);
 }
