@@ -53,9 +53,9 @@ struct AtSmem {
     static constexpr int tokens = D == 256 ? 64 : 128;  // of a key tile
     static constexpr int pages = tokens / kCachePage;
     static constexpr int q_tile = 128 * D * 2, tile = tokens * D * 2;
-    static constexpr int buffers = D == 256 ? 1 : 2;  // of K and of V
+    static constexpr int buffers = 2;                 // of K and of V
     static constexpr int codes = tokens * D;          // of K or of V
-    static constexpr int stages = D == 64 ? 4 : D == 256 ? 3 : SUB == 1 ? 2 : 1;  // of codes
+    static constexpr int stages = D == 64 ? 4 : D == 128 && SUB == 1 ? 2 : 1;  // of codes
     static constexpr int q = 0, k = SUB * q_tile, v = k + buffers * tile;
     static constexpr int kc = v + buffers * tile, vc = kc + stages * codes;
     static constexpr int note = vc + stages * codes;
@@ -63,7 +63,7 @@ struct AtSmem {
     static constexpr int bytes = bar + 384;
     static constexpr int before = k;  // until the roles begin
     static_assert(SUB * q_tile + 4 * (kCacheMaxBatch + 1) <= kc, "before");
-    static constexpr int sm_warps = 4 * SUB, turn_warps = 12 - sm_warps;
+    static constexpr int sm_warps = 4 * SUB, turn_warps = 4;  // SUB = 1: four for K, four for V
 };
 // mbarriers
 enum { kBarQ = 0, kBarDone = 2, kBarKFull = 4, kBarKFree = 6, kBarVFull = 8, kBarVFree = 10, kBarS = 12, kBarP = 14, kBarPV = 18, kBarTurn = 19, kBarNote = 21,  // P: halves of two buffers
@@ -321,56 +321,56 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
         const uint32_t stage_row = sb + M::q + x * M::q_tile + (row >> 3) * (16 * D) + (row & 7) * 16;
         uint32_t tile = 0, items = 0;
         bool ok = true;
+        constexpr int kC = D / 32;  // chunks of a lane in 8 rows
         for (int at = begin; at < end && ok; ++items) {
             if (items) at_next(it, p, R, G, PG);
             const int last = min(end, it.begin + it.tiles);
             const int r = it.rt * R + x * 128 + row, t = r / G;
             const bool live = t < it.row.n;
-            const int limit = live ? it.row.len - it.row.n + t : kNoRow;
+            const int limit = live ? it.row.len - it.row.n + t : INT_MAX / 2;  // (what rows of no query hold is not used)
             const int from = p.window && live ? limit - (p.window - 1) : 0;
             const int head = it.h * G + (r - t * G);
             float factor = 0.f;
-            {  // q, scaled by a power of two to below 2^15
+            {  // q, scaled by a power of two to below 2^15: 8 rows at a time, the next 8 on their way
                 const int64_t mine = live ? ((int64_t)it.b * p.T + t) * p.q_stride + (int64_t)head * D : -1;
-                constexpr int kC = D / 32;  // chunks of a lane in 8 rows
+                uint4 w[kC];
+                auto load = [&](int g) {
+                    const int64_t src = __shfl_sync(kFull, mine, 8 * g + (lane & 7));
+                    const uint4 *const q = reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(p.q) + src) + (lane >> 3);
 #pragma unroll
-                for (int g0 = 0; g0 < 4; g0 += 2) {
-                    uint4 w[2][kC];
+                    for (int i = 0; i < kC; ++i) w[i] = src >= 0 ? q[4 * i] : make_uint4(0, 0, 0, 0);
+                };
+                load(0);
+#pragma unroll 1
+                for (int g = 0; g < 4; ++g) {
+                    uint4 v[kC];
 #pragma unroll
-                    for (int g = 0; g < 2; ++g) {
-                        const int64_t src = __shfl_sync(kFull, mine, 8 * (g0 + g) + (lane & 7));
-                        const uint4 *const q = reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(p.q) + src) + (lane >> 3);
+                    for (int i = 0; i < kC; ++i) v[i] = w[i];
+                    if (g < 3) load(g + 1);
+                    uint32_t top = 0;  // largest magnitudes of both halves of the words
 #pragma unroll
-                        for (int i = 0; i < kC; ++i) w[g][i] = src >= 0 ? q[4 * i] : make_uint4(0, 0, 0, 0);
-                    }
+                    for (int i = 0; i < kC; ++i)
+                        top = __vmaxu2(__vmaxu2(__vmaxu2(top, v[i].x & 0x7fff7fffu), __vmaxu2(v[i].y & 0x7fff7fffu, v[i].z & 0x7fff7fffu)), v[i].w & 0x7fff7fffu);
+                    top = __vmaxu2(top, __shfl_xor_sync(kFull, top, 8));
+                    top = __vmaxu2(top, __shfl_xor_sync(kFull, top, 16));
+                    const int e = min(max((int)(max(top >> 16, top & 0xffffu) >> 7), 15), 254);
+                    const float up = __uint_as_float((uint32_t)(268 - e) << 23);
+                    if ((lane >> 3) == g) factor = p.scale * kLog2e / up;  // of this thread's own row
 #pragma unroll
-                    for (int g = 0; g < 2; ++g) {
-                        uint32_t top = 0;  // largest magnitudes of both halves of the words
+                    for (int i = 0; i < kC; ++i) {
+                        const uint32_t u[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+                        uint32_t h[4];
 #pragma unroll
-                        for (int i = 0; i < kC; ++i)
-                            top = __vmaxu2(__vmaxu2(__vmaxu2(top, w[g][i].x & 0x7fff7fffu), __vmaxu2(w[g][i].y & 0x7fff7fffu, w[g][i].z & 0x7fff7fffu)),
-                                           w[g][i].w & 0x7fff7fffu);
-                        top = __vmaxu2(top, __shfl_xor_sync(kFull, top, 8));
-                        top = __vmaxu2(top, __shfl_xor_sync(kFull, top, 16));
-                        const int e = min(max((int)(max(top >> 16, top & 0xffffu) >> 7), 15), 254);
-                        const float up = __uint_as_float((uint32_t)(268 - e) << 23);
-                        if ((lane >> 3) == g0 + g) factor = p.scale * kLog2e / up;  // of this thread's own row
-#pragma unroll
-                        for (int i = 0; i < kC; ++i) {
-                            const uint32_t u[4] = {w[g][i].x, w[g][i].y, w[g][i].z, w[g][i].w};
-                            uint32_t h[4];
-#pragma unroll
-                            for (int k = 0; k < 4; ++k)
-                                h[k] = at_half2(__uint_as_float(u[k] << 16) * up, __uint_as_float(u[k] & 0xffff0000u) * up);
-                            sts128(stage + (g0 + g) * (16 * D) + i * 512, make_uint4(h[0], h[1], h[2], h[3]));
-                        }
+                        for (int k = 0; k < 4; ++k)
+                            h[k] = at_half2(__uint_as_float(u[k] << 16) * up, __uint_as_float(u[k] & 0xffff0000u) * up);
+                        sts128(stage + g * (16 * D) + i * 512, make_uint4(h[0], h[1], h[2], h[3]));
                     }
                 }
-                fence_proxy_async_smem();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) at_arrive(bar(kBarQ + x));
             }
+            fence_proxy_async_smem();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) at_arrive(bar(kBarQ + x));
             float ref = -INFINITY, sum = 0.f;
             int ve = 0;
             const int first_tile = at - it.begin;
@@ -382,25 +382,33 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
                 const int i = at - it.begin;
                 const int token = (it.first + i * PG) * kCachePage;  // of column 0
                 const int hidden = note->hidden, e = note->e;
-                const bool masked = __any_sync(kFull, hidden != 0 || (limit != kNoRow && (limit < token + TN - 1 || from > token)));
                 ok = together(ok && wait(bar(kBarS + sbuf), (SUB == 2 ? tile : tile >> 1) & 1));
                 if (!ok) break;
                 tc_fence_after();
+                if (__any_sync(kFull, hidden != 0 || limit < token + TN - 1 || from > token)) {
+                    // columns that a row does not see become -inf where they are, 16 at a time (of the border tiles of an
+                    // item only: a small loop, for the instruction caches' sake, which all roles share)
+#pragma unroll 1
+                    for (int c = 0; c < 2 * PG; ++c) {
+                        const int lo = from - (token + 16 * c), hi = limit - (token + 16 * c);  // sees lo .. hi
+                        const bool all = (hidden >> (c >> 1)) & 1;
+                        if (!all && !__any_sync(kFull, lo > 0 || hi < 15)) continue;
+                        const uint32_t seen = hi < 0 || lo > 15 || all ? 0u : (0xffffu >> (15 - min(hi, 15))) & (0xffffu << max(lo, 0));
+                        uint32_t y[16];
+                        at_ld16(s_at + 16 * c, y);
+                        at_ld_wait(y);
+#pragma unroll
+                        for (int j = 0; j < 16; ++j)
+                            if (!(seen & (1u << j))) y[j] = 0xff800000u;
+                        at_st16(s_at + 16 * c, y);
+                    }
+                    at_st_wait();
+                }
                 uint32_t s[2 * PG][16];
 #pragma unroll
                 for (int c = 0; c < 2 * PG; ++c) at_ld16(s_at + 16 * c, s[c]);
 #pragma unroll
                 for (int c = 0; c < 2 * PG; ++c) at_ld_wait(s[c]);
-                if (masked) {
-                    const int lo = from - token, hi = limit - token;
-#pragma unroll
-                    for (int c = 0; c < 2 * PG; ++c) {
-                        const bool all = (hidden >> (c >> 1)) & 1;
-#pragma unroll
-                        for (int j = 0; j < 16; ++j)
-                            if (16 * c + j > hi || 16 * c + j < lo || all) s[c][j] = 0xff800000u;
-                    }
-                }
                 float top = -INFINITY;
 #pragma unroll
                 for (int c = 0; c < PG; ++c) {
@@ -465,35 +473,36 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
                 }
             }
             if (!ok) break;
+            const bool whole = it.begin >= begin && it.begin + it.tiles <= end, starts = it.begin >= begin;
+            const int64_t mine = live ? (((int64_t)it.b * p.T + t) * p.H + head) * D : -1;
+            if (threadIdx.x == 0 && starts && !whole)
+                split = AttSplit{it.b, it.rt, it.h, (it.begin + it.tiles - 1) / per, min(R, it.row.n * G - it.rt * R), {0, 0, 0}};
             ok = together(wait(bar(kBarDone + x), items & 1));  // the item's products into O
             if (!ok) break;
             tc_fence_after();
-            const bool whole = it.begin >= begin && it.begin + it.tiles <= end;
             const float unit = __uint_as_float((uint32_t)ve << 23) * (1.f / 1024.f);
             if (whole) {
                 const float y = sum == 0.f ? 0.f : unit / sum;
 #pragma unroll 1
                 for (int c = 0; c < D / 32; ++c) {
-                    uint32_t both[2][16];
-                    at_ld16(o_at + 32 * c, both[0]);
-                    at_ld16(o_at + 32 * c + 16, both[1]);
-                    at_ld_wait(both[0]);
-                    at_ld_wait(both[1]);
+                    uint32_t o[2][16];
+                    at_ld16(o_at + 32 * c, o[0]);
+                    at_ld16(o_at + 32 * c + 16, o[1]);
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
-                        const uint32_t *const s = &both[k >> 1][8 * (k & 1)];
+                        if ((k & 1) == 0) at_ld_wait(o[k >> 1]);
                         uint32_t h[4];
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
-                            const __nv_bfloat162 z = __floats2bfloat162_rn(__uint_as_float(s[2 * j]) * y, __uint_as_float(s[2 * j + 1]) * y);
+                            const __nv_bfloat162 z = __floats2bfloat162_rn(__uint_as_float(o[k >> 1][8 * (k & 1) + 2 * j]) * y,
+                                                                           __uint_as_float(o[k >> 1][8 * (k & 1) + 2 * j + 1]) * y);
                             memcpy(&h[j], &z, 4);
                         }
                         sts128(stage_row + (4 * c + k) * 128, make_uint4(h[0], h[1], h[2], h[3]));
                     }
                 }
                 __syncwarp();
-                const int64_t mine = live ? (((int64_t)it.b * p.T + t) * p.H + head) * D : -1;
-#pragma unroll
+#pragma unroll 1
                 for (int g = 0; g < 4; ++g) {
                     const int64_t dst = __shfl_sync(kFull, mine, 8 * g + (lane & 7));
                     __nv_bfloat16 *const o = static_cast<__nv_bfloat16 *>(p.o) + dst + 8 * (lane >> 3);
@@ -505,34 +514,32 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
                 }
                 __syncwarp();
             } else {
-                const int64_t slot = (int64_t)(2 * blockIdx.x + (it.begin >= begin ? 1 : 0)) * R + x * 128 + row;
+                const int64_t slot = (int64_t)(2 * blockIdx.x + (starts ? 1 : 0)) * R + x * 128 + row;
                 if (live) work.ml[slot] = make_float2(ref, sum);
 #pragma unroll 1
-                for (int c = 0; c < D / 16; ++c) {
-                    uint32_t s[16];
-                    at_ld16(o_at + 16 * c, s);
-                    at_ld_wait(s);
-                    if (live) {
+                for (int c = 0; c < D / 32; ++c) {
+                    uint32_t o[2][16];
+                    at_ld16(o_at + 32 * c, o[0]);
+                    at_ld16(o_at + 32 * c + 16, o[1]);
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        at_ld_wait(o[k]);
                         float z[16];
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) z[j] = __uint_as_float(s[j]) * unit;
-                        store_out<false, 16>(work.o + slot * D, 16 * c, z);
+                        for (int j = 0; j < 16; ++j) z[j] = __uint_as_float(o[k][j]) * unit;
+                        if (live) store_out<false, 16>(work.o + slot * D, 32 * c + 16 * k, z);
                     }
                 }
             }
             tc_fence_before();
         }
-        if (threadIdx.x == 0 && ok && it.begin >= begin && it.begin + it.tiles > end) {
-            split.b = it.b, split.rt = it.rt, split.h = it.h;
-            split.last = (it.begin + it.tiles - 1) / per;
-            split.rows = min(R, it.row.n * G - it.rt * R);
-        }
     } else if (begin < end && warp < 12) {
         at_fewer_regs<kAtTurnRegs>();
-        // ---- codes into operands ----
+        // ---- codes into operands: by four warps, with one block of rows by four for K and four for V ----
         constexpr int kQuads = D / 64;                             // 4 chunks of 16 codes
         constexpr int kUnits = (TN / 8) * kQuads / M::turn_warps;  // of 8 tokens x 4 chunks, of a warp
-        const int w = warp - M::sm_warps;
+        const int w = (warp - M::sm_warps) & 3;
+        const bool keys = SUB == 2 || warp < 8, values = SUB == 2 || warp >= 8;
         const int tok = lane & 7, mi = lane >> 3;
         auto turn = [&](uint32_t from, uint32_t free, uint32_t to, uint32_t to_free, bool wait_free, uint32_t parity, uint32_t full) {
             uint4 c[kUnits];
@@ -557,15 +564,15 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
             return true;
         };
         for (uint32_t i = 0; i < n_tiles; ++i) {
-            const uint32_t buf = M::buffers == 2 ? i & 1 : 0, use = M::buffers == 2 ? i >> 1 : i;
+            const uint32_t buf = i & 1, use = i >> 1;
             const uint32_t st = i % M::stages, lap = i / M::stages;
-            if (!together(wait(bar(kBarKcFull + st), lap & 1))) break;
-            if (!turn(sb + M::kc + st * M::codes, bar(kBarKcFree + st), sb + M::k + buf * M::tile, bar(kBarKFree + buf), use != 0, (use - 1) & 1,
-                      bar(kBarKFull + buf)))
+            if (keys && !(together(wait(bar(kBarKcFull + st), lap & 1)) &&
+                          turn(sb + M::kc + st * M::codes, bar(kBarKcFree + st), sb + M::k + buf * M::tile, bar(kBarKFree + buf), use != 0,
+                               (use - 1) & 1, bar(kBarKFull + buf))))
                 break;
-            if (!together(wait(bar(kBarVcFull + st), lap & 1))) break;
-            if (!turn(sb + M::vc + st * M::codes, bar(kBarVcFree + st), sb + M::v + buf * M::tile, bar(kBarVFree + buf), use != 0, (use - 1) & 1,
-                      bar(kBarVFull + buf)))
+            if (values && !(together(wait(bar(kBarVcFull + st), lap & 1)) &&
+                            turn(sb + M::vc + st * M::codes, bar(kBarVcFree + st), sb + M::v + buf * M::tile, bar(kBarVFree + buf), use != 0,
+                                 (use - 1) & 1, bar(kBarVFull + buf))))
                 break;
         }
     } else if (begin < end) {
@@ -648,8 +655,8 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
         // Q K^T at a time, so that one block's softmax runs under the other's products ----
         constexpr uint32_t kIdS = at_idesc(TN, false), kIdO = at_idesc(D, true);
         const int x = warp - 12;
-        auto key_buf = [&](uint32_t t) { return M::buffers == 2 ? t & 1u : 0u; };
-        auto key_use = [&](uint32_t t) { return (M::buffers == 2 ? t >> 1 : t) & 1u; };
+        auto key_buf = [&](uint32_t t) { return t & 1u; };
+        auto key_use = [&](uint32_t t) { return (t >> 1) & 1u; };
         const uint64_t dq = tc_desc(sb + M::q + x * M::q_tile, 128, 16 * D), dk = tc_desc(sb + M::k, 128, 16 * D), dv = tc_desc(sb + M::v, 16 * D, 128);
         const uint32_t q_lo = at_uniform((uint32_t)dq), k_lo = at_uniform((uint32_t)dk), v_lo = at_uniform((uint32_t)dv);
         const uint32_t k_hi = at_uniform((uint32_t)(dk >> 32)), v_hi = at_uniform((uint32_t)(dv >> 32)), tm = at_uniform(tmem);
@@ -715,7 +722,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
             for (int i = 0; i < 1000; ++i) __nanosleep(1000);
         }
     }
-    if (threadIdx.x == 0) work.split[blockIdx.x] = split;
+    if (threadIdx.x == 0) work.split[blockIdx.x] = split;  // (a range starts one such item at most, its last)
     __syncwarp();
     tc_fence_before();
     __syncthreads();
