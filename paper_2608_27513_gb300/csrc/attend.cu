@@ -118,7 +118,7 @@ __global__ void __launch_bounds__(AttCfg<D, MT, F32>::threads, 1) attend_kernel(
     extern __shared__ __align__(128) uint8_t sm[];
     int32_t *const before = reinterpret_cast<int32_t *>(sm + C::warps * C::warp_bytes);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
-    const int G = p.H / p.Hk;
+    const int G = p.group;
     uint8_t *const mine = sm + warp * C::warp_bytes;
     uint8_t *const about = mine + C::ring + C::qbytes;  // [stages] AttPage, then the barriers
     const uint32_t ring = smem_u32(mine), qs = ring + C::ring, bars = smem_u32(about) + C::stages * 32;
@@ -127,7 +127,7 @@ __global__ void __launch_bounds__(AttCfg<D, MT, F32>::threads, 1) attend_kernel(
         for (int i = 0; i < C::stages; ++i) mbar_init(bars + 8 * i, 1);
         fence_mbar_init();
     }
-    att_count(p, R, G, 1, before);
+    att_count(p, R, 1, before);
     const int warps = gridDim.x * C::warps;
     const AttWork work = att_work(p.workspace, warps, R);
     const int total = before[p.batch] * p.Hk, per = att_per(total, warps);
@@ -155,10 +155,10 @@ __global__ void __launch_bounds__(AttCfg<D, MT, F32>::threads, 1) attend_kernel(
                 const AttRow w = att_row(p, lo);
                 int rt = 0, tile = before[lo] * p.Hk;
                 if (my_record && lo == my.b) rt = my.rt, tile = my_tile;  // pages come in order
-                AttItem it = att_item(p, w, rt, R, G);
+                AttItem it = att_item(p, w, rt, R);
                 while (x - tile >= it.pages * p.Hk) {
                     tile += it.pages * p.Hk;
-                    it = att_item(p, w, ++rt, R, G);
+                    it = att_item(p, w, ++rt, R);
                 }
                 my_tile = tile;
                 const int at = x - tile;
@@ -213,7 +213,7 @@ __global__ void __launch_bounds__(AttCfg<D, MT, F32>::threads, 1) attend_kernel(
 #pragma unroll
             for (int hh = 0; hh < 2; ++hh) {
                 const int r = mt * 16 + hh * 8 + g;  // in the item
-                const int row = now.rt * R + r, t = row / G;
+                const int row = now.rt * R + r, t = att_div(p, row);
                 const float sum = quad_sum(l[mt][hh]);
                 const bool live = limit[mt][hh] != kNoRow;
                 const float y = whole ? (sum == 0.f ? 0.f : unit / sum) : unit;
@@ -247,7 +247,7 @@ __global__ void __launch_bounds__(AttCfg<D, MT, F32>::threads, 1) attend_kernel(
             float up[2];
 #pragma unroll
             for (int hh = 0; hh < 2; ++hh) {
-                const int row = now.rt * R + mt * 16 + hh * 8 + g, t = row / G;
+                const int row = now.rt * R + mt * 16 + hh * 8 + g, t = att_div(p, row);
                 live[hh] = t < w.n;
                 limit[mt][hh] = live[hh] ? w.len - w.n + t : kNoRow;
                 from[hh] = ((int64_t)now.b * p.T + t) * p.q_stride + (int64_t)(now.h * G + (row - t * G)) * D;
@@ -587,7 +587,7 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join_rows_kernel(const At
             if (x0 + u <= it.last) o.x = fmaf(y[u].x, f, o.x), o.y = fmaf(y[u].y, f, o.y), o.z = fmaf(y[u].z, f, o.z), o.w = fmaf(y[u].w, f, o.w);
         }
     }
-    const int G = p.H / p.Hk, row = it.rt * R + r, t = row / G;
+    const int G = p.group, row = it.rt * R + r, t = att_div(p, row);
     const float y = L == 0.f ? 0.f : 1.f / L;
     uint2 w;
     const __nv_bfloat162 a = __floats2bfloat162_rn(o.x * y, o.y * y), b = __floats2bfloat162_rn(o.z * y, o.w * y);
@@ -602,7 +602,7 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(const AttendA
     constexpr int R = 16;
     constexpr int V = D / 32;  // columns of a lane
     __shared__ float part[kJoinThreads / 32][D + 2];
-    const int G = p.H / p.Hk;
+    const int G = p.group;
     if ((int)blockIdx.x >= ranges) {
         if (blockIdx.y == 0) att_clear<D, BF>(p, blockIdx.x - ranges, slice);
         return;
@@ -617,7 +617,7 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(const AttendA
     const int team = warp / wpr, mate = warp % wpr, teams = kJoinThreads / 32 / wpr;
     for (int r0 = blockIdx.y * teams; r0 < rows; r0 += gridDim.y * teams) {
         const int r = r0 + team;
-        const int row = it.rt * R + r, t = row / G;
+        const int row = it.rt * R + r, t = att_div(p, row);
         const bool live = r < rows;
         if (!live && wpr == 1) continue;
         float o[V], M = -INFINITY, L = 0.f;
@@ -760,6 +760,8 @@ cudaError_t launch_attend(AttendArgs a, cudaStream_t s) {
     static std::atomic<uint32_t *> cache[64];
     const cudaError_t e = symbol_address_cached(&g_status_attend, cache, &a.status);
     if (e != cudaSuccess) return e;
+    a.group = a.H / a.Hk;
+    a.by_group = (uint32_t)(((1ull << 32) + a.group - 1) / a.group);  // (not used for a group of 1)
     return a.d == 64 ? launch_d<64>(a, s) : a.d == 128 ? launch_d<128>(a, s) : launch_d<256>(a, s);
 }
 

@@ -32,8 +32,14 @@ __device__ __forceinline__ AttRow att_row(const AttendArgs &p, int b) {
     r.n = p.q_lengths ? max(0, min(p.q_lengths[b], p.T)) : p.T;
     return r;
 }
-__device__ __forceinline__ AttItem att_item(const AttendArgs &p, AttRow w, int rt, int R, int G) {
-    const int t0 = rt * R / G, t1 = min(w.n - 1, (rt * R + R - 1) / G);
+// x / group for 0 <= x < 2^27: the product's quotient is at most one too large
+__device__ __forceinline__ int att_div(const AttendArgs &p, int x) {
+    if (p.group == 1) return x;
+    const int q = (int)__umulhi((uint32_t)x, p.by_group);
+    return q - (q * p.group > x ? 1 : 0);
+}
+__device__ __forceinline__ AttItem att_item(const AttendArgs &p, AttRow w, int rt, int R) {
+    const int t0 = att_div(p, rt * R), t1 = min(w.n - 1, att_div(p, rt * R + R - 1));
     const int hi = w.len - w.n + t1;  // the last token that its last query sees
     if (t0 > t1 || hi < 0) return AttItem{0, 0};
     const int lo = p.window ? max(0, w.len - w.n + t0 - (p.window - 1)) : 0;
@@ -93,13 +99,13 @@ __host__ __device__ inline AttWork att_work(uint8_t *w, int ranges, int R) {
 __device__ __forceinline__ int att_per(int total, int ranges) { return max(1, (total + ranges - 1) / ranges); }
 
 // before[b]: the units of batch rows before b, for one KV head (all threads)
-__device__ inline void att_count(const AttendArgs &p, int R, int G, int unit, int32_t *before) {
-    const int tiles = att_tiles(p.T, R, G);
+__device__ inline void att_count(const AttendArgs &p, int R, int unit, int32_t *before) {
+    const int tiles = att_tiles(p.T, R, p.group);
     for (int b = threadIdx.x; b <= p.batch; b += blockDim.x) before[b] = 0;
     __syncthreads();
     for (int i = threadIdx.x; i < p.batch * tiles; i += blockDim.x) {
         const int b = i / tiles;
-        const int n = att_units(att_item(p, att_row(p, b), i - b * tiles, R, G).pages, unit);
+        const int n = att_units(att_item(p, att_row(p, b), i - b * tiles, R).pages, unit);
         if (tiles == 1) before[b + 1] = n;
         else if (n) atomicAdd(before + b + 1, n);
     }

@@ -31,8 +31,7 @@ static __device__ uint32_t g_status_attend_tc;
 
 namespace {
 
-constexpr int kAtThreads = 16 * 32;  // (warp 15 only completes a warpgroup)
-constexpr int kAtSoftRegs = 176, kAtTurnRegs = 96, kAtIssueRegs = 64;  // of 128 each at launch
+constexpr int kAtThreads = 15 * 32;
 constexpr uint32_t kAtCols = 512;
 constexpr uint32_t kAtO = 256;  // S blocks at columns 0 and 128, O from here on
 constexpr float kAtLag = 4.f;
@@ -145,14 +144,6 @@ __device__ __forceinline__ void at_st16(uint32_t taddr, const uint32_t (&r)[16])
 }
 __device__ __forceinline__ void at_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-template <int N>
-__device__ __forceinline__ void at_more_regs() {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
-}
-template <int N>
-__device__ __forceinline__ void at_fewer_regs() {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
-}
 __device__ __forceinline__ uint32_t at_half2(float a, float b) {  // a in the low half
     const __half2 h = __floats2half2_rn(a, b);
     return *reinterpret_cast<const uint32_t *>(&h);
@@ -169,14 +160,14 @@ struct AtItem {
     int b, rt, h, first, pages, tiles, begin;
     AttRow row;
 };
-__device__ __forceinline__ void at_set(AtItem &it, const AttendArgs &p, int R, int G, int unit) {
-    const AttItem x = att_item(p, it.row, it.rt, R, G);
+__device__ __forceinline__ void at_set(AtItem &it, const AttendArgs &p, int R, int unit) {
+    const AttItem x = att_item(p, it.row, it.rt, R);
     it.first = x.first;
     it.pages = x.pages;
     it.tiles = att_units(x.pages, unit);
 }
 // the item that unit x < total lies in
-__device__ __forceinline__ AtItem at_seek(const AttendArgs &p, const int32_t *before, int x, int R, int G, int unit) {
+__device__ __forceinline__ AtItem at_seek(const AttendArgs &p, const int32_t *before, int x, int R, int unit) {
     AtItem it;
     int lo = 0, hi = p.batch;
     while (hi - lo > 1) {
@@ -191,7 +182,7 @@ __device__ __forceinline__ AtItem at_seek(const AttendArgs &p, const int32_t *be
     const int lane = threadIdx.x & 31;
     for (;; it.rt += 32) {  // 32 tiles of rows at a time
         const int rt = it.rt + lane;
-        int n = rt < att_tiles(it.row.n, R, G) ? att_units(att_item(p, it.row, rt, R, G).pages, unit) * p.Hk : 0;
+        int n = rt < att_tiles(it.row.n, R, p.group) ? att_units(att_item(p, it.row, rt, R).pages, unit) * p.Hk : 0;
         int sum = n;
 #pragma unroll
         for (int i = 1; i < 32; i <<= 1) {
@@ -206,25 +197,25 @@ __device__ __forceinline__ AtItem at_seek(const AttendArgs &p, const int32_t *be
             break;
         }
         at += __shfl_sync(kFull, sum, 31);
-        if (it.rt > att_tiles(it.row.n, R, G)) break;  // (not reached: x lies in this row)
+        if (it.rt > att_tiles(it.row.n, R, p.group)) break;  // (not reached: x lies in this row)
     }
-    at_set(it, p, R, G, unit);
+    at_set(it, p, R, unit);
     it.h = it.tiles ? (x - at) / it.tiles : 0;
     it.begin = at + it.h * it.tiles;
     return it;
 }
 // the item after `it`, given that there is one
-__device__ __forceinline__ void at_next(AtItem &it, const AttendArgs &p, int R, int G, int unit) {
+__device__ __forceinline__ void at_next(AtItem &it, const AttendArgs &p, int R, int unit) {
     it.begin += it.tiles;
     if (++it.h < p.Hk) return;
     it.h = 0;
     do {
-        if (++it.rt >= att_tiles(it.row.n, R, G)) {
+        if (++it.rt * R >= it.row.n * p.group) {
             it.rt = 0;
             if (++it.b >= p.batch) return;
             it.row = att_row(p, it.b);
         }
-        at_set(it, p, R, G, unit);
+        at_set(it, p, R, unit);
     } while (it.tiles == 0);
 }
 
@@ -258,9 +249,10 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
     constexpr int R = 128 * SUB, TN = M::tokens, PG = M::pages;
     extern __shared__ __align__(1024) uint8_t sm[];
     __shared__ uint32_t s_dead, s_tmem;
+    __shared__ AtItem s_next[4 * SUB];  // a softmax warp's next item, kept out of its registers
     const uint32_t sb = smem_u32(sm);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int G = p.H / p.Hk;
+    const int G = p.group;
     auto bar = [&](int i) { return sb + M::bar + 8 * i; };
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // the join waits for the end of this grid itself
     if (threadIdx.x == 0) {
@@ -293,7 +285,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
         tc_fence_before();
     }
     int32_t *const before = reinterpret_cast<int32_t *>(sm + M::before);
-    att_count(p, R, G, PG, before);  // (synchronizes)
+    att_count(p, R, PG, before);  // (synchronizes)
     tc_fence_after();
     const uint32_t tmem = s_tmem;
     const AttWork work = att_work(p.workspace, gridDim.x, R);
@@ -301,7 +293,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
     const int end = (int)min((int64_t)total, ((int64_t)blockIdx.x + 1) * per);
     const int begin = (int)min((int64_t)end, (int64_t)blockIdx.x * per);
     AtItem it{};
-    if (begin < end) it = at_seek(p, before, begin, R, G, PG);
+    if (begin < end) it = at_seek(p, before, begin, R, PG);
     __syncthreads();  // `before` is given up
     const AtWait wait{&s_dead};
     auto together = [](bool ok) { return __all_sync(kFull, ok) != 0; };
@@ -309,7 +301,6 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
     AttSplit split{0, 0, 0, -1, 0, {0, 0, 0}};  // (thread 0)
 
     if (begin < end && warp < M::sm_warps) {
-        at_more_regs<kAtSoftRegs>();
         // ---- softmax: thread = row of a block ----
         const int x = warp >> 2;            // block of rows
         const int row = threadIdx.x & 127;  // in the block: the lane of tensor memory
@@ -323,30 +314,47 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
         bool ok = true;
         constexpr int kC = D / 32;  // chunks of a lane in 8 rows
         for (int at = begin; at < end && ok; ++items) {
-            if (items) at_next(it, p, R, G, PG);
+            if (items) it = s_next[warp];
             const int last = min(end, it.begin + it.tiles);
-            const int r = it.rt * R + x * 128 + row, t = r / G;
+            const int r = it.rt * R + x * 128 + row, t = att_div(p, r);
             const bool live = t < it.row.n;
             const int limit = live ? it.row.len - it.row.n + t : INT_MAX / 2;  // (what rows of no query hold is not used)
             const int from = p.window && live ? limit - (p.window - 1) : 0;
             const int head = it.h * G + (r - t * G);
             float factor = 0.f;
-            {  // q, scaled by a power of two to below 2^15: 8 rows at a time, the next 8 on their way
+            {  // q: copied as it is to where its rows go, then scaled by a power of two to below 2^15, 8 rows at a time
                 const int64_t mine = live ? ((int64_t)it.b * p.T + t) * p.q_stride + (int64_t)head * D : -1;
-                uint4 w[kC];
-                auto load = [&](int g) {
+#pragma unroll 1
+                for (int g = 0; g < 4; ++g) {
                     const int64_t src = __shfl_sync(kFull, mine, 8 * g + (lane & 7));
-                    const uint4 *const q = reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(p.q) + src) + (lane >> 3);
+                    const __nv_bfloat16 *const q = static_cast<const __nv_bfloat16 *>(p.q) + src + 8 * (lane >> 3);
 #pragma unroll
-                    for (int i = 0; i < kC; ++i) w[i] = src >= 0 ? q[4 * i] : make_uint4(0, 0, 0, 0);
-                };
-                load(0);
+                    for (int i = 0; i < kC; ++i) {
+                        const uint32_t to = stage + g * (16 * D) + i * 512;
+                        if (src >= 0) cp_async16(to, q + 32 * i);
+                        else sts128(to, make_uint4(0, 0, 0, 0));
+                    }
+                }
+                cp_async_commit();
+                if (last < end) {  // the next item is found and its queries brought into L2 meanwhile
+                    AtItem next = it;
+                    at_next(next, p, R, PG);
+                    __syncwarp();
+                    if (lane == 0) s_next[warp] = next;
+                    __syncwarp();
+                    const int r2 = next.rt * R + x * 128 + row, t2 = att_div(p, r2);
+                    if (t2 < next.row.n) {
+                        const __nv_bfloat16 *const q = static_cast<const __nv_bfloat16 *>(p.q) + ((int64_t)next.b * p.T + t2) * p.q_stride + (int64_t)(next.h * G + r2 - t2 * G) * D;
+#pragma unroll
+                        for (int i = 0; i < D; i += 64) asm volatile("prefetch.global.L2 [%0];" ::"l"(q + i));
+                    }
+                }
+                cp_async_wait_all();
 #pragma unroll 1
                 for (int g = 0; g < 4; ++g) {
                     uint4 v[kC];
 #pragma unroll
-                    for (int i = 0; i < kC; ++i) v[i] = w[i];
-                    if (g < 3) load(g + 1);
+                    for (int i = 0; i < kC; ++i) v[i] = lds128(stage + g * (16 * D) + i * 512);
                     uint32_t top = 0;  // largest magnitudes of both halves of the words
 #pragma unroll
                     for (int i = 0; i < kC; ++i)
@@ -404,19 +412,24 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
                     }
                     at_st_wait();
                 }
-                uint32_t s[2 * PG][16];
-#pragma unroll
-                for (int c = 0; c < 2 * PG; ++c) at_ld16(s_at + 16 * c, s[c]);
-#pragma unroll
-                for (int c = 0; c < 2 * PG; ++c) at_ld_wait(s[c]);
+                // Half of the columns at a time, in loops: registers hold 64 scores, and the code stays small (the
+                // instruction caches are shared by all roles).
                 float top = -INFINITY;
+#pragma unroll 1
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t s[PG][16];
 #pragma unroll
-                for (int c = 0; c < PG; ++c) {
-                    float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                    for (int c = 0; c < PG; ++c) at_ld16(s_at + (16 * PG) * h + 16 * c, s[c]);
 #pragma unroll
-                    for (int j = 0; j < 32; j += 2)
-                        m[(j >> 1) & 3] = fmax3(m[(j >> 1) & 3], __uint_as_float(s[2 * c + (j >> 4)][j & 15]), __uint_as_float(s[2 * c + (j >> 4)][(j & 15) + 1]));
-                    top = fmaxf(top, fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])) * fmaxf(factor * note->factor[c], FLT_MIN));  // not 0: times a hidden -inf
+                    for (int c = 0; c < PG; ++c) at_ld_wait(s[c]);
+#pragma unroll
+                    for (int c = 0; c < PG / 2; ++c) {
+                        float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                        for (int j = 0; j < 32; j += 2)
+                            m[(j >> 1) & 3] = fmax3(m[(j >> 1) & 3], __uint_as_float(s[2 * c + (j >> 4)][j & 15]), __uint_as_float(s[2 * c + (j >> 4)][(j & 15) + 1]));
+                        top = fmaxf(top, fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])) * fmaxf(factor * note->factor[h * (PG / 2) + c], FLT_MIN));  // not 0: times a hidden -inf
+                    }
                 }
                 const bool moves = top > ref + kAtLag;
                 const float ref_new = moves ? top : ref;
@@ -445,31 +458,38 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
                 }
                 ve = e;
                 const float base = ref == -INFINITY ? 0.f : -ref;
+#pragma unroll 1
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t s[PG][16];
 #pragma unroll
-                for (int c = 0; c < PG; ++c) {
-                    const float2 f2 = splat2(fmaxf(factor * note->factor[c], FLT_MIN)), a2 = splat2(base + note->weight[c]);
-                    float2 z[16];
+                    for (int c = 0; c < PG; ++c) at_ld16(s_at + (16 * PG) * h + 16 * c, s[c]);
 #pragma unroll
-                    for (int j = 0; j < 16; ++j)
-                        z[j] = fma2(make_float2(__uint_as_float(s[2 * c + (j >> 3)][2 * (j & 7)]), __uint_as_float(s[2 * c + (j >> 3)][2 * (j & 7) + 1])), f2, a2);
-                    float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-                    uint32_t w[16];
+                    for (int c = 0; c < PG; ++c) at_ld_wait(s[c]);
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) z[j] = make_float2(ex2(z[j].x), ex2(z[j].y));
+                    for (int c = 0; c < PG / 2; ++c) {
+                        const int page = h * (PG / 2) + c;
+                        const float2 f2 = splat2(fmaxf(factor * note->factor[page], FLT_MIN)), a2 = splat2(base + note->weight[page]);
+                        float2 z[16];
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        part[j & 1] = add2(part[j & 1], z[j]);
-                        w[j] = at_half2(z[j].x, z[j].y);
+                        for (int j = 0; j < 16; ++j)
+                            z[j] = fma2(make_float2(__uint_as_float(s[2 * c + (j >> 3)][2 * (j & 7)]), __uint_as_float(s[2 * c + (j >> 3)][2 * (j & 7) + 1])), f2, a2);
+                        float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                        uint32_t w[16];
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) z[j] = make_float2(ex2(z[j].x), ex2(z[j].y));
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) {
+                            part[j & 1] = add2(part[j & 1], z[j]);
+                            w[j] = at_half2(z[j].x, z[j].y);
+                        }
+                        at_st16(s_at + 16 * page, w);
+                        const float2 both = add2(part[0], part[1]);
+                        sum = fmaf(both.x + both.y, note->back[page], sum);
                     }
-                    at_st16(s_at + 16 * c, w);
-                    const float2 both = add2(part[0], part[1]);
-                    sum = fmaf(both.x + both.y, note->back[c], sum);
-                    if (c == PG / 2 - 1 || c == PG - 1) {  // half of the tokens
-                        at_st_wait();
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) at_arrive(bar(kBarP + 2 * sbuf + (c == PG - 1)));
-                    }
+                    at_st_wait();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) at_arrive(bar(kBarP + 2 * sbuf + h));
                 }
             }
             if (!ok) break;
@@ -534,7 +554,6 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
             tc_fence_before();
         }
     } else if (begin < end && warp < 12) {
-        at_fewer_regs<kAtTurnRegs>();
         // ---- codes into operands: by four warps, with one block of rows by four for K and four for V ----
         constexpr int kQuads = D / 64;                             // 4 chunks of 16 codes
         constexpr int kUnits = (TN / 8) * kQuads / M::turn_warps;  // of 8 tokens x 4 chunks, of a warp
@@ -576,7 +595,6 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
                 break;
         }
     } else if (begin < end) {
-        at_fewer_regs<kAtIssueRegs>();
         if (warp == 14) {
         // ---- the pages' copies, and what the softmax needs of them: lane = page of a tile ----
         auto entry = [&](int x) {  // of tile x, which lies in `it`
@@ -596,7 +614,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
             if (i + 1 < n_tiles) {
                 const int x = begin + (int)i + 1;
                 if (x >= it.begin + it.tiles) {
-                    at_next(it, p, R, G, PG);
+                    at_next(it, p, R, PG);
                     fresh_next = true;
                     h_next = it.h;
                 }
@@ -710,7 +728,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
             if (SUB == 2 && lane == 0) at_arrive(bar(kBarTurn + x));
             first = last;
             if (last && more) {
-                at_next(it, p, R, G, PG);
+                at_next(it, p, R, PG);
                 ++items;
                 ok = together(wait(bar(kBarQ + x), items & 1) && keys(t + 1));
                 if (!ok) break;

@@ -133,7 +133,9 @@ struct AttendArgs {
     const void *q;
     int64_t q_stride;
     float scale;
-    int32_t window;  // 0: none
+    int32_t window;   // 0: none
+    int32_t group;    // H / Hk, and ceil(2^32 / group) to divide by it (set by the launcher)
+    uint32_t by_group;
     void *o;
     int32_t in_bf16;
     uint8_t *workspace;
