@@ -820,7 +820,25 @@ def _here(name, t, shape, dtype, device):
 
 def _call_device(torch, first):
     """The current device (no call on it where there is none: the first tensor is then refused)."""
-    return torch.cuda.current_device() if first.is_cuda else 0
+    if not first.is_cuda:
+        return 0
+    get = getattr(torch._C, "_cuda_getDevice", None)  # current_device() costs a microsecond
+    return torch.cuda.current_device() if get is None else get()
+
+
+def _raw_stream(torch, stream, device):
+    if stream is None:
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if raw is not None:
+            return raw(device)
+    return _stream(stream)
+
+
+def _output(torch, like, contiguous, stream):
+    """An uninitialized contiguous tensor of like's shape and type (empty_like costs half of what empty does)."""
+    if stream is not None:
+        return _new(like.shape, like.dtype, like, stream)
+    return torch.empty_like(like) if contiguous else torch.empty_like(like, memory_format=torch.contiguous_format)
 
 
 def rotary_frequencies(dim, base=10000.0, scaling="none", factor=1.0, trained=4096, turns=(32.0, 1.0), device="cuda"):
@@ -879,20 +897,28 @@ def rotary(q, k, positions, freq, interleaved=False, scale=1.0, q_out=None, k_ou
     per_row = positions.dim() == 1
     qp, qs = _token_rows("q", q, shape, dtype, dev)
     if q_out is None:
-        q_out = _new(shape, dtype, q, stream)
-    kp = ks = ko = None
-    Hk = 0
+        q_out = _output(torch, q, qs == H * d, stream)
+        qo = q_out.data_ptr()
+    else:
+        qo = _here("q_out", q_out, shape, dtype, dev)
+    kp = ko = None
+    Hk = ks = 0
     if k is not None:
         Hk = k.shape[2]
         k_shape = (B, T, Hk, d)
         kp, ks = _token_rows("k", k, k_shape, dtype, dev)
         if k_out is None:
-            k_out = _new(k_shape, dtype, k, stream)
-        ko = _here("k_out", k_out, k_shape, dtype, dev)
-    _check(lib().damp_rotary(qp, qs, H, kp, ks or 0, Hk, d, IN_BF16 if dtype == torch.bfloat16 else IN_FP32,
-                             _here("positions", positions, (B,) if per_row else (B, T), torch.int32, dev), per_row, B, T,
-                             _here("freq", freq, freq.shape, torch.float64, dev), 2 * freq.shape[0], bool(interleaved), scale,
-                             _here("q_out", q_out, shape, dtype, dev), ko, _stream(stream)), "damp_rotary")
+            k_out = _output(torch, k, ks == Hk * d, stream)
+            ko = k_out.data_ptr()
+        else:
+            ko = _here("k_out", k_out, k_shape, dtype, dev)
+    r = freq.shape[0]
+    status = lib().damp_rotary(qp, qs, H, kp, ks, Hk, d, IN_BF16 if dtype == torch.bfloat16 else IN_FP32,
+                               _here("positions", positions, (B,) if per_row else (B, T), torch.int32, dev), per_row, B, T,
+                               _here("freq", freq, (r,), torch.float64, dev), 2 * r, bool(interleaved), scale, qo, ko,
+                               _raw_stream(torch, stream, dev))
+    if status:
+        raise DampError(status, "damp_rotary")
     return q_out, k_out
 
 
@@ -923,9 +949,11 @@ def cache_append(layout, cache, k, v, pages, start, lengths=None, stream=None):
     kp, ks = _token_rows("k", k, shape, dtype, dev)
     vp, vs = _token_rows("v", v, shape, dtype, dev)
     pool, n, table, W = _cache(layout, cache, pages, B, dev, i32, torch.uint8)
-    _check(lib().damp_cache_append(layout._ref, pool, n, table, W, B, T, _here("start", start, (B,), i32, dev),
-                                   None if lengths is None else _here("lengths", lengths, (B,), i32, dev), kp, ks, vp, vs,
-                                   IN_BF16 if dtype == torch.bfloat16 else IN_FP32, _stream(stream)), "damp_cache_append")
+    status = lib().damp_cache_append(layout._ref, pool, n, table, W, B, T, _here("start", start, (B,), i32, dev),
+                                     None if lengths is None else _here("lengths", lengths, (B,), i32, dev), kp, ks, vp, vs,
+                                     IN_BF16 if dtype == torch.bfloat16 else IN_FP32, _raw_stream(torch, stream, dev))
+    if status:
+        raise DampError(status, "damp_cache_append")
 
 
 def cache_read(layout, cache, pages, lengths, tokens, start=None, dtype=None, k=None, v=None, stream=None):
@@ -949,11 +977,14 @@ def cache_read(layout, cache, pages, lengths, tokens, start=None, dtype=None, k=
     shape = (B, T, layout.num_kv_heads, layout.d)
     if k is None:
         k = _new(shape, dtype, cache, stream)
+    kp = _here("k", k, shape, dtype, dev)
     if v is None:
-        v = _new(shape, dtype, cache, stream)
-    _check(lib().damp_cache_read(layout._ref, pool, n, table, W, B, T, None if start is None else _here("start", start, (B,), i32, dev),
-                                 held, _here("k", k, shape, dtype, dev), _here("v", v, shape, dtype, dev),
-                                 IN_BF16 if dtype == torch.bfloat16 else IN_FP32, _stream(stream)), "damp_cache_read")
+        v = _output(torch, k, True, stream)
+    vp = _here("v", v, shape, dtype, dev)
+    status = lib().damp_cache_read(layout._ref, pool, n, table, W, B, T, None if start is None else _here("start", start, (B,), i32, dev),
+                                   held, kp, vp, IN_BF16 if dtype == torch.bfloat16 else IN_FP32, _raw_stream(torch, stream, dev))
+    if status:
+        raise DampError(status, "damp_cache_read")
     return k, v
 
 
@@ -977,15 +1008,21 @@ def cache_attend(layout, cache, q, pages, lengths, q_lengths=None, scale=None, w
     pool, n, table, W = _cache(layout, cache, pages, B, dev, i32, torch.uint8)
     held = _here("lengths", lengths, (B,), i32, dev)
     if o is None:
-        o = _new(shape, dtype, q, stream)
-    c, L = layout._ref, lib()
+        o = _output(torch, q, qs == layout.num_heads * d, stream)
+        op = o.data_ptr()
+    else:
+        op = _here("o", o, shape, dtype, dev)
+    L = lib()
     need = layout._workspace.get((dev, B, T, dt))
     if need is None:
-        need = layout._workspace[dev, B, T, dt] = L.damp_cache_attend_workspace(c, B, T, dt)
-    ws = _new((need,), torch.uint8, q, stream)
-    _check(L.damp_cache_attend(c, pool, n, table, W, B, T, held, None if q_lengths is None else _here("q_lengths", q_lengths, (B,), i32, dev),
-                               qp, qs, d ** -0.5 if scale is None else scale, 0 if window is None else min(window, 0x7fffffff),
-                               _here("o", o, shape, dtype, dev), dt, ws.data_ptr(), need, _stream(stream)), "damp_cache_attend")
+        need = layout._workspace[dev, B, T, dt] = L.damp_cache_attend_workspace(layout._ref, B, T, dt)
+    ws = q.new_empty(need // (4 if dt else 2)) if stream is None else _new((need,), torch.uint8, q, stream)
+    status = L.damp_cache_attend(layout._ref, pool, n, table, W, B, T, held,
+                                 None if q_lengths is None else _here("q_lengths", q_lengths, (B,), i32, dev), qp, qs,
+                                 d ** -0.5 if scale is None else scale, 0 if window is None else min(window, 0x7fffffff), op, dt,
+                                 ws.data_ptr(), need, _raw_stream(torch, stream, dev))
+    if status:
+        raise DampError(status, "damp_cache_attend")
     return o
 
 
