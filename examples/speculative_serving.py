@@ -1,17 +1,18 @@
 """Speculative decoding of a small recurrent language model on libdamp.
 
-A model of linear-attention layers (decay per head on FP32 states, or GDN on the packed state)
-with random weights serves a batch of requests:
+A model of linear-attention layers (decay per head on FP32 states, or GDN on the packed state) and
+softmax-attention layers between them (an 8-bit cache) with random weights serves a batch of requests:
 
   prompt    the prompts, of different lengths, run as one chunk per layer
   round     copy_slots saves every layer's state; the first layer alone drafts D tokens, step by
             step; copy_slots takes its state back; all layers run the drafted tokens as one chunk;
             verify_drafts accepts a prefix and draws the next token; copy_slots takes the states
             back and the chunk runs once more over the accepted tokens, whose numbers
-            (verify_drafts' counts) are the chunk's lengths on the device
+            (verify_drafts' counts) are the chunk's lengths on the device.  A cache needs no saved
+            copy: a request goes back to the number of tokens it held, later tokens are written over
   end       zero_slots frees finished requests, compact_slots closes the pools up
 
-    python examples/speculative_serving.py [--layers lin,gdn,lin] [--batch 8] [--drafts 4]
+    python examples/speculative_serving.py [--layers lin,gdn,attn,lin] [--batch 8] [--drafts 4]
 """
 import argparse
 import os
@@ -43,7 +44,7 @@ class Layer:
             self.pool = damp.new_state(self.layout, slots, device)
             self.perm = torch.arange(D_HEAD, dtype=torch.uint8, device=device).repeat(HEADS, 1)
 
-    def run(self, x, slot_idx, lengths=None):
+    def run(self, x, slot_idx, held, lengths=None):
         """x [B, T, width] -> x + the layer's output; the state of slot_idx moves on (row b by lengths[b])."""
         B, T, _ = x.shape
         unit = lambda z: torch.nn.functional.normalize(z.view(B, T, QK_HEADS, D_HEAD), dim=-1)
@@ -65,6 +66,32 @@ class Layer:
         return x + o.reshape(B, T, HEADS * D_HEAD) @ self.wo
 
 
+class AttentionLayer:
+    """One softmax-attention layer: its weights, its cache (a slot: PAGES pages) and the calls on it."""
+
+    PAGES = 8
+
+    def __init__(self, width, slots, gen, device):
+        n = lambda *s: torch.randn(*s, generator=gen, device=device)
+        self.wqkv = n(width, (HEADS + 2 * QK_HEADS) * D_HEAD) / width ** 0.5
+        self.wo = n(HEADS * D_HEAD, width) / 16
+        self.layout = damp.CacheLayout(HEADS, QK_HEADS, D_HEAD)
+        self.cache = damp.new_cache(self.layout, slots * self.PAGES, device)
+        self.pool = self.cache.view(slots, -1)
+        self.freq, self.scale = damp.rotary_frequencies(D_HEAD, device=device)
+
+    def run(self, x, slot_idx, held, lengths=None):
+        """x [B, T, width] -> x + the layer's output; row b, which holds held[b] tokens, takes lengths[b] more."""
+        B, T, _ = x.shape
+        qkv = (x @ self.wqkv).view(B, T, HEADS + 2 * QK_HEADS, D_HEAD)
+        q, k, v = qkv.split((HEADS, QK_HEADS, QK_HEADS), 2)
+        q, k = damp.rotary(q, k, held, self.freq, scale=self.scale)
+        pages = slot_idx[:, None] * self.PAGES + torch.arange(self.PAGES, dtype=torch.int32, device=x.device)
+        damp.cache_append(self.layout, self.cache, k, v, pages, held, lengths=lengths)
+        o = damp.cache_attend(self.layout, self.cache, q, pages, held + (T if lengths is None else lengths), q_lengths=lengths)
+        return x + o.reshape(B, T, HEADS * D_HEAD) @ self.wo
+
+
 class Server:
     """Requests in the first half of the slots, their saved states in the second half."""
 
@@ -73,15 +100,19 @@ class Server:
         self.slots, self.vocab, self.device = slots, vocab, device
         self.embed = torch.randn(vocab, width, generator=self.gen, device=device)
         self.head = torch.randn(width, vocab, generator=self.gen, device=device) * (4.0 / width ** 0.5)
-        self.layers = [Layer(k, width, 2 * slots, self.gen, device) for k in kinds]
+        self.layers = [AttentionLayer(width, 2 * slots, self.gen, device) if k == "attn" else Layer(k, width, 2 * slots, self.gen, device)
+                       for k in kinds]
         self.pools = [layer.pool for layer in self.layers]
+        self.states = [layer.pool for layer in self.layers if isinstance(layer, Layer)]  # what a round saves
+        self.held = torch.empty(0, dtype=torch.int32, device=device)  # tokens that have run
         self.slot_idx = torch.empty(0, dtype=torch.int32, device=device)
 
-    def logits(self, tokens, depth=None, lengths=None):
-        """Logits [B, T, vocab] of tokens [B, T]; the states of the first `depth` layers move on."""
+    def logits(self, tokens, depth=None, lengths=None, ahead=0):
+        """Logits [B, T, vocab] of tokens [B, T], `ahead` tokens after those held; the states of the first `depth`
+        layers move on."""
         x = self.embed[tokens.long()]
         for layer in self.layers[:depth]:
-            x = layer.run(x, self.slot_idx, lengths)
+            x = layer.run(x, self.slot_idx, self.held + ahead, lengths)
         return torch.nn.functional.rms_norm(x, x.shape[-1:]) @ self.head
 
     def prompt(self, tokens, lengths):
@@ -90,8 +121,15 @@ class Server:
         lengths = lengths.clamp(1, tokens.shape[1])
         self.slot_idx = torch.arange(B, dtype=torch.int32, device=self.device)
         damp.zero_slots(self.pools, self.slot_idx)
+        self.held = torch.zeros_like(self.slot_idx)
         self.logits(tokens, lengths=lengths - 1)
+        self.held = (lengths - 1).to(torch.int32)
         self.last = tokens.gather(1, lengths.long()[:, None] - 1).to(torch.int32)
+
+    @staticmethod
+    def copy(pools, src, dst):
+        if pools:  # (a model of softmax-attention layers alone has no state to save)
+            damp.copy_slots(pools, src, dst)
 
     def saved(self):
         return self.slot_idx + self.slots
@@ -104,21 +142,22 @@ class Server:
     def round(self, drafts, temperature):
         """One round for every request: (tokens [B, drafts + 1], count [B])."""
         B, saved = self.slot_idx.shape[0], self.saved()
-        damp.copy_slots(self.pools, self.slot_idx, saved)
+        self.copy(self.states, self.slot_idx, saved)
         token, drafted, q = self.last, [], []
-        for _ in range(drafts):
-            q.append(self.logits(token, depth=1))
+        for i in range(drafts):
+            q.append(self.logits(token, depth=1, ahead=i))
             token = self.draw(q[-1][:, 0], temperature)
             drafted.append(token)
-        damp.copy_slots(self.pools[:1], saved, self.slot_idx)
+        self.copy([p for p in self.states if p is self.pools[0]], saved, self.slot_idx)
         chunk = torch.cat([self.last] + drafted, 1)
         target = self.logits(chunk)
         u = torch.rand(B, drafts, generator=self.gen, device=self.device)
         noise = torch.empty(B, self.vocab, device=self.device).exponential_(generator=self.gen)
         tokens, count = damp.verify_drafts(target, torch.cat(drafted, 1), u, noise, draft_logits=torch.cat(q, 1),
                                            temperature=temperature)
-        damp.copy_slots(self.pools, saved, self.slot_idx)
+        self.copy(self.states, saved, self.slot_idx)
         self.logits(chunk, lengths=count)
+        self.held = self.held + count
         # logits that exclude every token give none (count 0): the request stays where it was
         last = tokens.gather(1, (count.long()[:, None] - 1).clamp(min=0))
         self.last = torch.where(count[:, None] > 0, last, self.last)
@@ -127,18 +166,19 @@ class Server:
     def step(self, temperature):
         """One token without drafts, for comparison: tokens [B, 1]."""
         self.last = self.draw(self.logits(self.last)[:, 0], temperature)
+        self.held = self.held + 1
         return self.last
 
     def finish(self, done):
         """Frees the requests of the mask `done` and closes the pools up."""
         damp.zero_slots(self.pools, self.slot_idx[done].contiguous())
         self.slot_idx = damp.compact_slots(self.pools, self.slot_idx[~done].contiguous())
-        self.last = self.last[~done].contiguous()
+        self.last, self.held = self.last[~done].contiguous(), self.held[~done].contiguous()
 
 
 def main():
     ap = argparse.ArgumentParser()
-    ap.add_argument("--layers", default="lin,gdn,lin")
+    ap.add_argument("--layers", default="lin,gdn,attn,lin")
     ap.add_argument("--batch", type=int, default=8)
     ap.add_argument("--drafts", type=int, default=4)
     ap.add_argument("--rounds", type=int, default=6)

@@ -1,7 +1,7 @@
 // attend.cu -- attention over the 8-bit cache: o_r = sum_j softmax_j(scale q_r.k_j) v_j.
 //
-// The rows of an item are the (query token, query head) pairs that share a (batch row, KV head), 16
-// or 32 of them; its keys are the pages from the first that its first query sees to the last that
+// The rows of an item are the (query token, query head) pairs that share a (batch row, KV head), 16 of
+// them; its keys are the pages from the first that its first query sees to the last that
 // its last query sees.  All pages of all items form one sequence, which is cut into equal ranges,
 // one per warp: the work is even whatever the lengths are, and the host need not know them.  A warp
 // keeps one item's running maximum m, sum l and output o in registers and passes over each page
@@ -30,15 +30,15 @@ static __device__ uint32_t g_status_attend;
 namespace {
 
 constexpr int kJoinThreads = 256;
-template <int D, int MT, bool F32>
+template <int D, bool F32>
 struct AttCfg {
-    static constexpr int R = 16 * MT;
+    static constexpr int R = 16;
     static constexpr int parts = F32 ? 2 : 1;
     static constexpr int warps = D == 256 ? 4 : 8;
     static constexpr int threads = warps * 32;
     static constexpr int rec = cache_record_bytes(D);
-    static constexpr bool q_smem = MT * (D / 2 + parts * D / 4) > 128;  // registers of o and q
-    static constexpr int qbytes = q_smem ? MT * parts * (D / 16) * 512 : 0;
+    static constexpr bool q_smem = D / 2 + parts * D / 4 > 128;  // registers of o and q
+    static constexpr int qbytes = q_smem ? parts * (D / 16) * 512 : 0;
     static constexpr int stages = std::min(4, (215000 / warps - qbytes) / (rec + 48));
     static constexpr int ring = stages * rec;
     static constexpr int warp_bytes = ring + qbytes + stages * 48;  // 32 bytes about the page, the barrier
@@ -49,16 +49,6 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-// bytes 0 and 2 (or as `sel` says) of w as FP16 codes minus 128: 0x64 above a byte is 1024 + byte
-__device__ __forceinline__ uint32_t half_codes(uint32_t w, uint32_t sel) {
-    const uint32_t h = prmt(w, 0x64646464u, sel);
-    const __half2 y = __hadd2(*reinterpret_cast<const __half2 *>(&h), __half2(__ushort_as_half(0xE480), __ushort_as_half(0xE480)));  // -1152
-    return *reinterpret_cast<const uint32_t *>(&y);
-}
-__device__ __forceinline__ uint32_t half_pair(float a, float b) {
-    const __half2 h = __floats2half2_rn(a, b);
-    return *reinterpret_cast<const uint32_t *>(&h);
 }
 // a and b as FP16 parts
 __device__ __forceinline__ void split_pair(float a, float b, uint32_t &hi, uint32_t &lo) {
@@ -110,9 +100,9 @@ struct AttPage {  // a page of the sequence, 32 bytes
     int bad, unused;
 };
 
-template <int D, int MT, bool F32>
-__global__ void __launch_bounds__(AttCfg<D, MT, F32>::threads, 1) attend_kernel(const AttendArgs p) {
-    using C = AttCfg<D, MT, F32>;
+template <int D, bool F32>
+__global__ void __launch_bounds__(AttCfg<D, F32>::threads, 1) attend_kernel(const AttendArgs p) {
+    using C = AttCfg<D, F32>;
     constexpr int R = C::R, kSteps = D / 16, kCols = D / 8;  // K steps of Q K^T, column tiles of P V
     constexpr bool BF = !F32;
     extern __shared__ __align__(128) uint8_t sm[];
@@ -195,9 +185,9 @@ __global__ void __launch_bounds__(AttCfg<D, MT, F32>::threads, 1) attend_kernel(
     // ---- the item at hand ----
     int item = -1;  // its first page in the sequence
     AttPage now{};
-    float o[MT][kCols][4], m[MT][2], l[MT][2], factor[MT][2];
-    int limit[MT][2];  // the last token that a row sees
-    uint32_t q[C::q_smem ? 1 : MT][C::q_smem ? 1 : C::parts][C::q_smem ? 1 : kSteps][4];
+    float o[kCols][4], m[2], l[2], factor[2];
+    int limit[2];  // the last token that a row sees
+    uint32_t q[C::q_smem ? 1 : C::parts][C::q_smem ? 1 : kSteps][4];
     int ve = 0;  // exponent field of the outputs' unit
 
     // the item at hand: written if it lies in the range, else a part of it, in the workspace or (own: for the CTA to
@@ -209,30 +199,27 @@ __global__ void __launch_bounds__(AttCfg<D, MT, F32>::threads, 1) attend_kernel(
         float2 *const mls = own ? reinterpret_cast<float2 *>(parts + R * D) : work.ml + (int64_t)slot * R;
         const float unit = __uint_as_float((uint32_t)ve << 23) * (1.f / 1024.f);
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
+        for (int hh = 0; hh < 2; ++hh) {
+            const int r = hh * 8 + g;  // in the item
+            const int row = now.rt * R + r, t = att_div(p, row);
+            const float sum = quad_sum(l[hh]);
+            const bool live = limit[hh] != kNoRow;
+            const float y = whole ? (sum == 0.f ? 0.f : unit / sum) : unit;
+            const int64_t to = ((int64_t)(now.b * (int64_t)p.T + t) * p.H + now.h * G + (row - t * G)) * D;
+            float *const part = parts + r * D;
+            if (live) {
+                if (!whole && c == 0) mls[r] = make_float2(m[hh], sum);
+                constexpr int N = D == 64 ? 8 : 16;
 #pragma unroll
-            for (int hh = 0; hh < 2; ++hh) {
-                const int r = mt * 16 + hh * 8 + g;  // in the item
-                const int row = now.rt * R + r, t = att_div(p, row);
-                const float sum = quad_sum(l[mt][hh]);
-                const bool live = limit[mt][hh] != kNoRow;
-                const float y = whole ? (sum == 0.f ? 0.f : unit / sum) : unit;
-                const int64_t to = ((int64_t)(now.b * (int64_t)p.T + t) * p.H + now.h * G + (row - t * G)) * D;
-                float *const part = parts + r * D;
-                if (live) {
-                    if (!whole && c == 0) mls[r] = make_float2(m[mt][hh], sum);
-                    constexpr int N = D == 64 ? 8 : 16;
+                for (int k = 0; k < 2 * kCols / N; ++k) {  // runs of N columns
+                    const int col = (k >> 1) * 128 + 2 * N * c + N * (k & 1);
+                    float x[N];
 #pragma unroll
-                    for (int k = 0; k < 2 * kCols / N; ++k) {  // runs of N columns
-                        const int col = (k >> 1) * 128 + 2 * N * c + N * (k & 1);
-                        float x[N];
-#pragma unroll
-                        for (int i = 0; i < N; ++i) x[i] = o[mt][(k >> 1) * 16 + i][2 * hh + (k & 1)] * y;
-                        if (whole)
-                            store_out<BF, N>(p.o, to + col, x);
-                        else
-                            store_out<false, N>(part, col, x);
-                    }
+                    for (int i = 0; i < N; ++i) x[i] = o[(k >> 1) * 16 + i][2 * hh + (k & 1)] * y;
+                    if (whole)
+                        store_out<BF, N>(p.o, to + col, x);
+                    else
+                        store_out<false, N>(part, col, x);
                 }
             }
         }
@@ -240,71 +227,68 @@ __global__ void __launch_bounds__(AttCfg<D, MT, F32>::threads, 1) attend_kernel(
     auto start = [&]() {
         const AttRow w = att_row(p, now.b);
         __syncwarp();
+        int64_t from[2];
+        bool live[2];
+        float up[2];
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            int64_t from[2];
-            bool live[2];
-            float up[2];
-#pragma unroll
-            for (int hh = 0; hh < 2; ++hh) {
-                const int row = now.rt * R + mt * 16 + hh * 8 + g, t = att_div(p, row);
-                live[hh] = t < w.n;
-                limit[mt][hh] = live[hh] ? w.len - w.n + t : kNoRow;
-                from[hh] = ((int64_t)now.b * p.T + t) * p.q_stride + (int64_t)(now.h * G + (row - t * G)) * D;
-                float top = 0.f;
-#pragma unroll
-                for (int j = 0; j < D / 64; ++j) {
-                    float x[16];
-                    load16<BF>(p.q, from[hh] + 16 * (c + 4 * j), live[hh], x);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(x[i]));
-                }
-                top = quad_max(top);
-                const int e = min(max((int)(__float_as_uint(top) >> 23), 15), 254);  // up to below 2^15
-                up[hh] = __uint_as_float((uint32_t)(268 - e) << 23);
-                factor[mt][hh] = p.scale * kLog2e / up[hh];
-                m[mt][hh] = -INFINITY;
-                l[mt][hh] = 0.f;
-            }
+        for (int hh = 0; hh < 2; ++hh) {
+            const int row = now.rt * R + hh * 8 + g, t = att_div(p, row);
+            live[hh] = t < w.n;
+            limit[hh] = live[hh] ? w.len - w.n + t : kNoRow;
+            from[hh] = ((int64_t)now.b * p.T + t) * p.q_stride + (int64_t)(now.h * G + (row - t * G)) * D;
+            float top = 0.f;
 #pragma unroll
             for (int j = 0; j < D / 64; ++j) {
-                float x[2][16];
+                float x[16];
+                load16<BF>(p.q, from[hh] + 16 * (c + 4 * j), live[hh], x);
 #pragma unroll
-                for (int hh = 0; hh < 2; ++hh) {
-                    load16<BF>(p.q, from[hh] + 16 * (c + 4 * j), live[hh], x[hh]);
+                for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(x[i]));
+            }
+            top = quad_max(top);
+            const int e = min(max((int)(__float_as_uint(top) >> 23), 15), 254);  // up to below 2^15
+            up[hh] = __uint_as_float((uint32_t)(268 - e) << 23);
+            factor[hh] = p.scale * kLog2e / up[hh];
+            m[hh] = -INFINITY;
+            l[hh] = 0.f;
+        }
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) x[hh][i] *= up[hh];
-                }
+        for (int j = 0; j < D / 64; ++j) {
+            float x[2][16];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    uint32_t hi[4], lo[4];
+            for (int hh = 0; hh < 2; ++hh) {
+                load16<BF>(p.q, from[hh] + 16 * (c + 4 * j), live[hh], x[hh]);
 #pragma unroll
-                    for (int k = 0; k < 2; ++k) {
+                for (int i = 0; i < 16; ++i) x[hh][i] *= up[hh];
+            }
 #pragma unroll
-                        for (int hh = 0; hh < 2; ++hh) {
-                            if (F32)
-                                split_pair(x[hh][4 * i + 2 * k], x[hh][4 * i + 2 * k + 1], hi[2 * k + hh], lo[2 * k + hh]);
-                            else
-                                hi[2 * k + hh] = half_pair(x[hh][4 * i + 2 * k], x[hh][4 * i + 2 * k + 1]);
-                        }
+            for (int i = 0; i < 4; ++i) {
+                uint32_t hi[4], lo[4];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+#pragma unroll
+                    for (int hh = 0; hh < 2; ++hh) {
+                        if (F32)
+                            split_pair(x[hh][4 * i + 2 * k], x[hh][4 * i + 2 * k + 1], hi[2 * k + hh], lo[2 * k + hh]);
+                        else
+                            hi[2 * k + hh] = half_pair(x[hh][4 * i + 2 * k], x[hh][4 * i + 2 * k + 1]);
                     }
-                    const int step = 4 * j + i;
-                    if constexpr (C::q_smem) {
-                        const uint32_t at = qs + ((mt * C::parts) * kSteps + step) * 512 + lane * 16;
-                        sts128(at, make_uint4(hi[0], hi[1], hi[2], hi[3]));
-                        if (F32) sts128(at + kSteps * 512, make_uint4(lo[0], lo[1], lo[2], lo[3]));
-                    } else {
+                }
+                const int step = 4 * j + i;
+                if constexpr (C::q_smem) {
+                    const uint32_t at = qs + step * 512 + lane * 16;
+                    sts128(at, make_uint4(hi[0], hi[1], hi[2], hi[3]));
+                    if (F32) sts128(at + kSteps * 512, make_uint4(lo[0], lo[1], lo[2], lo[3]));
+                } else {
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            q[mt][0][step][k] = hi[k];
-                            if constexpr (F32) q[mt][1][step][k] = lo[k];
-                        }
+                    for (int k = 0; k < 4; ++k) {
+                        q[0][step][k] = hi[k];
+                        if constexpr (F32) q[1][step][k] = lo[k];
                     }
                 }
             }
-#pragma unroll
-            for (int i = 0; i < kCols; ++i) o[mt][i][0] = o[mt][i][1] = o[mt][i][2] = o[mt][i][3] = 0.f;
         }
+#pragma unroll
+        for (int i = 0; i < kCols; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
         ve = 0;
         __syncwarp();
     };
@@ -338,11 +322,9 @@ __global__ void __launch_bounds__(AttCfg<D, MT, F32>::threads, 1) attend_kernel(
         const uint32_t kb = ring + stage * C::rec, vb = kb + cache_rows_bytes(D);
         if (!info->bad) {
             const float ks = __uint_as_float(lds32(vb + cache_rows_bytes(D))), vs = __uint_as_float(lds32(vb + cache_rows_bytes(D) + 4));
-            float s[MT][4][4];
+            float s[4][4];
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                for (int nt = 0; nt < 4; ++nt) s[mt][nt][0] = s[mt][nt][1] = s[mt][nt][2] = s[mt][nt][3] = 0.f;
+            for (int nt = 0; nt < 4; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
 #pragma unroll
             for (int j = 0; j < D / 64; ++j) {
                 uint4 kk[4];
@@ -351,27 +333,23 @@ __global__ void __launch_bounds__(AttCfg<D, MT, F32>::threads, 1) attend_kernel(
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int step = 4 * j + i;
-                    uint32_t a[MT][C::parts][4];
+                    uint32_t a[C::parts][4];
 #pragma unroll
-                    for (int mt = 0; mt < MT; ++mt)
+                    for (int pt = 0; pt < C::parts; ++pt) {
+                        if constexpr (C::q_smem) {
+                            const uint4 w = lds128(qs + (pt * kSteps + step) * 512 + lane * 16);
+                            a[pt][0] = w.x, a[pt][1] = w.y, a[pt][2] = w.z, a[pt][3] = w.w;
+                        } else {
 #pragma unroll
-                        for (int pt = 0; pt < C::parts; ++pt) {
-                            if constexpr (C::q_smem) {
-                                const uint4 w = lds128(qs + ((mt * C::parts + pt) * kSteps + step) * 512 + lane * 16);
-                                a[mt][pt][0] = w.x, a[mt][pt][1] = w.y, a[mt][pt][2] = w.z, a[mt][pt][3] = w.w;
-                            } else {
-#pragma unroll
-                                for (int k = 0; k < 4; ++k) a[mt][pt][k] = q[mt][pt][step][k];
-                            }
+                            for (int k = 0; k < 4; ++k) a[pt][k] = q[pt][step][k];
                         }
+                    }
 #pragma unroll
                     for (int nt = 0; nt < 4; ++nt) {
                         const uint32_t w = i == 0 ? kk[nt].x : i == 1 ? kk[nt].y : i == 2 ? kk[nt].z : kk[nt].w;
                         const uint32_t b0 = half_codes(w, 0x4140u), b1 = half_codes(w, 0x4342u);
 #pragma unroll
-                        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                            for (int pt = 0; pt < C::parts; ++pt) mma16816(s[mt][nt], a[mt][pt], b0, b1);
+                        for (int pt = 0; pt < C::parts; ++pt) mma16816(s[nt], a[pt], b0, b1);
                     }
                 }
             }
@@ -386,71 +364,62 @@ __global__ void __launch_bounds__(AttCfg<D, MT, F32>::threads, 1) attend_kernel(
             const int at = page * kCachePage;
             bool edge = false;
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                for (int hh = 0; hh < 2; ++hh) {
-                    const int k = limit[mt][hh];
-                    edge = edge || (k != kNoRow && (k < at + kCachePage - 1 || (p.window && k - (p.window - 1) > at)));
-                }
+            for (int hh = 0; hh < 2; ++hh) {
+                const int k = limit[hh];
+                edge = edge || (k != kNoRow && (k < at + kCachePage - 1 || (p.window && k - (p.window - 1) > at)));
+            }
             const bool masked = __any_sync(kFull, edge);
-            uint32_t pa[MT][C::parts][4][2];  // [column tile][row half]
-            float corr[MT][2];
+            uint32_t pa[C::parts][4][2];  // [column tile][row half]
+            float corr[2];
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
+            for (int hh = 0; hh < 2; ++hh) {
+                const float fac = factor[hh] * ks;
+                float x[8], top = -INFINITY;
 #pragma unroll
-                for (int hh = 0; hh < 2; ++hh) {
-                    const float fac = factor[mt][hh] * ks;
-                    float x[8], top = -INFINITY;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) x[i] = s[mt][i >> 1][2 * hh + (i & 1)] * fac;
-                    if (masked) {
-                        const int k = limit[mt][hh], from = p.window ? k - (p.window - 1) : 0;
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const int token = at + 8 * (i >> 1) + 2 * c + (i & 1);
-                            if (token > k || token < from) x[i] = -INFINITY;
-                        }
-                    }
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) top = fmaxf(top, x[i]);
-                    const float mn = fmaxf(m[mt][hh], quad_max(top)), mu = mn == -INFINITY ? 0.f : mn;
-                    corr[mt][hh] = ex2(m[mt][hh] - mu);
-                    moved = moved || mn != m[mt][hh];
-                    m[mt][hh] = mn;
-                    float sum = 0.f;
+                for (int i = 0; i < 8; ++i) x[i] = s[i >> 1][2 * hh + (i & 1)] * fac;
+                if (masked) {
+                    const int k = limit[hh], from = p.window ? k - (p.window - 1) : 0;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        x[i] = ex2(x[i] - mu);
-                        sum += x[i];
-                        x[i] *= wscale;
+                        const int token = at + 8 * (i >> 1) + 2 * c + (i & 1);
+                        if (token > k || token < from) x[i] = -INFINITY;
                     }
-                    l[mt][hh] = fmaf(l[mt][hh], corr[mt][hh], sum);
+                }
 #pragma unroll
-                    for (int nt = 0; nt < 4; ++nt) {
-                        if constexpr (F32)
-                            split_pair(x[2 * nt], x[2 * nt + 1], pa[mt][0][nt][hh], pa[mt][1][nt][hh]);
-                        else
-                            pa[mt][0][nt][hh] = half_pair(x[2 * nt], x[2 * nt + 1]);
-                    }
+                for (int i = 0; i < 8; ++i) top = fmaxf(top, x[i]);
+                const float mn = fmaxf(m[hh], quad_max(top)), mu = mn == -INFINITY ? 0.f : mn;
+                corr[hh] = ex2(m[hh] - mu);
+                moved = moved || mn != m[hh];
+                m[hh] = mn;
+                float sum = 0.f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    x[i] = ex2(x[i] - mu);
+                    sum += x[i];
+                    x[i] *= wscale;
+                }
+                l[hh] = fmaf(l[hh], corr[hh], sum);
+#pragma unroll
+                for (int nt = 0; nt < 4; ++nt) {
+                    if constexpr (F32)
+                        split_pair(x[2 * nt], x[2 * nt + 1], pa[0][nt][hh], pa[1][nt][hh]);
+                    else
+                        pa[0][nt][hh] = half_pair(x[2 * nt], x[2 * nt + 1]);
                 }
             }
             if (__any_sync(kFull, moved)) {
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
+                for (int i = 0; i < kCols; ++i)
 #pragma unroll
-                    for (int i = 0; i < kCols; ++i)
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) o[mt][i][k] *= corr[mt][k >> 1] * vcorr;
+                    for (int k = 0; k < 4; ++k) o[i][k] *= corr[k >> 1] * vcorr;
             }
 #pragma unroll
             for (int s2 = 0; s2 < 2; ++s2) {
-                uint32_t a[MT][C::parts][4];
+                uint32_t a[C::parts][4];
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
+                for (int pt = 0; pt < C::parts; ++pt)
 #pragma unroll
-                    for (int pt = 0; pt < C::parts; ++pt)
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) a[mt][pt][k] = pa[mt][pt][2 * s2 + (k >> 1)][k & 1];
+                    for (int k = 0; k < 4; ++k) a[pt][k] = pa[pt][2 * s2 + (k >> 1)][k & 1];
 #pragma unroll
                 for (int grp = 0; grp < (D + 127) / 128; ++grp) {
                     constexpr int W = D == 64 ? 2 : 4;  // words of codes per token
@@ -475,9 +444,7 @@ __global__ void __launch_bounds__(AttCfg<D, MT, F32>::threads, 1) attend_kernel(
 #pragma unroll
                         for (int k = 0; k < 4; ++k)
 #pragma unroll
-                            for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                                for (int pt = 0; pt < C::parts; ++pt) mma16816(o[mt][grp * 16 + 4 * i + k], a[mt][pt], b0[k], b1[k]);
+                            for (int pt = 0; pt < C::parts; ++pt) mma16816(o[grp * 16 + 4 * i + k], a[pt], b0[k], b1[k]);
                     }
                 }
             }
@@ -729,14 +696,14 @@ cudaError_t launch_join(const AttendArgs &a, int R, int ranges, cudaStream_t s) 
     cfg.gridDim = dim3((unsigned)(ranges + clear), (unsigned)((rows * wpr + kWarps - 1) / kWarps));
     return cudaLaunchKernelEx(&cfg, attend_join_kernel<D, BF>, a, ranges, wpr, slice);
 }
-template <int D, int MT, bool F32>
+template <int D, bool F32>
 cudaError_t launch_as(const AttendArgs &a, cudaStream_t s) {
-    using C = AttCfg<D, MT, F32>;
+    using C = AttCfg<D, F32>;
     const int smem = C::warps * C::warp_bytes + (a.batch + 1) * 4;
-    cudaError_t e = ensure_smem_limit(reinterpret_cast<const void *>(attend_kernel<D, MT, F32>), smem);
+    cudaError_t e = ensure_smem_limit(reinterpret_cast<const void *>(attend_kernel<D, F32>), smem);
     if (e != cudaSuccess) return e;
     const int grid = sm_count();
-    attend_kernel<D, MT, F32><<<grid, C::threads, smem, s>>>(a);
+    attend_kernel<D, F32><<<grid, C::threads, smem, s>>>(a);
     e = cudaGetLastError();
     return e != cudaSuccess ? e : launch_join<D, !F32>(a, C::R, grid * C::warps, s);
 }
@@ -746,7 +713,7 @@ cudaError_t launch_d(const AttendArgs &a, cudaStream_t s) {
         const cudaError_t e = launch_attend_tc(a, sm_count(), s);
         return e != cudaSuccess ? e : launch_join<D, true>(a, attend_tc_rows(a), sm_count(), s);
     }
-    return a.in_bf16 ? launch_as<D, 1, false>(a, s) : launch_as<D, 1, true>(a, s);
+    return a.in_bf16 ? launch_as<D, false>(a, s) : launch_as<D, true>(a, s);
 }
 
 }  // namespace

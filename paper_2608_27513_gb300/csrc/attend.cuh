@@ -53,6 +53,17 @@ __device__ __forceinline__ float ex2(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// bytes 0 and 2 (or as `sel` says) of w as FP16 codes minus 128: 0x64 above a byte is 1024 + byte
+__device__ __forceinline__ uint32_t half_codes(uint32_t w, uint32_t sel) {
+    const uint32_t h = prmt(w, 0x64646464u, sel);
+    const __half2 y = __hadd2(*reinterpret_cast<const __half2 *>(&h), __half2(__ushort_as_half(0xE480), __ushort_as_half(0xE480)));  // -1152
+    return *reinterpret_cast<const uint32_t *>(&y);
+}
+// a in the low half
+__device__ __forceinline__ uint32_t half_pair(float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
 // N (8 or 16) consecutive outputs
 template <bool BF, int N>
 __device__ __forceinline__ void store_out(void *o, int64_t at, const float (&x)[N]) {

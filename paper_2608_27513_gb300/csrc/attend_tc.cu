@@ -144,17 +144,6 @@ __device__ __forceinline__ void at_st16(uint32_t taddr, const uint32_t (&r)[16])
 }
 __device__ __forceinline__ void at_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-__device__ __forceinline__ uint32_t at_half2(float a, float b) {  // a in the low half
-    const __half2 h = __floats2half2_rn(a, b);
-    return *reinterpret_cast<const uint32_t *>(&h);
-}
-// bytes of w that `sel` names as FP16 codes minus 128
-__device__ __forceinline__ uint32_t at_codes(uint32_t w, uint32_t sel) {
-    const uint32_t h = prmt(w, 0x64646464u, sel);
-    const __half2 y = __hadd2(*reinterpret_cast<const __half2 *>(&h), __half2(__ushort_as_half(0xE480), __ushort_as_half(0xE480)));
-    return *reinterpret_cast<const uint32_t *>(&y);
-}
-
 // An item of the sequence, the same in all lanes of a warp.
 struct AtItem {
     int b, rt, h, first, pages, tiles, begin;
@@ -370,7 +359,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
                         uint32_t h[4];
 #pragma unroll
                         for (int k = 0; k < 4; ++k)
-                            h[k] = at_half2(__uint_as_float(u[k] << 16) * up, __uint_as_float(u[k] & 0xffff0000u) * up);
+                            h[k] = half_pair(__uint_as_float(u[k] << 16) * up, __uint_as_float(u[k] & 0xffff0000u) * up);
                         sts128(stage + g * (16 * D) + i * 512, make_uint4(h[0], h[1], h[2], h[3]));
                     }
                 }
@@ -480,7 +469,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
 #pragma unroll
                         for (int j = 0; j < 16; ++j) {
                             part[j & 1] = add2(part[j & 1], z[j]);
-                            w[j] = at_half2(z[j].x, z[j].y);
+                            w[j] = half_pair(z[j].x, z[j].y);
                         }
                         at_st16(s_at + 16 * page, w);
                         const float2 both = add2(part[0], part[1]);
@@ -574,8 +563,8 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
             for (int j = 0; j < kUnits; ++j) {
                 const int u = w + j * M::turn_warps, tg = u / kQuads, mq = u % kQuads;
                 const uint32_t at = to + tg * (16 * D) + (mq * 4 + mi) * 256 + tok * 16;
-                sts128(at, make_uint4(at_codes(c[j].x, 0x4140u), at_codes(c[j].x, 0x4342u), at_codes(c[j].y, 0x4140u), at_codes(c[j].y, 0x4342u)));
-                sts128(at + 128, make_uint4(at_codes(c[j].z, 0x4140u), at_codes(c[j].z, 0x4342u), at_codes(c[j].w, 0x4140u), at_codes(c[j].w, 0x4342u)));
+                sts128(at, make_uint4(half_codes(c[j].x, 0x4140u), half_codes(c[j].x, 0x4342u), half_codes(c[j].y, 0x4140u), half_codes(c[j].y, 0x4342u)));
+                sts128(at + 128, make_uint4(half_codes(c[j].z, 0x4140u), half_codes(c[j].z, 0x4342u), half_codes(c[j].w, 0x4140u), half_codes(c[j].w, 0x4342u)));
             }
             fence_proxy_async_smem();
             __syncwarp();

@@ -274,10 +274,54 @@ def test_attend_many_tokens(dtype, H, Hk, d, T, W, window):
                q_lengths=[T - 1, T, 0, 1])
 
 
+@pytest.mark.parametrize("H,Hk,d", [(4, 4, 64), (8, 2, 128), (8, 1, 256)])
+@pytest.mark.parametrize("window", [None, 100])
+def test_attend_many_items(H, Hk, d, window):
+    """More items than the GPU has ranges: whole ones, ones that end and begin in a range, rows of no query."""
+    B, T, W = 40, 150, 9
+    layout = damp.CacheLayout(H, Hk, d)
+    pool, pages = filled(layout, B, W, d)
+    g = gen(H)
+    q = 1.5 * randn(g, B, T, H, d)
+    n = torch.randint(0, W * R.PAGE + 1, (B,)).tolist()
+    new = torch.randint(0, T + 1, (B,)).tolist()
+    run_attend(layout, pool, pages, q.to(BF), n, "many items", window=window, q_lengths=new)
+    run_attend(layout, pool, pages, q[:, :4].to(BF).contiguous(), n, "many drafts", window=window)
+
+
+@pytest.mark.parametrize("H,T", [(65, 1), (65, 3), (67, 9), (200, 2), (3, 50)])
+def test_attend_groups(H, T):
+    """Groups of query heads that are no powers of two, one KV head."""
+    layout = damp.CacheLayout(H, 1, 64)
+    pool, pages = filled(layout, 3, 4, H)
+    q = randn(gen(T), 3, T, H, 64)
+    for dtype in (BF, F32):
+        run_attend(layout, pool, pages, q.to(dtype), [128, 55, 9], f"group of {H}", window=70)
+
+
+def test_attend_many_tokens_of_slices_and_bad_pages():
+    """Prompts whose queries are slices of a projection; bad pages in the middle, at the end and everywhere."""
+    layout = damp.CacheLayout(4, 2, 128)
+    pool, pages = filled(layout, 4, 6, 9)
+    x = randn(gen(1), 4, 100, 8, 128, dtype=BF)
+    pages[0, 2], pages[1, 5], pages[2] = -1, 1 << 20, -5
+    q = x[:, :, 1:5]
+    n = [190, 170, 192, 100]
+    o = damp.cache_attend(layout, pool, q, pages, i32(n))
+    assert damp.device_status() == damp.DEV_BAD_SLOT
+    want, bounds = R.attend(R.Cache(pool, 128), q, pages.cpu(), n)
+    R.check_attend(o, want, bounds, 192, 128, "slices and bad pages")
+    assert not o[2].any()
+
+
 def test_attend_clamps_lengths():
     layout = damp.CacheLayout(4, 2, 64)
     pool, pages = filled(layout, 3, 2, 8)
     q = randn(gen(1), 3, 3, 4, 64, dtype=BF)
+    long = randn(gen(2), 3, 80, 4, 64, dtype=BF)
+    a = damp.cache_attend(layout, pool, long, pages, i32([2**31 - 1, -5, 64]), q_lengths=i32([2**31 - 1, 3, -1]))
+    b = damp.cache_attend(layout, pool, long, pages, i32([64, 0, 64]), q_lengths=i32([80, 3, 0]))
+    assert torch.equal(a, b) and not b[0, :16].any() and b[0, 16:].any(dim=-1).all() and not b[1:].any()
     a = damp.cache_attend(layout, pool, q, pages, i32([2**31 - 1, -5, 64]), q_lengths=i32([2**31 - 1, 3, -1]))
     b = damp.cache_attend(layout, pool, q, pages, i32([64, 0, 64]), q_lengths=i32([3, 3, 0]))
     assert torch.equal(a, b) and not b[1:].any()
