@@ -496,7 +496,7 @@ typedef struct {
  *               j = lengths[b] - q_lengths[b] + t and sees tokens max(0, j - window + 1) .. j.
  *               A query that sees none gives zeros, and so do those past q_lengths[b].
  *   workspace   damp_cache_attend_workspace() bytes, 16-B aligned, of no use to any other call
- *               while this one runs
+ *               while this one runs (0 bytes for few rows of short tables: NULL is then allowed)
  *   Maxima, sums and outputs are FP32; weights enter the product with the values in FP16 (FP32
  *   inputs: as two FP16 parts each).  A NaN or infinity in a query reaches its own head's output
  *   alone.  How rows are split over the GPU depends on the lengths of the batch, and with it the
@@ -517,7 +517,8 @@ DAMP_API damp_status damp_cache_attend(const damp_cache_layout *layout, const vo
                                        const int32_t *lengths, const int32_t *q_lengths, const void *q,
                                        int64_t q_stride, float scale, int32_t window, void *o, int32_t dtype,
                                        void *workspace, int64_t workspace_bytes, void *stream);
-DAMP_API int64_t damp_cache_attend_workspace(const damp_cache_layout *layout, int32_t batch, int32_t T, int32_t dtype);
+DAMP_API int64_t damp_cache_attend_workspace(const damp_cache_layout *layout, int32_t batch, int32_t T, int32_t table,
+                                             int32_t dtype);
 
 /*
  * Write FP32 states into the packed cache: the hand-off from an FP32 prefix

@@ -1013,14 +1013,16 @@ def cache_attend(layout, cache, q, pages, lengths, q_lengths=None, scale=None, w
     else:
         op = _here("o", o, shape, dtype, dev)
     L = lib()
-    need = layout._workspace.get((dev, B, T, dt))
+    need = layout._workspace.get((dev, B, T, W, dt))
     if need is None:
-        need = layout._workspace[dev, B, T, dt] = L.damp_cache_attend_workspace(layout._ref, B, T, dt)
-    ws = q.new_empty(need // (4 if dt else 2)) if stream is None else _new((need,), torch.uint8, q, stream)
+        need = layout._workspace[dev, B, T, W, dt] = L.damp_cache_attend_workspace(layout._ref, B, T, W, dt)
+    ws = None
+    if need:
+        ws = q.new_empty(need // (4 if dt else 2)) if stream is None else _new((need,), torch.uint8, q, stream)
     status = L.damp_cache_attend(layout._ref, pool, n, table, W, B, T, held,
                                  None if q_lengths is None else _here("q_lengths", q_lengths, (B,), i32, dev), qp, qs,
                                  d ** -0.5 if scale is None else scale, 0 if window is None else min(window, 0x7fffffff), op, dt,
-                                 ws.data_ptr(), need, _raw_stream(torch, stream, dev))
+                                 None if ws is None else ws.data_ptr(), need, _raw_stream(torch, stream, dev))
     if status:
         raise DampError(status, "damp_cache_attend")
     return o

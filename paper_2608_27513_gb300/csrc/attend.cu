@@ -94,6 +94,251 @@ __device__ __forceinline__ void load16(const void *p, int64_t at, bool live, flo
         }
     }
 }
+// 16 rows of queries and what a warp has of their outputs.
+template <int D, bool F32>
+struct AttRows {
+    using C = AttCfg<D, F32>;
+    static constexpr int R = C::R, kSteps = D / 16, kCols = D / 8;  // K steps of Q K^T, column tiles of P V
+    static constexpr bool BF = !F32;
+    float o[kCols][4], m[2], l[2], factor[2];
+    int limit[2];  // the last token that a row sees
+    uint32_t q[C::q_smem ? 1 : C::parts][C::q_smem ? 1 : kSteps][4];
+    int ve;  // exponent field of the outputs' unit
+
+    // tile rt of a batch row's queries; qs: where in shared memory the operands go that registers do not hold
+    __device__ __forceinline__ void start(const AttendArgs &p, AttRow w, int b, int rt, int h, uint32_t qs, int lane) {
+        const int G = p.group, g = lane >> 2, c = lane & 3;
+        __syncwarp();
+        int64_t from[2];
+        bool live[2];
+        float up[2];
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh) {
+            const int row = rt * R + hh * 8 + g, t = att_div(p, row);
+            live[hh] = t < w.n;
+            limit[hh] = live[hh] ? w.len - w.n + t : kNoRow;
+            from[hh] = ((int64_t)b * p.T + t) * p.q_stride + (int64_t)(h * G + (row - t * G)) * D;
+            float top = 0.f;
+#pragma unroll
+            for (int j = 0; j < D / 64; ++j) {
+                float x[16];
+                load16<BF>(p.q, from[hh] + 16 * (c + 4 * j), live[hh], x);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(x[i]));
+            }
+            top = quad_max(top);
+            const int e = min(max((int)(__float_as_uint(top) >> 23), 15), 254);  // up to below 2^15
+            up[hh] = __uint_as_float((uint32_t)(268 - e) << 23);
+            factor[hh] = p.scale * kLog2e / up[hh];
+            m[hh] = -INFINITY;
+            l[hh] = 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < D / 64; ++j) {
+            float x[2][16];
+#pragma unroll
+            for (int hh = 0; hh < 2; ++hh) {
+                load16<BF>(p.q, from[hh] + 16 * (c + 4 * j), live[hh], x[hh]);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[hh][i] *= up[hh];
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint32_t hi[4], lo[4];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+#pragma unroll
+                    for (int hh = 0; hh < 2; ++hh) {
+                        if (F32)
+                            split_pair(x[hh][4 * i + 2 * k], x[hh][4 * i + 2 * k + 1], hi[2 * k + hh], lo[2 * k + hh]);
+                        else
+                            hi[2 * k + hh] = half_pair(x[hh][4 * i + 2 * k], x[hh][4 * i + 2 * k + 1]);
+                    }
+                }
+                const int step = 4 * j + i;
+                if constexpr (C::q_smem) {
+                    const uint32_t at = qs + step * 512 + lane * 16;
+                    sts128(at, make_uint4(hi[0], hi[1], hi[2], hi[3]));
+                    if (F32) sts128(at + kSteps * 512, make_uint4(lo[0], lo[1], lo[2], lo[3]));
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        q[0][step][k] = hi[k];
+                        if constexpr (F32) q[1][step][k] = lo[k];
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kCols; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+        ve = 0;
+        __syncwarp();
+    }
+    // one page, whose record lies at kb in shared memory
+    __device__ __forceinline__ void page(const AttendArgs &p, uint32_t kb, int page, uint32_t qs, int lane) {
+        const int g = lane >> 2, c = lane & 3;
+        const int kswz = cache_swizzle(g, D), vswz[2] = {cache_swizzle(2 * c, D), cache_swizzle(2 * c + 1, D)};
+        const uint32_t vb = kb + cache_rows_bytes(D);
+        const float ks = __uint_as_float(lds32(vb + cache_rows_bytes(D))), vs = __uint_as_float(lds32(vb + cache_rows_bytes(D) + 4));
+        float s[4][4];
+#pragma unroll
+        for (int nt = 0; nt < 4; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
+#pragma unroll
+        for (int j = 0; j < D / 64; ++j) {
+            uint4 kk[4];
+#pragma unroll
+            for (int nt = 0; nt < 4; ++nt) kk[nt] = lds128(kb + (8 * nt + g) * D + 16 * ((c + 4 * j) ^ kswz));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int step = 4 * j + i;
+                uint32_t a[C::parts][4];
+#pragma unroll
+                for (int pt = 0; pt < C::parts; ++pt) {
+                    if constexpr (C::q_smem) {
+                        const uint4 w = lds128(qs + (pt * kSteps + step) * 512 + lane * 16);
+                        a[pt][0] = w.x, a[pt][1] = w.y, a[pt][2] = w.z, a[pt][3] = w.w;
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) a[pt][k] = q[pt][step][k];
+                    }
+                }
+#pragma unroll
+                for (int nt = 0; nt < 4; ++nt) {
+                    const uint32_t w = i == 0 ? kk[nt].x : i == 1 ? kk[nt].y : i == 2 ? kk[nt].z : kk[nt].w;
+                    const uint32_t b0 = half_codes(w, 0x4140u), b1 = half_codes(w, 0x4342u);
+#pragma unroll
+                    for (int pt = 0; pt < C::parts; ++pt) mma16816(s[nt], a[pt], b0, b1);
+                }
+            }
+        }
+        // the outputs' unit: a power of two above every value scale so far
+        const int e = min((int)(__float_as_uint(vs) >> 23) + 1, 253);
+        const int ve_new = max(ve, vs > 0.f ? e : 0);
+        const float wscale = vs * __uint_as_float((uint32_t)(254 - max(ve_new, 1)) << 23) * 1024.f;
+        const int shift = 127 + ve - ve_new;
+        const float vcorr = shift > 0 ? __uint_as_float((uint32_t)shift << 23) : 0.f;
+        bool moved = ve_new != ve;
+        ve = ve_new;
+        const int at = page * kCachePage;
+        bool edge = false;
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh) {
+            const int k = limit[hh];
+            edge = edge || (k != kNoRow && (k < at + kCachePage - 1 || (p.window && k - (p.window - 1) > at)));
+        }
+        const bool masked = __any_sync(kFull, edge);
+        uint32_t pa[C::parts][4][2];  // [column tile][row half]
+        float corr[2];
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh) {
+            const float fac = factor[hh] * ks;
+            float x[8], top = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = s[i >> 1][2 * hh + (i & 1)] * fac;
+            if (masked) {
+                const int k = limit[hh], from = p.window ? k - (p.window - 1) : 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int token = at + 8 * (i >> 1) + 2 * c + (i & 1);
+                    if (token > k || token < from) x[i] = -INFINITY;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) top = fmaxf(top, x[i]);
+            const float mn = fmaxf(m[hh], quad_max(top)), mu = mn == -INFINITY ? 0.f : mn;
+            corr[hh] = ex2(m[hh] - mu);
+            moved = moved || mn != m[hh];
+            m[hh] = mn;
+            float sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                x[i] = ex2(x[i] - mu);
+                sum += x[i];
+                x[i] *= wscale;
+            }
+            l[hh] = fmaf(l[hh], corr[hh], sum);
+#pragma unroll
+            for (int nt = 0; nt < 4; ++nt) {
+                if constexpr (F32)
+                    split_pair(x[2 * nt], x[2 * nt + 1], pa[0][nt][hh], pa[1][nt][hh]);
+                else
+                    pa[0][nt][hh] = half_pair(x[2 * nt], x[2 * nt + 1]);
+            }
+        }
+        if (__any_sync(kFull, moved)) {
+#pragma unroll
+            for (int i = 0; i < kCols; ++i)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) o[i][k] *= corr[k >> 1] * vcorr;
+        }
+#pragma unroll
+        for (int s2 = 0; s2 < 2; ++s2) {
+            uint32_t a[C::parts][4];
+#pragma unroll
+            for (int pt = 0; pt < C::parts; ++pt)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) a[pt][k] = pa[pt][2 * s2 + (k >> 1)][k & 1];
+#pragma unroll
+            for (int grp = 0; grp < (D + 127) / 128; ++grp) {
+                constexpr int W = D == 64 ? 2 : 4;  // words of codes per token
+                uint32_t w[4][W];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const uint32_t row = vb + (16 * s2 + 8 * (k >> 1) + 2 * c + (k & 1)) * D;
+                    if constexpr (D == 64) {
+                        const uint2 y = lds64(row + 16 * ((g >> 1) ^ vswz[k & 1]) + 8 * (g & 1));
+                        w[k][0] = y.x, w[k][1] = y.y;
+                    } else {
+                        const uint4 y = lds128(row + 16 * ((g + 8 * grp) ^ vswz[k & 1]));
+                        w[k][0] = y.x, w[k][1] = y.y, w[k][W - 2] = y.z, w[k][W - 1] = y.w;
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < W; ++i) {
+                    const uint32_t t0 = prmt(w[0][i], w[1][i], 0x5140u), t1 = prmt(w[0][i], w[1][i], 0x7362u);
+                    const uint32_t u0 = prmt(w[2][i], w[3][i], 0x5140u), u1 = prmt(w[2][i], w[3][i], 0x7362u);
+                    const uint32_t b0[4] = {half_codes(t0, 0x4140u), half_codes(t0, 0x4342u), half_codes(t1, 0x4140u), half_codes(t1, 0x4342u)};
+                    const uint32_t b1[4] = {half_codes(u0, 0x4140u), half_codes(u0, 0x4342u), half_codes(u1, 0x4140u), half_codes(u1, 0x4342u)};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+#pragma unroll
+                        for (int pt = 0; pt < C::parts; ++pt) mma16816(o[grp * 16 + 4 * i + k], a[pt], b0[k], b1[k]);
+                }
+            }
+        }
+    }
+    // the outputs, where all pages were this warp's; else a part of them: rows of D values, and their (m, l)
+    __device__ __forceinline__ void leave(const AttendArgs &p, int b, int rt, int h, bool whole, float *parts, float2 *mls, int lane) {
+        const int G = p.group, g = lane >> 2, c = lane & 3;
+        const float unit = __uint_as_float((uint32_t)ve << 23) * (1.f / 1024.f);
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh) {
+            const int r = hh * 8 + g;  // in the item
+            const int row = rt * R + r, t = att_div(p, row);
+            const float sum = quad_sum(l[hh]);
+            const bool live = limit[hh] != kNoRow;
+            const float y = whole ? (sum == 0.f ? 0.f : unit / sum) : unit;
+            const int64_t to = ((int64_t)(b * (int64_t)p.T + t) * p.H + h * G + (row - t * G)) * D;
+            float *const part = parts + r * D;
+            if (live) {
+                if (!whole && c == 0) mls[r] = make_float2(m[hh], sum);
+                constexpr int N = D == 64 ? 8 : 16;
+#pragma unroll
+                for (int k = 0; k < 2 * kCols / N; ++k) {  // runs of N columns
+                    const int col = (k >> 1) * 128 + 2 * N * c + N * (k & 1);
+                    float x[N];
+#pragma unroll
+                    for (int i = 0; i < N; ++i) x[i] = o[(k >> 1) * 16 + i][2 * hh + (k & 1)] * y;
+                    if (whole)
+                        store_out<BF, N>(p.o, to + col, x);
+                    else
+                        store_out<false, N>(part, col, x);
+                }
+            }
+        }
+    }
+};
+
 struct AttPage {  // a page of the sequence, 32 bytes
     int b, rt, h, page;    // page: in the row's table
     int begin, count;      // of its item, in the sequence
@@ -103,11 +348,10 @@ struct AttPage {  // a page of the sequence, 32 bytes
 template <int D, bool F32>
 __global__ void __launch_bounds__(AttCfg<D, F32>::threads, 1) attend_kernel(const AttendArgs p) {
     using C = AttCfg<D, F32>;
-    constexpr int R = C::R, kSteps = D / 16, kCols = D / 8;  // K steps of Q K^T, column tiles of P V
-    constexpr bool BF = !F32;
+    constexpr int R = C::R;
     extern __shared__ __align__(128) uint8_t sm[];
     int32_t *const before = reinterpret_cast<int32_t *>(sm + C::warps * C::warp_bytes);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int G = p.group;
     uint8_t *const mine = sm + warp * C::warp_bytes;
     uint8_t *const about = mine + C::ring + C::qbytes;  // [stages] AttPage, then the barriers
@@ -185,115 +429,17 @@ __global__ void __launch_bounds__(AttCfg<D, F32>::threads, 1) attend_kernel(cons
     // ---- the item at hand ----
     int item = -1;  // its first page in the sequence
     AttPage now{};
-    float o[kCols][4], m[2], l[2], factor[2];
-    int limit[2];  // the last token that a row sees
-    uint32_t q[C::q_smem ? 1 : C::parts][C::q_smem ? 1 : kSteps][4];
-    int ve = 0;  // exponent field of the outputs' unit
+    AttRows<D, F32> rows;
 
     // the item at hand: written if it lies in the range, else a part of it, in the workspace or (own: for the CTA to
-    // join) in this warp's ring, rows of D values and then (m, l)
+    // join) in this warp's ring
     auto finish = [&](bool own) {
         const bool whole = now.begin >= begin && now.begin + now.count <= end;
-        const int slot = 2 * range + (now.begin >= begin ? 1 : 0);
-        float *const parts = own ? reinterpret_cast<float *>(mine) : work.o + (int64_t)slot * R * D;
-        float2 *const mls = own ? reinterpret_cast<float2 *>(parts + R * D) : work.ml + (int64_t)slot * R;
-        const float unit = __uint_as_float((uint32_t)ve << 23) * (1.f / 1024.f);
-#pragma unroll
-        for (int hh = 0; hh < 2; ++hh) {
-            const int r = hh * 8 + g;  // in the item
-            const int row = now.rt * R + r, t = att_div(p, row);
-            const float sum = quad_sum(l[hh]);
-            const bool live = limit[hh] != kNoRow;
-            const float y = whole ? (sum == 0.f ? 0.f : unit / sum) : unit;
-            const int64_t to = ((int64_t)(now.b * (int64_t)p.T + t) * p.H + now.h * G + (row - t * G)) * D;
-            float *const part = parts + r * D;
-            if (live) {
-                if (!whole && c == 0) mls[r] = make_float2(m[hh], sum);
-                constexpr int N = D == 64 ? 8 : 16;
-#pragma unroll
-                for (int k = 0; k < 2 * kCols / N; ++k) {  // runs of N columns
-                    const int col = (k >> 1) * 128 + 2 * N * c + N * (k & 1);
-                    float x[N];
-#pragma unroll
-                    for (int i = 0; i < N; ++i) x[i] = o[(k >> 1) * 16 + i][2 * hh + (k & 1)] * y;
-                    if (whole)
-                        store_out<BF, N>(p.o, to + col, x);
-                    else
-                        store_out<false, N>(part, col, x);
-                }
-            }
-        }
-    };
-    auto start = [&]() {
-        const AttRow w = att_row(p, now.b);
-        __syncwarp();
-        int64_t from[2];
-        bool live[2];
-        float up[2];
-#pragma unroll
-        for (int hh = 0; hh < 2; ++hh) {
-            const int row = now.rt * R + hh * 8 + g, t = att_div(p, row);
-            live[hh] = t < w.n;
-            limit[hh] = live[hh] ? w.len - w.n + t : kNoRow;
-            from[hh] = ((int64_t)now.b * p.T + t) * p.q_stride + (int64_t)(now.h * G + (row - t * G)) * D;
-            float top = 0.f;
-#pragma unroll
-            for (int j = 0; j < D / 64; ++j) {
-                float x[16];
-                load16<BF>(p.q, from[hh] + 16 * (c + 4 * j), live[hh], x);
-#pragma unroll
-                for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(x[i]));
-            }
-            top = quad_max(top);
-            const int e = min(max((int)(__float_as_uint(top) >> 23), 15), 254);  // up to below 2^15
-            up[hh] = __uint_as_float((uint32_t)(268 - e) << 23);
-            factor[hh] = p.scale * kLog2e / up[hh];
-            m[hh] = -INFINITY;
-            l[hh] = 0.f;
-        }
-#pragma unroll
-        for (int j = 0; j < D / 64; ++j) {
-            float x[2][16];
-#pragma unroll
-            for (int hh = 0; hh < 2; ++hh) {
-                load16<BF>(p.q, from[hh] + 16 * (c + 4 * j), live[hh], x[hh]);
-#pragma unroll
-                for (int i = 0; i < 16; ++i) x[hh][i] *= up[hh];
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                uint32_t hi[4], lo[4];
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-#pragma unroll
-                    for (int hh = 0; hh < 2; ++hh) {
-                        if (F32)
-                            split_pair(x[hh][4 * i + 2 * k], x[hh][4 * i + 2 * k + 1], hi[2 * k + hh], lo[2 * k + hh]);
-                        else
-                            hi[2 * k + hh] = half_pair(x[hh][4 * i + 2 * k], x[hh][4 * i + 2 * k + 1]);
-                    }
-                }
-                const int step = 4 * j + i;
-                if constexpr (C::q_smem) {
-                    const uint32_t at = qs + step * 512 + lane * 16;
-                    sts128(at, make_uint4(hi[0], hi[1], hi[2], hi[3]));
-                    if (F32) sts128(at + kSteps * 512, make_uint4(lo[0], lo[1], lo[2], lo[3]));
-                } else {
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        q[0][step][k] = hi[k];
-                        if constexpr (F32) q[1][step][k] = lo[k];
-                    }
-                }
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < kCols; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
-        ve = 0;
-        __syncwarp();
+        const int64_t slot = 2 * range + (now.begin >= begin ? 1 : 0);
+        float *const parts = own ? reinterpret_cast<float *>(mine) : work.o + slot * R * D;
+        rows.leave(p, now.b, now.rt, now.h, whole, parts, own ? reinterpret_cast<float2 *>(parts + R * D) : work.ml + slot * R, lane);
     };
 
-    const int kswz = cache_swizzle(g, D), vswz[2] = {cache_swizzle(2 * c, D), cache_swizzle(2 * c + 1, D)};
     int stage = 0;
     uint32_t parity = 0;
     for (int f = begin; f < end && !failed; ++f) {
@@ -316,139 +462,9 @@ __global__ void __launch_bounds__(AttCfg<D, F32>::threads, 1) attend_kernel(cons
             if (item >= 0) finish(false);
             now = *info;
             item = now.begin;
-            start();
+            rows.start(p, att_row(p, now.b), now.b, now.rt, now.h, qs, lane);
         }
-        const int page = info->page;
-        const uint32_t kb = ring + stage * C::rec, vb = kb + cache_rows_bytes(D);
-        if (!info->bad) {
-            const float ks = __uint_as_float(lds32(vb + cache_rows_bytes(D))), vs = __uint_as_float(lds32(vb + cache_rows_bytes(D) + 4));
-            float s[4][4];
-#pragma unroll
-            for (int nt = 0; nt < 4; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
-#pragma unroll
-            for (int j = 0; j < D / 64; ++j) {
-                uint4 kk[4];
-#pragma unroll
-                for (int nt = 0; nt < 4; ++nt) kk[nt] = lds128(kb + (8 * nt + g) * D + 16 * ((c + 4 * j) ^ kswz));
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int step = 4 * j + i;
-                    uint32_t a[C::parts][4];
-#pragma unroll
-                    for (int pt = 0; pt < C::parts; ++pt) {
-                        if constexpr (C::q_smem) {
-                            const uint4 w = lds128(qs + (pt * kSteps + step) * 512 + lane * 16);
-                            a[pt][0] = w.x, a[pt][1] = w.y, a[pt][2] = w.z, a[pt][3] = w.w;
-                        } else {
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) a[pt][k] = q[pt][step][k];
-                        }
-                    }
-#pragma unroll
-                    for (int nt = 0; nt < 4; ++nt) {
-                        const uint32_t w = i == 0 ? kk[nt].x : i == 1 ? kk[nt].y : i == 2 ? kk[nt].z : kk[nt].w;
-                        const uint32_t b0 = half_codes(w, 0x4140u), b1 = half_codes(w, 0x4342u);
-#pragma unroll
-                        for (int pt = 0; pt < C::parts; ++pt) mma16816(s[nt], a[pt], b0, b1);
-                    }
-                }
-            }
-            // the outputs' unit: a power of two above every value scale so far
-            const int e = min((int)(__float_as_uint(vs) >> 23) + 1, 253);
-            const int ve_new = max(ve, vs > 0.f ? e : 0);
-            const float wscale = vs * __uint_as_float((uint32_t)(254 - max(ve_new, 1)) << 23) * 1024.f;
-            const int shift = 127 + ve - ve_new;
-            const float vcorr = shift > 0 ? __uint_as_float((uint32_t)shift << 23) : 0.f;
-            bool moved = ve_new != ve;
-            ve = ve_new;
-            const int at = page * kCachePage;
-            bool edge = false;
-#pragma unroll
-            for (int hh = 0; hh < 2; ++hh) {
-                const int k = limit[hh];
-                edge = edge || (k != kNoRow && (k < at + kCachePage - 1 || (p.window && k - (p.window - 1) > at)));
-            }
-            const bool masked = __any_sync(kFull, edge);
-            uint32_t pa[C::parts][4][2];  // [column tile][row half]
-            float corr[2];
-#pragma unroll
-            for (int hh = 0; hh < 2; ++hh) {
-                const float fac = factor[hh] * ks;
-                float x[8], top = -INFINITY;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = s[i >> 1][2 * hh + (i & 1)] * fac;
-                if (masked) {
-                    const int k = limit[hh], from = p.window ? k - (p.window - 1) : 0;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int token = at + 8 * (i >> 1) + 2 * c + (i & 1);
-                        if (token > k || token < from) x[i] = -INFINITY;
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < 8; ++i) top = fmaxf(top, x[i]);
-                const float mn = fmaxf(m[hh], quad_max(top)), mu = mn == -INFINITY ? 0.f : mn;
-                corr[hh] = ex2(m[hh] - mu);
-                moved = moved || mn != m[hh];
-                m[hh] = mn;
-                float sum = 0.f;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    x[i] = ex2(x[i] - mu);
-                    sum += x[i];
-                    x[i] *= wscale;
-                }
-                l[hh] = fmaf(l[hh], corr[hh], sum);
-#pragma unroll
-                for (int nt = 0; nt < 4; ++nt) {
-                    if constexpr (F32)
-                        split_pair(x[2 * nt], x[2 * nt + 1], pa[0][nt][hh], pa[1][nt][hh]);
-                    else
-                        pa[0][nt][hh] = half_pair(x[2 * nt], x[2 * nt + 1]);
-                }
-            }
-            if (__any_sync(kFull, moved)) {
-#pragma unroll
-                for (int i = 0; i < kCols; ++i)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) o[i][k] *= corr[k >> 1] * vcorr;
-            }
-#pragma unroll
-            for (int s2 = 0; s2 < 2; ++s2) {
-                uint32_t a[C::parts][4];
-#pragma unroll
-                for (int pt = 0; pt < C::parts; ++pt)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) a[pt][k] = pa[pt][2 * s2 + (k >> 1)][k & 1];
-#pragma unroll
-                for (int grp = 0; grp < (D + 127) / 128; ++grp) {
-                    constexpr int W = D == 64 ? 2 : 4;  // words of codes per token
-                    uint32_t w[4][W];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const uint32_t row = vb + (16 * s2 + 8 * (k >> 1) + 2 * c + (k & 1)) * D;
-                        if constexpr (D == 64) {
-                            const uint2 y = lds64(row + 16 * ((g >> 1) ^ vswz[k & 1]) + 8 * (g & 1));
-                            w[k][0] = y.x, w[k][1] = y.y;
-                        } else {
-                            const uint4 y = lds128(row + 16 * ((g + 8 * grp) ^ vswz[k & 1]));
-                            w[k][0] = y.x, w[k][1] = y.y, w[k][W - 2] = y.z, w[k][W - 1] = y.w;
-                        }
-                    }
-#pragma unroll
-                    for (int i = 0; i < W; ++i) {
-                        const uint32_t t0 = prmt(w[0][i], w[1][i], 0x5140u), t1 = prmt(w[0][i], w[1][i], 0x7362u);
-                        const uint32_t u0 = prmt(w[2][i], w[3][i], 0x5140u), u1 = prmt(w[2][i], w[3][i], 0x7362u);
-                        const uint32_t b0[4] = {half_codes(t0, 0x4140u), half_codes(t0, 0x4342u), half_codes(t1, 0x4140u), half_codes(t1, 0x4342u)};
-                        const uint32_t b1[4] = {half_codes(u0, 0x4140u), half_codes(u0, 0x4342u), half_codes(u1, 0x4140u), half_codes(u1, 0x4342u)};
-#pragma unroll
-                        for (int k = 0; k < 4; ++k)
-#pragma unroll
-                            for (int pt = 0; pt < C::parts; ++pt) mma16816(o[grp * 16 + 4 * i + k], a[pt], b0[k], b1[k]);
-                    }
-                }
-            }
-        }
+        if (!info->bad) rows.page(p, ring + stage * C::rec, info->page, qs, lane);
         if (++stage == C::stages) {
             stage = 0;
             parity ^= 1u;
@@ -497,6 +513,104 @@ __global__ void __launch_bounds__(AttCfg<D, F32>::threads, 1) attend_kernel(cons
         const bool split = open && now.begin >= begin;
         work.split[range] = split ? AttSplit{now.b, now.rt, now.h, (now.begin + now.count - 1) / per, min(R, att_row(p, now.b).n * G - now.rt * R)} : AttSplit{0, 0, 0, -1};
     }
+}
+
+// A CTA per item, for contexts so short that its warps alone read them in the time that a second launch takes:
+// warp w has every C::warps-th page from w on, and the CTA joins the warps' parts and writes all of the item's rows.
+template <int D, bool F32>
+__global__ void __launch_bounds__(AttCfg<D, F32>::threads, 1) attend_items_kernel(const AttendArgs p, int tiles, int items) {
+    using C = AttCfg<D, F32>;
+    constexpr int R = C::R;
+    extern __shared__ __align__(128) uint8_t sm[];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint8_t *const mine = sm + warp * C::warp_bytes;
+    const uint32_t ring = smem_u32(mine), qs = ring + C::ring, bars = qs + C::qbytes;
+    if (lane == 0) {
+        for (int i = 0; i < C::stages; ++i) mbar_init(bars + 8 * i, 1);
+        fence_mbar_init();
+    }
+    __syncwarp();
+    uint32_t seq = 0;  // copies so far: stage seq % stages, its parity (seq / stages) % 2
+    bool failed = false;
+    for (int x = blockIdx.x; x < items; x += gridDim.x) {
+        const int h = x % p.Hk, bt = x / p.Hk, rt = bt % tiles, b = bt / tiles;
+        const AttRow w = att_row(p, b);
+        const AttItem it = att_item(p, w, rt, R);
+        const int n = failed || it.pages <= warp ? 0 : (it.pages - warp + C::warps - 1) / C::warps;  // pages of this warp, 32 at most
+        int64_t slot = -1;  // lane = one of them
+        if (lane < n) slot = cache_page(p.pages[(int64_t)b * p.table + it.first + warp + C::warps * lane], p.num_pages);
+        const unsigned bad = __ballot_sync(kFull, lane < n && slot < 0);
+        auto fetch = [&](int k) {
+            if (lane == k) {
+                const uint32_t s = (seq + k) % C::stages, bar = bars + 8 * s;
+                fence_proxy_async_smem();
+                if (slot < 0) {
+                    atomicOr(p.status, kDevBadSlot);
+                    mbar_arrive_expect_tx(bar, 0);
+                } else {
+                    mbar_arrive_expect_tx(bar, C::rec);
+                    bulk_g2s(ring + s * C::rec, p.pool + (slot * p.Hk + h) * C::rec, C::rec, bar);
+                }
+            }
+        };
+        for (int k = 0; k < min(n, C::stages); ++k) fetch(k);
+        AttRows<D, F32> rows;
+        if (n) rows.start(p, w, b, rt, h, qs, lane);
+        for (int k = 0; k < n; ++k) {
+            const uint32_t s = (seq + k) % C::stages;
+            if (!mbar_wait_bounded(bars + 8 * s, ((seq + k) / C::stages) & 1)) failed = true;
+            if (__any_sync(kFull, failed)) {
+                failed = true;
+                for (int y = k + 1; y < min(n, k + C::stages); ++y)  // the other copies in flight
+                    mbar_wait_bounded(bars + 8 * ((seq + y) % C::stages), ((seq + y) / C::stages) & 1);
+                break;
+            }
+            if (!((bad >> k) & 1)) rows.page(p, ring + s * C::rec, it.first + warp + C::warps * k, qs, lane);
+            __syncwarp();
+            if (k + C::stages < n) fetch(k + C::stages);
+        }
+        seq += n;
+        static_assert(R * (D + 2) * 4 <= C::ring, "parts");
+        if (n) rows.leave(p, b, rt, h, false, reinterpret_cast<float *>(mine), reinterpret_cast<float2 *>(mine + R * D * 4), lane);
+        __syncthreads();
+        const int parts = min(C::warps, it.pages);
+        for (int i = threadIdx.x; i < R * (D / 4); i += C::threads) {
+            const int r = i / (D / 4), col = 4 * (i - r * (D / 4)), row = rt * R + r, t = att_div(p, row);
+            if (t >= p.T) break;
+            float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (t < w.n) {
+                float M = -INFINITY, L = 0.f;
+#pragma unroll
+                for (int k = 0; k < C::warps; ++k)
+                    if (k < parts) M = fmaxf(M, reinterpret_cast<const float2 *>(sm + k * C::warp_bytes + R * D * 4)[r].x);
+                const float mu = M == -INFINITY ? 0.f : M;
+#pragma unroll
+                for (int k = 0; k < C::warps; ++k) {
+                    if (k < parts) {
+                        const float2 ml = reinterpret_cast<const float2 *>(sm + k * C::warp_bytes + R * D * 4)[r];
+                        const float f = ex2(ml.x - mu);
+                        L = fmaf(ml.y, f, L);
+                        const float4 z = *reinterpret_cast<const float4 *>(sm + k * C::warp_bytes + (r * D + col) * 4);
+                        y.x = fmaf(z.x, f, y.x), y.y = fmaf(z.y, f, y.y), y.z = fmaf(z.z, f, y.z), y.w = fmaf(z.w, f, y.w);
+                    }
+                }
+                const float u = L == 0.f ? 0.f : 1.f / L;
+                y.x *= u, y.y *= u, y.z *= u, y.w *= u;
+            }
+            const int64_t to = (((int64_t)b * p.T + t) * p.H + h * p.group + (row - t * p.group)) * D + col;
+            if (F32) {
+                *reinterpret_cast<float4 *>(static_cast<float *>(p.o) + to) = y;
+            } else {
+                uint2 z;
+                const __nv_bfloat162 lo = __floats2bfloat162_rn(y.x, y.y), hi = __floats2bfloat162_rn(y.z, y.w);
+                memcpy(&z.x, &lo, 4);
+                memcpy(&z.y, &hi, 4);
+                *reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(p.o) + to) = z;
+            }
+        }
+        __syncthreads();  // the parts are read before the rings take copies again
+    }
+    if (failed && lane == 0) atomicOr(p.status, kDevWaitTimeout);
 }
 
 // Clears the outputs of queries that see no token or are none: block i, `slice` queries of a row.
@@ -667,6 +781,8 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(const AttendA
     }
 }
 
+int64_t att_items(const AttendArgs &a, int R) { return (int64_t)a.batch * (((int64_t)a.T * (a.H / a.Hk) + R - 1) / R) * a.Hk; }
+
 // The second launch of a call, enqueued while the first runs.
 template <int D, bool BF>
 cudaError_t launch_join(const AttendArgs &a, int R, int ranges, cudaStream_t s) {
@@ -689,16 +805,34 @@ cudaError_t launch_join(const AttendArgs &a, int R, int ranges, cudaStream_t s) 
         }
     // few items may have many parts: a CTA per row (a context of 131071 tokens, 8 items of 4 rows: 10.2 us against 12.3
     // with a CTA per item; 2048 items: 25 against 9.6)
-    const int64_t items = (int64_t)a.batch * (((int64_t)a.T * (a.H / a.Hk) + R - 1) / R) * a.Hk;
+    const int64_t items = att_items(a, R);
     int wpr = kWarps;
     if (items * rows > 4 * (int64_t)sm_count())
         while (wpr > 1 && wpr * rows > kWarps) wpr /= 2;
     cfg.gridDim = dim3((unsigned)(ranges + clear), (unsigned)((rows * wpr + kWarps - 1) / kWarps));
     return cudaLaunchKernelEx(&cfg, attend_join_kernel<D, BF>, a, ranges, wpr, slice);
 }
+// Whether an item is a CTA's: two items per SM at most, of 8 pages per warp at most.  On the GPU alone (8 KV heads,
+// d = 128): 16 rows of 1000 tokens 10.9 us against 17.5 by ranges, of 2000 16.0 against 23.1; one row of 500 7.6 against
+// 11.3, of 1000 10.2 against 11.8, of 2000 15.5 against 12.8, of 4000 25.5 against 12.9; 60 rows of 1000 (480 items) 42
+// against 33.  2 KV heads, d = 256 (4 warps): 8 rows of 2000 28.7 against 21.1.  It saves the host a launch too.
+constexpr int kItemWarpPages = 8;
+bool att_by_items(const AttendArgs &a) {
+    return a.table <= kItemWarpPages * (a.d == 256 ? 4 : 8) && att_items(a, 16) <= 2 * (int64_t)sm_count();
+}
+
 template <int D, bool F32>
 cudaError_t launch_as(const AttendArgs &a, cudaStream_t s) {
     using C = AttCfg<D, F32>;
+    static_assert(kItemWarpPages <= 32 && (C::warps == 4) == (D == 256), "a page per lane");
+    if (att_by_items(a)) {
+        const int smem = C::warps * C::warp_bytes;
+        const cudaError_t e = ensure_smem_limit(reinterpret_cast<const void *>(attend_items_kernel<D, F32>), smem);
+        if (e != cudaSuccess) return e;
+        const int items = (int)att_items(a, C::R);
+        attend_items_kernel<D, F32><<<std::min(items, sm_count()), C::threads, smem, s>>>(a, (int)(items / a.Hk / a.batch), items);
+        return cudaGetLastError();
+    }
     const int smem = C::warps * C::warp_bytes + (a.batch + 1) * 4;
     cudaError_t e = ensure_smem_limit(reinterpret_cast<const void *>(attend_kernel<D, F32>), smem);
     if (e != cudaSuccess) return e;
@@ -720,6 +854,7 @@ cudaError_t launch_d(const AttendArgs &a, cudaStream_t s) {
 
 int64_t attend_workspace(const AttendArgs &a) {
     const bool tc = attend_tc_takes(a);
+    if (!tc && att_by_items(a)) return 0;
     return att_work_bytes(sm_count() * (tc ? 1 : a.d == 256 ? 4 : 8), tc ? attend_tc_rows(a) : 16, a.d);
 }
 

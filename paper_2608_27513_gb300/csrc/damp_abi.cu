@@ -841,14 +841,16 @@ damp_status damp_cache_read(const damp_cache_layout *layout, const void *cache, 
     return launch_cache_read(a, static_cast<cudaStream_t>(stream)) == cudaSuccess ? DAMP_OK : DAMP_ERR_CUDA;
 }
 
-int64_t damp_cache_attend_workspace(const damp_cache_layout *layout, int32_t batch, int32_t T, int32_t dtype) {
-    if (check_cache(layout) != DAMP_OK || batch < 1 || batch > kCacheMaxBatch || T < 1) return 0;
+int64_t damp_cache_attend_workspace(const damp_cache_layout *layout, int32_t batch, int32_t T, int32_t table,
+                                    int32_t dtype) {
+    if (check_cache(layout) != DAMP_OK || batch < 1 || batch > kCacheMaxBatch || T < 1 || table < 1) return 0;
     AttendArgs a{};
     a.H = layout->num_heads;
     a.Hk = layout->num_kv_heads;
     a.d = layout->d;
     a.batch = batch;
     a.T = T;
+    a.table = table;
     a.in_bf16 = dtype == DAMP_IN_BF16;
     return attend_workspace(a);
 }
@@ -875,13 +877,15 @@ damp_status damp_cache_attend(const damp_cache_layout *layout, const void *cache
     a.d = c.d;
     a.batch = batch;
     a.T = T;
+    a.table = table;
     a.in_bf16 = c.in_bf16;
-    if (workspace_bytes < attend_workspace(a)) return DAMP_ERR_SHAPE;
-    if (!cache || !pages || !lengths || !q || !o || !workspace) return DAMP_ERR_NULL;
+    const int64_t need = attend_workspace(a);
+    if (workspace_bytes < need) return DAMP_ERR_SHAPE;
+    if (!cache || !pages || !lengths || !q || !o || (need && !workspace)) return DAMP_ERR_NULL;
     if (!aligned(cache, 16) || !aligned(pages, 4) || !aligned(lengths, 4) || !aligned(q_lengths, 4) || !aligned(q, 16) ||
         !aligned(o, 16) || !aligned(workspace, 16))
         return DAMP_ERR_ALIGN;
-    const Range ro = range_of(o, n * row * es), rw = range_of(workspace, workspace_bytes);
+    const Range ro = range_of(o, n * row * es), rw = range_of(workspace, workspace ? workspace_bytes : 0);
     const Range inputs[] = {pool, lists, range_of(lengths, (int64_t)batch * 4), range_of(q_lengths, q_lengths ? (int64_t)batch * 4 : 0),
                             range_of(q, ((n - 1) * q_stride + row) * es)};
     if (overlap(ro, rw)) return DAMP_ERR_ALIAS;
@@ -890,7 +894,6 @@ damp_status damp_cache_attend(const damp_cache_layout *layout, const void *cache
     a.pool = c.pool;
     a.num_pages = num_pages;
     a.pages = pages;
-    a.table = table;
     a.lengths = lengths;
     a.q_lengths = q_lengths;
     a.q = q;

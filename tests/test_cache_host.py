@@ -81,11 +81,11 @@ def test_cache_rejects_bad_arguments(L, fb):
         a.update(over)
         return L.damp_cache_read(*a.values())
 
-    need = L.damp_cache_attend_workspace(layout(), 3, 5, 0)
+    need = L.damp_cache_attend_workspace(layout(), 3, 5, 200, 0)
     assert need > 0 and need <= 1 << 22
 
     def attend(**over):
-        a = dict(base, lengths=_p(fb, 2), q_lengths=None, q=_p(fb, 3), q_stride=256, scale=0.125, window=0, o=_p(fb, 4), dtype=0,
+        a = dict(base, table=200, lengths=_p(fb, 2), q_lengths=None, q=_p(fb, 3), q_stride=256, scale=0.125, window=0, o=_p(fb, 4), dtype=0,
                  ws=_p(fb, 5), ws_bytes=need, stream=None)
         a.update(over)
         return L.damp_cache_attend(*a.values())
@@ -126,8 +126,12 @@ def test_cache_rejects_bad_arguments(L, fb):
         assert attend(**{name: _p(fb, i, 8)}) == ALIGN
     for over in (dict(o=_p(fb, 3)), dict(o=_p(fb, 0)), dict(o=_p(fb, 5, 16)), dict(ws=_p(fb, 0)), dict(q_lengths=_p(fb, 4)), dict(ws=_p(fb, 2))):
         assert attend(**over) == ALIAS, over
-    for a in ((None, 3, 5, 0), (layout(4, 3, 64), 3, 5, 0), (layout(), 0, 5, 0), (layout(), 3, 0, 0), (layout(), 4097, 1, 0)):
+    for a in ((None, 3, 5, 200, 0), (layout(4, 3, 64), 3, 5, 200, 0), (layout(), 0, 5, 200, 0), (layout(), 3, 0, 200, 0), (layout(), 4097, 1, 200, 0),
+              (layout(), 3, 5, 0, 0)):
         assert L.damp_cache_attend_workspace(*a) == 0
+    # few rows of short tables need none
+    assert L.damp_cache_attend_workspace(layout(), 1, 1, 4, 0) == 0
+    assert attend(batch=0, ws=None, ws_bytes=0) == OK
 
 
 def test_binding_rejects_bad_tensors(L):

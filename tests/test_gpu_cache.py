@@ -244,9 +244,14 @@ def test_bad_pages_and_tokens():
 # ---- attention ----
 
 def run_attend(layout, pool, pages, q, lengths, what, **more):
-    o = damp.cache_attend(layout, pool, q, pages, i32(lengths), **{n: i32(x) if n == "q_lengths" and x is not None else x for n, x in more.items()})
+    """Against the reference, with the table as it is (a CTA per item where it is short) and with a long one, most of
+    whose entries hold no token (the work cut into ranges)."""
     want, bounds = R.attend(R.Cache(pool, layout.d), q, pages.cpu(), lengths, **more)
-    R.check_attend(o, want, bounds, int(max(lengths)), layout.d, what)
+    kw = {n: i32(x) if n == "q_lengths" and x is not None else x for n, x in more.items()}
+    wide = torch.cat((pages, torch.full((pages.shape[0], 70), -1, dtype=torch.int32, device=DEV)), 1)
+    for table in (pages, wide):
+        o = damp.cache_attend(layout, pool, q, table, i32(lengths), **kw)
+        R.check_attend(o, want, bounds, int(max(lengths)), layout.d, what)
     return o
 
 
