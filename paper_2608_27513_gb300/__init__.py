@@ -745,6 +745,9 @@ def verify_drafts(target_logits, draft_tokens, u, noise, draft_logits=None, temp
     return tokens, count
 
 
+_cache_layouts = {}
+
+
 @dataclass(frozen=True)
 class CacheLayout:
     """damp_cache_layout: query heads, KV heads (a divisor of them) and the head dimension (64, 128 or
@@ -754,14 +757,17 @@ class CacheLayout:
     d: int
 
     def __post_init__(self):
-        # what every call needs of the layout, made once
-        c = DampCacheLayout(self.num_heads, self.num_kv_heads, self.d)
-        object.__setattr__(self, "_c", c)
-        object.__setattr__(self, "_ref", ctypes.byref(c))
-        object.__setattr__(self, "_workspace", {})
+        # what every call needs of the layout, made once for equal ones: the struct, a reference to it, and the
+        # sizes of the workspaces by device, batch, tokens, table and type
+        key = (self.num_heads, self.num_kv_heads, self.d)
+        shared = _cache_layouts.get(key)
+        if shared is None:
+            c = DampCacheLayout(*key)
+            shared = _cache_layouts[key] = (c, ctypes.byref(c), {})
+        object.__setattr__(self, "_shared", shared)
 
     def c(self) -> DampCacheLayout:
-        return self._c
+        return self._shared[0]
 
     @property
     def record_bytes(self) -> int:
@@ -771,7 +777,7 @@ class CacheLayout:
 
 def cache_page_bytes(layout: CacheLayout) -> int:
     """Bytes of a page, all KV heads; 0 if the layout is invalid."""
-    return int(lib().damp_cache_page_bytes(layout._ref))
+    return int(lib().damp_cache_page_bytes(layout._shared[1]))
 
 
 def new_cache(layout: CacheLayout, num_pages: int, device="cuda"):
@@ -949,7 +955,7 @@ def cache_append(layout, cache, k, v, pages, start, lengths=None, stream=None):
     kp, ks = _token_rows("k", k, shape, dtype, dev)
     vp, vs = _token_rows("v", v, shape, dtype, dev)
     pool, n, table, W = _cache(layout, cache, pages, B, dev, i32, torch.uint8)
-    status = lib().damp_cache_append(layout._ref, pool, n, table, W, B, T, _here("start", start, (B,), i32, dev),
+    status = lib().damp_cache_append(layout._shared[1], pool, n, table, W, B, T, _here("start", start, (B,), i32, dev),
                                      None if lengths is None else _here("lengths", lengths, (B,), i32, dev), kp, ks, vp, vs,
                                      IN_BF16 if dtype == torch.bfloat16 else IN_FP32, _raw_stream(torch, stream, dev))
     if status:
@@ -981,7 +987,7 @@ def cache_read(layout, cache, pages, lengths, tokens, start=None, dtype=None, k=
     if v is None:
         v = _output(torch, k, True, stream)
     vp = _here("v", v, shape, dtype, dev)
-    status = lib().damp_cache_read(layout._ref, pool, n, table, W, B, T, None if start is None else _here("start", start, (B,), i32, dev),
+    status = lib().damp_cache_read(layout._shared[1], pool, n, table, W, B, T, None if start is None else _here("start", start, (B,), i32, dev),
                                    held, kp, vp, IN_BF16 if dtype == torch.bfloat16 else IN_FP32, _raw_stream(torch, stream, dev))
     if status:
         raise DampError(status, "damp_cache_read")
@@ -1013,13 +1019,14 @@ def cache_attend(layout, cache, q, pages, lengths, q_lengths=None, scale=None, w
     else:
         op = _here("o", o, shape, dtype, dev)
     L = lib()
-    need = layout._workspace.get((dev, B, T, W, dt))
+    sizes = layout._shared[2]
+    need = sizes.get((dev, B, T, W, dt))
     if need is None:
-        need = layout._workspace[dev, B, T, W, dt] = L.damp_cache_attend_workspace(layout._ref, B, T, W, dt)
+        need = sizes[dev, B, T, W, dt] = L.damp_cache_attend_workspace(layout._shared[1], B, T, W, dt)
     ws = None
     if need:
         ws = q.new_empty(need // (4 if dt else 2)) if stream is None else _new((need,), torch.uint8, q, stream)
-    status = L.damp_cache_attend(layout._ref, pool, n, table, W, B, T, held,
+    status = L.damp_cache_attend(layout._shared[1], pool, n, table, W, B, T, held,
                                  None if q_lengths is None else _here("q_lengths", q_lengths, (B,), i32, dev), qp, qs,
                                  d ** -0.5 if scale is None else scale, 0 if window is None else min(window, 0x7fffffff), op, dt,
                                  None if ws is None else ws.data_ptr(), need, _raw_stream(torch, stream, dev))

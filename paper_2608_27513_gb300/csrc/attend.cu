@@ -613,20 +613,6 @@ __global__ void __launch_bounds__(AttCfg<D, F32>::threads, 1) attend_items_kerne
     if (failed && lane == 0) atomicOr(p.status, kDevWaitTimeout);
 }
 
-// Clears the outputs of queries that see no token or are none: block i, `slice` queries of a row.
-template <int D, bool BF>
-__device__ __forceinline__ void att_clear(const AttendArgs &p, int i, int slice) {
-    const int slices = (p.T + slice - 1) / slice, b = i / slices;
-    const AttRow w = att_row(p, b);
-    const int t0 = (i - b * slices) * slice, t1 = min(p.T, t0 + slice);
-    const int64_t token = (int64_t)p.H * D / (BF ? 8 : 4);  // 16 bytes at a time
-    for (int side = 0; side < 2; ++side) {  // before the first token, after the last query
-        const int lo = side ? max(t0, w.n) : t0, hi = side ? t1 : min(t1, w.n - w.len);
-        uint4 *const o = static_cast<uint4 *>(p.o) + ((int64_t)b * p.T + lo) * token;
-        for (int64_t k = threadIdx.x; k < (hi - lo) * token; k += kJoinThreads) o[k] = make_uint4(0, 0, 0, 0);
-    }
-}
-
 // Joins the parts of items that several ranges hold, blockIdx.x: the range that the item starts in; the blocks
 // after those clear.  Items of many rows have few parts each: a thread per row and 4 columns.
 template <int D>
@@ -788,7 +774,7 @@ template <int D, bool BF>
 cudaError_t launch_join(const AttendArgs &a, int R, int ranges, cudaStream_t s) {
     constexpr int kWarps = kJoinThreads / 32;
     const int64_t rows = std::min<int64_t>(R, (int64_t)a.T * (a.H / a.Hk));
-    const int slice = (int)std::max<int64_t>(1, (256 << 10) / ((int64_t)a.H * a.d * (BF ? 2 : 4)));
+    const int slice = att_clear_slice(a.H, D, BF ? 2 : 4);
     const int64_t clear = (int64_t)a.batch * ((a.T + slice - 1) / slice);
     cudaLaunchConfig_t cfg{};
     cfg.blockDim = dim3(kJoinThreads);
@@ -845,7 +831,7 @@ template <int D>
 cudaError_t launch_d(const AttendArgs &a, cudaStream_t s) {
     if (attend_tc_takes(a)) {
         const cudaError_t e = launch_attend_tc(a, sm_count(), s);
-        return e != cudaSuccess ? e : launch_join<D, true>(a, attend_tc_rows(a), sm_count(), s);
+        return e != cudaSuccess || attend_tc_whole(a) ? e : launch_join<D, true>(a, attend_tc_rows(a), sm_count(), s);
     }
     return a.in_bf16 ? launch_as<D, false>(a, s) : launch_as<D, true>(a, s);
 }
@@ -854,7 +840,7 @@ cudaError_t launch_d(const AttendArgs &a, cudaStream_t s) {
 
 int64_t attend_workspace(const AttendArgs &a) {
     const bool tc = attend_tc_takes(a);
-    if (!tc && att_by_items(a)) return 0;
+    if (tc ? attend_tc_whole(a) : att_by_items(a)) return 0;
     return att_work_bytes(sm_count() * (tc ? 1 : a.d == 256 ? 4 : 8), tc ? attend_tc_rows(a) : 16, a.d);
 }
 

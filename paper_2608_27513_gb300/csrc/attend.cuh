@@ -138,9 +138,29 @@ __device__ inline void att_count(const AttendArgs &p, int R, int unit, int32_t *
     __syncthreads();
 }
 
+// Clears the outputs of queries that see no token or are none: block i, `slice` queries of a row.
+template <int D, bool BF>
+__device__ __forceinline__ void att_clear(const AttendArgs &p, int i, int slice) {
+    const int slices = (p.T + slice - 1) / slice, b = i / slices;
+    const AttRow w = att_row(p, b);
+    const int t0 = (i - b * slices) * slice, t1 = min(p.T, t0 + slice);
+    const int64_t token = (int64_t)p.H * D / (BF ? 8 : 4);  // 16 bytes at a time
+    for (int side = 0; side < 2; ++side) {  // before the first token, after the last query
+        const int lo = side ? max(t0, w.n) : t0, hi = side ? t1 : min(t1, w.n - w.len);
+        uint4 *const o = static_cast<uint4 *>(p.o) + ((int64_t)b * p.T + lo) * token;
+        for (int64_t k = threadIdx.x; k < (hi - lo) * token; k += blockDim.x) o[k] = make_uint4(0, 0, 0, 0);
+    }
+}
+// queries of a block that clears: 256 KB of outputs
+__host__ __device__ inline int att_clear_slice(int H, int D, int es) {
+    const int n = (256 << 10) / (H * D * es);
+    return n < 1 ? 1 : n;
+}
+
 // the products of prompts and drafts on the tensor cores (attend_tc.cu)
 bool attend_tc_takes(const AttendArgs &a);
 int attend_tc_rows(const AttendArgs &a);  // of an item
+bool attend_tc_whole(const AttendArgs &a);  // no item is split, one launch
 cudaError_t launch_attend_tc(AttendArgs a, int grid, cudaStream_t s);
 
 }  // namespace damp

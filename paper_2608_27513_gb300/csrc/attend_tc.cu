@@ -279,9 +279,21 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
     const uint32_t tmem = s_tmem;
     const AttWork work = att_work(p.workspace, gridDim.x, R);
     const int total = before[p.batch] * p.Hk, per = att_per(total, gridDim.x);
-    const int end = (int)min((int64_t)total, ((int64_t)blockIdx.x + 1) * per);
-    const int begin = (int)min((int64_t)end, (int64_t)blockIdx.x * per);
+    int end = (int)min((int64_t)total, ((int64_t)blockIdx.x + 1) * per);
+    int begin = (int)min((int64_t)end, (int64_t)blockIdx.x * per);
     AtItem it{};
+    if (p.whole) {  // the range takes the items that start in it, all of them
+        if (end < total) {
+            it = at_seek(p, before, end, R, PG);
+            if (it.begin < end) end = it.begin + it.tiles;
+        }
+        if (begin < total && begin > 0) {
+            it = at_seek(p, before, begin, R, PG);
+            if (it.begin < begin) begin = it.begin + it.tiles;
+        }
+        const int slice = att_clear_slice(p.H, D, 2), blocks = p.batch * ((p.T + slice - 1) / slice);
+        for (int i = blockIdx.x; i < blocks; i += gridDim.x) att_clear<D, true>(p, i, slice);
+    }
     if (begin < end) it = at_seek(p, before, begin, R, PG);
     __syncthreads();  // `before` is given up
     const AtWait wait{&s_dead};
@@ -729,7 +741,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
             for (int i = 0; i < 1000; ++i) __nanosleep(1000);
         }
     }
-    if (threadIdx.x == 0) work.split[blockIdx.x] = split;  // (a range starts one such item at most, its last)
+    if (threadIdx.x == 0 && !p.whole) work.split[blockIdx.x] = split;  // (a range starts one such item at most, its last)
     __syncwarp();
     tc_fence_before();
     __syncthreads();
@@ -755,7 +767,16 @@ bool attend_tc_takes(const AttendArgs &a) { return a.in_bf16 && (int64_t)a.T * (
 
 int attend_tc_rows(const AttendArgs &a) { return a.d <= 128 && (int64_t)a.T * (a.H / a.Hk) > 128 ? 256 : 128; }
 
+// Ranges end with items where that leaves them even (8 items per SM) or items are short (4 key tiles): no parts,
+// one launch.
+bool attend_tc_whole(const AttendArgs &a) {
+    const int64_t G = a.H / a.Hk, R = attend_tc_rows(a), items = (int64_t)a.batch * (((int64_t)a.T * G + R - 1) / R) * a.Hk;
+    const int tile = a.d == 256 ? 2 : 4;  // pages
+    return (a.table + tile - 1) / tile <= 4 || items >= 8 * (int64_t)sm_count();
+}
+
 cudaError_t launch_attend_tc(AttendArgs a, int grid, cudaStream_t s) {
+    a.whole = attend_tc_whole(a);
     static std::atomic<uint32_t *> cache[64];
     const cudaError_t e = symbol_address_cached(&g_status_attend_tc, cache, &a.status);
     if (e != cudaSuccess) return e;

@@ -136,6 +136,7 @@ struct AttendArgs {
     int32_t window;   // 0: none
     int32_t group;    // H / Hk, and ceil(2^32 / group) to divide by it (set by the launcher)
     uint32_t by_group;
+    int32_t whole;    // ranges end with items (set by the launcher)
     void *o;
     int32_t in_bf16;
     uint8_t *workspace;

@@ -294,6 +294,18 @@ def test_attend_many_items(H, Hk, d, window):
     run_attend(layout, pool, pages, q[:, :4].to(BF).contiguous(), n, "many drafts", window=window)
 
 
+def test_attend_very_many_items():
+    """So many items that ranges end with items though the table is long."""
+    layout = damp.CacheLayout(16, 8, 64)
+    B = 170
+    pool, some = filled(layout, 10, 3, 4)
+    pages = some[torch.arange(B, device=DEV) % 10].contiguous()  # rows that share their pages
+    g = gen(8)
+    q = randn(g, B, 40, 16, 64, dtype=BF)
+    n, new = torch.randint(0, 97, (B,)).tolist(), torch.randint(0, 41, (B,)).tolist()
+    run_attend(layout, pool, pages, q, n, "very many items", q_lengths=new)
+
+
 @pytest.mark.parametrize("H,T", [(65, 1), (65, 3), (67, 9), (200, 2), (3, 50)])
 def test_attend_groups(H, T):
     """Groups of query heads that are no powers of two, one KV head."""
