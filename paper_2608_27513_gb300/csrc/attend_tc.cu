@@ -34,7 +34,7 @@ namespace {
 constexpr int kAtThreads = 15 * 32;
 constexpr uint32_t kAtCols = 512;
 constexpr uint32_t kAtO = 256;  // S blocks at columns 0 and 128, O from here on
-constexpr float kAtLag = 4.f;
+constexpr float kAtLag = 5.9f;  // 2^15.9 is below the largest FP16
 constexpr int kAtNotes = 8;
 constexpr int kAtMaxPages = 4;  // of a key tile
 
@@ -59,7 +59,7 @@ struct AtSmem {
     static constexpr int kc = v + buffers * tile, vc = kc + stages * codes;
     static constexpr int note = vc + stages * codes;
     static constexpr int bar = note + kAtNotes * (int)sizeof(AtNote);
-    static constexpr int bytes = bar + 384;
+    static constexpr int bytes = bar + 448;
     static constexpr int before = k;  // until the roles begin
     static_assert(SUB * q_tile + 4 * (kCacheMaxBatch + 1) <= kc, "before");
     static constexpr int sm_warps = 4 * SUB, turn_warps = 4;  // SUB = 1: four for K, four for V
@@ -67,8 +67,8 @@ struct AtSmem {
 // mbarriers
 enum { kBarQ = 0, kBarDone = 2, kBarKFull = 4, kBarKFree = 6, kBarVFull = 8, kBarVFree = 10, kBarS = 12, kBarP = 14, kBarPV = 18, kBarTurn = 19, kBarNote = 21,  // P: halves of two buffers
       
-       kBarKcFull = kBarNote + kAtNotes, kBarKcFree = kBarKcFull + 4, kBarVcFull = kBarKcFree + 4, kBarVcFree = kBarVcFull + 4, kBarCount = kBarVcFree + 4 };
-static_assert(kBarCount * 8 <= 384, "barriers");
+       kBarKcFull = kBarNote + kAtNotes, kBarKcFree = kBarKcFull + 4, kBarVcFull = kBarKcFree + 4, kBarVcFree = kBarVcFull + 4, kBarRows = kBarVcFree + 4, kBarCount = kBarRows + 8 };
+static_assert(kBarCount * 8 <= 448, "barriers");
 
 // instruction descriptor: f16 x f16 -> FP32, M = 128, N columns, B MN-major if set
 __host__ __device__ constexpr uint32_t at_idesc(int n, bool b_mn) {
@@ -259,6 +259,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
             mbar_init(bar(kBarP + 2 * i + 1), 4);
         }
         mbar_init(bar(kBarPV), 1);
+        for (int i = 0; i < M::sm_warps; ++i) mbar_init(bar(kBarRows + i), 1);
         for (int i = 0; i < kAtNotes; ++i) mbar_init(bar(kBarNote + i), 1);
         for (int i = 0; i < M::stages; ++i) {
             mbar_init(bar(kBarKcFull + i), 1);
@@ -325,18 +326,14 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
             float factor = 0.f;
             {  // q: copied as it is to where its rows go, then scaled by a power of two to below 2^15, 8 rows at a time
                 const int64_t mine = live ? ((int64_t)it.b * p.T + t) * p.q_stride + (int64_t)head * D : -1;
-#pragma unroll 1
-                for (int g = 0; g < 4; ++g) {
-                    const int64_t src = __shfl_sync(kFull, mine, 8 * g + (lane & 7));
-                    const __nv_bfloat16 *const q = static_cast<const __nv_bfloat16 *>(p.q) + src + 8 * (lane >> 3);
-#pragma unroll
-                    for (int i = 0; i < kC; ++i) {
-                        const uint32_t to = stage + g * (16 * D) + i * 512;
-                        if (src >= 0) cp_async16(to, q + 32 * i);
-                        else sts128(to, make_uint4(0, 0, 0, 0));
-                    }
+                const uint32_t q_bar = bar(kBarRows + warp), rows = sb + M::q + x * M::q_tile + (warp & 3) * (64 * D);
+                const unsigned some = __ballot_sync(kFull, live);
+                if (lane == 0) mbar_arrive_expect_tx(q_bar, __popc(some) * 2 * D);
+                __syncwarp();
+                if (live) {
+                    fence_proxy_async_smem();  // (the item before was staged here)
+                    bulk_g2s(rows + lane * 2 * D, static_cast<const __nv_bfloat16 *>(p.q) + mine, 2 * D, q_bar);
                 }
-                cp_async_commit();
                 if (last < end) {  // the next item is found and its queries brought into L2 meanwhile
                     AtItem next = it;
                     at_next(next, p, R, PG);
@@ -350,12 +347,21 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
                         for (int i = 0; i < D; i += 64) asm volatile("prefetch.global.L2 [%0];" ::"l"(q + i));
                     }
                 }
-                cp_async_wait_all();
+                ok = together(wait(q_bar, items & 1));
+                if (!ok) break;
 #pragma unroll 1
                 for (int g = 0; g < 4; ++g) {
+                    // From rows to core matrices in the same 16 D bytes.  Lane = (row j, b = 4 i + its quarter): chunk
+                    // (b & ~7) | ((b + j) & 7), so that eight lanes touch eight 16-byte columns on either side.
                     uint4 v[kC];
+                    const int j = lane & 7;
+                    const bool there = (some >> (8 * g + j)) & 1;
 #pragma unroll
-                    for (int i = 0; i < kC; ++i) v[i] = lds128(stage + g * (16 * D) + i * 512);
+                    for (int i = 0; i < kC; ++i) {
+                        const int b = 4 * i + (lane >> 3), chunk = (b & ~7) | ((b + j) & 7);
+                        v[i] = there ? lds128(rows + (8 * g + j) * 2 * D + chunk * 16) : make_uint4(0, 0, 0, 0);
+                    }
+                    __syncwarp();
                     uint32_t top = 0;  // largest magnitudes of both halves of the words
 #pragma unroll
                     for (int i = 0; i < kC; ++i)
@@ -372,7 +378,8 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
 #pragma unroll
                         for (int k = 0; k < 4; ++k)
                             h[k] = half_pair(__uint_as_float(u[k] << 16) * up, __uint_as_float(u[k] & 0xffff0000u) * up);
-                        sts128(stage + g * (16 * D) + i * 512, make_uint4(h[0], h[1], h[2], h[3]));
+                        const int b = 4 * i + (lane >> 3), chunk = (b & ~7) | ((b + j) & 7);
+                        sts128(rows + g * (16 * D) + chunk * 128 + j * 16, make_uint4(h[0], h[1], h[2], h[3]));
                     }
                 }
             }
@@ -523,15 +530,30 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
                     }
                 }
                 __syncwarp();
+                // core matrices to rows, as the queries came, and the rows out
+                const uint32_t rows = sb + M::q + x * M::q_tile + (warp & 3) * (64 * D);
 #pragma unroll 1
                 for (int g = 0; g < 4; ++g) {
-                    const int64_t dst = __shfl_sync(kFull, mine, 8 * g + (lane & 7));
-                    __nv_bfloat16 *const o = static_cast<__nv_bfloat16 *>(p.o) + dst + 8 * (lane >> 3);
+                    uint4 v[kC];
+                    const int j = lane & 7;
 #pragma unroll
-                    for (int i = 0; i < D / 32; ++i) {
-                        const uint4 w = lds128(stage + g * (16 * D) + i * 512);
-                        if (dst >= 0) stg128(o + 32 * i, w);
+                    for (int i = 0; i < kC; ++i) {
+                        const int b = 4 * i + (lane >> 3), chunk = (b & ~7) | ((b + j) & 7);
+                        v[i] = lds128(rows + g * (16 * D) + chunk * 128 + j * 16);
                     }
+                    __syncwarp();
+#pragma unroll
+                    for (int i = 0; i < kC; ++i) {
+                        const int b = 4 * i + (lane >> 3), chunk = (b & ~7) | ((b + j) & 7);
+                        sts128(rows + (8 * g + j) * 2 * D + chunk * 16, v[i]);
+                    }
+                }
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (live) {
+                    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(static_cast<__nv_bfloat16 *>(p.o) + mine), "r"(rows + lane * 2 * D), "r"(2 * D) : "memory");
+                    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                    asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
                 }
                 __syncwarp();
             } else {
