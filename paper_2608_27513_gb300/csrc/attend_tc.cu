@@ -455,13 +455,17 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
                         tc_fence_after();
                     }
 #pragma unroll 1
-                    for (int c = 0; c < D / 16; ++c) {
-                        uint32_t y[16];
-                        at_ld16(o_at + 16 * c, y);
-                        at_ld_wait(y);
+                    for (int c = 0; c < D / 32; ++c) {
+                        uint32_t y[2][16];
+                        at_ld16(o_at + 32 * c, y[0]);
+                        at_ld16(o_at + 32 * c + 16, y[1]);
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) y[j] = __float_as_uint(__uint_as_float(y[j]) * corr);
-                        at_st16(o_at + 16 * c, y);
+                        for (int k = 0; k < 2; ++k) {
+                            at_ld_wait(y[k]);
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) y[k][j] = __float_as_uint(__uint_as_float(y[k][j]) * corr);
+                            at_st16(o_at + 32 * c + 16 * k, y[k]);
+                        }
                     }
                 }
                 ve = e;
