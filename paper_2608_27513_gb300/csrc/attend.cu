@@ -849,7 +849,7 @@ cudaError_t launch_attend(AttendArgs a, cudaStream_t s) {
     const cudaError_t e = symbol_address_cached(&g_status_attend, cache, &a.status);
     if (e != cudaSuccess) return e;
     a.group = a.H / a.Hk;
-    a.by_group = (uint32_t)(((1ull << 32) + a.group - 1) / a.group);  // (not used for a group of 1)
+    a.by_group = fast_div_by(a.group);
     return a.d == 64 ? launch_d<64>(a, s) : a.d == 128 ? launch_d<128>(a, s) : launch_d<256>(a, s);
 }
 

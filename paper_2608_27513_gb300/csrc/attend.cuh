@@ -32,12 +32,7 @@ __device__ __forceinline__ AttRow att_row(const AttendArgs &p, int b) {
     r.n = p.q_lengths ? max(0, min(p.q_lengths[b], p.T)) : p.T;
     return r;
 }
-// x / group for 0 <= x < 2^27: the product's quotient is at most one too large
-__device__ __forceinline__ int att_div(const AttendArgs &p, int x) {
-    if (p.group == 1) return x;
-    const int q = (int)__umulhi((uint32_t)x, p.by_group);
-    return q - (q * p.group > x ? 1 : 0);
-}
+__device__ __forceinline__ int att_div(const AttendArgs &p, int x) { return fast_div(x, p.group, p.by_group); }
 __device__ __forceinline__ AttItem att_item(const AttendArgs &p, AttRow w, int rt, int R) {
     const int t0 = att_div(p, rt * R), t1 = min(w.n - 1, att_div(p, rt * R + R - 1));
     const int hi = w.len - w.n + t1;  // the last token that its last query sees

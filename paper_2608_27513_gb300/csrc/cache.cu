@@ -66,18 +66,15 @@ __global__ void __launch_bounds__(kAppThreads) cache_append_kernel(const CacheAr
     __shared__ float part[4];
     const int lane = threadIdx.x & 31;
     const int tid = TPI == 32 ? lane : threadIdx.x;
-    const int64_t item = TPI == 32 ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5) : (int64_t)blockIdx.x;
-    // keys and values, heads, pages, rows from the fastest
-    const int which = (int)(item & 1);
-    const int64_t ih = item >> 1;
-    const int h = (int)(ih % p.Hk);
-    const int64_t ip = ih / p.Hk;
-    const int b = (int)(ip / touched);
-    if (b >= p.batch) return;  // (a whole warp; with 128 threads an item, never)
+    // of row blockIdx.y, from the fastest: keys and values, heads, pages
+    const int item = TPI == 32 ? blockIdx.x * 4 + (threadIdx.x >> 5) : blockIdx.x;
+    const int which = item & 1, b = blockIdx.y;
+    const int ahead = fast_div(item >> 1, p.Hk, p.by_heads), h = (item >> 1) - ahead * p.Hk;
+    if (ahead >= touched) return;  // (a whole warp; with 128 threads an item, never)
     const int start = p.start[b];
     const int fresh = p.lengths ? max(0, min(p.lengths[b], p.T)) : p.T;
     const int first_page = max(start, 0) / kCachePage;
-    const int64_t page = first_page + ip % touched;  // of the row
+    const int64_t page = first_page + ahead;  // of the row
     const int64_t lo = max((int64_t)start, page * kCachePage), hi = min((int64_t)start + fresh, (page + 1) * kCachePage);
     if (start < 0 || lo >= hi) {
         if (start < 0 && fresh > 0 && tid == 0) atomicOr(p.status, kDevBadSlot);
@@ -177,29 +174,29 @@ __global__ void __launch_bounds__(kAppThreads) cache_append_kernel(const CacheAr
 }
 
 // A thread turns N keys and N values, 16 bytes each once they are turned (so that a warp's stores are whole
-// lines), of kReadTokens tokens, all on their way at once.
-constexpr int kReadTokens = 2;
+// lines), of kReadPairs (token, head) pairs, all on their way at once.  Indices are divided in 32 bits by a
+// multiplication: with 64-bit divisions the instructions, not the bytes, took the time.
+constexpr int kReadPairs = 2;
 template <int D, bool BF>
 __global__ void __launch_bounds__(kReadThreads) cache_read_kernel(const CacheArgs p) {
-    constexpr int N = BF ? 8 : 4, kParts = D / N;
-    uint32_t code[kReadTokens][2][N / 4];
-    float2 scale[kReadTokens];
-    int64_t unit[kReadTokens];
+    constexpr int N = BF ? 8 : 4, kParts = D / N, kStep = kReadThreads / kParts;  // threads of a pair; pairs at a time
+    uint32_t code[kReadPairs][2][N / 4];
+    float2 scale[kReadPairs];
+    const int b = blockIdx.y, m = threadIdx.x % kParts, pairs = p.T * p.Hk;
+    const int pair0 = blockIdx.x * (kReadPairs * kStep) + threadIdx.x / kParts;
+    const int64_t first = p.start ? (int64_t)p.start[b] : 0;
+    const int held = cache_clamp(p.lengths[b], p.table);
 #pragma unroll
-    for (int i = 0; i < kReadTokens; ++i) {
-        const int64_t u = ((int64_t)blockIdx.x * kReadTokens + i) * kReadThreads + threadIdx.x;
-        const int m = (int)(u % kParts);
-        const int64_t uh = u / kParts, ut = uh / p.Hk;
-        const int h = (int)(uh - ut * p.Hk);
-        const int64_t b = ut / p.T;
-        unit[i] = b < p.batch ? u : -1;
+    for (int i = 0; i < kReadPairs; ++i) {
+        const int pair = pair0 + i * kStep;
         scale[i] = make_float2(0.f, 0.f);
 #pragma unroll
         for (int k = 0; k < N / 4; ++k) code[i][0][k] = code[i][1][k] = 0x80808080u;  // zeros
-        if (b < p.batch) {
-            const int64_t token = (p.start ? (int64_t)p.start[b] : 0) + (ut - b * p.T);
-            if (token >= 0 && token < cache_clamp(p.lengths[b], p.table)) {
-                const int64_t slot = cache_page(p.pages[b * p.table + token / kCachePage], p.num_pages);
+        if (pair < pairs) {
+            const int t = fast_div(pair, p.Hk, p.by_heads), h = pair - t * p.Hk;
+            const int64_t token = first + t;
+            if (token >= 0 && token < held) {
+                const int64_t slot = cache_page(p.pages[(int64_t)b * p.table + (int)token / kCachePage], p.num_pages);
                 if (slot < 0) {
                     if (m == 0) atomicOr(p.status, kDevBadSlot);
                 } else {
@@ -221,8 +218,10 @@ __global__ void __launch_bounds__(kReadThreads) cache_read_kernel(const CacheArg
         }
     }
 #pragma unroll
-    for (int i = 0; i < kReadTokens; ++i) {
-        if (unit[i] < 0) continue;
+    for (int i = 0; i < kReadPairs; ++i) {
+        const int pair = pair0 + i * kStep;
+        if (pair >= pairs) continue;
+        const int64_t unit = ((int64_t)b * pairs + pair) * kParts + m;
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
             const float s = which ? scale[i].y : scale[i].x;
@@ -239,7 +238,7 @@ __global__ void __launch_bounds__(kReadThreads) cache_read_kernel(const CacheArg
                     y[e] = __float_as_uint(x[e]);
                 }
             }
-            stg128(static_cast<uint4 *>(which ? p.v : p.k) + unit[i], make_uint4(y[0], y[1], y[2], y[3]));
+            stg128(static_cast<uint4 *>(which ? p.v : p.k) + unit, make_uint4(y[0], y[1], y[2], y[3]));
         }
     }
 }
@@ -247,17 +246,16 @@ __global__ void __launch_bounds__(kReadThreads) cache_read_kernel(const CacheArg
 template <int D, bool BF>
 void append_as(const CacheArgs &a, cudaStream_t s) {
     const int touched = (a.T + kCachePage - 2) / kCachePage + 1;  // pages that T tokens may lie in
-    const int64_t items = 2 * (int64_t)a.Hk * a.batch * touched;
+    const unsigned items = 2u * a.Hk * touched;
     if (a.T <= 8)
-        cache_append_kernel<D, 32, BF><<<(unsigned)((items + 3) / 4), kAppThreads, 0, s>>>(a, touched);
+        cache_append_kernel<D, 32, BF><<<dim3((items + 3) / 4, a.batch), kAppThreads, 0, s>>>(a, touched);
     else
-        cache_append_kernel<D, 128, BF><<<(unsigned)items, kAppThreads, 0, s>>>(a, touched);
+        cache_append_kernel<D, 128, BF><<<dim3(items, a.batch), kAppThreads, 0, s>>>(a, touched);
 }
 template <int D, bool BF>
 void read_as(const CacheArgs &a, cudaStream_t s) {
-    const int64_t units = (int64_t)a.batch * a.T * a.Hk * (D / (BF ? 8 : 4));
-    const int64_t per = kReadTokens * kReadThreads;
-    cache_read_kernel<D, BF><<<(unsigned)((units + per - 1) / per), kReadThreads, 0, s>>>(a);
+    const int per = kReadPairs * kReadThreads / (D / (BF ? 8 : 4)), pairs = a.T * a.Hk;
+    cache_read_kernel<D, BF><<<dim3((unsigned)((pairs - 1) / per + 1), a.batch), kReadThreads, 0, s>>>(a);
 }
 #define DAMP_BY_D(f, a, s)                                                                      \
     do {                                                                                        \
@@ -279,6 +277,7 @@ cudaError_t status_word(uint32_t **out) {
 cudaError_t launch_cache_append(CacheArgs a, cudaStream_t s) {
     const cudaError_t e = status_word(&a.status);
     if (e != cudaSuccess) return e;
+    a.by_heads = fast_div_by(a.Hk);
     DAMP_BY_D(append_as, a, s);
     return cudaGetLastError();
 }
@@ -286,6 +285,7 @@ cudaError_t launch_cache_append(CacheArgs a, cudaStream_t s) {
 cudaError_t launch_cache_read(CacheArgs a, cudaStream_t s) {
     const cudaError_t e = status_word(&a.status);
     if (e != cudaSuccess) return e;
+    a.by_heads = fast_div_by(a.Hk);
     DAMP_BY_D(read_as, a, s);
     return cudaGetLastError();
 }

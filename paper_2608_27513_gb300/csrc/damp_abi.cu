@@ -824,7 +824,7 @@ damp_status damp_cache_read(const damp_cache_layout *layout, const void *cache, 
     if (st != DAMP_OK) return st;
     const int64_t n = (int64_t)batch * T, row = (int64_t)a.Hk * a.d;
     if (n == 0) return DAMP_OK;
-    if (n > INT64_MAX / 16 / row || n * row / 4096 >= INT32_MAX) return DAMP_ERR_SHAPE;  // CTAs of 4096 values
+    if (T > INT32_MAX / 2 / a.Hk) return DAMP_ERR_SHAPE;  // (token, head) pairs of a row
     if (!cache || !pages || !lengths || !k || !v) return DAMP_ERR_NULL;
     if (!aligned(cache, 16) || !aligned(pages, 4) || !aligned(start, 4) || !aligned(lengths, 4) || !aligned(k, 16) ||
         !aligned(v, 16))

@@ -120,6 +120,7 @@ struct CacheArgs {
     void *k, *v;
     int64_t k_stride, v_stride;  // elements from token to token
     int32_t in_bf16;
+    uint32_t by_heads;  // ceil(2^32 / Hk), to divide by it (set by the launchers)
     uint32_t *status;  // set by the launchers
 };
 struct AttendArgs {
