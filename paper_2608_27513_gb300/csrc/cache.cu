@@ -161,12 +161,18 @@ __global__ void __launch_bounds__(kAppThreads) cache_append_kernel(const CacheAr
         const int u = tid + i * TPI;
         if (u < n) {
             uint32_t w[4];
+            if (bad) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float2 y = val[i].pair(2 * e), z = val[i].pair(2 * e + 1);
-                // |x| <= 127 s, s and r rounded once each: x r rounds to 127 at most where all is finite
-                w[e] = bad ? code4(scaled(y.x, r), scaled(y.y, r), scaled(z.x, r), scaled(z.y, r))
-                           : code4(__fmul_rn(y.x, r), __fmul_rn(y.y, r), __fmul_rn(z.x, r), __fmul_rn(z.y, r));
+                for (int e = 0; e < 4; ++e) {
+                    const float2 y = val[i].pair(2 * e), z = val[i].pair(2 * e + 1);
+                    w[e] = code4(scaled(y.x, r), scaled(y.y, r), scaled(z.x, r), scaled(z.y, r));
+                }
+            } else {  // |x| <= 127 s, s and r rounded once each: x r rounds to 127 at most where all is finite
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float2 y = val[i].pair(2 * e), z = val[i].pair(2 * e + 1);
+                    w[e] = code4(__fmul_rn(y.x, r), __fmul_rn(y.y, r), __fmul_rn(z.x, r), __fmul_rn(z.y, r));
+                }
             }
             *reinterpret_cast<uint4 *>(rows + cache_chunk(t0 + u / kChunks, u % kChunks, D)) = make_uint4(w[0], w[1], w[2], w[3]);
         }
@@ -176,7 +182,7 @@ __global__ void __launch_bounds__(kAppThreads) cache_append_kernel(const CacheAr
 // A thread turns N keys and N values, 16 bytes each once they are turned (so that a warp's stores are whole
 // lines), of kReadPairs (token, head) pairs, all on their way at once.  Indices are divided in 32 bits by a
 // multiplication: with 64-bit divisions the instructions, not the bytes, took the time.
-constexpr int kReadPairs = 2;
+constexpr int kReadPairs = 4;
 template <int D, bool BF>
 __global__ void __launch_bounds__(kReadThreads) cache_read_kernel(const CacheArgs p) {
     constexpr int N = BF ? 8 : 4, kParts = D / N, kStep = kReadThreads / kParts;  // threads of a pair; pairs at a time

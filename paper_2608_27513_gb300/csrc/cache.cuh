@@ -19,14 +19,6 @@ __host__ __device__ constexpr int cache_record_bytes(int d) { return 2 * cache_r
 // byte of chunk m of token t's row inside the keys or the values
 __device__ __forceinline__ int cache_chunk(int t, int m, int d) { return t * d + 16 * (m ^ cache_swizzle(t, d)); }
 
-// x / n for 0 <= x < 2^31, by = ceil(2^32 / n): the product's quotient is at most one too large
-__device__ __forceinline__ int fast_div(int x, int n, uint32_t by) {
-    if (n == 1) return x;
-    const uint32_t q = __umulhi((uint32_t)x, by);
-    return (int)(q - (q * (uint32_t)n > (uint32_t)x ? 1u : 0u));
-}
-inline uint32_t fast_div_by(int n) { return (uint32_t)(((1ull << 32) + n - 1) / n); }  // (of 1: not used)
-
 // tokens that a row's page table holds at most
 __device__ __forceinline__ int cache_clamp(int n, int table) { return max(0, min(n, table * kCachePage)); }
 // the page of an entry, -1 for a bad one

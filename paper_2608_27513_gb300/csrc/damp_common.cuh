@@ -178,6 +178,14 @@ __device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t sel) {
 }
 
 
+// x / n for 0 <= x < 2^31, by = ceil(2^32 / n): the product's quotient is at most one too large
+__device__ __forceinline__ int fast_div(int x, int n, uint32_t by) {
+    if (n == 1) return x;
+    const uint32_t q = __umulhi((uint32_t)x, by);
+    return (int)(q - (q * (uint32_t)n > (uint32_t)x ? 1u : 0u));
+}
+inline uint32_t fast_div_by(int n) { return (uint32_t)(((1ull << 32) + n - 1) / n); }  // (of 1: not used)
+
 __device__ __forceinline__ float fmin3(float a, float b, float c) {
     float d;
     asm("min.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));

@@ -104,6 +104,8 @@ struct RotaryArgs {
     const double *freq;    // radians per position, r / 2
     float scale;
     int32_t interleaved, in_bf16;
+    int32_t units;               // of work of a head, and what divides by it and by all heads (set by the launcher)
+    uint32_t by_units, by_heads;
 };
 
 // the 8-bit cache of softmax-attention layers (cache.cuh)
@@ -174,7 +176,7 @@ cudaError_t launch_copy_slots(SlotArgs a, cudaStream_t s);  // dst[i] <- src[i]
 cudaError_t launch_zero_slots(SlotArgs a, cudaStream_t s);  // dst[i]
 cudaError_t launch_compact_plan(SlotArgs a, int32_t *out, cudaStream_t s);  // live slots src -> new numbers
 cudaError_t launch_verify(VerifyArgs a, cudaStream_t s);
-cudaError_t launch_rotary(const RotaryArgs &a, cudaStream_t s);
+cudaError_t launch_rotary(RotaryArgs a, cudaStream_t s);
 cudaError_t launch_cache_append(CacheArgs a, cudaStream_t s);
 cudaError_t launch_cache_read(CacheArgs a, cudaStream_t s);
 cudaError_t launch_attend(AttendArgs a, cudaStream_t s);

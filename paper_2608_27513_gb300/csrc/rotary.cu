@@ -71,7 +71,7 @@ __device__ __forceinline__ void rot_store(void *p, int64_t at, const float (&x)[
 // or 2 V values to copy.  V = 1 takes any r, d, stride and alignment.
 template <int V, bool BF, bool INTER>
 __global__ void __launch_bounds__(kRotThreads) rotary_kernel(const RotaryArgs p, int tb) {
-    __shared__ float cs[kRotPairs], sn[kRotPairs];
+    __shared__ __align__(16) float cs[kRotPairs], sn[kRotPairs];
     const int half = p.r / 2;
     const int64_t t0 = (int64_t)blockIdx.x * tb;
     const int n = (int)min((int64_t)tb, p.tokens - t0);
@@ -87,12 +87,11 @@ __global__ void __launch_bounds__(kRotThreads) rotary_kernel(const RotaryArgs p,
         sn[i] = p.scale * s;
     }
     __syncthreads();
-    const int turned = half / V, units = turned + (p.d - p.r + 2 * V - 1) / (2 * V);
-    const int heads = p.heads[0] + p.heads[1];
+    const int turned = half / V, units = p.units, heads = p.heads[0] + p.heads[1];
     const int all = n * heads * units;
     for (int i = threadIdx.x; i < all; i += kRotThreads) {
-        const int th = i / units, u = i - th * units;
-        const int t = th / heads;
+        const int th = fast_div(i, units, p.by_units), u = i - th * units;
+        const int t = fast_div(th, heads, p.by_heads);
         int h = th - t * heads;
         const bool second = h >= p.heads[0];
         const void *x = second ? p.x[1] : p.x[0];
@@ -124,12 +123,13 @@ __global__ void __launch_bounds__(kRotThreads) rotary_kernel(const RotaryArgs p,
                 rot_load<V, BF>(x, from + j, a);
                 rot_load<V, BF>(x, from + half + j, b);
             }
-            float y[V], z[V];
+            float y[V], z[V], cv[V], sv[V];
+            rot_load<V, false>(cs, t * half + j, cv);
+            rot_load<V, false>(sn, t * half + j, sv);
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const float c = cs[t * half + j + e], s = sn[t * half + j + e];
-                y[e] = a[e] * c - b[e] * s;
-                z[e] = b[e] * c + a[e] * s;
+                y[e] = a[e] * cv[e] - b[e] * sv[e];
+                z[e] = b[e] * cv[e] + a[e] * sv[e];
             }
             if (INTER) {
                 if constexpr (V == 1) {
@@ -172,7 +172,7 @@ void launch_layout(const RotaryArgs &a, unsigned grid, int tb, cudaStream_t s) {
 
 }  // namespace
 
-cudaError_t launch_rotary(const RotaryArgs &a, cudaStream_t s) {
+cudaError_t launch_rotary(RotaryArgs a, cudaStream_t s) {
     // Vectors of 16 bytes where both halves of a pair, the rest of a head and every row start on one.
     const int V = a.in_bf16 ? 8 : 4;
     bool wide = (a.r / 2) % V == 0 && a.d % V == 0;
@@ -180,6 +180,10 @@ cudaError_t launch_rotary(const RotaryArgs &a, cudaStream_t s) {
         if (a.heads[i])
             wide = wide && reinterpret_cast<uintptr_t>(a.x[i]) % 16 == 0 && reinterpret_cast<uintptr_t>(a.out[i]) % 16 == 0 &&
                    a.stride[i] % V == 0;
+    const int unit = wide ? V : 1;
+    a.units = a.r / 2 / unit + (a.d - a.r + 2 * unit - 1) / (2 * unit);
+    a.by_units = fast_div_by(a.units);
+    a.by_heads = fast_div_by(a.heads[0] + a.heads[1]);
     // Tokens of a CTA: one while there are few (the time is latency), then enough to fill its threads
     // with cosines.
     const int most = std::max(1, std::min(kRotPairs, kRotThreads) / (a.r / 2));
