@@ -766,6 +766,9 @@ class CacheLayout:
             shared = _cache_layouts[key] = (c, ctypes.byref(c), {})
         object.__setattr__(self, "_shared", shared)
 
+    def __reduce__(self):  # copies and pickles: the reference to the struct is not for them
+        return CacheLayout, (self.num_heads, self.num_kv_heads, self.d)
+
     def c(self) -> DampCacheLayout:
         return self._shared[0]
 
@@ -796,6 +799,8 @@ def _token_rows(name, t, shape, dtype, device):
     if t.get_device() != device:
         _wrong_device(name, t, device)
     B, T, H, d = shape
+    if B * T > 0x7fffffff:
+        raise ValueError(f"{name} holds more than 2^31 - 1 tokens")
     if t.is_contiguous():
         return t.data_ptr(), H * d
     sb, st, sh, sd = t.stride()
@@ -935,6 +940,8 @@ def _cache(layout, cache, pages, B, dev, i32, u8):
     if pages is None or pages.dim() != 2:
         raise ValueError("pages must be an int32 tensor [B, pages of a row]")
     n, W = cache.shape[0], pages.shape[1]
+    if W > 1 << 25:
+        raise ValueError("pages holds more than 2^25 pages of a row")
     return (_here("cache", cache, (n, layout.num_kv_heads, 2 * CACHE_PAGE * layout.d + 16), u8, dev), n,
             _here("pages", pages, (B, W), i32, dev), W)
 

@@ -225,3 +225,24 @@ def test_reference_append_bounds():
     growths = sum(1 for t in range(1, 32) if x[0, t].abs().max() > x[0, :t].abs().max())
     assert (got - x[0, :, 0].double()).abs().max() <= step * (0.5 + 0.5 * growths) * (1 + 1e-5)
     assert torch.equal(R.Cache(ref.pool(), 64).pool(), ref.pool())
+
+
+def test_layouts_are_copied_and_pickled():
+    import copy
+    import pickle
+    A = damp.CacheLayout(8, 2, 128)
+    for B in (copy.deepcopy(A), copy.copy(A), pickle.loads(pickle.dumps(A)), pickle.loads(pickle.dumps({"attn": A}))["attn"]):
+        assert B == A and hash(B) == hash(A) and B.c().num_kv_heads == 2 and B.record_bytes == A.record_bytes
+
+
+def test_binding_refuses_sizes_past_32_bits(L):
+    """A size that does not fit the C call's 32 bits is refused, not cut off."""
+    many = (1 << 32) + 1
+    q = torch.empty((1, many, 1, 2), dtype=torch.bfloat16, device="meta")
+    with pytest.raises(ValueError, match="tokens"):
+        damp._token_rows("q", q, q.shape, torch.bfloat16, q.get_device())
+    A = damp.CacheLayout(4, 2, 64)
+    pool = torch.empty((3, 2, A.record_bytes), dtype=torch.uint8, device="meta")
+    pages = torch.empty((1, many), dtype=torch.int32, device="meta")
+    with pytest.raises(ValueError, match="pages"):
+        damp._cache(A, pool, pages, 1, pool.get_device(), torch.int32, torch.uint8)
