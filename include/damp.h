@@ -481,10 +481,10 @@ typedef struct {
  *   128 + rne((c - 128) (s0 r)).  Each operation is rounded to FP32 (codes depend on how the
  *   tokens of a page were split into calls, by half a step for each growth).  NaN is stored as
  *   0, an infinity as the block's largest magnitude; both set DAMP_DEV_NOT_FINITE.
- *   The pages that a call writes must be distinct.
+ *   The pages that a call writes must be distinct.  T up to 2^30.
  * damp_cache_read: k, v [batch][T][num_kv_heads][d] of dtype (contiguous, 16-B aligned) become
  *   the values of tokens start[b] + t (start NULL: t), zeros from lengths[b] on (the tokens
- *   held) and before 0.
+ *   held) and before 0.  T num_kv_heads up to 2^30 - 1.
  * damp_cache_attend: o = softmax over the row's tokens of (scale q.k) v.
  *   q           [batch][T][num_heads][d] of dtype, q_stride elements from token to token; 16-B
  *               aligned, the stride a multiple of 16 bytes
@@ -496,11 +496,11 @@ typedef struct {
  *               j = lengths[b] - q_lengths[b] + t and sees tokens max(0, j - window + 1) .. j.
  *               A query that sees none gives zeros, and so do those past q_lengths[b].
  *   workspace   damp_cache_attend_workspace() bytes, 16-B aligned, of no use to any other call
- *               while this one runs (0 bytes for few rows of short tables: NULL is then allowed)
+ *               while this one runs (0 bytes where no row is split over the GPU: NULL is then allowed)
  *   Maxima, sums and outputs are FP32; weights enter the product with the values in FP16 (FP32
  *   inputs: as two FP16 parts each).  A NaN or infinity in a query reaches its own head's output
  *   alone.  How rows are split over the GPU depends on the lengths of the batch, and with it the
- *   last bits.  ceil(T num_heads / num_kv_heads / 16) batch num_kv_heads table must be below 2^31.
+ *   last bits.  ceil(T num_heads / num_kv_heads / 16) batch num_kv_heads table is 2^30 at most.
  * Outputs must not overlap the cache or an input.  Integers are 4-B aligned.
  */
 DAMP_API int64_t damp_cache_page_bytes(const damp_cache_layout *layout); /* all heads; 0 if the layout is invalid */

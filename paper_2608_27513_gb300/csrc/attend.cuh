@@ -17,7 +17,6 @@ namespace damp {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kNoRow = INT_MIN / 2;  // below every token, with a window too (2^30 at most)
 
-
 // the pages of an item in its row's table
 struct AttItem {
     int first, pages;

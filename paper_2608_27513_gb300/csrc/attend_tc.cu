@@ -1,25 +1,41 @@
 // attend_tc.cu -- attention over the 8-bit cache for many rows (drafts, prompts) on tcgen05.
 //
 // An item has R = 128 SUB rows (attend.cuh): one or two blocks of 128 (query token, query head) pairs of a
-// KV head, which are the lanes of tensor memory.  Per key tile of 128 tokens (4 pages) and block
-//     S = Q K^T   (Q in shared memory, FP16)          128 x 128 x D
-//     P = 2^(S f + a - R)                              a thread per row
-//     O += P V    (P in tensor memory over S, FP16)    128 x D x 128
-// One CTA per SM walks over an equal range of the items' key tiles.  Items that lie in one range are
-// written at once, parts are joined by a second launch, as for single tokens.
+// KV head, which are the lanes of tensor memory.  Per key tile of 128 tokens (4 pages; 64 at d = 256) and block
+//     S = Q K^T            Q in shared memory, FP16         128 x 128 x D
+//     P = 2^(S f + a - R)  a thread per row; over S in tensor memory, FP16
+//     O += P V             in two halves of the tokens      128 x D x 128
+// One CTA per SM walks over an equal range of the items' key tiles.  Items that lie in one range are written at
+// once; parts are joined by a second launch, as for single tokens, unless ranges end with items (attend_tc_whole).
 //
-// Warps: 4 per block of rows for the softmax (SUB = 2: warps 0-7; SUB = 1: 0-3), 4 (8) that turn codes
-// into FP16 operands, one that issues the products.  With two blocks one's products run while the
-// other's softmax does; with one, S has two buffers and the next tile's Q K^T runs under the softmax.
-// The warps that turn codes hold the next tile's codes in registers (loaded a tile ahead), so no copy
-// waits in shared memory; a 16-byte chunk of codes becomes two 16-byte rows of core matrices (8 rows of
-// 8 FP16), which serve K as a K-major and V as an MN-major operand without another layout.
+// Warps.  Softmax: 4 per block of rows.  Codes to FP16: 4 (SUB = 1: 4 for K, 4 for V); a 16-byte chunk of codes
+// becomes two 16-byte rows of core matrices (8 rows of 8 FP16), which serve K as a K-major and V as an MN-major
+// operand without another layout.  Pages: one warp copies a tile's records in bulk, K and V apart, and notes the
+// scales.  Products: a warp per block of rows, which issues from descriptors in uniform registers in loops of few
+// instructions.  With two blocks a token goes back and forth between the issuing warps, a tile's P V and the next
+// tile's Q K^T at a time, so that one block's products run under the other's softmax: left alone both fall into
+// step (a piece of 4096 queries at the end of 32768 tokens, 32 heads, 8 KV heads, d = 128: 1.96 ms; with it, at
+// that state of the kernel, 1.58).  With one block S has two buffers, and the next tile's Q K^T runs under the
+// softmax.  Scores are read from tensor memory twice, half of a tile at a time, once for the maximum and once for
+// the weights: 64 in registers, at 128 registers a thread, and little code (all roles share the instruction caches;
+// all 128 scores held, with registers moved between warps, spilled and was no faster).
+//
+// Queries arrive and outputs leave as whole rows by bulk copies, and a warp transposes 32 of them between rows and
+// core matrices in place along diagonals, without bank conflicts: 16-byte accesses by threads took 5000 clocks an item.
+// Columns that a row does not see are overwritten in tensor memory, in the border tiles of an item alone.
 //
 // Rounding.  Codes - 128 are exact in FP16; BF16 queries are scaled by a power of two per row (exact
 // down to 2^-39 of the row's largest).  The value scales enter the weights: P = p s_v / 2^e 2^10 with
 // the running power of two 2^e above them, in FP16 (2^-12 relative, a BF16 output is rounded to 2^-9).
 // The row sum takes the unrounded p in FP32.  The reference R of the exponents is a maximum that may lag
-// behind by 2^4, so that O is rescaled (from tensor memory and back) only where it moves by more.
+// behind by 2^5.9 (2^10 2^5.9 is below the largest FP16), so that O is rescaled, from tensor memory and back,
+// only where it moves by more.
+//
+// Measured (GPU alone).  That piece: 1.515 ms, 1.36 PFLOP/s, 72 % of a large BF16 matrix product.  A block's chain
+// S, softmax, P V, Q K^T takes 3700 clocks a tile; the products of both blocks 2080 of them, the exponentials 1024
+// per block.  16 rows of up to 1000 queries in up to 1500 tokens, 32 heads, 16 KV heads, window 512: 251 us, where an
+// item is 6 tiles, 3 of them with borders, and 16 000 clocks of start and end.  61 rows of 5 queries in up to 2048
+// tokens, 16 heads, 2 KV heads, d = 256: 45 us; 40 of 128 rows are used, a tile of 64 tokens is a chain of 2500 clocks.
 #include "attend.cuh"
 #include "prefill_tc.cuh"
 
@@ -34,7 +50,7 @@ namespace {
 constexpr int kAtThreads = 15 * 32;
 constexpr uint32_t kAtCols = 512;
 constexpr uint32_t kAtO = 256;  // S blocks at columns 0 and 128, O from here on
-constexpr float kAtLag = 5.9f;  // 2^15.9 is below the largest FP16
+constexpr float kAtLag = 5.9f;  // 2^10 2^5.9 is below the largest FP16; half of the rescalings that 4 makes
 constexpr int kAtNotes = 8;
 constexpr int kAtMaxPages = 4;  // of a key tile
 
@@ -65,9 +81,14 @@ struct AtSmem {
     static constexpr int sm_warps = 4 * SUB, turn_warps = 4;  // SUB = 1: four for K, four for V
 };
 // mbarriers
-enum { kBarQ = 0, kBarDone = 2, kBarKFull = 4, kBarKFree = 6, kBarVFull = 8, kBarVFree = 10, kBarS = 12, kBarP = 14, kBarPV = 18, kBarTurn = 19, kBarNote = 21,  // P: halves of two buffers
-      
-       kBarKcFull = kBarNote + kAtNotes, kBarKcFree = kBarKcFull + 4, kBarVcFull = kBarKcFree + 4, kBarVcFree = kBarVcFull + 4, kBarRows = kBarVcFree + 4, kBarCount = kBarRows + 8 };
+enum {
+    kBarQ = 0, kBarDone = 2,  // of blocks of rows
+    kBarKFull = 4, kBarKFree = 6, kBarVFull = 8, kBarVFree = 10,  // operands, two buffers
+    kBarS = 12, kBarP = 14, kBarPV = 18,  // P: halves of two buffers
+    kBarTurn = 19, kBarNote = 21,
+    kBarKcFull = kBarNote + kAtNotes, kBarKcFree = kBarKcFull + 4, kBarVcFull = kBarKcFree + 4, kBarVcFree = kBarVcFull + 4,  // codes, up to 4 stages
+    kBarRows = kBarVcFree + 4, kBarCount = kBarRows + 8  // of softmax warps
+};
 static_assert(kBarCount * 8 <= 448, "barriers");
 
 // instruction descriptor: f16 x f16 -> FP32, M = 128, N columns, B MN-major if set
@@ -794,7 +815,8 @@ bool attend_tc_takes(const AttendArgs &a) { return a.in_bf16 && (int64_t)a.T * (
 int attend_tc_rows(const AttendArgs &a) { return a.d <= 128 && (int64_t)a.T * (a.H / a.Hk) > 128 ? 256 : 128; }
 
 // Ranges end with items where that leaves them even (8 items per SM) or items are short (4 key tiles): no parts,
-// one launch.
+// one launch (16 rows of up to 1000 queries in up to 1500 tokens, 2016 items: 291 us against 305 with parts at that
+// state of the kernel).
 bool attend_tc_whole(const AttendArgs &a) {
     const int64_t G = a.H / a.Hk, R = attend_tc_rows(a), items = (int64_t)a.batch * (((int64_t)a.T * G + R - 1) / R) * a.Hk;
     const int tile = a.d == 256 ? 2 : 4;  // pages

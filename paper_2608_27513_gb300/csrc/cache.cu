@@ -12,7 +12,13 @@
 // tokens at most.  A thread keeps the values of its chunks of 16 in registers between the maximum
 // and the codes, so each value is read once; codes are stored 16 bytes at a time.
 //
-// Read.  A thread turns chunks of 16 codes into values.  Both are bound by the bytes.
+// Measured: 8 rows of 1000 to 2000 tokens, 8 KV heads, d = 128, BF16, are written in 14.6 us (49 MB read, 72 % of the
+// issue slots: 32 instructions per 16 values, where the floor of the bytes is 11) and read back in 13.6; 256 rows of
+// one token each, written (and 37 earlier codes an item requantised where a scale grows) and their open pages read
+// back, in 9.9; one token of one row 4.4, two launches.  A warp per item below 9 tokens: 128 threads would find
+// no work in that many chunks.
+//
+// Read.  A thread turns whole 16 bytes of values, several on their way at once.  Bound by the bytes.
 #include "cache.cuh"
 
 #include <algorithm>

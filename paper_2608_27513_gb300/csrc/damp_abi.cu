@@ -795,7 +795,7 @@ damp_status damp_cache_append(const damp_cache_layout *layout, void *cache, int6
     if (k_stride < row || v_stride < row || k_stride * es % 16 || v_stride * es % 16) return DAMP_ERR_SHAPE;
     if (n == 0) return DAMP_OK;
     if (k_stride > INT64_MAX / 16 / n || v_stride > INT64_MAX / 16 / n) return DAMP_ERR_SHAPE;
-    if (2 * row / a.d * batch > INT32_MAX / ((T + 30) / 32 + 1)) return DAMP_ERR_SHAPE;  // CTAs
+    if (T > (1 << 30) || 2 * row / a.d * batch > INT32_MAX / ((T + 30) / 32 + 1)) return DAMP_ERR_SHAPE;  // a table's tokens; CTAs
     if (!cache || !pages || !start || !k || !v) return DAMP_ERR_NULL;
     if (!aligned(cache, 16) || !aligned(pages, 4) || !aligned(start, 4) || !aligned(lengths, 4) || !aligned(k, 16) ||
         !aligned(v, 16))
@@ -869,8 +869,8 @@ damp_status damp_cache_attend(const damp_cache_layout *layout, const void *cache
     if (window < 0 || !(scale > 0.f) || !(scale <= 3.4e38f) || q_stride < row || q_stride * es % 16) return DAMP_ERR_SHAPE;
     if (n == 0) return DAMP_OK;
     if (q_stride > INT64_MAX / 16 / n || T * G > (1 << 26)) return DAMP_ERR_SHAPE;
-    // pages of all items of 16 rows
-    if (((T * G + 15) / 16) * batch * c.Hk > INT32_MAX / table) return DAMP_ERR_SHAPE;
+    // pages of all items of 16 rows: 32-bit indices in the kernels, with room for what is added to them
+    if (((T * G + 15) / 16) * batch * c.Hk > (1 << 30) / table) return DAMP_ERR_SHAPE;
     AttendArgs a{};
     a.H = c.H;
     a.Hk = c.Hk;

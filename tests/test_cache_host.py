@@ -246,3 +246,13 @@ def test_binding_refuses_sizes_past_32_bits(L):
     pages = torch.empty((1, many), dtype=torch.int32, device="meta")
     with pytest.raises(ValueError, match="pages"):
         damp._cache(A, pool, pages, 1, pool.get_device(), torch.int32, torch.uint8)
+
+
+def test_sizes_near_the_limits_are_refused(L, fb):
+    """Sums of 32-bit indices in the kernels stay below 2^31."""
+    append = [layout(4, 1), _p(fb, 0), 8, _p(fb, 1), 2, 1, (1 << 31) - 8, _p(fb, 2), None, _p(fb, 3), 64, _p(fb, 4), 64, 0, None]
+    assert L.damp_cache_append(*append) == SHAPE
+    tiles, table = 6, 1 << 25  # 6 tiles of 16 rows, 3 batch rows, 2 KV heads: 1.2e9 pages
+    need = L.damp_cache_attend_workspace(layout(), 3, 8 * tiles, table, 0)
+    attend = [layout(), _p(fb, 0), 8, _p(fb, 1), table, 3, 8 * tiles, _p(fb, 2), None, _p(fb, 3), 256, 0.125, 0, _p(fb, 4), 0, _p(fb, 5), need, None]
+    assert L.damp_cache_attend(*attend) == SHAPE
