@@ -62,7 +62,7 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
 // add up over the pages.  For FP32 inputs 16 products at a time, the small part's first, are summed there and added
 // here.  Error norm against 64 bits, all sums there and as it is: a row of 1000 tokens, d = 64,
 // 7.3e-7 and 3.1e-7 (FP32 matrix products: 3.1e-7), 2 rows of up to 300 queries in up to 3000 tokens, d = 128, 2.4e-6
-// and 4.0e-7 (1.2e-6).  It costs 16 rows of 4000 tokens, 8 KV heads, d = 128, 53 us instead of 45, 64 rows with 2 KV heads,
+// and 4.0e-7 (1.2e-6), 4 rows of 640 queries in 8000 tokens, d = 64, 7.1e-6 before.  It costs 16 rows of 4000 tokens, 8 KV heads, d = 128, 53 us instead of 45, 64 rows with 2 KV heads,
 // d = 256, 113 instead of 73.  (BF16 outputs are rounded to 2^-9 anyway.)
 template <int PARTS>
 __device__ __forceinline__ void mma_add(float (&d)[4], const uint32_t (&a)[PARTS][4], uint32_t b0, uint32_t b1) {

@@ -355,6 +355,32 @@ def test_attend_long_context(dtype):
         run_attend(layout, pool, pages, q.to(dtype), n, "long", window=9000)
 
 
+def test_attend_sums_of_long_rows_are_rounded():
+    """FP32 sums over many pages in one place do not drift: the error's norm against 64 bits.
+
+    Roundings are of random sign, so their squares add up.  In units of 2^-24 of the output: two additions a page,
+    relative to a sum whose square is half of the last one's on average (1 page^-1); the sum of the weights, one a
+    page, a third of the square (1/3 page^-1); ex2 and the two parts of a weight, 4 units each (2^-22); the scores,
+    d / 16 + 4 additions and products of ln 2 times their size in powers of two, which is below 1 here.  Doubled."""
+    B, T, Hk, d, W = 4, 640, 8, 64, 250  # more items than the GPU has ranges: whole rows in one of them
+    layout = damp.CacheLayout(Hk, Hk, d)
+    pool, pages = filled(layout, B, W, 3, spread=False)
+    q = 0.25 * randn(gen(4), B, T, Hk, d)
+    o = damp.cache_attend(layout, pool, q, pages, i32([W * R.PAGE] * B))
+    cache, n = R.Cache(pool, d), W * R.PAGE
+    unseen = torch.arange(n, device=DEV) > torch.arange(n - T, n, device=DEV)[:, None]
+    err = size = 0.0
+    for b in range(B):
+        k, v = (cache.values(w, pages[b].cpu()).to(DEV) for w in (0, 1))
+        for h in range(Hk):
+            p = (q[b, :, h].double() @ k[:, h].T * d ** -0.5).masked_fill(unseen, -math.inf).softmax(-1)
+            want = p @ v[:, h]
+            err += (o[b, :, h].double() - want).square().sum().item()
+            size += want.square().sum().item()
+    limit = 2 * 2.0 ** -24 * math.sqrt(W * 4 / 3 + 4 ** 2 + 4 ** 2 + d / 16 + 4)
+    assert math.sqrt(err / size) <= limit, f"error norm {math.sqrt(err / size):g}, limit {limit:g}"
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("T", [1, 40])
 def test_attend_scales(dtype, T):
