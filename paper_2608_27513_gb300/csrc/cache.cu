@@ -12,11 +12,12 @@
 // tokens at most.  A thread keeps the values of its chunks of 16 in registers between the maximum
 // and the codes, so each value is read once; codes are stored 16 bytes at a time.
 //
-// Measured: 8 rows of 1000 to 2000 tokens, 8 KV heads, d = 128, BF16, are written in 14.6 us (49 MB read, 72 % of the
-// issue slots: 32 instructions per 16 values, where the floor of the bytes is 11) and read back in 13.6; 256 rows of
-// one token each, written (and 37 earlier codes an item requantised where a scale grows) and their open pages read
-// back, in 9.9; one token of one row 4.4, two launches.  A warp per item below 9 tokens: 128 threads would find
-// no work in that many chunks.
+// Measured: 8 rows of 1000 to 2000 tokens, 8 KV heads, d = 128, BF16, are written in 13.4 to 14.6 us (72 % of the issue
+// slots, 14 instructions a value with all that an item costs; the floor of the bytes is 11) and read back in 14; 256 rows
+// of one token each, written (earlier codes requantised where a scale grows) and their open pages read back, in 9.9;
+// one token of one row 4.2, two launches.  64 threads an item take 17.1 us for those prompts and 23.9 for 16 heads,
+// d = 64 (128: 16.1), a warp 15.2 and 13.2 (d = 256: 10.1 where 128 threads take 7.2).  Below 9 tokens 128 threads
+// would find no work.
 //
 // Read.  A thread turns whole 16 bytes of values, several on their way at once.  Bound by the bytes.
 #include "cache.cuh"
