@@ -16,8 +16,8 @@
 // slots, 14 instructions a value with all that an item costs; the floor of the bytes is 11) and read back in 14; 256 rows
 // of one token each, written (earlier codes requantised where a scale grows) and their open pages read back, in 9.9;
 // one token of one row 4.2, two launches.  64 threads an item take 17.1 us for those prompts and 23.9 for 16 heads,
-// d = 64 (128: 16.1), a warp 15.2 and 13.2 (d = 256: 10.1 where 128 threads take 7.2).  Below 9 tokens 128 threads
-// would find no work.
+// d = 64 (128: 16.1), a warp 15.2 and 13.2 to 14.5 (but d = 256 10.1 where 128 threads take 7.2, and d = 64 in FP32
+// 22 where they take 20; calls of 9 to 64 tokens 0.1 to 0.4 us longer).  Below 9 tokens 128 threads would find no work.
 //
 // Read.  A thread turns whole 16 bytes of values, several on their way at once.  Bound by the bytes.
 #include "cache.cuh"
