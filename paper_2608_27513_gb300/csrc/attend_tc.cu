@@ -694,10 +694,12 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
             AtNote *const note = reinterpret_cast<AtNote *>(sm + M::note) + i % kAtNotes;
             ve = max(ve, (int)__reduce_max_sync(kFull, scales.y > 0.f ? min((__float_as_uint(scales.y) >> 23) + 1u, 253u) : 0u));
             if (lane < PG) {
-                // value scales below 2^-40 of the unit count as that; a block of zeros stands for zeros at any scale
-                const float rel = fmaxf(scales.y * __uint_as_float((uint32_t)(254 - ve) << 23), 9.0949470177292824e-13f);
-                const float u = scales.y > 0.f ? rel * 1024.f : 1024.f;
-                note->factor[lane] = scales.x > 0.f ? scales.x : 1.f;
+                // A scale of 0 stands for zeros whatever the codes are: scores of 0 (times 0, FLT_MIN in the softmax, so
+                // that hidden columns stay -inf), weights that are 0 in FP16 but count in the sum.  So value scales below
+                // 2^-70 of the unit count as that: u = 2^-60, weights below 2^-54, less than half of FP16's smallest.
+                const float rel = fmaxf(scales.y * __uint_as_float((uint32_t)(254 - ve) << 23), 8.4703294725430034e-22f);
+                const float u = rel * 1024.f;
+                note->factor[lane] = scales.x;
                 note->weight[lane] = __log2f(u);
                 note->back[lane] = 1.f / u;
             }

@@ -1,0 +1,76 @@
+"""Attention over records of the 8-bit cache that cache_append did not write, or only in part: what a code stands for
+is (c - 128) times its scale whatever the kernel, a scale of 0 included."""
+import pytest
+import torch
+
+import paper_2608_27513_gb300 as damp
+from tests import cache_ref as R
+from tests.test_gpu_cache import BF, DEV, F32, filled, gen, i32, randn, run_attend
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True)
+def clean_status():
+    damp.device_status()
+    yield
+    assert damp.device_status() == 0
+
+
+def scales_of(pool, d):
+    """The scales [pages, Hk, 2] of a pool, a view."""
+    return pool[..., 64 * d:64 * d + 8].view(torch.float32)
+
+
+# one token, drafts in one block of rows, prompts in one and in two
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("H,Hk,d", [(8, 2, 64), (8, 2, 128), (16, 2, 256)])
+@pytest.mark.parametrize("T", [1, 6, 30, 90])
+def test_scale_zero_stands_for_zeros(dtype, H, Hk, d, T):
+    """Pages as new_cache and zero_slots leave them (codes 0, scales 0), and any codes under a scale of 0 of the keys, of
+    the values or of both."""
+    layout = damp.CacheLayout(H, Hk, d)
+    pool, pages = filled(layout, 3, 9, d + T)
+    g = gen(T)
+    codes = lambda n: torch.randint(0, 256, (n, Hk, 64 * d), generator=g, device=DEV, dtype=torch.uint8)
+    at = pages.long()
+    pool[at[0, 1]] = 0
+    damp.zero_slots([pool], pages[0, 5:7].contiguous())
+    pool[at[1, 2:6], :, :64 * d] = codes(4)
+    s = scales_of(pool, d)
+    s[at[1, 2], :, 0] = 0
+    s[at[1, 3], :, 1] = 0
+    s[at[1, 4]] = 0
+    s[at[1, 5], 0] = 0  # one head alone
+    pool[at[2]] = 0  # nothing was ever written
+    q = 1.5 * randn(g, 3, T, H, d)
+    run_attend(layout, pool, pages, q.to(dtype), [288, 280, 200], "scales of 0")
+    run_attend(layout, pool, pages, q.to(dtype), [250, 288, 100], "scales of 0, a window", window=100)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("T", [1, 20, 70])
+def test_zeros_appended_behind_tokens_that_nothing_wrote(dtype, T):
+    """start lies inside a zeroed page: the tokens before it stand for zeros, also where the tokens after it are zeros
+    and the scale stays 0; and as many tokens decode as read back."""
+    layout = damp.CacheLayout(8, 2, 128)
+    pool = damp.new_cache(layout, 8, DEV)
+    pages = i32([[0, 1, 2], [3, 4, 5]])
+    g = gen(T)
+    k, v = randn(g, 2, 50, 2, 128), randn(g, 2, 50, 2, 128)
+    k[0, :12] = 0  # the rest of the page that start lies in
+    v[0, :12] = 0
+    v[1, :, 0] = 0
+    start = [20, 9]
+    damp.cache_append(layout, pool, k, v, pages, i32(start))
+    q = randn(g, 2, T, 8, 128)
+    held = [70, 59]
+    run_attend(layout, pool, pages, q.to(dtype), held, "zeros behind unwritten tokens")
+    kr, vr = damp.cache_read(layout, pool, pages, i32(held), 96, dtype=F32)
+    ref = R.Cache(pool, 128)
+    for w, got in enumerate((kr, vr)):
+        for b in range(2):
+            want = ref.values(w, pages[b].cpu(), torch.float32)
+            want[held[b]:] = 0
+            assert torch.equal(got[b].cpu(), want)
+            assert not got[b, :start[b]].any()
