@@ -460,7 +460,7 @@ typedef struct {
  * The cache: a pool of num_pages pages of 32 tokens.  Page p, KV head h is a record of
  * 64 d + 16 bytes at (p num_kv_heads + h) (64 d + 16): 32 key rows of d codes, 32 value rows,
  * the FP32 scales of the keys and of the values, 8 unused bytes.  Code c (uint8) stands for
- * (c - 128) s.  Chunk m of 16 codes of the row of token t lies at chunk m ^ (h(t) mod d/16),
+ * (c - 128) s, zero where s is 0.  Chunk m of 16 codes of the row of token t lies at chunk m ^ (h(t) mod d/16),
  * h(t) = (t & 7) ^ ((t & 1) << 2).  Pages are slots of damp_copy_slots (a shared page is copied
  * before it is written) and damp_zero_slots.
  *   cache       the pool, 16-B aligned
@@ -497,9 +497,12 @@ typedef struct {
  *               A query that sees none gives zeros, and so do those past q_lengths[b].
  *   workspace   damp_cache_attend_workspace() bytes, 16-B aligned, of no use to any other call
  *               while this one runs (0 bytes where no row is split over the GPU: NULL is then allowed)
- *   Maxima, sums and outputs are FP32; weights enter the product with the values in FP16 (FP32
- *   inputs: as two FP16 parts each).  A NaN or infinity in a query reaches its own head's output
- *   alone.  How rows are split over the GPU depends on the lengths of the batch, and with it the
+ *   Maxima, sums and outputs are FP32.  Weights enter the product with the values times the page's
+ *   value scale over a power of two above the scales of all pages of which the query sees a token, in
+ *   FP16 (FP32 inputs: two FP16 parts each): a key's part of an output is within 2^-11 of itself (FP32:
+ *   2^-21), and 2^-34 of the largest value that those pages can hold.  What a query does not see, values
+ *   of its own pages apart, changes no bit of its output.  A NaN or infinity in a query reaches its own
+ *   head's output alone.  How rows are split over the GPU depends on the lengths of the batch, and with it the
  *   last bits.  ceil(T num_heads / num_kv_heads / 16) batch num_kv_heads table is 2^30 at most.
  * Outputs must not overlap the cache or an input.  Integers are 4-B aligned.
  */

@@ -12,9 +12,9 @@
 // waits for another.  Products run on m16n8k16 with FP16 operands and FP32 sums.  Codes minus 128
 // are exact in FP16.  A query row is scaled by a power of two to below 2^15 and rounded to FP16:
 // BF16 values lose nothing above 2^-39 of the row's largest (FP32: two FP16 parts, 22 bits).
-// Weights p s_v / 2^e, where 2^e is the running power of two above the pages' value scales, lie in
-// 0 .. 1 and enter as FP16 times 2^10 (2^-12 relative down to 2^-24 of the largest; an output in
-// BF16 is rounded to 2^-9 anyway), as two parts for FP32.  Sums, maxima and outputs are FP32.
+// Weights p s_v / 2^e, where 2^e is the running power of two above the value scales that a row has seen, lie in
+// 0 .. 1 and enter as FP16 times 2^10 (2^-11 relative down to 2^-24 of the largest; an output in
+// BF16 is rounded by 2^-8 anyway), as two parts for FP32.  Sums, maxima and outputs are FP32.
 //
 // The contraction index of Q K^T is permuted so that a lane's operands are 16 consecutive codes,
 // and the columns of P V so that a lane reads 16 consecutive codes of 4 tokens: 16-byte loads
@@ -38,6 +38,7 @@ static __device__ uint32_t g_status_attend;
 namespace {
 
 constexpr int kJoinThreads = 256;
+constexpr int kNoScale = -1000;  // below every exponent field
 template <int D, bool F32>
 struct AttCfg {
     static constexpr int R = 16;
@@ -63,7 +64,7 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
 // here.  Error norm against 64 bits, all sums there and as it is: a row of 1000 tokens, d = 64,
 // 7.3e-7 and 3.1e-7 (FP32 matrix products: 3.1e-7), 2 rows of up to 300 queries in up to 3000 tokens, d = 128, 2.4e-6
 // and 4.0e-7 (1.2e-6), 4 rows of 640 queries in 8000 tokens, d = 64, 7.1e-6 before.  It costs 16 rows of 4000 tokens, 8 KV heads, d = 128, 53 us instead of 45, 64 rows with 2 KV heads,
-// d = 256, 113 instead of 73.  (BF16 outputs are rounded to 2^-9 anyway.)
+// d = 256, 113 instead of 73.  (BF16 outputs are rounded by 2^-8 anyway.)
 template <int PARTS>
 __device__ __forceinline__ void mma_add(float (&d)[4], const uint32_t (&a)[PARTS][4], uint32_t b0, uint32_t b1) {
     if constexpr (PARTS == 2) {
@@ -129,7 +130,7 @@ struct AttRows {
     float o[kCols][4], m[2], l[2], factor[2];
     int limit[2];  // the last token that a row sees
     uint32_t q[C::q_smem ? 1 : C::parts][C::q_smem ? 1 : kSteps][4];
-    int ve;  // exponent field of the outputs' unit
+    int ve[2];  // exponent field of a row's unit: above the value scales of the pages that it has seen
 
     // tile rt of a batch row's queries; qs: where in shared memory the operands go that registers do not hold
     __device__ __forceinline__ void start(const AttendArgs &p, AttRow w, int b, int rt, int h, uint32_t qs, int lane) {
@@ -197,7 +198,7 @@ struct AttRows {
         }
 #pragma unroll
         for (int i = 0; i < kCols; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
-        ve = 0;
+        ve[0] = ve[1] = 0;
         __syncwarp();
     }
     // one page, whose record lies at kb in shared memory
@@ -236,14 +237,6 @@ struct AttRows {
                 }
             }
         }
-        // the outputs' unit: a power of two above every value scale so far
-        const int e = min((int)(__float_as_uint(vs) >> 23) + 1, 253);
-        const int ve_new = max(ve, vs > 0.f ? e : 0);
-        const float wscale = vs * __uint_as_float((uint32_t)(254 - max(ve_new, 1)) << 23) * 1024.f;
-        const int shift = 127 + ve - ve_new;
-        const float vcorr = shift > 0 ? __uint_as_float((uint32_t)shift << 23) : 0.f;
-        bool moved = ve_new != ve;
-        ve = ve_new;
         const int at = page * kCachePage;
         bool edge = false;
 #pragma unroll
@@ -252,27 +245,37 @@ struct AttRows {
             edge = edge || (k != kNoRow && (k < at + kCachePage - 1 || (p.window && k - (p.window - 1) > at)));
         }
         const bool masked = __any_sync(kFull, edge);
+        // vs = 2^(e - 127) mantissa / 2^10
+        const int e = vs > 0.f ? min((int)(__float_as_uint(vs) >> 23) + 1, 253) : kNoScale;
+        const float mantissa = vs > 0.f ? vs * __uint_as_float((uint32_t)(254 - e) << 23) * 1024.f : 0.f;
+        bool moved = false;
+        int fall[2];
         uint32_t pa[C::parts][4][2];  // [column tile][row half]
         float corr[2];
 #pragma unroll
         for (int hh = 0; hh < 2; ++hh) {
             const float fac = factor[hh] * ks;
+            const int last = limit[hh], from = p.window ? last - (p.window - 1) : 0;
+            // a row's unit: a power of two above the value scales of all pages so far of which it sees a token
+            const int mine = !masked || (last >= at && from < at + kCachePage) ? e : kNoScale, up = max(ve[hh], mine);
+            const float wscale = mantissa * __uint_as_float((uint32_t)max(127 + mine - up, 0) << 23);
+            fall[hh] = ve[hh] - up;
+            ve[hh] = up;
             float x[8], top = -INFINITY;
 #pragma unroll
             for (int i = 0; i < 8; ++i) x[i] = s[i >> 1][2 * hh + (i & 1)] * fac;
             if (masked) {
-                const int k = limit[hh], from = p.window ? k - (p.window - 1) : 0;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const int token = at + 8 * (i >> 1) + 2 * c + (i & 1);
-                    if (token > k || token < from) x[i] = -INFINITY;
+                    if (token > last || token < from) x[i] = -INFINITY;
                 }
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) top = fmaxf(top, x[i]);
             const float mn = fmaxf(m[hh], quad_max(top)), mu = mn == -INFINITY ? 0.f : mn;
             corr[hh] = ex2(m[hh] - mu);
-            moved = moved || mn != m[hh];
+            moved = moved || mn != m[hh] || fall[hh] != 0;
             m[hh] = mn;
             float sum = 0.f;
 #pragma unroll
@@ -292,9 +295,11 @@ struct AttRows {
         }
         if (__any_sync(kFull, moved)) {
 #pragma unroll
+            for (int hh = 0; hh < 2; ++hh) corr[hh] *= __uint_as_float((uint32_t)max(127 + fall[hh], 0) << 23);
+#pragma unroll
             for (int i = 0; i < kCols; ++i)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) o[i][k] *= corr[k >> 1] * vcorr;
+                for (int k = 0; k < 4; ++k) o[i][k] *= corr[k >> 1];
         }
 #pragma unroll
         for (int s2 = 0; s2 < 2; ++s2) {
@@ -333,9 +338,9 @@ struct AttRows {
     // the outputs, where all pages were this warp's; else a part of them: rows of D values, and their (m, l)
     __device__ __forceinline__ void leave(const AttendArgs &p, int b, int rt, int h, bool whole, float *parts, float2 *mls, int lane) {
         const int G = p.group, g = lane >> 2, c = lane & 3;
-        const float unit = __uint_as_float((uint32_t)ve << 23) * (1.f / 1024.f);
 #pragma unroll
         for (int hh = 0; hh < 2; ++hh) {
+            const float unit = __uint_as_float((uint32_t)ve[hh] << 23) * (1.f / 1024.f);
             const int r = hh * 8 + g;  // in the item
             const int row = rt * R + r, t = att_div(p, row);
             const float sum = quad_sum(l[hh]);

@@ -26,7 +26,8 @@
 //
 // Rounding.  Codes - 128 are exact in FP16; BF16 queries are scaled by a power of two per row (exact
 // down to 2^-39 of the row's largest).  The value scales enter the weights: P = p s_v / 2^e 2^10 with
-// the running power of two 2^e above them, in FP16 (2^-12 relative, a BF16 output is rounded to 2^-9).
+// the running power of two 2^e above those of the pages that the row has seen, in FP16 (2^-11 relative, a BF16 output is
+// rounded by 2^-8).  2^e is of the row, not of its block: what a row does not see changes no bit of its output.
 // The row sum takes the unrounded p in FP32.  The reference R of the exponents is a maximum that may lag
 // behind by 2^5.9 (2^10 2^5.9 is below the largest FP16), so that O is rescaled, from tensor memory and back,
 // only where it moves by more.
@@ -53,12 +54,14 @@ constexpr uint32_t kAtO = 256;  // S blocks at columns 0 and 128, O from here on
 constexpr float kAtLag = 5.9f;  // 2^10 2^5.9 is below the largest FP16; half of the rescalings that 4 makes
 constexpr int kAtNotes = 8;
 constexpr int kAtMaxPages = 4;  // of a key tile
+constexpr int kAtNoScale = -1000;  // below every exponent field
+constexpr float kAtLowest = -60.f;  // weights of value scales further below a row's unit: under 2^-54, 0 in FP16
 
 struct AtNote {  // of a key tile: what the softmax needs of its pages
     float factor[kAtMaxPages];  // key scale
-    float weight[kAtMaxPages];  // log2 of 2^10 times value scale over 2^e
-    float back[kAtMaxPages];    // 2^-weight, exactly what the sums divide by
-    int e;                      // exponent field of 2^e
+    float weight[kAtMaxPages];  // log2 of 2^10 times value scale over the tile's unit, a multiple of 2^-15
+    int e[kAtMaxPages];         // exponent field of the power of two above the value scale; kAtNoScale for 0
+    int top;                    // the largest e: the tile's unit
     int hidden;                 // bit i: page i is bad or missing
     int unused[2];
 };
@@ -409,7 +412,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
             __syncwarp();
             if (lane == 0) at_arrive(bar(kBarQ + x));
             float ref = -INFINITY, sum = 0.f;
-            int ve = 0;
+            int ve = 1;  // exponent field of the row's unit: above the value scales of the pages that it has seen
             const int first_tile = at - it.begin;
             for (; at < last; ++at, ++tile) {
                 const int sbuf = SUB == 2 ? x : tile & 1;
@@ -418,13 +421,19 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
                 const AtNote *const note = reinterpret_cast<const AtNote *>(sm + M::note) + tile % kAtNotes;
                 const int i = at - it.begin;
                 const int token = (it.first + i * PG) * kCachePage;  // of column 0
-                const int hidden = note->hidden, e = note->e;
+                const int hidden = note->hidden;
+                int e = max(ve, note->top);
                 ok = together(ok && wait(bar(kBarS + sbuf), (SUB == 2 ? tile : tile >> 1) & 1));
                 if (!ok) break;
                 tc_fence_after();
                 if (__any_sync(kFull, hidden != 0 || limit < token + TN - 1 || from > token)) {
-                    // columns that a row does not see become -inf where they are, 16 at a time (of the border tiles of an
-                    // item only: a small loop, for the instruction caches' sake, which all roles share)
+                    // A page that a row does not see leaves its unit as it is.  Columns that a row does not see become -inf
+                    // where they are, 16 at a time (of the border tiles of an item only: a small loop, for the instruction
+                    // caches' sake, which all roles share).
+                    e = ve;
+#pragma unroll
+                    for (int c = 0; c < PG; ++c)
+                        if (limit >= token + kCachePage * c && from < token + kCachePage * (c + 1)) e = max(e, note->e[c]);
 #pragma unroll 1
                     for (int c = 0; c < 2 * PG; ++c) {
                         const int lo = from - (token + 16 * c), hi = limit - (token + 16 * c);  // sees lo .. hi
@@ -447,6 +456,9 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
 #pragma unroll 1
                 for (int h = 0; h < 2; ++h) {
                     uint32_t s[PG][16];
+                    float f[PG / 2];  // while the scores are on their way
+#pragma unroll
+                    for (int c = 0; c < PG / 2; ++c) f[c] = fmaxf(factor * note->factor[h * (PG / 2) + c], FLT_MIN);  // not 0: times a hidden -inf
 #pragma unroll
                     for (int c = 0; c < PG; ++c) at_ld16(s_at + (16 * PG) * h + 16 * c, s[c]);
 #pragma unroll
@@ -457,7 +469,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
 #pragma unroll
                         for (int j = 0; j < 32; j += 2)
                             m[(j >> 1) & 3] = fmax3(m[(j >> 1) & 3], __uint_as_float(s[2 * c + (j >> 4)][j & 15]), __uint_as_float(s[2 * c + (j >> 4)][(j & 15) + 1]));
-                        top = fmaxf(top, fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])) * fmaxf(factor * note->factor[h * (PG / 2) + c], FLT_MIN));  // not 0: times a hidden -inf
+                        top = fmaxf(top, fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])) * f[c]);
                     }
                 }
                 const bool moves = top > ref + kAtLag;
@@ -491,9 +503,16 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
                 }
                 ve = e;
                 const float base = ref == -INFINITY ? 0.f : -ref;
+                const float over = (float)(note->top - e);  // the tile's unit over the row's
 #pragma unroll 1
                 for (int h = 0; h < 2; ++h) {
                     uint32_t s[PG][16];
+                    float f[PG / 2], weight[PG / 2];  // while the scores are on their way
+#pragma unroll
+                    for (int c = 0; c < PG / 2; ++c) {
+                        f[c] = fmaxf(factor * note->factor[h * (PG / 2) + c], FLT_MIN);
+                        weight[c] = fmaxf(over + note->weight[h * (PG / 2) + c], kAtLowest);  // (exact)
+                    }
 #pragma unroll
                     for (int c = 0; c < PG; ++c) at_ld16(s_at + (16 * PG) * h + 16 * c, s[c]);
 #pragma unroll
@@ -501,7 +520,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
 #pragma unroll
                     for (int c = 0; c < PG / 2; ++c) {
                         const int page = h * (PG / 2) + c;
-                        const float2 f2 = splat2(fmaxf(factor * note->factor[page], FLT_MIN)), a2 = splat2(base + note->weight[page]);
+                        const float2 f2 = splat2(f[c]), a2 = splat2(base + weight[c]);
                         float2 z[16];
 #pragma unroll
                         for (int j = 0; j < 16; ++j)
@@ -517,7 +536,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
                         }
                         at_st16(s_at + 16 * page, w);
                         const float2 both = add2(part[0], part[1]);
-                        sum = fmaf(both.x + both.y, note->back[page], sum);
+                        sum = fmaf(both.x + both.y, ex2(-weight[c]), sum);
                     }
                     at_st_wait();
                     tc_fence_before();
@@ -650,20 +669,16 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
             return lane < PG && i < it.pages ? p.pages[(int64_t)it.b * p.table + it.first + i] : INT_MIN;
         };
         int32_t next = entry(begin);
-        int h_next = it.h, ve = 0;
-        bool fresh_next = true;
+        int h_next = it.h;
         uint32_t i = 0;
         bool ok = true;
         for (; i < n_tiles; ++i) {
             const int32_t e = next;
             const int h = h_next;
-            if (fresh_next) ve = 1;
-            fresh_next = false;
             if (i + 1 < n_tiles) {
                 const int x = begin + (int)i + 1;
                 if (x >= it.begin + it.tiles) {
                     at_next(it, p, R, PG);
-                    fresh_next = true;
                     h_next = it.h;
                 }
                 next = entry(x);
@@ -692,19 +707,18 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
             }
             if (!ok) break;
             AtNote *const note = reinterpret_cast<AtNote *>(sm + M::note) + i % kAtNotes;
-            ve = max(ve, (int)__reduce_max_sync(kFull, scales.y > 0.f ? min((__float_as_uint(scales.y) >> 23) + 1u, 253u) : 0u));
+            // A scale of 0 stands for zeros whatever the codes are: scores of 0 (times 0, FLT_MIN in the softmax, so that hidden
+            // columns stay -inf), weights that are 0 in FP16 (at kAtLowest) but count in the sum.
+            const int ve = scales.y > 0.f ? (int)min((__float_as_uint(scales.y) >> 23) + 1u, 253u) : kAtNoScale;
+            const int top = __reduce_max_sync(kFull, ve);
             if (lane < PG) {
-                // A scale of 0 stands for zeros whatever the codes are: scores of 0 (times 0, FLT_MIN in the softmax, so
-                // that hidden columns stay -inf), weights that are 0 in FP16 but count in the sum.  So value scales below
-                // 2^-70 of the unit count as that: u = 2^-60, weights below 2^-54, less than half of FP16's smallest.
-                const float rel = fmaxf(scales.y * __uint_as_float((uint32_t)(254 - ve) << 23), 8.4703294725430034e-22f);
-                const float u = rel * 1024.f;
+                const float m = scales.y > 0.f ? __log2f(scales.y * __uint_as_float((uint32_t)(254 - ve) << 23)) : 0.f;
                 note->factor[lane] = scales.x;
-                note->weight[lane] = __log2f(u);
-                note->back[lane] = 1.f / u;
+                note->weight[lane] = rintf(m * 32768.f) * (1.f / 32768.f) + (float)(10 + ve - top);
+                note->e[lane] = ve;
             }
             if (lane == 0) {
-                note->e = ve;
+                note->top = top;
                 note->hidden = (int)(~shown & ((1u << PG) - 1u));
             }
             __syncwarp();

@@ -74,3 +74,32 @@ def test_zeros_appended_behind_tokens_that_nothing_wrote(dtype, T):
             want[held[b]:] = 0
             assert torch.equal(got[b].cpu(), want)
             assert not got[b, :start[b]].any()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("H,Hk,d", [(8, 2, 64), (8, 2, 128), (16, 2, 256), (32, 1, 128)])
+@pytest.mark.parametrize("T,window", [(2, None), (6, None), (30, None), (90, None), (90, 40), (6, 60), (1, 60)])
+def test_unseen_values_change_nothing(dtype, H, Hk, d, T, window):
+    """A page whose values are larger by 1e30, in the middle of a context: the queries before it and those whose window
+    has left it behind give the same bits as without it, the others its values."""
+    layout = damp.CacheLayout(H, Hk, d)
+    pool, pages = filled(layout, 3, 10, d + T)
+    large = pool.clone()
+    q = (1.5 * randn(gen(T), 3, T, H, d)).to(dtype)
+    held, at = [260, 255 + max(T, 4) // 2, 286], [8, 8, 6 if window else 8]
+    for b in range(3):
+        scales_of(large, d)[pages[b, at[b]].long(), :, 1] *= 1e30
+    seen = torch.zeros(3, T, dtype=torch.bool)
+    for b in range(3):
+        for t in range(T):
+            last = held[b] - T + t
+            first = max(0, last - window + 1) if window else 0
+            seen[b, t] = first < 32 * (at[b] + 1) and last >= 32 * at[b]
+    wide = torch.cat((pages, torch.full((3, 70), -1, dtype=torch.int32, device=DEV)), 1)
+    for table in (pages, wide):
+        a = damp.cache_attend(layout, large, q, table, i32(held), window=window)
+        b = damp.cache_attend(layout, pool, q, table, i32(held), window=window)
+        assert not seen.all()
+        assert torch.equal(a[~seen], b[~seen]) and b[~seen].any(-1).all()
+        want, bounds = R.attend(R.Cache(large, d), q, pages.cpu(), held, window=window)
+        R.check_attend(a, want, bounds, max(held), d, "large values")
