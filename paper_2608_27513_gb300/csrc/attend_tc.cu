@@ -664,9 +664,11 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
     } else if (begin < end) {
         if (warp == 14) {
         // ---- the pages' copies, and what the softmax needs of them: lane = page of a tile ----
+        bool there_next;  // lane is a page of the tile
         auto entry = [&](int x) {  // of tile x, which lies in `it`
             const int i = (x - it.begin) * PG + lane;
-            return lane < PG && i < it.pages ? p.pages[(int64_t)it.b * p.table + it.first + i] : INT_MIN;
+            there_next = lane < PG && i < it.pages;
+            return there_next ? p.pages[(int64_t)it.b * p.table + it.first + i] : -1;
         };
         int32_t next = entry(begin);
         int h_next = it.h;
@@ -675,6 +677,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
         for (; i < n_tiles; ++i) {
             const int32_t e = next;
             const int h = h_next;
+            const bool there = there_next;
             if (i + 1 < n_tiles) {
                 const int x = begin + (int)i + 1;
                 if (x >= it.begin + it.tiles) {
@@ -685,8 +688,8 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
             }
             const int64_t slot = cache_page(e, p.num_pages);
             const uint8_t *const record = p.pool + (slot * p.Hk + h) * cache_record_bytes(D);
-            if (slot < 0 && e != INT_MIN && lane < PG) atomicOr(p.status, kDevBadSlot);
-            const bool here = lane < PG && slot >= 0;
+            if (there && slot < 0) atomicOr(p.status, kDevBadSlot);
+            const bool here = there && slot >= 0;
             const unsigned shown = __ballot_sync(kFull, here);
             float2 scales = make_float2(0.f, 0.f);
             if (here) scales = *reinterpret_cast<const float2 *>(record + 2 * cache_rows_bytes(D));

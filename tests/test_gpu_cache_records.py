@@ -103,3 +103,19 @@ def test_unseen_values_change_nothing(dtype, H, Hk, d, T, window):
         assert torch.equal(a[~seen], b[~seen]) and b[~seen].any(-1).all()
         want, bounds = R.attend(R.Cache(large, d), q, pages.cpu(), held, window=window)
         R.check_attend(a, want, bounds, max(held), d, "large values")
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("T", [1, 6, 40])
+def test_every_bad_page_is_reported(dtype, T):
+    """Entries outside the pool at both ends of their range."""
+    layout = damp.CacheLayout(8, 2, 64)
+    pool, pages = filled(layout, 1, 4, T)
+    q = randn(gen(1), 1, T, 8, 64).to(dtype)
+    for bad in (-2**31, -2**31 + 1, -1, pool.shape[0], 2**31 - 1):
+        table = pages.clone()
+        table[0, 2] = bad
+        o = damp.cache_attend(layout, pool, q, table, i32([128]))
+        assert damp.device_status() == damp.DEV_BAD_SLOT, bad
+        want, bounds = R.attend(R.Cache(pool, 64), q, table.cpu(), [128])
+        R.check_attend(o, want, bounds, 128, 64, "bad pages")
