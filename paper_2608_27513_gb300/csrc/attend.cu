@@ -156,7 +156,7 @@ struct AttRows {
             top = quad_max(top);
             const int e = min(max((int)(__float_as_uint(top) >> 23), 15), 254);  // up to below 2^15
             up[hh] = __uint_as_float((uint32_t)(268 - e) << 23);
-            factor[hh] = p.scale * kLog2e / up[hh];
+            factor[hh] = p.scale * (kLog2e * __uint_as_float((uint32_t)(e - 14) << 23));  // over up: the scale meets its inverse first
             m[hh] = -INFINITY;
             l[hh] = 0.f;
         }

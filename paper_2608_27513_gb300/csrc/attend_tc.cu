@@ -394,7 +394,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
                     top = __vmaxu2(top, __shfl_xor_sync(kFull, top, 16));
                     const int e = min(max((int)(max(top >> 16, top & 0xffffu) >> 7), 15), 254);
                     const float up = __uint_as_float((uint32_t)(268 - e) << 23);
-                    if ((lane >> 3) == g) factor = p.scale * kLog2e / up;  // of this thread's own row
+                    if ((lane >> 3) == g) factor = p.scale * (kLog2e * __uint_as_float((uint32_t)(e - 14) << 23));  // over up, of this thread's own row
 #pragma unroll
                     for (int i = 0; i < kC; ++i) {
                         const uint32_t u[4] = {v[i].x, v[i].y, v[i].z, v[i].w};

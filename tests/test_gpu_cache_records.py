@@ -119,3 +119,17 @@ def test_every_bad_page_is_reported(dtype, T):
         assert damp.device_status() == damp.DEV_BAD_SLOT, bad
         want, bounds = R.attend(R.Cache(pool, 64), q, table.cpu(), [128])
         R.check_attend(o, want, bounds, 128, 64, "bad pages")
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("T", [1, 40])
+@pytest.mark.parametrize("scale,qsize,ksize", [(3e38, 1e-30, 1e-9), (1e-44, 1e30, 1e13), (1.2e-38, 1e20, 1e17)])
+def test_extreme_scales(dtype, T, scale, qsize, ksize):
+    """The largest and the smallest factors of q.k, with logits of ordinary size."""
+    layout = damp.CacheLayout(4, 2, 64)
+    pool, pages = damp.new_cache(layout, 3, DEV), i32([[2, 0, 1]])
+    g = gen(T)
+    k, v = ksize * randn(g, 1, 96, 2, 64), randn(g, 1, 96, 2, 64)
+    damp.cache_append(layout, pool, k, v, pages, i32([0]))
+    q = qsize * randn(g, 1, T, 4, 64)
+    run_attend(layout, pool, pages, q.to(dtype), [96], "extreme scales", scale=torch.tensor(scale, dtype=F32).item())
