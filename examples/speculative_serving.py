@@ -8,8 +8,9 @@ softmax-attention layers between them (an 8-bit cache) with random weights serve
             step; copy_slots takes its state back; all layers run the drafted tokens as one chunk;
             verify_drafts accepts a prefix and draws the next token; copy_slots takes the states
             back and the chunk runs once more over the accepted tokens, whose numbers
-            (verify_drafts' counts) are the chunk's lengths on the device.  A cache needs no saved
-            copy: a request goes back to the number of tokens it held, later tokens are written over
+            (verify_drafts' counts) are the chunk's lengths on the device.  Of a cache the page that
+            the next token goes into is saved and taken back: a request's later tokens are written
+            over, but a rejected token may have made that page's scale larger and its codes coarser
   end       zero_slots frees finished requests, compact_slots closes the pools up
 
     python examples/speculative_serving.py [--layers lin,gdn,attn,lin] [--batch 8] [--drafts 4]
@@ -103,7 +104,6 @@ class Server:
         self.layers = [AttentionLayer(width, 2 * slots, self.gen, device) if k == "attn" else Layer(k, width, 2 * slots, self.gen, device)
                        for k in kinds]
         self.pools = [layer.pool for layer in self.layers]
-        self.states = [layer.pool for layer in self.layers if isinstance(layer, Layer)]  # what a round saves
         self.held = torch.empty(0, dtype=torch.int32, device=device)  # tokens that have run
         self.slot_idx = torch.empty(0, dtype=torch.int32, device=device)
 
@@ -126,13 +126,23 @@ class Server:
         self.held = (lengths - 1).to(torch.int32)
         self.last = tokens.gather(1, lengths.long()[:, None] - 1).to(torch.int32)
 
-    @staticmethod
-    def copy(pools, src, dst):
-        if pools:  # (a model of softmax-attention layers alone has no state to save)
-            damp.copy_slots(pools, src, dst)
+    def save(self):
+        """Copies what a round changes of every layer: its state, of a cache the page that the next token goes into (later
+        ones are begun anew)."""
+        self._copy(self.layers, self.slot_idx, self.slot_idx + self.slots)
 
-    def saved(self):
-        return self.slot_idx + self.slots
+    def restore(self, layers):
+        self._copy(layers, self.slot_idx + self.slots, self.slot_idx)
+
+    def _copy(self, layers, src, dst):
+        states = [layer.pool for layer in layers if isinstance(layer, Layer)]
+        caches = [layer.cache for layer in layers if isinstance(layer, AttentionLayer)]
+        if states:
+            damp.copy_slots(states, src, dst)
+        if caches:
+            n = AttentionLayer.PAGES
+            page = (self.held // damp.CACHE_PAGE).clamp(max=n - 1)
+            damp.copy_slots(caches, src * n + page, dst * n + page)
 
     def draw(self, logits, temperature):
         noise = torch.empty_like(logits).exponential_(generator=self.gen)
@@ -141,21 +151,21 @@ class Server:
 
     def round(self, drafts, temperature):
         """One round for every request: (tokens [B, drafts + 1], count [B])."""
-        B, saved = self.slot_idx.shape[0], self.saved()
-        self.copy(self.states, self.slot_idx, saved)
+        B = self.slot_idx.shape[0]
+        self.save()
         token, drafted, q = self.last, [], []
         for i in range(drafts):
             q.append(self.logits(token, depth=1, ahead=i))
             token = self.draw(q[-1][:, 0], temperature)
             drafted.append(token)
-        self.copy([p for p in self.states if p is self.pools[0]], saved, self.slot_idx)
+        self.restore(self.layers[:1])
         chunk = torch.cat([self.last] + drafted, 1)
         target = self.logits(chunk)
         u = torch.rand(B, drafts, generator=self.gen, device=self.device)
         noise = torch.empty(B, self.vocab, device=self.device).exponential_(generator=self.gen)
         tokens, count = damp.verify_drafts(target, torch.cat(drafted, 1), u, noise, draft_logits=torch.cat(q, 1),
                                            temperature=temperature)
-        self.copy(self.states, saved, self.slot_idx)
+        self.restore(self.layers)
         self.logits(chunk, lengths=count)
         self.held = self.held + count
         # logits that exclude every token give none (count 0): the request stays where it was

@@ -479,8 +479,11 @@ typedef struct {
  *   the page's earlier scale s0 (0 if the page has no earlier token):  s = max(a / 127, s0)
  *   (0 below 2^-126), r = 1 / s, code = 128 + rne(x r); where s > s0 the earlier codes become
  *   128 + rne((c - 128) (s0 r)).  Each operation is rounded to FP32 (codes depend on how the
- *   tokens of a page were split into calls, by half a step for each growth).  NaN is stored as
- *   0, an infinity as the block's largest magnitude; both set DAMP_DEV_NOT_FINITE.
+ *   tokens of a page were split into calls, by half a step for each growth).  A page's scale only
+ *   grows until a call writes its first token: tokens that are taken back (start lowered, a rejected
+ *   draft) leave it, and the codes as they were rounded to it; a copy of the open page
+ *   (damp_copy_slots) made before and put back undoes that.  NaN is stored as
+ *   0, an infinity as the largest that the scale holds, 127 s; both set DAMP_DEV_NOT_FINITE.
  *   The pages that a call writes must be distinct.  T up to 2^30.
  * damp_cache_read: k, v [batch][T][num_kv_heads][d] of dtype (contiguous, 16-B aligned) become
  *   the values of tokens start[b] + t (start NULL: t), zeros from lengths[b] on (the tokens

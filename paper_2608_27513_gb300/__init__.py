@@ -950,7 +950,11 @@ def cache_append(layout, cache, k, v, pages, start, lengths=None, stream=None):
     """Write new tokens into the 8-bit cache (in place): k, v [B, T, H_kv, d] bfloat16 or float32; token t of
     row b becomes token start[b] + t of the row (start int32 [B]: the tokens it holds), whose page is
     pages[b, (start[b] + t) // CACHE_PAGE] (int32 [B, W]).  Row b has lengths[b] new tokens (default T).
-    k and v may be slices of the heads of one projection.  The pages written must be distinct."""
+    k and v may be slices of the heads of one projection.  The pages written must be distinct.
+
+    Tokens are taken back by a smaller start; the page that then is open keeps the scale that they gave it, and its
+    codes the rounding.  To leave no trace of them (a rejected draft), copy that page before (copy_slots) and
+    put it back."""
     import torch
     if k is None or k.dim() != 4:
         raise ValueError("k must be a [B, T, num_kv_heads, d] tensor")
