@@ -430,7 +430,8 @@ DAMP_API damp_status damp_verify_drafts(const void *target_logits, const void *d
  * damp_rotary: turns the first rotary_dim values of every head by the token's position.  Pair
  *   i, (x_i, x_{i + rotary_dim/2}) or with `interleaved` (x_2i, x_{2i+1}), becomes
  *   scale (a cos t - b sin t, b cos t + a sin t), t = position * freq[i]; the other values of
- *   a head are copied.  The angle is exact modulo a turn for any position.
+ *   a head are copied.  The angle is that of the double freq[i], modulo a turn, to 2^-64 of a turn per position,
+ *   for any position and frequencies below 2^64.
  *   q, k        [tokens][heads or kv_heads][d] of dtype, q_stride / k_stride elements from token
  *               to token (heads d at least); k may be NULL with kv_heads 0
  *   positions   int32 [batch][T] (tokens = batch T), or [batch] if positions_per_row is not 0:

@@ -6,9 +6,11 @@
 // its threads then walk over the heads of q and k with 16-byte loads and stores.
 //
 // Angles.  position * f in 32 bits loses 2^-24 of the whole angle, 0.06 radians at position 2^20.
-// Here f / 2 pi becomes a fixed-point fraction of a turn in 64 bits, and its product with the
-// position modulo 2^64 keeps the fraction exactly: 2^-64 of a turn per position, whatever the
-// position.  The upper 32 bits of it, as a signed number of half turns, go to sincospif.
+// Here f / 2 pi becomes a fixed-point fraction of a turn in 64 bits, by integers from the double's own bits and 128 bits
+// of 1 / 2 pi (in doubles the product is off by up to 2^-56 of a turn, 2^-25 at position 2^31), and its product
+// with the position modulo 2^64 keeps the fraction exactly: 2^-64 of a turn per position, whatever
+// the position.  What is left of it after quarter turns, half a quarter at most, goes to sincospif: rounding it
+// to FP32 costs 2^-24 of that rest (of a whole turn's range it cost up to 2^-25 half turns).
 //
 // Bound by the bytes (each value read and written once): 4 rows of 2048 tokens, 32 and 8 heads, d = 128, BF16, take
 // 29 us, 5.8 TB/s; a single token 1.9 us, a launch.
@@ -24,11 +26,34 @@ namespace {
 constexpr int kRotThreads = 256;
 constexpr int kRotPairs = 512;   // cosines and sines of a CTA
 
-// the fraction of a turn per position, in units of 2^-64
+// The fraction of a turn per position, f / 2 pi, in units of 2^-64.  f = m 2^(e - 1086) with a mantissa m of 64 bits,
+// 1 / 2 pi = c 2^-130 with c of 128 bits, of whose product the upper 128 bits are taken.
 __device__ __forceinline__ uint64_t turns_of(double f) {
-    const double t = f * 0.15915494309189533577;  // 1 / 2 pi
-    const double u = t - floor(t);
-    return u < 1.0 ? __double2ull_rz(u * 18446744073709551616.0) : 0ull;  // (NaN: 0)
+    constexpr uint64_t c_hi = 0xa2f9836e4e441529ull, c_lo = 0xfc2757d1f534ddc0ull;
+    const uint64_t bits = (uint64_t)__double_as_longlong(f);
+    const int e = (int)(bits >> 52) & 0x7ff;
+    const uint64_t m = (bits << 11) | (1ull << 63);
+    const uint64_t low = __umul64hi(m, c_lo), mid = m * c_hi;
+    const uint64_t lo = mid + low, hi = __umul64hi(m, c_hi) + (lo < low ? 1 : 0);  // f / 2 pi = (hi, lo) 2^(e - 1152)
+    const int right = 1088 - e;  // places to units of 2^-64; 65 for f = 1
+    uint64_t t = 0;
+    if (e == 0x7ff || right >= 129) t = 0;  // not finite; below 2^-65 turns
+    else if (right > 64) t = ((hi >> (right - 65)) + 1) >> 1;  // to the nearest
+    else if (right == 64) t = hi;
+    else if (right > 0) t = (hi << (64 - right)) | (lo >> right);
+    else if (right > -64) t = lo << -right;  // (frequencies from 2^65 on: the bits of 1 / 2 pi run out)
+    return bits >> 63 ? 0 - t : t;
+}
+// cosine and sine of an angle in units of 2^-64 turns
+__device__ __forceinline__ void sincos_of(uint64_t turn, float &s, float &c) {
+    const uint32_t quarter = (uint32_t)((turn + (1ull << 61)) >> 62);  // (4 is 0)
+    const int32_t rest = (int32_t)((int64_t)(turn - ((uint64_t)quarter << 62)) >> 30);  // of 2^-34 turns, an eighth at most
+    float a, b;
+    sincospif((float)rest * 1.1641532182693481e-10f, &a, &b);  // half turns: 2^-33
+    s = quarter & 1 ? b : a;
+    c = quarter & 1 ? a : b;
+    if (quarter & 2) s = -s;
+    if ((quarter + 1) & 2) c = -c;
 }
 
 template <int V>
@@ -81,9 +106,8 @@ __global__ void __launch_bounds__(kRotThreads) rotary_kernel(const RotaryArgs p,
         const int64_t token = t0 + t;
         const int64_t row = p.per_row ? token / p.T : token;
         const int64_t pos = (int64_t)p.positions[row] + (p.per_row ? token - row * p.T : 0);
-        const uint64_t turn = turns_of(p.freq[j]) * (uint64_t)pos;
         float s, c;
-        sincospif((float)(int32_t)(turn >> 32) * 4.656612873077393e-10f, &s, &c);  // half turns: 2^-31
+        sincos_of(turns_of(p.freq[j]) * (uint64_t)pos, s, c);
         cs[i] = p.scale * c;
         sn[i] = p.scale * s;
     }
