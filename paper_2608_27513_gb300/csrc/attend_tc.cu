@@ -833,13 +833,19 @@ bool attend_tc_takes(const AttendArgs &a) { return a.in_bf16 && (int64_t)a.T * (
 
 int attend_tc_rows(const AttendArgs &a) { return a.d <= 128 && (int64_t)a.T * (a.H / a.Hk) > 128 ? 256 : 128; }
 
-// Ranges end with items where that leaves them even (8 items per SM) or items are short (4 key tiles): no parts,
-// one launch (16 rows of up to 1000 queries in up to 1500 tokens, 2016 items: 291 us against 305 with parts at that
-// state of the kernel).
+// Ranges end with items, no parts and one launch, where no item can be long: 4 key tiles, or twice as many as there are
+// items per SM (8 at least), so that the longest adds little to what an SM has anyway.  The lengths are not known here: a
+// table's width and the window bound an item.  Whole items against parts, even lengths and ragged ones, us: 16 rows of
+// 1000 queries, 32 heads, 16 KV, window 512 273 / 328 and 278 / 338; 10 of 256 in 1000 tokens 65 / 66 and 71 / 73;
+// 320 of 5 in 1000, 32 heads, 8 KV 265 / 252 and 269 / 250, in 4000 822 / 562 and 840 / 543; but 256 rows of 5, one in
+// 131072 tokens and the others in 1000: 1376 and 322.  256 rows of 5 in 1000 tokens each under a table of 4096 pages, which
+// could hold such a row, pay for it: 218 and 228.
 bool attend_tc_whole(const AttendArgs &a) {
     const int64_t G = a.H / a.Hk, R = attend_tc_rows(a), items = (int64_t)a.batch * (((int64_t)a.T * G + R - 1) / R) * a.Hk;
-    const int tile = a.d == 256 ? 2 : 4;  // pages
-    return (a.table + tile - 1) / tile <= 4 || items >= 8 * (int64_t)sm_count();
+    const int64_t keys = a.window ? (int64_t)a.window + R / G + 1 : 32 * (int64_t)a.table;  // of an item
+    const int64_t tile = a.d == 256 ? 2 : 4, pages = std::min<int64_t>(a.table, (keys + kCachePage - 2) / kCachePage + 1);
+    const int64_t tiles = (pages + tile - 1) / tile;
+    return tiles <= 4 || (items >= 8 * (int64_t)sm_count() && tiles * sm_count() <= 2 * items);
 }
 
 cudaError_t launch_attend_tc(AttendArgs a, int grid, cudaStream_t s) {
