@@ -645,6 +645,19 @@ DAMP_API damp_status damp_test_kda_wait_timeout(const damp_layout *layout, void 
                                                 const void *q, const void *k, const void *v, const float *g,
                                                 const float *beta, float *o, int32_t in_dtype, void *stream);
 
+/*
+ * Test hook for the bounded waits of damp_cache_attend, as the one above: in every second range of the work (a
+ * warp's, a CTA's) the barriers of the pages, or if `queries` is not 0 of the queries (many rows), expect 16
+ * bytes more than is copied, with the wait limit cut to 10 ms.  What a range that gave up should have
+ * written stays as it was, or becomes NaN where another range holds a part of it;
+ * DAMP_DEV_WAIT_TIMEOUT is set.  Arguments as damp_cache_attend; d = 128 and BF16 alone (DAMP_ERR_SHAPE).
+ */
+DAMP_API damp_status damp_test_cache_attend_wait_timeout(const damp_cache_layout *layout, const void *cache, int64_t num_pages,
+                                                         const int32_t *pages, int32_t table, int32_t batch, int32_t T,
+                                                         const int32_t *lengths, const int32_t *q_lengths, const void *q,
+                                                         int64_t q_stride, float scale, int32_t window, void *o, int32_t dtype,
+                                                         void *workspace, int64_t workspace_bytes, int32_t queries, void *stream);
+
 /* Reads and clears the device status word of the current device (DAMP_DEV_* bits).
  * It first waits for all work on the current device (cudaDeviceSynchronize: the one
  * call of libdamp that synchronizes), so every kernel enqueued before the call, on

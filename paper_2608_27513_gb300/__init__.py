@@ -42,7 +42,7 @@ __all__ = [
     "head_groups", "test_kda_wait_timeout", "gdn_decode_step_groups", "kda_decode_step_groups",
     "calib_accumulate", "lin_decode_step", "lin_prefill_chunk", "copy_slots", "zero_slots", "compact_slots",
     "verify_drafts", "DEV_BAD_TOKEN", "CacheLayout", "CACHE_PAGE", "new_cache", "cache_page_bytes", "cache_append",
-    "cache_read", "cache_attend", "rotary", "rotary_frequencies", "DEV_NOT_FINITE",
+    "cache_read", "cache_attend", "test_cache_attend_wait_timeout", "rotary", "rotary_frequencies", "DEV_NOT_FINITE",
 ]
 
 LO_U8_AFFINE_G32_H32 = 0
@@ -1044,6 +1044,24 @@ def cache_attend(layout, cache, q, pages, lengths, q_lengths=None, scale=None, w
     if status:
         raise DampError(status, "damp_cache_attend")
     return o
+
+
+def test_cache_attend_wait_timeout(layout, cache, q, pages, lengths, o, queries=False):
+    """The bounded-wait test hook of cache_attend (damp_test_cache_attend_wait_timeout): in every second range of the work
+    the waits for pages (or for queries) run out after 10 ms.  For tests of the timeout path only."""
+    import torch
+    B, T, dt = q.shape[0], q.shape[1], IN_BF16 if q.dtype == torch.bfloat16 else IN_FP32
+    dev = _call_device(torch, q)
+    shape = (B, T, layout.num_heads, layout.d)
+    pool, n, table, W = _cache(layout, cache, pages, B, dev, torch.int32, torch.uint8)
+    need = lib().damp_cache_attend_workspace(layout._shared[1], B, T, W, dt)
+    ws = torch.empty(need, dtype=torch.uint8, device=q.device)
+    status = lib().damp_test_cache_attend_wait_timeout(
+        layout._shared[1], pool, n, table, W, B, T, _here("lengths", lengths, (B,), torch.int32, dev), None,
+        _here("q", q, shape, q.dtype, dev), layout.num_heads * layout.d, layout.d ** -0.5, 0, _here("o", o, shape, q.dtype, dev), dt,
+        ws.data_ptr(), need, bool(queries), _raw_stream(torch, None, dev))
+    if status:
+        raise DampError(status, "damp_test_cache_attend_wait_timeout")
 
 
 def device_status() -> int:

@@ -68,6 +68,7 @@ SIGNATURES = {
     "damp_cache_append": (_status, [_C, _P, _i64, _P, _i32, _i32, _i32, _P, _P, _P, _i64, _P, _i64, _i32, _P]),
     "damp_cache_read": (_status, [_C, _P, _i64, _P, _i32, _i32, _i32, _P, _P, _P, _P, _i32, _P]),
     "damp_cache_attend": (_status, [_C, _P, _i64, _P, _i32, _i32, _i32, _P, _P, _P, _i64, ctypes.c_float, _i32, _P, _i32, _P, _i64, _P]),
+    "damp_test_cache_attend_wait_timeout": (_status, [_C, _P, _i64, _P, _i32, _i32, _i32, _P, _P, _P, _i64, ctypes.c_float, _i32, _P, _i32, _P, _i64, _i32, _P]),
     "damp_cache_attend_workspace": (_i64, [_C, _i32, _i32, _i32, _i32]),
     "damp_quantize_state": (_status, [_L, _P, _P, _P, _i64, _P, _i32, _P]),
     "damp_dequantize_state": (_status, [_L, _P, _i64, _P, _i32, _P, _P, _P]),

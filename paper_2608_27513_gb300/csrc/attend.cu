@@ -373,7 +373,7 @@ struct AttPage {  // a page of the sequence, 32 bytes
     int bad, unused;
 };
 
-template <int D, bool F32>
+template <int D, bool F32, bool TEST>
 __global__ void __launch_bounds__(AttCfg<D, F32>::threads, 1) attend_kernel(const AttendArgs p) {
     using C = AttCfg<D, F32>;
     constexpr int R = C::R;
@@ -445,7 +445,7 @@ __global__ void __launch_bounds__(AttCfg<D, F32>::threads, 1) attend_kernel(cons
                 atomicOr(p.status, kDevBadSlot);
                 mbar_arrive_expect_tx(bar, 0);
             } else {
-                mbar_arrive_expect_tx(bar, C::rec);
+                mbar_arrive_expect_tx(bar, C::rec + att_extra<TEST>(p, range, 1));
                 bulk_g2s(ring + stage * C::rec, my_record, C::rec, bar);
             }
         }
@@ -476,12 +476,12 @@ __global__ void __launch_bounds__(AttCfg<D, F32>::threads, 1) attend_kernel(cons
             __syncwarp();  // the stage that is filled next has been read by all lanes
             if (ahead < end) fetch(ahead, stage == 0 ? C::stages - 1 : stage - 1);
         }
-        if (!mbar_wait_bounded(bars + 8 * stage, parity)) failed = true;
+        if (!mbar_wait_bounded(bars + 8 * stage, parity, kAttWait<TEST>)) failed = true;
         if (__any_sync(kFull, failed)) {
             failed = true;
             for (int x = f + 1; x < min(end, f + C::stages); ++x) {  // the other copies in flight
                 if (++stage == C::stages) stage = 0, parity ^= 1u;
-                mbar_wait_bounded(bars + 8 * stage, parity);
+                mbar_wait_bounded(bars + 8 * stage, parity, kAttWait<TEST>);
             }
             break;
         }
@@ -498,7 +498,11 @@ __global__ void __launch_bounds__(AttCfg<D, F32>::threads, 1) attend_kernel(cons
             parity ^= 1u;
         }
     }
-    if (failed && lane == 0) atomicOr(p.status, kDevWaitTimeout);
+    if (failed) {  // the join finds no part of an item that this range should have left, and makes NaN of it
+        if (lane == 0) atomicOr(p.status, kDevWaitTimeout);
+        work.ml[(int64_t)2 * range * R + lane] = make_float2(NAN, NAN);
+        static_assert(2 * R == 32, "both parts");
+    }
     // All warps of a CTA inside one item (a long context): their parts become one.
     __shared__ int tails[C::warps];
     const bool open = !failed && item >= 0 && !(now.begin >= begin && now.begin + now.count <= end);
@@ -545,7 +549,7 @@ __global__ void __launch_bounds__(AttCfg<D, F32>::threads, 1) attend_kernel(cons
 
 // A CTA per item, for contexts so short that its warps alone read them in the time that a second launch takes:
 // warp w has every C::warps-th page from w on, and the CTA joins the warps' parts and writes all of the item's rows.
-template <int D, bool F32>
+template <int D, bool F32, bool TEST>
 __global__ void __launch_bounds__(AttCfg<D, F32>::threads, 1) attend_items_kernel(const AttendArgs p, int tiles, int items) {
     using C = AttCfg<D, F32>;
     constexpr int R = C::R;
@@ -576,7 +580,7 @@ __global__ void __launch_bounds__(AttCfg<D, F32>::threads, 1) attend_items_kerne
                     atomicOr(p.status, kDevBadSlot);
                     mbar_arrive_expect_tx(bar, 0);
                 } else {
-                    mbar_arrive_expect_tx(bar, C::rec);
+                    mbar_arrive_expect_tx(bar, C::rec + att_extra<TEST>(p, blockIdx.x, 1));
                     bulk_g2s(ring + s * C::rec, p.pool + (slot * p.Hk + h) * C::rec, C::rec, bar);
                 }
             }
@@ -586,11 +590,11 @@ __global__ void __launch_bounds__(AttCfg<D, F32>::threads, 1) attend_items_kerne
         if (n) rows.start(p, w, b, rt, h, qs, lane);
         for (int k = 0; k < n; ++k) {
             const uint32_t s = (seq + k) % C::stages;
-            if (!mbar_wait_bounded(bars + 8 * s, ((seq + k) / C::stages) & 1)) failed = true;
+            if (!mbar_wait_bounded(bars + 8 * s, ((seq + k) / C::stages) & 1, kAttWait<TEST>)) failed = true;
             if (__any_sync(kFull, failed)) {
                 failed = true;
                 for (int y = k + 1; y < min(n, k + C::stages); ++y)  // the other copies in flight
-                    mbar_wait_bounded(bars + 8 * ((seq + y) % C::stages), ((seq + y) / C::stages) & 1);
+                    mbar_wait_bounded(bars + 8 * ((seq + y) % C::stages), ((seq + y) / C::stages) & 1, kAttWait<TEST>);
                 break;
             }
             if (!((bad >> k) & 1)) rows.page(p, ring + s * C::rec, it.first + warp + C::warps * k, qs, lane);
@@ -600,9 +604,9 @@ __global__ void __launch_bounds__(AttCfg<D, F32>::threads, 1) attend_items_kerne
         seq += n;
         static_assert(R * (D + 2) * 4 <= C::ring, "parts");
         if (n) rows.leave(p, b, rt, h, false, reinterpret_cast<float *>(mine), reinterpret_cast<float2 *>(mine + R * D * 4), lane);
-        __syncthreads();
+        const bool lost = __syncthreads_or(failed);  // rows without all of their pages are not written
         const int parts = min(C::warps, it.pages);
-        for (int i = threadIdx.x; i < R * (D / 4); i += C::threads) {
+        for (int i = threadIdx.x; i < R * (D / 4) && !lost; i += C::threads) {
             const int r = i / (D / 4), col = 4 * (i - r * (D / 4)), row = rt * R + r, t = att_div(p, row);
             if (t >= p.T) break;
             float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -835,23 +839,23 @@ bool att_by_items(const AttendArgs &a) {
     return a.table <= kItemWarpPages * (a.d == 256 ? 4 : 8) && att_items(a, 16) <= 2 * (int64_t)sm_count();
 }
 
-template <int D, bool F32>
+template <int D, bool F32, bool TEST>
 cudaError_t launch_as(const AttendArgs &a, cudaStream_t s) {
     using C = AttCfg<D, F32>;
     static_assert(kItemWarpPages <= 32 && (C::warps == 4) == (D == 256), "a page per lane");
     if (att_by_items(a)) {
         const int smem = C::warps * C::warp_bytes;
-        const cudaError_t e = ensure_smem_limit(reinterpret_cast<const void *>(attend_items_kernel<D, F32>), smem);
+        const cudaError_t e = ensure_smem_limit(reinterpret_cast<const void *>(attend_items_kernel<D, F32, TEST>), smem);
         if (e != cudaSuccess) return e;
         const int items = (int)att_items(a, C::R);
-        attend_items_kernel<D, F32><<<std::min(items, sm_count()), C::threads, smem, s>>>(a, (int)(items / a.Hk / a.batch), items);
+        attend_items_kernel<D, F32, TEST><<<std::min(items, sm_count()), C::threads, smem, s>>>(a, (int)(items / a.Hk / a.batch), items);
         return cudaGetLastError();
     }
     const int smem = C::warps * C::warp_bytes + (a.batch + 1) * 4;
-    cudaError_t e = ensure_smem_limit(reinterpret_cast<const void *>(attend_kernel<D, F32>), smem);
+    cudaError_t e = ensure_smem_limit(reinterpret_cast<const void *>(attend_kernel<D, F32, TEST>), smem);
     if (e != cudaSuccess) return e;
     const int grid = sm_count();
-    attend_kernel<D, F32><<<grid, C::threads, smem, s>>>(a);
+    attend_kernel<D, F32, TEST><<<grid, C::threads, smem, s>>>(a);
     e = cudaGetLastError();
     return e != cudaSuccess ? e : launch_join<D, !F32>(a, C::R, grid * C::warps, s);
 }
@@ -861,7 +865,11 @@ cudaError_t launch_d(const AttendArgs &a, cudaStream_t s) {
         const cudaError_t e = launch_attend_tc(a, sm_count(), s);
         return e != cudaSuccess || attend_tc_whole(a) ? e : launch_join<D, true>(a, attend_tc_rows(a), sm_count(), s);
     }
-    return a.in_bf16 ? launch_as<D, false>(a, s) : launch_as<D, true>(a, s);
+    if (a.test) {
+        if constexpr (D == 128) return a.in_bf16 ? launch_as<D, false, true>(a, s) : cudaErrorNotSupported;
+        return cudaErrorNotSupported;
+    }
+    return a.in_bf16 ? launch_as<D, false, false>(a, s) : launch_as<D, true, false>(a, s);
 }
 
 }  // namespace

@@ -42,6 +42,15 @@ __device__ __forceinline__ AttItem att_item(const AttendArgs &p, AttRow w, int r
 __device__ __forceinline__ int att_tiles(int n, int R, int G) { return (n * G + R - 1) / R; }
 __device__ __forceinline__ int att_units(int pages, int unit) { return (pages + unit - 1) / unit; }
 
+// limit of a wait; in the variant that tests the waits
+template <bool TEST>
+constexpr uint64_t kAttWait = TEST ? 10000000ull : 2000000000ull;
+// bytes that a barrier of range (or CTA) i expects beyond what is copied: none but in that variant
+template <bool TEST>
+__device__ __forceinline__ uint32_t att_extra(const AttendArgs &p, int i, int test) {
+    return TEST && p.test == test && (i & 1) ? 16u : 0u;
+}
+
 __device__ __forceinline__ float ex2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

@@ -241,13 +241,14 @@ __device__ __forceinline__ bool at_try_wait(uint32_t bar, uint32_t parity) {
                  : "memory");
     return ok != 0;
 }
-struct AtWait {  // bounded waits (about 2 s), all of which give up once one has
+template <bool TEST>
+struct AtWait {  // bounded waits, all of which give up once one has
     volatile uint32_t *dead;
     __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity) const {
         if (at_try_wait(bar, parity)) return true;
         const uint64_t t0 = global_timer_ns();
         for (uint32_t i = 0; !at_try_wait(bar, parity); ++i) {
-            if (*dead || global_timer_ns() - t0 > 2000000000ull || i >> 27) {
+            if (*dead || global_timer_ns() - t0 > kAttWait<TEST> || i >> 27) {
                 *dead = 1;
                 return false;
             }
@@ -256,12 +257,26 @@ struct AtWait {  // bounded waits (about 2 s), all of which give up once one has
     }
 };
 
-template <int D, int SUB>
+// What a CTA whose waits have run out does at its end (not inlined: the other code stays as it is).  Copies in flight end
+// before the shared memory does; the join finds no part of an item that this range should have left, and makes NaN of it.
+template <int STAGES>
+__device__ __noinline__ void at_lost(uint32_t *status, float2 *ml, int n, uint32_t rows_bar, uint32_t rows, uint32_t kc_bar, uint32_t vc_bar, uint32_t copied, uint32_t half, uint64_t limit) {
+    if (threadIdx.x == 0) atomicOr(status, kDevWaitTimeout);
+    if (rows) mbar_wait_bounded(rows_bar, rows - 1, limit);
+    for (uint32_t k = copied > STAGES ? copied - STAGES : 0; k < copied + half; ++k) {
+        mbar_wait_bounded(kc_bar + 8 * (k % STAGES), (k / STAGES) & 1, limit);
+        if (k < copied) mbar_wait_bounded(vc_bar + 8 * (k % STAGES), (k / STAGES) & 1, limit);
+    }
+    for (int i = threadIdx.x; i < n; i += kAtThreads) ml[i] = make_float2(NAN, NAN);
+}
+
+template <int D, int SUB, bool TEST>
 __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendArgs p) {
     using M = AtSmem<D, SUB>;
     constexpr int R = 128 * SUB, TN = M::tokens, PG = M::pages;
     extern __shared__ __align__(1024) uint8_t sm[];
-    __shared__ uint32_t s_dead, s_tmem;
+    __shared__ uint32_t s_dead, s_tmem, s_copied, s_half;  // tiles of codes that were copied, the keys of one more
+    __shared__ uint32_t s_rows[4 * SUB];  // 1 + the phase of a softmax warp's queries that it has given up
     __shared__ AtItem s_next[4 * SUB];  // a softmax warp's next item, kept out of its registers
     const uint32_t sb = smem_u32(sm);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -269,7 +284,8 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
     auto bar = [&](int i) { return sb + M::bar + 8 * i; };
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // the join waits for the end of this grid itself
     if (threadIdx.x == 0) {
-        s_dead = 0;
+        s_dead = s_half = s_copied = 0;
+        for (int i = 0; i < 4 * SUB; ++i) s_rows[i] = 0;
         for (int i = 0; i < 2; ++i) {
             mbar_init(bar(kBarQ + i), 4);
             mbar_init(bar(kBarDone + i), 1);
@@ -321,7 +337,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
     }
     if (begin < end) it = at_seek(p, before, begin, R, PG);
     __syncthreads();  // `before` is given up
-    const AtWait wait{&s_dead};
+    const AtWait<TEST> wait{&s_dead};
     auto together = [](bool ok) { return __all_sync(kFull, ok) != 0; };
     const uint32_t n_tiles = (uint32_t)(end - begin);  // of this range
     AttSplit split{0, 0, 0, -1, 0, {0, 0, 0}};  // (thread 0)
@@ -352,7 +368,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
                 const int64_t mine = live ? ((int64_t)it.b * p.T + t) * p.q_stride + (int64_t)head * D : -1;
                 const uint32_t q_bar = bar(kBarRows + warp), rows = sb + M::q + x * M::q_tile + (warp & 3) * (64 * D);
                 const unsigned some = __ballot_sync(kFull, live);
-                if (lane == 0) mbar_arrive_expect_tx(q_bar, __popc(some) * 2 * D);
+                if (lane == 0) mbar_arrive_expect_tx(q_bar, __popc(some) * 2 * D + att_extra<TEST>(p, blockIdx.x, 2));
                 __syncwarp();
                 if (live) {
                     fence_proxy_async_smem();  // (the item before was staged here)
@@ -372,7 +388,10 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
                     }
                 }
                 ok = together(wait(q_bar, items & 1));
-                if (!ok) break;
+                if (!ok) {
+                    if (lane == 0) s_rows[warp] = 1 + (items & 1);
+                    break;
+                }
 #pragma unroll 1
                 for (int g = 0; g < 4; ++g) {
                     // From rows to core matrices in the same 16 D bytes.  Lane = (row j, b = 4 i + its quarter): chunk
@@ -694,12 +713,15 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
             float2 scales = make_float2(0.f, 0.f);
             if (here) scales = *reinterpret_cast<const float2 *>(record + 2 * cache_rows_bytes(D));
             const uint32_t st = i % M::stages, lap = i / M::stages;
-            const uint32_t bytes = __popc(shown) * cache_rows_bytes(D);
+            const uint32_t bytes = __popc(shown) * cache_rows_bytes(D) + att_extra<TEST>(p, blockIdx.x, 1);
 #pragma unroll
             for (int which = 0; which < 2; ++which) {
                 const uint32_t full = bar((which ? kBarVcFull : kBarKcFull) + st);
                 if (lap) ok = together(wait(bar((which ? kBarVcFree : kBarKcFree) + st), (lap - 1) & 1));
-                if (!ok) break;
+                if (!ok) {
+                    if (lane == 0) s_half = which;
+                    break;
+                }
                 if (lane == 0) mbar_arrive_expect_tx(full, bytes);
                 __syncwarp();
                 if (here) {
@@ -727,14 +749,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
             __syncwarp();
             if (lane == 0) at_arrive(bar(kBarNote + i % kAtNotes));
         }
-        // copies in flight end before the shared memory does (they are waited for by the warps that read them, unless
-        // those gave up)
-        if (!ok || s_dead) {
-            for (uint32_t k = i > (uint32_t)M::stages ? i - M::stages : 0; k < i; ++k) {
-                mbar_wait_bounded(bar(kBarKcFull + k % M::stages), (k / M::stages) & 1);
-                mbar_wait_bounded(bar(kBarVcFull + k % M::stages), (k / M::stages) & 1);
-            }
-        }
+        if (lane == 0) s_copied = i;
         } else if (warp - 12 < SUB) {
         // ---- the products: a warp per block of rows; with two blocks they take turns, a tile's P V and the next tile's
         // Q K^T at a time, so that one block's softmax runs under the other's products ----
@@ -812,18 +827,21 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (threadIdx.x == 0 && s_dead) atomicOr(p.status, kDevWaitTimeout);
+    if (s_dead)
+        at_lost<M::stages>(p.status, att_work(p.workspace, gridDim.x, R).ml + (int64_t)2 * blockIdx.x * R, p.whole ? 0 : 2 * R, bar(kBarRows + warp),
+                           warp < M::sm_warps ? s_rows[warp] : 0, bar(kBarKcFull), bar(kBarVcFull), warp == 14 ? s_copied : 0, warp == 14 ? s_half : 0,
+                           kAttWait<TEST>);
     if (warp == 12)
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kAtCols) : "memory");
 }
 
-template <int D, int SUB>
+template <int D, int SUB, bool TEST>
 cudaError_t launch_tc(const AttendArgs &a, int grid, cudaStream_t s) {
     using M = AtSmem<D, SUB>;
     const int smem = M::bytes;
-    const cudaError_t e = ensure_smem_limit(reinterpret_cast<const void *>(attend_tc_kernel<D, SUB>), smem);
+    const cudaError_t e = ensure_smem_limit(reinterpret_cast<const void *>(attend_tc_kernel<D, SUB, TEST>), smem);
     if (e != cudaSuccess) return e;
-    attend_tc_kernel<D, SUB><<<grid, kAtThreads, smem, s>>>(a);
+    attend_tc_kernel<D, SUB, TEST><<<grid, kAtThreads, smem, s>>>(a);
     return cudaGetLastError();
 }
 
@@ -854,9 +872,10 @@ cudaError_t launch_attend_tc(AttendArgs a, int grid, cudaStream_t s) {
     const cudaError_t e = symbol_address_cached(&g_status_attend_tc, cache, &a.status);
     if (e != cudaSuccess) return e;
     const bool two = attend_tc_rows(a) == 256;
-    if (a.d == 64) return two ? launch_tc<64, 2>(a, grid, s) : launch_tc<64, 1>(a, grid, s);
-    if (a.d == 128) return two ? launch_tc<128, 2>(a, grid, s) : launch_tc<128, 1>(a, grid, s);
-    return launch_tc<256, 1>(a, grid, s);
+    if (a.test) return a.d != 128 ? cudaErrorNotSupported : two ? launch_tc<128, 2, true>(a, grid, s) : launch_tc<128, 1, true>(a, grid, s);
+    if (a.d == 64) return two ? launch_tc<64, 2, false>(a, grid, s) : launch_tc<64, 1, false>(a, grid, s);
+    if (a.d == 128) return two ? launch_tc<128, 2, false>(a, grid, s) : launch_tc<128, 1, false>(a, grid, s);
+    return launch_tc<256, 1, false>(a, grid, s);
 }
 
 cudaError_t take_status_attend_tc(uint32_t *bits) {

@@ -855,10 +855,11 @@ int64_t damp_cache_attend_workspace(const damp_cache_layout *layout, int32_t bat
     return attend_workspace(a);
 }
 
-damp_status damp_cache_attend(const damp_cache_layout *layout, const void *cache, int64_t num_pages,
-                              const int32_t *pages, int32_t table, int32_t batch, int32_t T, const int32_t *lengths,
-                              const int32_t *q_lengths, const void *q, int64_t q_stride, float scale, int32_t window,
-                              void *o, int32_t dtype, void *workspace, int64_t workspace_bytes, void *stream) {
+static damp_status cache_attend(const damp_cache_layout *layout, const void *cache, int64_t num_pages,
+                                const int32_t *pages, int32_t table, int32_t batch, int32_t T, const int32_t *lengths,
+                                const int32_t *q_lengths, const void *q, int64_t q_stride, float scale, int32_t window,
+                                void *o, int32_t dtype, void *workspace, int64_t workspace_bytes, void *stream,
+                                int32_t test) {
     CacheArgs c{};
     Range pool, lists;
     int64_t es = 0;
@@ -902,7 +903,26 @@ damp_status damp_cache_attend(const damp_cache_layout *layout, const void *cache
     a.window = window >= (1 << 30) ? 0 : window;  // a table holds 2^30 tokens at most
     a.o = o;
     a.workspace = static_cast<uint8_t *>(workspace);
+    a.test = test;
     return launch_attend(a, static_cast<cudaStream_t>(stream)) == cudaSuccess ? DAMP_OK : DAMP_ERR_CUDA;
+}
+
+damp_status damp_cache_attend(const damp_cache_layout *layout, const void *cache, int64_t num_pages,
+                              const int32_t *pages, int32_t table, int32_t batch, int32_t T, const int32_t *lengths,
+                              const int32_t *q_lengths, const void *q, int64_t q_stride, float scale, int32_t window,
+                              void *o, int32_t dtype, void *workspace, int64_t workspace_bytes, void *stream) {
+    return cache_attend(layout, cache, num_pages, pages, table, batch, T, lengths, q_lengths, q, q_stride, scale, window, o,
+                        dtype, workspace, workspace_bytes, stream, 0);
+}
+
+damp_status damp_test_cache_attend_wait_timeout(const damp_cache_layout *layout, const void *cache, int64_t num_pages,
+                                                const int32_t *pages, int32_t table, int32_t batch, int32_t T,
+                                                const int32_t *lengths, const int32_t *q_lengths, const void *q,
+                                                int64_t q_stride, float scale, int32_t window, void *o, int32_t dtype,
+                                                void *workspace, int64_t workspace_bytes, int32_t queries, void *stream) {
+    if (check_cache(layout) == DAMP_OK && (layout->d != 128 || dtype != DAMP_IN_BF16)) return DAMP_ERR_SHAPE;
+    return cache_attend(layout, cache, num_pages, pages, table, batch, T, lengths, q_lengths, q, q_stride, scale, window, o,
+                        dtype, workspace, workspace_bytes, stream, queries ? 2 : 1);
 }
 
 damp_status damp_quantize_state(const damp_layout *layout, const float *S, const uint8_t *perm, void *state,

@@ -144,6 +144,7 @@ struct AttendArgs {
     int32_t in_bf16;
     uint8_t *workspace;
     uint32_t *status;  // set by the launchers
+    int32_t test;  // 0; 1, 2: the variant in which odd ranges wait in vain for 16 bytes of their pages, of their queries
 };
 
 // Launchers (return the CUDA error of the launch; they perform no host-side argument checks).
