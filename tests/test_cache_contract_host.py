@@ -19,11 +19,13 @@ def L():
 def test_wait_test_hook_accepts_only_its_instances(L):
     """The test of the bounded waits runs d = 128 and BF16 alone, with the checks of the call that it tests."""
     fb = FakeBuffers(n=8, size=1 << 22)
+    need = L.damp_cache_attend_workspace(ctypes.byref(_lib.DampCacheLayout(8, 2, 128)), 2, 1, 2, 0)
+    assert need <= 1 << 22
 
     def call(layout=(8, 2, 128), batch=2, T=1, dtype=0, queries=0, **over):
         a = dict(layout=ctypes.byref(_lib.DampCacheLayout(*layout)), cache=fb[0], num_pages=8, pages=fb[1], table=2, batch=batch, T=T,
                  lengths=fb[2], q_lengths=None, q=fb[3], q_stride=layout[0] * layout[2], scale=0.125, window=0, o=fb[4], dtype=dtype,
-                 ws=None, ws_bytes=0, queries=queries, stream=None)
+                 ws=fb[5], ws_bytes=need, queries=queries, stream=None)
         a.update(over)
         return L.damp_test_cache_attend_wait_timeout(*a.values())
 
