@@ -1005,6 +1005,15 @@ def cache_read(layout, cache, pages, lengths, tokens, start=None, dtype=None, k=
     return k, v
 
 
+def _attend_workspace(layout, key):
+    """Bytes of cache_attend's workspace for key (device, B, T, W, type), kept for the next call: 1024 of them at most."""
+    sizes = layout._shared[2]
+    if len(sizes) >= 1024:
+        sizes.clear()
+    need = sizes[key] = int(lib().damp_cache_attend_workspace(layout._shared[1], *key[1:]))
+    return need
+
+
 def cache_attend(layout, cache, q, pages, lengths, q_lengths=None, scale=None, window=None, o=None, stream=None):
     """Attention over the 8-bit cache: q [B, T, H, d] bfloat16 or float32; row b holds lengths[b] tokens
     (int32 [B]), the last q_lengths[b] (default T) of which are its queries' own: query t is token
@@ -1030,10 +1039,9 @@ def cache_attend(layout, cache, q, pages, lengths, q_lengths=None, scale=None, w
     else:
         op = _here("o", o, shape, dtype, dev)
     L = lib()
-    sizes = layout._shared[2]
-    need = sizes.get((dev, B, T, W, dt))
+    need = layout._shared[2].get((dev, B, T, W, dt))
     if need is None:
-        need = sizes[dev, B, T, W, dt] = L.damp_cache_attend_workspace(layout._shared[1], B, T, W, dt)
+        need = _attend_workspace(layout, (dev, B, T, W, dt))
     ws = None
     if need:
         ws = q.new_empty(need // (4 if dt else 2)) if stream is None else _new((need,), torch.uint8, q, stream)

@@ -33,3 +33,13 @@ def test_wait_test_hook_accepts_only_its_instances(L):
     assert call(layout=(8, 2, 64), batch=0) == SHAPE and call(layout=(8, 2, 256)) == SHAPE and call(dtype=1) == SHAPE
     assert call(dtype=2) == SHAPE and call(layout=(8, 3, 128)) == SHAPE and call(layout=(8, 2, 96)) == SHAPE
     assert call(q=None) == NULL and call(o=fb[3]) == ALIAS
+
+
+def test_workspace_sizes_are_kept_up_to_a_limit(L):
+    """A server's batches, prompt lengths and tables vary without end; equal layouts share what is kept."""
+    layout, twin = damp.CacheLayout(8, 2, 64), damp.CacheLayout(8, 2, 64)
+    for T in range(1, 5001):
+        key = (0, 3, T, 70 + T % 7, 0)
+        assert damp._attend_workspace(layout, key) == L.damp_cache_attend_workspace(layout._shared[1], *key[1:])
+        assert twin._shared[2][key] == layout._shared[2][key]
+        assert len(layout._shared[2]) <= 1024
