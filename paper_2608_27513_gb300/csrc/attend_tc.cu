@@ -32,11 +32,11 @@
 // behind by 2^5.9 (2^10 2^5.9 is below the largest FP16), so that O is rescaled, from tensor memory and back,
 // only where it moves by more.
 //
-// Measured (GPU alone).  That piece: 1.515 ms, 1.36 PFLOP/s, 72 % of a large BF16 matrix product.  A block's chain
+// Measured (GPU alone).  That piece: 1.512 ms, 1.36 PFLOP/s, 72 % of a large BF16 matrix product.  A block's chain
 // S, softmax, P V, Q K^T takes 3700 clocks a tile; the products of both blocks 2080 of them, the exponentials 1024
-// per block.  16 rows of up to 1000 queries in up to 1500 tokens, 32 heads, 16 KV heads, window 512: 251 us, where an
+// per block.  16 rows of up to 1000 queries in up to 1500 tokens, 32 heads, 16 KV heads, window 512: 246 us, where an
 // item is 6 tiles, 3 of them with borders, and 16 000 clocks of start and end.  61 rows of 5 queries in up to 2048
-// tokens, 16 heads, 2 KV heads, d = 256: 45 us; 40 of 128 rows are used, a tile of 64 tokens is a chain of 2500 clocks.
+// tokens, 16 heads, 2 KV heads, d = 256: 44 us; 40 of 128 rows are used, a tile of 64 tokens is a chain of 2500 clocks.
 #include "attend.cuh"
 #include "prefill_tc.cuh"
 
@@ -469,6 +469,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
                     }
                     at_st_wait();
                 }
+                const float over = (float)(note->top - e);  // the tile's unit over the row's
                 // Half of the columns at a time, in loops: registers hold 64 scores, and the code stays small (the
                 // instruction caches are shared by all roles).
                 float top = -INFINITY;
@@ -522,15 +523,15 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
                 }
                 ve = e;
                 const float base = ref == -INFINITY ? 0.f : -ref;
-                const float over = (float)(note->top - e);  // the tile's unit over the row's
 #pragma unroll 1
                 for (int h = 0; h < 2; ++h) {
                     uint32_t s[PG][16];
-                    float f[PG / 2], weight[PG / 2];  // while the scores are on their way
+                    float f[PG / 2], weight[PG / 2], a[PG / 2];  // while the scores are on their way
 #pragma unroll
                     for (int c = 0; c < PG / 2; ++c) {
                         f[c] = fmaxf(factor * note->factor[h * (PG / 2) + c], FLT_MIN);
                         weight[c] = fmaxf(over + note->weight[h * (PG / 2) + c], kAtLowest);  // (exact)
+                        a[c] = base + weight[c];
                     }
 #pragma unroll
                     for (int c = 0; c < PG; ++c) at_ld16(s_at + (16 * PG) * h + 16 * c, s[c]);
@@ -539,7 +540,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
 #pragma unroll
                     for (int c = 0; c < PG / 2; ++c) {
                         const int page = h * (PG / 2) + c;
-                        const float2 f2 = splat2(f[c]), a2 = splat2(base + weight[c]);
+                        const float2 f2 = splat2(f[c]), a2 = splat2(a[c]);
                         float2 z[16];
 #pragma unroll
                         for (int j = 0; j < 16; ++j)
@@ -856,8 +857,8 @@ int attend_tc_rows(const AttendArgs &a) { return a.d <= 128 && (int64_t)a.T * (a
 // table's width and the window bound an item.  Whole items against parts, even lengths and ragged ones, us: 16 rows of
 // 1000 queries, 32 heads, 16 KV, window 512 273 / 328 and 278 / 338; 10 of 256 in 1000 tokens 65 / 66 and 71 / 73;
 // 320 of 5 in 1000, 32 heads, 8 KV 265 / 252 and 269 / 250, in 4000 822 / 562 and 840 / 543; but 256 rows of 5, one in
-// 131072 tokens and the others in 1000: 1376 and 322.  256 rows of 5 in 1000 tokens each under a table of 4096 pages, which
-// could hold such a row, pay for it: 218 and 228.
+// 131072 tokens and the others in 1000: 1376 and 317.  256 rows of 5 in 1000 tokens each under a table of 4096 pages, which
+// could hold such a row, pay for it: 217 and 225.
 bool attend_tc_whole(const AttendArgs &a) {
     const int64_t G = a.H / a.Hk, R = attend_tc_rows(a), items = (int64_t)a.batch * (((int64_t)a.T * G + R - 1) / R) * a.Hk;
     const int64_t keys = a.window ? (int64_t)a.window + R / G + 1 : 32 * (int64_t)a.table;  // of an item

@@ -6,7 +6,7 @@
 // scale grows from s to s', its earlier codes become rne(c (s r')): off by another half step of s'.
 // Every operation is one FP32 rounding, so that the codes are defined to the bit.  Scales below
 // 2^-126 are 0 (the block then holds zeros).  A NaN is stored as 0; an infinity takes no part in
-// the maximum and is held to the block's largest value; both set a status bit.
+// the maximum and is held to 127 s; both set a status bit.
 //
 // An item is one (row, page, head, keys or values): 128 threads, or a warp where a page receives 8
 // tokens at most.  A thread keeps the values of its chunks of 16 in registers between the maximum
