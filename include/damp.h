@@ -495,7 +495,7 @@ typedef struct {
  *   lengths     int32 [batch]: tokens held, those of the queries among them (their keys and values
  *               are appended before); clamped to 0 .. 32 table
  *   q_lengths   int32 [batch] or NULL (T): queries of each row, clamped to 0 .. T
- *   scale       positive;  window  0, or the number of tokens that a query sees, its own the last
+ *   scale       positive, with logits (scale q.k) up to 2^60 in magnitude;  window  0, or the number of tokens that a query sees, its own the last
  *   o           [batch][T][num_heads][d] of dtype, 16-B aligned: query t of row b is token
  *               j = lengths[b] - q_lengths[b] + t and sees tokens max(0, j - window + 1) .. j.
  *               A query that sees none gives zeros, and so do those past q_lengths[b].
@@ -504,7 +504,7 @@ typedef struct {
  *   Maxima, sums and outputs are FP32.  Weights enter the product with the values times the page's
  *   value scale over a power of two above the scales of all pages of which the query sees a token, in
  *   FP16 (FP32 inputs: two FP16 parts each): a key's part of an output is within 2^-11 of itself (FP32:
- *   2^-21), and 2^-34 of the largest value that those pages can hold.  What a query does not see, values
+ *   2^-21), and 2^-34 of the largest value that those pages can hold.  What a query does not see, the rest
  *   of its own pages apart, changes no bit of its output.  A NaN or infinity in a query reaches its own
  *   head's output alone.  How rows are split over the GPU depends on the lengths of the batch, and with it the
  *   last bits.  ceil(T num_heads / num_kv_heads / 16) batch num_kv_heads table is 2^30 at most.

@@ -32,9 +32,9 @@
 // behind by 2^5.9 (2^10 2^5.9 is below the largest FP16), so that O is rescaled, from tensor memory and back,
 // only where it moves by more.
 //
-// Measured (GPU alone).  That piece: 1.512 ms, 1.36 PFLOP/s, 72 % of a large BF16 matrix product.  A block's chain
+// Measured (GPU alone).  That piece: 1.523 ms, 1.35 PFLOP/s, 71 % of a large BF16 matrix product.  A block's chain
 // S, softmax, P V, Q K^T takes 3700 clocks a tile; the products of both blocks 2080 of them, the exponentials 1024
-// per block.  16 rows of up to 1000 queries in up to 1500 tokens, 32 heads, 16 KV heads, window 512: 246 us, where an
+// per block.  16 rows of up to 1000 queries in up to 1500 tokens, 32 heads, 16 KV heads, window 512: 249 us, where an
 // item is 6 tiles, 3 of them with borders, and 16 000 clocks of start and end.  61 rows of 5 queries in up to 2048
 // tokens, 16 heads, 2 KV heads, d = 256: 44 us; 40 of 128 rows are used, a tile of 64 tokens is a chain of 2500 clocks.
 #include "attend.cuh"
@@ -52,6 +52,12 @@ constexpr int kAtThreads = 15 * 32;
 constexpr uint32_t kAtCols = 512;
 constexpr uint32_t kAtO = 256;  // S blocks at columns 0 and 128, O from here on
 constexpr float kAtLag = 5.9f;  // 2^10 2^5.9 is below the largest FP16; half of the rescalings that 4 makes
+// A score S (below 2^30) times its factor f is taken off the reference in one fused operation, and so is off by half a unit of
+// the product: nothing below 2^20, but beyond FP16's range from 2^21 on.  Scores of rows with factors from kAtFar on become
+// S f / kAtLeast, rounded, where they are; their factor then is kAtLeast, as it is of key scales of 0 (2^-20 at most).
+constexpr float kAtFar = 9.765625e-4f;                 // 2^-10
+constexpr float kAtLeast = 8.8817841970012523e-16f;    // 2^-50
+constexpr float kAtMost = 1.5845632502852868e29f;      // 2^97: of f / kAtLeast, which leaves S finite
 constexpr int kAtNotes = 8;
 constexpr int kAtMaxPages = 4;  // of a key tile
 constexpr int kAtNoScale = -1000;  // below every exponent field
@@ -63,7 +69,8 @@ struct AtNote {  // of a key tile: what the softmax needs of its pages
     int e[kAtMaxPages];         // exponent field of the power of two above the value scale; kAtNoScale for 0
     int top;                    // the largest e: the tile's unit
     int hidden;                 // bit i: page i is bad or missing
-    int unused[2];
+    float reach;                // the largest key scale
+    int unused;
 };
 
 template <int D, int SUB>
@@ -440,19 +447,39 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
                 const AtNote *const note = reinterpret_cast<const AtNote *>(sm + M::note) + tile % kAtNotes;
                 const int i = at - it.begin;
                 const int token = (it.first + i * PG) * kCachePage;  // of column 0
-                const int hidden = note->hidden;
-                int e = max(ve, note->top);
+                const int4 about = *reinterpret_cast<const int4 *>(&note->top);  // top, hidden, reach
+                const int hidden = about.y;
+                int e = max(ve, about.x);
+                bool far = factor * __int_as_float(about.z) >= kAtFar;
                 ok = together(ok && wait(bar(kBarS + sbuf), (SUB == 2 ? tile : tile >> 1) & 1));
                 if (!ok) break;
                 tc_fence_after();
-                if (__any_sync(kFull, hidden != 0 || limit < token + TN - 1 || from > token)) {
-                    // A page that a row does not see leaves its unit as it is.  Columns that a row does not see become -inf
-                    // where they are, 16 at a time (of the border tiles of an item only: a small loop, for the instruction
-                    // caches' sake, which all roles share).
+                if (__any_sync(kFull, hidden != 0 || limit < token + TN - 1 || from > token || far)) {
+                    // A page that a row does not see leaves its unit and its products as they are.
+                    auto sees = [&](int c) { return limit >= token + kCachePage * c && from < token + kCachePage * (c + 1); };
                     e = ve;
 #pragma unroll
                     for (int c = 0; c < PG; ++c)
-                        if (limit >= token + kCachePage * c && from < token + kCachePage * (c + 1)) e = max(e, note->e[c]);
+                        if (sees(c)) e = max(e, note->e[c]);
+                    if (__any_sync(kFull, far)) {
+                        far = false;
+#pragma unroll 1
+                        for (int c = 0; c < PG; ++c) far = far || (sees(c) && factor * note->factor[c] >= kAtFar);
+                        const float up = far ? factor * (1.f / kAtLeast) : 0.f;
+#pragma unroll 1
+                        for (int c = 0; c < 2 * PG; ++c) {
+                            const float f = far ? fminf(up * note->factor[c >> 1], kAtMost) : 1.f;
+                            uint32_t y[16];
+                            at_ld16(s_at + 16 * c, y);
+                            at_ld_wait(y);
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) y[j] = __float_as_uint(__uint_as_float(y[j]) * f);
+                            at_st16(s_at + 16 * c, y);
+                        }
+                        at_st_wait();
+                    }
+                    // Columns that a row does not see become -inf where they are, 16 at a time (of the border tiles of an item
+                    // only: a small loop, for the instruction caches' sake, which all roles share).
 #pragma unroll 1
                     for (int c = 0; c < 2 * PG; ++c) {
                         const int lo = from - (token + 16 * c), hi = limit - (token + 16 * c);  // sees lo .. hi
@@ -469,7 +496,8 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
                     }
                     at_st_wait();
                 }
-                const float over = (float)(note->top - e);  // the tile's unit over the row's
+                const float over = (float)(about.x - e);  // the tile's unit over the row's
+                const float near = far ? 0.f : factor;
                 // Half of the columns at a time, in loops: registers hold 64 scores, and the code stays small (the
                 // instruction caches are shared by all roles).
                 float top = -INFINITY;
@@ -478,7 +506,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
                     uint32_t s[PG][16];
                     float f[PG / 2];  // while the scores are on their way
 #pragma unroll
-                    for (int c = 0; c < PG / 2; ++c) f[c] = fmaxf(factor * note->factor[h * (PG / 2) + c], FLT_MIN);  // not 0: times a hidden -inf
+                    for (int c = 0; c < PG / 2; ++c) f[c] = fmaxf(near * note->factor[h * (PG / 2) + c], kAtLeast);  // not 0: times a hidden -inf
 #pragma unroll
                     for (int c = 0; c < PG; ++c) at_ld16(s_at + (16 * PG) * h + 16 * c, s[c]);
 #pragma unroll
@@ -529,9 +557,9 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
                     float f[PG / 2], weight[PG / 2], a[PG / 2];  // while the scores are on their way
 #pragma unroll
                     for (int c = 0; c < PG / 2; ++c) {
-                        f[c] = fmaxf(factor * note->factor[h * (PG / 2) + c], FLT_MIN);
+                        f[c] = fmaxf(near * note->factor[h * (PG / 2) + c], kAtLeast);
                         weight[c] = fmaxf(over + note->weight[h * (PG / 2) + c], kAtLowest);  // (exact)
-                        a[c] = base + weight[c];
+                        a[c] = __fadd_rd(base, weight[c]);  // (to the nearest, 10 could become 16)
                     }
 #pragma unroll
                     for (int c = 0; c < PG; ++c) at_ld16(s_at + (16 * PG) * h + 16 * c, s[c]);
@@ -733,10 +761,11 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
             }
             if (!ok) break;
             AtNote *const note = reinterpret_cast<AtNote *>(sm + M::note) + i % kAtNotes;
-            // A scale of 0 stands for zeros whatever the codes are: scores of 0 (times 0, FLT_MIN in the softmax, so that hidden
+            // A scale of 0 stands for zeros whatever the codes are: scores of 0 (times kAtLeast in the softmax, so that hidden
             // columns stay -inf), weights that are 0 in FP16 (at kAtLowest) but count in the sum.
             const int ve = scales.y > 0.f ? (int)min((__float_as_uint(scales.y) >> 23) + 1u, 253u) : kAtNoScale;
             const int top = __reduce_max_sync(kFull, ve);
+            const uint32_t reach = __reduce_max_sync(kFull, __float_as_uint(fmaxf(scales.x, 0.f)));  // not negative: ordered as integers
             if (lane < PG) {
                 const float m = scales.y > 0.f ? __log2f(scales.y * __uint_as_float((uint32_t)(254 - ve) << 23)) : 0.f;
                 note->factor[lane] = scales.x;
@@ -745,6 +774,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attend_tc_kernel(const AttendAr
             }
             if (lane == 0) {
                 note->top = top;
+                note->reach = __uint_as_float(reach);
                 note->hidden = (int)(~shown & ((1u << PG) - 1u));
             }
             __syncwarp();
@@ -857,8 +887,8 @@ int attend_tc_rows(const AttendArgs &a) { return a.d <= 128 && (int64_t)a.T * (a
 // table's width and the window bound an item.  Whole items against parts, even lengths and ragged ones, us: 16 rows of
 // 1000 queries, 32 heads, 16 KV, window 512 273 / 328 and 278 / 338; 10 of 256 in 1000 tokens 65 / 66 and 71 / 73;
 // 320 of 5 in 1000, 32 heads, 8 KV 265 / 252 and 269 / 250, in 4000 822 / 562 and 840 / 543; but 256 rows of 5, one in
-// 131072 tokens and the others in 1000: 1376 and 317.  256 rows of 5 in 1000 tokens each under a table of 4096 pages, which
-// could hold such a row, pay for it: 217 and 225.
+// 131072 tokens and the others in 1000: 1376 and 329.  256 rows of 5 in 1000 tokens each under a table of 4096 pages, which
+// could hold such a row, pay for it: 222 and 244.
 bool attend_tc_whole(const AttendArgs &a) {
     const int64_t G = a.H / a.Hk, R = attend_tc_rows(a), items = (int64_t)a.batch * (((int64_t)a.T * G + R - 1) / R) * a.Hk;
     const int64_t keys = a.window ? (int64_t)a.window + R / G + 1 : 32 * (int64_t)a.table;  // of an item

@@ -1,5 +1,7 @@
 """Attention over records of the 8-bit cache that cache_append did not write, or only in part: what a code stands for
 is (c - 128) times its scale whatever the kernel, a scale of 0 included."""
+import math
+
 import pytest
 import torch
 
@@ -133,3 +135,60 @@ def test_extreme_scales(dtype, T, scale, qsize, ksize):
     damp.cache_append(layout, pool, k, v, pages, i32([0]))
     q = qsize * randn(g, 1, T, 4, 64)
     run_attend(layout, pool, pages, q.to(dtype), [96], "extreme scales", scale=torch.tensor(scale, dtype=F32).item())
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("H,Hk,d", [(8, 2, 64), (8, 2, 128), (16, 2, 256)])
+@pytest.mark.parametrize("T", [1, 6, 30, 90])
+def test_large_logits_pick_one_token(dtype, H, Hk, d, T):
+    """Logits far apart, up to sizes of which FP32 holds no unit any more: the largest takes all.
+
+    A logit is within (d + 8) 2^-23 of sum |q k| (and FP32 queries' two parts, 2^-21); where the largest leads by
+    more than twice that and by 40, the other weights are below e^-40 of its own, and the output is its value: a weight in
+    FP16 (2^-11; two parts 2^-20), rounded to BF16 (2^-8) or FP32 (2^-24), its exponential and the inverse (2^-20).
+    The others add e^-40 of the largest value each, to values of 0 as well."""
+    layout = damp.CacheLayout(H, Hk, d)
+    pool, pages = filled(layout, 2, 9, d + T)
+    held = [288, 250]
+    ref = R.Cache(pool, d)
+    eps = (2.0 ** -11 + 2.0 ** -8 if dtype == BF else 2.0 ** -20 + 2.0 ** -24) + 2.0 ** -20
+    few = dtype == F32 or T * (H // Hk) <= 16  # 16 rows at a time: up to FP32's range; else up to 2^60
+    for size in (300.0, 1e4, 1e6, 1e9, 1e13, 1e16) + ((1e20, 1e30, 1e36) if few else ()):
+        q = (size * randn(gen(T), 2, T, H, d)).to(dtype)
+        o = damp.cache_attend(layout, pool, q, pages, i32(held)).double().cpu()
+        assert torch.isfinite(o).all(), size
+        sure = 0
+        for b in range(2):
+            k, v = (ref.values(w, pages[b].cpu())[:held[b]] for w in (0, 1))
+            unseen = torch.arange(held[b]) > torch.arange(held[b] - T, held[b])[:, None]
+            for h in range(H):
+                x = q[b, :, h].double().cpu()
+                z = (x @ k[:, h // (H // Hk)].T * d ** -0.5).masked_fill(unseen, float("-inf"))
+                reach = (x.abs() @ k[:, h // (H // Hk)].abs().T * d ** -0.5).amax(-1)
+                two, at = z.topk(2, -1)
+                clear = two[:, 0] - two[:, 1] > 40 + 2 * reach * ((d + 8) * 2.0 ** -23 + 2.0 ** -21)
+                sure += int(clear.sum())
+                want = v[at[:, 0], h // (H // Hk)]
+                rest = held[b] * math.exp(-40) * v.abs().max()
+                assert ((o[b, :, h] - want).abs()[clear] <= eps * want.abs()[clear] + rest).all(), size
+        assert sure > T * H  # of 2 T H; more than half
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("T,window", [(6, None), (30, None), (90, None), (90, 40), (30, 70)])
+def test_unseen_keys_change_nothing(dtype, d, T, window):
+    """As test_unseen_values_change_nothing with keys larger by 1e12: bits of the queries that do not see them."""
+    layout = damp.CacheLayout(8, 2, d)
+    pool, pages = filled(layout, 2, 10, d + T)
+    large, at, held = pool.clone(), [8, 6], [255 + max(T, 4) // 2, 286]
+    for b in range(2):
+        scales_of(large, d)[pages[b, at[b]].long(), :, 0] *= 1e12
+    q = (1.5 * randn(gen(T), 2, T, 8, d)).to(dtype)
+    last = torch.tensor(held)[:, None] - T + torch.arange(T)
+    first = (last - (window - 1)).clamp(min=0) if window else torch.zeros_like(last)
+    page = torch.tensor(at)[:, None]
+    seen = (first < 32 * (page + 1)) & (last >= 32 * page)
+    a, b = (damp.cache_attend(layout, x, q, pages, i32(held), window=window) for x in (large, pool))
+    assert not seen.all() and torch.equal(a[~seen], b[~seen]) and b[~seen].any(-1).all()
+    assert torch.isfinite(a).all()
