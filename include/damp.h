@@ -461,8 +461,8 @@ typedef struct {
  * The cache: a pool of num_pages pages of 32 tokens.  Page p, KV head h is a record of
  * 64 d + 16 bytes at (p num_kv_heads + h) (64 d + 16): 32 key rows of d codes, 32 value rows,
  * the FP32 scales of the keys and of the values, 8 unused bytes.  Code c (uint8) stands for
- * (c - 128) s, zero where s is 0.  Chunk m of 16 codes of the row of token t lies at chunk m ^ (h(t) mod d/16),
- * h(t) = (t & 7) ^ ((t & 1) << 2).  Pages are slots of damp_copy_slots (a shared page is copied
+ * (c - 128) s, zero where s is 0.  Chunk m of 16 codes of the row of token t lies at chunk
+ * m ^ (h(t) mod d/16), h(t) = (t & 7) ^ ((t & 1) << 2).  Pages are slots of damp_copy_slots (a shared page is copied
  * before it is written) and damp_zero_slots.
  *   cache       the pool, 16-B aligned
  *   pages       int32 [batch][table]: token j of row b lies in page pages[b][j / 32]; entries of
@@ -495,7 +495,8 @@ typedef struct {
  *   lengths     int32 [batch]: tokens held, those of the queries among them (their keys and values
  *               are appended before); clamped to 0 .. 32 table
  *   q_lengths   int32 [batch] or NULL (T): queries of each row, clamped to 0 .. T
- *   scale       positive, with logits (scale q.k) up to 2^60 in magnitude;  window  0, or the number of tokens that a query sees, its own the last
+ *   scale       positive, with logits (scale q.k) up to 2^60 in magnitude;  window  0, or the number
+ *               of tokens that a query sees, its own the last
  *   o           [batch][T][num_heads][d] of dtype, 16-B aligned: query t of row b is token
  *               j = lengths[b] - q_lengths[b] + t and sees tokens max(0, j - window + 1) .. j.
  *               A query that sees none gives zeros, and so do those past q_lengths[b].
